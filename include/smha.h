@@ -322,6 +322,47 @@ smha_status_t smha_plan_row_form(const smha_plan_t *plan, int B, int H, int d, i
 
 void smha_plan_destroy(smha_plan_t *plan); /* NULL is allowed */
 
+/* ---- Attention within a causal window and a few first keys that stay visible (sinks) ----
+ *
+ * No plan: which keys a query sees is arithmetic on positions.  H query heads share Hkv key heads, H / Hkv in a
+ * row each.  Query i of sequence b stands at position p = offsets[b] + i and exists where 0 <= p < lengths[b]; it
+ * sees key j iff j <= p and (p - j < window or j < n_sink).
+ *   Q, O            device, [B][H][Sq][d]; K, V: [B][Hkv][Sk][d]; all of `dtype` (F16 or BF16); d a multiple of 8
+ *                   up to 128.  *_strides, alignment and the 2 GiB limit as in smha_forward, but batch and head
+ *                   strides of tensors that are only read may be zero
+ *   lse             device, float [B][H][Sq], packed: log of the sum of the exponentials of the scaled scores, -inf
+ *                   where a query sees nothing or does not exist; NULL in smha_sink_forward if it is not wanted
+ *   offsets         device, int32 [B]; NULL: Sk - Sq for every sequence (the queries are its last ones)
+ *   lengths         device, int32 [B], keys per sequence, taken as 0 or Sk where outside 0 .. Sk; NULL: Sk
+ *   window          keys that a query sees, itself included; 0: all before it
+ *   n_sink          first keys that every later query sees
+ * offsets and lengths are read by the kernels: nothing synchronises, and a captured call follows their values.
+ * Queries that do not exist give zero rows in O and dQ, keys at and past a sequence's length zero rows in dK
+ * and dV; neither's values are read into any result, whatever they are.  Values that are visible to some query have to
+ * be finite (a NaN or infinity there may reach other queries of the same 128).
+ * Errors: INVALID_ARG (null, sizes, a negative window or n_sink, too small a workspace), SHAPE (H no multiple of Hkv),
+ * UNSUPPORTED (d, dtype, alignment, strides, sizes), HIP.  Enqueues on hip_stream, on the current device. */
+smha_status_t smha_sink_forward(const void *Q, const void *K, const void *V, void *O, float *lse, int B, int H, int Hkv,
+                                int Sq, int Sk, int d, smha_dtype_t dtype, const int64_t q_strides[3],
+                                const int64_t k_strides[3], const int64_t v_strides[3], const int64_t o_strides[3],
+                                const int32_t *offsets, const int32_t *lengths, int window, int n_sink, float scale,
+                                void *hip_stream);
+
+/* Bytes of device memory that smha_sink_backward needs for such a call. */
+smha_status_t smha_sink_workspace(int B, int H, int Hkv, int Sq, int Sk, int d, int window, int n_sink, size_t *need);
+
+/* Gradients of Q, K and V (of `dtype`, written whole) from O and lse of the forward with the same arguments and dO, the
+ * gradient of O.  The result does not depend on the order in which workgroups run: the parts of sums that were cut
+ * are added in a fixed order.  workspace: device, 16-byte aligned, smha_sink_workspace bytes or more; the call's alone
+ * until it has run. */
+smha_status_t smha_sink_backward(const void *Q, const void *K, const void *V, const void *O, const float *lse,
+                                 const void *dO, void *dQ, void *dK, void *dV, int B, int H, int Hkv, int Sq, int Sk, int d,
+                                 smha_dtype_t dtype, const int64_t q_strides[3], const int64_t k_strides[3],
+                                 const int64_t v_strides[3], const int64_t o_strides[3], const int64_t do_strides[3],
+                                 const int64_t dq_strides[3], const int64_t dk_strides[3], const int64_t dv_strides[3],
+                                 const int32_t *offsets, const int32_t *lengths, int window, int n_sink, float scale,
+                                 void *workspace, size_t workspace_bytes, void *hip_stream);
+
 const char *smha_status_string(smha_status_t status);
 
 /* Symbol names of kernels, for matching profiler output (name and duration bookkeeping is left to the caller).

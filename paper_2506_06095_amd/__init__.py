@@ -10,3 +10,12 @@ from .binding import (  # noqa: F401
     smha_call_kernel_name, smha_forward, smha_forward_static, smha_kernel_name, smha_plan_destroy, smha_plan_export, smha_plan_from_dense,
     smha_plan_from_dense_rect,
     smha_plan_from_desc, smha_plan_info, smha_plan_prepare, smha_plan_work_order, smha_status_string)
+
+_OPERATORS = {name: "sink" for name in ("sink_attention", "smha_sink_backward", "smha_sink_forward", "smha_sink_workspace")}
+
+
+def __getattr__(name):  # (these modules need torch when they are imported, which plans on the host do not)
+    if name in _OPERATORS:
+        import importlib
+        return getattr(importlib.import_module(f".{_OPERATORS[name]}", __name__), name)
+    raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

@@ -104,6 +104,11 @@ def _load():
     lib.smha_plan_work_order.restype = lib.smha_plan_call_order.restype = C.c_int
     lib.smha_plan_row_form.argtypes = [vp, C.c_int, C.c_int, C.c_int, C.POINTER(C.c_int), C.POINTER(C.c_int)]
     lib.smha_plan_row_form.restype = C.c_int
+    i64p, i = C.POINTER(C.c_int64), C.c_int
+    lib.smha_sink_forward.argtypes = [vp] * 5 + [i] * 7 + [i64p] * 4 + [vp, vp, i, i, C.c_float, vp]
+    lib.smha_sink_workspace.argtypes = [i] * 8 + [C.POINTER(C.c_size_t)]
+    lib.smha_sink_backward.argtypes = [vp] * 9 + [i] * 7 + [i64p] * 8 + [vp, vp, i, i, C.c_float, vp, C.c_size_t, vp]
+    lib.smha_sink_forward.restype = lib.smha_sink_workspace.restype = lib.smha_sink_backward.restype = i
     lib.smha_plan_destroy.argtypes = [vp]
     lib.smha_plan_destroy.restype = None
     lib.smha_status_string.argtypes = [C.c_int]

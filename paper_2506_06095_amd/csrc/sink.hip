@@ -1,0 +1,736 @@
+// Attention within a causal window and a few first keys that stay visible (sinks): forward and backward.
+//
+//   position of query i of sequence b: p = offset_b + i; it exists where 0 <= p < length_b
+//   key j is visible to it iff j <= p and (p - j < window or j < n_sink)
+//   s = scale q.k,  lse = log sum exp s,  P = exp(s - lse),  O = P V
+//   delta = sum_c dO_c O_c,  dP = dO V^T,  dS = P (dP - delta),  dQ = scale dS K,  dK = scale dS^T Q,  dV = P^T dO
+//
+// G = H / Hkv query heads share a key head (dK and dV are sums over them).  No mask and no plan: what a tile needs is arithmetic on
+// positions, and offsets and lengths are read on the device, so that a call neither synchronises nor depends on their values.
+//
+// All products run on v_mfma_f32_32x32x16 in the orientation in which the accumulators of the scores are the other products'
+// B operand as they stand (P and dS never go through LDS), and tiles sit in LDS row-major, chunks of 16 bytes swizzled so that both
+// ways of reading them are spread over the banks: rows 16 bytes at a time (A operand of the first products), and transposing reads
+// of 4 rows x 16 columns (A operand of the second ones).  See smha_block_fwd for the operand layouts.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+
+#include "device_common.hpp"
+#include "smha.h"
+
+namespace smha {
+
+struct SinkParams {
+    const uint16_t *Q, *K, *V, *dO;
+    const uint16_t *Oin;  // backward: the forward's output
+    uint16_t *O;
+    uint16_t *dQ, *dK, *dV;
+    float *lse;           // [B][H][Sq]
+    Strides qs, ks, vs, os, gs, dqs, dks, dvs;
+    int B, H, Hkv, G, Sq, Sk, d;
+    int window, n_sink;   // 1 .. Sk (a window of Sk keys limits nothing), 0 .. Sk
+    const int32_t *offsets, *lengths;
+    float c, scale;       // c = scale * log2(e)
+    int per_xcd;          // work items per XCD
+    // backward
+    float *stats;         // [2][B][H][Sqp]: lse * log2(e) (inf where there is no query), delta
+    int Sqp;
+    float *parts;         // partial dK, dV of key tiles that are cut along their queries
+    int n_tiles, n_sink_tiles, chunk, cut_sink, cut_rest;  // key tiles, those with sinks; steps of a part; parts at most
+};
+
+constexpr uint32_t kNoChunk = 0x80000000u;  // a column that the head does not have: past every buffer, with any row's offset added
+constexpr uint32_t kPast = 0x7FFFFF00u;     // a row that is not to be read
+
+// Both of a tile's reading orders: 16 rows at one chunk (16-byte reads), and 4 rows x 4 chunks (transposing reads).  The two low bits
+// of the row choose the aligned group of four chunks, the next two the place in it.
+template <int D> __device__ __forceinline__ int swz(int row) {
+    if constexpr (D == 128) return ((row & 3) << 2) | ((row >> 2) & 3);
+    else return ((row & 2) << 1) | ((row >> 2) & 3);
+}
+
+struct Sequence {
+    int len, off;  // keys, first query's position
+    int qa, qb;    // queries qa .. qb - 1 exist
+};
+__device__ __forceinline__ Sequence sequence(const SinkParams &p, int b) {
+    Sequence s;
+    s.len = p.lengths ? min(max(uniform_load(p.lengths + b), 0), p.Sk) : p.Sk;
+    s.off = p.offsets ? min(max(uniform_load(p.offsets + b), -p.Sq), p.Sk) : p.Sk - p.Sq;
+    s.qa = max(0, -s.off);
+    s.qb = min(p.Sq, s.len - s.off);
+    return s;
+}
+
+// bits 0 .. n - 1
+__device__ __forceinline__ uint64_t low_bits(int n) { return n <= 0 ? 0 : n >= 64 ? ~0ull : (1ull << n) - 1; }
+__device__ __forceinline__ uint32_t low_bits32(int n) { return n <= 0 ? 0 : n >= 32 ? ~0u : (1u << n) - 1; }
+// the keys k0 .. k0 + 63 that a query at position pos sees
+__device__ __forceinline__ uint64_t seen_keys(int pos, int k0, int window, int n_sink) {
+    return low_bits(pos - k0 + 1) & (~low_bits(pos - window + 1 - k0) | low_bits(n_sink - k0));
+}
+// whether queries at positions p0 .. p1 see any / all of keys k0 .. k1
+__device__ __forceinline__ bool any_seen(int p0, int p1, int k0, int k1, int window, int n_sink) {
+    return k0 <= p1 && (p0 - k1 < window || k0 < n_sink);
+}
+__device__ __forceinline__ bool all_seen(int p0, int p1, int k0, int k1, int window, int n_sink) {
+    return k1 <= p0 && (p1 - k0 < window || k1 < n_sink);
+}
+
+typedef uint32_t u32x16 __attribute__((ext_vector_type(16)));
+// all ones where accumulator r of the lane (8 (r / 4) + r % 4 of the lane's half) has its bit set
+__device__ __forceinline__ u32x16 keep_of(uint32_t bits) {
+    u32x16 keep;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) keep[r] = (uint32_t)__builtin_amdgcn_sbfe((int)bits, 8 * (r / 4) + (r % 4), 1);
+    return keep;
+}
+__device__ __forceinline__ f32x16 zeros16() { return f32x16{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}; }
+
+// A tile of 64 rows into LDS by a workgroup's four waves: wave w brings the 1 KiB blocks w, w + 4, ...
+template <int D> struct TileLoad {
+    static constexpr int CPR = D / 8, LPW = CPR / 4, RSTEP = 4 * 64 / CPR;  // chunks a row, loads a wave, rows between two of its loads
+    uint32_t go;  // the lane's offset in the wave's first block
+    int row;
+    __device__ __forceinline__ TileLoad(int w, int lane, int row_bytes, int d) {
+        row = (w * 64 + lane) / CPR;
+        const int c = (lane % CPR) ^ swz<D>(row);
+        go = c < (d >> 3) ? (uint32_t)(row * row_bytes + c * 16) : kNoChunk;
+    }
+    // rows r0 .. r0 + 63; those in [gap0, gap1) read as zeros, as do those past the buffer
+    __device__ __forceinline__ void operator()(u32x4 rsrc, uint32_t lds, int w, int r0, int row_bytes, int gap0, int gap1) const {
+#pragma unroll
+        for (int i = 0; i < LPW; ++i) {
+            const int r = r0 + row + i * RSTEP;
+            const uint32_t at = go + (uint32_t)((r0 + i * RSTEP) * row_bytes);
+            load_to_lds(rsrc, lds + (w + 4 * i) * 1024, (int)(r >= gap0 && r < gap1 ? kPast : at));
+        }
+    }
+};
+
+// The next tile is in LDS and this one may be overwritten, for every wave.  (The last line keeps reads of LDS where they are: for the
+// compiler the barrier touches no memory.)
+__device__ __forceinline__ void tiles_landed() {
+    __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// A wave's 32 x D accumulators (acc[dt][r] = row j, column 32 dt + 8 (r / 4) + 4 hh + r % 4) to rows row0 .. of a tensor with 16-bit values,
+// through 32 rows of LDS so that whole rows are written; rows from `rows` on are left out.
+template <int D, bool BF16>
+__device__ __forceinline__ void store_rows(const f32x16 (&acc)[D / 32], float factor, char *slab, int lane, uint16_t *base, int64_t pitch, int row0, int rows, int d) {
+    constexpr int CPR = D / 8;
+    const int j = lane & 31, hh = lane >> 5;
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const u32x2 v = {pack2<BF16>(acc[dt][4 * g] * factor, acc[dt][4 * g + 1] * factor), pack2<BF16>(acc[dt][4 * g + 2] * factor, acc[dt][4 * g + 3] * factor)};
+            *reinterpret_cast<u32x2 *>(slab + j * D * 2 + (((4 * dt + g) ^ swz<D>(j)) * 16) + hh * 8) = v;
+        }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < CPR / 2; ++i) {
+        const int row = (i * 64 + lane) / CPR, c = (lane % CPR) ^ swz<D>(row);
+        const u32x4 v = *reinterpret_cast<const u32x4 *>(slab + i * 1024 + lane * 16);
+        if (row0 + row < rows && c < (d >> 3)) *reinterpret_cast<u32x4 *>(base + (row0 + row) * pitch + c * 8) = v;
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+}
+
+// A wave's 32 rows as the B operand of products over the columns: lane (j, hh) holds columns 16 s + 8 hh .. of row j.  Rows outside [a, b) are zeros.
+template <int D>
+__device__ __forceinline__ void load_operand(u32x4 (&f)[D / 16], const uint16_t *base, int64_t pitch, int row0, int a, int b, int d, int lane) {
+    const __amdgpu_buffer_rsrc_t r = make_rsrc(base, b > 0 ? ((int64_t)(b - 1) * pitch + d) * 2 : 0);
+    const int j = lane & 31, hh = lane >> 5, row = row0 + j;
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s)
+        f[s] = buf_load16(r, row >= a && row < b && 16 * s + 8 * hh < d ? (int)(row * pitch * 2) + 32 * s + 16 * hh : (int)kPast);
+}
+
+// ---------------------------------------------------------------------------------------
+// Forward
+// ---------------------------------------------------------------------------------------
+// A workgroup is four waves of 32 queries; they share 64-key tiles of K and V, two of each in LDS (the next lands while one is used).
+// The tiles are those of the sinks and those of the window of any of the 128 queries; a wave passes over tiles that its own
+// queries do not see, and forms masks only on tiles that they see in part.
+// P is rounded to the inputs' type for the second product: half a step, 2^-9 (bfloat16) or 2^-12 (binary16) of each weight, independent
+// from weight to weight, which leaves the output as far off as its own rounding does.  Sums and statistics are 32 bits.
+template <int D, bool BF16>
+__global__ void __launch_bounds__(256, D == 64 ? 4 : 2) smha_sink_fwd(const SinkParams p) {
+    constexpr int NS = D / 16, NDT = D / 32, TB = 64 * D * 2;
+    constexpr int PF = D == 128 ? 8 : 4;
+    __shared__ __attribute__((aligned(1024))) char smem[4 * TB];  // K[0], K[1], V[0], V[1]
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_void *)smem;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = lane & 31, hh = lane >> 5;
+    const float NEG_INF = -__builtin_inff();
+
+    // an XCD takes a run of heads, so that the heads that share keys do it in one L2; a head's last queries (the longest lists) first
+    const int nt = (p.Sq + 127) / 128, idx = (int)(blockIdx.x & 7) * p.per_xcd + (int)(blockIdx.x >> 3);
+    if (idx >= p.B * p.H * nt) return;
+    const int bh = idx / nt, q0 = (nt - 1 - (idx - bh * nt)) * 128, b = bh / p.H, h = bh - b * p.H, hk = h / p.G;
+    const Sequence s = sequence(p, b);
+    const int window = p.window, n_sink = p.n_sink;
+
+    // the workgroup's keys: sinks [0, .), then the window's tiles
+    const int first = s.off + max(q0, s.qa), last = s.off + min(q0 + 128, s.qb) - 1;  // positions
+    int n_head = 0, t0 = 0, n = 0, gap0 = 0, gap1 = 0;
+    if (first <= last) {
+        const int from = max(0, first - window + 1);
+        n_head = (min(n_sink, from) + 63) / 64;
+        t0 = max(from / 64, n_head);
+        n = n_head + last / 64 + 1 - t0;
+        if (n_sink < from) gap0 = n_sink, gap1 = from;  // keys that none of these queries sees
+    }
+    const int ksb = (int)p.ks.s * 2, vsb = (int)p.vs.s * 2;
+    const u32x4 rK = make_rsrc4(p.K + b * p.ks.b + hk * p.ks.h, n ? ((int64_t)last * p.ks.s + p.d) * 2 : 0);
+    const u32x4 rV = make_rsrc4(p.V + b * p.vs.b + hk * p.vs.h, n ? ((int64_t)last * p.vs.s + p.d) * 2 : 0);
+    const TileLoad<D> loadK(w, lane, ksb, p.d), loadV(w, lane, vsb, p.d);
+    auto key_of = [&](int t) __attribute__((always_inline)) { return 64 * (t < n_head ? t : t0 + t - n_head); };
+
+    const int qw = q0 + 32 * w, qpos = s.off + qw + j;
+    const bool exists = qw + j >= s.qa && qw + j < s.qb;
+    const int wp0 = s.off + max(qw, s.qa), wp1 = s.off + min(qw + 32, s.qb) - 1;  // the wave's positions
+    const bool whole = qw >= s.qa && qw + 32 <= s.qb;
+    if (n > 0) {
+        loadK(rK, lds0, w, key_of(0), ksb, gap0, gap1);
+        loadV(rV, lds0 + 2 * TB, w, key_of(0), vsb, gap0, gap1);
+    }
+    u32x4 qf[NS];
+    load_operand<D>(qf, p.Q + b * p.qs.b + h * p.qs.h, p.qs.s, qw, s.qa, s.qb, p.d, lane);
+
+    const int rd = j * D * 2 + ((hh ^ swz<D>(j)) * 16);
+    const int tr_row = 4 * hh + ((lane & 15) >> 2);
+    const int tr = tr_row * D * 2 + ((swz<D>(tr_row) ^ (2 * ((lane >> 4) & 1) + ((lane & 3) >> 1))) * 16) + (lane & 1) * 8;
+    float m_run = NEG_INF, l_run = 0.f;
+    const float thr = 8.0f / p.c;
+    f32x16 o[NDT];
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt) o[dt] = zeros16();
+    tiles_landed();
+
+    for (int t = 0; t < n; ++t) {
+        const int par = t & 1, key = key_of(t);
+        if (t + 1 < n) {
+            loadK(rK, lds0 + (par ^ 1) * TB, w, key_of(t + 1), ksb, gap0, gap1);
+            loadV(rV, lds0 + (2 + (par ^ 1)) * TB, w, key_of(t + 1), vsb, gap0, gap1);
+        }
+        if (wp0 <= wp1 && any_seen(wp0, wp1, key, key + 63, window, n_sink)) {
+            const char *const Kt = smem + par * TB, *const Vt = smem + (2 + par) * TB;
+            // acc[kt][r] = score of query j and key 32 kt + 8 (r / 4) + 4 hh + r % 4
+            f32x16 acc[2] = {zeros16(), zeros16()};
+            auto k_frag = [&](int i) __attribute__((always_inline)) { return *reinterpret_cast<const u32x4 *>(Kt + ((rd ^ (32 * (i >> 1))) + 64 * (i & 1) * D)); };
+            u32x4 kf[PF];
+#pragma unroll
+            for (int i = 0; i < PF; ++i) kf[i] = k_frag(i);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < 2 * NS; ++i) {
+                acc[i & 1] = mfma32<BF16>(kf[i % PF], qf[i >> 1], acc[i & 1]);
+                if (i + PF < 2 * NS) kf[i % PF] = k_frag(i + PF);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            __builtin_amdgcn_s_setprio(1);
+            if (!(whole && all_seen(wp0, wp1, key, key + 63, window, n_sink))) {
+                const uint64_t word = exists ? seen_keys(qpos, key, window, n_sink) : 0;
+#pragma unroll
+                for (int kt = 0; kt < 2; ++kt) {
+                    const u32x16 keep = keep_of((uint32_t)(word >> (32 * kt)) >> (4 * hh)), sc = __builtin_bit_cast(u32x16, acc[kt]);
+                    acc[kt] = __builtin_bit_cast(f32x16, (sc & keep) | (~keep & 0xFF800000u));
+                }
+            }
+            // probabilities are formed against a reference that is raised only where a score is over it by 8 / c: they stay below 2^8
+            float mc = (m_run == NEG_INF ? 0.f : m_run) * p.c, mt = NEG_INF;
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) mt = fmaxf(mt, acc[kt][r]);
+            if (__builtin_amdgcn_ballot_w64(mt > m_run + thr) != 0) {
+                mt = fmaxf(mt, __shfl_xor(mt, 32));
+                const float m_new = fmaxf(m_run, mt), m_use = m_new == NEG_INF ? 0.f : m_new;
+                const float alpha = fast_exp2((m_run - m_use) * p.c);
+                m_run = m_new;
+                mc = m_use * p.c;
+                l_run *= alpha;
+#pragma unroll
+                for (int dt = 0; dt < NDT; ++dt) o[dt] *= alpha;
+            }
+            u32x4 pf[4];
+            auto p_pair = [&](int cu, int q) __attribute__((always_inline)) {  // pair q of the 16 keys cu
+                const float e0 = fast_exp2(fmaf(acc[cu >> 1][8 * (cu & 1) + 2 * q], p.c, -mc));
+                const float e1 = fast_exp2(fmaf(acc[cu >> 1][8 * (cu & 1) + 2 * q + 1], p.c, -mc));
+                pf[cu][q] = pack2<BF16>(e0, e1);
+                l_run += e0 + e1;
+            };
+            auto v_frag = [&](int i) __attribute__((always_inline)) {  // i = cu NDT + dt: keys 16 cu + 8 a + 4 hh .., columns 32 dt + j
+                const char *const at = Vt + ((tr ^ (64 * (i % NDT))) + 32 * (i / NDT) * D), *const at8 = Vt + ((tr ^ (64 * (i % NDT)) ^ 32) + 32 * (i / NDT) * D + 16 * D);
+                const u32x2 lo = lds_read_tr(reinterpret_cast<const uint16_t *>(at)), hi = lds_read_tr(reinterpret_cast<const uint16_t *>(at8));
+                return u32x4{lo[0], lo[1], hi[0], hi[1]};
+            };
+            u32x4 vf[PF];
+#pragma unroll
+            for (int i = 0; i < PF; ++i) vf[i] = v_frag(i);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) p_pair(0, q);
+#pragma unroll
+            for (int i = 0; i < 4 * NDT; ++i) {
+                const int cu = i / NDT, dt = i % NDT;
+                o[dt] = mfma32<BF16>(vf[i % PF], pf[cu], o[dt]);
+                if (i + PF < 4 * NDT) vf[i % PF] = v_frag(i + PF);
+                if (cu < 3) {
+#pragma unroll
+                    for (int q = (4 * dt + NDT - 1) / NDT; q < (4 * dt + NDT + 3) / NDT; ++q) p_pair(cu + 1, q);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            __builtin_amdgcn_s_setprio(0);
+        }
+        tiles_landed();
+    }
+    const float l = l_run + __shfl_xor(l_run, 32);
+    if (p.lse && hh == 0 && qw + j < p.Sq)
+        p.lse[(int64_t)bh * p.Sq + qw + j] = l > 0.f ? (m_run * p.c + __builtin_amdgcn_logf(l)) * 0.6931471805599453f : NEG_INF;
+    store_rows<D, BF16>(o, l > 0.f ? 1.0f / l : 0.f, smem + w * (32 * D * 2), lane, p.O + b * p.os.b + h * p.os.h, p.os.s, qw, p.Sq, p.d);
+}
+
+// ---------------------------------------------------------------------------------------
+// Backward
+// ---------------------------------------------------------------------------------------
+// lse and delta of every query in the form that the two kernels below take them; queries that do not exist get lse = inf, so that
+// their probabilities are zero.  16 lanes a row.
+template <bool BF16>
+__global__ void __launch_bounds__(256) smha_sink_stats(const SinkParams p) {
+    const int64_t row = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4), rows = (int64_t)p.B * p.H * p.Sqp;
+    if (row >= rows) return;
+    const int bh = (int)(row / p.Sqp), q = (int)(row - (int64_t)bh * p.Sqp), b = bh / p.H, h = bh - b * p.H, c = threadIdx.x & 15;
+    const int len = p.lengths ? min(max(p.lengths[b], 0), p.Sk) : p.Sk;
+    const int off = p.offsets ? min(max(p.offsets[b], -p.Sq), p.Sk) : p.Sk - p.Sq;
+    const bool exists = q < p.Sq && off + q >= 0 && off + q < len;
+    float sum = 0.f;
+    if (exists && 8 * c < p.d) {
+        const u32x4 o = *reinterpret_cast<const u32x4 *>(p.Oin + b * p.os.b + h * p.os.h + q * p.os.s + 8 * c);
+        const u32x4 g = *reinterpret_cast<const u32x4 *>(p.dO + b * p.gs.b + h * p.gs.h + q * p.gs.s + 8 * c);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            sum = fmaf(widen16<BF16>(o[e] & 0xFFFFu), widen16<BF16>(g[e] & 0xFFFFu), sum);
+            sum = fmaf(widen16<BF16>(o[e] >> 16), widen16<BF16>(g[e] >> 16), sum);
+        }
+    }
+#pragma unroll
+    for (int m = 8; m > 0; m >>= 1) sum += __shfl_xor(sum, m);
+    if (c == 0) {
+        p.stats[row] = exists ? p.lse[(int64_t)bh * p.Sq + q] * 1.4426950408889634f : __builtin_inff();
+        p.stats[rows + row] = sum;
+    }
+}
+
+// dQ: four waves of 32 queries over the same key tiles as the forward; a lane owns a query, so lse and delta are its own two registers.
+// dS is rounded to the inputs' type for the product with K, as P is in the forward.
+template <int D, bool BF16>
+__global__ void __launch_bounds__(256, 2) smha_sink_bwd_q(const SinkParams p) {
+    constexpr int NS = D / 16, NDT = D / 32, TB = 64 * D * 2;
+    __shared__ __attribute__((aligned(1024))) char smem[4 * TB];  // K[0], K[1], V[0], V[1]
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_void *)smem;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = lane & 31, hh = lane >> 5;
+
+    const int nt = (p.Sq + 127) / 128, idx = (int)(blockIdx.x & 7) * p.per_xcd + (int)(blockIdx.x >> 3);
+    if (idx >= p.B * p.H * nt) return;
+    const int bh = idx / nt, q0 = (nt - 1 - (idx - bh * nt)) * 128, b = bh / p.H, h = bh - b * p.H, hk = h / p.G;
+    const Sequence s = sequence(p, b);
+    const int window = p.window, n_sink = p.n_sink;
+    const int first = s.off + max(q0, s.qa), last = s.off + min(q0 + 128, s.qb) - 1;
+    int n_head = 0, t0 = 0, n = 0, gap0 = 0, gap1 = 0;
+    if (first <= last) {
+        const int from = max(0, first - window + 1);
+        n_head = (min(n_sink, from) + 63) / 64;
+        t0 = max(from / 64, n_head);
+        n = n_head + last / 64 + 1 - t0;
+        if (n_sink < from) gap0 = n_sink, gap1 = from;
+    }
+    const int ksb = (int)p.ks.s * 2, vsb = (int)p.vs.s * 2;
+    const u32x4 rK = make_rsrc4(p.K + b * p.ks.b + hk * p.ks.h, n ? ((int64_t)last * p.ks.s + p.d) * 2 : 0);
+    const u32x4 rV = make_rsrc4(p.V + b * p.vs.b + hk * p.vs.h, n ? ((int64_t)last * p.vs.s + p.d) * 2 : 0);
+    const TileLoad<D> loadK(w, lane, ksb, p.d), loadV(w, lane, vsb, p.d);
+    auto key_of = [&](int t) __attribute__((always_inline)) { return 64 * (t < n_head ? t : t0 + t - n_head); };
+    const int qw = q0 + 32 * w, qpos = s.off + qw + j;
+    const bool exists = qw + j >= s.qa && qw + j < s.qb;
+    const int wp0 = s.off + max(qw, s.qa), wp1 = s.off + min(qw + 32, s.qb) - 1;
+    const bool whole = qw >= s.qa && qw + 32 <= s.qb;
+    if (n > 0) {
+        loadK(rK, lds0, w, key_of(0), ksb, gap0, gap1);
+        loadV(rV, lds0 + 2 * TB, w, key_of(0), vsb, gap0, gap1);
+    }
+    u32x4 qf[NS], gf[NS];
+    load_operand<D>(qf, p.Q + b * p.qs.b + h * p.qs.h, p.qs.s, qw, s.qa, s.qb, p.d, lane);
+    load_operand<D>(gf, p.dO + b * p.gs.b + h * p.gs.h, p.gs.s, qw, s.qa, s.qb, p.d, lane);
+    const int64_t row = (int64_t)bh * p.Sqp + qw + j;
+    const float lse2 = p.stats[row], delta = p.stats[(int64_t)p.B * p.H * p.Sqp + row];
+
+    const int rd = j * D * 2 + ((hh ^ swz<D>(j)) * 16);
+    const int tr_row = 4 * hh + ((lane & 15) >> 2);
+    const int tr = tr_row * D * 2 + ((swz<D>(tr_row) ^ (2 * ((lane >> 4) & 1) + ((lane & 3) >> 1))) * 16) + (lane & 1) * 8;
+    f32x16 dq[NDT];
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt) dq[dt] = zeros16();
+    tiles_landed();
+    for (int t = 0; t < n; ++t) {
+        const int par = t & 1, key = key_of(t);
+        if (t + 1 < n) {
+            loadK(rK, lds0 + (par ^ 1) * TB, w, key_of(t + 1), ksb, gap0, gap1);
+            loadV(rV, lds0 + (2 + (par ^ 1)) * TB, w, key_of(t + 1), vsb, gap0, gap1);
+        }
+        if (wp0 <= wp1) {
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt) {
+                const int k0 = key + 32 * kt;
+                if (!any_seen(wp0, wp1, k0, k0 + 31, window, n_sink)) continue;
+                const char *const Kt = smem + par * TB + kt * (TB / 2), *const Vt = smem + (2 + par) * TB + kt * (TB / 2);
+                f32x16 sc = zeros16(), dp = zeros16();
+#pragma unroll
+                for (int i = 0; i < NS; ++i) sc = mfma32<BF16>(*reinterpret_cast<const u32x4 *>(Kt + (rd ^ (32 * i))), qf[i], sc);
+#pragma unroll
+                for (int i = 0; i < NS; ++i) dp = mfma32<BF16>(*reinterpret_cast<const u32x4 *>(Vt + (rd ^ (32 * i))), gf[i], dp);
+                f32x16 ds;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) ds[r] = fast_exp2(fmaf(sc[r], p.c, -lse2)) * (dp[r] - delta);
+                if (!(whole && all_seen(wp0, wp1, k0, k0 + 31, window, n_sink))) {
+                    const u32x16 keep = keep_of((uint32_t)(exists ? seen_keys(qpos, k0, window, n_sink) : 0) >> (4 * hh));
+                    ds = __builtin_bit_cast(f32x16, __builtin_bit_cast(u32x16, ds) & keep);
+                }
+                u32x4 pf[2];
+#pragma unroll
+                for (int q = 0; q < 8; ++q) pf[q >> 2][q & 3] = pack2<BF16>(ds[2 * q], ds[2 * q + 1]);
+#pragma unroll
+                for (int i = 0; i < 2 * NDT; ++i) {
+                    const int cu = i / NDT, dt = i % NDT;
+                    const char *const at = Kt + ((tr ^ (64 * dt)) + 32 * cu * D), *const at8 = Kt + ((tr ^ (64 * dt) ^ 32) + 32 * cu * D + 16 * D);
+                    const u32x2 lo = lds_read_tr(reinterpret_cast<const uint16_t *>(at)), hi = lds_read_tr(reinterpret_cast<const uint16_t *>(at8));
+                    dq[dt] = mfma32<BF16>(u32x4{lo[0], lo[1], hi[0], hi[1]}, pf[cu], dq[dt]);
+                }
+            }
+        }
+        tiles_landed();
+    }
+    store_rows<D, BF16>(dq, p.scale, smem + w * (32 * D * 2), lane, p.dQ + b * p.dqs.b + h * p.dqs.h, p.dqs.s, qw, p.Sq, p.d);
+}
+
+// The queries that see a tile of 128 keys, as steps of 64 queries of one head: qt0 .. qt0 + nq - 1 of each of the G heads.
+struct KeyTile {
+    int qt0, nq;
+};
+__device__ __forceinline__ KeyTile key_tile(const SinkParams &p, const Sequence &s, int k0) {
+    // the earliest query at or after the first key, the last that has the last key in its window
+    const int k1 = min(k0 + 128, s.len) - 1;
+    const int qa = max(s.qa, k0 - s.off);
+    int qb = s.qb;
+    if (k0 >= p.n_sink) qb = min(qb, k1 + p.window - s.off);
+    if (k0 >= s.len || qa >= qb) return {0, 0};
+    return {qa / 64, (qb - 1) / 64 - qa / 64 + 1};
+}
+
+// dK and dV: four waves of 32 keys each, K and V in registers as B operands, over 64-query tiles of Q and dO (and their lse and
+// delta) in LDS, two of each.  A lane owns a key.  A tile's steps (its queries, head by head) may be cut into parts that other
+// workgroups take: the sinks' tiles are seen by every query, and few key heads would leave most of the chip idle.
+// Parts go to memory in 32 bits and are added in order by smha_sink_sum.
+template <int D, bool BF16>
+__global__ void __launch_bounds__(256, 2) smha_sink_bwd_kv(const SinkParams p) {
+    constexpr int NS = D / 16, NDT = D / 32, TB = 64 * D * 2;
+    __shared__ __attribute__((aligned(1024))) char smem[4 * TB];           // Q[0], Q[1], dO[0], dO[1]
+    __shared__ __attribute__((aligned(1024))) float stats[2][2][64];       // [buffer][lse, delta][query]
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_void *)smem, stats0 = (uint32_t)(uintptr_t)(lds_void *)stats;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = lane & 31, hh = lane >> 5;
+
+    const int per = p.n_sink_tiles * p.cut_sink + (p.n_tiles - p.n_sink_tiles) * p.cut_rest;  // items of a key head
+    const int idx = (int)(blockIdx.x & 7) * p.per_xcd + (int)(blockIdx.x >> 3);
+    if (idx >= p.B * p.Hkv * per) return;
+    const int bh = idx / per, item = idx - bh * per, b = bh / p.Hkv, hk = bh - b * p.Hkv;
+    int tile, part, cut;
+    if (item < p.n_sink_tiles * p.cut_sink) {
+        cut = p.cut_sink;
+        tile = item / cut;
+        part = item - tile * cut;
+    } else {
+        cut = p.cut_rest;
+        const int rest = item - p.n_sink_tiles * p.cut_sink;
+        tile = p.n_sink_tiles + rest / cut;
+        part = rest % cut;
+    }
+    const Sequence s = sequence(p, b);
+    const int window = p.window, n_sink = p.n_sink, k0 = tile * 128;
+    const KeyTile kt = key_tile(p, s, k0);
+    const int steps = kt.nq * p.G, begin = part * p.chunk, end = cut == 1 ? steps : min(steps, begin + p.chunk);
+    if (part > 0 && begin >= end) return;
+    const bool alone = steps <= p.chunk || cut == 1;
+
+    const int kw = k0 + 32 * w;
+    u32x4 kf[NS], vf[NS];
+    load_operand<D>(kf, p.K + b * p.ks.b + hk * p.ks.h, p.ks.s, kw, 0, s.len, p.d, lane);
+    load_operand<D>(vf, p.V + b * p.vs.b + hk * p.vs.h, p.vs.s, kw, 0, s.len, p.d, lane);
+    const int qsb = (int)p.qs.s * 2, gsb = (int)p.gs.s * 2;
+    const TileLoad<D> loadQ(w, lane, qsb, p.d), loadG(w, lane, gsb, p.d);
+    const int64_t rows = (int64_t)p.B * p.H * p.Sqp;
+    auto request = [&](int g, int q, int par) __attribute__((always_inline)) {
+        const int h = hk * p.G + g;
+        const u32x4 rQ = make_rsrc4(p.Q + b * p.qs.b + h * p.qs.h, ((int64_t)(s.qb - 1) * p.qs.s + p.d) * 2);
+        const u32x4 rG = make_rsrc4(p.dO + b * p.gs.b + h * p.gs.h, ((int64_t)(s.qb - 1) * p.gs.s + p.d) * 2);
+        loadQ(rQ, lds0 + par * TB, w, q, qsb, 0, s.qa);
+        loadG(rG, lds0 + (2 + par) * TB, w, q, gsb, 0, s.qa);
+        if (w < 2) {
+            const u32x4 rS = make_rsrc4(p.stats + w * rows + ((int64_t)b * p.H + h) * p.Sqp, (int64_t)p.Sqp * 4);
+            load_words_to_lds(rS, stats0 + (par * 2 + w) * 256, (uint32_t)((q + lane) * 4));
+        }
+    };
+    int g = 0, qt = 0;
+    if (begin < end) {
+        g = begin / kt.nq;
+        qt = begin - g * kt.nq;
+        request(g, 64 * (kt.qt0 + qt), 0);
+    }
+    const int rd = j * D * 2 + ((hh ^ swz<D>(j)) * 16);
+    const int tr_row = 4 * hh + ((lane & 15) >> 2);
+    const int tr = tr_row * D * 2 + ((swz<D>(tr_row) ^ (2 * ((lane >> 4) & 1) + ((lane & 3) >> 1))) * 16) + (lane & 1) * 8;
+    f32x16 dk[NDT], dv[NDT];
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt) dk[dt] = dv[dt] = zeros16();
+    tiles_landed();
+    for (int t = begin; t < end; ++t) {
+        const int par = (t - begin) & 1, q64 = 64 * (kt.qt0 + qt);
+        if (++qt == kt.nq) qt = 0, ++g;
+        if (t + 1 < end) request(g, 64 * (kt.qt0 + qt), par ^ 1);
+#pragma unroll
+        for (int sub = 0; sub < 2; ++sub) {
+            const int q = q64 + 32 * sub, p0 = s.off + max(q, s.qa), p1 = s.off + min(q + 32, s.qb) - 1;
+            if (p0 > p1 || !any_seen(p0, p1, kw, kw + 31, window, n_sink)) continue;
+            const char *const Qt = smem + par * TB + sub * (TB / 2), *const Gt = smem + (2 + par) * TB + sub * (TB / 2);
+            // sc[r] = score of key j and query 8 (r / 4) + 4 hh + r % 4
+            f32x16 sc = zeros16(), dp = zeros16();
+#pragma unroll
+            for (int i = 0; i < NS; ++i) sc = mfma32<BF16>(*reinterpret_cast<const u32x4 *>(Qt + (rd ^ (32 * i))), kf[i], sc);
+#pragma unroll
+            for (int i = 0; i < NS; ++i) dp = mfma32<BF16>(*reinterpret_cast<const u32x4 *>(Gt + (rd ^ (32 * i))), vf[i], dp);
+            f32x16 ds;
+#pragma unroll
+            for (int r4 = 0; r4 < 4; ++r4) {
+                const f32x4 l = *reinterpret_cast<const f32x4 *>(&stats[par][0][32 * sub + 8 * r4 + 4 * hh]);
+                const f32x4 dl = *reinterpret_cast<const f32x4 *>(&stats[par][1][32 * sub + 8 * r4 + 4 * hh]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    sc[4 * r4 + e] = fast_exp2(fmaf(sc[4 * r4 + e], p.c, -l[e]));
+                    ds[4 * r4 + e] = sc[4 * r4 + e] * (dp[4 * r4 + e] - dl[e]);
+                }
+            }
+            if (!all_seen(s.off + q, s.off + q + 31, kw, kw + 31, window, n_sink) || q < s.qa || q + 32 > s.qb) {
+                // queries at or after this key (or those that exist), and in whose window it is
+                const int k = kw + j, at = s.off + q;
+                const uint32_t within = k < n_sink ? ~0u : low_bits32(k + window - at);
+                const uint32_t word = within & ~low_bits32(max(k - at, s.qa - q)) & low_bits32(s.qb - q);
+                const u32x16 keep = keep_of(word >> (4 * hh));
+                sc = __builtin_bit_cast(f32x16, __builtin_bit_cast(u32x16, sc) & keep);
+                ds = __builtin_bit_cast(f32x16, __builtin_bit_cast(u32x16, ds) & keep);
+            }
+            u32x4 pf[2], sf[2];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                pf[i >> 2][i & 3] = pack2<BF16>(sc[2 * i], sc[2 * i + 1]);
+                sf[i >> 2][i & 3] = pack2<BF16>(ds[2 * i], ds[2 * i + 1]);
+            }
+#pragma unroll
+            for (int i = 0; i < 2 * NDT; ++i) {
+                const int cu = i / NDT, dt = i % NDT, at = (tr ^ (64 * dt)) + 32 * cu * D, at8 = (tr ^ (64 * dt) ^ 32) + 32 * cu * D + 16 * D;
+                const u32x2 lo = lds_read_tr(reinterpret_cast<const uint16_t *>(Gt + at)), hi = lds_read_tr(reinterpret_cast<const uint16_t *>(Gt + at8));
+                dv[dt] = mfma32<BF16>(u32x4{lo[0], lo[1], hi[0], hi[1]}, pf[cu], dv[dt]);
+                const u32x2 lo2 = lds_read_tr(reinterpret_cast<const uint16_t *>(Qt + at)), hi2 = lds_read_tr(reinterpret_cast<const uint16_t *>(Qt + at8));
+                dk[dt] = mfma32<BF16>(u32x4{lo2[0], lo2[1], hi2[0], hi2[1]}, sf[cu], dk[dt]);
+            }
+        }
+        tiles_landed();
+    }
+    if (alone) {
+        char *const slab = smem + w * (32 * D * 2);
+        store_rows<D, BF16>(dv, 1.f, slab, lane, p.dV + b * p.dvs.b + hk * p.dvs.h, p.dvs.s, kw, p.Sk, p.d);
+        store_rows<D, BF16>(dk, p.scale, slab, lane, p.dK + b * p.dks.b + hk * p.dks.h, p.dks.s, kw, p.Sk, p.d);
+        return;
+    }
+    // [item][dV, dK][wave][4 accumulators][lane][4]
+    float *const mine = p.parts + ((int64_t)idx * 2 * 4 + w) * (D / 8) * 256 + lane * 4;
+#pragma unroll
+    for (int i = 0; i < D / 8; ++i) {
+        *reinterpret_cast<f32x4 *>(mine + i * 256) = f32x4{dv[i / 4][4 * (i % 4)], dv[i / 4][4 * (i % 4) + 1], dv[i / 4][4 * (i % 4) + 2], dv[i / 4][4 * (i % 4) + 3]};
+        *reinterpret_cast<f32x4 *>(mine + 4 * (D / 8) * 256 + i * 256) = f32x4{dk[i / 4][4 * (i % 4)], dk[i / 4][4 * (i % 4) + 1], dk[i / 4][4 * (i % 4) + 2], dk[i / 4][4 * (i % 4) + 3]};
+    }
+}
+
+// The parts of a key tile that was cut, added in order.  A workgroup takes one wave's 32 keys of dK or dV.
+template <int D, bool BF16>
+__global__ void __launch_bounds__(256) smha_sink_sum(const SinkParams p) {
+    const int tile_at = (int)blockIdx.x >> 3, w = (int)blockIdx.x & 3, is_k = ((int)blockIdx.x >> 2) & 1;
+    const int bh = tile_at / p.n_tiles, tile = tile_at - bh * p.n_tiles, b = bh / p.Hkv, hk = bh - b * p.Hkv;
+    const int per = p.n_sink_tiles * p.cut_sink + (p.n_tiles - p.n_sink_tiles) * p.cut_rest;
+    const bool sink = tile < p.n_sink_tiles;
+    const int cut = sink ? p.cut_sink : p.cut_rest;
+    const int item = sink ? tile * cut : p.n_sink_tiles * p.cut_sink + (tile - p.n_sink_tiles) * cut;
+    const Sequence s = sequence(p, b);
+    const int steps = key_tile(p, s, tile * 128).nq * p.G;
+    if (cut == 1 || steps <= p.chunk) return;  // it was written whole
+    const int parts = (steps + p.chunk - 1) / p.chunk;
+    uint16_t *const out = is_k ? p.dK + b * p.dks.b + hk * p.dks.h : p.dV + b * p.dvs.b + hk * p.dvs.h;
+    const int64_t pitch = is_k ? p.dks.s : p.dvs.s;
+    const float factor = is_k ? p.scale : 1.f;
+    const float *const from = p.parts + (((int64_t)bh * per + item) * 8 + is_k * 4 + w) * (D / 8) * 256;
+    for (int i = threadIdx.x; i < D / 8 * 64; i += 256) {
+        f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+        for (int c = 0; c < parts; ++c) sum += *reinterpret_cast<const f32x4 *>(from + (int64_t)c * 8 * (D / 8) * 256 + i * 4);
+        const int quad = i >> 6, lane = i & 63, key = tile * 128 + 32 * w + (lane & 31), col = 8 * quad + 4 * (lane >> 5);
+        if (key < p.Sk && col < p.d)
+            *reinterpret_cast<u32x2 *>(out + key * pitch + col) = u32x2{pack2<BF16>(sum[0] * factor, sum[1] * factor), pack2<BF16>(sum[2] * factor, sum[3] * factor)};
+    }
+}
+
+// ---------------------------------------------------------------------------------------
+// Launches
+// ---------------------------------------------------------------------------------------
+static bool strides_fit(const int64_t *s, int64_t rows, int d) {
+    if (!s) return rows * d * 2 < ((int64_t)1 << 31);
+    // (a head is addressed through 32-bit offsets; batch and head strides may be zero where a tensor is only read)
+    return s[0] % 8 == 0 && s[1] % 8 == 0 && s[2] % 8 == 0 && s[0] >= 0 && s[1] >= 0 && s[2] >= d && (rows * s[2] + d) * 2 < ((int64_t)1 << 31);
+}
+
+static Strides strides_of(const int64_t *s, int64_t heads, int64_t rows, int d) {
+    return s ? Strides{s[0], s[1], s[2]} : Strides{heads * rows * d, rows * d, d};
+}
+
+// What both directions check and fill in.
+static smha_status_t sink_params(SinkParams &sp, int B, int H, int Hkv, int Sq, int Sk, int d, smha_dtype_t dtype, const int32_t *offsets, const int32_t *lengths,
+                                 int window, int n_sink, float scale) {
+    if (B < 1 || H < 1 || Hkv < 1 || Sq < 1 || Sk < 1 || window < 0 || n_sink < 0) return SMHA_ERR_INVALID_ARG;
+    if (H % Hkv) return SMHA_ERR_SHAPE;
+    if (dtype != SMHA_F16 && dtype != SMHA_BF16) return SMHA_ERR_UNSUPPORTED;
+    if (d < 8 || d > 128 || d % 8) return SMHA_ERR_UNSUPPORTED;
+    // (work items are numbered in 32 bits)
+    if ((int64_t)B * H > (1 << 24) || (int64_t)B * H * (std::max(Sq, Sk) / 64 + 2) > (1 << 28)) return SMHA_ERR_UNSUPPORTED;
+    sp.B = B; sp.H = H; sp.Hkv = Hkv; sp.G = H / Hkv; sp.Sq = Sq; sp.Sk = Sk; sp.d = d;
+    sp.window = window == 0 || window > Sk ? Sk : window;
+    sp.n_sink = std::min(n_sink, Sk);
+    sp.offsets = offsets; sp.lengths = lengths;
+    sp.scale = scale > 0.f ? scale : 1.0f / std::sqrt((float)d);
+    sp.c = sp.scale * 1.4426950408889634f;
+    sp.Sqp = (Sq + 127) / 128 * 128;
+    return SMHA_OK;
+}
+
+// How dK and dV are cut: enough parts for two rounds of the workgroups that the chip holds (two on each of 256 compute units), of at least
+// 24 steps, so that the 128 x D partial sums that each part writes stay a small share of its work.
+static void sink_cuts(SinkParams &sp) {
+    const int64_t nq = (sp.Sq + 63) / 64;
+    const int64_t near = std::min<int64_t>(nq, (sp.window + 127 + 63) / 64 + 1);
+    sp.n_tiles = (sp.Sk + 127) / 128;
+    sp.n_sink_tiles = sp.window < sp.Sk ? (sp.n_sink + 127) / 128 : 0;
+    const int64_t all = (int64_t)sp.B * sp.Hkv * sp.G * (sp.n_sink_tiles * nq + (sp.n_tiles - sp.n_sink_tiles) * (sp.window < sp.Sk ? near : (nq + 1) / 2));
+    sp.chunk = (int)std::max<int64_t>(24, (all + 1023) / 1024);
+    sp.cut_sink = (int)((nq * sp.G + sp.chunk - 1) / sp.chunk);
+    sp.cut_rest = (int)((near * sp.G + sp.chunk - 1) / sp.chunk);
+    if (sp.n_sink_tiles == 0) sp.cut_sink = 1;
+}
+
+static int64_t sink_stats_bytes(const SinkParams &sp) { return (int64_t)2 * sp.B * sp.H * sp.Sqp * 4; }
+static int64_t sink_items(const SinkParams &sp) {
+    return (int64_t)sp.B * sp.Hkv * ((int64_t)sp.n_sink_tiles * sp.cut_sink + (int64_t)(sp.n_tiles - sp.n_sink_tiles) * sp.cut_rest);
+}
+static int sink_width(int d) { return d <= 64 ? 64 : 128; }
+
+template <int D, bool BF16> static hipError_t launch_sink_fwd(SinkParams &sp, hipStream_t stream) {
+    const int64_t items = (int64_t)sp.B * sp.H * ((sp.Sq + 127) / 128);
+    sp.per_xcd = (int)((items + 7) / 8);
+    hipLaunchKernelGGL((smha_sink_fwd<D, BF16>), dim3(8 * sp.per_xcd), dim3(256), 0, stream, sp);
+    return hipGetLastError();
+}
+
+template <int D, bool BF16> static hipError_t launch_sink_bwd(SinkParams &sp, hipStream_t stream) {
+    const int64_t rows = (int64_t)sp.B * sp.H * sp.Sqp;
+    hipLaunchKernelGGL((smha_sink_stats<BF16>), dim3((unsigned)((rows + 15) / 16)), dim3(256), 0, stream, sp);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    sp.per_xcd = (int)((sink_items(sp) + 7) / 8);
+    hipLaunchKernelGGL((smha_sink_bwd_kv<D, BF16>), dim3(8 * sp.per_xcd), dim3(256), 0, stream, sp);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    if (sp.cut_sink > 1 || sp.cut_rest > 1) {
+        hipLaunchKernelGGL((smha_sink_sum<D, BF16>), dim3((unsigned)(8 * sp.B * sp.Hkv * sp.n_tiles)), dim3(256), 0, stream, sp);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+    sp.per_xcd = (int)(((int64_t)sp.B * sp.H * ((sp.Sq + 127) / 128) + 7) / 8);
+    hipLaunchKernelGGL((smha_sink_bwd_q<D, BF16>), dim3(8 * sp.per_xcd), dim3(256), 0, stream, sp);
+    return hipGetLastError();
+}
+
+}  // namespace smha
+
+using namespace smha;
+
+extern "C" smha_status_t smha_sink_forward(const void *Q, const void *K, const void *V, void *O, float *lse, int B, int H, int Hkv, int Sq, int Sk, int d,
+                                           smha_dtype_t dtype, const int64_t q_strides[3], const int64_t k_strides[3], const int64_t v_strides[3],
+                                           const int64_t o_strides[3], const int32_t *offsets, const int32_t *lengths, int window, int n_sink, float scale,
+                                           void *hip_stream) {
+    if (!Q || !K || !V || !O) return SMHA_ERR_INVALID_ARG;
+    SinkParams sp{};
+    const smha_status_t st = sink_params(sp, B, H, Hkv, Sq, Sk, d, dtype, offsets, lengths, window, n_sink, scale);
+    if (st != SMHA_OK) return st;
+    if (((uintptr_t)Q | (uintptr_t)K | (uintptr_t)V | (uintptr_t)O) & 15) return SMHA_ERR_UNSUPPORTED;
+    if (!strides_fit(q_strides, Sq + 128, d) || !strides_fit(k_strides, (int64_t)Sk + 128, d) || !strides_fit(v_strides, (int64_t)Sk + 128, d) || !strides_fit(o_strides, Sq + 128, d))
+        return SMHA_ERR_UNSUPPORTED;
+    sp.Q = (const uint16_t *)Q; sp.K = (const uint16_t *)K; sp.V = (const uint16_t *)V; sp.O = (uint16_t *)O; sp.lse = lse;
+    sp.qs = strides_of(q_strides, H, Sq, d); sp.ks = strides_of(k_strides, Hkv, Sk, d); sp.vs = strides_of(v_strides, Hkv, Sk, d); sp.os = strides_of(o_strides, H, Sq, d);
+    const hipStream_t stream = (hipStream_t)hip_stream;
+    const bool bf16 = dtype == SMHA_BF16;
+    const hipError_t e = sink_width(d) == 64 ? (bf16 ? launch_sink_fwd<64, true>(sp, stream) : launch_sink_fwd<64, false>(sp, stream))
+                                             : (bf16 ? launch_sink_fwd<128, true>(sp, stream) : launch_sink_fwd<128, false>(sp, stream));
+    return e == hipSuccess ? SMHA_OK : SMHA_ERR_HIP;
+}
+
+extern "C" smha_status_t smha_sink_workspace(int B, int H, int Hkv, int Sq, int Sk, int d, int window, int n_sink, size_t *need) {
+    if (!need) return SMHA_ERR_INVALID_ARG;
+    SinkParams sp{};
+    const smha_status_t st = sink_params(sp, B, H, Hkv, Sq, Sk, d, SMHA_F16, nullptr, nullptr, window, n_sink, 0.f);
+    if (st != SMHA_OK) return st;
+    sink_cuts(sp);
+    const bool cut = sp.cut_sink > 1 || sp.cut_rest > 1;
+    *need = (size_t)(sink_stats_bytes(sp) + (cut ? sink_items(sp) * 2 * 128 * sink_width(d) * 4 : 0));
+    return SMHA_OK;
+}
+
+extern "C" smha_status_t smha_sink_backward(const void *Q, const void *K, const void *V, const void *O, const float *lse, const void *dO, void *dQ, void *dK, void *dV,
+                                            int B, int H, int Hkv, int Sq, int Sk, int d, smha_dtype_t dtype, const int64_t q_strides[3],
+                                            const int64_t k_strides[3], const int64_t v_strides[3], const int64_t o_strides[3], const int64_t do_strides[3],
+                                            const int64_t dq_strides[3], const int64_t dk_strides[3], const int64_t dv_strides[3], const int32_t *offsets,
+                                            const int32_t *lengths, int window, int n_sink, float scale, void *workspace, size_t workspace_bytes,
+                                            void *hip_stream) {
+    if (!Q || !K || !V || !O || !lse || !dO || !dQ || !dK || !dV || !workspace) return SMHA_ERR_INVALID_ARG;
+    SinkParams sp{};
+    const smha_status_t st = sink_params(sp, B, H, Hkv, Sq, Sk, d, dtype, offsets, lengths, window, n_sink, scale);
+    if (st != SMHA_OK) return st;
+    size_t need = 0;
+    (void)smha_sink_workspace(B, H, Hkv, Sq, Sk, d, window, n_sink, &need);
+    if (workspace_bytes < need) return SMHA_ERR_INVALID_ARG;
+    if (((uintptr_t)Q | (uintptr_t)K | (uintptr_t)V | (uintptr_t)O | (uintptr_t)dO | (uintptr_t)dQ | (uintptr_t)dK | (uintptr_t)dV | (uintptr_t)workspace) & 15)
+        return SMHA_ERR_UNSUPPORTED;
+    for (const int64_t *s : {q_strides, o_strides, do_strides, dq_strides})
+        if (!strides_fit(s, Sq + 128, d)) return SMHA_ERR_UNSUPPORTED;
+    for (const int64_t *s : {k_strides, v_strides, dk_strides, dv_strides})
+        if (!strides_fit(s, (int64_t)Sk + 128, d)) return SMHA_ERR_UNSUPPORTED;
+    sink_cuts(sp);
+    sp.Q = (const uint16_t *)Q; sp.K = (const uint16_t *)K; sp.V = (const uint16_t *)V; sp.Oin = (const uint16_t *)O; sp.dO = (const uint16_t *)dO;
+    sp.dQ = (uint16_t *)dQ; sp.dK = (uint16_t *)dK; sp.dV = (uint16_t *)dV; sp.lse = const_cast<float *>(lse);
+    sp.qs = strides_of(q_strides, H, Sq, d); sp.ks = strides_of(k_strides, Hkv, Sk, d); sp.vs = strides_of(v_strides, Hkv, Sk, d);
+    sp.os = strides_of(o_strides, H, Sq, d); sp.gs = strides_of(do_strides, H, Sq, d);
+    sp.dqs = strides_of(dq_strides, H, Sq, d); sp.dks = strides_of(dk_strides, Hkv, Sk, d); sp.dvs = strides_of(dv_strides, Hkv, Sk, d);
+    sp.stats = (float *)workspace;
+    sp.parts = (float *)((char *)workspace + sink_stats_bytes(sp));
+    const hipStream_t stream = (hipStream_t)hip_stream;
+    const bool bf16 = dtype == SMHA_BF16;
+    const hipError_t e = sink_width(d) == 64 ? (bf16 ? launch_sink_bwd<64, true>(sp, stream) : launch_sink_bwd<64, false>(sp, stream))
+                                             : (bf16 ? launch_sink_bwd<128, true>(sp, stream) : launch_sink_bwd<128, false>(sp, stream));
+    return e == hipSuccess ? SMHA_OK : SMHA_ERR_HIP;
+}
