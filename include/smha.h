@@ -363,6 +363,52 @@ smha_status_t smha_sink_backward(const void *Q, const void *K, const void *V, co
                                  const int32_t *offsets, const int32_t *lengths, int window, int n_sink, float scale,
                                  void *workspace, size_t workspace_bytes, void *hip_stream);
 
+/* ---- Attention of new tokens on a cache ----
+ *
+ * The last T tokens of every sequence, whose keys are in the cache already; H query heads share Hkv key heads.
+ *   Q, O            device, [B][H][T][d]; K, V: [B][Hkv][Sk][d], of which sequence b uses the first lengths[b] keys (device, int32
+ *                   [B], taken as 0 or Sk where outside 0 .. Sk; the new tokens' keys are the last of them).
+ *                   Types, head sizes, strides, alignment as in smha_sink_forward
+ *   PK, PV          device, [Hkv][P][d], strides {head, key}: keys before those of every sequence, one copy for all; P = 0: none
+ *   weights         device, float [B][Hkv][Sk], strides {batch, head} (NULL = packed): what attention each of a sequence's own keys
+ *                   received, summed over the T tokens and H / Hkv heads, is added; NULL: not wanted
+ *   window, n_sink  as in smha_sink_forward, in a sequence's own keys; a window together with a prefix is UNSUPPORTED
+ * Token t of sequence b stands at own key lengths[b] - T + t and sees the keys up to it (in its window, or sinks) and all of the
+ * prefix.  Below 0 there is no such token: its output row is zero and it adds to no weight.
+ * lengths are read by the kernels (nothing synchronises; a captured call follows them), which divide the keys of all sequences evenly
+ * over the chip whatever the lengths are.  The result does not depend on the order in which workgroups run.
+ * workspace: device, 16-byte aligned, smha_cache_workspace bytes or more; the call's alone until it has run.  (weigh: nonzero with
+ * weights: 4 H T Sk bytes a sequence more.)
+ * Errors as for smha_sink_forward. */
+smha_status_t smha_cache_workspace(int B, int H, int Hkv, int T, int Sk, int P, int d, int window, int n_sink, int weigh,
+                                   size_t *need);
+smha_status_t smha_cache_forward(const void *Q, const void *K, const void *V, const void *PK, const void *PV, void *O,
+                                 float *weights, const int32_t *lengths, int B, int H, int Hkv, int T, int Sk, int P, int d,
+                                 smha_dtype_t dtype, const int64_t q_strides[3], const int64_t k_strides[3],
+                                 const int64_t v_strides[3], const int64_t pk_strides[2], const int64_t pv_strides[2],
+                                 const int64_t o_strides[3], const int64_t w_strides[2], int window, int n_sink, float scale,
+                                 void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* ---- Eviction from a cache by accumulated attention ----
+ *
+ * Every key head of every sequence keeps min(lengths[b], budget) keys.  Where it has more, keys stay in the order of
+ * (recent first: position > highest position - recent; then by weight, falling; then by slot, rising); recent keys and weights of
+ * +inf are equals, and so are NaN and -inf.  Keys that stay keep their slots, but those in slots from `budget` on move, in order, to
+ * the slots before it that were freed, with their weights and positions.  Slots from the new length on get weight 0 and
+ * position -1; their keys and values stay as they are.
+ *   K, V            device, [B][Hkv][Sk][d], any 16-bit type, changed in place; strides as in smha_forward, but a head may be of any size
+ *   weights         device, float [B][Hkv][Sk], positions: int32 [B][Hkv][Sk], lengths: int32 [B]; packed
+ *   *_out           what they are then; each may be the input itself, or must not overlap any
+ * Not affected by NaN or infinities among the weights beyond what is said above.  No floating-point sums: exact.
+ * workspace: device, smha_cache_evict_workspace bytes or more; the call's alone until it has run.
+ * Errors: INVALID_ARG (null, sizes, budget < 1, recent < 0, too small a workspace), UNSUPPORTED (d not a multiple of 8 up to 128, alignment,
+ * strides, more than 65535 heads in all, Sk above 2^28), HIP. */
+smha_status_t smha_cache_evict_workspace(int B, int Hkv, int Sk, int d, int budget, int recent, size_t *need);
+smha_status_t smha_cache_evict(void *K, void *V, const float *weights, const int32_t *positions, const int32_t *lengths,
+                               float *weights_out, int32_t *positions_out, int32_t *lengths_out, int B, int Hkv, int Sk, int d,
+                               int budget, int recent, const int64_t k_strides[3], const int64_t v_strides[3], void *workspace,
+                               size_t workspace_bytes, void *hip_stream);
+
 const char *smha_status_string(smha_status_t status);
 
 /* Symbol names of kernels, for matching profiler output (name and duration bookkeeping is left to the caller).

@@ -11,7 +11,8 @@ from .binding import (  # noqa: F401
     smha_plan_from_dense_rect,
     smha_plan_from_desc, smha_plan_info, smha_plan_prepare, smha_plan_work_order, smha_status_string)
 
-_OPERATORS = {name: "sink" for name in ("sink_attention", "smha_sink_backward", "smha_sink_forward", "smha_sink_workspace")}
+_OPERATORS = {**{name: "sink" for name in ("sink_attention", "smha_sink_backward", "smha_sink_forward", "smha_sink_workspace")},
+              **{name: "cache" for name in ("cache_attention", "cache_evict", "smha_cache_evict_workspace", "smha_cache_workspace")}}
 
 
 def __getattr__(name):  # (these modules need torch when they are imported, which plans on the host do not)

@@ -108,6 +108,12 @@ def _load():
     lib.smha_sink_forward.argtypes = [vp] * 5 + [i] * 7 + [i64p] * 4 + [vp, vp, i, i, C.c_float, vp]
     lib.smha_sink_workspace.argtypes = [i] * 8 + [C.POINTER(C.c_size_t)]
     lib.smha_sink_backward.argtypes = [vp] * 9 + [i] * 7 + [i64p] * 8 + [vp, vp, i, i, C.c_float, vp, C.c_size_t, vp]
+    lib.smha_cache_workspace.argtypes = [i] * 10 + [C.POINTER(C.c_size_t)]
+    lib.smha_cache_forward.argtypes = [vp] * 8 + [i] * 8 + [i64p] * 7 + [i, i, C.c_float, vp, C.c_size_t, vp]
+    lib.smha_cache_evict_workspace.argtypes = [i] * 6 + [C.POINTER(C.c_size_t)]
+    lib.smha_cache_evict.argtypes = [vp] * 8 + [i] * 6 + [i64p] * 2 + [vp, C.c_size_t, vp]
+    for entry in ("workspace", "forward", "evict_workspace", "evict"):
+        getattr(lib, f"smha_cache_{entry}").restype = i
     lib.smha_sink_forward.restype = lib.smha_sink_workspace.restype = lib.smha_sink_backward.restype = i
     lib.smha_plan_destroy.argtypes = [vp]
     lib.smha_plan_destroy.restype = None

@@ -17,7 +17,7 @@ LIB = os.path.join(HERE, "libsmha.so")
 EXT = os.path.join(HERE, "_smha_torch.so")
 EXT_SOURCE = os.path.join(CSRC, "torch_binding.cpp")
 ABI_HEADER = os.path.join(ROOT, "include", "smha.h")
-SOURCES = ["kernels.hip", "sink.hip", "plan.cpp"]
+SOURCES = ["kernels.hip", "sink.hip", "cache.hip", "plan.cpp"]
 HEADERS = ["smha_internal.hpp", "device_common.hpp", "device_pool.hpp", "block_fwd2.inc", "block_fwd16.inc", "wave_fwd.inc", ABI_HEADER]
 
 

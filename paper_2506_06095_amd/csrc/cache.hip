@@ -1,0 +1,801 @@
+// Attention of a few new tokens on a cache, with a window and sinks, with a prefix that all sequences share, with an account of what
+// attention each key received; and the eviction of keys by that account.
+//
+// Attention.  Query t of sequence b stands at position len_b - T + t of the sequence's own keys.  The rows that read the same keys, G = H / Hkv
+// query heads times T tokens of one sequence (own keys) or of all sequences (prefix keys), are taken 32 at a time; the keys are
+// read in tiles of 32 by waves that share nothing while they read.  What bounds such a call is memory (a key's 4 d bytes meet
+// 4 d G T operations), so what matters is that every compute unit reads, and all of them about as much: the tiles of all
+// sequences are counted on the device and cut into as many segments, of about the same length, as workgroups fit the chip
+// (segments()); lengths are never needed on the host.  A workgroup's four waves take a segment's tiles in turn and join in LDS; segments
+// of the same rows are joined by a second kernel, in a fixed order, which also adds up the keys' accounts from the scores
+// that the first left in memory: 4 G T bytes a key where reading the key once more would take 2 d.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+
+#include "device_common.hpp"
+#include "smha.h"
+
+namespace smha {
+
+struct CacheParams {
+    const uint16_t *Q, *K, *V, *PK, *PV;
+    uint16_t *O;
+    float *weights;
+    Strides qs, ks, vs, os;
+    int64_t pk_h, pk_s, pv_h, pv_s, w_b, w_h;
+    const int32_t *lengths;
+    int B, H, Hkv, G, T, Sk, P, d;
+    int window, n_sink;
+    float c;
+    int slots;       // segments wanted
+    int own_tiles, prefix_tiles;  // 32-row tiles of G T rows, of B G T rows (0 without a prefix)
+    int segs;        // segments there is room for
+    int score_pitch; // keys per row of `scores`
+    int2 *info;      // [prefix groups, own groups]: first segment, segments
+    float *stats;    // [segment][2][32]: reference (log2 units), sum
+    float *parts;    // [segment][32][D]
+    float *scores;   // [B][Hkv][G T][score_pitch], log2 units
+};
+
+// What one sequence's own keys are to its queries: the tiles of the sinks, then those of the window.
+struct OwnKeys {
+    int len, head, t0, n, gap0, gap1;
+    __device__ __forceinline__ int key(int t) const { return 32 * (t < head ? t : t0 + t - head); }
+};
+__device__ __forceinline__ OwnKeys own_keys(int length, int T, int Sk, int window, int n_sink) {
+    OwnKeys k;
+    k.len = min(max(length, 0), Sk);
+    const int from = max(0, max(k.len - T, 0) - window + 1);  // the first key in the first query's window
+    k.head = (min(n_sink, from) + 31) / 32;
+    k.t0 = max(from / 32, k.head);
+    k.n = k.len > 0 ? k.head + (k.len - 1) / 32 + 1 - k.t0 : 0;
+    k.gap0 = n_sink < from ? n_sink : 0;
+    k.gap1 = n_sink < from ? from : 0;
+    return k;
+}
+
+struct Segment {
+    int seg;             // its number; -1: none
+    int b, hk, rows0;    // rows0: first of the 32 rows; b = -1: prefix
+    int part, parts, n;  // of the group's n tiles
+    int group;
+};
+
+__device__ __forceinline__ int wave_sum(int v) {
+#pragma unroll
+    for (int m = 32; m > 0; m >>= 1) v += __shfl_xor(v, m);
+    return v;
+}
+
+// The segment of a workgroup.  Every wave of the launch computes the same cut: c tiles a segment, the least multiple of four (a team's
+// turn) for which a few corrections find no more than `slots` segments.
+__device__ __forceinline__ Segment segment_of(const CacheParams &p, int lane) {
+    const int prefix_groups = p.Hkv * p.prefix_tiles, per_b = p.Hkv * p.own_tiles;
+    const int prefix_n = p.prefix_tiles ? (p.P + 31) / 32 : 0;
+    auto tiles = [&](int b) __attribute__((always_inline)) { return b < p.B ? own_keys(p.lengths[b], p.T, p.Sk, p.window, p.n_sink).n : 0; };
+    const int first64 = tiles(lane);
+    int sum = first64;
+    for (int b = 64 + lane; b - lane < p.B; b += 64) sum += tiles(b);
+    const int total = prefix_groups * prefix_n + per_b * wave_sum(sum);
+    int c = max(4, ((total + p.slots - 1) / p.slots + 3) & ~3), count = 0;
+    for (int turn = 0;; ++turn) {
+        sum = (first64 + c - 1) / c;
+        for (int b = 64 + lane; b - lane < p.B; b += 64) sum += (tiles(b) + c - 1) / c;
+        count = prefix_groups * ((prefix_n + c - 1) / c) + per_b * wave_sum(sum);
+        if (count <= p.slots || turn == 3) break;
+        c = ((int)(((int64_t)c * count + p.slots - 1) / p.slots) + 3) & ~3;
+    }
+    count = __builtin_amdgcn_readfirstlane(count);
+    c = __builtin_amdgcn_readfirstlane(c);
+    // an XCD takes a run of segments: those that read the same keys are neighbours
+    const int per_xcd = (count + 7) / 8, slot = (int)blockIdx.x >> 3;
+    int at = (int)(blockIdx.x & 7) * per_xcd + slot;
+    Segment s{-1, -1, 0, 0, 0, 1, 0, 0};
+    if (slot >= per_xcd || at >= count) return s;
+    s.seg = at;
+    const int prefix_segs = prefix_groups * ((prefix_n + c - 1) / c);
+    if (at < prefix_segs) {
+        s.parts = (prefix_n + c - 1) / c;
+        s.group = at / s.parts;
+        s.part = at - s.group * s.parts;
+        s.hk = s.group / p.prefix_tiles;
+        s.rows0 = 32 * (s.group - s.hk * p.prefix_tiles);
+        s.n = prefix_n;
+        return s;
+    }
+    at -= prefix_segs;
+    for (int b0 = 0; b0 < p.B; b0 += 64) {
+        const int n = b0 ? tiles(b0 + lane) : first64, mine = per_b * ((n + c - 1) / c);
+        int upto = mine;
+#pragma unroll
+        for (int m = 1; m < 64; m <<= 1) {
+            const int below = __shfl_up(upto, m);
+            if (lane >= m) upto += below;
+        }
+        const uint64_t past = __builtin_amdgcn_ballot_w64(upto > at);
+        if (past) {
+            const int who = __builtin_ctzll(past);
+            const int rest = at - (__builtin_amdgcn_readlane(upto, who) - __builtin_amdgcn_readlane(mine, who));
+            s.n = __builtin_amdgcn_readlane(n, who);
+            s.parts = (s.n + c - 1) / c;
+            s.b = b0 + who;
+            const int in_b = rest / s.parts;
+            s.part = rest - in_b * s.parts;
+            s.hk = in_b / p.own_tiles;
+            s.rows0 = 32 * (in_b - s.hk * p.own_tiles);
+            s.group = prefix_groups + s.b * per_b + in_b;
+            return s;
+        }
+        at -= __builtin_amdgcn_readlane(upto, 63);
+    }
+    s.seg = -1;  // (not reached: the segments counted are those found)
+    return s;
+}
+
+// K, V: one buffer of 32 keys each a wave, refilled as soon as its fragments are read: K of the next tile lands under this tile's softmax
+// and second product, V of the next under the next tile's scores.  Eight waves a compute unit at 128 columns, 16 at 64.
+// Probabilities are rounded to the inputs' type for the second product (half a step each, as in smha_sink_fwd); sums are 32 bits.
+template <int D, bool BF16, bool WEIGH>
+__global__ void __launch_bounds__(256, D == 64 ? 4 : 2) smha_cache_part(const CacheParams p) {
+    constexpr int NS = D / 16, NDT = D / 32, CPR = D / 8, LPT = CPR / 2, RPL = 64 / CPR, NO = 16 / RPL, TB = 32 * D * 2;
+    __shared__ __attribute__((aligned(1024))) char all_tiles[4 * 2 * TB];  // per wave: K, V
+    __shared__ float team[4][2][32];                                        // references and sums
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = lane & 31, hh = lane >> 5;
+    char *const smem = all_tiles + w * 2 * TB;
+    const uint32_t lds = (uint32_t)(uintptr_t)(lds_void *)smem;
+    const float NEG_INF = -__builtin_inff();
+    const Segment s = segment_of(p, lane);
+    if (s.seg < 0) return;
+    const bool prefix = s.b < 0;
+    const OwnKeys own = prefix ? OwnKeys{p.P, 0, 0, s.n, 0, 0} : own_keys(uniform_load(p.lengths + s.b), p.T, p.Sk, p.window, p.n_sink);
+
+    // this lane's row
+    const int GT = p.G * p.T, row = s.rows0 + j, rows = prefix ? p.B * GT : GT;
+    const int rb = prefix ? min(row / GT, p.B - 1) : s.b, in_b = prefix ? row - rb * GT : row, g = in_b / p.T, t = in_b - g * p.T;
+    const int len_r = prefix ? min(max(p.lengths[rb], 0), p.Sk) : own.len;
+    const int pos = row < rows ? len_r - p.T + t : -1;  // below 0: no such query
+    u32x4 qf[NS];
+    {
+        const uint16_t *const q = p.Q + rb * p.qs.b + (s.hk * p.G + g) * p.qs.h + t * p.qs.s + 8 * hh;
+#pragma unroll
+        for (int i = 0; i < NS; ++i) {
+            qf[i] = u32x4{0, 0, 0, 0};
+            if (pos >= 0 && 16 * i + 8 * hh < p.d) qf[i] = *reinterpret_cast<const u32x4 *>(q + 16 * i);
+        }
+    }
+    const int64_t ks = prefix ? p.pk_s : p.ks.s, vs = prefix ? p.pv_s : p.vs.s;
+    const uint16_t *const Kb = prefix ? p.PK + s.hk * p.pk_h : p.K + s.b * p.ks.b + s.hk * p.ks.h;
+    const uint16_t *const Vb = prefix ? p.PV + s.hk * p.pv_h : p.V + s.b * p.vs.b + s.hk * p.vs.h;
+    const u32x4 rK = make_rsrc4(Kb, ((int64_t)(own.len - 1) * ks + p.d) * 2), rV = make_rsrc4(Vb, ((int64_t)(own.len - 1) * vs + p.d) * 2);
+    const int ksb = (int)ks * 2, vsb = (int)vs * 2, row0 = lane / CPR;
+    uint32_t k_go[NO], v_go[NO];
+#pragma unroll
+    for (int o = 0; o < NO; ++o) {
+        const int ch = (lane % CPR) ^ swz_both<D>(row0 + RPL * o);
+        k_go[o] = ch < (p.d >> 3) ? (uint32_t)(row0 * ksb + ch * 16) : kNoChunk;
+        v_go[o] = ch < (p.d >> 3) ? (uint32_t)(row0 * vsb + ch * 16) : kNoChunk;
+    }
+    // keys in the gap between the sinks and the window read as zeros: no query sees them, and they may hold anything
+    auto request = [&](u32x4 rsrc, uint32_t to, const uint32_t (&go)[NO], int pitch, int key) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < LPT; ++i) {
+            const int r = key + row0 + RPL * i;
+            const uint32_t at = go[i % NO] + (uint32_t)((key + RPL * i) * pitch);
+            load_to_lds(rsrc, to + i * 1024, (int)(r >= own.gap0 && r < own.gap1 ? kPast : at));
+        }
+    };
+    const int begin = (int)((int64_t)s.n * s.part / s.parts) + w, end = (int)((int64_t)s.n * (s.part + 1) / s.parts);
+    if (begin < end) {
+        request(rK, lds, k_go, ksb, own.key(begin));
+        request(rV, lds + TB, v_go, vsb, own.key(begin));
+    }
+    const int rd = j * D * 2 + ((hh ^ swz_both<D>(j)) * 16);
+    const int tr_row = 4 * hh + ((lane & 15) >> 2);
+    const int tr = tr_row * D * 2 + ((swz_both<D>(tr_row) ^ (2 * ((lane >> 4) & 1) + ((lane & 3) >> 1))) * 16) + (lane & 1) * 8;
+    float *const score_row = WEIGH && !prefix && row < rows ? p.scores + (((int64_t)s.b * p.Hkv + s.hk) * GT + row) * p.score_pitch : nullptr;
+
+    float m_run = NEG_INF, l_run = 0.f;
+    const float thr = 8.0f / p.c;
+    f32x16 o[NDT];
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt) o[dt] = zeros16();
+    for (int tile = begin; tile < end; tile += 4) {
+        const int key = own.key(tile);
+        const bool more = tile + 4 < end;
+        wait_all_but<LPT>();  // K has landed (V's requests came after)
+        f32x16 acc = zeros16();
+        u32x4 kf[NS];
+#pragma unroll
+        for (int i = 0; i < NS; ++i) kf[i] = *reinterpret_cast<const u32x4 *>(smem + (rd ^ (32 * i)));
+#pragma unroll
+        for (int i = 0; i < NS; ++i) acc = mfma32<BF16>(kf[i], qf[i], acc);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // K's buffer is read
+        if (!WEIGH && more) request(rK, lds, k_go, ksb, own.key(tile + 4));
+        uint32_t word;
+        if (prefix) word = pos >= 0 ? low_bits32(p.P - key) : 0;
+        else word = pos >= 0 ? low_bits32(pos - key + 1) & (~low_bits32(pos - p.window + 1 - key) | low_bits32(p.n_sink - key)) : 0;
+        if (__builtin_amdgcn_ballot_w64(word != ~0u) != 0) {
+            const u32x16 keep = keep_of(word >> (4 * hh)), sc = __builtin_bit_cast(u32x16, acc);
+            acc = __builtin_bit_cast(f32x16, (sc & keep) | (~keep & 0xFF800000u));
+        }
+        if constexpr (WEIGH) {
+            // (before the next K is requested: the waits below count that many requests)
+            if (score_row) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const f32x4 v = {acc[4 * q] * p.c, acc[4 * q + 1] * p.c, acc[4 * q + 2] * p.c, acc[4 * q + 3] * p.c};
+                    *reinterpret_cast<f32x4 *>(score_row + key + 8 * q + 4 * hh) = v;
+                }
+            }
+            asm volatile("" ::: "memory");
+            if (more) request(rK, lds, k_go, ksb, own.key(tile + 4));
+        }
+        float mt = NEG_INF;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) mt = fmaxf(mt, acc[r]);
+        if (__builtin_amdgcn_ballot_w64(mt > m_run + thr) != 0) {
+            mt = fmaxf(mt, __shfl_xor(mt, 32));
+            const float m_new = fmaxf(m_run, mt), alpha = fast_exp2((m_run - (m_new == NEG_INF ? 0.f : m_new)) * p.c);
+            m_run = m_new;
+            l_run *= alpha;
+#pragma unroll
+            for (int dt = 0; dt < NDT; ++dt) o[dt] *= alpha;
+        }
+        const float mc = (m_run == NEG_INF ? 0.f : m_run) * p.c;
+        u32x4 pf[2];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+            const float e0 = fast_exp2(fmaf(acc[2 * q], p.c, -mc)), e1 = fast_exp2(fmaf(acc[2 * q + 1], p.c, -mc));
+            pf[q >> 2][q & 3] = pack2<BF16>(e0, e1);
+            l_run += e0 + e1;
+        }
+        if (more) wait_all_but<LPT>();  // V has landed
+        else wait_all_but<0>();
+#pragma unroll
+        for (int i = 0; i < 2 * NDT; ++i) {
+            const char *const at = smem + TB + ((tr ^ (64 * (i % NDT))) + 32 * (i / NDT) * D), *const at8 = smem + TB + ((tr ^ (64 * (i % NDT)) ^ 32) + 32 * (i / NDT) * D + 16 * D);
+            const u32x2 lo = lds_read_tr(reinterpret_cast<const uint16_t *>(at)), hi = lds_read_tr(reinterpret_cast<const uint16_t *>(at8));
+            o[i % NDT] = mfma32<BF16>(u32x4{lo[0], lo[1], hi[0], hi[1]}, pf[i / NDT], o[i % NDT]);
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // V's buffer is read
+        if (more) request(rV, lds + TB, v_go, vsb, own.key(tile + 4));
+    }
+
+    // The team joins: every wave leaves its accumulators in its own tiles' place and takes a quarter of the columns of all four.
+    constexpr int NR = D / 2, NQ = NR / 4;  // accumulators a lane holds, and takes
+    const float l = l_run + __shfl_xor(l_run, 32);
+    float *const mine = reinterpret_cast<float *>(smem);
+#pragma unroll
+    for (int i = 0; i < NR / 4; ++i)
+        *reinterpret_cast<f32x4 *>(mine + (i * 64 + lane) * 4) = f32x4{o[i / 4][4 * (i % 4)], o[i / 4][4 * (i % 4) + 1], o[i / 4][4 * (i % 4) + 2], o[i / 4][4 * (i % 4) + 3]};
+    if (hh == 0) {
+        team[w][0][j] = m_run * p.c;
+        team[w][1][j] = l;
+    }
+    __syncthreads();
+    float mu[4], m_all = NEG_INF, l_all = 0.f, out[NQ];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+        mu[u] = team[u][0][j];
+        m_all = fmaxf(m_all, mu[u]);
+    }
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) out[i] = 0.f;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+        const float share = mu[u] != NEG_INF ? fast_exp2(mu[u] - m_all) : 0.f;
+        l_all = fmaf(share, team[u][1][j], l_all);
+        const float *const his = reinterpret_cast<const float *>(all_tiles + u * 2 * TB);
+#pragma unroll
+        for (int i = 0; i < NQ / 4; ++i) {
+            const f32x4 v = *reinterpret_cast<const f32x4 *>(his + ((w * (NQ / 4) + i) * 64 + lane) * 4);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) out[4 * i + e] = fmaf(share, v[e], out[4 * i + e]);
+        }
+    }
+    if (s.part == 0 && threadIdx.x == 0) p.info[s.group] = int2{s.seg, s.parts};
+    const bool whole = s.parts == 1 && p.prefix_tiles == 0;  // nothing to join with
+    if (row < rows) {
+        if (!whole || WEIGH) {
+            if (w == 0 && hh == 0) {
+                p.stats[(int64_t)s.seg * 64 + j] = m_all;
+                p.stats[(int64_t)s.seg * 64 + 32 + j] = l_all;
+            }
+        }
+        const float inv = l_all > 0.f ? 1.0f / l_all : 0.f;
+        uint16_t *const to = p.O + rb * p.os.b + (s.hk * p.G + g) * p.os.h + t * p.os.s;
+        float *const part = p.parts + ((int64_t)s.seg * 32 + j) * D;
+#pragma unroll
+        for (int i = 0; i < NQ; i += 4) {
+            const int r = NQ * w + i, col = 32 * (r >> 4) + 8 * ((r & 15) >> 2) + 4 * hh;
+            if (whole) {
+                if (col < p.d) store4<BF16 ? SMHA_BF16 : SMHA_F16>(to, col, out[i] * inv, out[i + 1] * inv, out[i + 2] * inv, out[i + 3] * inv);
+            } else {
+                *reinterpret_cast<f32x4 *>(part + col) = f32x4{out[i], out[i + 1], out[i + 2], out[i + 3]};
+            }
+        }
+    }
+}
+
+// The segments of one row (those of the prefix, then its own): their common reference and sum.
+struct RowParts {
+    int first[2], count[2], row[2];  // segments, and the row in them: prefix, own
+};
+__device__ __forceinline__ RowParts row_parts(const CacheParams &p, int b, int hk, int in_b, bool own) {
+    RowParts r{{0, 0}, {0, 0}, {0, 0}};
+    if (p.prefix_tiles) {
+        const int row = b * p.G * p.T + in_b;
+        const int2 i = p.info[hk * p.prefix_tiles + row / 32];
+        r.first[0] = i.x;
+        r.count[0] = i.y;
+        r.row[0] = row & 31;
+    }
+    if (own) {
+        const int2 i = p.info[p.Hkv * p.prefix_tiles + (b * p.Hkv + hk) * p.own_tiles + in_b / 32];
+        r.first[1] = i.x;
+        r.count[1] = i.y;
+        r.row[1] = in_b & 31;
+    }
+    return r;
+}
+
+// The first workgroups join rows, one a workgroup; the others add to the accounts of 1024 keys of a key head.
+template <int D, bool BF16>
+__global__ void __launch_bounds__(256) smha_cache_join(const CacheParams p, int row_groups, int key_groups) {
+    __shared__ float lds_ml[2][4];
+    __shared__ float lds_o[4][D];
+    __shared__ float lds_lse[256];
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, GT = p.G * p.T;
+    const float NEG_INF = -__builtin_inff();
+    if ((int)blockIdx.x < row_groups) {
+        const int id = blockIdx.x, b = id / (p.Hkv * GT), hk = id / GT - b * p.Hkv, in_b = id % GT, g = in_b / p.T, t = in_b - g * p.T;
+        const int len = min(max(p.lengths[b], 0), p.Sk);
+        uint16_t *const to = p.O + b * p.os.b + (hk * p.G + g) * p.os.h + t * p.os.s;
+        if (len - p.T + t < 0) {  // no such query
+            for (int c = threadIdx.x; c < p.d; c += 256) to[c] = 0;
+            return;
+        }
+        const RowParts r = row_parts(p, b, hk, in_b, len > 0);
+        if (!p.prefix_tiles && r.count[1] == 1) return;  // written whole
+        const int n = r.count[0] + r.count[1];
+        auto segment = [&](int i) __attribute__((always_inline)) { return i < r.count[0] ? r.first[0] + i : r.first[1] + i - r.count[0]; };
+        auto place = [&](int i) __attribute__((always_inline)) { return i < r.count[0] ? r.row[0] : r.row[1]; };
+        float m = NEG_INF;
+        for (int i = threadIdx.x; i < n; i += 256) m = fmaxf(m, p.stats[(int64_t)segment(i) * 64 + place(i)]);
+#pragma unroll
+        for (int x = 32; x > 0; x >>= 1) m = fmaxf(m, __shfl_xor(m, x));
+        if (lane == 0) lds_ml[0][w] = m;
+        __syncthreads();
+        m = fmaxf(fmaxf(lds_ml[0][0], lds_ml[0][1]), fmaxf(lds_ml[0][2], lds_ml[0][3]));
+        // wave w takes segments w, w + 4, ...; a lane D / 64 columns
+        float sum = 0.f, acc[D / 64];
+#pragma unroll
+        for (int e = 0; e < D / 64; ++e) acc[e] = 0.f;
+#pragma unroll 4
+        for (int i = w; i < n; i += 4) {
+            const int64_t at = segment(i);
+            const float ref = p.stats[at * 64 + place(i)], share = ref != NEG_INF ? fast_exp2(ref - m) : 0.f;
+            sum = fmaf(share, p.stats[at * 64 + 32 + place(i)], sum);
+#pragma unroll
+            for (int e = 0; e < D / 64; ++e) acc[e] = fmaf(share, p.parts[(at * 32 + place(i)) * D + lane + 64 * e], acc[e]);
+        }
+        if (lane == 0) lds_ml[1][w] = sum;
+#pragma unroll
+        for (int e = 0; e < D / 64; ++e) lds_o[w][lane + 64 * e] = acc[e];
+        __syncthreads();
+        const float l = lds_ml[1][0] + lds_ml[1][1] + lds_ml[1][2] + lds_ml[1][3], inv = l > 0.f ? 1.0f / l : 0.f;
+        for (int c = threadIdx.x; c < p.d; c += 256) {
+            const float v = (lds_o[0][c] + lds_o[1][c] + lds_o[2][c] + lds_o[3][c]) * inv;
+            to[c] = (uint16_t)pack2<BF16>(v, 0.f);
+        }
+        return;
+    }
+    const int id = (int)blockIdx.x - row_groups, bh = id / key_groups, b = bh / p.Hkv, hk = bh - b * p.Hkv;
+    const OwnKeys own = own_keys(p.lengths[b], p.T, p.Sk, p.window, p.n_sink);
+    const int first = (id - bh * key_groups) * 1024 + (int)threadIdx.x * 4;  // four keys a thread
+    if (first - (int)threadIdx.x * 4 >= own.len) return;
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+    float *const account = p.weights + b * p.w_b + hk * p.w_h;
+    // (of a row of 32 keys all were scored or none)
+    const bool scored = first < own.len && (first < 32 * own.head || first >= 32 * own.t0);
+    for (int r0 = 0; r0 < GT; r0 += 256) {
+        const int nr = min(256, GT - r0);
+        __syncthreads();
+        if ((int)threadIdx.x < nr) {
+            const RowParts r = row_parts(p, b, hk, r0 + threadIdx.x, true);
+            float m = NEG_INF, l = 0.f;
+            for (int k = 0; k < 2; ++k)
+                for (int i = 0; i < r.count[k]; ++i) m = fmaxf(m, p.stats[(int64_t)(r.first[k] + i) * 64 + r.row[k]]);
+            for (int k = 0; k < 2; ++k)
+                for (int i = 0; i < r.count[k]; ++i) {
+                    const int64_t at = (int64_t)(r.first[k] + i) * 64 + r.row[k];
+                    if (p.stats[at] != NEG_INF) l = fmaf(fast_exp2(p.stats[at] - m), p.stats[at + 32], l);
+                }
+            lds_lse[threadIdx.x] = l > 0.f ? m + __builtin_amdgcn_logf(l) : __builtin_inff();  // (inf: a row without keys adds nothing)
+        }
+        __syncthreads();
+        if (scored) {
+            const float *const row = p.scores + ((int64_t)bh * GT + r0) * p.score_pitch + first;
+            for (int r = 0; r < nr; ++r) {
+                const f32x4 v = *reinterpret_cast<const f32x4 *>(row + (int64_t)r * p.score_pitch);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum[e] += fast_exp2(v[e] - lds_lse[r]);
+            }
+        }
+    }
+    if (scored)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (first + e < own.len) account[first + e] += sum[e];
+}
+
+// ---------------------------------------------------------------------------------------
+// Eviction
+// ---------------------------------------------------------------------------------------
+struct EvictParams {
+    uint16_t *K, *V;
+    Strides ks, vs;
+    const float *w;
+    const int32_t *pos, *lengths;
+    float *w_out;
+    int32_t *pos_out, *len_out;
+    int64_t w_b, w_h, p_b, p_h, wo_b, wo_h, po_b, po_h;
+    int B, Hkv, Sk, d, budget, recent, moves;  // moves: most that a head makes
+    int32_t *lists;                             // [B Hkv][1 + 2 moves]: count, where to, where from
+};
+
+// An order of 32-bit floats as unsigned numbers, NaN with the lowest, -0 with +0.
+__device__ __forceinline__ uint32_t ordered(float x) {
+    if (!(x == x)) return 0x007FFFFFu;  // -inf's
+    const uint32_t u = __builtin_bit_cast(uint32_t, x + 0.0f);
+    return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+
+// One workgroup of 16 waves a key head.  Wave w holds the keys of slots (w KPT + i) 64 + lane as unsigned numbers that order them, so
+// that a lane's and a register's order is the slots' order.  The budget-th largest is found two bits at a time by counting; of
+// those that equal it the first slots stay.  What stays past the new end goes, in order, where keys before it left.
+template <int KPT>
+__global__ void __launch_bounds__(1024) smha_cache_select(const EvictParams p) {
+    __shared__ int counts[2][16][3];
+    __shared__ int totals[16][3];
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int bh = blockIdx.x, b = bh / p.Hkv, hk = bh - b * p.Hkv;
+    const int len = min(max(p.lengths[b], 0), p.Sk), end = min(len, p.budget);
+    const float *const W = p.w + b * p.w_b + hk * p.w_h;
+    const int32_t *const P = p.pos + b * p.p_b + hk * p.p_h;
+    float *const Wo = p.w_out + b * p.wo_b + hk * p.wo_h;
+    int32_t *const Po = p.pos_out + b * p.po_b + hk * p.po_h;
+    int32_t *const list = p.lists + (int64_t)bh * (1 + 2 * (int64_t)p.moves);
+    const bool copies = W != Wo || P != Po;
+    if (len <= p.budget) {
+        if (threadIdx.x == 0) list[0] = 0;
+        if (copies)
+            for (int i = threadIdx.x; i < len; i += 1024) {
+                Wo[i] = W[i];
+                Po[i] = P[i];
+            }
+        for (int i = len + threadIdx.x; i < p.Sk; i += 1024) {
+            Wo[i] = 0.f;
+            Po[i] = -1;
+        }
+        return;
+    }
+    // the youngest
+    int newest = -1;
+    bool any = false;
+    for (int i = threadIdx.x; i < len; i += 1024) {
+        const int x = P[i];
+        newest = any ? max(newest, x) : x;
+        any = true;
+    }
+    if (!any) newest = INT32_MIN;
+#pragma unroll
+    for (int m = 32; m > 0; m >>= 1) newest = max(newest, __shfl_xor(newest, m));
+    if (lane == 0) counts[0][w][0] = newest;
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < 16; ++u) newest = max(newest, counts[0][u][0]);
+    __syncthreads();
+    const int64_t young = (int64_t)newest - p.recent;  // positions past this stay, whatever their account
+    const int per_wave = ((len + 1023) / 1024) * 64;   // slots of a wave
+    const int base = w * per_wave + lane, n = min(KPT ? KPT : INT32_MAX, per_wave / 64);
+    auto key_at = [&](int slot) __attribute__((always_inline)) -> uint32_t {
+        if (slot >= len) return 0u;  // (below every live key's)
+        return (int64_t)P[slot] > young ? 0xFF800000u : ordered(W[slot]);
+    };
+    uint32_t held[KPT ? KPT : 1];
+    if constexpr (KPT > 0) {
+#pragma unroll
+        for (int i = 0; i < KPT; ++i) held[i] = i < n ? key_at(base + 64 * i) : 0u;
+    }
+    auto key_of = [&](int i) __attribute__((always_inline)) -> uint32_t {
+        if constexpr (KPT > 0) return held[i];
+        else return key_at(base + 64 * i);
+    };
+    auto each = [&](auto &&f) __attribute__((always_inline)) {
+        if constexpr (KPT > 0) {
+#pragma unroll
+            for (int i = 0; i < KPT; ++i)
+                if (i < n) f(i, key_of(i));
+        } else {
+            for (int i = 0; i < n; ++i) f(i, key_of(i));
+        }
+    };
+    // the largest x that `end` keys or more reach
+    uint32_t least = 0;
+    for (int shift = 30, turn = 0; shift >= 0; shift -= 2, turn ^= 1) {
+        int c1 = 0, c2 = 0, c3 = 0;
+        const uint32_t t1 = least | (1u << shift), t2 = least | (2u << shift), t3 = least | (3u << shift);
+        each([&](int, uint32_t k) __attribute__((always_inline)) {
+            c1 += __builtin_popcountll(__builtin_amdgcn_ballot_w64(k >= t1));
+            c2 += __builtin_popcountll(__builtin_amdgcn_ballot_w64(k >= t2));
+            c3 += __builtin_popcountll(__builtin_amdgcn_ballot_w64(k >= t3));
+        });
+        if (lane == 0) {
+            counts[turn][w][0] = c1;
+            counts[turn][w][1] = c2;
+            counts[turn][w][2] = c3;
+        }
+        __syncthreads();
+        c1 = c2 = c3 = 0;
+#pragma unroll
+        for (int u = 0; u < 16; ++u) {
+            c1 += counts[turn][u][0];
+            c2 += counts[turn][u][1];
+            c3 += counts[turn][u][2];
+        }
+        least = c3 >= end ? t3 : c2 >= end ? t2 : c1 >= end ? t1 : least;
+    }
+    // per wave: keys over the least, keys at it; then who stays
+    int over = 0, equal = 0;
+    each([&](int, uint32_t k) __attribute__((always_inline)) {
+        over += __builtin_popcountll(__builtin_amdgcn_ballot_w64(k > least));
+        equal += __builtin_popcountll(__builtin_amdgcn_ballot_w64(k == least));
+    });
+    if (lane == 0) {
+        totals[w][0] = over;
+        totals[w][1] = equal;
+    }
+    __syncthreads();
+    int all_over = 0, equal_before = 0;
+#pragma unroll
+    for (int u = 0; u < 16; ++u) {
+        all_over += totals[u][0];
+        if (u < w) equal_before += totals[u][1];
+    }
+    const int equal_stay = end - all_over;  // the first so many of those at the least
+    const uint64_t below = (1ull << lane) - 1;
+    // freed slots before the end, kept slots from it on, per wave
+    int freed = 0, kept = 0, equal_at = equal_before;
+    auto stays = [&](uint32_t k, int &eq) __attribute__((always_inline)) {
+        const uint64_t same = __builtin_amdgcn_ballot_w64(k == least);
+        const bool yes = k > least || (k == least && eq + __builtin_popcountll(same & below) < equal_stay);
+        eq += __builtin_popcountll(same);
+        return yes;
+    };
+    each([&](int i, uint32_t k) __attribute__((always_inline)) {
+        const int slot = base + 64 * i;
+        const bool yes = stays(k, equal_at) && slot < len;
+        freed += __builtin_popcountll(__builtin_amdgcn_ballot_w64(!yes && slot < end));
+        kept += __builtin_popcountll(__builtin_amdgcn_ballot_w64(yes && slot >= end));
+    });
+    __syncthreads();
+    if (lane == 0) {
+        totals[w][0] = freed;
+        totals[w][1] = kept;
+    }
+    __syncthreads();
+    int to = 0, from = 0, moves = 0;
+#pragma unroll
+    for (int u = 0; u < 16; ++u) {
+        if (u < w) to += totals[u][0], from += totals[u][1];
+        moves += totals[u][0];
+    }
+    equal_at = equal_before;
+    each([&](int i, uint32_t k) __attribute__((always_inline)) {
+        const int slot = base + 64 * i;
+        const bool yes = stays(k, equal_at) && slot < len, out = !yes && slot < end, in = yes && slot >= end;
+        const uint64_t outs = __builtin_amdgcn_ballot_w64(out), ins = __builtin_amdgcn_ballot_w64(in);
+        if (out) list[1 + to + __builtin_popcountll(outs & below)] = slot;
+        if (in) list[1 + p.moves + from + __builtin_popcountll(ins & below)] = slot;
+        to += __builtin_popcountll(outs);
+        from += __builtin_popcountll(ins);
+        if (copies && yes && slot < end) {
+            Wo[slot] = W[slot];
+            Po[slot] = P[slot];
+        }
+    });
+    if (threadIdx.x == 0) list[0] = moves;
+    __syncthreads();
+    for (int i = threadIdx.x; i < moves; i += 1024) {
+        const int to_slot = list[1 + i], from_slot = list[1 + p.moves + i];
+        Wo[to_slot] = W[from_slot];
+        Po[to_slot] = P[from_slot];
+    }
+    __syncthreads();
+    for (int i = end + threadIdx.x; i < p.Sk; i += 1024) {
+        Wo[i] = 0.f;
+        Po[i] = -1;
+    }
+}
+
+// K and V rows along the lists: what is read lies past the new end, what is written before it.
+__global__ void __launch_bounds__(256) smha_cache_move(const EvictParams p) {
+    const int bh = blockIdx.y, b = bh / p.Hkv, hk = bh - b * p.Hkv;
+    if (blockIdx.x == 0 && hk == 0 && threadIdx.x == 0) p.len_out[b] = min(min(max(p.lengths[b], 0), p.Sk), p.budget);
+    const int32_t *const list = p.lists + (int64_t)bh * (1 + 2 * (int64_t)p.moves);
+    const int n = list[0], lane = threadIdx.x & 15;
+    uint16_t *const K = p.K + b * p.ks.b + hk * p.ks.h, *const V = p.V + b * p.vs.b + hk * p.vs.h;
+    for (int i = blockIdx.x * 16 + (threadIdx.x >> 4); i < n; i += gridDim.x * 16) {
+        const int64_t to = list[1 + i], from = list[1 + p.moves + i];
+        if (8 * lane < p.d) {
+            const u32x4 k = *reinterpret_cast<const u32x4 *>(K + from * p.ks.s + 8 * lane), v = *reinterpret_cast<const u32x4 *>(V + from * p.vs.s + 8 * lane);
+            *reinterpret_cast<u32x4 *>(K + to * p.ks.s + 8 * lane) = k;
+            *reinterpret_cast<u32x4 *>(V + to * p.vs.s + 8 * lane) = v;
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------
+// Launches
+// ---------------------------------------------------------------------------------------
+static bool cache_strides_fit(const int64_t *s, int64_t rows, int d) {
+    if (!s) return (rows + 64) * d * 2 < ((int64_t)1 << 31);
+    return s[0] % 8 == 0 && s[1] % 8 == 0 && s[2] % 8 == 0 && s[0] >= 0 && s[1] >= 0 && s[2] >= d && ((rows + 64) * s[2] + d) * 2 < ((int64_t)1 << 31);
+}
+static Strides cache_strides(const int64_t *s, int64_t heads, int64_t rows, int d) {
+    return s ? Strides{s[0], s[1], s[2]} : Strides{heads * rows * d, rows * d, d};
+}
+
+struct CacheLayout {
+    size_t info, stats, parts, scores, total;
+};
+static size_t up(size_t n) { return (n + 255) & ~(size_t)255; }
+
+// Sizes and the workspace's layout; what both entry points refuse.
+static smha_status_t cache_params(CacheParams &cp, CacheLayout &at, int B, int H, int Hkv, int T, int Sk, int P, int d, smha_dtype_t dtype, int window, int n_sink,
+                                  bool weigh) {
+    if (B < 1 || H < 1 || Hkv < 1 || T < 1 || Sk < 1 || P < 0 || window < 0 || n_sink < 0) return SMHA_ERR_INVALID_ARG;
+    if (H % Hkv) return SMHA_ERR_SHAPE;
+    if (dtype != SMHA_F16 && dtype != SMHA_BF16) return SMHA_ERR_UNSUPPORTED;
+    if (d < 8 || d > 128 || d % 8) return SMHA_ERR_UNSUPPORTED;
+    if (P > 0 && window > 0) return SMHA_ERR_UNSUPPORTED;  // (the window would have to run back into the prefix)
+    cp.B = B; cp.H = H; cp.Hkv = Hkv; cp.G = H / Hkv; cp.T = T; cp.Sk = Sk; cp.P = P; cp.d = d;
+    cp.window = window == 0 || window > Sk ? Sk : window;
+    cp.n_sink = std::min(n_sink, Sk);
+    const int64_t rows = (int64_t)cp.G * T, own_tiles = (rows + 31) / 32, prefix_tiles = P ? ((int64_t)B * rows + 31) / 32 : 0;
+    const int64_t groups = (int64_t)Hkv * (prefix_tiles + B * own_tiles);
+    // (tiles and rows are counted in 32 bits)
+    if ((int64_t)B * H * T > (1 << 24) || groups * (std::max(Sk, P) / 32 + 8) > (1 << 30)) return SMHA_ERR_UNSUPPORTED;
+    cp.own_tiles = (int)own_tiles;
+    cp.prefix_tiles = (int)prefix_tiles;
+    const int D = d <= 64 ? 64 : 128;
+    cp.slots = 256 * (D == 64 ? 4 : 2);  // what the chip holds at once: 32 or 64 KB of LDS a workgroup
+    // no more segments than that and one a group, and none shorter than four tiles unless it is a group
+    const int64_t own_most = (std::min<int64_t>(Sk, (int64_t)cp.window + cp.n_sink + T) / 32 + 3 + 3) / 4;
+    const int64_t most = Hkv * (prefix_tiles * ((P / 32 + 1 + 3) / 4) + B * own_tiles * own_most);
+    cp.segs = (int)std::min<int64_t>(cp.slots + groups, most);
+    cp.score_pitch = (Sk + 31) / 32 * 32;
+    at.info = 0;
+    at.stats = up(groups * sizeof(int2));
+    at.parts = at.stats + up((size_t)cp.segs * 64 * 4);
+    at.scores = at.parts + up((size_t)cp.segs * 32 * D * 4);
+    at.total = at.scores + (weigh ? (size_t)B * Hkv * rows * cp.score_pitch * 4 : 0);
+    return SMHA_OK;
+}
+
+template <int D, bool BF16> static hipError_t launch_cache(const CacheParams &cp, hipStream_t stream) {
+    const dim3 grid(8 * ((cp.segs + 7) / 8));
+    if (cp.weights) hipLaunchKernelGGL((smha_cache_part<D, BF16, true>), grid, dim3(256), 0, stream, cp);
+    else hipLaunchKernelGGL((smha_cache_part<D, BF16, false>), grid, dim3(256), 0, stream, cp);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    const int rows = cp.B * cp.H * cp.T, keys = cp.weights ? (cp.Sk + 1023) / 1024 : 0;
+    hipLaunchKernelGGL((smha_cache_join<D, BF16>), dim3((unsigned)(rows + cp.B * cp.Hkv * keys)), dim3(256), 0, stream, cp, rows, keys);
+    return hipGetLastError();
+}
+
+}  // namespace smha
+
+using namespace smha;
+
+extern "C" smha_status_t smha_cache_workspace(int B, int H, int Hkv, int T, int Sk, int P, int d, int window, int n_sink, int weigh, size_t *need) {
+    if (!need) return SMHA_ERR_INVALID_ARG;
+    CacheParams cp{};
+    CacheLayout at{};
+    const smha_status_t st = cache_params(cp, at, B, H, Hkv, T, Sk, P, d, SMHA_F16, window, n_sink, weigh != 0);
+    if (st != SMHA_OK) return st;
+    *need = at.total;
+    return SMHA_OK;
+}
+
+extern "C" smha_status_t smha_cache_forward(const void *Q, const void *K, const void *V, const void *PK, const void *PV, void *O, float *weights,
+                                            const int32_t *lengths, int B, int H, int Hkv, int T, int Sk, int P, int d, smha_dtype_t dtype,
+                                            const int64_t q_strides[3], const int64_t k_strides[3], const int64_t v_strides[3], const int64_t pk_strides[2],
+                                            const int64_t pv_strides[2], const int64_t o_strides[3], const int64_t w_strides[2], int window, int n_sink, float scale,
+                                            void *workspace, size_t workspace_bytes, void *hip_stream) {
+    if (!Q || !K || !V || !O || !lengths || !workspace || (P > 0 && (!PK || !PV))) return SMHA_ERR_INVALID_ARG;
+    CacheParams cp{};
+    CacheLayout at{};
+    const smha_status_t st = cache_params(cp, at, B, H, Hkv, T, Sk, P, d, dtype, window, n_sink, weights != nullptr);
+    if (st != SMHA_OK) return st;
+    if (workspace_bytes < at.total) return SMHA_ERR_INVALID_ARG;
+    if (((uintptr_t)Q | (uintptr_t)K | (uintptr_t)V | (uintptr_t)O | (uintptr_t)workspace | (P ? (uintptr_t)PK | (uintptr_t)PV : 0)) & 15) return SMHA_ERR_UNSUPPORTED;
+    if (!cache_strides_fit(q_strides, T, d) || !cache_strides_fit(k_strides, Sk, d) || !cache_strides_fit(v_strides, Sk, d) || !cache_strides_fit(o_strides, T, d))
+        return SMHA_ERR_UNSUPPORTED;
+    if (P) {
+        for (const int64_t *s : {pk_strides, pv_strides}) {
+            const int64_t three[3] = {0, s ? s[0] : (int64_t)P * d, s ? s[1] : d};
+            if (!cache_strides_fit(three, P, d)) return SMHA_ERR_UNSUPPORTED;
+        }
+    }
+    cp.Q = (const uint16_t *)Q; cp.K = (const uint16_t *)K; cp.V = (const uint16_t *)V; cp.O = (uint16_t *)O;
+    cp.PK = (const uint16_t *)PK; cp.PV = (const uint16_t *)PV;
+    cp.weights = weights; cp.lengths = lengths;
+    cp.qs = cache_strides(q_strides, H, T, d); cp.ks = cache_strides(k_strides, Hkv, Sk, d); cp.vs = cache_strides(v_strides, Hkv, Sk, d);
+    cp.os = cache_strides(o_strides, H, T, d);
+    cp.pk_h = pk_strides ? pk_strides[0] : (int64_t)P * d; cp.pk_s = pk_strides ? pk_strides[1] : d;
+    cp.pv_h = pv_strides ? pv_strides[0] : (int64_t)P * d; cp.pv_s = pv_strides ? pv_strides[1] : d;
+    cp.w_b = w_strides ? w_strides[0] : (int64_t)Hkv * Sk; cp.w_h = w_strides ? w_strides[1] : Sk;
+    cp.c = (scale > 0.f ? scale : 1.0f / std::sqrt((float)d)) * 1.4426950408889634f;
+    char *const ws = (char *)workspace;
+    cp.info = (int2 *)(ws + at.info); cp.stats = (float *)(ws + at.stats); cp.parts = (float *)(ws + at.parts); cp.scores = (float *)(ws + at.scores);
+    const hipStream_t stream = (hipStream_t)hip_stream;
+    const bool bf16 = dtype == SMHA_BF16;
+    const hipError_t e = d <= 64 ? (bf16 ? launch_cache<64, true>(cp, stream) : launch_cache<64, false>(cp, stream))
+                                 : (bf16 ? launch_cache<128, true>(cp, stream) : launch_cache<128, false>(cp, stream));
+    return e == hipSuccess ? SMHA_OK : SMHA_ERR_HIP;
+}
+
+static smha_status_t evict_sizes(int B, int Hkv, int Sk, int d, int budget, int recent, size_t *need) {
+    if (B < 1 || Hkv < 1 || Sk < 1 || budget < 1 || recent < 0) return SMHA_ERR_INVALID_ARG;
+    if (d < 8 || d > 128 || d % 8 || (int64_t)B * Hkv > 65535 || Sk > (1 << 28)) return SMHA_ERR_UNSUPPORTED;
+    const int64_t moves = std::max(0, std::min(budget, Sk - budget));
+    *need = (size_t)((int64_t)B * Hkv * (1 + 2 * moves) * 4);
+    return SMHA_OK;
+}
+
+extern "C" smha_status_t smha_cache_evict_workspace(int B, int Hkv, int Sk, int d, int budget, int recent, size_t *need) {
+    if (!need) return SMHA_ERR_INVALID_ARG;
+    size_t n = 0;
+    const smha_status_t st = evict_sizes(B, Hkv, Sk, d, budget, recent, &n);
+    if (st == SMHA_OK) *need = n;
+    return st;
+}
+
+extern "C" smha_status_t smha_cache_evict(void *K, void *V, const float *weights, const int32_t *positions, const int32_t *lengths, float *weights_out,
+                                          int32_t *positions_out, int32_t *lengths_out, int B, int Hkv, int Sk, int d, int budget, int recent,
+                                          const int64_t k_strides[3], const int64_t v_strides[3], void *workspace, size_t workspace_bytes, void *hip_stream) {
+    if (!K || !V || !weights || !positions || !lengths || !weights_out || !positions_out || !lengths_out || !workspace) return SMHA_ERR_INVALID_ARG;
+    size_t need = 0;
+    const smha_status_t st = evict_sizes(B, Hkv, Sk, d, budget, recent, &need);
+    if (st != SMHA_OK) return st;
+    if (workspace_bytes < need) return SMHA_ERR_INVALID_ARG;
+    if (((uintptr_t)K | (uintptr_t)V) & 15 || (uintptr_t)workspace & 3) return SMHA_ERR_UNSUPPORTED;
+    for (const int64_t *s : {k_strides, v_strides})
+        if (s && (s[0] % 8 || s[1] % 8 || s[2] % 8 || s[0] < 0 || s[1] < 0 || s[2] < d)) return SMHA_ERR_UNSUPPORTED;
+    EvictParams ep{};
+    ep.K = (uint16_t *)K; ep.V = (uint16_t *)V;
+    ep.ks = cache_strides(k_strides, Hkv, Sk, d); ep.vs = cache_strides(v_strides, Hkv, Sk, d);
+    ep.w = weights; ep.pos = positions; ep.lengths = lengths; ep.w_out = weights_out; ep.pos_out = positions_out; ep.len_out = lengths_out;
+    ep.w_h = ep.p_h = ep.wo_h = ep.po_h = Sk;
+    ep.w_b = ep.p_b = ep.wo_b = ep.po_b = (int64_t)Hkv * Sk;
+    ep.B = B; ep.Hkv = Hkv; ep.Sk = Sk; ep.d = d; ep.budget = budget; ep.recent = recent;
+    ep.moves = std::max(0, std::min(budget, Sk - budget));
+    ep.lists = (int32_t *)workspace;
+    const hipStream_t stream = (hipStream_t)hip_stream;
+    const dim3 grid(B * Hkv);
+    if (Sk <= 4096) hipLaunchKernelGGL(smha_cache_select<4>, grid, dim3(1024), 0, stream, ep);
+    else if (Sk <= 8192) hipLaunchKernelGGL(smha_cache_select<8>, grid, dim3(1024), 0, stream, ep);
+    else if (Sk <= 16384) hipLaunchKernelGGL(smha_cache_select<16>, grid, dim3(1024), 0, stream, ep);
+    else if (Sk <= 32768) hipLaunchKernelGGL(smha_cache_select<32>, grid, dim3(1024), 0, stream, ep);
+    else hipLaunchKernelGGL(smha_cache_select<0>, grid, dim3(1024), 0, stream, ep);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return SMHA_ERR_HIP;
+    hipLaunchKernelGGL(smha_cache_move, dim3((unsigned)std::max(1, std::min(64, (ep.moves + 63) / 64)), B * Hkv), dim3(256), 0, stream, ep);
+    e = hipGetLastError();
+    return e == hipSuccess ? SMHA_OK : SMHA_ERR_HIP;
+}

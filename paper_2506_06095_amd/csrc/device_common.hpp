@@ -153,4 +153,28 @@ __device__ __forceinline__ void store4(void *O, int64_t elem_off, float a, float
     }
 }
 
+// --- for kernels whose masks are arithmetic on positions
+constexpr uint32_t kNoChunk = 0x80000000u;  // a column that the head does not have: past every buffer, with any row's offset added
+constexpr uint32_t kPast = 0x7FFFFF00u;     // a row that is not to be read
+
+// Both of a tile's reading orders: 16 rows at one chunk (16-byte reads), and 4 rows x 4 chunks (transposing reads).  The two low bits
+// of the row choose the aligned group of four chunks, the next two the place in it.
+template <int D> __device__ __forceinline__ int swz_both(int row) {
+    if constexpr (D == 128) return ((row & 3) << 2) | ((row >> 2) & 3);
+    else return ((row & 2) << 1) | ((row >> 2) & 3);
+}
+
+// bits 0 .. n - 1
+__device__ __forceinline__ uint64_t low_bits(int n) { return n <= 0 ? 0 : n >= 64 ? ~0ull : (1ull << n) - 1; }
+__device__ __forceinline__ uint32_t low_bits32(int n) { return n <= 0 ? 0 : n >= 32 ? ~0u : (1u << n) - 1; }
+typedef uint32_t u32x16 __attribute__((ext_vector_type(16)));
+// all ones where accumulator r of the lane (8 (r / 4) + r % 4 of the lane's half) has its bit set
+__device__ __forceinline__ u32x16 keep_of(uint32_t bits) {
+    u32x16 keep;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) keep[r] = (uint32_t)__builtin_amdgcn_sbfe((int)bits, 8 * (r / 4) + (r % 4), 1);
+    return keep;
+}
+__device__ __forceinline__ f32x16 zeros16() { return f32x16{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}; }
+
 }  // namespace smha

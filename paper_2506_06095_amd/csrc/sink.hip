@@ -42,16 +42,6 @@ struct SinkParams {
     int n_tiles, n_sink_tiles, chunk, cut_sink, cut_rest;  // key tiles, those with sinks; steps of a part; parts at most
 };
 
-constexpr uint32_t kNoChunk = 0x80000000u;  // a column that the head does not have: past every buffer, with any row's offset added
-constexpr uint32_t kPast = 0x7FFFFF00u;     // a row that is not to be read
-
-// Both of a tile's reading orders: 16 rows at one chunk (16-byte reads), and 4 rows x 4 chunks (transposing reads).  The two low bits
-// of the row choose the aligned group of four chunks, the next two the place in it.
-template <int D> __device__ __forceinline__ int swz(int row) {
-    if constexpr (D == 128) return ((row & 3) << 2) | ((row >> 2) & 3);
-    else return ((row & 2) << 1) | ((row >> 2) & 3);
-}
-
 struct Sequence {
     int len, off;  // keys, first query's position
     int qa, qb;    // queries qa .. qb - 1 exist
@@ -65,9 +55,6 @@ __device__ __forceinline__ Sequence sequence(const SinkParams &p, int b) {
     return s;
 }
 
-// bits 0 .. n - 1
-__device__ __forceinline__ uint64_t low_bits(int n) { return n <= 0 ? 0 : n >= 64 ? ~0ull : (1ull << n) - 1; }
-__device__ __forceinline__ uint32_t low_bits32(int n) { return n <= 0 ? 0 : n >= 32 ? ~0u : (1u << n) - 1; }
 // the keys k0 .. k0 + 63 that a query at position pos sees
 __device__ __forceinline__ uint64_t seen_keys(int pos, int k0, int window, int n_sink) {
     return low_bits(pos - k0 + 1) & (~low_bits(pos - window + 1 - k0) | low_bits(n_sink - k0));
@@ -80,16 +67,6 @@ __device__ __forceinline__ bool all_seen(int p0, int p1, int k0, int k1, int win
     return k1 <= p0 && (p1 - k0 < window || k1 < n_sink);
 }
 
-typedef uint32_t u32x16 __attribute__((ext_vector_type(16)));
-// all ones where accumulator r of the lane (8 (r / 4) + r % 4 of the lane's half) has its bit set
-__device__ __forceinline__ u32x16 keep_of(uint32_t bits) {
-    u32x16 keep;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) keep[r] = (uint32_t)__builtin_amdgcn_sbfe((int)bits, 8 * (r / 4) + (r % 4), 1);
-    return keep;
-}
-__device__ __forceinline__ f32x16 zeros16() { return f32x16{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}; }
-
 // A tile of 64 rows into LDS by a workgroup's four waves: wave w brings the 1 KiB blocks w, w + 4, ...
 template <int D> struct TileLoad {
     static constexpr int CPR = D / 8, LPW = CPR / 4, RSTEP = 4 * 64 / CPR;  // chunks a row, loads a wave, rows between two of its loads
@@ -97,7 +74,7 @@ template <int D> struct TileLoad {
     int row;
     __device__ __forceinline__ TileLoad(int w, int lane, int row_bytes, int d) {
         row = (w * 64 + lane) / CPR;
-        const int c = (lane % CPR) ^ swz<D>(row);
+        const int c = (lane % CPR) ^ swz_both<D>(row);
         go = c < (d >> 3) ? (uint32_t)(row * row_bytes + c * 16) : kNoChunk;
     }
     // rows r0 .. r0 + 63; those in [gap0, gap1) read as zeros, as do those past the buffer
@@ -130,12 +107,12 @@ __device__ __forceinline__ void store_rows(const f32x16 (&acc)[D / 32], float fa
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
             const u32x2 v = {pack2<BF16>(acc[dt][4 * g] * factor, acc[dt][4 * g + 1] * factor), pack2<BF16>(acc[dt][4 * g + 2] * factor, acc[dt][4 * g + 3] * factor)};
-            *reinterpret_cast<u32x2 *>(slab + j * D * 2 + (((4 * dt + g) ^ swz<D>(j)) * 16) + hh * 8) = v;
+            *reinterpret_cast<u32x2 *>(slab + j * D * 2 + (((4 * dt + g) ^ swz_both<D>(j)) * 16) + hh * 8) = v;
         }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 #pragma unroll
     for (int i = 0; i < CPR / 2; ++i) {
-        const int row = (i * 64 + lane) / CPR, c = (lane % CPR) ^ swz<D>(row);
+        const int row = (i * 64 + lane) / CPR, c = (lane % CPR) ^ swz_both<D>(row);
         const u32x4 v = *reinterpret_cast<const u32x4 *>(slab + i * 1024 + lane * 16);
         if (row0 + row < rows && c < (d >> 3)) *reinterpret_cast<u32x4 *>(base + (row0 + row) * pitch + c * 8) = v;
     }
@@ -203,9 +180,9 @@ __global__ void __launch_bounds__(256, D == 64 ? 4 : 2) smha_sink_fwd(const Sink
     u32x4 qf[NS];
     load_operand<D>(qf, p.Q + b * p.qs.b + h * p.qs.h, p.qs.s, qw, s.qa, s.qb, p.d, lane);
 
-    const int rd = j * D * 2 + ((hh ^ swz<D>(j)) * 16);
+    const int rd = j * D * 2 + ((hh ^ swz_both<D>(j)) * 16);
     const int tr_row = 4 * hh + ((lane & 15) >> 2);
-    const int tr = tr_row * D * 2 + ((swz<D>(tr_row) ^ (2 * ((lane >> 4) & 1) + ((lane & 3) >> 1))) * 16) + (lane & 1) * 8;
+    const int tr = tr_row * D * 2 + ((swz_both<D>(tr_row) ^ (2 * ((lane >> 4) & 1) + ((lane & 3) >> 1))) * 16) + (lane & 1) * 8;
     float m_run = NEG_INF, l_run = 0.f;
     const float thr = 8.0f / p.c;
     f32x16 o[NDT];
@@ -370,9 +347,9 @@ __global__ void __launch_bounds__(256, 2) smha_sink_bwd_q(const SinkParams p) {
     const int64_t row = (int64_t)bh * p.Sqp + qw + j;
     const float lse2 = p.stats[row], delta = p.stats[(int64_t)p.B * p.H * p.Sqp + row];
 
-    const int rd = j * D * 2 + ((hh ^ swz<D>(j)) * 16);
+    const int rd = j * D * 2 + ((hh ^ swz_both<D>(j)) * 16);
     const int tr_row = 4 * hh + ((lane & 15) >> 2);
-    const int tr = tr_row * D * 2 + ((swz<D>(tr_row) ^ (2 * ((lane >> 4) & 1) + ((lane & 3) >> 1))) * 16) + (lane & 1) * 8;
+    const int tr = tr_row * D * 2 + ((swz_both<D>(tr_row) ^ (2 * ((lane >> 4) & 1) + ((lane & 3) >> 1))) * 16) + (lane & 1) * 8;
     f32x16 dq[NDT];
 #pragma unroll
     for (int dt = 0; dt < NDT; ++dt) dq[dt] = zeros16();
@@ -490,9 +467,9 @@ __global__ void __launch_bounds__(256, 2) smha_sink_bwd_kv(const SinkParams p) {
         qt = begin - g * kt.nq;
         request(g, 64 * (kt.qt0 + qt), 0);
     }
-    const int rd = j * D * 2 + ((hh ^ swz<D>(j)) * 16);
+    const int rd = j * D * 2 + ((hh ^ swz_both<D>(j)) * 16);
     const int tr_row = 4 * hh + ((lane & 15) >> 2);
-    const int tr = tr_row * D * 2 + ((swz<D>(tr_row) ^ (2 * ((lane >> 4) & 1) + ((lane & 3) >> 1))) * 16) + (lane & 1) * 8;
+    const int tr = tr_row * D * 2 + ((swz_both<D>(tr_row) ^ (2 * ((lane >> 4) & 1) + ((lane & 3) >> 1))) * 16) + (lane & 1) * 8;
     f32x16 dk[NDT], dv[NDT];
 #pragma unroll
     for (int dt = 0; dt < NDT; ++dt) dk[dt] = dv[dt] = zeros16();
