@@ -332,6 +332,8 @@ void smha_plan_destroy(smha_plan_t *plan); /* NULL is allowed */
  *                   strides of tensors that are only read may be zero
  *   lse             device, float [B][H][Sq], packed: log of the sum of the exponentials of the scaled scores, -inf
  *                   where a query sees nothing or does not exist; NULL in smha_sink_forward if it is not wanted
+ *   O_rest          device, [B][H][Sq][d] of `dtype`, packed: what the rounding of O left out, for the backward pass, whose dQ and
+ *                   dK are less exact without it; NULL if it is not wanted
  *   offsets         device, int32 [B]; NULL: Sk - Sq for every sequence (the queries are its last ones)
  *   lengths         device, int32 [B], keys per sequence, taken as 0 or Sk where outside 0 .. Sk; NULL: Sk
  *   window          keys that a query sees, itself included; 0: all before it
@@ -342,8 +344,8 @@ void smha_plan_destroy(smha_plan_t *plan); /* NULL is allowed */
  * be finite (a NaN or infinity there may reach other queries of the same 128).
  * Errors: INVALID_ARG (null, sizes, a negative window or n_sink, too small a workspace), SHAPE (H no multiple of Hkv),
  * UNSUPPORTED (d, dtype, alignment, strides, sizes), HIP.  Enqueues on hip_stream, on the current device. */
-smha_status_t smha_sink_forward(const void *Q, const void *K, const void *V, void *O, float *lse, int B, int H, int Hkv,
-                                int Sq, int Sk, int d, smha_dtype_t dtype, const int64_t q_strides[3],
+smha_status_t smha_sink_forward(const void *Q, const void *K, const void *V, void *O, float *lse, void *O_rest, int B, int H,
+                                int Hkv, int Sq, int Sk, int d, smha_dtype_t dtype, const int64_t q_strides[3],
                                 const int64_t k_strides[3], const int64_t v_strides[3], const int64_t o_strides[3],
                                 const int32_t *offsets, const int32_t *lengths, int window, int n_sink, float scale,
                                 void *hip_stream);
@@ -351,12 +353,12 @@ smha_status_t smha_sink_forward(const void *Q, const void *K, const void *V, voi
 /* Bytes of device memory that smha_sink_backward needs for such a call. */
 smha_status_t smha_sink_workspace(int B, int H, int Hkv, int Sq, int Sk, int d, int window, int n_sink, size_t *need);
 
-/* Gradients of Q, K and V (of `dtype`, written whole) from O and lse of the forward with the same arguments and dO, the
+/* Gradients of Q, K and V (of `dtype`, written whole) from O, O_rest (or NULL) and lse of the forward with the same arguments and dO, the
  * gradient of O.  The result does not depend on the order in which workgroups run: the parts of sums that were cut
  * are added in a fixed order.  workspace: device, 16-byte aligned, smha_sink_workspace bytes or more; the call's alone
  * until it has run. */
-smha_status_t smha_sink_backward(const void *Q, const void *K, const void *V, const void *O, const float *lse,
-                                 const void *dO, void *dQ, void *dK, void *dV, int B, int H, int Hkv, int Sq, int Sk, int d,
+smha_status_t smha_sink_backward(const void *Q, const void *K, const void *V, const void *O, const void *O_rest,
+                                 const float *lse, const void *dO, void *dQ, void *dK, void *dV, int B, int H, int Hkv, int Sq, int Sk, int d,
                                  smha_dtype_t dtype, const int64_t q_strides[3], const int64_t k_strides[3],
                                  const int64_t v_strides[3], const int64_t o_strides[3], const int64_t do_strides[3],
                                  const int64_t dq_strides[3], const int64_t dk_strides[3], const int64_t dv_strides[3],

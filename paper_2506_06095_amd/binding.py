@@ -105,9 +105,9 @@ def _load():
     lib.smha_plan_row_form.argtypes = [vp, C.c_int, C.c_int, C.c_int, C.POINTER(C.c_int), C.POINTER(C.c_int)]
     lib.smha_plan_row_form.restype = C.c_int
     i64p, i = C.POINTER(C.c_int64), C.c_int
-    lib.smha_sink_forward.argtypes = [vp] * 5 + [i] * 7 + [i64p] * 4 + [vp, vp, i, i, C.c_float, vp]
+    lib.smha_sink_forward.argtypes = [vp] * 6 + [i] * 7 + [i64p] * 4 + [vp, vp, i, i, C.c_float, vp]
     lib.smha_sink_workspace.argtypes = [i] * 8 + [C.POINTER(C.c_size_t)]
-    lib.smha_sink_backward.argtypes = [vp] * 9 + [i] * 7 + [i64p] * 8 + [vp, vp, i, i, C.c_float, vp, C.c_size_t, vp]
+    lib.smha_sink_backward.argtypes = [vp] * 10 + [i] * 7 + [i64p] * 8 + [vp, vp, i, i, C.c_float, vp, C.c_size_t, vp]
     lib.smha_cache_workspace.argtypes = [i] * 10 + [C.POINTER(C.c_size_t)]
     lib.smha_cache_forward.argtypes = [vp] * 8 + [i] * 8 + [i64p] * 7 + [i, i, C.c_float, vp, C.c_size_t, vp]
     lib.smha_cache_evict_workspace.argtypes = [i] * 6 + [C.POINTER(C.c_size_t)]

@@ -26,7 +26,7 @@ namespace smha {
 struct SinkParams {
     const uint16_t *Q, *K, *V, *dO;
     const uint16_t *Oin;  // backward: the forward's output
-    uint16_t *O;
+    uint16_t *O, *rest;   // rest: what O's rounding left out, packed, or null
     uint16_t *dQ, *dK, *dV;
     float *lse;           // [B][H][Sq]
     Strides qs, ks, vs, os, gs, dqs, dks, dvs;
@@ -98,7 +98,8 @@ __device__ __forceinline__ void tiles_landed() {
 
 // A wave's 32 x D accumulators (acc[dt][r] = row j, column 32 dt + 8 (r / 4) + 4 hh + r % 4) to rows row0 .. of a tensor with 16-bit values,
 // through 32 rows of LDS so that whole rows are written; rows from `rows` on are left out.
-template <int D, bool BF16>
+// REST: not the rounded values, but what their rounding leaves out.
+template <int D, bool BF16, bool REST = false>
 __device__ __forceinline__ void store_rows(const f32x16 (&acc)[D / 32], float factor, char *slab, int lane, uint16_t *base, int64_t pitch, int row0, int rows, int d) {
     constexpr int CPR = D / 8;
     const int j = lane & 31, hh = lane >> 5;
@@ -106,7 +107,13 @@ __device__ __forceinline__ void store_rows(const f32x16 (&acc)[D / 32], float fa
     for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
-            const u32x2 v = {pack2<BF16>(acc[dt][4 * g] * factor, acc[dt][4 * g + 1] * factor), pack2<BF16>(acc[dt][4 * g + 2] * factor, acc[dt][4 * g + 3] * factor)};
+            float x[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = acc[dt][4 * g + e] * factor;
+            u32x2 v = {pack2<BF16>(x[0], x[1]), pack2<BF16>(x[2], x[3])};
+            if constexpr (REST)
+                v = u32x2{pack2<BF16>(x[0] - widen16<BF16>(v[0] & 0xFFFFu), x[1] - widen16<BF16>(v[0] >> 16)),
+                          pack2<BF16>(x[2] - widen16<BF16>(v[1] & 0xFFFFu), x[3] - widen16<BF16>(v[1] >> 16))};
             *reinterpret_cast<u32x2 *>(slab + j * D * 2 + (((4 * dt + g) ^ swz_both<D>(j)) * 16) + hh * 8) = v;
         }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -271,14 +278,17 @@ __global__ void __launch_bounds__(256, D == 64 ? 4 : 2) smha_sink_fwd(const Sink
     const float l = l_run + __shfl_xor(l_run, 32);
     if (p.lse && hh == 0 && qw + j < p.Sq)
         p.lse[(int64_t)bh * p.Sq + qw + j] = l > 0.f ? (m_run * p.c + __builtin_amdgcn_logf(l)) * 0.6931471805599453f : NEG_INF;
-    store_rows<D, BF16>(o, l > 0.f ? 1.0f / l : 0.f, smem + w * (32 * D * 2), lane, p.O + b * p.os.b + h * p.os.h, p.os.s, qw, p.Sq, p.d);
+    const float inv = l > 0.f ? 1.0f / l : 0.f;
+    store_rows<D, BF16>(o, inv, smem + w * (32 * D * 2), lane, p.O + b * p.os.b + h * p.os.h, p.os.s, qw, p.Sq, p.d);
+    if (p.rest) store_rows<D, BF16, true>(o, inv, smem + w * (32 * D * 2), lane, p.rest + (int64_t)bh * p.Sq * p.d, p.d, qw, p.Sq, p.d);
 }
 
 // ---------------------------------------------------------------------------------------
 // Backward
 // ---------------------------------------------------------------------------------------
 // lse and delta of every query in the form that the two kernels below take them; queries that do not exist get lse = inf, so that
-// their probabilities are zero.  16 lanes a row.
+// their probabilities are zero.  16 lanes a row.  delta from the rounded output alone is as far off as dS is by its own rounding (dQ and dK
+// 1.52 times as far from 64 bits as an evaluation in 32 bits that is rounded once, 1.42 times with what the rounding left out).
 template <bool BF16>
 __global__ void __launch_bounds__(256) smha_sink_stats(const SinkParams p) {
     const int64_t row = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4), rows = (int64_t)p.B * p.H * p.Sqp;
@@ -291,10 +301,12 @@ __global__ void __launch_bounds__(256) smha_sink_stats(const SinkParams p) {
     if (exists && 8 * c < p.d) {
         const u32x4 o = *reinterpret_cast<const u32x4 *>(p.Oin + b * p.os.b + h * p.os.h + q * p.os.s + 8 * c);
         const u32x4 g = *reinterpret_cast<const u32x4 *>(p.dO + b * p.gs.b + h * p.gs.h + q * p.gs.s + 8 * c);
+        u32x4 rest = {0, 0, 0, 0};
+        if (p.rest) rest = *reinterpret_cast<const u32x4 *>(p.rest + ((int64_t)bh * p.Sq + q) * p.d + 8 * c);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            sum = fmaf(widen16<BF16>(o[e] & 0xFFFFu), widen16<BF16>(g[e] & 0xFFFFu), sum);
-            sum = fmaf(widen16<BF16>(o[e] >> 16), widen16<BF16>(g[e] >> 16), sum);
+            sum = fmaf(widen16<BF16>(o[e] & 0xFFFFu) + widen16<BF16>(rest[e] & 0xFFFFu), widen16<BF16>(g[e] & 0xFFFFu), sum);
+            sum = fmaf(widen16<BF16>(o[e] >> 16) + widen16<BF16>(rest[e] >> 16), widen16<BF16>(g[e] >> 16), sum);
         }
     }
 #pragma unroll
@@ -647,7 +659,7 @@ template <int D, bool BF16> static hipError_t launch_sink_bwd(SinkParams &sp, hi
 
 using namespace smha;
 
-extern "C" smha_status_t smha_sink_forward(const void *Q, const void *K, const void *V, void *O, float *lse, int B, int H, int Hkv, int Sq, int Sk, int d,
+extern "C" smha_status_t smha_sink_forward(const void *Q, const void *K, const void *V, void *O, float *lse, void *O_rest, int B, int H, int Hkv, int Sq, int Sk, int d,
                                            smha_dtype_t dtype, const int64_t q_strides[3], const int64_t k_strides[3], const int64_t v_strides[3],
                                            const int64_t o_strides[3], const int32_t *offsets, const int32_t *lengths, int window, int n_sink, float scale,
                                            void *hip_stream) {
@@ -655,10 +667,10 @@ extern "C" smha_status_t smha_sink_forward(const void *Q, const void *K, const v
     SinkParams sp{};
     const smha_status_t st = sink_params(sp, B, H, Hkv, Sq, Sk, d, dtype, offsets, lengths, window, n_sink, scale);
     if (st != SMHA_OK) return st;
-    if (((uintptr_t)Q | (uintptr_t)K | (uintptr_t)V | (uintptr_t)O) & 15) return SMHA_ERR_UNSUPPORTED;
+    if (((uintptr_t)Q | (uintptr_t)K | (uintptr_t)V | (uintptr_t)O | (uintptr_t)O_rest) & 15) return SMHA_ERR_UNSUPPORTED;
     if (!strides_fit(q_strides, Sq + 128, d) || !strides_fit(k_strides, (int64_t)Sk + 128, d) || !strides_fit(v_strides, (int64_t)Sk + 128, d) || !strides_fit(o_strides, Sq + 128, d))
         return SMHA_ERR_UNSUPPORTED;
-    sp.Q = (const uint16_t *)Q; sp.K = (const uint16_t *)K; sp.V = (const uint16_t *)V; sp.O = (uint16_t *)O; sp.lse = lse;
+    sp.Q = (const uint16_t *)Q; sp.K = (const uint16_t *)K; sp.V = (const uint16_t *)V; sp.O = (uint16_t *)O; sp.lse = lse; sp.rest = (uint16_t *)O_rest;
     sp.qs = strides_of(q_strides, H, Sq, d); sp.ks = strides_of(k_strides, Hkv, Sk, d); sp.vs = strides_of(v_strides, Hkv, Sk, d); sp.os = strides_of(o_strides, H, Sq, d);
     const hipStream_t stream = (hipStream_t)hip_stream;
     const bool bf16 = dtype == SMHA_BF16;
@@ -678,7 +690,7 @@ extern "C" smha_status_t smha_sink_workspace(int B, int H, int Hkv, int Sq, int 
     return SMHA_OK;
 }
 
-extern "C" smha_status_t smha_sink_backward(const void *Q, const void *K, const void *V, const void *O, const float *lse, const void *dO, void *dQ, void *dK, void *dV,
+extern "C" smha_status_t smha_sink_backward(const void *Q, const void *K, const void *V, const void *O, const void *O_rest, const float *lse, const void *dO, void *dQ, void *dK, void *dV,
                                             int B, int H, int Hkv, int Sq, int Sk, int d, smha_dtype_t dtype, const int64_t q_strides[3],
                                             const int64_t k_strides[3], const int64_t v_strides[3], const int64_t o_strides[3], const int64_t do_strides[3],
                                             const int64_t dq_strides[3], const int64_t dk_strides[3], const int64_t dv_strides[3], const int32_t *offsets,
@@ -691,14 +703,14 @@ extern "C" smha_status_t smha_sink_backward(const void *Q, const void *K, const 
     size_t need = 0;
     (void)smha_sink_workspace(B, H, Hkv, Sq, Sk, d, window, n_sink, &need);
     if (workspace_bytes < need) return SMHA_ERR_INVALID_ARG;
-    if (((uintptr_t)Q | (uintptr_t)K | (uintptr_t)V | (uintptr_t)O | (uintptr_t)dO | (uintptr_t)dQ | (uintptr_t)dK | (uintptr_t)dV | (uintptr_t)workspace) & 15)
+    if (((uintptr_t)Q | (uintptr_t)K | (uintptr_t)V | (uintptr_t)O | (uintptr_t)O_rest | (uintptr_t)dO | (uintptr_t)dQ | (uintptr_t)dK | (uintptr_t)dV | (uintptr_t)workspace) & 15)
         return SMHA_ERR_UNSUPPORTED;
     for (const int64_t *s : {q_strides, o_strides, do_strides, dq_strides})
         if (!strides_fit(s, Sq + 128, d)) return SMHA_ERR_UNSUPPORTED;
     for (const int64_t *s : {k_strides, v_strides, dk_strides, dv_strides})
         if (!strides_fit(s, (int64_t)Sk + 128, d)) return SMHA_ERR_UNSUPPORTED;
     sink_cuts(sp);
-    sp.Q = (const uint16_t *)Q; sp.K = (const uint16_t *)K; sp.V = (const uint16_t *)V; sp.Oin = (const uint16_t *)O; sp.dO = (const uint16_t *)dO;
+    sp.Q = (const uint16_t *)Q; sp.K = (const uint16_t *)K; sp.V = (const uint16_t *)V; sp.Oin = (const uint16_t *)O; sp.rest = (uint16_t *)const_cast<void *>(O_rest); sp.dO = (const uint16_t *)dO;
     sp.dQ = (uint16_t *)dQ; sp.dK = (uint16_t *)dK; sp.dV = (uint16_t *)dV; sp.lse = const_cast<float *>(lse);
     sp.qs = strides_of(q_strides, H, Sq, d); sp.ks = strides_of(k_strides, Hkv, Sk, d); sp.vs = strides_of(v_strides, Hkv, Sk, d);
     sp.os = strides_of(o_strides, H, Sq, d); sp.gs = strides_of(do_strides, H, Sq, d);

@@ -65,8 +65,16 @@ def _check_int(value, name):
     return value
 
 
-def smha_sink_forward(Q, K, V, O, lse=None, window: int = 0, n_sink: int = 0, offsets=None, lengths=None, scale: float = 0.0, stream=None) -> None:
-    """O [B,H,Sq,d] and, where it is given, lse (float32 [B,H,Sq], contiguous) of Q [B,H,Sq,d], K, V [B,Hkv,Sk,d].  Enqueues on `stream`
+def _check_rest(rest, like):
+    if rest is not None and (rest.shape != like.shape or rest.dtype != like.dtype or rest.device != like.device or not rest.is_contiguous()):
+        raise ValueError("O_rest must be a contiguous tensor like O")
+    return rest.data_ptr() if rest is not None else None
+
+
+def smha_sink_forward(Q, K, V, O, lse=None, window: int = 0, n_sink: int = 0, offsets=None, lengths=None, scale: float = 0.0, stream=None,
+                      O_rest=None) -> None:
+    """O [B,H,Sq,d] and, where they are given, lse (float32 [B,H,Sq], contiguous) and O_rest (like O, contiguous: what O's rounding left out,
+    for the backward pass) of Q [B,H,Sq,d], K, V [B,Hkv,Sk,d].  Enqueues on `stream`
     (default: torch's current stream of Q's device); does not synchronise."""
     _check_qkv(Q, K, V)
     B, H, Sq, d = Q.shape
@@ -76,8 +84,8 @@ def smha_sink_forward(Q, K, V, O, lse=None, window: int = 0, n_sink: int = 0, of
         raise ValueError("lse must be a contiguous float32 [B,H,Sq] tensor on the same GPU")
     at, n = _check_per_sequence(offsets, "offsets", Q), _check_per_sequence(lengths, "lengths", Q)
     with _on_device(Q):
-        st = _load().smha_sink_forward(Q.data_ptr(), K.data_ptr(), V.data_ptr(), O.data_ptr(), lse.data_ptr() if lse is not None else None, B, H, K.shape[1],
-                                       Sq, K.shape[2], d, _CODES[Q.dtype], _strides(Q), _strides(K), _strides(V), _strides(O), at, n,
+        st = _load().smha_sink_forward(Q.data_ptr(), K.data_ptr(), V.data_ptr(), O.data_ptr(), lse.data_ptr() if lse is not None else None,
+                                       _check_rest(O_rest, Q), B, H, K.shape[1], Sq, K.shape[2], d, _CODES[Q.dtype], _strides(Q), _strides(K), _strides(V), _strides(O), at, n,
                                        _check_int(window, "window"), _check_int(n_sink, "n_sink"), float(scale), _handle(stream, Q.device))
     if st != 0:
         raise SmhaError(st, "smha_sink_forward")
@@ -93,7 +101,7 @@ def smha_sink_workspace(B: int, H: int, Hkv: int, Sq: int, Sk: int, d: int, wind
 
 
 def smha_sink_backward(Q, K, V, O, lse, dO, dQ, dK, dV, window: int = 0, n_sink: int = 0, offsets=None, lengths=None, scale: float = 0.0, workspace=None,
-                       stream=None) -> None:
+                       stream=None, O_rest=None) -> None:
     """dQ, dK, dV (like Q, K, V) from what smha_sink_forward took and gave and the gradient dO of O.  workspace: a uint8 tensor of
     smha_sink_workspace bytes; by default one is allocated (on `stream`, if that is torch's current one or a torch stream)."""
     _check_qkv(Q, K, V)
@@ -113,7 +121,7 @@ def smha_sink_backward(Q, K, V, O, lse, dO, dQ, dK, dV, window: int = 0, n_sink:
                 workspace = torch.empty(smha_sink_workspace(B, H, K.shape[1], Sq, K.shape[2], d, window, n_sink), dtype=torch.uint8, device=Q.device)
         elif workspace.dtype != torch.uint8 or workspace.device != Q.device or not workspace.is_contiguous():
             raise ValueError("workspace must be a contiguous uint8 tensor on the same GPU")
-        st = _load().smha_sink_backward(*(t.data_ptr() for t in (Q, K, V, O, lse, dO, dQ, dK, dV)), B, H, K.shape[1], Sq, K.shape[2], d, _CODES[Q.dtype],
+        st = _load().smha_sink_backward(*(t.data_ptr() for t in (Q, K, V, O)), _check_rest(O_rest, Q), *(t.data_ptr() for t in (lse, dO, dQ, dK, dV)), B, H, K.shape[1], Sq, K.shape[2], d, _CODES[Q.dtype],
                                         *(_strides(t) for t in (Q, K, V, O, dO, dQ, dK, dV)), at, n, window, n_sink, float(scale),
                                         workspace.data_ptr(), workspace.numel(), _handle(stream, Q.device))
     if st != 0:
@@ -131,18 +139,20 @@ class _SinkAttention(torch.autograd.Function):
     def forward(ctx, q, k, v, window, n_sink, offsets, lengths, scale):
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
         lse = torch.empty(q.shape[:3], dtype=torch.float32, device=q.device)
-        smha_sink_forward(q, k, v, out, lse, window, n_sink, offsets, lengths, scale)
-        ctx.save_for_backward(q, k, v, out, lse, offsets, lengths)
+        rest = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        smha_sink_forward(q, k, v, out, lse, window, n_sink, offsets, lengths, scale, O_rest=rest)
+        ctx.save_for_backward(q, k, v, out, rest, lse, offsets, lengths)
         ctx.rest = window, n_sink, scale
         return out
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, grad):
-        q, k, v, out, lse, offsets, lengths = ctx.saved_tensors
+        q, k, v, out, rest, lse, offsets, lengths = ctx.saved_tensors
         window, n_sink, scale = ctx.rest
         dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
-        smha_sink_backward(q, k, v, out, lse, grad if _takes(grad) else grad.contiguous(), dq, dk, dv, window, n_sink, offsets, lengths, scale)
+        smha_sink_backward(q, k, v, out, lse, grad if _takes(grad) else grad.contiguous(), dq, dk, dv, window, n_sink, offsets, lengths, scale,
+                           O_rest=rest)
         return dq, dk, dv, None, None, None, None, None
 
 

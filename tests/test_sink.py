@@ -259,7 +259,7 @@ def test_refusals():
 
     def forward(q=ptr, o=ptr, B=1, H=4, Hkv=2, Sq=8, Sk=8, d=64, dtype=0, strides=None, window=4, n_sink=0):
         s = (C.c_int64 * 3)(*strides) if strides else None
-        return lib.smha_sink_forward(q, ptr, ptr, o, None, B, H, Hkv, Sq, Sk, d, dtype, s, None, None, None, None, None, window, n_sink, 0.0, None)
+        return lib.smha_sink_forward(q, ptr, ptr, o, None, None, B, H, Hkv, Sq, Sk, d, dtype, s, None, None, None, None, None, window, n_sink, 0.0, None)
 
     invalid, unsupported, shape = 1, 2, 3
     assert forward(q=None) == invalid and forward(B=0) == invalid and forward(Sk=0) == invalid
@@ -274,7 +274,7 @@ def test_refusals():
     assert need.value == 2 * 4 * 128 * 4
 
     def backward(workspace, size):
-        return lib.smha_sink_backward(*[ptr] * 9, 1, 4, 2, 8, 8, 64, 0, *[None] * 8, None, None, 4, 0, 0.0, workspace, size, None)
+        return lib.smha_sink_backward(*[ptr] * 10, 1, 4, 2, 8, 8, 64, 0, *[None] * 8, None, None, 4, 0, 0.0, workspace, size, None)
 
     assert backward(None, need.value) == invalid and backward(ptr, need.value - 1) == invalid
 
