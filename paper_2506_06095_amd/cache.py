@@ -9,8 +9,11 @@ import ctypes as C
 
 import torch
 
-from .binding import SmhaError, _load
+from .binding import SmhaError, _load, native_call
 from .sink import _CODES, _check_int, _check_per_sequence, _check_qkv, _handle, _on_device, _strides
+
+
+_attention = _evict = None  # functions of _smha_torch
 
 
 def _stream_to_allocate_on(stream, workspace):
@@ -46,6 +49,16 @@ def cache_attention(q, k, v, lengths, *, window: int = 0, n_sink: int = 0, prefi
     prefix: (keys, values), each [Hkv,P,d]: tokens before those of every sequence, which all of them see (not with a window).
     weights: float32 [B,Hkv,Sk]; each key's attention, summed over the tokens and the heads that share it, is added to it.
     No gradients.  workspace: a uint8 tensor of smha_cache_workspace bytes, by default one is allocated."""
+    if out is None and workspace is None and stream is None:  # the native way, for every call that it takes (csrc/torch_binding.cpp)
+        global _attention
+        if _attention is None:
+            _attention = native_call("cache_attention")
+        pk, pv = prefix if prefix is not None else (None, None)
+        got = _attention(q, k, v, lengths, window, n_sink, pk, pv, weights, float(scale))
+        if got is not None:
+            if type(got) is int:
+                raise SmhaError(got, "smha_cache_forward")
+            return got
     _check_qkv(q, k, v)
     if torch.is_grad_enabled() and (q.requires_grad or k.requires_grad or v.requires_grad):
         raise ValueError("cache_attention has no gradients: sink_attention has")
@@ -116,6 +129,15 @@ def cache_evict(k, v, weights, positions, lengths, budget: int, recent: int = 0,
     their slots, except that those that stay past the budget move, in order, to the slots before it that were freed.  Slots from the
     new length on get weight 0 and position -1, and keep their keys.
     out: the three tensors to write to, by default new ones; they may be the inputs themselves."""
+    if out is None and workspace is None and stream is None:
+        global _evict
+        if _evict is None:
+            _evict = native_call("cache_evict")
+        got = _evict(k, v, weights, positions, lengths, budget, recent)
+        if got is not None:
+            if type(got) is int:
+                raise SmhaError(got, "smha_cache_evict")
+            return got
     if k.dim() != 4 or k.shape != v.shape or k.dtype not in _CODES or v.dtype != k.dtype:
         raise ValueError("k, v must be [B,Hkv,Sk,d], float16 or bfloat16, alike")
     if not k.is_cuda or v.device != k.device:

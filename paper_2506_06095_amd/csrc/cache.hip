@@ -70,8 +70,9 @@ __device__ __forceinline__ int wave_sum(int v) {
     return v;
 }
 
-// The segment of a workgroup.  Every wave of the launch computes the same cut: c tiles a segment, the least multiple of four (a team's
-// turn) for which a few corrections find no more than `slots` segments.
+// The segment of a workgroup.  Every wave of the launch computes the same cut: c tiles a segment at most, so many (in fours, a team's turn) that
+// all tiles make `slots` segments.  Groups shorter than that are a segment each, and then there are more: what does not fit at first
+// starts as others end.
 __device__ __forceinline__ Segment segment_of(const CacheParams &p, int lane) {
     const int prefix_groups = p.Hkv * p.prefix_tiles, per_b = p.Hkv * p.own_tiles;
     const int prefix_n = p.prefix_tiles ? (p.P + 31) / 32 : 0;
@@ -80,25 +81,18 @@ __device__ __forceinline__ Segment segment_of(const CacheParams &p, int lane) {
     int sum = first64;
     for (int b = 64 + lane; b - lane < p.B; b += 64) sum += tiles(b);
     const int total = prefix_groups * prefix_n + per_b * wave_sum(sum);
-    int c = max(4, ((total + p.slots - 1) / p.slots + 3) & ~3), count = 0;
-    for (int turn = 0;; ++turn) {
-        sum = (first64 + c - 1) / c;
-        for (int b = 64 + lane; b - lane < p.B; b += 64) sum += (tiles(b) + c - 1) / c;
-        count = prefix_groups * ((prefix_n + c - 1) / c) + per_b * wave_sum(sum);
-        if (count <= p.slots || turn == 3) break;
-        c = ((int)(((int64_t)c * count + p.slots - 1) / p.slots) + 3) & ~3;
-    }
-    count = __builtin_amdgcn_readfirstlane(count);
-    c = __builtin_amdgcn_readfirstlane(c);
-    // an XCD takes a run of segments: those that read the same keys are neighbours
-    const int per_xcd = (count + 7) / 8, slot = (int)blockIdx.x >> 3;
-    int at = (int)(blockIdx.x & 7) * per_xcd + slot;
+    const int c = __builtin_amdgcn_readfirstlane(max(4, ((total + p.slots - 1) / p.slots + 3) & ~3));
+    sum = (first64 + c - 1) / c;
+    for (int b = 64 + lane; b - lane < p.B; b += 64) sum += (tiles(b) + c - 1) / c;
+    const int own_segs = __builtin_amdgcn_readfirstlane(per_b * wave_sum(sum)), prefix_parts = (prefix_n + c - 1) / c, prefix_segs = prefix_groups * prefix_parts;
+    // an XCD takes a run of the prefix's segments, which are the longest, and then one of the others: those that read the same keys are neighbours
+    const int xcd = (int)blockIdx.x & 7, slot = (int)blockIdx.x >> 3, prefix_run = (prefix_segs + 7) / 8, own_run = (own_segs + 7) / 8;
     Segment s{-1, -1, 0, 0, 0, 1, 0, 0};
-    if (slot >= per_xcd || at >= count) return s;
-    s.seg = at;
-    const int prefix_segs = prefix_groups * ((prefix_n + c - 1) / c);
-    if (at < prefix_segs) {
-        s.parts = (prefix_n + c - 1) / c;
+    if (slot < prefix_run) {
+        const int at = xcd * prefix_run + slot;
+        if (at >= prefix_segs) return s;
+        s.seg = at;
+        s.parts = prefix_parts;
         s.group = at / s.parts;
         s.part = at - s.group * s.parts;
         s.hk = s.group / p.prefix_tiles;
@@ -106,7 +100,9 @@ __device__ __forceinline__ Segment segment_of(const CacheParams &p, int lane) {
         s.n = prefix_n;
         return s;
     }
-    at -= prefix_segs;
+    int at = xcd * own_run + slot - prefix_run;
+    if (slot - prefix_run >= own_run || at >= own_segs) return s;
+    s.seg = prefix_segs + at;
     for (int b0 = 0; b0 < p.B; b0 += 64) {
         const int n = b0 ? tiles(b0 + lane) : first64, mine = per_b * ((n + c - 1) / c);
         int upto = mine;
@@ -404,17 +400,27 @@ __global__ void __launch_bounds__(256) smha_cache_join(const CacheParams p, int 
     for (int r0 = 0; r0 < GT; r0 += 256) {
         const int nr = min(256, GT - r0);
         __syncthreads();
-        if ((int)threadIdx.x < nr) {
-            const RowParts r = row_parts(p, b, hk, r0 + threadIdx.x, true);
+        for (int r1 = w; r1 < nr; r1 += 4) {  // a wave a row, a lane a segment
+            const RowParts r = row_parts(p, b, hk, r0 + r1, true);
+            const int n = r.count[0] + r.count[1];
             float m = NEG_INF, l = 0.f;
-            for (int k = 0; k < 2; ++k)
-                for (int i = 0; i < r.count[k]; ++i) m = fmaxf(m, p.stats[(int64_t)(r.first[k] + i) * 64 + r.row[k]]);
-            for (int k = 0; k < 2; ++k)
-                for (int i = 0; i < r.count[k]; ++i) {
-                    const int64_t at = (int64_t)(r.first[k] + i) * 64 + r.row[k];
-                    if (p.stats[at] != NEG_INF) l = fmaf(fast_exp2(p.stats[at] - m), p.stats[at + 32], l);
+            for (int i = lane; i - lane < n; i += 64) {
+                float ref = NEG_INF, part = 0.f;
+                if (i < n) {
+                    const int64_t at = (int64_t)(i < r.count[0] ? r.first[0] + i : r.first[1] + i - r.count[0]) * 64 + (i < r.count[0] ? r.row[0] : r.row[1]);
+                    ref = p.stats[at];
+                    part = p.stats[at + 32];
                 }
-            lds_lse[threadIdx.x] = l > 0.f ? m + __builtin_amdgcn_logf(l) : __builtin_inff();  // (inf: a row without keys adds nothing)
+                float top = fmaxf(m, ref);
+#pragma unroll
+                for (int x = 32; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
+                float sum = ref != NEG_INF ? fast_exp2(ref - top) * part : 0.f;
+#pragma unroll
+                for (int x = 32; x > 0; x >>= 1) sum += __shfl_xor(sum, x);
+                l = (m != NEG_INF ? l * fast_exp2(m - top) : 0.f) + sum;
+                m = top;
+            }
+            if (lane == 0) lds_lse[r1] = l > 0.f ? m + __builtin_amdgcn_logf(l) : __builtin_inff();  // (inf: a row without keys adds nothing)
         }
         __syncthreads();
         if (scored) {
@@ -442,7 +448,6 @@ struct EvictParams {
     const int32_t *pos, *lengths;
     float *w_out;
     int32_t *pos_out, *len_out;
-    int64_t w_b, w_h, p_b, p_h, wo_b, wo_h, po_b, po_h;
     int B, Hkv, Sk, d, budget, recent, moves;  // moves: most that a head makes
     int32_t *lists;                             // [B Hkv][1 + 2 moves]: count, where to, where from
 };
@@ -454,20 +459,23 @@ __device__ __forceinline__ uint32_t ordered(float x) {
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// One workgroup of 16 waves a key head.  Wave w holds the keys of slots (w KPT + i) 64 + lane as unsigned numbers that order them, so
-// that a lane's and a register's order is the slots' order.  The budget-th largest is found two bits at a time by counting; of
-// those that equal it the first slots stay.  What stays past the new end goes, in order, where keys before it left.
+// One workgroup of 16 waves a key head.  Wave w holds the keys of slots (w n + i) 64 + lane as unsigned numbers that order them, so that a lane's
+// and a register's order is the slots' order.  The budget-th largest is found by counting, 11, 11 and 10 bits at a time, in a
+// histogram in LDS (11 bits of a float are a quarter of an octave: lanes of a wave meet in few bins but seldom all in one, and where
+// they do one of them counts for all); of the keys that equal it the first slots stay.  What stays past the new end goes, in
+// order, where keys before it left.  (Counting with ballots, two bits at a time: 26.5 us for 128 heads of 4352 keys, 110 for 32 of 32768.)
 template <int KPT>
 __global__ void __launch_bounds__(1024) smha_cache_select(const EvictParams p) {
-    __shared__ int counts[2][16][3];
-    __shared__ int totals[16][3];
+    __shared__ int bins[2048];
+    __shared__ int totals[16][2];
+    __shared__ int found[2];
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int bh = blockIdx.x, b = bh / p.Hkv, hk = bh - b * p.Hkv;
     const int len = min(max(p.lengths[b], 0), p.Sk), end = min(len, p.budget);
-    const float *const W = p.w + b * p.w_b + hk * p.w_h;
-    const int32_t *const P = p.pos + b * p.p_b + hk * p.p_h;
-    float *const Wo = p.w_out + b * p.wo_b + hk * p.wo_h;
-    int32_t *const Po = p.pos_out + b * p.po_b + hk * p.po_h;
+    const float *const W = p.w + (int64_t)bh * p.Sk;
+    const int32_t *const P = p.pos + (int64_t)bh * p.Sk;
+    float *const Wo = p.w_out + (int64_t)bh * p.Sk;
+    int32_t *const Po = p.pos_out + (int64_t)bh * p.Sk;
     int32_t *const list = p.lists + (int64_t)bh * (1 + 2 * (int64_t)p.moves);
     const bool copies = W != Wo || P != Po;
     if (len <= p.budget) {
@@ -483,89 +491,106 @@ __global__ void __launch_bounds__(1024) smha_cache_select(const EvictParams p) {
         }
         return;
     }
-    // the youngest
-    int newest = -1;
-    bool any = false;
-    for (int i = threadIdx.x; i < len; i += 1024) {
-        const int x = P[i];
-        newest = any ? max(newest, x) : x;
-        any = true;
-    }
-    if (!any) newest = INT32_MIN;
-#pragma unroll
-    for (int m = 32; m > 0; m >>= 1) newest = max(newest, __shfl_xor(newest, m));
-    if (lane == 0) counts[0][w][0] = newest;
-    __syncthreads();
-#pragma unroll
-    for (int u = 0; u < 16; ++u) newest = max(newest, counts[0][u][0]);
-    __syncthreads();
-    const int64_t young = (int64_t)newest - p.recent;  // positions past this stay, whatever their account
-    const int per_wave = ((len + 1023) / 1024) * 64;   // slots of a wave
-    const int base = w * per_wave + lane, n = min(KPT ? KPT : INT32_MAX, per_wave / 64);
-    auto key_at = [&](int slot) __attribute__((always_inline)) -> uint32_t {
-        if (slot >= len) return 0u;  // (below every live key's)
-        return (int64_t)P[slot] > young ? 0xFF800000u : ordered(W[slot]);
-    };
-    uint32_t held[KPT ? KPT : 1];
+    const int n = (len + 1023) / 1024, base = w * 64 * n + lane;  // keys a lane, its first slot
+    constexpr int HELD = KPT ? KPT : 1;
+    float held_w[HELD];
+    int32_t held_p[HELD];
+    int newest = INT32_MIN;
     if constexpr (KPT > 0) {
 #pragma unroll
-        for (int i = 0; i < KPT; ++i) held[i] = i < n ? key_at(base + 64 * i) : 0u;
+        for (int i = 0; i < KPT; ++i) {
+            const int slot = min(base + 64 * i, len - 1);  // (past the end: the last one again)
+            held_w[i] = i < n ? W[slot] : 0.f;
+            held_p[i] = i < n ? P[slot] : INT32_MIN;
+        }
+#pragma unroll
+        for (int i = 0; i < KPT; ++i) newest = max(newest, held_p[i]);
+    } else {
+        for (int i = threadIdx.x; i < len; i += 1024) newest = max(newest, P[i]);
     }
-    auto key_of = [&](int i) __attribute__((always_inline)) -> uint32_t {
-        if constexpr (KPT > 0) return held[i];
-        else return key_at(base + 64 * i);
+#pragma unroll
+    for (int m = 32; m > 0; m >>= 1) newest = max(newest, __shfl_xor(newest, m));
+    if (lane == 0) totals[w][0] = newest;
+    for (int i = threadIdx.x; i < 2048; i += 1024) bins[i] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < 16; ++u) newest = max(newest, totals[u][0]);
+    const int64_t young = (int64_t)newest - p.recent;  // positions past this stay, whatever their account
+    auto key_from = [&](int slot, float x, int32_t at) __attribute__((always_inline)) -> uint32_t {
+        return slot >= len ? 0u : (int64_t)at > young ? 0xFF800000u : ordered(x);  // (0: below every live key's)
     };
+    uint32_t held[HELD];
+    if constexpr (KPT > 0) {
+#pragma unroll
+        for (int i = 0; i < KPT; ++i) held[i] = key_from(base + 64 * i, held_w[i], held_p[i]);
+    }
     auto each = [&](auto &&f) __attribute__((always_inline)) {
         if constexpr (KPT > 0) {
 #pragma unroll
             for (int i = 0; i < KPT; ++i)
-                if (i < n) f(i, key_of(i));
+                if (i < n) f(i, held[i]);
         } else {
-            for (int i = 0; i < n; ++i) f(i, key_of(i));
+            for (int i = 0; i < n; ++i) {
+                const int slot = base + 64 * i;
+                f(i, slot < len ? key_from(slot, W[slot], P[slot]) : 0u);
+            }
         }
     };
-    // the largest x that `end` keys or more reach
+    // the largest number that `end` keys or more reach: its bits from the top, and how many keys are over what is known of it
     uint32_t least = 0;
-    for (int shift = 30, turn = 0; shift >= 0; shift -= 2, turn ^= 1) {
-        int c1 = 0, c2 = 0, c3 = 0;
-        const uint32_t t1 = least | (1u << shift), t2 = least | (2u << shift), t3 = least | (3u << shift);
+    int all_over = 0;
+#pragma unroll
+    for (int pass = 0; pass < 3; ++pass) {
+        const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, width = pass == 2 ? 10 : 11;
         each([&](int, uint32_t k) __attribute__((always_inline)) {
-            c1 += __builtin_popcountll(__builtin_amdgcn_ballot_w64(k >= t1));
-            c2 += __builtin_popcountll(__builtin_amdgcn_ballot_w64(k >= t2));
-            c3 += __builtin_popcountll(__builtin_amdgcn_ballot_w64(k >= t3));
+            const bool in = pass == 0 ? k != 0 : (k >> (shift + width)) == (least >> (shift + width)) && k != 0;
+            const int bin = (int)(k >> shift) & ((1 << width) - 1);
+            const uint64_t who = __builtin_amdgcn_ballot_w64(in);
+            if (who) {
+                const int one = __builtin_amdgcn_readlane(bin, __builtin_ctzll(who));
+                if (__builtin_amdgcn_ballot_w64(in && bin != one) == 0) {
+                    if (lane == 0) atomicAdd(&bins[one], __builtin_popcountll(who));
+                } else if (in) {
+                    atomicAdd(&bins[bin], 1);
+                }
+            }
         });
-        if (lane == 0) {
-            counts[turn][w][0] = c1;
-            counts[turn][w][1] = c2;
-            counts[turn][w][2] = c3;
+        __syncthreads();
+        // a thread's two bins, from the top, and those over them
+        const int top = 2047 - 2 * (int)threadIdx.x, n1 = bins[top], n0 = bins[top - 1];
+        int upto = n1 + n0;
+#pragma unroll
+        for (int m = 1; m < 64; m <<= 1) {
+            const int below = __shfl_up(upto, m);
+            if (lane >= m) upto += below;
+        }
+        if (lane == 63) totals[w][1] = upto;
+        __syncthreads();
+        bins[top] = bins[top - 1] = 0;
+        int over = all_over + upto - n1 - n0;
+#pragma unroll
+        for (int u = 0; u < 16; ++u)
+            if (u < w) over += totals[u][1];
+        if (over < end && over + n1 >= end) {
+            found[0] = top;
+            found[1] = over;
+        } else if (over + n1 < end && over + n1 + n0 >= end) {
+            found[0] = top - 1;
+            found[1] = over + n1;
         }
         __syncthreads();
-        c1 = c2 = c3 = 0;
-#pragma unroll
-        for (int u = 0; u < 16; ++u) {
-            c1 += counts[turn][u][0];
-            c2 += counts[turn][u][1];
-            c3 += counts[turn][u][2];
-        }
-        least = c3 >= end ? t3 : c2 >= end ? t2 : c1 >= end ? t1 : least;
+        least |= (uint32_t)found[0] << shift;
+        all_over = found[1];
     }
-    // per wave: keys over the least, keys at it; then who stays
-    int over = 0, equal = 0;
-    each([&](int, uint32_t k) __attribute__((always_inline)) {
-        over += __builtin_popcountll(__builtin_amdgcn_ballot_w64(k > least));
-        equal += __builtin_popcountll(__builtin_amdgcn_ballot_w64(k == least));
-    });
-    if (lane == 0) {
-        totals[w][0] = over;
-        totals[w][1] = equal;
-    }
+    // who stays: keys over the least, and the first of those at it
+    int equal = 0;
+    each([&](int, uint32_t k) __attribute__((always_inline)) { equal += __builtin_popcountll(__builtin_amdgcn_ballot_w64(k == least)); });
+    if (lane == 0) totals[w][0] = equal;
     __syncthreads();
-    int all_over = 0, equal_before = 0;
+    int equal_before = 0;
 #pragma unroll
-    for (int u = 0; u < 16; ++u) {
-        all_over += totals[u][0];
-        if (u < w) equal_before += totals[u][1];
-    }
+    for (int u = 0; u < 16; ++u)
+        if (u < w) equal_before += totals[u][0];
     const int equal_stay = end - all_over;  // the first so many of those at the least
     const uint64_t below = (1ull << lane) - 1;
     // freed slots before the end, kept slots from it on, per wave
@@ -688,7 +713,7 @@ static smha_status_t cache_params(CacheParams &cp, CacheLayout &at, int B, int H
 }
 
 template <int D, bool BF16> static hipError_t launch_cache(const CacheParams &cp, hipStream_t stream) {
-    const dim3 grid(8 * ((cp.segs + 7) / 8));
+    const dim3 grid(8 * ((cp.segs + 7) / 8 + 1));  // (two runs an XCD, each rounded up)
     if (cp.weights) hipLaunchKernelGGL((smha_cache_part<D, BF16, true>), grid, dim3(256), 0, stream, cp);
     else hipLaunchKernelGGL((smha_cache_part<D, BF16, false>), grid, dim3(256), 0, stream, cp);
     const hipError_t e = hipGetLastError();
@@ -781,8 +806,6 @@ extern "C" smha_status_t smha_cache_evict(void *K, void *V, const float *weights
     ep.K = (uint16_t *)K; ep.V = (uint16_t *)V;
     ep.ks = cache_strides(k_strides, Hkv, Sk, d); ep.vs = cache_strides(v_strides, Hkv, Sk, d);
     ep.w = weights; ep.pos = positions; ep.lengths = lengths; ep.w_out = weights_out; ep.pos_out = positions_out; ep.len_out = lengths_out;
-    ep.w_h = ep.p_h = ep.wo_h = ep.po_h = Sk;
-    ep.w_b = ep.p_b = ep.wo_b = ep.po_b = (int64_t)Hkv * Sk;
     ep.B = B; ep.Hkv = Hkv; ep.Sk = Sk; ep.d = d; ep.budget = budget; ep.recent = recent;
     ep.moves = std::max(0, std::min(budget, Sk - budget));
     ep.lists = (int32_t *)workspace;

@@ -11,9 +11,12 @@
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
 #include <c10/core/impl/TorchDispatchModeTLS.h>
+#include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
+#include <torch/csrc/autograd/custom_function.h>
+#include <torch/csrc/autograd/functions/basic_ops.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "smha.h"
@@ -22,12 +25,12 @@ namespace {
 
 using Forward = decltype(&smha_forward);
 
-bool plain(PyObject *obj) {
+bool plain(PyObject *obj, int64_t dims = 4) {
     if (!THPVariable_CheckExact(obj)) return false;
     const at::Tensor &t = THPVariable_Unpack(obj);
     constexpr c10::DispatchKeySet ordinary({c10::DispatchKey::CUDA, c10::DispatchKey::AutogradCUDA, c10::DispatchKey::ADInplaceOrView,
                                             c10::DispatchKey::AutocastCUDA});
-    return t.defined() && (t.key_set() | ordinary) == ordinary && t.is_cuda() && t.dim() == 4 && !t.has_names() &&
+    return t.defined() && (t.key_set() | ordinary) == ordinary && t.is_cuda() && t.dim() == dims && !t.has_names() &&
            !t.unsafeGetTensorImpl()->has_symbolic_sizes_strides();
 }
 
@@ -100,7 +103,286 @@ PyObject *forward(PyObject *, PyObject *const *args, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
-PyMethodDef methods[] = {{"forward", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(forward)), METH_FASTCALL, nullptr}, {nullptr, nullptr, 0, nullptr}};
+// ---- attention with sinks, attention on a cache, eviction (sink.py and cache.py: the same calls, and the errors of those that are refused here)
+
+struct Entries {
+    decltype(&smha_sink_forward) sink_forward;
+    decltype(&smha_sink_backward) sink_backward;
+    decltype(&smha_sink_workspace) sink_workspace;
+    decltype(&smha_cache_forward) cache_forward;
+    decltype(&smha_cache_workspace) cache_workspace;
+    decltype(&smha_cache_evict) cache_evict;
+    decltype(&smha_cache_evict_workspace) cache_evict_workspace;
+} entries;
+
+// link(the addresses of those, in that order)
+PyObject *link(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    void *at[7];
+    if (n != 7) {
+        PyErr_SetString(PyExc_TypeError, "seven addresses");
+        return nullptr;
+    }
+    for (int i = 0; i < 7; ++i) at[i] = PyLong_AsVoidPtr(args[i]);
+    if (PyErr_Occurred()) return nullptr;
+    entries = {reinterpret_cast<decltype(entries.sink_forward)>(at[0]), reinterpret_cast<decltype(entries.sink_backward)>(at[1]),
+               reinterpret_cast<decltype(entries.sink_workspace)>(at[2]), reinterpret_cast<decltype(entries.cache_forward)>(at[3]),
+               reinterpret_cast<decltype(entries.cache_workspace)>(at[4]), reinterpret_cast<decltype(entries.cache_evict)>(at[5]),
+               reinterpret_cast<decltype(entries.cache_evict_workspace)>(at[6])};
+    Py_RETURN_NONE;
+}
+
+// {batch, head, token} strides, null where packed; what a dimension of size 1 has is not looked at.
+struct Strides3 {
+    int64_t s[3];
+    const int64_t *ptr = nullptr;
+    bool ok = true;
+    explicit Strides3(const at::Tensor &t) {
+        if (t.is_contiguous()) return;
+        const auto n = t.sizes(), st = t.strides();
+        ok = st[3] == 1 || n[3] == 1;
+        s[0] = n[0] > 1 ? st[0] : 0;
+        s[1] = n[1] > 1 ? st[1] : 0;
+        s[2] = n[2] > 1 ? st[2] : n[3];
+        ptr = s;
+    }
+    Strides3(const Strides3 &) = delete;
+};
+
+bool int_from(PyObject *o, int &to) {  // 0 .. 2^31 - 1
+    if (!PyLong_CheckExact(o)) return false;
+    const int64_t v = PyLong_AsLongLong(o);
+    if (PyErr_Occurred()) {
+        PyErr_Clear();
+        return false;
+    }
+    to = (int)v;
+    return v >= 0 && v <= INT32_MAX;
+}
+
+bool small_sizes(const at::Tensor &t) {
+    for (const int64_t n : t.sizes())
+        if (n > INT32_MAX) return false;
+    return true;
+}
+
+// int32 [B] on q's GPU, or None
+bool per_sequence(PyObject *o, const at::Tensor &q, const int32_t *&to, at::Tensor &held) {
+    to = nullptr;
+    if (o == Py_None) return true;
+    if (!plain(o, 1)) return false;
+    held = THPVariable_Unpack(o);
+    if (held.scalar_type() != at::kInt || held.size(0) != q.size(0) || held.device() != q.device() || !held.is_contiguous()) return false;
+    to = held.data_ptr<int32_t>();
+    return true;
+}
+
+bool heads_fit(const at::Tensor &q, const at::Tensor &k, const at::Tensor &v) {
+    const int type = code_of(q.scalar_type());
+    return (type == SMHA_F16 || type == SMHA_BF16) && k.scalar_type() == q.scalar_type() && v.scalar_type() == q.scalar_type() && k.sizes() == v.sizes() &&
+           q.size(0) == k.size(0) && q.size(3) == k.size(3) && k.size(1) > 0 && q.size(1) % k.size(1) == 0 && k.device() == q.device() &&
+           v.device() == q.device() && small_sizes(q) && small_sizes(k);
+}
+
+struct SinkCall {
+    int window, n_sink;
+    float scale;
+};
+
+smha_status_t run_sink_forward(const at::Tensor &q, const at::Tensor &k, const at::Tensor &v, at::Tensor &o, float *lse, void *rest, const int32_t *offsets,
+                               const int32_t *lengths, const SinkCall &c) {
+    const Strides3 qs(q), ks(k), vs(v);
+    return entries.sink_forward(q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse, rest, (int)q.size(0), (int)q.size(1), (int)k.size(1),
+                                (int)q.size(2), (int)k.size(2), (int)q.size(3), (smha_dtype_t)code_of(q.scalar_type()), qs.ptr, ks.ptr, vs.ptr, nullptr, offsets, lengths,
+                                c.window, c.n_sink, c.scale, c10::hip::getCurrentHIPStream(q.device().index()).stream());
+}
+
+struct SinkFailed {
+    smha_status_t status;
+};
+
+at::Tensor packed_like(const at::Tensor &t) { return at::empty(t.sizes(), t.options(), at::MemoryFormat::Contiguous); }
+
+struct SinkFunction : torch::autograd::Function<SinkFunction> {
+    static at::Tensor forward(torch::autograd::AutogradContext *ctx, const at::Tensor &q, const at::Tensor &k, const at::Tensor &v,
+                              const std::optional<at::Tensor> &offsets, const std::optional<at::Tensor> &lengths, int64_t window, int64_t n_sink, double scale) {
+        at::Tensor o = packed_like(q), rest = packed_like(q);
+        at::Tensor lse = at::empty({q.size(0), q.size(1), q.size(2)}, q.options().dtype(at::kFloat));
+        const smha_status_t st = run_sink_forward(q, k, v, o, lse.data_ptr<float>(), rest.data_ptr(), offsets ? offsets->data_ptr<int32_t>() : nullptr,
+                                                  lengths ? lengths->data_ptr<int32_t>() : nullptr, {(int)window, (int)n_sink, (float)scale});
+        if (st != SMHA_OK) throw SinkFailed{st};
+        ctx->save_for_backward({q, k, v, o, rest, lse, offsets.value_or(at::Tensor()), lengths.value_or(at::Tensor())});
+        ctx->saved_data["window"] = window;
+        ctx->saved_data["n_sink"] = n_sink;
+        ctx->saved_data["scale"] = scale;
+        return o;
+    }
+
+    static torch::autograd::variable_list backward(torch::autograd::AutogradContext *ctx, const torch::autograd::variable_list &grads) {
+        const auto saved = ctx->get_saved_variables();
+        const at::Tensor &q = saved[0], &k = saved[1], &v = saved[2], &o = saved[3], &rest = saved[4], &lse = saved[5], &offsets = saved[6], &lengths = saved[7];
+        if (!grads[0].defined()) return torch::autograd::variable_list(8);
+        at::Tensor g = grads[0].detach(), dq, dk, dv;
+        {
+            const at::AutoGradMode off(false);
+            const auto gs = g.strides();
+            // (autograd may hand on expanded or transposed gradients)
+            const bool takes = reinterpret_cast<uintptr_t>(g.data_ptr()) % 16 == 0 &&
+                               (g.is_contiguous() || (gs[3] == 1 && gs[0] % 8 == 0 && gs[1] % 8 == 0 && gs[2] % 8 == 0 && gs[2] >= g.size(3)));
+            if (!takes) g = g.clone(at::MemoryFormat::Contiguous);
+            dq = packed_like(q);
+            dk = packed_like(k);
+            dv = packed_like(v);
+            const int B = (int)q.size(0), H = (int)q.size(1), Hkv = (int)k.size(1), Sq = (int)q.size(2), Sk = (int)k.size(2), d = (int)q.size(3);
+            const int window = (int)ctx->saved_data["window"].toInt(), n_sink = (int)ctx->saved_data["n_sink"].toInt();
+            const c10::DeviceGuard guard(q.device());
+            size_t need = 0;
+            smha_status_t st = entries.sink_workspace(B, H, Hkv, Sq, Sk, d, window, n_sink, &need);
+            const Strides3 qs(q), ks(k), vs(v), ds(g);
+            if (st == SMHA_OK) {
+                at::Tensor ws = at::empty({(int64_t)need}, q.options().dtype(at::kByte));
+                st = entries.sink_backward(q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), rest.data_ptr(), lse.data_ptr<float>(), g.data_ptr(), dq.data_ptr(),
+                                           dk.data_ptr(), dv.data_ptr(), B, H, Hkv, Sq, Sk, d, (smha_dtype_t)code_of(q.scalar_type()), qs.ptr, ks.ptr, vs.ptr, nullptr, ds.ptr,
+                                           nullptr, nullptr, nullptr, offsets.defined() ? offsets.data_ptr<int32_t>() : nullptr,
+                                           lengths.defined() ? lengths.data_ptr<int32_t>() : nullptr, window, n_sink, (float)ctx->saved_data["scale"].toDouble(),
+                                           ws.data_ptr(), need, c10::hip::getCurrentHIPStream(q.device().index()).stream());
+            }
+            TORCH_CHECK(st == SMHA_OK, "smha_sink_backward: status ", (int)st);
+        }
+        torch::autograd::variable_list out = {dq, dk, dv};
+        if (at::GradMode::is_enabled()) {  // (a graph of the gradients is wanted: they have none of their own)
+            for (auto &t : out) t.requires_grad_();
+            out = (*std::make_shared<torch::autograd::DelayedError>("sink_attention cannot be differentiated twice", (int64_t)out.size()))(std::move(out));
+        }
+        out.resize(8);
+        return out;
+    }
+};
+
+// sink_attention(q, k, v, window, n_sink, offsets, lengths, scale) -> the output, a status, or None
+PyObject *sink_attention(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (n != 8 || !entries.sink_forward || at::impl::torch_function_mode_enabled() || c10::impl::TorchDispatchModeTLS::any_modes_set()) Py_RETURN_NONE;
+    if (!plain(args[0]) || !plain(args[1]) || !plain(args[2]) || !PyFloat_CheckExact(args[7])) Py_RETURN_NONE;
+    const at::Tensor &q = THPVariable_Unpack(args[0]), &k = THPVariable_Unpack(args[1]), &v = THPVariable_Unpack(args[2]);
+    SinkCall c{0, 0, (float)PyFloat_AS_DOUBLE(args[7])};
+    if (!int_from(args[3], c.window) || !int_from(args[4], c.n_sink) || !heads_fit(q, k, v)) Py_RETURN_NONE;
+    const int32_t *offsets, *lengths;
+    at::Tensor offsets_t, lengths_t;
+    if (!per_sequence(args[5], q, offsets, offsets_t) || !per_sequence(args[6], q, lengths, lengths_t)) Py_RETURN_NONE;
+    if (!Strides3(q).ok || !Strides3(k).ok || !Strides3(v).ok) Py_RETURN_NONE;
+    const c10::DeviceGuard guard(q.device());
+    at::Tensor o;
+    if (at::GradMode::is_enabled() && (q.requires_grad() || k.requires_grad() || v.requires_grad())) {
+        try {
+            using Maybe = std::optional<at::Tensor>;
+            o = SinkFunction::apply(q, k, v, offsets ? Maybe(offsets_t) : Maybe(), lengths ? Maybe(lengths_t) : Maybe(), (int64_t)c.window, (int64_t)c.n_sink, PyFloat_AS_DOUBLE(args[7]));
+        } catch (const SinkFailed &e) {
+            return PyLong_FromLong((long)e.status);
+        }
+    } else {
+        o = packed_like(q);
+        const smha_status_t st = run_sink_forward(q, k, v, o, nullptr, nullptr, offsets, lengths, c);
+        if (st != SMHA_OK) return PyLong_FromLong((long)st);
+    }
+    return THPVariable_Wrap(std::move(o));
+    END_HANDLE_TH_ERRORS
+}
+
+// cache_attention(q, k, v, lengths, window, n_sink, prefix keys or None, prefix values or None, weights or None, scale) -> the output, a status, or None
+PyObject *cache_attention(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (n != 10 || !entries.cache_forward || at::impl::torch_function_mode_enabled() || c10::impl::TorchDispatchModeTLS::any_modes_set()) Py_RETURN_NONE;
+    if (!plain(args[0]) || !plain(args[1]) || !plain(args[2]) || !PyFloat_CheckExact(args[9])) Py_RETURN_NONE;
+    const at::Tensor &q = THPVariable_Unpack(args[0]), &k = THPVariable_Unpack(args[1]), &v = THPVariable_Unpack(args[2]);
+    if (!heads_fit(q, k, v) || (at::GradMode::is_enabled() && (q.requires_grad() || k.requires_grad() || v.requires_grad()))) Py_RETURN_NONE;
+    const int32_t *lengths;
+    at::Tensor lengths_t;
+    int window, n_sink;
+    if (args[3] == Py_None || !per_sequence(args[3], q, lengths, lengths_t) || !int_from(args[4], window) || !int_from(args[5], n_sink)) Py_RETURN_NONE;
+    const int B = (int)q.size(0), H = (int)q.size(1), T = (int)q.size(2), d = (int)q.size(3), Hkv = (int)k.size(1), Sk = (int)k.size(2);
+    int P = 0;
+    const void *pk = nullptr, *pv = nullptr;
+    if (args[6] != Py_None || args[7] != Py_None) {
+        if (!plain(args[6], 3) || !plain(args[7], 3)) Py_RETURN_NONE;
+        const at::Tensor &a = THPVariable_Unpack(args[6]), &b = THPVariable_Unpack(args[7]);
+        if (a.sizes() != b.sizes() || a.size(0) != Hkv || a.size(2) != d || a.size(1) > INT32_MAX || a.scalar_type() != q.scalar_type() ||
+            b.scalar_type() != q.scalar_type() || a.device() != q.device() || b.device() != q.device() || !a.is_contiguous() || !b.is_contiguous())
+            Py_RETURN_NONE;
+        P = (int)a.size(1);
+        pk = a.data_ptr();
+        pv = b.data_ptr();
+    }
+    float *weights = nullptr;
+    if (args[8] != Py_None) {
+        if (!plain(args[8], 3)) Py_RETURN_NONE;
+        const at::Tensor &w = THPVariable_Unpack(args[8]);
+        if (w.scalar_type() != at::kFloat || w.size(0) != B || w.size(1) != Hkv || w.size(2) != Sk || w.device() != q.device() || !w.is_contiguous()) Py_RETURN_NONE;
+        weights = w.data_ptr<float>();
+    }
+    const Strides3 qs(q), ks(k), vs(v);
+    if (!qs.ok || !ks.ok || !vs.ok) Py_RETURN_NONE;
+    const c10::DeviceGuard guard(q.device());
+    size_t need = 0;
+    smha_status_t st = entries.cache_workspace(B, H, Hkv, T, Sk, P, d, window, n_sink, weights != nullptr, &need);
+    if (st != SMHA_OK) return PyLong_FromLong((long)st);
+    const at::AutoGradMode off(false);
+    at::Tensor o = packed_like(q), ws = at::empty({(int64_t)need}, q.options().dtype(at::kByte));
+    st = entries.cache_forward(q.data_ptr(), k.data_ptr(), v.data_ptr(), pk, pv, o.data_ptr(), weights, lengths, B, H, Hkv, T, Sk, P, d,
+                               (smha_dtype_t)code_of(q.scalar_type()), qs.ptr, ks.ptr, vs.ptr, nullptr, nullptr, nullptr, nullptr, window, n_sink,
+                               (float)PyFloat_AS_DOUBLE(args[9]), ws.data_ptr(), need, c10::hip::getCurrentHIPStream(q.device().index()).stream());
+    if (st != SMHA_OK) return PyLong_FromLong((long)st);
+    return THPVariable_Wrap(std::move(o));
+    END_HANDLE_TH_ERRORS
+}
+
+// cache_evict(k, v, weights, positions, lengths, budget, recent) -> (weights, positions, lengths), a status, or None
+PyObject *cache_evict(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (n != 7 || !entries.cache_evict || at::impl::torch_function_mode_enabled() || c10::impl::TorchDispatchModeTLS::any_modes_set()) Py_RETURN_NONE;
+    if (!plain(args[0]) || !plain(args[1]) || !plain(args[2], 3) || !plain(args[3], 3) || !plain(args[4], 1)) Py_RETURN_NONE;
+    const at::Tensor &k = THPVariable_Unpack(args[0]), &v = THPVariable_Unpack(args[1]), &w = THPVariable_Unpack(args[2]), &p = THPVariable_Unpack(args[3]),
+                     &len = THPVariable_Unpack(args[4]);
+    int budget, recent;
+    if (!int_from(args[5], budget) || !int_from(args[6], recent)) Py_RETURN_NONE;
+    const int type = code_of(k.scalar_type());
+    if ((type != SMHA_F16 && type != SMHA_BF16) || v.scalar_type() != k.scalar_type() || k.sizes() != v.sizes() || v.device() != k.device() || !small_sizes(k)) Py_RETURN_NONE;
+    if (at::GradMode::is_enabled() && (k.requires_grad() || v.requires_grad())) Py_RETURN_NONE;
+    for (const at::Tensor *t : {&w, &p})
+        if (t->sizes() != k.sizes().slice(0, 3) || t->device() != k.device() || !t->is_contiguous()) Py_RETURN_NONE;
+    if (w.scalar_type() != at::kFloat || p.scalar_type() != at::kInt || len.scalar_type() != at::kInt || len.size(0) != k.size(0) || len.device() != k.device() ||
+        !len.is_contiguous())
+        Py_RETURN_NONE;
+    for (const at::Tensor *t : {&k, &v})
+        for (int i = 0; i < 3; ++i)
+            if (t->size(i) > 1 && t->stride(i) < t->size(3)) Py_RETURN_NONE;
+    const Strides3 ks(k), vs(v);
+    if (!ks.ok || !vs.ok) Py_RETURN_NONE;
+    const int B = (int)k.size(0), Hkv = (int)k.size(1), Sk = (int)k.size(2), d = (int)k.size(3);
+    const c10::DeviceGuard guard(k.device());
+    size_t need = 0;
+    smha_status_t st = entries.cache_evict_workspace(B, Hkv, Sk, d, budget, recent, &need);
+    if (st != SMHA_OK) return PyLong_FromLong((long)st);
+    const at::AutoGradMode off(false);
+    at::Tensor w2 = packed_like(w), p2 = packed_like(p), len2 = packed_like(len), ws = at::empty({(int64_t)need}, k.options().dtype(at::kByte));
+    st = entries.cache_evict(k.data_ptr(), v.data_ptr(), w.data_ptr<float>(), p.data_ptr<int32_t>(), len.data_ptr<int32_t>(), w2.data_ptr<float>(),
+                             p2.data_ptr<int32_t>(), len2.data_ptr<int32_t>(), B, Hkv, Sk, d, budget, recent, ks.ptr, vs.ptr, ws.data_ptr(), need,
+                             c10::hip::getCurrentHIPStream(k.device().index()).stream());
+    if (st != SMHA_OK) return PyLong_FromLong((long)st);
+    PyObject *out = PyTuple_New(3);
+    if (!out) return nullptr;
+    PyTuple_SET_ITEM(out, 0, THPVariable_Wrap(std::move(w2)));
+    PyTuple_SET_ITEM(out, 1, THPVariable_Wrap(std::move(p2)));
+    PyTuple_SET_ITEM(out, 2, THPVariable_Wrap(std::move(len2)));
+    return out;
+    END_HANDLE_TH_ERRORS
+}
+
+using Fast = PyObject *(*)(PyObject *, PyObject *const *, Py_ssize_t);
+PyCFunction fast(Fast f) { return reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)); }
+
+PyMethodDef methods[] = {{"link", fast(link), METH_FASTCALL, nullptr}, {"sink_attention", fast(sink_attention), METH_FASTCALL, nullptr},
+                         {"cache_attention", fast(cache_attention), METH_FASTCALL, nullptr}, {"cache_evict", fast(cache_evict), METH_FASTCALL, nullptr},
+                         {"forward", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(forward)), METH_FASTCALL, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_smha_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -9,7 +9,7 @@ import ctypes as C
 
 import torch
 
-from .binding import SMHA_BF16, SMHA_F16, SmhaError, _current_raw_stream, _load
+from .binding import SMHA_BF16, SMHA_F16, SmhaError, _current_raw_stream, _load, native_call
 
 _CODES = {torch.float16: SMHA_F16, torch.bfloat16: SMHA_BF16}
 _PACKED = None
@@ -156,6 +156,9 @@ class _SinkAttention(torch.autograd.Function):
         return dq, dk, dv, None, None, None, None, None
 
 
+_call = None  # the native way, for every call that it takes
+
+
 def sink_attention(q, k, v, window: int = 0, n_sink: int = 0, *, offsets=None, lengths=None, scale: float = 0.0):
     """softmax(scale q k^T over visible keys) v, differentiable in q, k and v.
 
@@ -163,8 +166,16 @@ def sink_attention(q, k, v, window: int = 0, n_sink: int = 0, *, offsets=None, l
     offsets[b] + i (default Sk - Sq + i) and exists where that is in 0 .. lengths[b] - 1 (default Sk); it sees key j iff j is not after it and
     either within the last `window` keys (0: any) or one of the first `n_sink`.  offsets, lengths: int32 [B] on the GPU, read there.  scale: 0
     for 1/sqrt(d).  Queries that do not exist give zeros, and neither they nor keys past a length receive or pass on gradients."""
+    global _call
+    if _call is None:
+        _call = native_call("sink_attention")
+    got = _call(q, k, v, window, n_sink, offsets, lengths, float(scale))
+    if got is not None:
+        if type(got) is int:
+            raise SmhaError(got, "smha_sink_forward")
+        return got
+    _check_qkv(q, k, v)
     if torch.is_grad_enabled() and (q.requires_grad or k.requires_grad or v.requires_grad):
-        _check_qkv(q, k, v)
         return _SinkAttention.apply(q, k, v, window, n_sink, offsets, lengths, scale)
     out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
     smha_sink_forward(q, k, v, out, None, window, n_sink, offsets, lengths, scale)
