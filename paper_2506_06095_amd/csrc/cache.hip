@@ -485,10 +485,6 @@ __global__ void __launch_bounds__(1024) smha_cache_select(const EvictParams p) {
                 Wo[i] = W[i];
                 Po[i] = P[i];
             }
-        for (int i = len + threadIdx.x; i < p.Sk; i += 1024) {
-            Wo[i] = 0.f;
-            Po[i] = -1;
-        }
         return;
     }
     const int n = (len + 1023) / 1024, base = w * 64 * n + lane;  // keys a lane, its first slot
@@ -582,31 +578,72 @@ __global__ void __launch_bounds__(1024) smha_cache_select(const EvictParams p) {
         least |= (uint32_t)found[0] << shift;
         all_over = found[1];
     }
-    // who stays: keys over the least, and the first of those at it
-    int equal = 0;
-    each([&](int, uint32_t k) __attribute__((always_inline)) { equal += __builtin_popcountll(__builtin_amdgcn_ballot_w64(k == least)); });
-    if (lane == 0) totals[w][0] = equal;
+    // Who stays, as a bit of a word for each of up to 32 keys of the lane: those over the least, and the first of those at it.
+    const int equal_stay = end - all_over;
+    const uint64_t below = (1ull << lane) - 1;
+    constexpr int GROUP = KPT ? KPT : 32;  // keys of such a word
+    auto words = [&](int i0, uint32_t &over, uint32_t &equal) __attribute__((always_inline)) {
+        over = equal = 0;
+#pragma unroll
+        for (int i = 0; i < GROUP; ++i) {
+            uint32_t k;
+            if constexpr (KPT > 0) {
+                k = i < n ? held[i] : 0u;
+            } else {
+                const int slot = base + 64 * (i0 + i);
+                k = i0 + i < n && slot < len ? key_from(slot, W[slot], P[slot]) : 0u;
+            }
+            over |= (uint32_t)(k > least) << i;
+            equal |= (uint32_t)(k == least) << i;
+        }
+    };
+    // the place of every set bit of the wave in the order of slots, from `at` on
+    auto in_order = [&](uint32_t word, int &at, auto &&f) __attribute__((always_inline)) {
+        if (__builtin_amdgcn_ballot_w64(word != 0) == 0) return;
+        for (int i = 0; i < GROUP; ++i) {
+            const bool mine = (word >> i) & 1;
+            const uint64_t who = __builtin_amdgcn_ballot_w64(mine);
+            if (who == 0) continue;
+            if (mine) f(i, at + __builtin_popcountll(who & below));
+            at += __builtin_popcountll(who);
+        }
+    };
+    uint32_t over, equal;
+    int count = 0;
+    for (int i0 = 0; i0 < n; i0 += GROUP) {
+        words(i0, over, equal);
+        count += __builtin_popcount(equal);
+    }
+    count = wave_sum(count);
+    if (lane == 0) totals[w][0] = count;
     __syncthreads();
-    int equal_before = 0;
+    int equal_at = 0;
 #pragma unroll
     for (int u = 0; u < 16; ++u)
-        if (u < w) equal_before += totals[u][0];
-    const int equal_stay = end - all_over;  // the first so many of those at the least
-    const uint64_t below = (1ull << lane) - 1;
-    // freed slots before the end, kept slots from it on, per wave
-    int freed = 0, kept = 0, equal_at = equal_before;
-    auto stays = [&](uint32_t k, int &eq) __attribute__((always_inline)) {
-        const uint64_t same = __builtin_amdgcn_ballot_w64(k == least);
-        const bool yes = k > least || (k == least && eq + __builtin_popcountll(same & below) < equal_stay);
-        eq += __builtin_popcountll(same);
-        return yes;
+        if (u < w) equal_at += totals[u][0];
+    const int equal_first = equal_at;
+    // bits of `over` and of the equals that stay
+    auto staying = [&](int i0) __attribute__((always_inline)) {
+        words(i0, over, equal);
+        uint32_t stay = over;
+        in_order(equal, equal_at, [&](int i, int place) __attribute__((always_inline)) {
+            if (place < equal_stay) stay |= 1u << i;
+        });
+        return stay;
     };
-    each([&](int i, uint32_t k) __attribute__((always_inline)) {
-        const int slot = base + 64 * i;
-        const bool yes = stays(k, equal_at) && slot < len;
-        freed += __builtin_popcountll(__builtin_amdgcn_ballot_w64(!yes && slot < end));
-        kept += __builtin_popcountll(__builtin_amdgcn_ballot_w64(yes && slot >= end));
-    });
+    // of the group's keys, those in slots before the end
+    // (a lane has n keys: later bits of a word are other waves' slots)
+    auto before_end = [&](int i0) __attribute__((always_inline)) { return low_bits32(min((end - (base + 64 * i0) + 63) >> 6, n - i0)); };
+    int freed = 0, kept = 0;
+    uint32_t stay = 0;
+    for (int i0 = 0; i0 < n; i0 += GROUP) {
+        stay = staying(i0);
+        const uint32_t early = before_end(i0);
+        freed += __builtin_popcount(~stay & early);
+        kept += __builtin_popcount(stay & ~early);
+    }
+    freed = wave_sum(freed);
+    kept = wave_sum(kept);
     __syncthreads();
     if (lane == 0) {
         totals[w][0] = freed;
@@ -619,20 +656,28 @@ __global__ void __launch_bounds__(1024) smha_cache_select(const EvictParams p) {
         if (u < w) to += totals[u][0], from += totals[u][1];
         moves += totals[u][0];
     }
-    equal_at = equal_before;
-    each([&](int i, uint32_t k) __attribute__((always_inline)) {
-        const int slot = base + 64 * i;
-        const bool yes = stays(k, equal_at) && slot < len, out = !yes && slot < end, in = yes && slot >= end;
-        const uint64_t outs = __builtin_amdgcn_ballot_w64(out), ins = __builtin_amdgcn_ballot_w64(in);
-        if (out) list[1 + to + __builtin_popcountll(outs & below)] = slot;
-        if (in) list[1 + p.moves + from + __builtin_popcountll(ins & below)] = slot;
-        to += __builtin_popcountll(outs);
-        from += __builtin_popcountll(ins);
-        if (copies && yes && slot < end) {
-            Wo[slot] = W[slot];
-            Po[slot] = P[slot];
+    equal_at = equal_first;
+    for (int i0 = 0; i0 < n; i0 += GROUP) {
+        if constexpr (KPT == 0) stay = staying(i0);
+        const uint32_t early = before_end(i0);
+        in_order(~stay & early, to, [&](int i, int place) __attribute__((always_inline)) { list[1 + place] = base + 64 * (i0 + i); });
+        in_order(stay & ~early, from, [&](int i, int place) __attribute__((always_inline)) { list[1 + p.moves + place] = base + 64 * (i0 + i); });
+        if (copies) {
+#pragma unroll
+            for (int i = 0; i < GROUP; ++i) {
+                const int slot = base + 64 * (i0 + i);
+                if ((stay & early) >> i & 1) {
+                    if constexpr (KPT > 0 && KPT < 32) {  // (32 of each would not fit the registers)
+                        Wo[slot] = held_w[i];
+                        Po[slot] = held_p[i];
+                    } else {
+                        Wo[slot] = W[slot];
+                        Po[slot] = P[slot];
+                    }
+                }
+            }
         }
-    });
+    }
     if (threadIdx.x == 0) list[0] = moves;
     __syncthreads();
     for (int i = threadIdx.x; i < moves; i += 1024) {
@@ -640,17 +685,13 @@ __global__ void __launch_bounds__(1024) smha_cache_select(const EvictParams p) {
         Wo[to_slot] = W[from_slot];
         Po[to_slot] = P[from_slot];
     }
-    __syncthreads();
-    for (int i = end + threadIdx.x; i < p.Sk; i += 1024) {
-        Wo[i] = 0.f;
-        Po[i] = -1;
-    }
 }
 
-// K and V rows along the lists: what is read lies past the new end, what is written before it.
+// K and V rows along the lists: what is read lies past the new end, what is written before it.  And what lies past it afterwards.
 __global__ void __launch_bounds__(256) smha_cache_move(const EvictParams p) {
     const int bh = blockIdx.y, b = bh / p.Hkv, hk = bh - b * p.Hkv;
-    if (blockIdx.x == 0 && hk == 0 && threadIdx.x == 0) p.len_out[b] = min(min(max(p.lengths[b], 0), p.Sk), p.budget);
+    const int end = min(min(max(p.lengths[b], 0), p.Sk), p.budget);  // (the same where len_out is lengths and has been written already)
+    if (blockIdx.x == 0 && hk == 0 && threadIdx.x == 0) p.len_out[b] = end;
     const int32_t *const list = p.lists + (int64_t)bh * (1 + 2 * (int64_t)p.moves);
     const int n = list[0], lane = threadIdx.x & 15;
     uint16_t *const K = p.K + b * p.ks.b + hk * p.ks.h, *const V = p.V + b * p.vs.b + hk * p.vs.h;
@@ -661,6 +702,10 @@ __global__ void __launch_bounds__(256) smha_cache_move(const EvictParams p) {
             *reinterpret_cast<u32x4 *>(K + to * p.ks.s + 8 * lane) = k;
             *reinterpret_cast<u32x4 *>(V + to * p.vs.s + 8 * lane) = v;
         }
+    }
+    for (int i = end + (int)(blockIdx.x * 256 + threadIdx.x); i < p.Sk; i += (int)gridDim.x * 256) {
+        p.w_out[(int64_t)bh * p.Sk + i] = 0.f;
+        p.pos_out[(int64_t)bh * p.Sk + i] = -1;
     }
 }
 
