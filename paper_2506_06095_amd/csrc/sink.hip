@@ -12,11 +12,13 @@
 // B operand as they stand (P and dS never go through LDS), and tiles sit in LDS row-major, chunks of 16 bytes swizzled so that both
 // ways of reading them are spread over the banks: rows 16 bytes at a time (A operand of the first products), and transposing reads
 // of 4 rows x 16 columns (A operand of the second ones).  See smha_block_fwd for the operand layouts.
+// Kernels <D, C> keep rows of D columns in LDS and form products over C of them, 32, 64, 96 or 128, the next above the head size.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <type_traits>
 
 #include "device_common.hpp"
 #include "smha.h"
@@ -39,7 +41,8 @@ struct SinkParams {
     float *stats;         // [2][B][H][Sqp]: lse * log2(e) (inf where there is no query), delta
     int Sqp;
     float *parts;         // partial dK, dV of key tiles that are cut along their queries
-    int n_tiles, n_sink_tiles, chunk, cut_sink, cut_rest;  // key tiles, those with sinks; steps of a part; parts at most
+    int n_tiles, n_sink_tiles;              // key tiles, those with sinks
+    int chunk_sink, chunk_rest, cut_sink, cut_rest;  // steps of a part, parts at most: of a tile with sinks, of another
 };
 
 struct Sequence {
@@ -67,9 +70,9 @@ __device__ __forceinline__ bool all_seen(int p0, int p1, int k0, int k1, int win
     return k1 <= p0 && (p1 - k0 < window || k1 < n_sink);
 }
 
-// A tile of 64 rows into LDS by a workgroup's four waves: wave w brings the 1 KiB blocks w, w + 4, ...
-template <int D> struct TileLoad {
-    static constexpr int CPR = D / 8, LPW = CPR / 4, RSTEP = 4 * 64 / CPR;  // chunks a row, loads a wave, rows between two of its loads
+// A tile of ROWS rows into LDS by a workgroup's four waves: wave w brings the 1 KiB blocks w, w + 4, ...
+template <int D, int ROWS = 64> struct TileLoad {
+    static constexpr int CPR = D / 8, LPW = CPR * ROWS / 256, RSTEP = 4 * 64 / CPR;  // chunks a row, loads a wave, rows between two of its loads
     uint32_t go;  // the lane's offset in the wave's first block
     int row;
     __device__ __forceinline__ TileLoad(int w, int lane, int row_bytes, int d) {
@@ -77,7 +80,7 @@ template <int D> struct TileLoad {
         const int c = (lane % CPR) ^ swz_both<D>(row);
         go = c < (d >> 3) ? (uint32_t)(row * row_bytes + c * 16) : kNoChunk;
     }
-    // rows r0 .. r0 + 63; those in [gap0, gap1) read as zeros, as do those past the buffer
+    // rows r0 ..; those in [gap0, gap1) read as zeros, as do those past the buffer
     __device__ __forceinline__ void operator()(u32x4 rsrc, uint32_t lds, int w, int r0, int row_bytes, int gap0, int gap1) const {
 #pragma unroll
         for (int i = 0; i < LPW; ++i) {
@@ -99,12 +102,12 @@ __device__ __forceinline__ void tiles_landed() {
 // A wave's 32 x D accumulators (acc[dt][r] = row j, column 32 dt + 8 (r / 4) + 4 hh + r % 4) to rows row0 .. of a tensor with 16-bit values,
 // through 32 rows of LDS so that whole rows are written; rows from `rows` on are left out.
 // REST: not the rounded values, but what their rounding leaves out.
-template <int D, bool BF16, bool REST = false>
-__device__ __forceinline__ void store_rows(const f32x16 (&acc)[D / 32], float factor, char *slab, int lane, uint16_t *base, int64_t pitch, int row0, int rows, int d) {
+template <int D, int C, bool BF16, bool REST = false>
+__device__ __forceinline__ void store_rows(const f32x16 (&acc)[C / 32], float factor, char *slab, int lane, uint16_t *base, int64_t pitch, int row0, int rows, int d) {
     constexpr int CPR = D / 8;
     const int j = lane & 31, hh = lane >> 5;
 #pragma unroll
-    for (int dt = 0; dt < D / 32; ++dt)
+    for (int dt = 0; dt < C / 32; ++dt)
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
             float x[4];
@@ -127,12 +130,12 @@ __device__ __forceinline__ void store_rows(const f32x16 (&acc)[D / 32], float fa
 }
 
 // A wave's 32 rows as the B operand of products over the columns: lane (j, hh) holds columns 16 s + 8 hh .. of row j.  Rows outside [a, b) are zeros.
-template <int D>
-__device__ __forceinline__ void load_operand(u32x4 (&f)[D / 16], const uint16_t *base, int64_t pitch, int row0, int a, int b, int d, int lane) {
+template <int C>
+__device__ __forceinline__ void load_operand(u32x4 (&f)[C / 16], const uint16_t *base, int64_t pitch, int row0, int a, int b, int d, int lane) {
     const __amdgpu_buffer_rsrc_t r = make_rsrc(base, b > 0 ? ((int64_t)(b - 1) * pitch + d) * 2 : 0);
     const int j = lane & 31, hh = lane >> 5, row = row0 + j;
 #pragma unroll
-    for (int s = 0; s < D / 16; ++s)
+    for (int s = 0; s < C / 16; ++s)
         f[s] = buf_load16(r, row >= a && row < b && 16 * s + 8 * hh < d ? (int)(row * pitch * 2) + 32 * s + 16 * hh : (int)kPast);
 }
 
@@ -144,10 +147,10 @@ __device__ __forceinline__ void load_operand(u32x4 (&f)[D / 16], const uint16_t 
 // queries do not see, and forms masks only on tiles that they see in part.
 // P is rounded to the inputs' type for the second product: half a step, 2^-9 (bfloat16) or 2^-12 (binary16) of each weight, independent
 // from weight to weight, which leaves the output as far off as its own rounding does.  Sums and statistics are 32 bits.
-template <int D, bool BF16>
+template <int D, int C, bool BF16>
 __global__ void __launch_bounds__(256, D == 64 ? 4 : 2) smha_sink_fwd(const SinkParams p) {
-    constexpr int NS = D / 16, NDT = D / 32, TB = 64 * D * 2;
-    constexpr int PF = D == 128 ? 8 : 4;
+    constexpr int NS = C / 16, NDT = C / 32, TB = 64 * D * 2;
+    constexpr int PF = C == 128 ? 8 : 4;  // operands requested ahead
     __shared__ __attribute__((aligned(1024))) char smem[4 * TB];  // K[0], K[1], V[0], V[1]
     const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_void *)smem;
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = lane & 31, hh = lane >> 5;
@@ -185,7 +188,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 4 : 2) smha_sink_fwd(const Sink
         loadV(rV, lds0 + 2 * TB, w, key_of(0), vsb, gap0, gap1);
     }
     u32x4 qf[NS];
-    load_operand<D>(qf, p.Q + b * p.qs.b + h * p.qs.h, p.qs.s, qw, s.qa, s.qb, p.d, lane);
+    load_operand<C>(qf, p.Q + b * p.qs.b + h * p.qs.h, p.qs.s, qw, s.qa, s.qb, p.d, lane);
 
     const int rd = j * D * 2 + ((hh ^ swz_both<D>(j)) * 16);
     const int tr_row = 4 * hh + ((lane & 15) >> 2);
@@ -279,8 +282,8 @@ __global__ void __launch_bounds__(256, D == 64 ? 4 : 2) smha_sink_fwd(const Sink
     if (p.lse && hh == 0 && qw + j < p.Sq)
         p.lse[(int64_t)bh * p.Sq + qw + j] = l > 0.f ? (m_run * p.c + __builtin_amdgcn_logf(l)) * 0.6931471805599453f : NEG_INF;
     const float inv = l > 0.f ? 1.0f / l : 0.f;
-    store_rows<D, BF16>(o, inv, smem + w * (32 * D * 2), lane, p.O + b * p.os.b + h * p.os.h, p.os.s, qw, p.Sq, p.d);
-    if (p.rest) store_rows<D, BF16, true>(o, inv, smem + w * (32 * D * 2), lane, p.rest + (int64_t)bh * p.Sq * p.d, p.d, qw, p.Sq, p.d);
+    store_rows<D, C, BF16>(o, inv, smem + w * (32 * D * 2), lane, p.O + b * p.os.b + h * p.os.h, p.os.s, qw, p.Sq, p.d);
+    if (p.rest) store_rows<D, C, BF16, true>(o, inv, smem + w * (32 * D * 2), lane, p.rest + (int64_t)bh * p.Sq * p.d, p.d, qw, p.Sq, p.d);
 }
 
 // ---------------------------------------------------------------------------------------
@@ -319,9 +322,9 @@ __global__ void __launch_bounds__(256) smha_sink_stats(const SinkParams p) {
 
 // dQ: four waves of 32 queries over the same key tiles as the forward; a lane owns a query, so lse and delta are its own two registers.
 // dS is rounded to the inputs' type for the product with K, as P is in the forward.
-template <int D, bool BF16>
+template <int D, int C, bool BF16>
 __global__ void __launch_bounds__(256, 2) smha_sink_bwd_q(const SinkParams p) {
-    constexpr int NS = D / 16, NDT = D / 32, TB = 64 * D * 2;
+    constexpr int NS = C / 16, NDT = C / 32, TB = 64 * D * 2;
     __shared__ __attribute__((aligned(1024))) char smem[4 * TB];  // K[0], K[1], V[0], V[1]
     const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_void *)smem;
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = lane & 31, hh = lane >> 5;
@@ -354,8 +357,8 @@ __global__ void __launch_bounds__(256, 2) smha_sink_bwd_q(const SinkParams p) {
         loadV(rV, lds0 + 2 * TB, w, key_of(0), vsb, gap0, gap1);
     }
     u32x4 qf[NS], gf[NS];
-    load_operand<D>(qf, p.Q + b * p.qs.b + h * p.qs.h, p.qs.s, qw, s.qa, s.qb, p.d, lane);
-    load_operand<D>(gf, p.dO + b * p.gs.b + h * p.gs.h, p.gs.s, qw, s.qa, s.qb, p.d, lane);
+    load_operand<C>(qf, p.Q + b * p.qs.b + h * p.qs.h, p.qs.s, qw, s.qa, s.qb, p.d, lane);
+    load_operand<C>(gf, p.dO + b * p.gs.b + h * p.gs.h, p.gs.s, qw, s.qa, s.qb, p.d, lane);
     const int64_t row = (int64_t)bh * p.Sqp + qw + j;
     const float lse2 = p.stats[row], delta = p.stats[(int64_t)p.B * p.H * p.Sqp + row];
 
@@ -404,10 +407,10 @@ __global__ void __launch_bounds__(256, 2) smha_sink_bwd_q(const SinkParams p) {
         }
         tiles_landed();
     }
-    store_rows<D, BF16>(dq, p.scale, smem + w * (32 * D * 2), lane, p.dQ + b * p.dqs.b + h * p.dqs.h, p.dqs.s, qw, p.Sq, p.d);
+    store_rows<D, C, BF16>(dq, p.scale, smem + w * (32 * D * 2), lane, p.dQ + b * p.dqs.b + h * p.dqs.h, p.dqs.s, qw, p.Sq, p.d);
 }
 
-// The queries that see a tile of 128 keys, as steps of 64 queries of one head: qt0 .. qt0 + nq - 1 of each of the G heads.
+// The queries that see a tile of 128 keys, as steps of 32 queries of one head: qt0 .. qt0 + nq - 1 of each of the G heads.
 struct KeyTile {
     int qt0, nq;
 };
@@ -418,18 +421,24 @@ __device__ __forceinline__ KeyTile key_tile(const SinkParams &p, const Sequence 
     int qb = s.qb;
     if (k0 >= p.n_sink) qb = min(qb, k1 + p.window - s.off);
     if (k0 >= s.len || qa >= qb) return {0, 0};
-    return {qa / 64, (qb - 1) / 64 - qa / 64 + 1};
+    return {qa / 32, (qb - 1) / 32 - qa / 32 + 1};
 }
 
-// dK and dV: four waves of 32 keys each, K and V in registers as B operands, over 64-query tiles of Q and dO (and their lse and
-// delta) in LDS, two of each.  A lane owns a key.  A tile's steps (its queries, head by head) may be cut into parts that other
-// workgroups take: the sinks' tiles are seen by every query, and few key heads would leave most of the chip idle.
-// Parts go to memory in 32 bits and are added in order by smha_sink_sum.
-template <int D, bool BF16>
-__global__ void __launch_bounds__(256, 2) smha_sink_bwd_kv(const SinkParams p) {
-    constexpr int NS = D / 16, NDT = D / 32, TB = 64 * D * 2;
-    __shared__ __attribute__((aligned(1024))) char smem[4 * TB];           // Q[0], Q[1], dO[0], dO[1]
-    __shared__ __attribute__((aligned(1024))) float stats[2][2][64];       // [buffer][lse, delta][query]
+// Parts of `chunk` steps at most, all alike.
+__device__ __forceinline__ int parts_of(int steps, int cut, int chunk) { return max(1, min(cut, (steps + chunk - 1) / chunk)); }
+
+// dK and dV: four waves of 32 keys each over 32-query tiles of Q and dO (and their lse and delta) in LDS, two of each.  A lane owns a key.
+// At 128 columns a wave holds 128 registers of dK and dV; V's 32 beside them leave room for operands that are requested four products
+// ahead, K's do not, and so K stays in LDS (with both in registers every product waited for its operand, and what had spilled was waited for
+// with the tile in flight: 1090 us for 1 x 32 x 8192 x 128, window 4096).  The exponentials run under the product that gives dP, the rest of
+// dS under the one that gives dV.
+// A tile's steps (its queries, head by head) may be cut into parts that other workgroups take: the sinks' tiles are seen by every
+// query, and few key heads would leave most of the chip idle.  Parts go to memory in 32 bits and are added in order by smha_sink_sum.
+template <int D, int C, bool BF16>
+__global__ void __launch_bounds__(256, D == 64 ? 3 : 2) smha_sink_bwd_kv(const SinkParams p) {
+    constexpr int NS = C / 16, NDT = C / 32, TB = 32 * D * 2, PF = 4;
+    __shared__ __attribute__((aligned(1024))) char smem[4 * TB + 4 * TB];  // K, Q[0], Q[1], dO[0], dO[1]
+    __shared__ __attribute__((aligned(1024))) float stats[2][2][64];       // [buffer][lse, delta][query] (32 of 64)
     const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_void *)smem, stats0 = (uint32_t)(uintptr_t)(lds_void *)stats;
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = lane & 31, hh = lane >> 5;
 
@@ -451,110 +460,161 @@ __global__ void __launch_bounds__(256, 2) smha_sink_bwd_kv(const SinkParams p) {
     const Sequence s = sequence(p, b);
     const int window = p.window, n_sink = p.n_sink, k0 = tile * 128;
     const KeyTile kt = key_tile(p, s, k0);
-    const int steps = kt.nq * p.G, begin = part * p.chunk, end = cut == 1 ? steps : min(steps, begin + p.chunk);
-    if (part > 0 && begin >= end) return;
-    const bool alone = steps <= p.chunk || cut == 1;
+    const int steps = kt.nq * p.G, parts = parts_of(steps, cut, tile < p.n_sink_tiles ? p.chunk_sink : p.chunk_rest);
+    if (part >= parts) return;
+    const int begin = (int)((int64_t)steps * part / parts), end = (int)((int64_t)steps * (part + 1) / parts);
 
     const int kw = k0 + 32 * w;
-    u32x4 kf[NS], vf[NS];
-    load_operand<D>(kf, p.K + b * p.ks.b + hk * p.ks.h, p.ks.s, kw, 0, s.len, p.d, lane);
-    load_operand<D>(vf, p.V + b * p.vs.b + hk * p.vs.h, p.vs.s, kw, 0, s.len, p.d, lane);
     const int qsb = (int)p.qs.s * 2, gsb = (int)p.gs.s * 2;
-    const TileLoad<D> loadQ(w, lane, qsb, p.d), loadG(w, lane, gsb, p.d);
+    const TileLoad<D, 32> loadQ(w, lane, qsb, p.d), loadG(w, lane, gsb, p.d);
     const int64_t rows = (int64_t)p.B * p.H * p.Sqp;
+    constexpr int Q_AT = 4 * TB, G_AT = 6 * TB;
     auto request = [&](int g, int q, int par) __attribute__((always_inline)) {
         const int h = hk * p.G + g;
         const u32x4 rQ = make_rsrc4(p.Q + b * p.qs.b + h * p.qs.h, ((int64_t)(s.qb - 1) * p.qs.s + p.d) * 2);
         const u32x4 rG = make_rsrc4(p.dO + b * p.gs.b + h * p.gs.h, ((int64_t)(s.qb - 1) * p.gs.s + p.d) * 2);
-        loadQ(rQ, lds0 + par * TB, w, q, qsb, 0, s.qa);
-        loadG(rG, lds0 + (2 + par) * TB, w, q, gsb, 0, s.qa);
-        if (w < 2) {
+        loadQ(rQ, lds0 + Q_AT + par * TB, w, q, qsb, 0, s.qa);
+        loadG(rG, lds0 + G_AT + par * TB, w, q, gsb, 0, s.qa);
+        if (w < 2) {  // (64 queries' worth, of which the first 32 are used)
             const u32x4 rS = make_rsrc4(p.stats + w * rows + ((int64_t)b * p.H + h) * p.Sqp, (int64_t)p.Sqp * 4);
             load_words_to_lds(rS, stats0 + (par * 2 + w) * 256, (uint32_t)((q + lane) * 4));
         }
     };
     int g = 0, qt = 0;
+    u32x4 vf[NS];
+    load_operand<C>(vf, p.V + b * p.vs.b + hk * p.vs.h, p.vs.s, kw, 0, s.len, p.d, lane);
     if (begin < end) {
+        const int ksb = (int)p.ks.s * 2;
+        const TileLoad<D, 128> loadK(w, lane, ksb, p.d);
+        loadK(make_rsrc4(p.K + b * p.ks.b + hk * p.ks.h, ((int64_t)(s.len - 1) * p.ks.s + p.d) * 2), lds0, w, k0, ksb, 0, 0);
         g = begin / kt.nq;
         qt = begin - g * kt.nq;
-        request(g, 64 * (kt.qt0 + qt), 0);
+        request(g, 32 * (kt.qt0 + qt), 0);
     }
-    const int rd = j * D * 2 + ((hh ^ swz_both<D>(j)) * 16);
+    const int rd_ = j * D * 2 + ((hh ^ swz_both<D>(j)) * 16);
     const int tr_row = 4 * hh + ((lane & 15) >> 2);
-    const int tr = tr_row * D * 2 + ((swz_both<D>(tr_row) ^ (2 * ((lane >> 4) & 1) + ((lane & 3) >> 1))) * 16) + (lane & 1) * 8;
+    const int tr_ = tr_row * D * 2 + ((swz_both<D>(tr_row) ^ (2 * ((lane >> 4) & 1) + ((lane & 3) >> 1))) * 16) + (lane & 1) * 8;
+    const char *const Kt = smem + w * TB;
     f32x16 dk[NDT], dv[NDT];
 #pragma unroll
     for (int dt = 0; dt < NDT; ++dt) dk[dt] = dv[dt] = zeros16();
     tiles_landed();
     for (int t = begin; t < end; ++t) {
-        const int par = (t - begin) & 1, q64 = 64 * (kt.qt0 + qt);
+        const int par = (t - begin) & 1, q = 32 * (kt.qt0 + qt);
         if (++qt == kt.nq) qt = 0, ++g;
-        if (t + 1 < end) request(g, 64 * (kt.qt0 + qt), par ^ 1);
-#pragma unroll
-        for (int sub = 0; sub < 2; ++sub) {
-            const int q = q64 + 32 * sub, p0 = s.off + max(q, s.qa), p1 = s.off + min(q + 32, s.qb) - 1;
-            if (p0 > p1 || !any_seen(p0, p1, kw, kw + 31, window, n_sink)) continue;
-            const char *const Qt = smem + par * TB + sub * (TB / 2), *const Gt = smem + (2 + par) * TB + sub * (TB / 2);
+        if (t + 1 < end) request(g, 32 * (kt.qt0 + qt), par ^ 1);
+        const int p0 = s.off + max(q, s.qa), p1 = s.off + min(q + 32, s.qb) - 1;
+        if (p0 <= p1 && any_seen(p0, p1, kw, kw + 31, window, n_sink)) {
+            const char *const Qt = smem + Q_AT + par * TB, *const Gt = smem + G_AT + par * TB;
+            int rd = rd_, tr = tr_;
+            asm volatile("" : "+v"(rd), "+v"(tr));  // (operand addresses are made here, not kept in registers across steps)
+            auto row_frag = [&](const char *base, int i) __attribute__((always_inline)) { return *reinterpret_cast<const u32x4 *>(base + (rd ^ (32 * i))); };
+            auto col_frag = [&](const char *base, int i) __attribute__((always_inline)) {  // i = cu NDT + dt: queries 16 cu + 8 a + 4 hh .., columns 32 dt + j
+                const int cu = i / NDT, dt = i % NDT;
+                const u32x2 lo = lds_read_tr(reinterpret_cast<const uint16_t *>(base + ((tr ^ (64 * dt)) + 32 * cu * D)));
+                const u32x2 hi = lds_read_tr(reinterpret_cast<const uint16_t *>(base + ((tr ^ (64 * dt) ^ 32) + 32 * cu * D + 16 * D)));
+                return u32x4{lo[0], lo[1], hi[0], hi[1]};
+            };
+            // The left operands of the step's products, in their order: Q's rows, dO's rows, dO's columns, Q's columns.
+            auto operand = [&](int n) __attribute__((always_inline)) {
+                return n < NS ? row_frag(Qt, n) : n < 2 * NS ? row_frag(Gt, n - NS) : n < 2 * NS + 2 * NDT ? col_frag(Gt, n - 2 * NS) : col_frag(Qt, n - 2 * NS - 2 * NDT);
+            };
+            constexpr int ALL = 2 * NS + 4 * NDT;
+            u32x4 f[PF], fk[PF];
+            auto next = [&](int n) __attribute__((always_inline)) {  // product n has its operand: the one PF on is requested
+                if (n + PF < ALL) f[n % PF] = operand(n + PF);
+            };
             // sc[r] = score of key j and query 8 (r / 4) + 4 hh + r % 4
             f32x16 sc = zeros16(), dp = zeros16();
 #pragma unroll
-            for (int i = 0; i < NS; ++i) sc = mfma32<BF16>(*reinterpret_cast<const u32x4 *>(Qt + (rd ^ (32 * i))), kf[i], sc);
-#pragma unroll
-            for (int i = 0; i < NS; ++i) dp = mfma32<BF16>(*reinterpret_cast<const u32x4 *>(Gt + (rd ^ (32 * i))), vf[i], dp);
-            f32x16 ds;
-#pragma unroll
-            for (int r4 = 0; r4 < 4; ++r4) {
-                const f32x4 l = *reinterpret_cast<const f32x4 *>(&stats[par][0][32 * sub + 8 * r4 + 4 * hh]);
-                const f32x4 dl = *reinterpret_cast<const f32x4 *>(&stats[par][1][32 * sub + 8 * r4 + 4 * hh]);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    sc[4 * r4 + e] = fast_exp2(fmaf(sc[4 * r4 + e], p.c, -l[e]));
-                    ds[4 * r4 + e] = sc[4 * r4 + e] * (dp[4 * r4 + e] - dl[e]);
-                }
+            for (int i = 0; i < PF; ++i) {
+                if (i < NS) fk[i] = row_frag(Kt, i);
+                f[i] = operand(i);
             }
-            if (!all_seen(s.off + q, s.off + q + 31, kw, kw + 31, window, n_sink) || q < s.qa || q + 32 > s.qb) {
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < NS; ++i) {
+                sc = mfma32<BF16>(f[i % PF], fk[i % PF], sc);
+                if (i + PF < NS) fk[i % PF] = row_frag(Kt, i + PF);
+                next(i);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            const float *const lse_at = &stats[par][0][4 * hh], *const delta_at = &stats[par][1][4 * hh];
+            f32x4 of[2];  // lse, then delta: of[r4 & 1] is that of accumulators 4 r4 .. 4 r4 + 3
+            of[0] = *reinterpret_cast<const f32x4 *>(lse_at);
+            const bool part_seen = !all_seen(s.off + q, s.off + q + 31, kw, kw + 31, window, n_sink) || q < s.qa || q + 32 > s.qb;
+            uint32_t word = ~0u;
+            if (part_seen) {
                 // queries at or after this key (or those that exist), and in whose window it is
-                const int k = kw + j, at = s.off + q;
-                const uint32_t within = k < n_sink ? ~0u : low_bits32(k + window - at);
-                const uint32_t word = within & ~low_bits32(max(k - at, s.qa - q)) & low_bits32(s.qb - q);
-                const u32x16 keep = keep_of(word >> (4 * hh));
-                sc = __builtin_bit_cast(f32x16, __builtin_bit_cast(u32x16, sc) & keep);
-                ds = __builtin_bit_cast(f32x16, __builtin_bit_cast(u32x16, ds) & keep);
+                int me;  // (the lane's number, made here: kept across steps it would be one register too many)
+                asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=&v"(me));
+                const int k = kw + (me & 31), at = s.off + q;
+                word = (k < n_sink ? ~0u : low_bits32(k + window - at)) & ~low_bits32(max(k - at, s.qa - q)) & low_bits32(s.qb - q);
+                const u32x16 keep = keep_of(word >> (4 * hh)), raw = __builtin_bit_cast(u32x16, sc);
+                sc = __builtin_bit_cast(f32x16, (raw & keep) | (~keep & 0xFF800000u));
             }
-            u32x4 pf[2], sf[2];
+            __builtin_amdgcn_sched_barrier(0);
+            // dP, and P from the scores
+            u32x4 pf[2];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                pf[i >> 2][i & 3] = pack2<BF16>(sc[2 * i], sc[2 * i + 1]);
-                sf[i >> 2][i & 3] = pack2<BF16>(ds[2 * i], ds[2 * i + 1]);
+            for (int i = 0; i < NS; ++i) {
+                dp = mfma32<BF16>(f[(NS + i) % PF], vf[i], dp);
+                next(NS + i);
+#pragma unroll
+                for (int r = 16 * i / NS; r < 16 * (i + 1) / NS; ++r) {
+                    if (r % 4 == 0 && r < 12) of[(r / 4 + 1) & 1] = *reinterpret_cast<const f32x4 *>(lse_at + 2 * r + 8);
+                    sc[r] = fast_exp2(fmaf(sc[r], p.c, -of[(r / 4) & 1][r % 4]));
+                }
+                __builtin_amdgcn_sched_barrier(0);
             }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) pf[i >> 2][i & 3] = pack2<BF16>(sc[2 * i], sc[2 * i + 1]);
+            of[0] = *reinterpret_cast<const f32x4 *>(delta_at);
+            __builtin_amdgcn_sched_barrier(0);
+            // dV, and dS from P and dP
 #pragma unroll
             for (int i = 0; i < 2 * NDT; ++i) {
-                const int cu = i / NDT, dt = i % NDT, at = (tr ^ (64 * dt)) + 32 * cu * D, at8 = (tr ^ (64 * dt) ^ 32) + 32 * cu * D + 16 * D;
-                const u32x2 lo = lds_read_tr(reinterpret_cast<const uint16_t *>(Gt + at)), hi = lds_read_tr(reinterpret_cast<const uint16_t *>(Gt + at8));
-                dv[dt] = mfma32<BF16>(u32x4{lo[0], lo[1], hi[0], hi[1]}, pf[cu], dv[dt]);
-                const u32x2 lo2 = lds_read_tr(reinterpret_cast<const uint16_t *>(Qt + at)), hi2 = lds_read_tr(reinterpret_cast<const uint16_t *>(Qt + at8));
-                dk[dt] = mfma32<BF16>(u32x4{lo2[0], lo2[1], hi2[0], hi2[1]}, sf[cu], dk[dt]);
+                dv[i % NDT] = mfma32<BF16>(f[(2 * NS + i) % PF], pf[i / NDT], dv[i % NDT]);
+                next(2 * NS + i);
+#pragma unroll
+                for (int r = 16 * i / (2 * NDT); r < 16 * (i + 1) / (2 * NDT); ++r) {
+                    if (r % 4 == 0 && r < 12) of[(r / 4 + 1) & 1] = *reinterpret_cast<const f32x4 *>(delta_at + 2 * r + 8);
+                    dp[r] = sc[r] * (dp[r] - of[(r / 4) & 1][r % 4]);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if (part_seen) {  // (where P is zero dP may be anything)
+                const u32x16 keep = keep_of(word >> (4 * hh));
+                dp = __builtin_bit_cast(f32x16, __builtin_bit_cast(u32x16, dp) & keep);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) pf[i >> 2][i & 3] = pack2<BF16>(dp[2 * i], dp[2 * i + 1]);
+#pragma unroll
+            for (int i = 0; i < 2 * NDT; ++i) {
+                dk[i % NDT] = mfma32<BF16>(f[(2 * NS + 2 * NDT + i) % PF], pf[i / NDT], dk[i % NDT]);
+                next(2 * NS + 2 * NDT + i);
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
         tiles_landed();
     }
-    if (alone) {
-        char *const slab = smem + w * (32 * D * 2);
-        store_rows<D, BF16>(dv, 1.f, slab, lane, p.dV + b * p.dvs.b + hk * p.dvs.h, p.dvs.s, kw, p.Sk, p.d);
-        store_rows<D, BF16>(dk, p.scale, slab, lane, p.dK + b * p.dks.b + hk * p.dks.h, p.dks.s, kw, p.Sk, p.d);
+    if (parts == 1) {
+        char *const slab = smem + w * TB;
+        store_rows<D, C, BF16>(dv, 1.f, slab, lane, p.dV + b * p.dvs.b + hk * p.dvs.h, p.dvs.s, kw, p.Sk, p.d);
+        store_rows<D, C, BF16>(dk, p.scale, slab, lane, p.dK + b * p.dks.b + hk * p.dks.h, p.dks.s, kw, p.Sk, p.d);
         return;
     }
     // [item][dV, dK][wave][4 accumulators][lane][4]
-    float *const mine = p.parts + ((int64_t)idx * 2 * 4 + w) * (D / 8) * 256 + lane * 4;
+    float *const mine = p.parts + ((int64_t)idx * 2 * 4 + w) * (C / 8) * 256 + lane * 4;
 #pragma unroll
-    for (int i = 0; i < D / 8; ++i) {
+    for (int i = 0; i < C / 8; ++i) {
         *reinterpret_cast<f32x4 *>(mine + i * 256) = f32x4{dv[i / 4][4 * (i % 4)], dv[i / 4][4 * (i % 4) + 1], dv[i / 4][4 * (i % 4) + 2], dv[i / 4][4 * (i % 4) + 3]};
-        *reinterpret_cast<f32x4 *>(mine + 4 * (D / 8) * 256 + i * 256) = f32x4{dk[i / 4][4 * (i % 4)], dk[i / 4][4 * (i % 4) + 1], dk[i / 4][4 * (i % 4) + 2], dk[i / 4][4 * (i % 4) + 3]};
+        *reinterpret_cast<f32x4 *>(mine + 4 * (C / 8) * 256 + i * 256) = f32x4{dk[i / 4][4 * (i % 4)], dk[i / 4][4 * (i % 4) + 1], dk[i / 4][4 * (i % 4) + 2], dk[i / 4][4 * (i % 4) + 3]};
     }
 }
 
 // The parts of a key tile that was cut, added in order.  A workgroup takes one wave's 32 keys of dK or dV.
-template <int D, bool BF16>
+template <int C, bool BF16>
 __global__ void __launch_bounds__(256) smha_sink_sum(const SinkParams p) {
     const int tile_at = (int)blockIdx.x >> 3, w = (int)blockIdx.x & 3, is_k = ((int)blockIdx.x >> 2) & 1;
     const int bh = tile_at / p.n_tiles, tile = tile_at - bh * p.n_tiles, b = bh / p.Hkv, hk = bh - b * p.Hkv;
@@ -563,16 +623,15 @@ __global__ void __launch_bounds__(256) smha_sink_sum(const SinkParams p) {
     const int cut = sink ? p.cut_sink : p.cut_rest;
     const int item = sink ? tile * cut : p.n_sink_tiles * p.cut_sink + (tile - p.n_sink_tiles) * cut;
     const Sequence s = sequence(p, b);
-    const int steps = key_tile(p, s, tile * 128).nq * p.G;
-    if (cut == 1 || steps <= p.chunk) return;  // it was written whole
-    const int parts = (steps + p.chunk - 1) / p.chunk;
+    const int parts = parts_of(key_tile(p, s, tile * 128).nq * p.G, cut, sink ? p.chunk_sink : p.chunk_rest);
+    if (parts == 1) return;  // it was written whole
     uint16_t *const out = is_k ? p.dK + b * p.dks.b + hk * p.dks.h : p.dV + b * p.dvs.b + hk * p.dvs.h;
     const int64_t pitch = is_k ? p.dks.s : p.dvs.s;
     const float factor = is_k ? p.scale : 1.f;
-    const float *const from = p.parts + (((int64_t)bh * per + item) * 8 + is_k * 4 + w) * (D / 8) * 256;
-    for (int i = threadIdx.x; i < D / 8 * 64; i += 256) {
+    const float *const from = p.parts + (((int64_t)bh * per + item) * 8 + is_k * 4 + w) * (C / 8) * 256;
+    for (int i = threadIdx.x; i < C / 8 * 64; i += 256) {
         f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-        for (int c = 0; c < parts; ++c) sum += *reinterpret_cast<const f32x4 *>(from + (int64_t)c * 8 * (D / 8) * 256 + i * 4);
+        for (int c = 0; c < parts; ++c) sum += *reinterpret_cast<const f32x4 *>(from + (int64_t)c * 8 * (C / 8) * 256 + i * 4);
         const int quad = i >> 6, lane = i & 63, key = tile * 128 + 32 * w + (lane & 31), col = 8 * quad + 4 * (lane >> 5);
         if (key < p.Sk && col < p.d)
             *reinterpret_cast<u32x2 *>(out + key * pitch + col) = u32x2{pack2<BF16>(sum[0] * factor, sum[1] * factor), pack2<BF16>(sum[2] * factor, sum[3] * factor)};
@@ -611,17 +670,22 @@ static smha_status_t sink_params(SinkParams &sp, int B, int H, int Hkv, int Sq, 
     return SMHA_OK;
 }
 
-// How dK and dV are cut: enough parts for two rounds of the workgroups that the chip holds (two on each of 256 compute units), of at least
-// 24 steps, so that the 128 x D partial sums that each part writes stay a small share of its work.
+// How dK and dV are cut.  512 workgroups fit the chip, and a part costs 8 D 128 bytes of traffic: about one part for each of them evens out
+// the load, fewer leave units idle, more are slower again.  A tile with sinks is its queries' only in one or two of its waves, whose steps
+// are short: its parts are a little longer.  us of a backward pass, with tiles cut into 1, 2, 4 and 8 parts (as many for those with sinks as were
+// best): 4 x 12 x 1537 x 80, window 256: 96, 110, 133, 216 (here 1); 2 x 16 on 4 x 4096 x 128, window 1024: 293, 292, 300, 324 (2); 1 x 32 on 8 x 4096 x
+// 64, window 512: 151, 136, 135, 139 (2); 1 x 8 on 1 x 8192 x 128, window 1024: 371, 240, 218, 222 (7); 1 x 16 on 4 x 2000 x 96, window 300: 97, 77, 71, 74 (6);
+// 1 x 20 on 4 x 6000 x 128, all before: 1355, 932, 879, 915 (5).
 static void sink_cuts(SinkParams &sp) {
-    const int64_t nq = (sp.Sq + 63) / 64;
-    const int64_t near = std::min<int64_t>(nq, (sp.window + 127 + 63) / 64 + 1);
+    const int64_t nq = (sp.Sq + 31) / 32;
+    const int64_t near = std::min<int64_t>(nq, (sp.window + 127 + 31) / 32 + 1);
     sp.n_tiles = (sp.Sk + 127) / 128;
     sp.n_sink_tiles = sp.window < sp.Sk ? (sp.n_sink + 127) / 128 : 0;
     const int64_t all = (int64_t)sp.B * sp.Hkv * sp.G * (sp.n_sink_tiles * nq + (sp.n_tiles - sp.n_sink_tiles) * (sp.window < sp.Sk ? near : (nq + 1) / 2));
-    sp.chunk = (int)std::max<int64_t>(24, (all + 1023) / 1024);
-    sp.cut_sink = (int)((nq * sp.G + sp.chunk - 1) / sp.chunk);
-    sp.cut_rest = (int)((near * sp.G + sp.chunk - 1) / sp.chunk);
+    sp.chunk_rest = (int)std::max<int64_t>(8, (all + 447) / 448);
+    sp.chunk_sink = (int)std::max<int64_t>(12, (all + 399) / 400);
+    sp.cut_sink = (int)((nq * sp.G + sp.chunk_sink - 1) / sp.chunk_sink);
+    sp.cut_rest = (int)((near * sp.G + sp.chunk_rest - 1) / sp.chunk_rest);
     if (sp.n_sink_tiles == 0) sp.cut_sink = 1;
 }
 
@@ -629,29 +693,29 @@ static int64_t sink_stats_bytes(const SinkParams &sp) { return (int64_t)2 * sp.B
 static int64_t sink_items(const SinkParams &sp) {
     return (int64_t)sp.B * sp.Hkv * ((int64_t)sp.n_sink_tiles * sp.cut_sink + (int64_t)(sp.n_tiles - sp.n_sink_tiles) * sp.cut_rest);
 }
-static int sink_width(int d) { return d <= 64 ? 64 : 128; }
+static int sink_width(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : d <= 96 ? 96 : 128; }
 
-template <int D, bool BF16> static hipError_t launch_sink_fwd(SinkParams &sp, hipStream_t stream) {
+template <int D, int C, bool BF16> static hipError_t launch_sink_fwd(SinkParams &sp, hipStream_t stream) {
     const int64_t items = (int64_t)sp.B * sp.H * ((sp.Sq + 127) / 128);
     sp.per_xcd = (int)((items + 7) / 8);
-    hipLaunchKernelGGL((smha_sink_fwd<D, BF16>), dim3(8 * sp.per_xcd), dim3(256), 0, stream, sp);
+    hipLaunchKernelGGL((smha_sink_fwd<D, C, BF16>), dim3(8 * sp.per_xcd), dim3(256), 0, stream, sp);
     return hipGetLastError();
 }
 
-template <int D, bool BF16> static hipError_t launch_sink_bwd(SinkParams &sp, hipStream_t stream) {
+template <int D, int C, bool BF16> static hipError_t launch_sink_bwd(SinkParams &sp, hipStream_t stream) {
     const int64_t rows = (int64_t)sp.B * sp.H * sp.Sqp;
     hipLaunchKernelGGL((smha_sink_stats<BF16>), dim3((unsigned)((rows + 15) / 16)), dim3(256), 0, stream, sp);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     sp.per_xcd = (int)((sink_items(sp) + 7) / 8);
-    hipLaunchKernelGGL((smha_sink_bwd_kv<D, BF16>), dim3(8 * sp.per_xcd), dim3(256), 0, stream, sp);
+    hipLaunchKernelGGL((smha_sink_bwd_kv<D, C, BF16>), dim3(8 * sp.per_xcd), dim3(256), 0, stream, sp);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     if (sp.cut_sink > 1 || sp.cut_rest > 1) {
-        hipLaunchKernelGGL((smha_sink_sum<D, BF16>), dim3((unsigned)(8 * sp.B * sp.Hkv * sp.n_tiles)), dim3(256), 0, stream, sp);
+        hipLaunchKernelGGL((smha_sink_sum<C, BF16>), dim3((unsigned)(8 * sp.B * sp.Hkv * sp.n_tiles)), dim3(256), 0, stream, sp);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
     sp.per_xcd = (int)(((int64_t)sp.B * sp.H * ((sp.Sq + 127) / 128) + 7) / 8);
-    hipLaunchKernelGGL((smha_sink_bwd_q<D, BF16>), dim3(8 * sp.per_xcd), dim3(256), 0, stream, sp);
+    hipLaunchKernelGGL((smha_sink_bwd_q<D, C, BF16>), dim3(8 * sp.per_xcd), dim3(256), 0, stream, sp);
     return hipGetLastError();
 }
 
@@ -673,9 +737,16 @@ extern "C" smha_status_t smha_sink_forward(const void *Q, const void *K, const v
     sp.Q = (const uint16_t *)Q; sp.K = (const uint16_t *)K; sp.V = (const uint16_t *)V; sp.O = (uint16_t *)O; sp.lse = lse; sp.rest = (uint16_t *)O_rest;
     sp.qs = strides_of(q_strides, H, Sq, d); sp.ks = strides_of(k_strides, Hkv, Sk, d); sp.vs = strides_of(v_strides, Hkv, Sk, d); sp.os = strides_of(o_strides, H, Sq, d);
     const hipStream_t stream = (hipStream_t)hip_stream;
-    const bool bf16 = dtype == SMHA_BF16;
-    const hipError_t e = sink_width(d) == 64 ? (bf16 ? launch_sink_fwd<64, true>(sp, stream) : launch_sink_fwd<64, false>(sp, stream))
-                                             : (bf16 ? launch_sink_fwd<128, true>(sp, stream) : launch_sink_fwd<128, false>(sp, stream));
+    auto go = [&](auto bf16) {
+        constexpr bool BF = decltype(bf16)::value;
+        switch (sink_width(d)) {
+            case 32: return launch_sink_fwd<64, 32, BF>(sp, stream);
+            case 64: return launch_sink_fwd<64, 64, BF>(sp, stream);
+            case 96: return launch_sink_fwd<128, 96, BF>(sp, stream);
+            default: return launch_sink_fwd<128, 128, BF>(sp, stream);
+        }
+    };
+    const hipError_t e = dtype == SMHA_BF16 ? go(std::true_type()) : go(std::false_type());
     return e == hipSuccess ? SMHA_OK : SMHA_ERR_HIP;
 }
 
@@ -718,8 +789,15 @@ extern "C" smha_status_t smha_sink_backward(const void *Q, const void *K, const 
     sp.stats = (float *)workspace;
     sp.parts = (float *)((char *)workspace + sink_stats_bytes(sp));
     const hipStream_t stream = (hipStream_t)hip_stream;
-    const bool bf16 = dtype == SMHA_BF16;
-    const hipError_t e = sink_width(d) == 64 ? (bf16 ? launch_sink_bwd<64, true>(sp, stream) : launch_sink_bwd<64, false>(sp, stream))
-                                             : (bf16 ? launch_sink_bwd<128, true>(sp, stream) : launch_sink_bwd<128, false>(sp, stream));
+    auto go = [&](auto bf16) {
+        constexpr bool BF = decltype(bf16)::value;
+        switch (sink_width(d)) {
+            case 32: return launch_sink_bwd<64, 32, BF>(sp, stream);
+            case 64: return launch_sink_bwd<64, 64, BF>(sp, stream);
+            case 96: return launch_sink_bwd<128, 96, BF>(sp, stream);
+            default: return launch_sink_bwd<128, 128, BF>(sp, stream);
+        }
+    };
+    const hipError_t e = dtype == SMHA_BF16 ? go(std::true_type()) : go(std::false_type());
     return e == hipSuccess ? SMHA_OK : SMHA_ERR_HIP;
 }
