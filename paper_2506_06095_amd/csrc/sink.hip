@@ -324,7 +324,7 @@ __global__ void __launch_bounds__(256) smha_sink_stats(const SinkParams p) {
 // dS is rounded to the inputs' type for the product with K, as P is in the forward.
 template <int D, int C, bool BF16>
 __global__ void __launch_bounds__(256, 2) smha_sink_bwd_q(const SinkParams p) {
-    constexpr int NS = C / 16, NDT = C / 32, TB = 64 * D * 2;
+    constexpr int NS = C / 16, NDT = C / 32, TB = 64 * D * 2, PF = C == 128 ? 6 : 4;
     __shared__ __attribute__((aligned(1024))) char smem[4 * TB];  // K[0], K[1], V[0], V[1]
     const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_void *)smem;
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = lane & 31, hh = lane >> 5;
@@ -381,27 +381,63 @@ __global__ void __launch_bounds__(256, 2) smha_sink_bwd_q(const SinkParams p) {
                 const int k0 = key + 32 * kt;
                 if (!any_seen(wp0, wp1, k0, k0 + 31, window, n_sink)) continue;
                 const char *const Kt = smem + par * TB + kt * (TB / 2), *const Vt = smem + (2 + par) * TB + kt * (TB / 2);
+                // The left operands of the three products, in their order: K's rows, V's rows, K's columns; requested PF products ahead.
+                auto operand = [&](int n) __attribute__((always_inline)) {
+                    if (n < 2 * NS) return *reinterpret_cast<const u32x4 *>((n < NS ? Kt : Vt) + (rd ^ (32 * (n % NS))));
+                    const int cu = (n - 2 * NS) / NDT, dt = (n - 2 * NS) % NDT;
+                    const u32x2 lo = lds_read_tr(reinterpret_cast<const uint16_t *>(Kt + ((tr ^ (64 * dt)) + 32 * cu * D)));
+                    const u32x2 hi = lds_read_tr(reinterpret_cast<const uint16_t *>(Kt + ((tr ^ (64 * dt) ^ 32) + 32 * cu * D + 16 * D)));
+                    return u32x4{lo[0], lo[1], hi[0], hi[1]};
+                };
+                constexpr int ALL = 2 * NS + 2 * NDT;
+                u32x4 f[PF];
                 f32x16 sc = zeros16(), dp = zeros16();
 #pragma unroll
-                for (int i = 0; i < NS; ++i) sc = mfma32<BF16>(*reinterpret_cast<const u32x4 *>(Kt + (rd ^ (32 * i))), qf[i], sc);
+                for (int i = 0; i < PF; ++i) f[i] = operand(i);
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int i = 0; i < NS; ++i) dp = mfma32<BF16>(*reinterpret_cast<const u32x4 *>(Vt + (rd ^ (32 * i))), gf[i], dp);
-                f32x16 ds;
+                for (int i = 0; i < NS; ++i) {
+                    sc = mfma32<BF16>(f[i % PF], qf[i], sc);
+                    if (i + PF < ALL) f[i % PF] = operand(i + PF);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                u32x16 keep;
+                const bool part_seen = !(whole && all_seen(wp0, wp1, k0, k0 + 31, window, n_sink));
+                if (part_seen) {
+                    keep = keep_of((uint32_t)(exists ? seen_keys(qpos, k0, window, n_sink) : 0) >> (4 * hh));
+                    const u32x16 raw = __builtin_bit_cast(u32x16, sc);
+                    sc = __builtin_bit_cast(f32x16, (raw & keep) | (~keep & 0xFF800000u));
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                // dP, and P from the scores
 #pragma unroll
-                for (int r = 0; r < 16; ++r) ds[r] = fast_exp2(fmaf(sc[r], p.c, -lse2)) * (dp[r] - delta);
-                if (!(whole && all_seen(wp0, wp1, k0, k0 + 31, window, n_sink))) {
-                    const u32x16 keep = keep_of((uint32_t)(exists ? seen_keys(qpos, k0, window, n_sink) : 0) >> (4 * hh));
-                    ds = __builtin_bit_cast(f32x16, __builtin_bit_cast(u32x16, ds) & keep);
+                for (int i = 0; i < NS; ++i) {
+                    dp = mfma32<BF16>(f[(NS + i) % PF], gf[i], dp);
+                    if (NS + i + PF < ALL) f[(NS + i) % PF] = operand(NS + i + PF);
+#pragma unroll
+                    for (int r = 16 * i / NS; r < 16 * (i + 1) / NS; ++r) sc[r] = fast_exp2(fmaf(sc[r], p.c, -lse2));
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                if (part_seen) {  // (where P is zero dP may be anything)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) dp[r] = sc[r] != 0.f ? dp[r] : delta;
                 }
                 u32x4 pf[2];
+                auto ds_pair = [&](int q) __attribute__((always_inline)) {
+                    pf[q >> 2][q & 3] = pack2<BF16>(sc[2 * q] * (dp[2 * q] - delta), sc[2 * q + 1] * (dp[2 * q + 1] - delta));
+                };
 #pragma unroll
-                for (int q = 0; q < 8; ++q) pf[q >> 2][q & 3] = pack2<BF16>(ds[2 * q], ds[2 * q + 1]);
+                for (int q = 0; q < 4; ++q) ds_pair(q);
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int i = 0; i < 2 * NDT; ++i) {
-                    const int cu = i / NDT, dt = i % NDT;
-                    const char *const at = Kt + ((tr ^ (64 * dt)) + 32 * cu * D), *const at8 = Kt + ((tr ^ (64 * dt) ^ 32) + 32 * cu * D + 16 * D);
-                    const u32x2 lo = lds_read_tr(reinterpret_cast<const uint16_t *>(at)), hi = lds_read_tr(reinterpret_cast<const uint16_t *>(at8));
-                    dq[dt] = mfma32<BF16>(u32x4{lo[0], lo[1], hi[0], hi[1]}, pf[cu], dq[dt]);
+                    dq[i % NDT] = mfma32<BF16>(f[(2 * NS + i) % PF], pf[i / NDT], dq[i % NDT]);
+                    if (2 * NS + i + PF < ALL) f[(2 * NS + i) % PF] = operand(2 * NS + i + PF);
+                    if (i < NDT) {  // the other 16 keys' dS, under these products
+#pragma unroll
+                        for (int q = 4 + 4 * i / NDT; q < 4 + 4 * (i + 1) / NDT; ++q) ds_pair(q);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
                 }
             }
         }
