@@ -31,12 +31,14 @@ struct CacheParams {
     int window, n_sink;
     float c;
     int slots;       // segments wanted
-    int own_tiles, prefix_tiles;  // 32-row tiles of G T rows, of B G T rows (0 without a prefix)
-    int segs;        // segments there is room for
+    int own_tiles, prefix_tiles;  // 32-row tiles of G T rows; tiles of B G T rows (0 without a prefix), of
+    int wide;                     // 128 rows and 64 keys (prefix_wide), else of 32 and 32
+    int prefix_segs, segs;        // segments there is room for: of the prefix, in all
     int score_pitch; // keys per row of `scores`
-    int2 *info;      // [prefix groups, own groups]: first segment, segments
-    float *stats;    // [segment][2][32]: reference (log2 units), sum
-    float *parts;    // [segment][32][D]
+    // A segment's results are places of 32 rows: one, or four of a wide one.  The prefix's segments come first.
+    int2 *info;      // [prefix groups, own groups]: first place, segments
+    float *stats;    // [place][2][32]: reference (log2 units), sum
+    float *parts;    // [place][32][D]
     float *scores;   // [B][Hkv][G T][score_pitch], log2 units
 };
 
@@ -58,8 +60,8 @@ __device__ __forceinline__ OwnKeys own_keys(int length, int T, int Sk, int windo
 }
 
 struct Segment {
-    int seg;             // its number; -1: none
-    int b, hk, rows0;    // rows0: first of the 32 rows; b = -1: prefix
+    int place;           // of its results; -1: no segment
+    int b, hk, rows0;    // rows0: first of its rows; b = -1: prefix
     int part, parts, n;  // of the group's n tiles
     int group;
 };
@@ -72,37 +74,37 @@ __device__ __forceinline__ int wave_sum(int v) {
 
 // The segment of a workgroup.  Every wave of the launch computes the same cut: c tiles a segment at most, so many (in fours, a team's turn) that
 // all tiles make `slots` segments.  Groups shorter than that are a segment each, and then there are more: what does not fit at first
-// starts as others end.
+// starts as others end.  A wide tile takes about as long as three of the others, which its waves share.
 __device__ __forceinline__ Segment segment_of(const CacheParams &p, int lane) {
     const int prefix_groups = p.Hkv * p.prefix_tiles, per_b = p.Hkv * p.own_tiles;
-    const int prefix_n = p.prefix_tiles ? (p.P + 31) / 32 : 0;
+    const int prefix_n = !p.prefix_tiles ? 0 : p.wide ? (p.P + 63) / 64 : (p.P + 31) / 32, weight = p.wide ? 3 : 1;
     auto tiles = [&](int b) __attribute__((always_inline)) { return b < p.B ? own_keys(p.lengths[b], p.T, p.Sk, p.window, p.n_sink).n : 0; };
     const int first64 = tiles(lane);
     int sum = first64;
     for (int b = 64 + lane; b - lane < p.B; b += 64) sum += tiles(b);
-    const int total = prefix_groups * prefix_n + per_b * wave_sum(sum);
+    const int total = prefix_groups * prefix_n * weight + per_b * wave_sum(sum);
     const int c = __builtin_amdgcn_readfirstlane(max(4, ((total + p.slots - 1) / p.slots + 3) & ~3));
     sum = (first64 + c - 1) / c;
     for (int b = 64 + lane; b - lane < p.B; b += 64) sum += (tiles(b) + c - 1) / c;
-    const int own_segs = __builtin_amdgcn_readfirstlane(per_b * wave_sum(sum)), prefix_parts = (prefix_n + c - 1) / c, prefix_segs = prefix_groups * prefix_parts;
+    const int own_segs = __builtin_amdgcn_readfirstlane(per_b * wave_sum(sum)), prefix_c = (c + weight - 1) / weight, prefix_parts = (prefix_n + prefix_c - 1) / prefix_c, prefix_segs = prefix_groups * prefix_parts;
     // an XCD takes a run of the prefix's segments, which are the longest, and then one of the others: those that read the same keys are neighbours
     const int xcd = (int)blockIdx.x & 7, slot = (int)blockIdx.x >> 3, prefix_run = (prefix_segs + 7) / 8, own_run = (own_segs + 7) / 8;
     Segment s{-1, -1, 0, 0, 0, 1, 0, 0};
     if (slot < prefix_run) {
         const int at = xcd * prefix_run + slot;
         if (at >= prefix_segs) return s;
-        s.seg = at;
+        s.place = p.wide ? 4 * at : at;
         s.parts = prefix_parts;
         s.group = at / s.parts;
         s.part = at - s.group * s.parts;
         s.hk = s.group / p.prefix_tiles;
-        s.rows0 = 32 * (s.group - s.hk * p.prefix_tiles);
+        s.rows0 = (p.wide ? 128 : 32) * (s.group - s.hk * p.prefix_tiles);
         s.n = prefix_n;
         return s;
     }
     int at = xcd * own_run + slot - prefix_run;
     if (slot - prefix_run >= own_run || at >= own_segs) return s;
-    s.seg = prefix_segs + at;
+    s.place = (p.wide ? 4 : 1) * p.prefix_segs + at;
     for (int b0 = 0; b0 < p.B; b0 += 64) {
         const int n = b0 ? tiles(b0 + lane) : first64, mine = per_b * ((n + c - 1) / c);
         int upto = mine;
@@ -127,15 +129,128 @@ __device__ __forceinline__ Segment segment_of(const CacheParams &p, int lane) {
         }
         at -= __builtin_amdgcn_readlane(upto, 63);
     }
-    s.seg = -1;  // (not reached: the segments counted are those found)
+    s.place = -1;  // (not reached: the segments counted are those found)
     return s;
+}
+
+// A segment of a prefix that many rows read: four waves of 32 rows share 64-key tiles, two of each in LDS, as in smha_sink_fwd, but every key is
+// visible.  (By the waves on their own, 32 rows and 32 keys at a time, K and V come from L2 four times as often, and its path into LDS sets the
+// pace: 64 x 32 on 8 heads, 8192 shared keys and 280 of their own 42 us.)
+template <int D, bool BF16>
+__device__ __forceinline__ void prefix_wide(const CacheParams &p, const Segment &s, char *smem, const u32x4 (&qf)[D / 16], int lane, int w) {
+    constexpr int NS = D / 16, NDT = D / 32, TB = 64 * D * 2, PF = D == 128 ? 8 : 4;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_void *)smem;
+    const int j = lane & 31, hh = lane >> 5;
+    const float NEG_INF = -__builtin_inff();
+    const int ksb = (int)p.pk_s * 2, vsb = (int)p.pv_s * 2;
+    const u32x4 rK = make_rsrc4(p.PK + s.hk * p.pk_h, ((int64_t)(p.P - 1) * p.pk_s + p.d) * 2), rV = make_rsrc4(p.PV + s.hk * p.pv_h, ((int64_t)(p.P - 1) * p.pv_s + p.d) * 2);
+    const TileLoad<D> loadK(w, lane, ksb, p.d), loadV(w, lane, vsb, p.d);
+    const int begin = (int)((int64_t)s.n * s.part / s.parts), end = (int)((int64_t)s.n * (s.part + 1) / s.parts);
+    loadK(rK, lds0, w, 64 * begin, ksb, 0, 0);
+    loadV(rV, lds0 + 2 * TB, w, 64 * begin, vsb, 0, 0);
+    const int rd = j * D * 2 + ((hh ^ swz_both<D>(j)) * 16);
+    const int tr_row = 4 * hh + ((lane & 15) >> 2);
+    const int tr = tr_row * D * 2 + ((swz_both<D>(tr_row) ^ (2 * ((lane >> 4) & 1) + ((lane & 3) >> 1))) * 16) + (lane & 1) * 8;
+    float m_run = NEG_INF, l_run = 0.f;
+    const float thr = 8.0f / p.c;
+    f32x16 o[NDT];
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt) o[dt] = zeros16();
+    tiles_landed();
+    for (int t = begin; t < end; ++t) {
+        const int par = (t - begin) & 1;
+        if (t + 1 < end) {
+            loadK(rK, lds0 + (par ^ 1) * TB, w, 64 * (t + 1), ksb, 0, 0);
+            loadV(rV, lds0 + (2 + (par ^ 1)) * TB, w, 64 * (t + 1), vsb, 0, 0);
+        }
+        const char *const Kt = smem + par * TB, *const Vt = smem + (2 + par) * TB;
+        f32x16 acc[2] = {zeros16(), zeros16()};
+        auto k_frag = [&](int i) __attribute__((always_inline)) { return *reinterpret_cast<const u32x4 *>(Kt + ((rd ^ (32 * (i >> 1))) + 64 * (i & 1) * D)); };
+        u32x4 kf[PF];
+#pragma unroll
+        for (int i = 0; i < PF; ++i) kf[i] = k_frag(i);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < 2 * NS; ++i) {
+            acc[i & 1] = mfma32<BF16>(kf[i % PF], qf[i >> 1], acc[i & 1]);
+            if (i + PF < 2 * NS) kf[i % PF] = k_frag(i + PF);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        __builtin_amdgcn_s_setprio(1);
+        if (64 * t + 64 > p.P) {
+            const uint64_t word = low_bits(p.P - 64 * t);
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt) {
+                const u32x16 keep = keep_of((uint32_t)(word >> (32 * kt)) >> (4 * hh)), sc = __builtin_bit_cast(u32x16, acc[kt]);
+                acc[kt] = __builtin_bit_cast(f32x16, (sc & keep) | (~keep & 0xFF800000u));
+            }
+        }
+        float mt = NEG_INF;
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) mt = fmaxf(mt, acc[kt][r]);
+        if (__builtin_amdgcn_ballot_w64(mt > m_run + thr) != 0) {
+            mt = fmaxf(mt, __shfl_xor(mt, 32));
+            const float m_new = fmaxf(m_run, mt), alpha = fast_exp2((m_run - (m_new == NEG_INF ? 0.f : m_new)) * p.c);
+            m_run = m_new;
+            l_run *= alpha;
+#pragma unroll
+            for (int dt = 0; dt < NDT; ++dt) o[dt] *= alpha;
+        }
+        const float mc = (m_run == NEG_INF ? 0.f : m_run) * p.c;
+        u32x4 pf[4];
+        auto p_pair = [&](int cu, int q) __attribute__((always_inline)) {
+            const float e0 = fast_exp2(fmaf(acc[cu >> 1][8 * (cu & 1) + 2 * q], p.c, -mc)), e1 = fast_exp2(fmaf(acc[cu >> 1][8 * (cu & 1) + 2 * q + 1], p.c, -mc));
+            pf[cu][q] = pack2<BF16>(e0, e1);
+            l_run += e0 + e1;
+        };
+        auto v_frag = [&](int i) __attribute__((always_inline)) {
+            const char *const at = Vt + ((tr ^ (64 * (i % NDT))) + 32 * (i / NDT) * D), *const at8 = Vt + ((tr ^ (64 * (i % NDT)) ^ 32) + 32 * (i / NDT) * D + 16 * D);
+            const u32x2 lo = lds_read_tr(reinterpret_cast<const uint16_t *>(at)), hi = lds_read_tr(reinterpret_cast<const uint16_t *>(at8));
+            return u32x4{lo[0], lo[1], hi[0], hi[1]};
+        };
+        u32x4 vf[PF];
+#pragma unroll
+        for (int i = 0; i < PF; ++i) vf[i] = v_frag(i);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) p_pair(0, q);
+#pragma unroll
+        for (int i = 0; i < 4 * NDT; ++i) {
+            const int cu = i / NDT, dt = i % NDT;
+            o[dt] = mfma32<BF16>(vf[i % PF], pf[cu], o[dt]);
+            if (i + PF < 4 * NDT) vf[i % PF] = v_frag(i + PF);
+            if (cu < 3) {
+#pragma unroll
+                for (int q = (4 * dt + NDT - 1) / NDT; q < (4 * dt + NDT + 3) / NDT; ++q) p_pair(cu + 1, q);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        __builtin_amdgcn_s_setprio(0);
+        tiles_landed();
+    }
+    const float l = l_run + __shfl_xor(l_run, 32);
+    if (s.part == 0 && threadIdx.x == 0) p.info[s.group] = int2{s.place, s.parts};
+    if (s.rows0 + 32 * w + j < p.B * p.G * p.T) {
+        const int64_t place = s.place + w;
+        if (hh == 0) {
+            p.stats[place * 64 + j] = m_run * p.c;
+            p.stats[place * 64 + 32 + j] = l;
+        }
+        float *const part = p.parts + (place * 32 + j) * D + 4 * hh;
+#pragma unroll
+        for (int i = 0; i < D / 8; ++i)
+            *reinterpret_cast<f32x4 *>(part + 8 * i) = f32x4{o[i / 4][4 * (i % 4)], o[i / 4][4 * (i % 4) + 1], o[i / 4][4 * (i % 4) + 2], o[i / 4][4 * (i % 4) + 3]};
+    }
 }
 
 // K, V: one buffer of 32 keys each a wave, refilled as soon as its fragments are read: K of the next tile lands under this tile's softmax
 // and second product, V of the next under the next tile's scores.  Eight waves a compute unit at 128 columns, 16 at 64.
 // Probabilities are rounded to the inputs' type for the second product (half a step each, as in smha_sink_fwd); sums are 32 bits.
-template <int D, bool BF16, bool WEIGH>
-__global__ void __launch_bounds__(256, D == 64 ? 4 : 2) smha_cache_part(const CacheParams p) {
+// (WIDE: with the wide segments of a prefix, whose registers leave a workgroup less to a unit at 64 columns)
+constexpr int cache_groups(int D, bool wide) { return D == 128 ? 2 : wide ? 3 : 4; }
+template <int D, bool BF16, bool WEIGH, bool WIDE>
+__global__ void __launch_bounds__(256, cache_groups(D, WIDE)) smha_cache_part(const CacheParams p) {
     constexpr int NS = D / 16, NDT = D / 32, CPR = D / 8, LPT = CPR / 2, RPL = 64 / CPR, NO = 16 / RPL, TB = 32 * D * 2;
     __shared__ __attribute__((aligned(1024))) char all_tiles[4 * 2 * TB];  // per wave: K, V
     __shared__ float team[4][2][32];                                        // references and sums
@@ -144,12 +259,12 @@ __global__ void __launch_bounds__(256, D == 64 ? 4 : 2) smha_cache_part(const Ca
     const uint32_t lds = (uint32_t)(uintptr_t)(lds_void *)smem;
     const float NEG_INF = -__builtin_inff();
     const Segment s = segment_of(p, lane);
-    if (s.seg < 0) return;
+    if (s.place < 0) return;
     const bool prefix = s.b < 0;
     const OwnKeys own = prefix ? OwnKeys{p.P, 0, 0, s.n, 0, 0} : own_keys(uniform_load(p.lengths + s.b), p.T, p.Sk, p.window, p.n_sink);
 
     // this lane's row
-    const int GT = p.G * p.T, row = s.rows0 + j, rows = prefix ? p.B * GT : GT;
+    const int GT = p.G * p.T, row = s.rows0 + (WIDE && prefix ? 32 * w : 0) + j, rows = prefix ? p.B * GT : GT;
     const int rb = prefix ? min(row / GT, p.B - 1) : s.b, in_b = prefix ? row - rb * GT : row, g = in_b / p.T, t = in_b - g * p.T;
     const int len_r = prefix ? min(max(p.lengths[rb], 0), p.Sk) : own.len;
     const int pos = row < rows ? len_r - p.T + t : -1;  // below 0: no such query
@@ -161,6 +276,9 @@ __global__ void __launch_bounds__(256, D == 64 ? 4 : 2) smha_cache_part(const Ca
             qf[i] = u32x4{0, 0, 0, 0};
             if (pos >= 0 && 16 * i + 8 * hh < p.d) qf[i] = *reinterpret_cast<const u32x4 *>(q + 16 * i);
         }
+    }
+    if constexpr (WIDE) {
+        if (prefix) return prefix_wide<D, BF16>(p, s, all_tiles, qf, lane, w);
     }
     const int64_t ks = prefix ? p.pk_s : p.ks.s, vs = prefix ? p.pv_s : p.vs.s;
     const uint16_t *const Kb = prefix ? p.PK + s.hk * p.pk_h : p.K + s.b * p.ks.b + s.hk * p.ks.h;
@@ -292,18 +410,18 @@ __global__ void __launch_bounds__(256, D == 64 ? 4 : 2) smha_cache_part(const Ca
             for (int e = 0; e < 4; ++e) out[4 * i + e] = fmaf(share, v[e], out[4 * i + e]);
         }
     }
-    if (s.part == 0 && threadIdx.x == 0) p.info[s.group] = int2{s.seg, s.parts};
+    if (s.part == 0 && threadIdx.x == 0) p.info[s.group] = int2{s.place, s.parts};
     const bool whole = s.parts == 1 && p.prefix_tiles == 0;  // nothing to join with
     if (row < rows) {
         if (!whole || WEIGH) {
             if (w == 0 && hh == 0) {
-                p.stats[(int64_t)s.seg * 64 + j] = m_all;
-                p.stats[(int64_t)s.seg * 64 + 32 + j] = l_all;
+                p.stats[(int64_t)s.place * 64 + j] = m_all;
+                p.stats[(int64_t)s.place * 64 + 32 + j] = l_all;
             }
         }
         const float inv = l_all > 0.f ? 1.0f / l_all : 0.f;
         uint16_t *const to = p.O + rb * p.os.b + (s.hk * p.G + g) * p.os.h + t * p.os.s;
-        float *const part = p.parts + ((int64_t)s.seg * 32 + j) * D;
+        float *const part = p.parts + ((int64_t)s.place * 32 + j) * D;
 #pragma unroll
         for (int i = 0; i < NQ; i += 4) {
             const int r = NQ * w + i, col = 32 * (r >> 4) + 8 * ((r & 15) >> 2) + 4 * hh;
@@ -316,16 +434,21 @@ __global__ void __launch_bounds__(256, D == 64 ? 4 : 2) smha_cache_part(const Ca
     }
 }
 
-// The segments of one row (those of the prefix, then its own): their common reference and sum.
+// The segments of one row: those of the prefix, then its own.
 struct RowParts {
-    int first[2], count[2], row[2];  // segments, and the row in them: prefix, own
+    int first[2], count[2], row[2];  // places' first, segments, and the row in them
+    int step;                        // places of a prefix segment
+    __device__ __forceinline__ int n() const { return count[0] + count[1]; }
+    // where segment i of the row has its reference in `stats`, and its columns in `parts` (in rows)
+    __device__ __forceinline__ int64_t stat(int i) const { return i < count[0] ? (int64_t)(first[0] + step * i) * 64 + row[0] : (int64_t)(first[1] + i - count[0]) * 64 + row[1]; }
+    __device__ __forceinline__ int64_t part(int i) const { return i < count[0] ? (int64_t)(first[0] + step * i) * 32 + row[0] : (int64_t)(first[1] + i - count[0]) * 32 + row[1]; }
 };
 __device__ __forceinline__ RowParts row_parts(const CacheParams &p, int b, int hk, int in_b, bool own) {
-    RowParts r{{0, 0}, {0, 0}, {0, 0}};
+    RowParts r{{0, 0}, {0, 0}, {0, 0}, p.wide ? 4 : 1};
     if (p.prefix_tiles) {
         const int row = b * p.G * p.T + in_b;
-        const int2 i = p.info[hk * p.prefix_tiles + row / 32];
-        r.first[0] = i.x;
+        const int2 i = p.info[hk * p.prefix_tiles + row / (p.wide ? 128 : 32)];
+        r.first[0] = i.x + (p.wide ? (row >> 5) & 3 : 0);
         r.count[0] = i.y;
         r.row[0] = row & 31;
     }
@@ -356,11 +479,9 @@ __global__ void __launch_bounds__(256) smha_cache_join(const CacheParams p, int 
         }
         const RowParts r = row_parts(p, b, hk, in_b, len > 0);
         if (!p.prefix_tiles && r.count[1] == 1) return;  // written whole
-        const int n = r.count[0] + r.count[1];
-        auto segment = [&](int i) __attribute__((always_inline)) { return i < r.count[0] ? r.first[0] + i : r.first[1] + i - r.count[0]; };
-        auto place = [&](int i) __attribute__((always_inline)) { return i < r.count[0] ? r.row[0] : r.row[1]; };
+        const int n = r.n();
         float m = NEG_INF;
-        for (int i = threadIdx.x; i < n; i += 256) m = fmaxf(m, p.stats[(int64_t)segment(i) * 64 + place(i)]);
+        for (int i = threadIdx.x; i < n; i += 256) m = fmaxf(m, p.stats[r.stat(i)]);
 #pragma unroll
         for (int x = 32; x > 0; x >>= 1) m = fmaxf(m, __shfl_xor(m, x));
         if (lane == 0) lds_ml[0][w] = m;
@@ -372,11 +493,11 @@ __global__ void __launch_bounds__(256) smha_cache_join(const CacheParams p, int 
         for (int e = 0; e < D / 64; ++e) acc[e] = 0.f;
 #pragma unroll 4
         for (int i = w; i < n; i += 4) {
-            const int64_t at = segment(i);
-            const float ref = p.stats[at * 64 + place(i)], share = ref != NEG_INF ? fast_exp2(ref - m) : 0.f;
-            sum = fmaf(share, p.stats[at * 64 + 32 + place(i)], sum);
+            const int64_t at = r.stat(i), part = r.part(i) * D;
+            const float ref = p.stats[at], share = ref != NEG_INF ? fast_exp2(ref - m) : 0.f;
+            sum = fmaf(share, p.stats[at + 32], sum);
 #pragma unroll
-            for (int e = 0; e < D / 64; ++e) acc[e] = fmaf(share, p.parts[(at * 32 + place(i)) * D + lane + 64 * e], acc[e]);
+            for (int e = 0; e < D / 64; ++e) acc[e] = fmaf(share, p.parts[part + lane + 64 * e], acc[e]);
         }
         if (lane == 0) lds_ml[1][w] = sum;
 #pragma unroll
@@ -402,12 +523,12 @@ __global__ void __launch_bounds__(256) smha_cache_join(const CacheParams p, int 
         __syncthreads();
         for (int r1 = w; r1 < nr; r1 += 4) {  // a wave a row, a lane a segment
             const RowParts r = row_parts(p, b, hk, r0 + r1, true);
-            const int n = r.count[0] + r.count[1];
+            const int n = r.n();
             float m = NEG_INF, l = 0.f;
             for (int i = lane; i - lane < n; i += 64) {
                 float ref = NEG_INF, part = 0.f;
                 if (i < n) {
-                    const int64_t at = (int64_t)(i < r.count[0] ? r.first[0] + i : r.first[1] + i - r.count[0]) * 64 + (i < r.count[0] ? r.row[0] : r.row[1]);
+                    const int64_t at = r.stat(i);
                     ref = p.stats[at];
                     part = p.stats[at + 32];
                 }
@@ -736,31 +857,37 @@ static smha_status_t cache_params(CacheParams &cp, CacheLayout &at, int B, int H
     cp.B = B; cp.H = H; cp.Hkv = Hkv; cp.G = H / Hkv; cp.T = T; cp.Sk = Sk; cp.P = P; cp.d = d;
     cp.window = window == 0 || window > Sk ? Sk : window;
     cp.n_sink = std::min(n_sink, Sk);
-    const int64_t rows = (int64_t)cp.G * T, own_tiles = (rows + 31) / 32, prefix_tiles = P ? ((int64_t)B * rows + 31) / 32 : 0;
+    const int64_t rows = (int64_t)cp.G * T, own_tiles = (rows + 31) / 32;
+    cp.wide = P > 0 && B * rows > 64;  // (one or two tiles of 32 rows: reading the keys once or twice by waves on their own fills the chip better)
+    const int64_t prefix_tiles = !P ? 0 : cp.wide ? (B * rows + 127) / 128 : (B * rows + 31) / 32;
     const int64_t groups = (int64_t)Hkv * (prefix_tiles + B * own_tiles);
     // (tiles and rows are counted in 32 bits)
     if ((int64_t)B * H * T > (1 << 24) || groups * (std::max(Sk, P) / 32 + 8) > (1 << 30)) return SMHA_ERR_UNSUPPORTED;
     cp.own_tiles = (int)own_tiles;
     cp.prefix_tiles = (int)prefix_tiles;
     const int D = d <= 64 ? 64 : 128;
-    cp.slots = 256 * (D == 64 ? 4 : 2);  // what the chip holds at once: 32 or 64 KB of LDS a workgroup
+    cp.slots = 256 * cache_groups(D, cp.wide);  // what the chip holds at once
     // no more segments than that and one a group, and none shorter than four tiles unless it is a group
     const int64_t own_most = (std::min<int64_t>(Sk, (int64_t)cp.window + cp.n_sink + T) / 32 + 3 + 3) / 4;
-    const int64_t most = Hkv * (prefix_tiles * ((P / 32 + 1 + 3) / 4) + B * own_tiles * own_most);
-    cp.segs = (int)std::min<int64_t>(cp.slots + groups, most);
+    const int64_t prefix_most = Hkv * prefix_tiles * (cp.wide ? (P / 64 + 1 + 1) / 2 : (P / 32 + 1 + 3) / 4);
+    cp.prefix_segs = (int)std::min<int64_t>(cp.slots + Hkv * prefix_tiles, prefix_most);
+    const int64_t own_segs = std::min<int64_t>(cp.slots + (int64_t)B * Hkv * own_tiles, B * Hkv * own_tiles * own_most);
+    cp.segs = (int)(cp.prefix_segs + own_segs);
+    const int64_t places = (cp.wide ? 4 : 1) * (int64_t)cp.prefix_segs + own_segs;
     cp.score_pitch = (Sk + 31) / 32 * 32;
     at.info = 0;
     at.stats = up(groups * sizeof(int2));
-    at.parts = at.stats + up((size_t)cp.segs * 64 * 4);
-    at.scores = at.parts + up((size_t)cp.segs * 32 * D * 4);
+    at.parts = at.stats + up((size_t)places * 64 * 4);
+    at.scores = at.parts + up((size_t)places * 32 * D * 4);
     at.total = at.scores + (weigh ? (size_t)B * Hkv * rows * cp.score_pitch * 4 : 0);
     return SMHA_OK;
 }
 
 template <int D, bool BF16> static hipError_t launch_cache(const CacheParams &cp, hipStream_t stream) {
     const dim3 grid(8 * ((cp.segs + 7) / 8 + 1));  // (two runs an XCD, each rounded up)
-    if (cp.weights) hipLaunchKernelGGL((smha_cache_part<D, BF16, true>), grid, dim3(256), 0, stream, cp);
-    else hipLaunchKernelGGL((smha_cache_part<D, BF16, false>), grid, dim3(256), 0, stream, cp);
+    auto *const part = cp.weights ? (cp.wide ? smha_cache_part<D, BF16, true, true> : smha_cache_part<D, BF16, true, false>)
+                                  : (cp.wide ? smha_cache_part<D, BF16, false, true> : smha_cache_part<D, BF16, false, false>);
+    hipLaunchKernelGGL(part, grid, dim3(256), 0, stream, cp);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     const int rows = cp.B * cp.H * cp.T, keys = cp.weights ? (cp.Sk + 1023) / 1024 : 0;

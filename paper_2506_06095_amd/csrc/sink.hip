@@ -70,35 +70,6 @@ __device__ __forceinline__ bool all_seen(int p0, int p1, int k0, int k1, int win
     return k1 <= p0 && (p1 - k0 < window || k1 < n_sink);
 }
 
-// A tile of ROWS rows into LDS by a workgroup's four waves: wave w brings the 1 KiB blocks w, w + 4, ...
-template <int D, int ROWS = 64> struct TileLoad {
-    static constexpr int CPR = D / 8, LPW = CPR * ROWS / 256, RSTEP = 4 * 64 / CPR;  // chunks a row, loads a wave, rows between two of its loads
-    uint32_t go;  // the lane's offset in the wave's first block
-    int row;
-    __device__ __forceinline__ TileLoad(int w, int lane, int row_bytes, int d) {
-        row = (w * 64 + lane) / CPR;
-        const int c = (lane % CPR) ^ swz_both<D>(row);
-        go = c < (d >> 3) ? (uint32_t)(row * row_bytes + c * 16) : kNoChunk;
-    }
-    // rows r0 ..; those in [gap0, gap1) read as zeros, as do those past the buffer
-    __device__ __forceinline__ void operator()(u32x4 rsrc, uint32_t lds, int w, int r0, int row_bytes, int gap0, int gap1) const {
-#pragma unroll
-        for (int i = 0; i < LPW; ++i) {
-            const int r = r0 + row + i * RSTEP;
-            const uint32_t at = go + (uint32_t)((r0 + i * RSTEP) * row_bytes);
-            load_to_lds(rsrc, lds + (w + 4 * i) * 1024, (int)(r >= gap0 && r < gap1 ? kPast : at));
-        }
-    }
-};
-
-// The next tile is in LDS and this one may be overwritten, for every wave.  (The last line keeps reads of LDS where they are: for the
-// compiler the barrier touches no memory.)
-__device__ __forceinline__ void tiles_landed() {
-    __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0)
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-}
-
 // A wave's 32 x D accumulators (acc[dt][r] = row j, column 32 dt + 8 (r / 4) + 4 hh + r % 4) to rows row0 .. of a tensor with 16-bit values,
 // through 32 rows of LDS so that whole rows are written; rows from `rows` on are left out.
 // REST: not the rounded values, but what their rounding leaves out.
