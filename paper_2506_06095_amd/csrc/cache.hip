@@ -33,6 +33,7 @@ struct CacheParams {
     int slots;       // segments wanted
     int own_tiles, prefix_tiles;  // 32-row tiles of G T rows; tiles of B G T rows (0 without a prefix), of
     int wide;                     // 128 rows and 64 keys (prefix_wide), else of 32 and 32
+    int direct;                   // a workgroup a group (see CacheForm)
     int prefix_segs, segs;        // segments there is room for: of the prefix, in all
     int score_pitch; // keys per row of `scores`
     // A segment's results are places of 32 rows: one, or four of a wide one.  The prefix's segments come first.
@@ -63,7 +64,7 @@ struct Segment {
     int place;           // of its results; -1: no segment
     int b, hk, rows0;    // rows0: first of its rows; b = -1: prefix
     int part, parts, n;  // of the group's n tiles
-    int group;
+    int group, length;   // length: lengths[b]
 };
 
 __device__ __forceinline__ int wave_sum(int v) {
@@ -78,8 +79,9 @@ __device__ __forceinline__ int wave_sum(int v) {
 __device__ __forceinline__ Segment segment_of(const CacheParams &p, int lane) {
     const int prefix_groups = p.Hkv * p.prefix_tiles, per_b = p.Hkv * p.own_tiles;
     const int prefix_n = !p.prefix_tiles ? 0 : p.wide ? (p.P + 63) / 64 : (p.P + 31) / 32, weight = p.wide ? 3 : 1;
-    auto tiles = [&](int b) __attribute__((always_inline)) { return b < p.B ? own_keys(p.lengths[b], p.T, p.Sk, p.window, p.n_sink).n : 0; };
-    const int first64 = tiles(lane);
+    auto tiles_at = [&](int length) __attribute__((always_inline)) { return own_keys(length, p.T, p.Sk, p.window, p.n_sink).n; };
+    auto tiles = [&](int b) __attribute__((always_inline)) { return b < p.B ? tiles_at(p.lengths[b]) : 0; };
+    const int length64 = lane < p.B ? p.lengths[lane] : 0, first64 = lane < p.B ? tiles_at(length64) : 0;
     int sum = first64;
     for (int b = 64 + lane; b - lane < p.B; b += 64) sum += tiles(b);
     const int total = prefix_groups * prefix_n * weight + per_b * wave_sum(sum);
@@ -89,7 +91,7 @@ __device__ __forceinline__ Segment segment_of(const CacheParams &p, int lane) {
     const int own_segs = __builtin_amdgcn_readfirstlane(per_b * wave_sum(sum)), prefix_c = (c + weight - 1) / weight, prefix_parts = (prefix_n + prefix_c - 1) / prefix_c, prefix_segs = prefix_groups * prefix_parts;
     // an XCD takes a run of the prefix's segments, which are the longest, and then one of the others: those that read the same keys are neighbours
     const int xcd = (int)blockIdx.x & 7, slot = (int)blockIdx.x >> 3, prefix_run = (prefix_segs + 7) / 8, own_run = (own_segs + 7) / 8;
-    Segment s{-1, -1, 0, 0, 0, 1, 0, 0};
+    Segment s{-1, -1, 0, 0, 0, 1, 0, 0, 0};
     if (slot < prefix_run) {
         const int at = xcd * prefix_run + slot;
         if (at >= prefix_segs) return s;
@@ -106,7 +108,8 @@ __device__ __forceinline__ Segment segment_of(const CacheParams &p, int lane) {
     if (slot - prefix_run >= own_run || at >= own_segs) return s;
     s.place = (p.wide ? 4 : 1) * p.prefix_segs + at;
     for (int b0 = 0; b0 < p.B; b0 += 64) {
-        const int n = b0 ? tiles(b0 + lane) : first64, mine = per_b * ((n + c - 1) / c);
+        const int length = b0 == 0 ? length64 : b0 + lane < p.B ? p.lengths[b0 + lane] : 0;
+        const int n = b0 == 0 ? first64 : b0 + lane < p.B ? tiles_at(length) : 0, mine = per_b * ((n + c - 1) / c);
         int upto = mine;
 #pragma unroll
         for (int m = 1; m < 64; m <<= 1) {
@@ -118,6 +121,7 @@ __device__ __forceinline__ Segment segment_of(const CacheParams &p, int lane) {
             const int who = __builtin_ctzll(past);
             const int rest = at - (__builtin_amdgcn_readlane(upto, who) - __builtin_amdgcn_readlane(mine, who));
             s.n = __builtin_amdgcn_readlane(n, who);
+            s.length = __builtin_amdgcn_readlane(length, who);
             s.parts = (s.n + c - 1) / c;
             s.b = b0 + who;
             const int in_b = rest / s.parts;
@@ -247,10 +251,14 @@ __device__ __forceinline__ void prefix_wide(const CacheParams &p, const Segment 
 // K, V: one buffer of 32 keys each a wave, refilled as soon as its fragments are read: K of the next tile lands under this tile's softmax
 // and second product, V of the next under the next tile's scores.  Eight waves a compute unit at 128 columns, 16 at 64.
 // Probabilities are rounded to the inputs' type for the second product (half a step each, as in smha_sink_fwd); sums are 32 bits.
-// (WIDE: with the wide segments of a prefix, whose registers leave a workgroup less to a unit at 64 columns)
-constexpr int cache_groups(int D, bool wide) { return D == 128 ? 2 : wide ? 3 : 4; }
-template <int D, bool BF16, bool WEIGH, bool WIDE>
-__global__ void __launch_bounds__(256, cache_groups(D, WIDE)) smha_cache_part(const CacheParams p) {
+// Forms: segments cut over the chip; with the wide segments of a prefix too (whose registers leave a workgroup less to a unit at 64 columns); or,
+// where a group has few tiles whatever the lengths are, a workgroup a group, which reads the prefix's keys and the sequence's own one after the
+// other and writes the output: nothing is counted, cut or joined, and the call is one launch.
+enum CacheForm { kCut, kWide, kDirect };
+constexpr int cache_groups(int D, int form) { return D == 128 ? 2 : form == kWide ? 3 : 4; }
+constexpr int kDirectTiles = 16;
+template <int D, bool BF16, bool WEIGH, int FORM>
+__global__ void __launch_bounds__(256, cache_groups(D, FORM)) smha_cache_part(const CacheParams p) {
     constexpr int NS = D / 16, NDT = D / 32, CPR = D / 8, LPT = CPR / 2, RPL = 64 / CPR, NO = 16 / RPL, TB = 32 * D * 2;
     __shared__ __attribute__((aligned(1024))) char all_tiles[4 * 2 * TB];  // per wave: K, V
     __shared__ float team[4][2][32];                                        // references and sums
@@ -258,10 +266,26 @@ __global__ void __launch_bounds__(256, cache_groups(D, WIDE)) smha_cache_part(co
     char *const smem = all_tiles + w * 2 * TB;
     const uint32_t lds = (uint32_t)(uintptr_t)(lds_void *)smem;
     const float NEG_INF = -__builtin_inff();
-    const Segment s = segment_of(p, lane);
-    if (s.place < 0) return;
-    const bool prefix = s.b < 0;
-    const OwnKeys own = prefix ? OwnKeys{p.P, 0, 0, s.n, 0, 0} : own_keys(uniform_load(p.lengths + s.b), p.T, p.Sk, p.window, p.n_sink);
+    constexpr bool WIDE = FORM == kWide, DIRECT = FORM == kDirect;
+    Segment s;
+    if constexpr (DIRECT) {
+        const int per_xcd = (int)gridDim.x >> 3, group = (int)(blockIdx.x & 7) * per_xcd + ((int)blockIdx.x >> 3);
+        if (group >= p.B * p.Hkv * p.own_tiles) return;
+        const int bh = group / p.own_tiles;
+        s.b = bh / p.Hkv;
+        s.hk = bh - s.b * p.Hkv;
+        s.rows0 = 32 * (group - bh * p.own_tiles);
+        s.length = uniform_load(p.lengths + s.b);
+        s.part = 0;
+        s.parts = 1;
+    } else {
+        s = segment_of(p, lane);
+        if (s.place < 0) return;
+    }
+    const bool prefix = !DIRECT && s.b < 0;
+    const OwnKeys own = prefix ? OwnKeys{p.P, 0, 0, s.n, 0, 0} : own_keys(s.length, p.T, p.Sk, p.window, p.n_sink);
+    const int prefix_n = DIRECT ? (p.P + 31) / 32 : 0;  // tiles of the prefix before the sequence's own
+    if constexpr (DIRECT) s.n = prefix_n + own.n;
 
     // this lane's row
     const int GT = p.G * p.T, row = s.rows0 + (WIDE && prefix ? 32 * w : 0) + j, rows = prefix ? p.B * GT : GT;
@@ -280,31 +304,55 @@ __global__ void __launch_bounds__(256, cache_groups(D, WIDE)) smha_cache_part(co
     if constexpr (WIDE) {
         if (prefix) return prefix_wide<D, BF16>(p, s, all_tiles, qf, lane, w);
     }
-    const int64_t ks = prefix ? p.pk_s : p.ks.s, vs = prefix ? p.pv_s : p.vs.s;
-    const uint16_t *const Kb = prefix ? p.PK + s.hk * p.pk_h : p.K + s.b * p.ks.b + s.hk * p.ks.h;
-    const uint16_t *const Vb = prefix ? p.PV + s.hk * p.pv_h : p.V + s.b * p.vs.b + s.hk * p.vs.h;
-    const u32x4 rK = make_rsrc4(Kb, ((int64_t)(own.len - 1) * ks + p.d) * 2), rV = make_rsrc4(Vb, ((int64_t)(own.len - 1) * vs + p.d) * 2);
-    const int ksb = (int)ks * 2, vsb = (int)vs * 2, row0 = lane / CPR;
-    uint32_t k_go[NO], v_go[NO];
+    // Where tiles come from: this segment's keys, and the prefix's where they are read first.
+    struct From {
+        u32x4 rK, rV;
+        int ksb, vsb;
+        uint32_t k_go[NO], v_go[NO];
+    };
+    const int row0 = lane / CPR;
+    auto from = [&](const uint16_t *K, const uint16_t *V, int64_t ks, int64_t vs, int len) __attribute__((always_inline)) {
+        From f;
+        f.rK = make_rsrc4(K, len > 0 ? ((int64_t)(len - 1) * ks + p.d) * 2 : 0);
+        f.rV = make_rsrc4(V, len > 0 ? ((int64_t)(len - 1) * vs + p.d) * 2 : 0);
+        f.ksb = (int)ks * 2;
+        f.vsb = (int)vs * 2;
 #pragma unroll
-    for (int o = 0; o < NO; ++o) {
-        const int ch = (lane % CPR) ^ swz_both<D>(row0 + RPL * o);
-        k_go[o] = ch < (p.d >> 3) ? (uint32_t)(row0 * ksb + ch * 16) : kNoChunk;
-        v_go[o] = ch < (p.d >> 3) ? (uint32_t)(row0 * vsb + ch * 16) : kNoChunk;
+        for (int o = 0; o < NO; ++o) {
+            const int ch = (lane % CPR) ^ swz_both<D>(row0 + RPL * o);
+            f.k_go[o] = ch < (p.d >> 3) ? (uint32_t)(row0 * f.ksb + ch * 16) : kNoChunk;
+            f.v_go[o] = ch < (p.d >> 3) ? (uint32_t)(row0 * f.vsb + ch * 16) : kNoChunk;
+        }
+        return f;
+    };
+    const From mine_f = prefix ? from(p.PK + s.hk * p.pk_h, p.PV + s.hk * p.pv_h, p.pk_s, p.pv_s, p.P)
+                               : from(p.K + s.b * p.ks.b + s.hk * p.ks.h, p.V + s.b * p.vs.b + s.hk * p.vs.h, p.ks.s, p.vs.s, own.len);
+    From first_f = mine_f;
+    if constexpr (DIRECT) {
+        if (p.P) first_f = from(p.PK + s.hk * p.pk_h, p.PV + s.hk * p.pv_h, p.pk_s, p.pv_s, p.P);
     }
+    auto key_of = [&](int tile) __attribute__((always_inline)) { return DIRECT && tile < prefix_n ? 32 * tile : own.key(tile - prefix_n); };
     // keys in the gap between the sinks and the window read as zeros: no query sees them, and they may hold anything
-    auto request = [&](u32x4 rsrc, uint32_t to, const uint32_t (&go)[NO], int pitch, int key) __attribute__((always_inline)) {
+    auto request = [&](u32x4 rsrc, uint32_t to, const uint32_t (&go)[NO], int pitch, int key, int gap0, int gap1) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < LPT; ++i) {
             const int r = key + row0 + RPL * i;
             const uint32_t at = go[i % NO] + (uint32_t)((key + RPL * i) * pitch);
-            load_to_lds(rsrc, to + i * 1024, (int)(r >= own.gap0 && r < own.gap1 ? kPast : at));
+            load_to_lds(rsrc, to + i * 1024, (int)(r >= gap0 && r < gap1 ? kPast : at));
         }
+    };
+    auto request_k = [&](int tile) __attribute__((always_inline)) {
+        if (DIRECT && tile < prefix_n) request(first_f.rK, lds, first_f.k_go, first_f.ksb, key_of(tile), 0, 0);
+        else request(mine_f.rK, lds, mine_f.k_go, mine_f.ksb, key_of(tile), own.gap0, own.gap1);
+    };
+    auto request_v = [&](int tile) __attribute__((always_inline)) {
+        if (DIRECT && tile < prefix_n) request(first_f.rV, lds + TB, first_f.v_go, first_f.vsb, key_of(tile), 0, 0);
+        else request(mine_f.rV, lds + TB, mine_f.v_go, mine_f.vsb, key_of(tile), own.gap0, own.gap1);
     };
     const int begin = (int)((int64_t)s.n * s.part / s.parts) + w, end = (int)((int64_t)s.n * (s.part + 1) / s.parts);
     if (begin < end) {
-        request(rK, lds, k_go, ksb, own.key(begin));
-        request(rV, lds + TB, v_go, vsb, own.key(begin));
+        request_k(begin);
+        request_v(begin);
     }
     const int rd = j * D * 2 + ((hh ^ swz_both<D>(j)) * 16);
     const int tr_row = 4 * hh + ((lane & 15) >> 2);
@@ -317,7 +365,7 @@ __global__ void __launch_bounds__(256, cache_groups(D, WIDE)) smha_cache_part(co
 #pragma unroll
     for (int dt = 0; dt < NDT; ++dt) o[dt] = zeros16();
     for (int tile = begin; tile < end; tile += 4) {
-        const int key = own.key(tile);
+        const int key = key_of(tile);
         const bool more = tile + 4 < end;
         wait_all_but<LPT>();  // K has landed (V's requests came after)
         f32x16 acc = zeros16();
@@ -327,9 +375,9 @@ __global__ void __launch_bounds__(256, cache_groups(D, WIDE)) smha_cache_part(co
 #pragma unroll
         for (int i = 0; i < NS; ++i) acc = mfma32<BF16>(kf[i], qf[i], acc);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // K's buffer is read
-        if (!WEIGH && more) request(rK, lds, k_go, ksb, own.key(tile + 4));
+        if (!WEIGH && more) request_k(tile + 4);
         uint32_t word;
-        if (prefix) word = pos >= 0 ? low_bits32(p.P - key) : 0;
+        if (prefix || (DIRECT && tile < prefix_n)) word = pos >= 0 ? low_bits32(p.P - key) : 0;
         else word = pos >= 0 ? low_bits32(pos - key + 1) & (~low_bits32(pos - p.window + 1 - key) | low_bits32(p.n_sink - key)) : 0;
         if (__builtin_amdgcn_ballot_w64(word != ~0u) != 0) {
             const u32x16 keep = keep_of(word >> (4 * hh)), sc = __builtin_bit_cast(u32x16, acc);
@@ -345,7 +393,7 @@ __global__ void __launch_bounds__(256, cache_groups(D, WIDE)) smha_cache_part(co
                 }
             }
             asm volatile("" ::: "memory");
-            if (more) request(rK, lds, k_go, ksb, own.key(tile + 4));
+            if (more) request_k(tile + 4);
         }
         float mt = NEG_INF;
 #pragma unroll
@@ -375,7 +423,7 @@ __global__ void __launch_bounds__(256, cache_groups(D, WIDE)) smha_cache_part(co
             o[i % NDT] = mfma32<BF16>(u32x4{lo[0], lo[1], hi[0], hi[1]}, pf[i / NDT], o[i % NDT]);
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // V's buffer is read
-        if (more) request(rV, lds + TB, v_go, vsb, own.key(tile + 4));
+        if (more) request_v(tile + 4);
     }
 
     // The team joins: every wave leaves its accumulators in its own tiles' place and takes a quarter of the columns of all four.
@@ -410,8 +458,8 @@ __global__ void __launch_bounds__(256, cache_groups(D, WIDE)) smha_cache_part(co
             for (int e = 0; e < 4; ++e) out[4 * i + e] = fmaf(share, v[e], out[4 * i + e]);
         }
     }
-    if (s.part == 0 && threadIdx.x == 0) p.info[s.group] = int2{s.place, s.parts};
-    const bool whole = s.parts == 1 && p.prefix_tiles == 0;  // nothing to join with
+    if (!DIRECT && s.part == 0 && threadIdx.x == 0) p.info[s.group] = int2{s.place, s.parts};
+    const bool whole = DIRECT || (s.parts == 1 && p.prefix_tiles == 0);  // nothing to join with
     if (row < rows) {
         if (!whole || WEIGH) {
             if (w == 0 && hh == 0) {
@@ -472,42 +520,67 @@ __global__ void __launch_bounds__(256) smha_cache_join(const CacheParams p, int 
     if ((int)blockIdx.x < row_groups) {
         const int id = blockIdx.x, b = id / (p.Hkv * GT), hk = id / GT - b * p.Hkv, in_b = id % GT, g = in_b / p.T, t = in_b - g * p.T;
         const int len = min(max(p.lengths[b], 0), p.Sk);
+        RowParts r = row_parts(p, b, hk, in_b, true);  // (of a sequence without keys its own are not there)
+        if (len == 0) r.count[1] = 0;
         uint16_t *const to = p.O + b * p.os.b + (hk * p.G + g) * p.os.h + t * p.os.s;
         if (len - p.T + t < 0) {  // no such query
             for (int c = threadIdx.x; c < p.d; c += 256) to[c] = 0;
             return;
         }
-        const RowParts r = row_parts(p, b, hk, in_b, len > 0);
         if (!p.prefix_tiles && r.count[1] == 1) return;  // written whole
+        // Wave w takes segments w, w + 4, ..., four at a time; a lane D / 64 columns.  (All of a turn's loads travel together: a call's rows
+        // fit the chip at once, and what such a row lasts is its chain of trips to memory.)
+        constexpr int E = D / 64;
         const int n = r.n();
-        float m = NEG_INF;
-        for (int i = threadIdx.x; i < n; i += 256) m = fmaxf(m, p.stats[r.stat(i)]);
+        float m = NEG_INF, sum = 0.f, acc[E];
 #pragma unroll
-        for (int x = 32; x > 0; x >>= 1) m = fmaxf(m, __shfl_xor(m, x));
-        if (lane == 0) lds_ml[0][w] = m;
-        __syncthreads();
-        m = fmaxf(fmaxf(lds_ml[0][0], lds_ml[0][1]), fmaxf(lds_ml[0][2], lds_ml[0][3]));
-        // wave w takes segments w, w + 4, ...; a lane D / 64 columns
-        float sum = 0.f, acc[D / 64];
+        for (int e = 0; e < E; ++e) acc[e] = 0.f;
+        for (int i0 = w; i0 < n; i0 += 16) {
+            float ref[4], part[4], x[4][E], top = m;
 #pragma unroll
-        for (int e = 0; e < D / 64; ++e) acc[e] = 0.f;
-#pragma unroll 4
-        for (int i = w; i < n; i += 4) {
-            const int64_t at = r.stat(i), part = r.part(i) * D;
-            const float ref = p.stats[at], share = ref != NEG_INF ? fast_exp2(ref - m) : 0.f;
-            sum = fmaf(share, p.stats[at + 32], sum);
+            for (int u = 0; u < 4; ++u) {
+                const int i = i0 + 4 * u < n ? i0 + 4 * u : i0;
+                const float *const at = p.parts + r.part(i) * D + E * lane;
+                ref[u] = p.stats[r.stat(i)];
+                part[u] = p.stats[r.stat(i) + 32];
 #pragma unroll
-            for (int e = 0; e < D / 64; ++e) acc[e] = fmaf(share, p.parts[part + lane + 64 * e], acc[e]);
+                for (int e = 0; e < E; ++e) x[u][e] = at[e];
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                if (i0 + 4 * u >= n) ref[u] = NEG_INF;
+                top = fmaxf(top, ref[u]);
+            }
+            const float old = m != NEG_INF ? fast_exp2(m - top) : 0.f;
+            sum *= old;
+#pragma unroll
+            for (int e = 0; e < E; ++e) acc[e] *= old;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const float share = ref[u] != NEG_INF ? fast_exp2(ref[u] - top) : 0.f;
+                sum = fmaf(share, part[u], sum);
+#pragma unroll
+                for (int e = 0; e < E; ++e) acc[e] = ref[u] != NEG_INF ? fmaf(share, x[u][e], acc[e]) : acc[e];
+            }
+            m = top;
         }
-        if (lane == 0) lds_ml[1][w] = sum;
-#pragma unroll
-        for (int e = 0; e < D / 64; ++e) lds_o[w][lane + 64 * e] = acc[e];
-        __syncthreads();
-        const float l = lds_ml[1][0] + lds_ml[1][1] + lds_ml[1][2] + lds_ml[1][3], inv = l > 0.f ? 1.0f / l : 0.f;
-        for (int c = threadIdx.x; c < p.d; c += 256) {
-            const float v = (lds_o[0][c] + lds_o[1][c] + lds_o[2][c] + lds_o[3][c]) * inv;
-            to[c] = (uint16_t)pack2<BF16>(v, 0.f);
+        if (lane == 0) {
+            lds_ml[0][w] = m;
+            lds_ml[1][w] = sum;
         }
+#pragma unroll
+        for (int e = 0; e < E; ++e) lds_o[w][E * lane + e] = acc[e];
+        __syncthreads();
+        const float top = fmaxf(fmaxf(lds_ml[0][0], lds_ml[0][1]), fmaxf(lds_ml[0][2], lds_ml[0][3]));
+        float share[4], l = 0.f;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            share[u] = lds_ml[0][u] != NEG_INF ? fast_exp2(lds_ml[0][u] - top) : 0.f;
+            l = fmaf(share[u], lds_ml[1][u], l);
+        }
+        const float inv = l > 0.f ? 1.0f / l : 0.f;
+        for (int c = threadIdx.x; c < p.d; c += 256)
+            to[c] = (uint16_t)pack2<BF16>((share[0] * lds_o[0][c] + share[1] * lds_o[1][c] + share[2] * lds_o[2][c] + share[3] * lds_o[3][c]) * inv, 0.f);
         return;
     }
     const int id = (int)blockIdx.x - row_groups, bh = id / key_groups, b = bh / p.Hkv, hk = bh - b * p.Hkv;
@@ -858,7 +931,9 @@ static smha_status_t cache_params(CacheParams &cp, CacheLayout &at, int B, int H
     cp.window = window == 0 || window > Sk ? Sk : window;
     cp.n_sink = std::min(n_sink, Sk);
     const int64_t rows = (int64_t)cp.G * T, own_tiles = (rows + 31) / 32;
-    cp.wide = P > 0 && B * rows > 64;  // (one or two tiles of 32 rows: reading the keys once or twice by waves on their own fills the chip better)
+    const int64_t own_tiles_most = std::min<int64_t>(Sk, (int64_t)cp.window + cp.n_sink + T) / 32 + 3;
+    cp.direct = !weigh && own_tiles_most + (P + 31) / 32 <= kDirectTiles;
+    cp.wide = !cp.direct && P > 0 && B * rows > 64;  // (one or two tiles of 32 rows: reading the keys once or twice by waves on their own fills the chip better)
     const int64_t prefix_tiles = !P ? 0 : cp.wide ? (B * rows + 127) / 128 : (B * rows + 31) / 32;
     const int64_t groups = (int64_t)Hkv * (prefix_tiles + B * own_tiles);
     // (tiles and rows are counted in 32 bits)
@@ -866,15 +941,19 @@ static smha_status_t cache_params(CacheParams &cp, CacheLayout &at, int B, int H
     cp.own_tiles = (int)own_tiles;
     cp.prefix_tiles = (int)prefix_tiles;
     const int D = d <= 64 ? 64 : 128;
-    cp.slots = 256 * cache_groups(D, cp.wide);  // what the chip holds at once
+    cp.slots = 256 * cache_groups(D, cp.wide ? kWide : kCut);  // what the chip holds at once
     // no more segments than that and one a group, and none shorter than four tiles unless it is a group
-    const int64_t own_most = (std::min<int64_t>(Sk, (int64_t)cp.window + cp.n_sink + T) / 32 + 3 + 3) / 4;
+    const int64_t own_most = (own_tiles_most + 3) / 4;
     const int64_t prefix_most = Hkv * prefix_tiles * (cp.wide ? (P / 64 + 1 + 1) / 2 : (P / 32 + 1 + 3) / 4);
     cp.prefix_segs = (int)std::min<int64_t>(cp.slots + Hkv * prefix_tiles, prefix_most);
     const int64_t own_segs = std::min<int64_t>(cp.slots + (int64_t)B * Hkv * own_tiles, B * Hkv * own_tiles * own_most);
     cp.segs = (int)(cp.prefix_segs + own_segs);
     const int64_t places = (cp.wide ? 4 : 1) * (int64_t)cp.prefix_segs + own_segs;
     cp.score_pitch = (Sk + 31) / 32 * 32;
+    if (cp.direct) {  // (nothing is kept: a size for callers that allocate what they are told)
+        at.total = 16;
+        return SMHA_OK;
+    }
     at.info = 0;
     at.stats = up(groups * sizeof(int2));
     at.parts = at.stats + up((size_t)places * 64 * 4);
@@ -884,9 +963,14 @@ static smha_status_t cache_params(CacheParams &cp, CacheLayout &at, int B, int H
 }
 
 template <int D, bool BF16> static hipError_t launch_cache(const CacheParams &cp, hipStream_t stream) {
+    if (cp.direct) {
+        const int groups = cp.B * cp.Hkv * cp.own_tiles;
+        hipLaunchKernelGGL((smha_cache_part<D, BF16, false, kDirect>), dim3(8 * ((groups + 7) / 8)), dim3(256), 0, stream, cp);
+        return hipGetLastError();
+    }
     const dim3 grid(8 * ((cp.segs + 7) / 8 + 1));  // (two runs an XCD, each rounded up)
-    auto *const part = cp.weights ? (cp.wide ? smha_cache_part<D, BF16, true, true> : smha_cache_part<D, BF16, true, false>)
-                                  : (cp.wide ? smha_cache_part<D, BF16, false, true> : smha_cache_part<D, BF16, false, false>);
+    auto *const part = cp.weights ? (cp.wide ? smha_cache_part<D, BF16, true, kWide> : smha_cache_part<D, BF16, true, kCut>)
+                                  : (cp.wide ? smha_cache_part<D, BF16, false, kWide> : smha_cache_part<D, BF16, false, kCut>);
     hipLaunchKernelGGL(part, grid, dim3(256), 0, stream, cp);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;

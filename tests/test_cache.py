@@ -109,7 +109,8 @@ def test_attention_is_the_formula(case, dtype, weigh):
         untouched = received == 0
         assert torch.equal(weights.cpu()[untouched], before.cpu()[untouched])
     again = torch.full_like(out, math.nan)
-    assert smha.cache_attention(q, k, v, int32(lengths), window=window, n_sink=n_sink, prefix=prefix, out=again) is again
+    weights = before.clone() if weigh else None
+    assert smha.cache_attention(q, k, v, int32(lengths), window=window, n_sink=n_sink, prefix=prefix, weights=weights, out=again) is again
     assert torch.equal(again, out)
 
 
@@ -118,12 +119,14 @@ def test_what_is_not_seen_may_hold_anything():
     q, k, v, _ = make(2, 8, 2, 2, 600, 128)
     lengths, window, n_sink = [555, 1], 100, 5
     want = smha.cache_attention(q, k, v, int32(lengths), window=window, n_sink=n_sink)
+    want_weighed = smha.cache_attention(q, k, v, int32(lengths), window=window, n_sink=n_sink, weights=torch.zeros(2, 2, 600, device="cuda"))
     for t in (k, v):
         t[0, :, 555:] = math.nan
         t[0, :, 5:455 - 1] = math.inf
         t[1, :, 1:] = math.nan
     weights = torch.zeros(2, 2, 600, device="cuda")
-    assert torch.equal(smha.cache_attention(q, k, v, int32(lengths), window=window, n_sink=n_sink, weights=weights), want)
+    assert torch.equal(smha.cache_attention(q, k, v, int32(lengths), window=window, n_sink=n_sink), want)
+    assert torch.equal(smha.cache_attention(q, k, v, int32(lengths), window=window, n_sink=n_sink, weights=weights), want_weighed)
     # (sequence 1's first token does not exist: its 8 queries are one token's)
     assert abs(float(weights[0].sum()) - 16) < 1e-3 and abs(float(weights[1].sum()) - 8) < 1e-3
     assert bool((weights[0, :, 5:454] == 0).all()) and bool((weights[:, :, 555:] == 0).all())
@@ -156,11 +159,12 @@ def test_strides_streams_and_a_captured_call():
     want = smha.cache_attention(q, k, v, n, prefix=prefix, weights=plain_w)
     got = smha.cache_attention(q, big_k[:, :, 50:350, :64], big_v[:, :, 50:350, :64], n, prefix=(pk, pv), weights=wide[:, :, 10:310])
     assert torch.equal(got, want) and torch.equal(wide[:, :, 10:310], plain_w) and not wide[:, :, :10].any() and not wide[:, :, 310:].any()
+    plain = smha.cache_attention(q, k, v, n, prefix=prefix)
     side = torch.cuda.Stream()
     torch.cuda.synchronize()
     got = smha.cache_attention(q, k, v, n, prefix=prefix, stream=side)
     side.synchronize()
-    assert torch.equal(got, want)
+    assert torch.equal(got, plain)
     graph = torch.cuda.CUDAGraph()
     weights = torch.zeros(3, 2, 300, device="cuda")
     with torch.cuda.graph(graph):
@@ -344,7 +348,8 @@ def test_refusals():
         return lib.smha_cache_forward(q, ptr, ptr, pk, pk, ptr, None, lengths, B, H, Hkv, T, Sk, P, d, dtype, None, s, None, None, None, None, None, window, n_sink,
                                       0.0, ws, size, None)
 
-    assert forward(q=None) == invalid and forward(lengths=None) == invalid and forward(ws=None) == invalid and forward(size=100) == invalid
+    assert forward(q=None) == invalid and forward(lengths=None) == invalid and forward(ws=None) == invalid and forward(size=15) == invalid
+    assert forward(Sk=4000, size=1000) == invalid
     assert forward(B=0) == invalid and forward(T=0) == invalid and forward(P=-1) == invalid and forward(P=5) == invalid and forward(window=-1) == invalid
     assert forward(H=3) == shape
     assert forward(d=136) == unsupported and forward(d=20) == unsupported and forward(dtype=2) == unsupported
@@ -385,4 +390,4 @@ def test_refusals_of_the_binding():
     with pytest.raises(smha.SmhaError):
         smha.cache_attention(q, k, v, n, prefix=prefix, window=4)
     with pytest.raises(smha.SmhaError):
-        smha.cache_attention(q, k, v, n, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
+        smha.cache_attention(q, k, v, n, workspace=torch.empty(8, dtype=torch.uint8, device="cuda"))
