@@ -75,20 +75,22 @@ __device__ __forceinline__ int wave_sum(int v) {
 
 // The segment of a workgroup.  Every wave of the launch computes the same cut: c tiles a segment at most, so many (in fours, a team's turn) that
 // all tiles make `slots` segments.  Groups shorter than that are a segment each, and then there are more: what does not fit at first
-// starts as others end.  A wide tile takes about as long as three of the others, which its waves share.
+// starts as others end.  (A wide tile counts like one of the others, though it lasts longer: each of a wide segment's 128 rows leaves a result to
+// join, and more and shorter segments cost more than they even out.  64 x 32 on 8 heads, 8192 shared keys and 280 of their own, counted
+// as 1, 2, 3, 4: 38.1, 42.3, 44.4, 46.7 us.)
 __device__ __forceinline__ Segment segment_of(const CacheParams &p, int lane) {
     const int prefix_groups = p.Hkv * p.prefix_tiles, per_b = p.Hkv * p.own_tiles;
-    const int prefix_n = !p.prefix_tiles ? 0 : p.wide ? (p.P + 63) / 64 : (p.P + 31) / 32, weight = p.wide ? 3 : 1;
+    const int prefix_n = !p.prefix_tiles ? 0 : p.wide ? (p.P + 63) / 64 : (p.P + 31) / 32;
     auto tiles_at = [&](int length) __attribute__((always_inline)) { return own_keys(length, p.T, p.Sk, p.window, p.n_sink).n; };
     auto tiles = [&](int b) __attribute__((always_inline)) { return b < p.B ? tiles_at(p.lengths[b]) : 0; };
     const int length64 = lane < p.B ? p.lengths[lane] : 0, first64 = lane < p.B ? tiles_at(length64) : 0;
     int sum = first64;
     for (int b = 64 + lane; b - lane < p.B; b += 64) sum += tiles(b);
-    const int total = prefix_groups * prefix_n * weight + per_b * wave_sum(sum);
+    const int total = prefix_groups * prefix_n + per_b * wave_sum(sum);
     const int c = __builtin_amdgcn_readfirstlane(max(4, ((total + p.slots - 1) / p.slots + 3) & ~3));
     sum = (first64 + c - 1) / c;
     for (int b = 64 + lane; b - lane < p.B; b += 64) sum += (tiles(b) + c - 1) / c;
-    const int own_segs = __builtin_amdgcn_readfirstlane(per_b * wave_sum(sum)), prefix_c = (c + weight - 1) / weight, prefix_parts = (prefix_n + prefix_c - 1) / prefix_c, prefix_segs = prefix_groups * prefix_parts;
+    const int own_segs = __builtin_amdgcn_readfirstlane(per_b * wave_sum(sum)), prefix_parts = (prefix_n + c - 1) / c, prefix_segs = prefix_groups * prefix_parts;
     // an XCD takes a run of the prefix's segments, which are the longest, and then one of the others: those that read the same keys are neighbours
     const int xcd = (int)blockIdx.x & 7, slot = (int)blockIdx.x >> 3, prefix_run = (prefix_segs + 7) / 8, own_run = (own_segs + 7) / 8;
     Segment s{-1, -1, 0, 0, 0, 1, 0, 0, 0};
@@ -646,6 +648,36 @@ struct EvictParams {
     int32_t *lists;                             // [B Hkv][1 + 2 moves]: count, where to, where from
 };
 
+// Running sums over a wave's lanes, and over groups of 16 of them, without LDS.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int add_moved(int v) { return v + __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xF, false); }
+__device__ __forceinline__ int row_scan(int v) {
+    v = add_moved<0x111, 0xF>(v);  // row_shr 1, 2, 4, 8
+    v = add_moved<0x112, 0xF>(v);
+    v = add_moved<0x114, 0xF>(v);
+    return add_moved<0x118, 0xF>(v);
+}
+__device__ __forceinline__ int wave_scan(int v) {
+    v = row_scan(v);
+    v = add_moved<0x142, 0xA>(v);     // the first and third row's sums to the second and fourth
+    return add_moved<0x143, 0xC>(v);  // the first half's to the second
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int max_moved(int v) { return max(v, __builtin_amdgcn_update_dpp(v, v, CTRL, ROWS, 0xF, false)); }
+__device__ __forceinline__ int row_max(int v) {  // lane 15 of each row of 16: the row's
+    v = max_moved<0x111, 0xF>(v);
+    v = max_moved<0x112, 0xF>(v);
+    v = max_moved<0x114, 0xF>(v);
+    return max_moved<0x118, 0xF>(v);
+}
+__device__ __forceinline__ int wave_max(int v) { return __builtin_amdgcn_readlane(max_moved<0x143, 0xC>(max_moved<0x142, 0xA>(row_max(v))), 63); }
+// Of 16 waves' numbers: those before wave w, and all.
+__device__ __forceinline__ void before_and_all(const int *numbers, int lane, int w, int &before, int &all) {
+    const int upto = row_scan(numbers[lane & 15]);
+    all = __builtin_amdgcn_readlane(upto, 15);
+    before = w ? __builtin_amdgcn_readlane(upto, w - 1) : 0;
+}
+
 // An order of 32-bit floats as unsigned numbers, NaN with the lowest, -0 with +0.
 __device__ __forceinline__ uint32_t ordered(float x) {
     if (!(x == x)) return 0x007FFFFFu;  // -inf's
@@ -661,68 +693,74 @@ __device__ __forceinline__ uint32_t ordered(float x) {
 template <int KPT>
 __global__ void __launch_bounds__(1024) smha_cache_select(const EvictParams p) {
     __shared__ int bins[2048];
-    __shared__ int totals[16][2];
+    __shared__ int totals[3][16];
     __shared__ int found[2];
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int bh = blockIdx.x, b = bh / p.Hkv, hk = bh - b * p.Hkv;
-    const int len = min(max(p.lengths[b], 0), p.Sk), end = min(len, p.budget);
+    const int bh = blockIdx.x, b = bh / p.Hkv;
+    const int len = min(max(uniform_load(p.lengths + b), 0), p.Sk), end = min(len, p.budget);
     const float *const W = p.w + (int64_t)bh * p.Sk;
     const int32_t *const P = p.pos + (int64_t)bh * p.Sk;
     float *const Wo = p.w_out + (int64_t)bh * p.Sk;
     int32_t *const Po = p.pos_out + (int64_t)bh * p.Sk;
     int32_t *const list = p.lists + (int64_t)bh * (1 + 2 * (int64_t)p.moves);
-    const bool copies = W != Wo || P != Po;
-    if (len <= p.budget) {
-        if (threadIdx.x == 0) list[0] = 0;
-        if (copies)
-            for (int i = threadIdx.x; i < len; i += 1024) {
-                Wo[i] = W[i];
-                Po[i] = P[i];
-            }
-        return;
-    }
     const int n = (len + 1023) / 1024, base = w * 64 * n + lane;  // keys a lane, its first slot
     constexpr int HELD = KPT ? KPT : 1;
-    float held_w[HELD];
+    uint32_t held[HELD];  // first the weights
     int32_t held_p[HELD];
+    if constexpr (KPT > 0) {
+        if (len > p.budget) {
+#pragma unroll
+            for (int i = 0; i < KPT; ++i) {
+                const int slot = min(base + 64 * i, len - 1);  // (past the end: the last one again)
+                if (i < n) {
+                    held[i] = __builtin_bit_cast(uint32_t, W[slot]);
+                    held_p[i] = P[slot];
+                }
+            }
+        }
+    }
+    // (all slots before the end: those that are freed are written again below)
+    if (Wo != W)
+        for (int i = threadIdx.x; i < end; i += 1024) Wo[i] = W[i];
+    if (Po != P)
+        for (int i = threadIdx.x; i < end; i += 1024) Po[i] = P[i];
+    if (len <= p.budget) {
+        if (threadIdx.x == 0) list[0] = 0;
+        return;
+    }
     int newest = INT32_MIN;
     if constexpr (KPT > 0) {
 #pragma unroll
-        for (int i = 0; i < KPT; ++i) {
-            const int slot = min(base + 64 * i, len - 1);  // (past the end: the last one again)
-            held_w[i] = i < n ? W[slot] : 0.f;
-            held_p[i] = i < n ? P[slot] : INT32_MIN;
-        }
-#pragma unroll
-        for (int i = 0; i < KPT; ++i) newest = max(newest, held_p[i]);
+        for (int i = 0; i < KPT; ++i)
+            if (i < n) newest = max(newest, held_p[i]);
     } else {
         for (int i = threadIdx.x; i < len; i += 1024) newest = max(newest, P[i]);
     }
-#pragma unroll
-    for (int m = 32; m > 0; m >>= 1) newest = max(newest, __shfl_xor(newest, m));
-    if (lane == 0) totals[w][0] = newest;
+    newest = wave_max(newest);
+    if (lane == 0) totals[0][w] = newest;
     for (int i = threadIdx.x; i < 2048; i += 1024) bins[i] = 0;
     __syncthreads();
-#pragma unroll
-    for (int u = 0; u < 16; ++u) newest = max(newest, totals[u][0]);
-    const int64_t young = (int64_t)newest - p.recent;  // positions past this stay, whatever their account
+    newest = __builtin_amdgcn_readlane(row_max(totals[0][lane & 15]), 15);
+    // positions past this stay, whatever their account; where there are none so low, all
+    const bool all_young = (int64_t)newest - p.recent < INT32_MIN;
+    const int young = all_young ? INT32_MIN : newest - p.recent;
     auto key_from = [&](int slot, float x, int32_t at) __attribute__((always_inline)) -> uint32_t {
-        return slot >= len ? 0u : (int64_t)at > young ? 0xFF800000u : ordered(x);  // (0: below every live key's)
+        return slot >= len ? 0u : all_young || at > young ? 0xFF800000u : ordered(x);  // (0: below every live key's)
     };
-    uint32_t held[HELD];
     if constexpr (KPT > 0) {
 #pragma unroll
-        for (int i = 0; i < KPT; ++i) held[i] = key_from(base + 64 * i, held_w[i], held_p[i]);
+        for (int i = 0; i < KPT; ++i)
+            if (i < n) held[i] = key_from(base + 64 * i, __builtin_bit_cast(float, held[i]), held_p[i]);
     }
     auto each = [&](auto &&f) __attribute__((always_inline)) {
         if constexpr (KPT > 0) {
 #pragma unroll
             for (int i = 0; i < KPT; ++i)
-                if (i < n) f(i, held[i]);
+                if (i < n) f(held[i]);
         } else {
             for (int i = 0; i < n; ++i) {
                 const int slot = base + 64 * i;
-                f(i, slot < len ? key_from(slot, W[slot], P[slot]) : 0u);
+                f(slot < len ? key_from(slot, W[slot], P[slot]) : 0u);
             }
         }
     };
@@ -732,35 +770,29 @@ __global__ void __launch_bounds__(1024) smha_cache_select(const EvictParams p) {
 #pragma unroll
     for (int pass = 0; pass < 3; ++pass) {
         const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, width = pass == 2 ? 10 : 11;
-        each([&](int, uint32_t k) __attribute__((always_inline)) {
-            const bool in = pass == 0 ? k != 0 : (k >> (shift + width)) == (least >> (shift + width)) && k != 0;
-            const int bin = (int)(k >> shift) & ((1 << width) - 1);
+        each([&](uint32_t k) __attribute__((always_inline)) {
+            // (what is known of `least` is not zero: no live key's is, and the others' numbers do not match it)
+            const bool in = pass == 0 ? k != 0 : (k >> (shift + width)) == (least >> (shift + width));
             const uint64_t who = __builtin_amdgcn_ballot_w64(in);
-            if (who) {
-                const int one = __builtin_amdgcn_readlane(bin, __builtin_ctzll(who));
-                if (__builtin_amdgcn_ballot_w64(in && bin != one) == 0) {
-                    if (lane == 0) atomicAdd(&bins[one], __builtin_popcountll(who));
-                } else if (in) {
-                    atomicAdd(&bins[bin], 1);
-                }
+            if (who == 0) return;
+            const int bin = (int)(k >> shift) & ((1 << width) - 1);
+            const int one = __builtin_amdgcn_readlane(bin, __builtin_ctzll(who));
+            if (__builtin_amdgcn_ballot_w64(in && bin != one) == 0) {
+                if (lane == 0) atomicAdd(&bins[one], __builtin_popcountll(who));
+            } else if (in) {
+                atomicAdd(&bins[bin], 1);
             }
         });
         __syncthreads();
         // a thread's two bins, from the top, and those over them
         const int top = 2047 - 2 * (int)threadIdx.x, n1 = bins[top], n0 = bins[top - 1];
-        int upto = n1 + n0;
-#pragma unroll
-        for (int m = 1; m < 64; m <<= 1) {
-            const int below = __shfl_up(upto, m);
-            if (lane >= m) upto += below;
-        }
-        if (lane == 63) totals[w][1] = upto;
+        const int upto = wave_scan(n1 + n0);
+        if (lane == 63) totals[1][w] = upto;
         __syncthreads();
         bins[top] = bins[top - 1] = 0;
-        int over = all_over + upto - n1 - n0;
-#pragma unroll
-        for (int u = 0; u < 16; ++u)
-            if (u < w) over += totals[u][1];
+        int before, all;
+        before_and_all(totals[1], lane, w, before, all);
+        const int over = all_over + before + upto - n1 - n0;
         if (over < end && over + n1 >= end) {
             found[0] = top;
             found[1] = over;
@@ -776,16 +808,17 @@ __global__ void __launch_bounds__(1024) smha_cache_select(const EvictParams p) {
     const int equal_stay = end - all_over;
     const uint64_t below = (1ull << lane) - 1;
     constexpr int GROUP = KPT ? KPT : 32;  // keys of such a word
-    auto words = [&](int i0, uint32_t &over, uint32_t &equal) __attribute__((always_inline)) {
+    uint32_t over, equal;
+    auto words = [&](int i0) __attribute__((always_inline)) {
         over = equal = 0;
 #pragma unroll
         for (int i = 0; i < GROUP; ++i) {
-            uint32_t k;
+            uint32_t k = 0u;
             if constexpr (KPT > 0) {
-                k = i < n ? held[i] : 0u;
+                if (i < n) k = held[i];
             } else {
                 const int slot = base + 64 * (i0 + i);
-                k = i0 + i < n && slot < len ? key_from(slot, W[slot], P[slot]) : 0u;
+                if (i0 + i < n && slot < len) k = key_from(slot, W[slot], P[slot]);
             }
             over |= (uint32_t)(k > least) << i;
             equal |= (uint32_t)(k == least) << i;
@@ -802,31 +835,27 @@ __global__ void __launch_bounds__(1024) smha_cache_select(const EvictParams p) {
             at += __builtin_popcountll(who);
         }
     };
-    uint32_t over, equal;
     int count = 0;
     for (int i0 = 0; i0 < n; i0 += GROUP) {
-        words(i0, over, equal);
+        words(i0);
         count += __builtin_popcount(equal);
     }
-    count = wave_sum(count);
-    if (lane == 0) totals[w][0] = count;
+    count = wave_scan(count);
+    if (lane == 63) totals[0][w] = count;
     __syncthreads();
-    int equal_at = 0;
-#pragma unroll
-    for (int u = 0; u < 16; ++u)
-        if (u < w) equal_at += totals[u][0];
-    const int equal_first = equal_at;
+    int equal_first, all;
+    before_and_all(totals[0], lane, w, equal_first, all);
+    int equal_at = equal_first;
     // bits of `over` and of the equals that stay
     auto staying = [&](int i0) __attribute__((always_inline)) {
-        words(i0, over, equal);
+        if constexpr (KPT == 0) words(i0);
         uint32_t stay = over;
         in_order(equal, equal_at, [&](int i, int place) __attribute__((always_inline)) {
             if (place < equal_stay) stay |= 1u << i;
         });
         return stay;
     };
-    // of the group's keys, those in slots before the end
-    // (a lane has n keys: later bits of a word are other waves' slots)
+    // of the group's keys, those in slots before the end (a lane has n keys: later bits of a word are other waves' slots)
     auto before_end = [&](int i0) __attribute__((always_inline)) { return low_bits32(min((end - (base + 64 * i0) + 63) >> 6, n - i0)); };
     int freed = 0, kept = 0;
     uint32_t stay = 0;
@@ -836,41 +865,22 @@ __global__ void __launch_bounds__(1024) smha_cache_select(const EvictParams p) {
         freed += __builtin_popcount(~stay & early);
         kept += __builtin_popcount(stay & ~early);
     }
-    freed = wave_sum(freed);
-    kept = wave_sum(kept);
-    __syncthreads();
-    if (lane == 0) {
-        totals[w][0] = freed;
-        totals[w][1] = kept;
+    freed = wave_scan(freed);
+    kept = wave_scan(kept);
+    if (lane == 63) {
+        totals[1][w] = freed;
+        totals[2][w] = kept;
     }
     __syncthreads();
-    int to = 0, from = 0, moves = 0;
-#pragma unroll
-    for (int u = 0; u < 16; ++u) {
-        if (u < w) to += totals[u][0], from += totals[u][1];
-        moves += totals[u][0];
-    }
+    int to, from, moves;
+    before_and_all(totals[2], lane, w, from, all);
+    before_and_all(totals[1], lane, w, to, moves);
     equal_at = equal_first;
     for (int i0 = 0; i0 < n; i0 += GROUP) {
         if constexpr (KPT == 0) stay = staying(i0);
         const uint32_t early = before_end(i0);
         in_order(~stay & early, to, [&](int i, int place) __attribute__((always_inline)) { list[1 + place] = base + 64 * (i0 + i); });
         in_order(stay & ~early, from, [&](int i, int place) __attribute__((always_inline)) { list[1 + p.moves + place] = base + 64 * (i0 + i); });
-        if (copies) {
-#pragma unroll
-            for (int i = 0; i < GROUP; ++i) {
-                const int slot = base + 64 * (i0 + i);
-                if ((stay & early) >> i & 1) {
-                    if constexpr (KPT > 0 && KPT < 32) {  // (32 of each would not fit the registers)
-                        Wo[slot] = held_w[i];
-                        Po[slot] = held_p[i];
-                    } else {
-                        Wo[slot] = W[slot];
-                        Po[slot] = P[slot];
-                    }
-                }
-            }
-        }
     }
     if (threadIdx.x == 0) list[0] = moves;
     __syncthreads();
@@ -931,7 +941,7 @@ static smha_status_t cache_params(CacheParams &cp, CacheLayout &at, int B, int H
     cp.window = window == 0 || window > Sk ? Sk : window;
     cp.n_sink = std::min(n_sink, Sk);
     const int64_t rows = (int64_t)cp.G * T, own_tiles = (rows + 31) / 32;
-    const int64_t own_tiles_most = std::min<int64_t>(Sk, (int64_t)cp.window + cp.n_sink + T) / 32 + 3;
+    const int64_t own_tiles_most = std::min<int64_t>((Sk + 31) / 32, ((int64_t)cp.window + cp.n_sink + T) / 32 + 3);
     cp.direct = !weigh && own_tiles_most + (P + 31) / 32 <= kDirectTiles;
     cp.wide = !cp.direct && P > 0 && B * rows > 64;  // (one or two tiles of 32 rows: reading the keys once or twice by waves on their own fills the chip better)
     const int64_t prefix_tiles = !P ? 0 : cp.wide ? (B * rows + 127) / 128 : (B * rows + 31) / 32;
@@ -944,7 +954,7 @@ static smha_status_t cache_params(CacheParams &cp, CacheLayout &at, int B, int H
     cp.slots = 256 * cache_groups(D, cp.wide ? kWide : kCut);  // what the chip holds at once
     // no more segments than that and one a group, and none shorter than four tiles unless it is a group
     const int64_t own_most = (own_tiles_most + 3) / 4;
-    const int64_t prefix_most = Hkv * prefix_tiles * (cp.wide ? (P / 64 + 1 + 1) / 2 : (P / 32 + 1 + 3) / 4);
+    const int64_t prefix_most = Hkv * prefix_tiles * (((cp.wide ? P / 64 : P / 32) + 1 + 3) / 4);
     cp.prefix_segs = (int)std::min<int64_t>(cp.slots + Hkv * prefix_tiles, prefix_most);
     const int64_t own_segs = std::min<int64_t>(cp.slots + (int64_t)B * Hkv * own_tiles, B * Hkv * own_tiles * own_most);
     cp.segs = (int)(cp.prefix_segs + own_segs);
