@@ -260,38 +260,11 @@ __global__ void __launch_bounds__(256, D == 64 ? 4 : 2) smha_sink_fwd(const Sink
 // ---------------------------------------------------------------------------------------
 // Backward
 // ---------------------------------------------------------------------------------------
-// lse and delta of every query in the form that the two kernels below take them; queries that do not exist get lse = inf, so that
-// their probabilities are zero.  16 lanes a row.  delta from the rounded output alone is as far off as dS is by its own rounding (dQ and dK
-// 1.52 times as far from 64 bits as an evaluation in 32 bits that is rounded once, 1.42 times with what the rounding left out).
-template <bool BF16>
-__global__ void __launch_bounds__(256) smha_sink_stats(const SinkParams p) {
-    const int64_t row = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4), rows = (int64_t)p.B * p.H * p.Sqp;
-    if (row >= rows) return;
-    const int bh = (int)(row / p.Sqp), q = (int)(row - (int64_t)bh * p.Sqp), b = bh / p.H, h = bh - b * p.H, c = threadIdx.x & 15;
-    const int len = p.lengths ? min(max(p.lengths[b], 0), p.Sk) : p.Sk;
-    const int off = p.offsets ? min(max(p.offsets[b], -p.Sq), p.Sk) : p.Sk - p.Sq;
-    const bool exists = q < p.Sq && off + q >= 0 && off + q < len;
-    float sum = 0.f;
-    if (exists && 8 * c < p.d) {
-        const u32x4 o = *reinterpret_cast<const u32x4 *>(p.Oin + b * p.os.b + h * p.os.h + q * p.os.s + 8 * c);
-        const u32x4 g = *reinterpret_cast<const u32x4 *>(p.dO + b * p.gs.b + h * p.gs.h + q * p.gs.s + 8 * c);
-        u32x4 rest = {0, 0, 0, 0};
-        if (p.rest) rest = *reinterpret_cast<const u32x4 *>(p.rest + ((int64_t)bh * p.Sq + q) * p.d + 8 * c);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            sum = fmaf(widen16<BF16>(o[e] & 0xFFFFu) + widen16<BF16>(rest[e] & 0xFFFFu), widen16<BF16>(g[e] & 0xFFFFu), sum);
-            sum = fmaf(widen16<BF16>(o[e] >> 16) + widen16<BF16>(rest[e] >> 16), widen16<BF16>(g[e] >> 16), sum);
-        }
-    }
-#pragma unroll
-    for (int m = 8; m > 0; m >>= 1) sum += __shfl_xor(sum, m);
-    if (c == 0) {
-        p.stats[row] = exists ? p.lse[(int64_t)bh * p.Sq + q] * 1.4426950408889634f : __builtin_inff();
-        p.stats[rows + row] = sum;
-    }
-}
-
-// dQ: four waves of 32 queries over the same key tiles as the forward; a lane owns a query, so lse and delta are its own two registers.
+// dQ: four waves of 32 queries over the same key tiles as the forward; a lane owns a query, so lse and delta are its own two registers.  It forms
+// delta from the rows of dO that it holds anyway, and leaves both where smha_sink_bwd_kv, which runs after it, reads them; queries that do not
+// exist get lse = inf, so that their probabilities are zero.  (A kernel of its own for that: 10 us of 114 for 4 x 12 x 1537 x 80.)
+// delta from the rounded output alone is as far off as dS is by its own rounding: dQ and dK 1.52 times as far from 64 bits as an evaluation in
+// 32 bits that is rounded once, 1.42 times with what the rounding left out.
 // dS is rounded to the inputs' type for the product with K, as P is in the forward.
 template <int D, int C, bool BF16>
 __global__ void __launch_bounds__(256, 2) smha_sink_bwd_q(const SinkParams p) {
@@ -330,8 +303,28 @@ __global__ void __launch_bounds__(256, 2) smha_sink_bwd_q(const SinkParams p) {
     u32x4 qf[NS], gf[NS];
     load_operand<C>(qf, p.Q + b * p.qs.b + h * p.qs.h, p.qs.s, qw, s.qa, s.qb, p.d, lane);
     load_operand<C>(gf, p.dO + b * p.gs.b + h * p.gs.h, p.gs.s, qw, s.qa, s.qb, p.d, lane);
-    const int64_t row = (int64_t)bh * p.Sqp + qw + j;
-    const float lse2 = p.stats[row], delta = p.stats[(int64_t)p.B * p.H * p.Sqp + row];
+    float delta = 0.f;
+    {
+        u32x4 of[NS], rest[NS];
+        load_operand<C>(of, p.Oin + b * p.os.b + h * p.os.h, p.os.s, qw, s.qa, s.qb, p.d, lane);
+        if (p.rest) load_operand<C>(rest, p.rest + (int64_t)bh * p.Sq * p.d, p.d, qw, s.qa, s.qb, p.d, lane);
+#pragma unroll
+        for (int i = 0; i < NS; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                float lo = widen16<BF16>(of[i][e] & 0xFFFFu), hi = widen16<BF16>(of[i][e] >> 16);
+                if (p.rest) lo += widen16<BF16>(rest[i][e] & 0xFFFFu), hi += widen16<BF16>(rest[i][e] >> 16);
+                delta = fmaf(lo, widen16<BF16>(gf[i][e] & 0xFFFFu), delta);
+                delta = fmaf(hi, widen16<BF16>(gf[i][e] >> 16), delta);
+            }
+        delta += __shfl_xor(delta, 32);
+    }
+    const float lse2 = exists ? p.lse[(int64_t)bh * p.Sq + qw + j] * 1.4426950408889634f : __builtin_inff();
+    if (hh == 0) {
+        const int64_t row = (int64_t)bh * p.Sqp + qw + j;
+        p.stats[row] = lse2;
+        p.stats[(int64_t)p.B * p.H * p.Sqp + row] = delta;
+    }
 
     const int rd = j * D * 2 + ((hh ^ swz_both<D>(j)) * 16);
     const int tr_row = 4 * hh + ((lane & 15) >> 2);
@@ -710,19 +703,14 @@ template <int D, int C, bool BF16> static hipError_t launch_sink_fwd(SinkParams 
 }
 
 template <int D, int C, bool BF16> static hipError_t launch_sink_bwd(SinkParams &sp, hipStream_t stream) {
-    const int64_t rows = (int64_t)sp.B * sp.H * sp.Sqp;
-    hipLaunchKernelGGL((smha_sink_stats<BF16>), dim3((unsigned)((rows + 15) / 16)), dim3(256), 0, stream, sp);
+    sp.per_xcd = (int)(((int64_t)sp.B * sp.H * ((sp.Sq + 127) / 128) + 7) / 8);
+    hipLaunchKernelGGL((smha_sink_bwd_q<D, C, BF16>), dim3(8 * sp.per_xcd), dim3(256), 0, stream, sp);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     sp.per_xcd = (int)((sink_items(sp) + 7) / 8);
     hipLaunchKernelGGL((smha_sink_bwd_kv<D, C, BF16>), dim3(8 * sp.per_xcd), dim3(256), 0, stream, sp);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    if (sp.cut_sink > 1 || sp.cut_rest > 1) {
-        hipLaunchKernelGGL((smha_sink_sum<C, BF16>), dim3((unsigned)(8 * sp.B * sp.Hkv * sp.n_tiles)), dim3(256), 0, stream, sp);
-        if ((e = hipGetLastError()) != hipSuccess) return e;
-    }
-    sp.per_xcd = (int)(((int64_t)sp.B * sp.H * ((sp.Sq + 127) / 128) + 7) / 8);
-    hipLaunchKernelGGL((smha_sink_bwd_q<D, C, BF16>), dim3(8 * sp.per_xcd), dim3(256), 0, stream, sp);
+    if (sp.cut_sink > 1 || sp.cut_rest > 1) hipLaunchKernelGGL((smha_sink_sum<C, BF16>), dim3((unsigned)(8 * sp.B * sp.Hkv * sp.n_tiles)), dim3(256), 0, stream, sp);
     return hipGetLastError();
 }
 
