@@ -16,12 +16,12 @@ from .sink import _CODES, _check_int, _check_per_sequence, _check_qkv, _handle, 
 _attention = _evict = None  # functions of _smha_torch
 
 
-def _stream_to_allocate_on(stream, workspace):
-    """What makes torch allocate for the stream that a call runs on."""
-    if stream is None or workspace is not None:
+def _allocating_on(stream, given):
+    """What makes torch allocate for the stream that a call runs on; `given`: nothing has to be allocated."""
+    if stream is None or given:
         return contextlib.nullcontext()
     if not isinstance(stream, torch.cuda.Stream):
-        raise ValueError("a call on a bare stream handle needs a workspace and its outputs")
+        raise ValueError("a call on a bare stream handle needs its workspace and outputs")
     return torch.cuda.stream(stream)
 
 
@@ -86,7 +86,7 @@ def cache_attention(q, k, v, lengths, *, window: int = 0, n_sink: int = 0, prefi
             ws = (C.c_int64 * 2)(weights.stride(0), weights.stride(1))
     if out is not None and (out.shape != q.shape or out.dtype != q.dtype or out.device != q.device):
         raise ValueError("out must be like q")
-    with _on_device(q), _stream_to_allocate_on(stream, workspace):
+    with _on_device(q), _allocating_on(stream, workspace is not None and out is not None):
         if out is None:
             out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
         if workspace is None:
@@ -160,7 +160,7 @@ def cache_evict(k, v, weights, positions, lengths, budget: int, recent: int = 0,
         for t, like in zip(out, given):
             if t.dtype != like.dtype or t.shape != like.shape or t.device != k.device or not t.is_contiguous():
                 raise ValueError("out must be three tensors like weights, positions and lengths")
-    with _on_device(k), _stream_to_allocate_on(stream, workspace if out is not None else None):
+    with _on_device(k), _allocating_on(stream, workspace is not None and out is not None):
         if out is None:
             out = tuple(torch.empty_like(t) for t in given)
         if workspace is None:

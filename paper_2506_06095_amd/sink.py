@@ -103,7 +103,8 @@ def smha_sink_workspace(B: int, H: int, Hkv: int, Sq: int, Sk: int, d: int, wind
 def smha_sink_backward(Q, K, V, O, lse, dO, dQ, dK, dV, window: int = 0, n_sink: int = 0, offsets=None, lengths=None, scale: float = 0.0, workspace=None,
                        stream=None, O_rest=None) -> None:
     """dQ, dK, dV (like Q, K, V) from what smha_sink_forward took and gave and the gradient dO of O.  workspace: a uint8 tensor of
-    smha_sink_workspace bytes; by default one is allocated (on `stream`, if that is torch's current one or a torch stream)."""
+    smha_sink_workspace bytes; by default one is allocated.  (In binary16, dS is rounded to it like the gradients themselves: gradients of O have to be
+    scaled so that they and their products with V keep within its range.)"""
     _check_qkv(Q, K, V)
     B, H, Sq, d = Q.shape
     for t, like, name in ((O, Q, "O"), (dO, Q, "dO"), (dQ, Q, "dQ"), (dK, K, "dK"), (dV, V, "dV")):

@@ -182,6 +182,57 @@ def test_strides_streams_and_a_captured_call():
         assert torch.equal(out, eager) and torch.equal(weights, expect), lengths
 
 
+@pytest.mark.gpu
+def test_the_way_through_python_is_the_native_one(monkeypatch):
+    """The calls that the native path leaves to Python: the same bits."""
+    from paper_2506_06095_amd import cache
+    q, k, v, prefix = make(3, 8, 2, 2, 700, 64, layout="bshd", P=300)
+    n = int32([700, 1, 333])
+
+    def run():
+        w = torch.zeros(3, 2, 700, device="cuda")
+        kk, vv = k.clone(), v.clone()
+        pos = torch.arange(700, dtype=torch.int32, device="cuda").expand(3, 2, 700).contiguous()
+        out = smha.cache_attention(q, kk, vv, n, prefix=prefix, weights=w)
+        near = smha.cache_attention(q, kk, vv, n, window=50, n_sink=4)
+        return (out, near, *smha.cache_evict(kk, vv, w, pos, n, 200, 16), kk, vv)
+
+    native = run()
+    monkeypatch.setattr(cache, "_attention", lambda *args: None)
+    monkeypatch.setattr(cache, "_evict", lambda *args: None)
+    assert all(torch.equal(a, b) for a, b in zip(native, run()))
+
+
+@pytest.mark.gpu
+def test_a_cache_past_32_bits():
+    """Keys and values of more than 4 GiB in all, 1 GiB a head, and accounts to match: the last sequence's last head, whose every offset is past 2^31
+    elements, against the formula on the GPU in 64 bits."""
+    B, Hkv, Sk, d = 2, 2, 8 << 20, 64
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    k, v = (torch.empty(B, Hkv, Sk, d, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    k[1, 1].normal_(generator=gen)
+    v[1, 1].normal_(generator=gen)
+    q = torch.zeros(B, 4, 1, d, dtype=torch.bfloat16, device="cuda")
+    q[1, 2:] = torch.randn(2, 1, d, generator=gen, device="cuda").bfloat16()
+    weights = torch.zeros(B, Hkv, Sk, device="cuda")
+    lengths = [1, Sk - 3]
+    k[0, :, 0] = v[0, :, 0] = k[1, 0] = v[1, 0] = 0
+    out = smha.cache_attention(q, k, v, int32(lengths), weights=weights)
+    u, received = 2.0 ** -8, torch.zeros(Sk, dtype=torch.float64, device="cuda")
+    for h in (2, 3):
+        K, V = k[1, 1, :lengths[1]].double(), v[1, 1, :lengths[1]].double()
+        p = torch.softmax(K @ q[1, h, 0].double() / 8, 0)
+        want, bound = p @ V, (u + F) * (p @ V.abs())
+        assert bool(((out[1, h, 0].double() - want).abs() <= bound * (1 + u) + u * want.abs()).all())
+        received[:lengths[1]] += p
+        del K, V
+    # (the log-sum-exp of eight million terms, in 32 bits: each of the 4096 lanes' sums of some thousand is off by at most as many half steps)
+    assert bool(((weights[1, 1].double() - received).abs() <= (F + 4096 * 2.0 ** -24) * received).all())
+    w2, pos, n = smha.cache_evict(k, v, weights, torch.arange(Sk, dtype=torch.int32, device="cuda").expand(B, Hkv, Sk).contiguous(), int32(lengths), 1000, 0)
+    kept = torch.sort(weights[1, 1, :lengths[1]], descending=True, stable=True).indices[:1000].sort().values
+    assert n.tolist() == [1, 1000] and torch.equal(pos[1, 1, :1000].long().sort().values, kept) and torch.equal(w2[1, 1, :1000], weights[1, 1][pos[1, 1, :1000].long()])
+
+
 # --- eviction
 
 def plain_evict(k, v, w, pos, lengths, budget, recent):
@@ -200,7 +251,8 @@ def plain_evict(k, v, w, pos, lengths, budget, recent):
                     return (-x, j)
 
                 kept = sorted(sorted(range(n), key=rank)[:end])
-                to = [j for j in range(end) if j not in set(kept)]
+                stays = set(kept)
+                to = [j for j in range(end) if j not in stays]
                 at = [j for j in kept if j >= end]
                 for t in (k, v, w, pos):
                     t[b, h, to] = t[b, h, at]
@@ -234,6 +286,7 @@ EVICT = [
     (1, 2, 20000, 16, [20000], 17000, 20, "spread"),
     (1, 1, 40000, 8, [39999], 20000, 7, "ties"),             # more slots than a workgroup holds in registers
     (1, 2, 300, 64, [300], 1000, 3, "spread"),               # nothing to do
+    (3, 1, 130, 64, [500, -7, 130], 100, 10, "spread"),      # lengths outside the cache
 ]
 
 
@@ -246,6 +299,8 @@ def test_eviction_is_the_plain_selection(case, in_place):
     n = int32(lengths)
     want = [t.cpu().clone() for t in (k, v, w, pos)]
     want.append(plain_evict(*want, lengths, budget, recent))
+    if n.max() > Sk or n.min() < 0:
+        assert want[-1].tolist() == [min(max(x, 0), Sk, budget) for x in lengths]
     given = [t.clone() for t in (w, pos, n)]
     out = smha.cache_evict(k, v, w, pos, n, budget, recent, out=(w, pos, n) if in_place else None)
     if in_place:

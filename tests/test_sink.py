@@ -141,6 +141,57 @@ def test_forward_and_backward_are_the_formulas(case, dtype):
 
 
 @pytest.mark.gpu
+def test_the_way_through_python_is_the_native_one(monkeypatch):
+    """The calls that the native path leaves to Python: the same bits, gradients among them."""
+    from paper_2506_06095_amd import sink
+    q, k, v, g = tensors(2, 4, 2, 150, 150, 64, torch.bfloat16, "bshd")
+    n = int32([150, 70])
+
+    def run():
+        x = [t.detach().requires_grad_() for t in (q, k, v)]
+        out = smha.sink_attention(*x, 40, 3, lengths=n)
+        with torch.no_grad():
+            assert torch.equal(smha.sink_attention(*x, 40, 3, lengths=n), out)
+        return (out, *torch.autograd.grad(out, x, g))
+
+    native = run()
+    assert type(native[0].grad_fn).__name__ != "_SinkAttentionBackward"
+    monkeypatch.setattr(sink, "_call", lambda *args: None)
+    general = run()
+    assert type(general[0].grad_fn).__name__ == "_SinkAttentionBackward"
+    assert all(torch.equal(a, b) for a, b in zip(native, general))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("native", [True, False])
+def test_gradients_for_some_inputs_and_no_second_derivative(monkeypatch, native):
+    from paper_2506_06095_amd import sink
+    if not native:
+        monkeypatch.setattr(sink, "_call", lambda *args: None)
+    q, k, v, g = tensors(1, 2, 2, 64, 64, 64, torch.float16)
+    x = [t.detach().requires_grad_() for t in (q, k, v)]
+    want = torch.autograd.grad(smha.sink_attention(*x, 16, 1), x, g)
+    only_k = k.detach().requires_grad_()
+    (dk,) = torch.autograd.grad(smha.sink_attention(q, only_k, v, 16, 1), (only_k,), g)
+    assert torch.equal(dk, want[1])
+    dq, dk, dv = torch.autograd.grad(smha.sink_attention(*x, 16, 1), x, g, create_graph=True)
+    assert torch.equal(dq, want[0]) and torch.equal(dv, want[2])
+    with pytest.raises(RuntimeError, match="twice" if native else "does not require grad"):
+        dq.float().sum().backward()
+
+
+@pytest.mark.gpu
+def test_inputs_changed_before_the_backward_pass_are_noticed():
+    q, k, v, g = tensors(1, 2, 2, 64, 64, 64, torch.float16)
+    q.requires_grad_()
+    n = int32([50])
+    out = smha.sink_attention(q, k, v, 16, 1, lengths=n)
+    n += 1
+    with pytest.raises(RuntimeError, match="inplace"):
+        out.backward(g)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("d", [64, 128])
 def test_what_does_not_exist_may_hold_anything(d):
     """NaN and infinities in keys past the length, in keys that no query sees and in queries that do not exist change nothing."""
