@@ -58,6 +58,23 @@ __device__ __forceinline__ Sequence sequence(const SinkParams &p, int b) {
     return s;
 }
 
+// A workgroup's 128 queries.  An XCD takes a run of (key head, sequence, query head): the heads that share keys do it in one L2, and every
+// XCD has sequences of all lengths (by sequence first, 4 x 12 x 1537 x 80 with lengths of 60 to 100 %: XCDs with the longest ones had 78 workgroups in
+// 64 places).  A head's last queries, which have the longest lists, come first.
+struct QueryTile {
+    int b, hk, h, q0;
+    __device__ __forceinline__ explicit QueryTile(const SinkParams &p) {
+        const int nt = (p.Sq + 127) / 128, idx = (int)(blockIdx.x & 7) * p.per_xcd + (int)(blockIdx.x >> 3);
+        q0 = b = hk = h = -1;
+        if (idx >= p.B * p.H * nt) return;
+        const int run = idx / nt, group = run / p.G;
+        hk = group / p.B;
+        b = group - hk * p.B;
+        h = hk * p.G + run - group * p.G;
+        q0 = (nt - 1 - (idx - run * nt)) * 128;
+    }
+};
+
 // the keys k0 .. k0 + 63 that a query at position pos sees
 __device__ __forceinline__ uint64_t seen_keys(int pos, int k0, int window, int n_sink) {
     return low_bits(pos - k0 + 1) & (~low_bits(pos - window + 1 - k0) | low_bits(n_sink - k0));
@@ -127,10 +144,9 @@ __global__ void __launch_bounds__(256, D == 64 ? 4 : 2) smha_sink_fwd(const Sink
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = lane & 31, hh = lane >> 5;
     const float NEG_INF = -__builtin_inff();
 
-    // an XCD takes a run of heads, so that the heads that share keys do it in one L2; a head's last queries (the longest lists) first
-    const int nt = (p.Sq + 127) / 128, idx = (int)(blockIdx.x & 7) * p.per_xcd + (int)(blockIdx.x >> 3);
-    if (idx >= p.B * p.H * nt) return;
-    const int bh = idx / nt, q0 = (nt - 1 - (idx - bh * nt)) * 128, b = bh / p.H, h = bh - b * p.H, hk = h / p.G;
+    const QueryTile at(p);
+    if (at.q0 < 0) return;
+    const int q0 = at.q0, b = at.b, h = at.h, hk = at.hk, bh = b * p.H + h;
     const Sequence s = sequence(p, b);
     const int window = p.window, n_sink = p.n_sink;
 
@@ -273,9 +289,9 @@ __global__ void __launch_bounds__(256, 2) smha_sink_bwd_q(const SinkParams p) {
     const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_void *)smem;
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = lane & 31, hh = lane >> 5;
 
-    const int nt = (p.Sq + 127) / 128, idx = (int)(blockIdx.x & 7) * p.per_xcd + (int)(blockIdx.x >> 3);
-    if (idx >= p.B * p.H * nt) return;
-    const int bh = idx / nt, q0 = (nt - 1 - (idx - bh * nt)) * 128, b = bh / p.H, h = bh - b * p.H, hk = h / p.G;
+    const QueryTile at(p);
+    if (at.q0 < 0) return;
+    const int q0 = at.q0, b = at.b, h = at.h, hk = at.hk, bh = b * p.H + h;
     const Sequence s = sequence(p, b);
     const int window = p.window, n_sink = p.n_sink;
     const int first = s.off + max(q0, s.qa), last = s.off + min(q0 + 128, s.qb) - 1;
@@ -445,7 +461,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) smha_sink_bwd_kv(const S
     const int per = p.n_sink_tiles * p.cut_sink + (p.n_tiles - p.n_sink_tiles) * p.cut_rest;  // items of a key head
     const int idx = (int)(blockIdx.x & 7) * p.per_xcd + (int)(blockIdx.x >> 3);
     if (idx >= p.B * p.Hkv * per) return;
-    const int bh = idx / per, item = idx - bh * per, b = bh / p.Hkv, hk = bh - b * p.Hkv;
+    const int group = idx / per, item = idx - group * per, hk = group / p.B, b = group - hk * p.B;  // (see QueryTile)
     int tile, part, cut;
     if (item < p.n_sink_tiles * p.cut_sink) {
         cut = p.cut_sink;
@@ -628,7 +644,7 @@ __global__ void __launch_bounds__(256) smha_sink_sum(const SinkParams p) {
     uint16_t *const out = is_k ? p.dK + b * p.dks.b + hk * p.dks.h : p.dV + b * p.dvs.b + hk * p.dvs.h;
     const int64_t pitch = is_k ? p.dks.s : p.dvs.s;
     const float factor = is_k ? p.scale : 1.f;
-    const float *const from = p.parts + (((int64_t)bh * per + item) * 8 + is_k * 4 + w) * (C / 8) * 256;
+    const float *const from = p.parts + (((int64_t)(hk * p.B + b) * per + item) * 8 + is_k * 4 + w) * (C / 8) * 256;
     for (int i = threadIdx.x; i < C / 8 * 64; i += 256) {
         f32x4 sum = {0.f, 0.f, 0.f, 0.f};
         for (int c = 0; c < parts; ++c) sum += *reinterpret_cast<const f32x4 *>(from + (int64_t)c * 8 * (C / 8) * 256 + i * 4);
