@@ -389,6 +389,7 @@ __global__ void __launch_bounds__(256, 2) smha_sink_bwd_q(const SinkParams p) {
                     sc = __builtin_bit_cast(f32x16, (raw & keep) | (~keep & 0xFF800000u));
                 }
                 __builtin_amdgcn_sched_barrier(0);
+                __builtin_amdgcn_s_setprio(1);
                 // dP, and P from the scores
 #pragma unroll
                 for (int i = 0; i < NS; ++i) {
@@ -419,6 +420,7 @@ __global__ void __launch_bounds__(256, 2) smha_sink_bwd_q(const SinkParams p) {
                     }
                     __builtin_amdgcn_sched_barrier(0);
                 }
+                __builtin_amdgcn_s_setprio(0);
             }
         }
         tiles_landed();
@@ -570,6 +572,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) smha_sink_bwd_kv(const S
                 sc = __builtin_bit_cast(f32x16, (raw & keep) | (~keep & 0xFF800000u));
             }
             __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_setprio(1);
             // dP, and P from the scores
             u32x4 pf[2];
 #pragma unroll
@@ -611,6 +614,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) smha_sink_bwd_kv(const S
                 next(2 * NS + 2 * NDT + i);
                 __builtin_amdgcn_sched_barrier(0);
             }
+            __builtin_amdgcn_s_setprio(0);
         }
         tiles_landed();
     }
