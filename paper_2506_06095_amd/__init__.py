@@ -1,7 +1,9 @@
 """smha: masked multi-head attention for MI355X (gfx950) behind a C ABI.
 
+Beside plans: attention with a window and sinks (`sink`), on a cache, and eviction from it (`cache`).
+
 The compute lives in libsmha.so (HIP); this package is the thin ctypes binding
-(`binding`) and the in-tree build step (`build`).  There is no CPU fallback: if
+(`binding`, `sink`, `cache`) and the in-tree build step (`build`).  There is no CPU fallback: if
 the library is missing or no GPU is usable, calls raise.
 """
 from .binding import (  # noqa: F401
