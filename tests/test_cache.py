@@ -76,6 +76,7 @@ CASES = [
     (2, 6, 2, 3, 333, 80, 50, 7, 0, [333, 2], "bhsd"),                  # fewer keys than tokens
     (2, 16, 2, 5, 700, 128, 100, 40, 0, [699, 130], "bshd"),            # 40 rows on a key head
     (2, 16, 1, 4, 97, 32, 0, 0, 0, [97, 33], "bhsd"),                   # 64 rows
+    (1, 16, 2, 40, 120, 64, 60, 3, 0, [119], "bhsd"),                   # 320 rows
     (1, 4, 1, 1, 20000, 128, 0, 0, 0, [19999], "bhsd"),                 # many segments
     (2, 4, 2, 1, 9000, 64, 4096, 130, 0, [9000, 8999], "bhsd"),
     (70, 2, 1, 1, 64, 8, 0, 0, 0, [(7 * i) % 65 for i in range(70)], "bhsd"),   # more sequences than lanes

@@ -355,3 +355,5 @@ def test_refusals_of_the_binding_on_the_gpu():
     with pytest.raises(smha.SmhaError):
         wide = torch.zeros(1, 4, 8, 136, dtype=torch.float16, device="cuda")
         smha.sink_attention(wide, wide, wide, 4)
+    with pytest.raises(smha.SmhaError):
+        smha.sink_attention(wide.requires_grad_(), wide, wide, 4)
