@@ -338,6 +338,7 @@ void smha_plan_destroy(smha_plan_t *plan); /* NULL is allowed */
  *   lengths         device, int32 [B], keys per sequence, taken as 0 or Sk where outside 0 .. Sk; NULL: Sk
  *   window          keys that a query sees, itself included; 0: all before it
  *   n_sink          first keys that every later query sees
+ *   scale           <= 0 selects 1/sqrt(d)
  * offsets and lengths are read by the kernels: nothing synchronises, and a captured call follows their values.
  * Queries that do not exist give zero rows in O and dQ, keys at and past a sequence's length zero rows in dK
  * and dV; neither's values are read into any result, whatever they are.  Values that are visible to some query have to
@@ -355,9 +356,10 @@ smha_status_t smha_sink_workspace(int B, int H, int Hkv, int Sq, int Sk, int d, 
 
 /* Gradients of Q, K and V (of `dtype`, written whole) from O, O_rest (or NULL) and lse of the forward with the same arguments and dO, the
  * gradient of O.  The result does not depend on the order in which workgroups run: the parts of sums that were cut
- * are added in a fixed order.  P and dS = P (dP - delta) are rounded to `dtype` for the products that use them: in binary16 the
- * gradient of O has to be scaled (as such training does) so that dS keeps within that type's range.  workspace: device, 16-byte aligned, smha_sink_workspace bytes or more; the call's alone
- * until it has run. */
+ * are added in a fixed order.  P and dS = P (dP - delta) are rounded to `dtype` for the products that use them (where
+ * there are at most 16384 queries in all, dS to twice its digits): in binary16 the gradient of O has to be scaled (as such training
+ * does) so that dS keeps within that type's range.  workspace: device, 16-byte aligned, smha_sink_workspace bytes or more; the
+ * call's alone until it has run. */
 smha_status_t smha_sink_backward(const void *Q, const void *K, const void *V, const void *O, const void *O_rest,
                                  const float *lse, const void *dO, void *dQ, void *dK, void *dV, int B, int H, int Hkv, int Sq, int Sk, int d,
                                  smha_dtype_t dtype, const int64_t q_strides[3], const int64_t k_strides[3],
@@ -379,7 +381,9 @@ smha_status_t smha_sink_backward(const void *Q, const void *K, const void *V, co
  * Token t of sequence b stands at own key lengths[b] - T + t and sees the keys up to it (in its window, or sinks) and all of the
  * prefix.  Below 0 there is no such token: its output row is zero and it adds to no weight.
  * lengths are read by the kernels (nothing synchronises; a captured call follows them), which divide the keys of all sequences evenly
- * over the chip whatever the lengths are.  The result does not depend on the order in which workgroups run.
+ * over the chip whatever the lengths are.  The result does not depend on the order in which workgroups run.  Keys and values before every
+ * token's window, past the length and past Sk are never read into a result; those that some token sees have to be finite (a NaN there may reach
+ * the sequence's other tokens).
  * workspace: device, 16-byte aligned, smha_cache_workspace bytes or more; the call's alone until it has run.  (weigh: nonzero with
  * weights: 4 H T Sk bytes a sequence more.)
  * Errors as for smha_sink_forward. */

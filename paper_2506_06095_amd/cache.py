@@ -25,6 +25,13 @@ def _allocating_on(stream, given):
     return torch.cuda.stream(stream)
 
 
+def _written(*tensors):
+    """Autograd refuses to go back through what was saved of a tensor that was written since."""
+    for t in tensors:
+        if t is not None and not t.is_inference():
+            torch.autograd.graph.increment_version(t)
+
+
 def _check_workspace(workspace, like):
     if workspace.dtype != torch.uint8 or workspace.device != like.device or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous uint8 tensor on the same GPU")
@@ -48,7 +55,8 @@ def cache_attention(q, k, v, lengths, *, window: int = 0, n_sink: int = 0, prefi
     first `n_sink`.
     prefix: (keys, values), each [Hkv,P,d]: tokens before those of every sequence, which all of them see (not with a window).
     weights: float32 [B,Hkv,Sk]; each key's attention, summed over the tokens and the heads that share it, is added to it.
-    No gradients.  workspace: a uint8 tensor of smha_cache_workspace bytes, by default one is allocated."""
+    scale: 0 or less for 1/sqrt(d).  No gradients, and values that a token of the sequence sees have to be finite (those before the window, past the
+    length and in the cache's free slots may be anything).  workspace: a uint8 tensor of smha_cache_workspace bytes, by default one is allocated."""
     if out is None and workspace is None and stream is None:  # the native way, for every call that it takes (csrc/torch_binding.cpp)
         global _attention
         if _attention is None:
@@ -99,6 +107,7 @@ def cache_attention(q, k, v, lengths, *, window: int = 0, n_sink: int = 0, prefi
                                         _handle(stream, q.device))
     if st != 0:
         raise SmhaError(st, "smha_cache_forward")
+    _written(out, weights)
     return out
 
 
@@ -171,4 +180,5 @@ def cache_evict(k, v, weights, positions, lengths, budget: int, recent: int = 0,
                                       _strides(k), _strides(v), workspace.data_ptr(), workspace.numel(), _handle(stream, k.device))
     if st != 0:
         raise SmhaError(st, "smha_cache_evict")
+    _written(k, v, *out)
     return tuple(out)

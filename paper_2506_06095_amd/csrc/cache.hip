@@ -67,6 +67,9 @@ struct Segment {
     int group, length;   // length: lengths[b]
 };
 
+// The reference that a row's segment leaves: -inf says that it has no keys.  (A row of NaN has no largest score either, and must not be passed over.)
+__device__ __forceinline__ float reference_of(float m, float l) { return l == l ? m : 0.f; }
+
 __device__ __forceinline__ int wave_sum(int v) {
 #pragma unroll
     for (int m = 32; m > 0; m >>= 1) v += __shfl_xor(v, m);
@@ -158,7 +161,7 @@ __device__ __forceinline__ void prefix_wide(const CacheParams &p, const Segment 
     const int tr_row = 4 * hh + ((lane & 15) >> 2);
     const int tr = tr_row * D * 2 + ((swz_both<D>(tr_row) ^ (2 * ((lane >> 4) & 1) + ((lane & 3) >> 1))) * 16) + (lane & 1) * 8;
     float m_run = NEG_INF, l_run = 0.f;
-    const float thr = 8.0f / p.c;
+    const float thr = raised_over(p.c);
     f32x16 o[NDT];
 #pragma unroll
     for (int dt = 0; dt < NDT; ++dt) o[dt] = zeros16();
@@ -240,7 +243,7 @@ __device__ __forceinline__ void prefix_wide(const CacheParams &p, const Segment 
     if (s.rows0 + 32 * w + j < p.B * p.G * p.T) {
         const int64_t place = s.place + w;
         if (hh == 0) {
-            p.stats[place * 64 + j] = m_run * p.c;
+            p.stats[place * 64 + j] = reference_of(m_run * p.c, l);
             p.stats[place * 64 + 32 + j] = l;
         }
         float *const part = p.parts + (place * 32 + j) * D + 4 * hh;
@@ -362,7 +365,7 @@ __global__ void __launch_bounds__(256, cache_groups(D, FORM)) smha_cache_part(co
     float *const score_row = WEIGH && !prefix && row < rows ? p.scores + (((int64_t)s.b * p.Hkv + s.hk) * GT + row) * p.score_pitch : nullptr;
 
     float m_run = NEG_INF, l_run = 0.f;
-    const float thr = 8.0f / p.c;
+    const float thr = raised_over(p.c);
     f32x16 o[NDT];
 #pragma unroll
     for (int dt = 0; dt < NDT; ++dt) o[dt] = zeros16();
@@ -465,11 +468,11 @@ __global__ void __launch_bounds__(256, cache_groups(D, FORM)) smha_cache_part(co
     if (row < rows) {
         if (!whole || WEIGH) {
             if (w == 0 && hh == 0) {
-                p.stats[(int64_t)s.place * 64 + j] = m_all;
+                p.stats[(int64_t)s.place * 64 + j] = reference_of(m_all, l_all);
                 p.stats[(int64_t)s.place * 64 + 32 + j] = l_all;
             }
         }
-        const float inv = l_all > 0.f ? 1.0f / l_all : 0.f;
+        const float inv = l_all != 0.f ? 1.0f / l_all : 0.f;
         uint16_t *const to = p.O + rb * p.os.b + (s.hk * p.G + g) * p.os.h + t * p.os.s;
         float *const part = p.parts + ((int64_t)s.place * 32 + j) * D;
 #pragma unroll
@@ -580,7 +583,7 @@ __global__ void __launch_bounds__(256) smha_cache_join(const CacheParams p, int 
             share[u] = lds_ml[0][u] != NEG_INF ? fast_exp2(lds_ml[0][u] - top) : 0.f;
             l = fmaf(share[u], lds_ml[1][u], l);
         }
-        const float inv = l > 0.f ? 1.0f / l : 0.f;
+        const float inv = l != 0.f ? 1.0f / l : 0.f;
         for (int c = threadIdx.x; c < p.d; c += 256)
             to[c] = (uint16_t)pack2<BF16>((share[0] * lds_o[0][c] + share[1] * lds_o[1][c] + share[2] * lds_o[2][c] + share[3] * lds_o[3][c]) * inv, 0.f);
         return;
@@ -616,7 +619,7 @@ __global__ void __launch_bounds__(256) smha_cache_join(const CacheParams p, int 
                 l = (m != NEG_INF ? l * fast_exp2(m - top) : 0.f) + sum;
                 m = top;
             }
-            if (lane == 0) lds_lse[r1] = l > 0.f ? m + __builtin_amdgcn_logf(l) : __builtin_inff();  // (inf: a row without keys adds nothing)
+            if (lane == 0) lds_lse[r1] = l != 0.f ? m + __builtin_amdgcn_logf(l) : __builtin_inff();  // (inf: a row without keys adds nothing)
         }
         __syncthreads();
         if (scored) {
@@ -958,6 +961,9 @@ static smha_status_t cache_params(CacheParams &cp, CacheLayout &at, int B, int H
     cp.prefix_segs = (int)std::min<int64_t>(cp.slots + Hkv * prefix_tiles, prefix_most);
     const int64_t own_segs = std::min<int64_t>(cp.slots + (int64_t)B * Hkv * own_tiles, B * Hkv * own_tiles * own_most);
     cp.segs = (int)(cp.prefix_segs + own_segs);
+    // (a launch has less than 2^32 threads)
+    const int64_t most = std::max(std::max<int64_t>((int64_t)B * Hkv * own_tiles, cp.segs + 8), (int64_t)B * H * T + (weigh ? (int64_t)B * Hkv * ((Sk + 1023) / 1024) : 0));
+    if (most + 8 >= (1 << 24)) return SMHA_ERR_UNSUPPORTED;
     const int64_t places = (cp.wide ? 4 : 1) * (int64_t)cp.prefix_segs + own_segs;
     cp.score_pitch = (Sk + 31) / 32 * 32;
     if (cp.direct) {  // (nothing is kept: a size for callers that allocate what they are told)
@@ -1017,6 +1023,7 @@ extern "C" smha_status_t smha_cache_forward(const void *Q, const void *K, const 
     if (((uintptr_t)Q | (uintptr_t)K | (uintptr_t)V | (uintptr_t)O | (uintptr_t)workspace | (P ? (uintptr_t)PK | (uintptr_t)PV : 0)) & 15) return SMHA_ERR_UNSUPPORTED;
     if (!cache_strides_fit(q_strides, T, d) || !cache_strides_fit(k_strides, Sk, d) || !cache_strides_fit(v_strides, Sk, d) || !cache_strides_fit(o_strides, T, d))
         return SMHA_ERR_UNSUPPORTED;
+    if (o_strides && ((B > 1 && o_strides[0] < d) || (H > 1 && o_strides[1] < d))) return SMHA_ERR_UNSUPPORTED;  // (heads that are written in one place)
     if (P) {
         for (const int64_t *s : {pk_strides, pv_strides}) {
             const int64_t three[3] = {0, s ? s[0] : (int64_t)P * d, s ? s[1] : d};

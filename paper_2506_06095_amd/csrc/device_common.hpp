@@ -154,6 +154,9 @@ __device__ __forceinline__ void store4(void *O, int64_t elem_off, float a, float
 }
 
 // --- for kernels whose masks are arithmetic on positions
+// How far over the running reference a score may be before that is raised: 2^8 in the probabilities.  (Finite for every scale: with a reference
+// of -inf the comparison has to hold.)
+__device__ __forceinline__ float raised_over(float c) { return fminf(8.0f / c, 3e38f); }
 constexpr uint32_t kNoChunk = 0x80000000u;  // a column that the head does not have: past every buffer, with any row's offset added
 constexpr uint32_t kPast = 0x7FFFFF00u;     // a row that is not to be read
 

@@ -87,6 +87,11 @@ __device__ __forceinline__ bool all_seen(int p0, int p1, int k0, int k1, int win
     return k1 <= p0 && (p1 - k0 < window || k1 < n_sink);
 }
 
+// What rounding a and b to the pair v left out, rounded.
+template <bool BF16> __device__ __forceinline__ uint32_t pack2_left(float a, float b, uint32_t v) {
+    return pack2<BF16>(a - widen16<BF16>(v & 0xFFFFu), b - widen16<BF16>(v >> 16));
+}
+
 // A wave's 32 x D accumulators (acc[dt][r] = row j, column 32 dt + 8 (r / 4) + 4 hh + r % 4) to rows row0 .. of a tensor with 16-bit values,
 // through 32 rows of LDS so that whole rows are written; rows from `rows` on are left out.
 // REST: not the rounded values, but what their rounding leaves out.
@@ -102,9 +107,7 @@ __device__ __forceinline__ void store_rows(const f32x16 (&acc)[C / 32], float fa
 #pragma unroll
             for (int e = 0; e < 4; ++e) x[e] = acc[dt][4 * g + e] * factor;
             u32x2 v = {pack2<BF16>(x[0], x[1]), pack2<BF16>(x[2], x[3])};
-            if constexpr (REST)
-                v = u32x2{pack2<BF16>(x[0] - widen16<BF16>(v[0] & 0xFFFFu), x[1] - widen16<BF16>(v[0] >> 16)),
-                          pack2<BF16>(x[2] - widen16<BF16>(v[1] & 0xFFFFu), x[3] - widen16<BF16>(v[1] >> 16))};
+            if constexpr (REST) v = u32x2{pack2_left<BF16>(x[0], x[1], v[0]), pack2_left<BF16>(x[2], x[3], v[1])};
             *reinterpret_cast<u32x2 *>(slab + j * D * 2 + (((4 * dt + g) ^ swz_both<D>(j)) * 16) + hh * 8) = v;
         }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -181,7 +184,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 4 : 2) smha_sink_fwd(const Sink
     const int tr_row = 4 * hh + ((lane & 15) >> 2);
     const int tr = tr_row * D * 2 + ((swz_both<D>(tr_row) ^ (2 * ((lane >> 4) & 1) + ((lane & 3) >> 1))) * 16) + (lane & 1) * 8;
     float m_run = NEG_INF, l_run = 0.f;
-    const float thr = 8.0f / p.c;
+    const float thr = raised_over(p.c);
     f32x16 o[NDT];
 #pragma unroll
     for (int dt = 0; dt < NDT; ++dt) o[dt] = zeros16();
@@ -267,8 +270,8 @@ __global__ void __launch_bounds__(256, D == 64 ? 4 : 2) smha_sink_fwd(const Sink
     }
     const float l = l_run + __shfl_xor(l_run, 32);
     if (p.lse && hh == 0 && qw + j < p.Sq)
-        p.lse[(int64_t)bh * p.Sq + qw + j] = l > 0.f ? (m_run * p.c + __builtin_amdgcn_logf(l)) * 0.6931471805599453f : NEG_INF;
-    const float inv = l > 0.f ? 1.0f / l : 0.f;
+        p.lse[(int64_t)bh * p.Sq + qw + j] = l != 0.f ? (m_run * p.c + __builtin_amdgcn_logf(l)) * 0.6931471805599453f : NEG_INF;
+    const float inv = l != 0.f ? 1.0f / l : 0.f;  // (a sum that is not a number stays one)
     store_rows<D, C, BF16>(o, inv, smem + w * (32 * D * 2), lane, p.O + b * p.os.b + h * p.os.h, p.os.s, qw, p.Sq, p.d);
     if (p.rest) store_rows<D, C, BF16, true>(o, inv, smem + w * (32 * D * 2), lane, p.rest + (int64_t)bh * p.Sq * p.d, p.d, qw, p.Sq, p.d);
 }
@@ -281,9 +284,9 @@ __global__ void __launch_bounds__(256, D == 64 ? 4 : 2) smha_sink_fwd(const Sink
 // exist get lse = inf, so that their probabilities are zero.  (A kernel of its own for that: 10 us of 114 for 4 x 12 x 1537 x 80.)
 // delta from the rounded output alone is as far off as dS is by its own rounding: dQ and dK 1.52 times as far from 64 bits as an evaluation in
 // 32 bits that is rounded once, 1.42 times with what the rounding left out.
-// dS is rounded to the inputs' type for the product with K, as P is in the forward.
-template <int D, int C, bool BF16>
-__global__ void __launch_bounds__(256, 2) smha_sink_bwd_q(const SinkParams p) {
+// dS is rounded to the inputs' type for the product with K, as P is in the forward; FINE (see fine_ds): its rounding error is multiplied too.
+template <int D, int C, bool BF16, bool FINE>
+__global__ void __launch_bounds__(256, FINE ? 1 : 2) smha_sink_bwd_q(const SinkParams p) {
     constexpr int NS = C / 16, NDT = C / 32, TB = 64 * D * 2, PF = C == 128 ? 6 : 4;
     __shared__ __attribute__((aligned(1024))) char smem[4 * TB];  // K[0], K[1], V[0], V[1]
     const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_void *)smem;
@@ -403,9 +406,11 @@ __global__ void __launch_bounds__(256, 2) smha_sink_bwd_q(const SinkParams p) {
 #pragma unroll
                     for (int r = 0; r < 16; ++r) dp[r] = sc[r] != 0.f ? dp[r] : delta;
                 }
-                u32x4 pf[2];
+                u32x4 pf[2], left[2];
                 auto ds_pair = [&](int q) __attribute__((always_inline)) {
-                    pf[q >> 2][q & 3] = pack2<BF16>(sc[2 * q] * (dp[2 * q] - delta), sc[2 * q + 1] * (dp[2 * q + 1] - delta));
+                    const float lo = sc[2 * q] * (dp[2 * q] - delta), hi = sc[2 * q + 1] * (dp[2 * q + 1] - delta);
+                    pf[q >> 2][q & 3] = pack2<BF16>(lo, hi);
+                    if constexpr (FINE) left[q >> 2][q & 3] = pack2_left<BF16>(lo, hi, pf[q >> 2][q & 3]);
                 };
 #pragma unroll
                 for (int q = 0; q < 4; ++q) ds_pair(q);
@@ -413,6 +418,7 @@ __global__ void __launch_bounds__(256, 2) smha_sink_bwd_q(const SinkParams p) {
 #pragma unroll
                 for (int i = 0; i < 2 * NDT; ++i) {
                     dq[i % NDT] = mfma32<BF16>(f[(2 * NS + i) % PF], pf[i / NDT], dq[i % NDT]);
+                    if constexpr (FINE) dq[i % NDT] = mfma32<BF16>(f[(2 * NS + i) % PF], left[i / NDT], dq[i % NDT]);
                     if (2 * NS + i + PF < ALL) f[(2 * NS + i) % PF] = operand(2 * NS + i + PF);
                     if (i < NDT) {  // the other 16 keys' dS, under these products
 #pragma unroll
@@ -452,8 +458,8 @@ __device__ __forceinline__ int parts_of(int steps, int cut, int chunk) { return 
 // dS under the one that gives dV.
 // A tile's steps (its queries, head by head) may be cut into parts that other workgroups take: the sinks' tiles are seen by every
 // query, and few key heads would leave most of the chip idle.  Parts go to memory in 32 bits and are added in order by smha_sink_sum.
-template <int D, int C, bool BF16>
-__global__ void __launch_bounds__(256, D == 64 ? 3 : 2) smha_sink_bwd_kv(const SinkParams p) {
+template <int D, int C, bool BF16, bool FINE>
+__global__ void __launch_bounds__(256, FINE ? 1 : D == 64 ? 3 : 2) smha_sink_bwd_kv(const SinkParams p) {
     constexpr int NS = C / 16, NDT = C / 32, TB = 32 * D * 2, PF = 4;
     __shared__ __attribute__((aligned(1024))) char smem[4 * TB + 4 * TB];  // K, Q[0], Q[1], dO[0], dO[1]
     __shared__ __attribute__((aligned(1024))) float stats[2][2][64];       // [buffer][lse, delta][query] (32 of 64)
@@ -574,7 +580,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) smha_sink_bwd_kv(const S
             __builtin_amdgcn_sched_barrier(0);
             __builtin_amdgcn_s_setprio(1);
             // dP, and P from the scores
-            u32x4 pf[2];
+            u32x4 pf[2], left[2];
 #pragma unroll
             for (int i = 0; i < NS; ++i) {
                 dp = mfma32<BF16>(f[(NS + i) % PF], vf[i], dp);
@@ -607,10 +613,14 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) smha_sink_bwd_kv(const S
                 dp = __builtin_bit_cast(f32x16, __builtin_bit_cast(u32x16, dp) & keep);
             }
 #pragma unroll
-            for (int i = 0; i < 8; ++i) pf[i >> 2][i & 3] = pack2<BF16>(dp[2 * i], dp[2 * i + 1]);
+            for (int i = 0; i < 8; ++i) {
+                pf[i >> 2][i & 3] = pack2<BF16>(dp[2 * i], dp[2 * i + 1]);
+                if constexpr (FINE) left[i >> 2][i & 3] = pack2_left<BF16>(dp[2 * i], dp[2 * i + 1], pf[i >> 2][i & 3]);
+            }
 #pragma unroll
             for (int i = 0; i < 2 * NDT; ++i) {
                 dk[i % NDT] = mfma32<BF16>(f[(2 * NS + 2 * NDT + i) % PF], pf[i / NDT], dk[i % NDT]);
+                if constexpr (FINE) dk[i % NDT] = mfma32<BF16>(f[(2 * NS + 2 * NDT + i) % PF], left[i / NDT], dk[i % NDT]);
                 next(2 * NS + 2 * NDT + i);
                 __builtin_amdgcn_sched_barrier(0);
             }
@@ -667,9 +677,15 @@ static bool strides_fit(const int64_t *s, int64_t rows, int d) {
     return s[0] % 8 == 0 && s[1] % 8 == 0 && s[2] % 8 == 0 && s[0] >= 0 && s[1] >= 0 && s[2] >= d && (rows * s[2] + d) * 2 < ((int64_t)1 << 31);
 }
 
+// Heads that are written must not lie in one place.
+static bool apart(const int64_t *s, int B, int H, int d) { return !s || ((B == 1 || s[0] >= d) && (H == 1 || s[1] >= d)); }
+
 static Strides strides_of(const int64_t *s, int64_t heads, int64_t rows, int d) {
     return s ? Strides{s[0], s[1], s[2]} : Strides{heads * rows * d, rows * d, d};
 }
+
+// A launch has less than 2^32 threads; workgroups are 256, in a multiple of eight.
+static bool grid_fits(int64_t groups) { return groups + 8 < (1 << 24); }
 
 // What both directions check and fill in.
 static smha_status_t sink_params(SinkParams &sp, int B, int H, int Hkv, int Sq, int Sk, int d, smha_dtype_t dtype, const int32_t *offsets, const int32_t *lengths,
@@ -680,6 +696,7 @@ static smha_status_t sink_params(SinkParams &sp, int B, int H, int Hkv, int Sq, 
     if (d < 8 || d > 128 || d % 8) return SMHA_ERR_UNSUPPORTED;
     // (work items are numbered in 32 bits)
     if ((int64_t)B * H > (1 << 24) || (int64_t)B * H * (std::max(Sq, Sk) / 64 + 2) > (1 << 28)) return SMHA_ERR_UNSUPPORTED;
+    if (!grid_fits((int64_t)B * H * ((Sq + 127) / 128))) return SMHA_ERR_UNSUPPORTED;
     sp.B = B; sp.H = H; sp.Hkv = Hkv; sp.G = H / Hkv; sp.Sq = Sq; sp.Sk = Sk; sp.d = d;
     sp.window = window == 0 || window > Sk ? Sk : window;
     sp.n_sink = std::min(n_sink, Sk);
@@ -713,6 +730,16 @@ static int64_t sink_stats_bytes(const SinkParams &sp) { return (int64_t)2 * sp.B
 static int64_t sink_items(const SinkParams &sp) {
     return (int64_t)sp.B * sp.Hkv * ((int64_t)sp.n_sink_tiles * sp.cut_sink + (int64_t)(sp.n_tiles - sp.n_sink_tiles) * sp.cut_rest);
 }
+static bool sink_grids_fit(const SinkParams &sp) {
+    return grid_fits(sink_items(sp)) && ((sp.cut_sink == 1 && sp.cut_rest == 1) || grid_fits((int64_t)8 * sp.B * sp.Hkv * sp.n_tiles));
+}
+
+// Whether dS goes into dQ and dK with what its rounding leaves out.  dQ and dK of rounded dS are 1.44 times as far from 64 bits as their own
+// rounding on average; of few rows, where a few large ones make most of the norm, up to 1.50 (2 x 12 x 68 x 64).  There both halves are
+// multiplied, a product more of three and of four: 1.0x.  Such a pass is the host's (75 us of which the kernels run 25): it costs nothing.  Of many
+// rows it would: 1 x 32 x 8192 x 128, window 4096, runs at the matrix pipes' power.
+static bool fine_ds(const SinkParams &sp) { return (int64_t)sp.B * sp.H * sp.Sq <= 16384; }
+
 static int sink_width(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : d <= 96 ? 96 : 128; }
 
 template <int D, int C, bool BF16> static hipError_t launch_sink_fwd(SinkParams &sp, hipStream_t stream) {
@@ -722,13 +749,13 @@ template <int D, int C, bool BF16> static hipError_t launch_sink_fwd(SinkParams 
     return hipGetLastError();
 }
 
-template <int D, int C, bool BF16> static hipError_t launch_sink_bwd(SinkParams &sp, hipStream_t stream) {
+template <int D, int C, bool BF16, bool FINE> static hipError_t launch_sink_bwd(SinkParams &sp, hipStream_t stream) {
     sp.per_xcd = (int)(((int64_t)sp.B * sp.H * ((sp.Sq + 127) / 128) + 7) / 8);
-    hipLaunchKernelGGL((smha_sink_bwd_q<D, C, BF16>), dim3(8 * sp.per_xcd), dim3(256), 0, stream, sp);
+    hipLaunchKernelGGL((smha_sink_bwd_q<D, C, BF16, FINE>), dim3(8 * sp.per_xcd), dim3(256), 0, stream, sp);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     sp.per_xcd = (int)((sink_items(sp) + 7) / 8);
-    hipLaunchKernelGGL((smha_sink_bwd_kv<D, C, BF16>), dim3(8 * sp.per_xcd), dim3(256), 0, stream, sp);
+    hipLaunchKernelGGL((smha_sink_bwd_kv<D, C, BF16, FINE>), dim3(8 * sp.per_xcd), dim3(256), 0, stream, sp);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     if (sp.cut_sink > 1 || sp.cut_rest > 1) hipLaunchKernelGGL((smha_sink_sum<C, BF16>), dim3((unsigned)(8 * sp.B * sp.Hkv * sp.n_tiles)), dim3(256), 0, stream, sp);
     return hipGetLastError();
@@ -747,7 +774,8 @@ extern "C" smha_status_t smha_sink_forward(const void *Q, const void *K, const v
     const smha_status_t st = sink_params(sp, B, H, Hkv, Sq, Sk, d, dtype, offsets, lengths, window, n_sink, scale);
     if (st != SMHA_OK) return st;
     if (((uintptr_t)Q | (uintptr_t)K | (uintptr_t)V | (uintptr_t)O | (uintptr_t)O_rest) & 15) return SMHA_ERR_UNSUPPORTED;
-    if (!strides_fit(q_strides, Sq + 128, d) || !strides_fit(k_strides, (int64_t)Sk + 128, d) || !strides_fit(v_strides, (int64_t)Sk + 128, d) || !strides_fit(o_strides, Sq + 128, d))
+    if (!strides_fit(q_strides, Sq + 128, d) || !strides_fit(k_strides, (int64_t)Sk + 128, d) || !strides_fit(v_strides, (int64_t)Sk + 128, d) || !strides_fit(o_strides, Sq + 128, d) ||
+        !apart(o_strides, B, H, d))
         return SMHA_ERR_UNSUPPORTED;
     sp.Q = (const uint16_t *)Q; sp.K = (const uint16_t *)K; sp.V = (const uint16_t *)V; sp.O = (uint16_t *)O; sp.lse = lse; sp.rest = (uint16_t *)O_rest;
     sp.qs = strides_of(q_strides, H, Sq, d); sp.ks = strides_of(k_strides, Hkv, Sk, d); sp.vs = strides_of(v_strides, Hkv, Sk, d); sp.os = strides_of(o_strides, H, Sq, d);
@@ -771,6 +799,7 @@ extern "C" smha_status_t smha_sink_workspace(int B, int H, int Hkv, int Sq, int 
     const smha_status_t st = sink_params(sp, B, H, Hkv, Sq, Sk, d, SMHA_F16, nullptr, nullptr, window, n_sink, 0.f);
     if (st != SMHA_OK) return st;
     sink_cuts(sp);
+    if (!sink_grids_fit(sp)) return SMHA_ERR_UNSUPPORTED;
     const bool cut = sp.cut_sink > 1 || sp.cut_rest > 1;
     *need = (size_t)(sink_stats_bytes(sp) + (cut ? sink_items(sp) * 2 * 128 * sink_width(d) * 4 : 0));
     return SMHA_OK;
@@ -787,7 +816,8 @@ extern "C" smha_status_t smha_sink_backward(const void *Q, const void *K, const 
     const smha_status_t st = sink_params(sp, B, H, Hkv, Sq, Sk, d, dtype, offsets, lengths, window, n_sink, scale);
     if (st != SMHA_OK) return st;
     size_t need = 0;
-    (void)smha_sink_workspace(B, H, Hkv, Sq, Sk, d, window, n_sink, &need);
+    const smha_status_t fits = smha_sink_workspace(B, H, Hkv, Sq, Sk, d, window, n_sink, &need);
+    if (fits != SMHA_OK) return fits;
     if (workspace_bytes < need) return SMHA_ERR_INVALID_ARG;
     if (((uintptr_t)Q | (uintptr_t)K | (uintptr_t)V | (uintptr_t)O | (uintptr_t)O_rest | (uintptr_t)dO | (uintptr_t)dQ | (uintptr_t)dK | (uintptr_t)dV | (uintptr_t)workspace) & 15)
         return SMHA_ERR_UNSUPPORTED;
@@ -795,6 +825,7 @@ extern "C" smha_status_t smha_sink_backward(const void *Q, const void *K, const 
         if (!strides_fit(s, Sq + 128, d)) return SMHA_ERR_UNSUPPORTED;
     for (const int64_t *s : {k_strides, v_strides, dk_strides, dv_strides})
         if (!strides_fit(s, (int64_t)Sk + 128, d)) return SMHA_ERR_UNSUPPORTED;
+    if (!apart(dq_strides, B, H, d) || !apart(dk_strides, B, Hkv, d) || !apart(dv_strides, B, Hkv, d)) return SMHA_ERR_UNSUPPORTED;
     sink_cuts(sp);
     sp.Q = (const uint16_t *)Q; sp.K = (const uint16_t *)K; sp.V = (const uint16_t *)V; sp.Oin = (const uint16_t *)O; sp.rest = (uint16_t *)const_cast<void *>(O_rest); sp.dO = (const uint16_t *)dO;
     sp.dQ = (uint16_t *)dQ; sp.dK = (uint16_t *)dK; sp.dV = (uint16_t *)dV; sp.lse = const_cast<float *>(lse);
@@ -804,15 +835,16 @@ extern "C" smha_status_t smha_sink_backward(const void *Q, const void *K, const 
     sp.stats = (float *)workspace;
     sp.parts = (float *)((char *)workspace + sink_stats_bytes(sp));
     const hipStream_t stream = (hipStream_t)hip_stream;
-    auto go = [&](auto bf16) {
-        constexpr bool BF = decltype(bf16)::value;
+    auto go = [&](auto bf16, auto fine) {
+        constexpr bool BF = decltype(bf16)::value, FINE = decltype(fine)::value;
         switch (sink_width(d)) {
-            case 32: return launch_sink_bwd<64, 32, BF>(sp, stream);
-            case 64: return launch_sink_bwd<64, 64, BF>(sp, stream);
-            case 96: return launch_sink_bwd<128, 96, BF>(sp, stream);
-            default: return launch_sink_bwd<128, 128, BF>(sp, stream);
+            case 32: return launch_sink_bwd<64, 32, BF, FINE>(sp, stream);
+            case 64: return launch_sink_bwd<64, 64, BF, FINE>(sp, stream);
+            case 96: return launch_sink_bwd<128, 96, BF, FINE>(sp, stream);
+            default: return launch_sink_bwd<128, 128, BF, FINE>(sp, stream);
         }
     };
-    const hipError_t e = dtype == SMHA_BF16 ? go(std::true_type()) : go(std::false_type());
+    auto by_type = [&](auto fine) { return dtype == SMHA_BF16 ? go(std::true_type(), fine) : go(std::false_type(), fine); };
+    const hipError_t e = fine_ds(sp) ? by_type(std::true_type()) : by_type(std::false_type());
     return e == hipSuccess ? SMHA_OK : SMHA_ERR_HIP;
 }

@@ -288,6 +288,11 @@ PyObject *sink_attention(PyObject *, PyObject *const *args, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
+// A tensor that was written: autograd refuses to go back through what was saved of it.
+void written(const at::Tensor &t) {
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+
 // cache_attention(q, k, v, lengths, window, n_sink, prefix keys or None, prefix values or None, weights or None, scale) -> the output, a status, or None
 PyObject *cache_attention(PyObject *, PyObject *const *args, Py_ssize_t n) {
     HANDLE_TH_ERRORS
@@ -313,10 +318,12 @@ PyObject *cache_attention(PyObject *, PyObject *const *args, Py_ssize_t n) {
         pv = b.data_ptr();
     }
     float *weights = nullptr;
+    at::Tensor weights_t;
     if (args[8] != Py_None) {
         if (!plain(args[8], 3)) Py_RETURN_NONE;
         const at::Tensor &w = THPVariable_Unpack(args[8]);
         if (w.scalar_type() != at::kFloat || w.size(0) != B || w.size(1) != Hkv || w.size(2) != Sk || w.device() != q.device() || !w.is_contiguous()) Py_RETURN_NONE;
+        weights_t = w;
         weights = w.data_ptr<float>();
     }
     const Strides3 qs(q), ks(k), vs(v);
@@ -331,6 +338,7 @@ PyObject *cache_attention(PyObject *, PyObject *const *args, Py_ssize_t n) {
                                (smha_dtype_t)code_of(q.scalar_type()), qs.ptr, ks.ptr, vs.ptr, nullptr, nullptr, nullptr, nullptr, window, n_sink,
                                (float)PyFloat_AS_DOUBLE(args[9]), ws.data_ptr(), need, c10::hip::getCurrentHIPStream(q.device().index()).stream());
     if (st != SMHA_OK) return PyLong_FromLong((long)st);
+    if (weights) written(weights_t);
     return THPVariable_Wrap(std::move(o));
     END_HANDLE_TH_ERRORS
 }
@@ -368,6 +376,8 @@ PyObject *cache_evict(PyObject *, PyObject *const *args, Py_ssize_t n) {
                              p2.data_ptr<int32_t>(), len2.data_ptr<int32_t>(), B, Hkv, Sk, d, budget, recent, ks.ptr, vs.ptr, ws.data_ptr(), need,
                              c10::hip::getCurrentHIPStream(k.device().index()).stream());
     if (st != SMHA_OK) return PyLong_FromLong((long)st);
+    written(k);
+    written(v);
     PyObject *out = PyTuple_New(3);
     if (!out) return nullptr;
     PyTuple_SET_ITEM(out, 0, THPVariable_Wrap(std::move(w2)));

@@ -166,7 +166,8 @@ def sink_attention(q, k, v, window: int = 0, n_sink: int = 0, *, offsets=None, l
     q [B,H,Sq,d]; k, v [B,Hkv,Sk,d], H a multiple of Hkv; float16 or bfloat16, d a multiple of 8 up to 128.  Query i of sequence b stands at
     offsets[b] + i (default Sk - Sq + i) and exists where that is in 0 .. lengths[b] - 1 (default Sk); it sees key j iff j is not after it and
     either within the last `window` keys (0: any) or one of the first `n_sink`.  offsets, lengths: int32 [B] on the GPU, read there.  scale: 0
-    for 1/sqrt(d).  Queries that do not exist give zeros, and neither they nor keys past a length receive or pass on gradients."""
+    or less for 1/sqrt(d).  Queries that do not exist give zeros, and neither they nor keys past a length receive or pass on gradients.
+    (A pass is captured into a graph where no eager graph of the same leaves is alive, as torch wants it.)"""
     global _call
     if _call is None:
         _call = native_call("sink_attention")

@@ -134,6 +134,67 @@ def test_what_is_not_seen_may_hold_anything():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("Sk, P", [(64, 0), (64, 70), (3000, 0), (50, 5000)])   # direct, direct with a prefix, cut, wide
+def test_a_token_that_is_not_a_number_gives_none(Sk, P):
+    q, k, v, prefix = make(12, 8, 1, 1, Sk, 64, P=P)
+    n = int32([Sk] * 12)
+    want, bound, _ = reference(q, k, v, n.tolist(), 0, 0, prefix)
+    q[3, 5] = math.nan
+    weights = torch.zeros(12, 1, Sk, device="cuda")
+    out = smha.cache_attention(q, k, v, n, prefix=prefix)
+    weighed = smha.cache_attention(q, k, v, n, prefix=prefix, weights=weights)
+    assert bool(weights[3].isnan().all()) and not weights[:3].isnan().any() and not weights[4:].isnan().any()
+    for got in (out, weighed):
+        assert bool(got[3, 5].isnan().all())
+        got[3, 5] = want[3, 5].to(got)
+        check(got, want, bound, "others")
+
+
+@pytest.mark.gpu
+def test_autograd_notices_a_cache_that_was_written():
+    """What was saved of keys that an eviction moved, or of an account, is not used for gradients."""
+    q, k, v, _ = make(2, 4, 2, 1, 40, 64)
+    w, pos, n = torch.rand(2, 2, 40, device="cuda"), torch.arange(40, dtype=torch.int32, device="cuda").expand(2, 2, 40).contiguous(), int32([40, 30])
+    for write in (lambda: smha.cache_evict(k, v, w, pos, n, 20), lambda: smha.cache_evict(k, v, w, pos, n, 20, out=(w, pos, n))):
+        x = q.detach().requires_grad_()
+        out = smha.sink_attention(x, k, v, 10, 2)
+        write()
+        with pytest.raises(RuntimeError, match="inplace"):
+            out.float().sum().backward()
+    x = torch.ones(2, 2, 40, device="cuda", requires_grad=True)
+    product = (x * w).sum()
+    smha.cache_attention(q, k, v, n, weights=w)
+    with pytest.raises(RuntimeError, match="inplace"):
+        product.backward()
+    with torch.inference_mode():
+        a, b, c, _ = make(1, 4, 2, 1, 40, 64)
+        smha.cache_attention(a, b, c, int32([40]), weights=torch.zeros(1, 2, 40, device="cuda"))
+        smha.cache_evict(b, c, torch.zeros(1, 2, 40, device="cuda"), torch.zeros(1, 2, 40, dtype=torch.int32, device="cuda"), int32([40]), 20)
+
+
+@pytest.mark.gpu
+def test_two_calls_at_once():
+    """On two streams, whose kernels and workspaces may overlap in time."""
+    calls = [make(6, 16, 4, 1, 3000, 128, dtype=torch.bfloat16, seed=seed, P=0) for seed in (1, 2)]
+    n = int32([3000, 10, 2999, 1500, 0, 700])
+
+    def one(q, k, v, _):
+        w = torch.zeros(6, 4, 3000, device="cuda")
+        return smha.cache_attention(q, k, v, n, weights=w), w
+
+    want = [one(*c) for c in calls]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in calls]
+    for _ in range(3):
+        got = []
+        for stream, c in zip(streams, calls):
+            with torch.cuda.stream(stream):
+                got.append(one(*c))
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for x, y in zip(got, want) for a, b in zip(x, y))
+
+
+@pytest.mark.gpu
 def test_one_token_is_the_last_query_of_a_whole_pass():
     """Token by token on a growing cache as sink_attention on the whole sequence (both within their bounds of the same formula)."""
     S, window, n_sink = 150, 40, 3
@@ -399,9 +460,9 @@ def test_refusals():
     ptr = C.c_void_p(4096)
     invalid, unsupported, shape = 1, 2, 3
 
-    def forward(q=ptr, lengths=ptr, pk=None, B=1, H=4, Hkv=2, T=1, Sk=8, P=0, d=64, dtype=0, ks=None, window=0, n_sink=0, ws=ptr, size=1 << 40):
-        s = (C.c_int64 * 3)(*ks) if ks else None
-        return lib.smha_cache_forward(q, ptr, ptr, pk, pk, ptr, None, lengths, B, H, Hkv, T, Sk, P, d, dtype, None, s, None, None, None, None, None, window, n_sink,
+    def forward(q=ptr, lengths=ptr, pk=None, B=1, H=4, Hkv=2, T=1, Sk=8, P=0, d=64, dtype=0, ks=None, window=0, n_sink=0, ws=ptr, size=1 << 40, out=None):
+        s, out = ((C.c_int64 * 3)(*x) if x else None for x in (ks, out))
+        return lib.smha_cache_forward(q, ptr, ptr, pk, pk, ptr, None, lengths, B, H, Hkv, T, Sk, P, d, dtype, None, s, None, None, None, out, None, window, n_sink,
                                       0.0, ws, size, None)
 
     assert forward(q=None) == invalid and forward(lengths=None) == invalid and forward(ws=None) == invalid and forward(size=15) == invalid
@@ -412,6 +473,9 @@ def test_refusals():
     assert forward(P=5, pk=ptr, window=3) == unsupported
     assert forward(ks=(1024, 512, 32)) == unsupported and forward(ks=(1024, 512, 68)) == unsupported
     assert forward(q=C.c_void_p(4104)) == unsupported and forward(Sk=1 << 25) == unsupported
+
+    assert forward(B=2, out=(0, 64, 64)) == unsupported and forward(out=(256, 0, 64)) == unsupported  # heads written in one place
+    assert forward(B=1 << 12, H=1 << 12, Hkv=1 << 12) == unsupported  # more workgroups than a launch has
 
     def evict(k=ptr, B=1, Hkv=2, Sk=8, d=64, budget=4, recent=1, ks=None, size=1 << 30):
         s = (C.c_int64 * 3)(*ks) if ks else None

@@ -115,6 +115,12 @@ CASES = [
     (1, 8, 1, 1500, 1500, 64, 0, 0, None, [1400], "bshd"),
     (2, 2, 2, 100, 1000, 128, 64, 64, [900, 0], [1000, 100], "bhsd"),  # keys that no query sees
     (2, 2, 1, 40, 500, 64, 50, 20, [500, -40], [500, 500], "bhsd"),   # all queries outside
+    # more than 16384 queries, whose dS is multiplied rounded
+    (9, 8, 2, 240, 240, 64, 50, 4, None, [240, 1, 0, 100, 129, 64, 239, 33, 200], "bshd"),
+    (9, 8, 8, 240, 240, 32, 0, 0, None, None, "bhsd"),
+    (9, 8, 1, 240, 250, 80, 16, 1, [10, 0, -100, 10, 10, 200, 5, 10, 10], [250, 240, 250, 250, 130, 250, 128, 10, 250], "bhsd"),
+    (9, 8, 4, 240, 240, 128, 100, 130, None, None, "bshd"),
+    (1, 16, 1, 1100, 1100, 128, 300, 2, None, None, "bhsd"),          # and key tiles cut into parts
 ]
 
 
@@ -301,6 +307,104 @@ def test_other_streams_and_a_captured_step():
         assert all(torch.equal(a, b) for a, b in zip(captured, eager)), seed
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16], ids=["f16", "bf16"])
+def test_few_queries_have_finer_gradients(dtype):
+    """The same sequences alone and among copies that make more than 16384 queries of them.  Alone, dQ and dK are off by their own rounding (1, in its
+    units) and that of P in delta (0.1 of its square); among many by dS's rounding too (1 more): errors as sqrt(1.1) to sqrt(2.1), 0.72."""
+    q, k, v, g = tensors(2, 12, 12, 100, 100, 64, dtype)
+    want = reference(q, k, v, g, 16, 1, None, None, 0.0)
+
+    def error(copies):
+        x = [t.repeat(copies, 1, 1, 1).requires_grad_() for t in (q, k, v)]
+        dq, dk, _ = torch.autograd.grad(smha.sink_attention(*x, 16, 1), x, g.repeat(copies, 1, 1, 1))
+        return [float((got[:2].cpu().double() - want[name][0]).norm()) for got, name in ((dq, "dq"), (dk, "dk"))]
+
+    assert 2 * 12 * 100 <= 16384 < 7 * 2 * 12 * 100
+    for few, many in zip(error(1), error(7)):
+        assert few <= 0.85 * many, (few, many)
+
+
+@pytest.mark.gpu
+def test_a_query_that_is_not_a_number_gives_none():
+    q, k, v, g = tensors(1, 4, 2, 200, 200, 64, torch.bfloat16)
+    want = reference(q, k, v, g, 50, 3, None, None, 0.0)
+    q[0, 1, 77] = math.nan
+    out, lse = torch.empty_like(q), torch.empty(1, 4, 200, device="cuda")
+    smha.smha_sink_forward(q, k, v, out, lse, 50, 3)
+    assert bool(out[0, 1, 77].isnan().all()) and bool(lse[0, 1, 77].isnan())
+    out[0, 1, 77], lse[0, 1, 77] = want["out"][0][0, 1, 77].cuda(), want["lse"][0][0, 1, 77].cuda()
+    check(out, want["out"], "out")
+    check(lse, want["lse"], "lse")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("scale", [1e-38, 1e-20, 30.0])
+def test_scales(scale):
+    """Scores that are all alike, and scores of thousands.  A score, a sum of 64 products in 32 bits, is exact to 64 half steps of the products'
+    magnitudes; its product with log2(e), the difference to the largest and the log-sum-exp take a few more."""
+    q, k, v, _ = tensors(1, 2, 2, 90, 90, 64, torch.float16)
+    out, lse = torch.empty_like(q), torch.empty(1, 2, 90, device="cuda")
+    smha.smha_sink_forward(q, k, v, out, lse, 40, 2, scale=scale)
+    seen = visible(90, 90, 0, 90, 40, 2)
+    Q, K, V = (t.cpu().double() for t in (q, k, v))
+    s = (Q @ K.mT * scale).masked_fill(~seen, -math.inf)
+    P = torch.softmax(s, -1)
+    e = 70 * 2.0 ** -24 * (Q.abs() @ K.abs().mT * scale).masked_fill(~seen, 0).amax(-1, keepdim=True) + F
+    u = 2.0 ** -11
+    assert bool(((out.cpu().double() - P @ V).abs() <= (u + 2 * e) * (P @ V.abs()) * (1 + u) + u * (P @ V).abs() + 2.0 ** -24 * V.abs().sum(-2, keepdim=True)).all())
+    assert bool(((lse.cpu().double() - torch.logsumexp(s, -1)).abs() <= 2 * e[..., 0] + 2.0 ** -24 * torch.logsumexp(s, -1).abs()).all())
+
+
+@pytest.mark.gpu
+def test_two_passes_at_once():
+    """On two streams, whose kernels and workspaces may overlap in time."""
+    inputs = [tensors(2, 8, 2, 700, 700, 128, torch.bfloat16, seed=seed) for seed in (1, 2)]
+
+    def one(q, k, v, g):
+        x = [t.detach().requires_grad_() for t in (q, k, v)]
+        out = smha.sink_attention(*x, 200, 4)
+        return (out, *torch.autograd.grad(out, x, g))
+
+    want = [one(*t) for t in inputs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in inputs]
+    for _ in range(3):
+        got = []
+        for stream, t in zip(streams, inputs):
+            with torch.cuda.stream(stream):
+                got.append(one(*t))
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for x, y in zip(got, want) for a, b in zip(x, y))
+
+
+@pytest.mark.gpu
+def test_a_captured_step_of_autograd():
+    shape = (2, 4, 2, 300, 300, 64, torch.bfloat16)
+    q, k, v, g = tensors(*shape)
+    x = [t.requires_grad_() for t in (q, k, v)]
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        out = smha.sink_attention(*x, 60, 4)
+        captured = (out, *torch.autograd.grad(out, x, g))
+    for seed in (1, 2, 3):
+        fresh = tensors(*shape, seed=seed)
+        with torch.no_grad():
+            for t, new in zip((q, k, v, g), fresh):
+                t.copy_(new)
+        y = [t.requires_grad_() for t in fresh[:3]]
+        eager = smha.sink_attention(*y, 60, 4)
+        eager = (eager, *torch.autograd.grad(eager, y, fresh[3]))
+        with torch.no_grad():
+            for t in captured:
+                t.fill_(math.nan)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(captured, eager)), seed
+
+
 def test_refusals():
     """On the CPU: what the C ABI says to arguments that do not fit, before it looks for a GPU."""
     import ctypes as C
@@ -308,9 +412,9 @@ def test_refusals():
     lib = _load()
     ptr = C.c_void_p(4096)
 
-    def forward(q=ptr, o=ptr, B=1, H=4, Hkv=2, Sq=8, Sk=8, d=64, dtype=0, strides=None, window=4, n_sink=0):
-        s = (C.c_int64 * 3)(*strides) if strides else None
-        return lib.smha_sink_forward(q, ptr, ptr, o, None, None, B, H, Hkv, Sq, Sk, d, dtype, s, None, None, None, None, None, window, n_sink, 0.0, None)
+    def forward(q=ptr, o=ptr, B=1, H=4, Hkv=2, Sq=8, Sk=8, d=64, dtype=0, strides=None, window=4, n_sink=0, out=None):
+        s, out = ((C.c_int64 * 3)(*x) if x else None for x in (strides, out))
+        return lib.smha_sink_forward(q, ptr, ptr, o, None, None, B, H, Hkv, Sq, Sk, d, dtype, s, None, None, out, None, None, window, n_sink, 0.0, None)
 
     invalid, unsupported, shape = 1, 2, 3
     assert forward(q=None) == invalid and forward(B=0) == invalid and forward(Sk=0) == invalid
@@ -320,14 +424,19 @@ def test_refusals():
     assert forward(q=C.c_void_p(4100)) == unsupported
     assert forward(strides=(2048, 512, 60)) == unsupported and forward(strides=(2048, 512, 56)) == unsupported and forward(strides=(-8, 512, 64)) == unsupported
     assert forward(Sk=1 << 25) == unsupported
+    assert forward(B=2, out=(0, 512, 64)) == unsupported and forward(out=(2048, 0, 64)) == unsupported  # heads written in one place
+    assert forward(B=1 << 12, H=1 << 12) == unsupported  # more workgroups than a launch has
     need = C.c_size_t(0)
     assert lib.smha_sink_workspace(1, 4, 2, 8, 8, 64, 4, 0, None) == invalid and lib.smha_sink_workspace(1, 4, 2, 8, 8, 64, 4, 0, C.byref(need)) == 0
     assert need.value == 2 * 4 * 128 * 4
 
-    def backward(workspace, size):
-        return lib.smha_sink_backward(*[ptr] * 10, 1, 4, 2, 8, 8, 64, 0, *[None] * 8, None, None, 4, 0, 0.0, workspace, size, None)
+    def backward(workspace, size, **written):
+        strides = [(C.c_int64 * 3)(*written[n]) if n in written else None for n in ("q", "k", "v", "o", "do", "dq", "dk", "dv")]
+        return lib.smha_sink_backward(*[ptr] * 10, 1, 4, 2, 8, 8, 64, 0, *strides, None, None, 4, 0, 0.0, workspace, size, None)
 
     assert backward(None, need.value) == invalid and backward(ptr, need.value - 1) == invalid
+    for name in ("dq", "dk", "dv"):
+        assert backward(ptr, need.value, **{name: (1024, 0, 64)}) == unsupported, name
 
 
 def test_refusals_of_the_binding():
