@@ -356,8 +356,8 @@ smha_status_t smha_sink_workspace(int B, int H, int Hkv, int Sq, int Sk, int d, 
 
 /* Gradients of Q, K and V (of `dtype`, written whole) from O, O_rest (or NULL) and lse of the forward with the same arguments and dO, the
  * gradient of O.  The result does not depend on the order in which workgroups run: the parts of sums that were cut
- * are added in a fixed order.  P and dS = P (dP - delta) are rounded to `dtype` for the products that use them (where
- * there are at most 16384 queries in all, dS to twice its digits): in binary16 the gradient of O has to be scaled (as such training
+ * are added in a fixed order.  P and dS = P (dP - delta) are rounded to `dtype` for the products that use them (of
+ * at most 8192 queries in all that see few keys, dS to twice its digits): in binary16 the gradient of O has to be scaled (as such training
  * does) so that dS keeps within that type's range.  workspace: device, 16-byte aligned, smha_sink_workspace bytes or more; the
  * call's alone until it has run. */
 smha_status_t smha_sink_backward(const void *Q, const void *K, const void *V, const void *O, const void *O_rest,

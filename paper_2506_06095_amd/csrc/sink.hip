@@ -286,7 +286,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 4 : 2) smha_sink_fwd(const Sink
 // 32 bits that is rounded once, 1.42 times with what the rounding left out.
 // dS is rounded to the inputs' type for the product with K, as P is in the forward; FINE (see fine_ds): its rounding error is multiplied too.
 template <int D, int C, bool BF16, bool FINE>
-__global__ void __launch_bounds__(256, FINE ? 1 : 2) smha_sink_bwd_q(const SinkParams p) {
+__global__ void __launch_bounds__(256, 2) smha_sink_bwd_q(const SinkParams p) {
     constexpr int NS = C / 16, NDT = C / 32, TB = 64 * D * 2, PF = C == 128 ? 6 : 4;
     __shared__ __attribute__((aligned(1024))) char smem[4 * TB];  // K[0], K[1], V[0], V[1]
     const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_void *)smem;
@@ -459,7 +459,7 @@ __device__ __forceinline__ int parts_of(int steps, int cut, int chunk) { return 
 // A tile's steps (its queries, head by head) may be cut into parts that other workgroups take: the sinks' tiles are seen by every
 // query, and few key heads would leave most of the chip idle.  Parts go to memory in 32 bits and are added in order by smha_sink_sum.
 template <int D, int C, bool BF16, bool FINE>
-__global__ void __launch_bounds__(256, FINE ? 1 : D == 64 ? 3 : 2) smha_sink_bwd_kv(const SinkParams p) {
+__global__ void __launch_bounds__(256, D == 64 && !FINE ? 3 : 2) smha_sink_bwd_kv(const SinkParams p) {
     constexpr int NS = C / 16, NDT = C / 32, TB = 32 * D * 2, PF = 4;
     __shared__ __attribute__((aligned(1024))) char smem[4 * TB + 4 * TB];  // K, Q[0], Q[1], dO[0], dO[1]
     __shared__ __attribute__((aligned(1024))) float stats[2][2][64];       // [buffer][lse, delta][query] (32 of 64)
@@ -735,10 +735,12 @@ static bool sink_grids_fit(const SinkParams &sp) {
 }
 
 // Whether dS goes into dQ and dK with what its rounding leaves out.  dQ and dK of rounded dS are 1.44 times as far from 64 bits as their own
-// rounding on average; of few rows, where a few large ones make most of the norm, up to 1.50 (2 x 12 x 68 x 64).  There both halves are
-// multiplied, a product more of three and of four: 1.0x.  Such a pass is the host's (75 us of which the kernels run 25): it costs nothing.  Of many
-// rows it would: 1 x 32 x 8192 x 128, window 4096, runs at the matrix pipes' power.
-static bool fine_ds(const SinkParams &sp) { return (int64_t)sp.B * sp.H * sp.Sq <= 16384; }
+// rounding on average; of few queries, where a few large rows make most of the norm, up to 1.50 (2 x 12 x 68 x 64).  There both halves are
+// multiplied, a product more of three and of four: 1.05 (1.10 where windows are shortest).  us of a backward pass without and with them: 2 x 4 x 128 x 64, window 16: 15.6,
+// 16.4; 1 x 8 x 1024 x 64, window 256: 28.8, 30.9; 1 x 8 x 700 x 128: 48.9, 54.2; 1 x 2 x 1400 x 128: 73.2, 80.8 (most of which the host's 75 us
+// for a pass hide).  Of more queries errors average out, and products are what such a call lasts.
+static bool fine_ds(const SinkParams &sp) { const int64_t queries = (int64_t)sp.B * sp.H * sp.Sq;
+    return queries <= 8192 && queries * std::min<int64_t>(sp.Sk, (int64_t)sp.window + sp.n_sink) <= 1 << 22; }
 
 static int sink_width(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : d <= 96 ? 96 : 128; }
 

@@ -115,7 +115,7 @@ CASES = [
     (1, 8, 1, 1500, 1500, 64, 0, 0, None, [1400], "bshd"),
     (2, 2, 2, 100, 1000, 128, 64, 64, [900, 0], [1000, 100], "bhsd"),  # keys that no query sees
     (2, 2, 1, 40, 500, 64, 50, 20, [500, -40], [500, 500], "bhsd"),   # all queries outside
-    # more than 16384 queries, whose dS is multiplied rounded
+    # more than 8192 queries, whose dS is multiplied rounded
     (9, 8, 2, 240, 240, 64, 50, 4, None, [240, 1, 0, 100, 129, 64, 239, 33, 200], "bshd"),
     (9, 8, 8, 240, 240, 32, 0, 0, None, None, "bhsd"),
     (9, 8, 1, 240, 250, 80, 16, 1, [10, 0, -100, 10, 10, 200, 5, 10, 10], [250, 240, 250, 250, 130, 250, 128, 10, 250], "bhsd"),
@@ -310,7 +310,7 @@ def test_other_streams_and_a_captured_step():
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16], ids=["f16", "bf16"])
 def test_few_queries_have_finer_gradients(dtype):
-    """The same sequences alone and among copies that make more than 16384 queries of them.  Alone, dQ and dK are off by their own rounding (1, in its
+    """The same sequences alone and among copies that make more than 8192 queries of them.  Alone, dQ and dK are off by their own rounding (1, in its
     units) and that of P in delta (0.1 of its square); among many by dS's rounding too (1 more): errors as sqrt(1.1) to sqrt(2.1), 0.72."""
     q, k, v, g = tensors(2, 12, 12, 100, 100, 64, dtype)
     want = reference(q, k, v, g, 16, 1, None, None, 0.0)
@@ -320,7 +320,7 @@ def test_few_queries_have_finer_gradients(dtype):
         dq, dk, _ = torch.autograd.grad(smha.sink_attention(*x, 16, 1), x, g.repeat(copies, 1, 1, 1))
         return [float((got[:2].cpu().double() - want[name][0]).norm()) for got, name in ((dq, "dq"), (dk, "dk"))]
 
-    assert 2 * 12 * 100 <= 16384 < 7 * 2 * 12 * 100
+    assert 2 * 12 * 100 <= 8192 < 7 * 2 * 12 * 100
     for few, many in zip(error(1), error(7)):
         assert few <= 0.85 * many, (few, many)
 
