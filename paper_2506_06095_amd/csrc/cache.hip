@@ -693,7 +693,9 @@ __device__ __forceinline__ uint32_t ordered(float x) {
 // histogram in LDS (11 bits of a float are a quarter of an octave: lanes of a wave meet in few bins but seldom all in one, and where
 // they do one of them counts for all); of the keys that equal it the first slots stay.  What stays past the new end goes, in
 // order, where keys before it left.  (Counting with ballots, two bits at a time: 26.5 us for 128 heads of 4352 keys, 110 for 32 of 32768.)
-template <int KPT>
+// WHOLE: the rows are moved here too, which saves a launch where few move (evict_whole); their lists then take the histogram's place in LDS.
+constexpr int kWholeMoves = 512;
+template <int KPT, bool WHOLE>
 __global__ void __launch_bounds__(1024) smha_cache_select(const EvictParams p) {
     __shared__ int bins[2048];
     __shared__ int totals[3][16];
@@ -727,8 +729,17 @@ __global__ void __launch_bounds__(1024) smha_cache_select(const EvictParams p) {
         for (int i = threadIdx.x; i < end; i += 1024) Wo[i] = W[i];
     if (Po != P)
         for (int i = threadIdx.x; i < end; i += 1024) Po[i] = P[i];
+    // What lies past the new end; and the new length.
+    auto finish = [&]() __attribute__((always_inline)) {
+        for (int i = end + threadIdx.x; i < p.Sk; i += 1024) {
+            Wo[i] = 0.f;
+            Po[i] = -1;
+        }
+        if (threadIdx.x == 0 && bh == b * p.Hkv) p.len_out[b] = end;
+    };
     if (len <= p.budget) {
-        if (threadIdx.x == 0) list[0] = 0;
+        if constexpr (WHOLE) finish();
+        else if (threadIdx.x == 0) list[0] = 0;
         return;
     }
     int newest = INT32_MIN;
@@ -879,6 +890,45 @@ __global__ void __launch_bounds__(1024) smha_cache_select(const EvictParams p) {
     before_and_all(totals[2], lane, w, from, all);
     before_and_all(totals[1], lane, w, to, moves);
     equal_at = equal_first;
+    if constexpr (WHOLE) {
+        for (int i0 = 0; i0 < n; i0 += GROUP) {
+            if constexpr (KPT == 0) stay = staying(i0);
+            const uint32_t early = before_end(i0);
+            in_order(~stay & early, to, [&](int i, int place) __attribute__((always_inline)) { bins[place] = base + 64 * (i0 + i); });
+            in_order(stay & ~early, from, [&](int i, int place) __attribute__((always_inline)) { bins[kWholeMoves + place] = base + 64 * (i0 + i); });
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < moves; i += 1024) {
+            Wo[bins[i]] = W[bins[kWholeMoves + i]];
+            Po[bins[i]] = P[bins[kWholeMoves + i]];
+        }
+        const int hk = bh - b * p.Hkv, col = 8 * (threadIdx.x & 15), first = threadIdx.x >> 4;
+        uint16_t *const K = p.K + b * p.ks.b + hk * p.ks.h, *const V = p.V + b * p.vs.b + hk * p.vs.h;
+        constexpr int U = 4;  // rows of 16 lanes that travel together
+        for (int i0 = first; i0 < moves; i0 += 64 * U) {
+            u32x4 k[U], v[U];
+            const bool has = col < p.d;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int64_t from_row = bins[kWholeMoves + min(i0 + 64 * u, moves - 1)];
+                if (has) {
+                    k[u] = *reinterpret_cast<const u32x4 *>(K + from_row * p.ks.s + col);
+                    v[u] = *reinterpret_cast<const u32x4 *>(V + from_row * p.vs.s + col);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int64_t to_row = bins[min(i0 + 64 * u, moves - 1)];
+                if (has && i0 + 64 * u < moves) {
+                    *reinterpret_cast<u32x4 *>(K + to_row * p.ks.s + col) = k[u];
+                    *reinterpret_cast<u32x4 *>(V + to_row * p.vs.s + col) = v[u];
+                }
+            }
+        }
+        __syncthreads();  // (weights may be read and written in one place)
+        finish();
+        return;
+    }
     for (int i0 = 0; i0 < n; i0 += GROUP) {
         if constexpr (KPT == 0) stay = staying(i0);
         const uint32_t early = before_end(i0);
@@ -1048,6 +1098,12 @@ extern "C" smha_status_t smha_cache_forward(const void *Q, const void *K, const 
     return e == hipSuccess ? SMHA_OK : SMHA_ERR_HIP;
 }
 
+// Whether a head's own workgroup moves its rows.  us of a call by two kernels and by one: 16 x 8 heads of 4352 keys to 4096, x 128: 17.5, 15.3; 2 heads
+// of 1100 to 1024: 9.8, 8.1; 32 heads of 8192 to 7936, 7680, 7168: 16.7, 17.4, 19.1 and 14.9, 17.1, 23.3 (one compute unit moves 1 MB);
+// 512 heads of 8192 to 7680: 76.6, 72.7.  Lengths that are written where they are read need the second kernel: a sequence's other heads may still
+// have to read them.
+static bool evict_whole(const EvictParams &ep) { return ep.moves <= kWholeMoves && ep.len_out != ep.lengths; }
+
 static smha_status_t evict_sizes(int B, int Hkv, int Sk, int d, int budget, int recent, size_t *need) {
     if (B < 1 || Hkv < 1 || Sk < 1 || budget < 1 || recent < 0) return SMHA_ERR_INVALID_ARG;
     if (d < 8 || d > 128 || d % 8 || (int64_t)B * Hkv > 65535 || Sk > (1 << 28)) return SMHA_ERR_UNSUPPORTED;
@@ -1084,13 +1140,16 @@ extern "C" smha_status_t smha_cache_evict(void *K, void *V, const float *weights
     ep.lists = (int32_t *)workspace;
     const hipStream_t stream = (hipStream_t)hip_stream;
     const dim3 grid(B * Hkv);
-    if (Sk <= 4096) hipLaunchKernelGGL(smha_cache_select<4>, grid, dim3(1024), 0, stream, ep);
-    else if (Sk <= 8192) hipLaunchKernelGGL(smha_cache_select<8>, grid, dim3(1024), 0, stream, ep);
-    else if (Sk <= 16384) hipLaunchKernelGGL(smha_cache_select<16>, grid, dim3(1024), 0, stream, ep);
-    else if (Sk <= 32768) hipLaunchKernelGGL(smha_cache_select<32>, grid, dim3(1024), 0, stream, ep);
-    else hipLaunchKernelGGL(smha_cache_select<0>, grid, dim3(1024), 0, stream, ep);
+    const bool whole = evict_whole(ep);
+    auto *const select = Sk <= 4096    ? (whole ? smha_cache_select<4, true> : smha_cache_select<4, false>)
+                         : Sk <= 8192  ? (whole ? smha_cache_select<8, true> : smha_cache_select<8, false>)
+                         : Sk <= 16384 ? (whole ? smha_cache_select<16, true> : smha_cache_select<16, false>)
+                         : Sk <= 32768 ? (whole ? smha_cache_select<32, true> : smha_cache_select<32, false>)
+                                       : (whole ? smha_cache_select<0, true> : smha_cache_select<0, false>);
+    hipLaunchKernelGGL(select, grid, dim3(1024), 0, stream, ep);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return SMHA_ERR_HIP;
+    if (whole) return SMHA_OK;
     hipLaunchKernelGGL(smha_cache_move, dim3((unsigned)std::max(1, std::min(64, (ep.moves + 63) / 64)), B * Hkv), dim3(256), 0, stream, ep);
     e = hipGetLastError();
     return e == hipSuccess ? SMHA_OK : SMHA_ERR_HIP;

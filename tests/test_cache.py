@@ -349,11 +349,14 @@ EVICT = [
     (1, 1, 40000, 8, [39999], 20000, 7, "ties"),             # more slots than a workgroup holds in registers
     (1, 2, 300, 64, [300], 1000, 3, "spread"),               # nothing to do
     (3, 1, 130, 64, [500, -7, 130], 100, 10, "spread"),      # lengths outside the cache
+    (2, 2, 1024, 72, [1024, 700], 512, 30, "spread"),        # as many moves as one workgroup makes, and one more
+    (1, 3, 1026, 64, [1026], 513, 0, "ties"),
+    (1, 2, 40000, 8, [40000], 39500, 7, "spread"),
 ]
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("in_place", [False, True], ids=["", "in_place"])
+@pytest.mark.parametrize("in_place", [0, 3, 2], ids=["", "in_place", "weights_and_positions_in_place"])
 @pytest.mark.parametrize("case", EVICT, ids=lambda c: "x".join(str(x) for x in (*c[:4], *c[5:])))
 def test_eviction_is_the_plain_selection(case, in_place):
     B, Hkv, Sk, d, lengths, budget, recent, values = case
@@ -364,11 +367,11 @@ def test_eviction_is_the_plain_selection(case, in_place):
     if n.max() > Sk or n.min() < 0:
         assert want[-1].tolist() == [min(max(x, 0), Sk, budget) for x in lengths]
     given = [t.clone() for t in (w, pos, n)]
-    out = smha.cache_evict(k, v, w, pos, n, budget, recent, out=(w, pos, n) if in_place else None)
+    to = (w, pos, n if in_place == 3 else torch.full_like(n, -5)) if in_place else None
+    out = smha.cache_evict(k, v, w, pos, n, budget, recent, out=to)
     if in_place:
-        assert all(a is b for a, b in zip(out, (w, pos, n)))
-    else:
-        assert all(torch.equal(a.view(torch.int32), b.view(torch.int32)) for a, b in zip((w, pos, n), given))
+        assert all(a is b for a, b in zip(out, to))
+    assert all(torch.equal(a.view(torch.int32), b.view(torch.int32)) for a, b in list(zip((w, pos, n), given))[in_place:])
     for name, a, b in zip(("k", "v", "weights", "positions", "lengths"), (k, v, *out), want):
         a = a.cpu()
         same = (a == b) | (a.isnan() & b.isnan()) if a.is_floating_point() else a == b
