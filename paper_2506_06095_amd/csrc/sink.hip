@@ -643,11 +643,13 @@ __global__ void __launch_bounds__(256, D == 64 && !FINE ? 3 : 2) smha_sink_bwd_k
     }
 }
 
-// The parts of a key tile that was cut, added in order.  A workgroup takes one wave's 32 keys of dK or dV.
+// The parts of a key tile that was cut, added in order, four on the way at once.  A workgroup takes one wave's 32 keys of dK or dV.  Where only
+// tiles with sinks are cut it is launched for those alone.
 template <int C, bool BF16>
 __global__ void __launch_bounds__(256) smha_sink_sum(const SinkParams p) {
     const int tile_at = (int)blockIdx.x >> 3, w = (int)blockIdx.x & 3, is_k = ((int)blockIdx.x >> 2) & 1;
-    const int bh = tile_at / p.n_tiles, tile = tile_at - bh * p.n_tiles, b = bh / p.Hkv, hk = bh - b * p.Hkv;
+    const int tiles = p.cut_rest > 1 ? p.n_tiles : p.n_sink_tiles;
+    const int bh = tile_at / tiles, tile = tile_at - bh * tiles, b = bh / p.Hkv, hk = bh - b * p.Hkv;
     const int per = p.n_sink_tiles * p.cut_sink + (p.n_tiles - p.n_sink_tiles) * p.cut_rest;
     const bool sink = tile < p.n_sink_tiles;
     const int cut = sink ? p.cut_sink : p.cut_rest;
@@ -661,7 +663,14 @@ __global__ void __launch_bounds__(256) smha_sink_sum(const SinkParams p) {
     const float *const from = p.parts + (((int64_t)(hk * p.B + b) * per + item) * 8 + is_k * 4 + w) * (C / 8) * 256;
     for (int i = threadIdx.x; i < C / 8 * 64; i += 256) {
         f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-        for (int c = 0; c < parts; ++c) sum += *reinterpret_cast<const f32x4 *>(from + (int64_t)c * 8 * (C / 8) * 256 + i * 4);
+        for (int c0 = 0; c0 < parts; c0 += 4) {
+            f32x4 x[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) x[u] = *reinterpret_cast<const f32x4 *>(from + (int64_t)min(c0 + u, parts - 1) * 8 * (C / 8) * 256 + i * 4);
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (c0 + u < parts) sum += x[u];
+        }
         const int quad = i >> 6, lane = i & 63, key = tile * 128 + 32 * w + (lane & 31), col = 8 * quad + 4 * (lane >> 5);
         if (key < p.Sk && col < p.d)
             *reinterpret_cast<u32x2 *>(out + key * pitch + col) = u32x2{pack2<BF16>(sum[0] * factor, sum[1] * factor), pack2<BF16>(sum[2] * factor, sum[3] * factor)};
@@ -759,7 +768,7 @@ template <int D, int C, bool BF16, bool FINE> static hipError_t launch_sink_bwd(
     sp.per_xcd = (int)((sink_items(sp) + 7) / 8);
     hipLaunchKernelGGL((smha_sink_bwd_kv<D, C, BF16, FINE>), dim3(8 * sp.per_xcd), dim3(256), 0, stream, sp);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    if (sp.cut_sink > 1 || sp.cut_rest > 1) hipLaunchKernelGGL((smha_sink_sum<C, BF16>), dim3((unsigned)(8 * sp.B * sp.Hkv * sp.n_tiles)), dim3(256), 0, stream, sp);
+    if (sp.cut_sink > 1 || sp.cut_rest > 1) hipLaunchKernelGGL((smha_sink_sum<C, BF16>), dim3((unsigned)(8 * sp.B * sp.Hkv * (sp.cut_rest > 1 ? sp.n_tiles : sp.n_sink_tiles))), dim3(256), 0, stream, sp);
     return hipGetLastError();
 }
 
