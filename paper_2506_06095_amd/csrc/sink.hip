@@ -38,7 +38,7 @@ struct SinkParams {
     float c, scale;       // c = scale * log2(e)
     int per_xcd;          // work items per XCD
     // backward
-    float *stats;         // [2][B][H][Sqp]: lse * log2(e) (inf where there is no query), delta
+    float *stats;         // [2][B][H][Sqp]: lse * log2(e) (inf where there is no query), -delta
     int Sqp;
     float *parts;         // partial dK, dV of key tiles that are cut along their queries
     int n_tiles, n_sink_tiles;              // key tiles, those with sinks
@@ -342,7 +342,7 @@ __global__ void __launch_bounds__(256, 2) smha_sink_bwd_q(const SinkParams p) {
     if (hh == 0) {
         const int64_t row = (int64_t)bh * p.Sqp + qw + j;
         p.stats[row] = lse2;
-        p.stats[(int64_t)p.B * p.H * p.Sqp + row] = delta;
+        p.stats[(int64_t)p.B * p.H * p.Sqp + row] = -delta;
     }
 
     const int rd = j * D * 2 + ((hh ^ swz_both<D>(j)) * 16);
@@ -518,7 +518,6 @@ __global__ void __launch_bounds__(256, D == 64 && !FINE ? 3 : 2) smha_sink_bwd_k
     const int rd_ = j * D * 2 + ((hh ^ swz_both<D>(j)) * 16);
     const int tr_row = 4 * hh + ((lane & 15) >> 2);
     const int tr_ = tr_row * D * 2 + ((swz_both<D>(tr_row) ^ (2 * ((lane >> 4) & 1) + ((lane & 3) >> 1))) * 16) + (lane & 1) * 8;
-    const char *const Kt = smem + w * TB;
     f32x16 dk[NDT], dv[NDT];
 #pragma unroll
     for (int dt = 0; dt < NDT; ++dt) dk[dt] = dv[dt] = zeros16();
@@ -529,43 +528,48 @@ __global__ void __launch_bounds__(256, D == 64 && !FINE ? 3 : 2) smha_sink_bwd_k
         if (t + 1 < end) request(g, 32 * (kt.qt0 + qt), par ^ 1);
         const int p0 = s.off + max(q, s.qa), p1 = s.off + min(q + 32, s.qb) - 1;
         if (p0 <= p1 && any_seen(p0, p1, kw, kw + 31, window, n_sink)) {
-            const char *const Qt = smem + Q_AT + par * TB, *const Gt = smem + G_AT + par * TB;
-            int rd = rd_, tr = tr_;
-            asm volatile("" : "+v"(rd), "+v"(tr));  // (operand addresses are made here, not kept in registers across steps)
-            auto row_frag = [&](const char *base, int i) __attribute__((always_inline)) { return *reinterpret_cast<const u32x4 *>(base + (rd ^ (32 * i))); };
-            auto col_frag = [&](const char *base, int i) __attribute__((always_inline)) {  // i = cu NDT + dt: queries 16 cu + 8 a + 4 hh .., columns 32 dt + j
+            int rd = rd_ + par * TB, rdk = rd_ + w * TB, tr = tr_ + par * TB;
+            asm volatile("" : "+v"(rd), "+v"(rdk), "+v"(tr));  // (operand addresses are made here, not kept in registers across steps)
+            auto row_frag = [&](int base, int at, int i) __attribute__((always_inline)) { return *reinterpret_cast<const u32x4 *>(smem + ((at ^ (32 * i)) + base)); };
+            auto col_frag = [&](int base, int i) __attribute__((always_inline)) {  // i = cu NDT + dt: queries 16 cu + 8 a + 4 hh .., columns 32 dt + j
                 const int cu = i / NDT, dt = i % NDT;
-                const u32x2 lo = lds_read_tr(reinterpret_cast<const uint16_t *>(base + ((tr ^ (64 * dt)) + 32 * cu * D)));
-                const u32x2 hi = lds_read_tr(reinterpret_cast<const uint16_t *>(base + ((tr ^ (64 * dt) ^ 32) + 32 * cu * D + 16 * D)));
+                const u32x2 lo = lds_read_tr(reinterpret_cast<const uint16_t *>(smem + ((tr ^ (64 * dt)) + (base + 32 * cu * D))));
+                const u32x2 hi = lds_read_tr(reinterpret_cast<const uint16_t *>(smem + ((tr ^ (64 * dt) ^ 32) + (base + 32 * cu * D + 16 * D))));
                 return u32x4{lo[0], lo[1], hi[0], hi[1]};
             };
             // The left operands of the step's products, in their order: Q's rows, dO's rows, dO's columns, Q's columns.
             auto operand = [&](int n) __attribute__((always_inline)) {
-                return n < NS ? row_frag(Qt, n) : n < 2 * NS ? row_frag(Gt, n - NS) : n < 2 * NS + 2 * NDT ? col_frag(Gt, n - 2 * NS) : col_frag(Qt, n - 2 * NS - 2 * NDT);
+                return n < NS ? row_frag(Q_AT, rd, n) : n < 2 * NS ? row_frag(G_AT, rd, n - NS) : n < 2 * NS + 2 * NDT ? col_frag(G_AT, n - 2 * NS) : col_frag(Q_AT, n - 2 * NS - 2 * NDT);
             };
             constexpr int ALL = 2 * NS + 4 * NDT;
             u32x4 f[PF], fk[PF];
             auto next = [&](int n) __attribute__((always_inline)) {  // product n has its operand: the one PF on is requested
                 if (n + PF < ALL) f[n % PF] = operand(n + PF);
             };
-            // sc[r] = score of key j and query 8 (r / 4) + 4 hh + r % 4
-            f32x16 sc = zeros16(), dp = zeros16();
+            // sc[r] = score of key j and query 8 (r / 4) + 4 hh + r % 4; dp: likewise, dP - delta, whose sum begins at -delta
+            f32x16 sc = zeros16(), dp;
 #pragma unroll
             for (int i = 0; i < PF; ++i) {
-                if (i < NS) fk[i] = row_frag(Kt, i);
+                if (i < NS) fk[i] = row_frag(0, rdk, i);
                 f[i] = operand(i);
             }
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int i = 0; i < NS; ++i) {
                 sc = mfma32<BF16>(f[i % PF], fk[i % PF], sc);
-                if (i + PF < NS) fk[i % PF] = row_frag(Kt, i + PF);
+                if (i + PF < NS) fk[i % PF] = row_frag(0, rdk, i + PF);
                 next(i);
                 __builtin_amdgcn_sched_barrier(0);
             }
             const float *const lse_at = &stats[par][0][4 * hh], *const delta_at = &stats[par][1][4 * hh];
-            f32x4 of[2];  // lse, then delta: of[r4 & 1] is that of accumulators 4 r4 .. 4 r4 + 3
+            f32x4 of[2];  // lse: of[r4 & 1] is that of accumulators 4 r4 .. 4 r4 + 3
             of[0] = *reinterpret_cast<const f32x4 *>(lse_at);
+#pragma unroll
+            for (int r4 = 0; r4 < 4; ++r4) {
+                const f32x4 x = *reinterpret_cast<const f32x4 *>(delta_at + 8 * r4);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) dp[4 * r4 + e] = x[e];
+            }
             const bool part_seen = !all_seen(s.off + q, s.off + q + 31, kw, kw + 31, window, n_sink) || q < s.qa || q + 32 > s.qb;
             uint32_t word = ~0u;
             if (part_seen) {
@@ -594,7 +598,6 @@ __global__ void __launch_bounds__(256, D == 64 && !FINE ? 3 : 2) smha_sink_bwd_k
             }
 #pragma unroll
             for (int i = 0; i < 8; ++i) pf[i >> 2][i & 3] = pack2<BF16>(sc[2 * i], sc[2 * i + 1]);
-            of[0] = *reinterpret_cast<const f32x4 *>(delta_at);
             __builtin_amdgcn_sched_barrier(0);
             // dV, and dS from P and dP
 #pragma unroll
@@ -602,10 +605,7 @@ __global__ void __launch_bounds__(256, D == 64 && !FINE ? 3 : 2) smha_sink_bwd_k
                 dv[i % NDT] = mfma32<BF16>(f[(2 * NS + i) % PF], pf[i / NDT], dv[i % NDT]);
                 next(2 * NS + i);
 #pragma unroll
-                for (int r = 16 * i / (2 * NDT); r < 16 * (i + 1) / (2 * NDT); ++r) {
-                    if (r % 4 == 0 && r < 12) of[(r / 4 + 1) & 1] = *reinterpret_cast<const f32x4 *>(delta_at + 2 * r + 8);
-                    dp[r] = sc[r] * (dp[r] - of[(r / 4) & 1][r % 4]);
-                }
+                for (int r = 16 * i / (2 * NDT); r < 16 * (i + 1) / (2 * NDT); ++r) dp[r] *= sc[r];
                 __builtin_amdgcn_sched_barrier(0);
             }
             if (part_seen) {  // (where P is zero dP may be anything)
