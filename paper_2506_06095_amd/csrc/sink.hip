@@ -36,7 +36,7 @@ struct SinkParams {
     int window, n_sink;   // 1 .. Sk (a window of Sk keys limits nothing), 0 .. Sk
     const int32_t *offsets, *lengths;
     float c, scale;       // c = scale * log2(e)
-    int per_xcd;          // work items per XCD
+    int per, together;    // work items of a key head of a sequence; such heads whose items are taken in turn
     // backward
     float *stats;         // [2][B][H][Sqp]: lse * log2(e) (inf where there is no query), -delta
     int Sqp;
@@ -58,20 +58,36 @@ __device__ __forceinline__ Sequence sequence(const SinkParams &p, int b) {
     return s;
 }
 
-// A workgroup's 128 queries.  An XCD takes a run of (key head, sequence, query head): the heads that share keys do it in one L2, and every
-// XCD has sequences of all lengths (by sequence first, 4 x 12 x 1537 x 80 with lengths of 60 to 100 %: XCDs with the longest ones had 78 workgroups in
-// 64 places).  A head's last queries, which have the longest lists, come first.
+// What a workgroup of a launch takes: item `item` of the key head `hk` of sequence `b`.  `together` of these groups go through their items in turn, the
+// longest first, so that what starts last is short; a multiple of eight of them keep to an XCD each, whose L2 their workgroups share, and
+// no more go together than a few rounds of the chip.  (By group, each XCD a run of them: a backward pass of 8 x 32 on 8 x 4096 x 128, window
+// 1024, 4 sinks 2229 us, 1778 so, the sinks' tiles of the last groups began last; 1 x 32 x 4096 x 128, window 2048: 453, 386;
+// 4 x 16 x 1024 x 128, window 128: 68, 63.)
+struct Turn {
+    int b, hk, item;
+    __device__ __forceinline__ explicit Turn(const SinkParams &p) {
+        const int at = blockIdx.x, n = p.B * p.Hkv, block = at / (p.together * p.per), first = block * p.together, groups = min(p.together, n - first);
+        const int rest = at - first * p.per;
+        item = rest / groups;
+        const int group = first + rest - item * groups;
+        b = group / p.Hkv;  // (an XCD has sequences of all lengths: by key head first, 4 x 12 x 1537 x 80 with 60 to 100 % of it had one length each: 94 us a pass for 83)
+        hk = group - b * p.Hkv;
+    }
+};
+// `at_once`: workgroups of an XCD that go together, about.  Keys' tiles 256 (2 x 16 x 8192 x 64, backward: 954 us with 128, 918), queries' 128 (the
+// same, forward: 304 us, 310 with 256); all of 16 x 32 x 2048 x 128, window 1024: 590 and 1710 us -> 790 and 1963.
+static inline int sink_together(int groups, int per, int at_once) { return std::min(groups, 8 * std::max(1, (at_once + per - 1) / per)); }
+
+// A workgroup's 128 queries.  A head's last queries, which have the longest lists, come first.
 struct QueryTile {
     int b, hk, h, q0;
     __device__ __forceinline__ explicit QueryTile(const SinkParams &p) {
-        const int nt = (p.Sq + 127) / 128, idx = (int)(blockIdx.x & 7) * p.per_xcd + (int)(blockIdx.x >> 3);
-        q0 = b = hk = h = -1;
-        if (idx >= p.B * p.H * nt) return;
-        const int run = idx / nt, group = run / p.G;
-        hk = group / p.B;
-        b = group - hk * p.B;
-        h = hk * p.G + run - group * p.G;
-        q0 = (nt - 1 - (idx - run * nt)) * 128;
+        const Turn turn(p);
+        const int nt = (p.Sq + 127) / 128, down = turn.item / p.G;
+        b = turn.b;
+        hk = turn.hk;
+        h = hk * p.G + turn.item - down * p.G;
+        q0 = (nt - 1 - down) * 128;
     }
 };
 
@@ -148,7 +164,6 @@ __global__ void __launch_bounds__(256, D == 64 ? 4 : 2) smha_sink_fwd(const Sink
     const float NEG_INF = -__builtin_inff();
 
     const QueryTile at(p);
-    if (at.q0 < 0) return;
     const int q0 = at.q0, b = at.b, h = at.h, hk = at.hk, bh = b * p.H + h;
     const Sequence s = sequence(p, b);
     const int window = p.window, n_sink = p.n_sink;
@@ -293,7 +308,6 @@ __global__ void __launch_bounds__(256, 2) smha_sink_bwd_q(const SinkParams p) {
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = lane & 31, hh = lane >> 5;
 
     const QueryTile at(p);
-    if (at.q0 < 0) return;
     const int q0 = at.q0, b = at.b, h = at.h, hk = at.hk, bh = b * p.H + h;
     const Sequence s = sequence(p, b);
     const int window = p.window, n_sink = p.n_sink;
@@ -466,20 +480,21 @@ __global__ void __launch_bounds__(256, D == 64 && !FINE ? 3 : 2) smha_sink_bwd_k
     const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_void *)smem, stats0 = (uint32_t)(uintptr_t)(lds_void *)stats;
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = lane & 31, hh = lane >> 5;
 
-    const int per = p.n_sink_tiles * p.cut_sink + (p.n_tiles - p.n_sink_tiles) * p.cut_rest;  // items of a key head
-    const int idx = (int)(blockIdx.x & 7) * p.per_xcd + (int)(blockIdx.x >> 3);
-    if (idx >= p.B * p.Hkv * per) return;
-    const int group = idx / per, item = idx - group * per, hk = group / p.B, b = group - hk * p.B;  // (see QueryTile)
-    int tile, part, cut;
-    if (item < p.n_sink_tiles * p.cut_sink) {
+    // the sinks' tiles, then the others' last parts (which only the longest have), ..., their first
+    const Turn turn(p);
+    const int b = turn.b, hk = turn.hk, n_sinks = p.n_sink_tiles * p.cut_sink, n_rest = p.n_tiles - p.n_sink_tiles;
+    int tile, part, cut, place;  // place: of its sums
+    if (turn.item < n_sinks) {
         cut = p.cut_sink;
-        tile = item / cut;
-        part = item - tile * cut;
+        part = turn.item / p.n_sink_tiles;
+        tile = turn.item - part * p.n_sink_tiles;
+        place = tile * cut + part;
     } else {
         cut = p.cut_rest;
-        const int rest = item - p.n_sink_tiles * p.cut_sink;
-        tile = p.n_sink_tiles + rest / cut;
-        part = rest % cut;
+        const int at = turn.item - n_sinks, turns = at / n_rest;
+        part = cut - 1 - turns;
+        place = n_sinks + (at - turns * n_rest) * cut + part;
+        tile = p.n_sink_tiles + at - turns * n_rest;
     }
     const Sequence s = sequence(p, b);
     const int window = p.window, n_sink = p.n_sink, k0 = tile * 128;
@@ -635,7 +650,7 @@ __global__ void __launch_bounds__(256, D == 64 && !FINE ? 3 : 2) smha_sink_bwd_k
         return;
     }
     // [item][dV, dK][wave][4 accumulators][lane][4]
-    float *const mine = p.parts + ((int64_t)idx * 2 * 4 + w) * (C / 8) * 256 + lane * 4;
+    float *const mine = p.parts + (((int64_t)(hk * p.B + b) * p.per + place) * 2 * 4 + w) * (C / 8) * 256 + lane * 4;
 #pragma unroll
     for (int i = 0; i < C / 8; ++i) {
         *reinterpret_cast<f32x4 *>(mine + i * 256) = f32x4{dv[i / 4][4 * (i % 4)], dv[i / 4][4 * (i % 4) + 1], dv[i / 4][4 * (i % 4) + 2], dv[i / 4][4 * (i % 4) + 3]};
@@ -650,7 +665,6 @@ __global__ void __launch_bounds__(256) smha_sink_sum(const SinkParams p) {
     const int tile_at = (int)blockIdx.x >> 3, w = (int)blockIdx.x & 3, is_k = ((int)blockIdx.x >> 2) & 1;
     const int tiles = p.cut_rest > 1 ? p.n_tiles : p.n_sink_tiles;
     const int bh = tile_at / tiles, tile = tile_at - bh * tiles, b = bh / p.Hkv, hk = bh - b * p.Hkv;
-    const int per = p.n_sink_tiles * p.cut_sink + (p.n_tiles - p.n_sink_tiles) * p.cut_rest;
     const bool sink = tile < p.n_sink_tiles;
     const int cut = sink ? p.cut_sink : p.cut_rest;
     const int item = sink ? tile * cut : p.n_sink_tiles * p.cut_sink + (tile - p.n_sink_tiles) * cut;
@@ -660,7 +674,7 @@ __global__ void __launch_bounds__(256) smha_sink_sum(const SinkParams p) {
     uint16_t *const out = is_k ? p.dK + b * p.dks.b + hk * p.dks.h : p.dV + b * p.dvs.b + hk * p.dvs.h;
     const int64_t pitch = is_k ? p.dks.s : p.dvs.s;
     const float factor = is_k ? p.scale : 1.f;
-    const float *const from = p.parts + (((int64_t)(hk * p.B + b) * per + item) * 8 + is_k * 4 + w) * (C / 8) * 256;
+    const float *const from = p.parts + (((int64_t)(hk * p.B + b) * p.per + item) * 8 + is_k * 4 + w) * (C / 8) * 256;
     for (int i = threadIdx.x; i < C / 8 * 64; i += 256) {
         f32x4 sum = {0.f, 0.f, 0.f, 0.f};
         for (int c0 = 0; c0 < parts; c0 += 4) {
@@ -716,19 +730,21 @@ static smha_status_t sink_params(SinkParams &sp, int B, int H, int Hkv, int Sq, 
     return SMHA_OK;
 }
 
-// How dK and dV are cut.  512 workgroups fit the chip, and a part costs 8 D 128 bytes of traffic: about one part for each of them evens out
-// the load, fewer leave units idle, more are slower again.  A tile with sinks is its queries' only in one or two of its waves, whose steps
-// are short: its parts are a little longer.  us of a backward pass, with tiles cut into 1, 2, 4 and 8 parts (as many for those with sinks as were
-// best): 4 x 12 x 1537 x 80, window 256: 96, 110, 133, 216 (here 1); 2 x 16 on 4 x 4096 x 128, window 1024: 293, 292, 300, 324 (2); 1 x 32 on 8 x 4096 x
-// 64, window 512: 151, 136, 135, 139 (2); 1 x 8 on 1 x 8192 x 128, window 1024: 371, 240, 218, 222 (7); 1 x 16 on 4 x 2000 x 96, window 300: 97, 77, 71, 74 (6);
-// 1 x 20 on 4 x 6000 x 128, all before: 1355, 932, 879, 915 (5).
+// How dK and dV are cut.  512 workgroups fit the chip, and a part costs 8 D 128 bytes of traffic: parts of a little more than a 512th of all steps
+// even out the load, longer ones leave units idle, shorter ones are slower again.  `all` counts every tile of a window as a whole one; without a
+// window tiles differ more and may be longer, since the longest begin first.  A tile with sinks is its queries' only in one or two of its
+// waves, whose steps are short: its parts are a little longer.  us of a backward pass, parts of 0.7, 1, 1.25, 1.5 and 2 of a 512th of the true steps at most: 2 x 16 on
+// 4 x 4096 x 128, window 1024: 273, 282, 258, 264, 294; 1 x 32 on 8 x 4096 x 64, window 512: 121, 119, 118, 126, 124; 1 x 8 on 1 x 8192 x 128, window 1024: 177, 188, 160,
+// 163, 174 (359 whole); all before: 1 x 20 on 4 x 6000 x 128: 650, 713, 633, 654, 725 (1130 whole); 2 x 32 on 8 x 4096 x 128: 931, 989, 953, 948, 1002; 3 x
+// 10 on 5 x 3000 x 128: 296, 309, 296, 288, 307; 7 x 12 x 1000 x 64: 89, 86, 85, 72, 72.
 static void sink_cuts(SinkParams &sp) {
     const int64_t nq = (sp.Sq + 31) / 32;
     const int64_t near = std::min<int64_t>(nq, (sp.window + 127 + 31) / 32 + 1);
     sp.n_tiles = (sp.Sk + 127) / 128;
     sp.n_sink_tiles = sp.window < sp.Sk ? (sp.n_sink + 127) / 128 : 0;
     const int64_t all = (int64_t)sp.B * sp.Hkv * sp.G * (sp.n_sink_tiles * nq + (sp.n_tiles - sp.n_sink_tiles) * (sp.window < sp.Sk ? near : (nq + 1) / 2));
-    sp.chunk_rest = (int)std::max<int64_t>(8, (all + 447) / 448);
+    const int64_t parts = sp.window < sp.Sk ? 448 : 341;
+    sp.chunk_rest = (int)std::max<int64_t>(8, (all + parts - 1) / parts);
     sp.chunk_sink = (int)std::max<int64_t>(12, (all + 399) / 400);
     sp.cut_sink = (int)((nq * sp.G + sp.chunk_sink - 1) / sp.chunk_sink);
     sp.cut_rest = (int)((near * sp.G + sp.chunk_rest - 1) / sp.chunk_rest);
@@ -754,19 +770,21 @@ static bool fine_ds(const SinkParams &sp) { const int64_t queries = (int64_t)sp.
 static int sink_width(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : d <= 96 ? 96 : 128; }
 
 template <int D, int C, bool BF16> static hipError_t launch_sink_fwd(SinkParams &sp, hipStream_t stream) {
-    const int64_t items = (int64_t)sp.B * sp.H * ((sp.Sq + 127) / 128);
-    sp.per_xcd = (int)((items + 7) / 8);
-    hipLaunchKernelGGL((smha_sink_fwd<D, C, BF16>), dim3(8 * sp.per_xcd), dim3(256), 0, stream, sp);
+    sp.per = sp.G * ((sp.Sq + 127) / 128);
+    sp.together = sink_together(sp.B * sp.Hkv, sp.per, 128);
+    hipLaunchKernelGGL((smha_sink_fwd<D, C, BF16>), dim3((unsigned)(sp.B * sp.Hkv * sp.per)), dim3(256), 0, stream, sp);
     return hipGetLastError();
 }
 
 template <int D, int C, bool BF16, bool FINE> static hipError_t launch_sink_bwd(SinkParams &sp, hipStream_t stream) {
-    sp.per_xcd = (int)(((int64_t)sp.B * sp.H * ((sp.Sq + 127) / 128) + 7) / 8);
-    hipLaunchKernelGGL((smha_sink_bwd_q<D, C, BF16, FINE>), dim3(8 * sp.per_xcd), dim3(256), 0, stream, sp);
+    sp.per = sp.G * ((sp.Sq + 127) / 128);
+    sp.together = sink_together(sp.B * sp.Hkv, sp.per, 128);
+    hipLaunchKernelGGL((smha_sink_bwd_q<D, C, BF16, FINE>), dim3((unsigned)(sp.B * sp.Hkv * sp.per)), dim3(256), 0, stream, sp);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    sp.per_xcd = (int)((sink_items(sp) + 7) / 8);
-    hipLaunchKernelGGL((smha_sink_bwd_kv<D, C, BF16, FINE>), dim3(8 * sp.per_xcd), dim3(256), 0, stream, sp);
+    sp.per = (int)(sink_items(sp) / (sp.B * sp.Hkv));
+    sp.together = sink_together(sp.B * sp.Hkv, sp.per, 256);
+    hipLaunchKernelGGL((smha_sink_bwd_kv<D, C, BF16, FINE>), dim3((unsigned)(sp.B * sp.Hkv * sp.per)), dim3(256), 0, stream, sp);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     if (sp.cut_sink > 1 || sp.cut_rest > 1) hipLaunchKernelGGL((smha_sink_sum<C, BF16>), dim3((unsigned)(8 * sp.B * sp.Hkv * (sp.cut_rest > 1 ? sp.n_tiles : sp.n_sink_tiles))), dim3(256), 0, stream, sp);
     return hipGetLastError();
