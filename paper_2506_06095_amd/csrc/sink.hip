@@ -154,6 +154,8 @@ __device__ __forceinline__ void load_operand(u32x4 (&f)[C / 16], const uint16_t 
 // queries do not see, and forms masks only on tiles that they see in part.
 // P is rounded to the inputs' type for the second product: half a step, 2^-9 (bfloat16) or 2^-12 (binary16) of each weight, independent
 // from weight to weight, which leaves the output as far off as its own rounding does.  Sums and statistics are 32 bits.
+// Bound by power: 1 x 32 on 8 x 8192 x 128, window 4096, 128 sinks: 435 us, matrix pipes busy half of the cycles at 2.0 GHz (55 % in a large library
+// product).  Waves in the mixed phase (masks, exponentials, second product) go first.
 template <int D, int C, bool BF16>
 __global__ void __launch_bounds__(256, D == 64 ? 4 : 2) smha_sink_fwd(const SinkParams p) {
     constexpr int NS = C / 16, NDT = C / 32, TB = 64 * D * 2;
@@ -300,6 +302,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 4 : 2) smha_sink_fwd(const Sink
 // delta from the rounded output alone is as far off as dS is by its own rounding: dQ and dK 1.52 times as far from 64 bits as an evaluation in
 // 32 bits that is rounded once, 1.42 times with what the rounding left out.
 // dS is rounded to the inputs' type for the product with K, as P is in the forward; FINE (see fine_ds): its rounding error is multiplied too.
+// 575 us for the forward's case above, matrix pipes busy 59 %.
 template <int D, int C, bool BF16, bool FINE>
 __global__ void __launch_bounds__(256, 2) smha_sink_bwd_q(const SinkParams p) {
     constexpr int NS = C / 16, NDT = C / 32, TB = 64 * D * 2, PF = C == 128 ? 6 : 4;
@@ -468,8 +471,8 @@ __device__ __forceinline__ int parts_of(int steps, int cut, int chunk) { return 
 // dK and dV: four waves of 32 keys each over 32-query tiles of Q and dO (and their lse and delta) in LDS, two of each.  A lane owns a key.
 // At 128 columns a wave holds 128 registers of dK and dV; V's 32 beside them leave room for operands that are requested four products
 // ahead, K's do not, and so K stays in LDS (with both in registers every product waited for its operand, and what had spilled was waited for
-// with the tile in flight: 1090 us for 1 x 32 x 8192 x 128, window 4096).  The exponentials run under the product that gives dP, the rest of
-// dS under the one that gives dV.
+// with the tile in flight: 1090 us for the case above, 860 so, matrix pipes busy 49 %).  The exponentials run under the product that gives
+// dP, the rest of dS under the one that gives dV.
 // A tile's steps (its queries, head by head) may be cut into parts that other workgroups take: the sinks' tiles are seen by every
 // query, and few key heads would leave most of the chip idle.  Parts go to memory in 32 bits and are added in order by smha_sink_sum.
 template <int D, int C, bool BF16, bool FINE>
