@@ -384,8 +384,8 @@ smha_status_t smha_sink_backward(const void *Q, const void *K, const void *V, co
  * over the chip whatever the lengths are.  The result does not depend on the order in which workgroups run.  Keys and values before every
  * token's window, past the length and past Sk are never read into a result; those that some token sees have to be finite (a NaN there may reach
  * the sequence's other tokens).
- * workspace: device, 16-byte aligned, smha_cache_workspace bytes or more; the call's alone until it has run.  (weigh: nonzero with
- * weights: 4 H T Sk bytes a sequence more.)
+ * workspace: device, 16-byte aligned, smha_cache_workspace bytes or more (0, and then NULL will do, where there are few
+ * keys); the call's alone until it has run.  (weigh: nonzero with weights: 4 H T Sk bytes a sequence more.)
  * Errors as for smha_sink_forward. */
 smha_status_t smha_cache_workspace(int B, int H, int Hkv, int T, int Sk, int P, int d, int window, int n_sink, int weigh,
                                    size_t *need);

@@ -1018,8 +1018,8 @@ static smha_status_t cache_params(CacheParams &cp, CacheLayout &at, int B, int H
     if (most + 8 >= (1 << 24)) return SMHA_ERR_UNSUPPORTED;
     const int64_t places = (cp.wide ? 4 : 1) * (int64_t)cp.prefix_segs + own_segs;
     cp.score_pitch = (Sk + 31) / 32 * 32;
-    if (cp.direct) {  // (nothing is kept: a size for callers that allocate what they are told)
-        at.total = 16;
+    if (cp.direct) {  // (nothing is kept)
+        at.total = 0;
         return SMHA_OK;
     }
     at.info = 0;
@@ -1066,12 +1066,12 @@ extern "C" smha_status_t smha_cache_forward(const void *Q, const void *K, const 
                                             const int64_t q_strides[3], const int64_t k_strides[3], const int64_t v_strides[3], const int64_t pk_strides[2],
                                             const int64_t pv_strides[2], const int64_t o_strides[3], const int64_t w_strides[2], int window, int n_sink, float scale,
                                             void *workspace, size_t workspace_bytes, void *hip_stream) {
-    if (!Q || !K || !V || !O || !lengths || !workspace || (P > 0 && (!PK || !PV))) return SMHA_ERR_INVALID_ARG;
+    if (!Q || !K || !V || !O || !lengths || (P > 0 && (!PK || !PV))) return SMHA_ERR_INVALID_ARG;
     CacheParams cp{};
     CacheLayout at{};
     const smha_status_t st = cache_params(cp, at, B, H, Hkv, T, Sk, P, d, dtype, window, n_sink, weights != nullptr);
     if (st != SMHA_OK) return st;
-    if (workspace_bytes < at.total) return SMHA_ERR_INVALID_ARG;
+    if (workspace_bytes < at.total || (at.total && !workspace)) return SMHA_ERR_INVALID_ARG;
     if (((uintptr_t)Q | (uintptr_t)K | (uintptr_t)V | (uintptr_t)O | (uintptr_t)workspace | (P ? (uintptr_t)PK | (uintptr_t)PV : 0)) & 15) return SMHA_ERR_UNSUPPORTED;
     if (!cache_strides_fit(q_strides, T, d) || !cache_strides_fit(k_strides, Sk, d) || !cache_strides_fit(v_strides, Sk, d) || !cache_strides_fit(o_strides, T, d))
         return SMHA_ERR_UNSUPPORTED;

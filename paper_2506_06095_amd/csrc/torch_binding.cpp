@@ -333,10 +333,11 @@ PyObject *cache_attention(PyObject *, PyObject *const *args, Py_ssize_t n) {
     smha_status_t st = entries.cache_workspace(B, H, Hkv, T, Sk, P, d, window, n_sink, weights != nullptr, &need);
     if (st != SMHA_OK) return PyLong_FromLong((long)st);
     const at::AutoGradMode off(false);
-    at::Tensor o = packed_like(q), ws = at::empty({(int64_t)need}, q.options().dtype(at::kByte));
+    at::Tensor o = packed_like(q), ws;
+    if (need) ws = at::empty({(int64_t)need}, q.options().dtype(at::kByte));
     st = entries.cache_forward(q.data_ptr(), k.data_ptr(), v.data_ptr(), pk, pv, o.data_ptr(), weights, lengths, B, H, Hkv, T, Sk, P, d,
                                (smha_dtype_t)code_of(q.scalar_type()), qs.ptr, ks.ptr, vs.ptr, nullptr, nullptr, nullptr, nullptr, window, n_sink,
-                               (float)PyFloat_AS_DOUBLE(args[9]), ws.data_ptr(), need, c10::hip::getCurrentHIPStream(q.device().index()).stream());
+                               (float)PyFloat_AS_DOUBLE(args[9]), need ? ws.data_ptr() : nullptr, need, c10::hip::getCurrentHIPStream(q.device().index()).stream());
     if (st != SMHA_OK) return PyLong_FromLong((long)st);
     if (weights) written(weights_t);
     return THPVariable_Wrap(std::move(o));

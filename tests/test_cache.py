@@ -468,8 +468,10 @@ def test_refusals():
         return lib.smha_cache_forward(q, ptr, ptr, pk, pk, ptr, None, lengths, B, H, Hkv, T, Sk, P, d, dtype, None, s, None, None, None, out, None, window, n_sink,
                                       0.0, ws, size, None)
 
-    assert forward(q=None) == invalid and forward(lengths=None) == invalid and forward(ws=None) == invalid and forward(size=15) == invalid
+    assert forward(q=None) == invalid and forward(lengths=None) == invalid and forward(Sk=4000, ws=None) == invalid
     assert forward(Sk=4000, size=1000) == invalid
+    few = C.c_size_t(7)
+    assert lib.smha_cache_workspace(1, 4, 2, 1, 8, 0, 64, 0, 0, 0, C.byref(few)) == 0 and few.value == 0  # (few keys: nothing to keep)
     assert forward(B=0) == invalid and forward(T=0) == invalid and forward(P=-1) == invalid and forward(P=5) == invalid and forward(window=-1) == invalid
     assert forward(H=3) == shape
     assert forward(d=136) == unsupported and forward(d=20) == unsupported and forward(dtype=2) == unsupported
@@ -513,4 +515,4 @@ def test_refusals_of_the_binding():
     with pytest.raises(smha.SmhaError):
         smha.cache_attention(q, k, v, n, prefix=prefix, window=4)
     with pytest.raises(smha.SmhaError):
-        smha.cache_attention(q, k, v, n, workspace=torch.empty(8, dtype=torch.uint8, device="cuda"))
+        smha.cache_attention(*make(2, 4, 2, 1, 2000, 64)[:3], n, workspace=torch.empty(8, dtype=torch.uint8, device="cuda"))
