@@ -725,11 +725,22 @@ __global__ void __launch_bounds__(1024) smha_cache_select(const EvictParams p) {
             }
         }
     }
-    // (all slots before the end: those that are freed are written again below)
-    if (Wo != W)
-        for (int i = threadIdx.x; i < end; i += 1024) Wo[i] = W[i];
-    if (Po != P)
-        for (int i = threadIdx.x; i < end; i += 1024) Po[i] = P[i];
+    // All slots before the end (those that are freed are written again below): from the registers where most stay, else only the first waves have
+    // some.  (128 heads of 20000 keys to 19000: 46.2 us by reading again, 42.0 so; 32 of 32768 to 2048: 41.9, 45.6.)
+    if (KPT > 0 && len > p.budget && end > len / 2) {
+#pragma unroll
+        for (int i = 0; i < HELD; ++i) {
+            if (i < n && base + 64 * i < end) {
+                if (Wo != W) Wo[base + 64 * i] = __builtin_bit_cast(float, held[i]);
+                if (Po != P) Po[base + 64 * i] = held_p[i];
+            }
+        }
+    } else {
+        if (Wo != W)
+            for (int i = threadIdx.x; i < end; i += 1024) Wo[i] = W[i];
+        if (Po != P)
+            for (int i = threadIdx.x; i < end; i += 1024) Po[i] = P[i];
+    }
     // What lies past the new end; and the new length.
     auto finish = [&]() __attribute__((always_inline)) {
         for (int i = end + threadIdx.x; i < p.Sk; i += 1024) {
