@@ -684,9 +684,9 @@ __device__ __forceinline__ void before_and_all(const int *numbers, int lane, int
 
 // An order of 32-bit floats as unsigned numbers, NaN with the lowest, -0 with +0.
 __device__ __forceinline__ uint32_t ordered(float x) {
-    if (!(x == x)) return 0x007FFFFFu;  // -inf's
-    const uint32_t u = __builtin_bit_cast(uint32_t, x + 0.0f);
-    return u & 0x80000000u ? ~u : u | 0x80000000u;
+    const int u = __builtin_bit_cast(int, x + 0.0f);
+    const uint32_t o = (uint32_t)(u ^ (u >> 31 | (int)0x80000000u));
+    return x == x ? o : 0x007FFFFFu;  // -inf's
 }
 
 // One workgroup of 16 waves a key head.  Wave w holds the keys of slots (w n + i) 64 + lane as unsigned numbers that order them, so that a lane's
@@ -718,6 +718,8 @@ __global__ void __launch_bounds__(1024) smha_cache_select(const EvictParams p) {
 #pragma unroll
             for (int i = 0; i < KPT; ++i) {
                 const int slot = min(base + 64 * i, len - 1);  // (past the end: the last one again)
+                held[i] = 0u;
+                held_p[i] = INT32_MIN;
                 if (i < n) {
                     held[i] = __builtin_bit_cast(uint32_t, W[slot]);
                     held_p[i] = P[slot];
@@ -725,6 +727,7 @@ __global__ void __launch_bounds__(1024) smha_cache_select(const EvictParams p) {
             }
         }
     }
+    auto beyond = [&](int i) __attribute__((always_inline)) { return i % (KPT < 8 ? 1 : KPT < 16 ? 2 : 4) == 0 && i >= n; };  // where a lane has no more keys (those it holds past them are 0)
     // All slots before the end (those that are freed are written again below): from the registers where most stay, else only the first waves have
     // some.  (128 heads of 20000 keys to 19000: 46.2 us by reading again, 42.0 so; 32 of 32768 to 2048: 41.9, 45.6.)
     if (KPT > 0 && len > p.budget && end > len / 2) {
@@ -757,8 +760,7 @@ __global__ void __launch_bounds__(1024) smha_cache_select(const EvictParams p) {
     int newest = INT32_MIN;
     if constexpr (KPT > 0) {
 #pragma unroll
-        for (int i = 0; i < KPT; ++i)
-            if (i < n) newest = max(newest, held_p[i]);
+        for (int i = 0; i < KPT; ++i) newest = max(newest, held_p[i]);
     } else {
         for (int i = threadIdx.x; i < len; i += 1024) newest = max(newest, P[i]);
     }
@@ -770,19 +772,25 @@ __global__ void __launch_bounds__(1024) smha_cache_select(const EvictParams p) {
     // positions past this stay, whatever their account; where there are none so low, all
     const bool all_young = (int64_t)newest - p.recent < INT32_MIN;
     const int young = all_young ? INT32_MIN : newest - p.recent;
+    const int limit = min(len, (w + 1) * 64 * n);  // the wave's slots end here
     auto key_from = [&](int slot, float x, int32_t at) __attribute__((always_inline)) -> uint32_t {
-        return slot >= len ? 0u : all_young || at > young ? 0xFF800000u : ordered(x);  // (0: below every live key's)
+        const uint32_t o = ordered(x), k = (all_young | (at > young)) ? 0xFF800000u : o;
+        return slot < limit ? k : 0u;  // (0: below every live key's, which are in the fourth bin or later)
     };
     if constexpr (KPT > 0) {
 #pragma unroll
-        for (int i = 0; i < KPT; ++i)
-            if (i < n) held[i] = key_from(base + 64 * i, __builtin_bit_cast(float, held[i]), held_p[i]);
+        for (int i = 0; i < KPT; ++i) {
+            if (beyond(i)) break;
+            held[i] = key_from(base + 64 * i, __builtin_bit_cast(float, held[i]), held_p[i]);
+        }
     }
     auto each = [&](auto &&f) __attribute__((always_inline)) {
         if constexpr (KPT > 0) {
 #pragma unroll
-            for (int i = 0; i < KPT; ++i)
-                if (i < n) f(held[i]);
+            for (int i = 0; i < KPT; ++i) {
+                if (beyond(i)) break;
+                f(held[i]);
+            }
         } else {
             for (int i = 0; i < n; ++i) {
                 const int slot = base + 64 * i;
@@ -797,16 +805,15 @@ __global__ void __launch_bounds__(1024) smha_cache_select(const EvictParams p) {
     for (int pass = 0; pass < 3; ++pass) {
         const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, width = pass == 2 ? 10 : 11;
         each([&](uint32_t k) __attribute__((always_inline)) {
-            // (what is known of `least` is not zero: no live key's is, and the others' numbers do not match it)
-            const bool in = pass == 0 ? k != 0 : (k >> (shift + width)) == (least >> (shift + width));
-            const uint64_t who = __builtin_amdgcn_ballot_w64(in);
-            if (who == 0) return;
+            // (what is known of `least` is not zero: no live key's is, and the others' numbers do not match it; at first they are counted in bin 0)
+            const bool in = pass == 0 || ((k ^ least) >> (shift + width)) == 0;
+            if (__builtin_amdgcn_ballot_w64(in) == 0) return;
             const int bin = (int)(k >> shift) & ((1 << width) - 1);
-            const int one = __builtin_amdgcn_readlane(bin, __builtin_ctzll(who));
-            if (__builtin_amdgcn_ballot_w64(in && bin != one) == 0) {
-                if (lane == 0) atomicAdd(&bins[one], __builtin_popcountll(who));
-            } else if (in) {
-                atomicAdd(&bins[bin], 1);
+            if (in) {
+                const int one = __builtin_amdgcn_readfirstlane(bin);
+                const uint64_t other = __builtin_amdgcn_ballot_w64(bin != one);
+                if (other != 0) atomicAdd(&bins[bin], 1);
+                else if (const uint64_t who = __builtin_amdgcn_ballot_w64(true); lane == __builtin_ctzll(who)) atomicAdd(&bins[one], __builtin_popcountll(who));
             }
         });
         __syncthreads();
@@ -841,7 +848,8 @@ __global__ void __launch_bounds__(1024) smha_cache_select(const EvictParams p) {
         for (int i = 0; i < GROUP; ++i) {
             uint32_t k = 0u;
             if constexpr (KPT > 0) {
-                if (i < n) k = held[i];
+                if (beyond(i)) break;
+                k = held[i];
             } else {
                 const int slot = base + 64 * (i0 + i);
                 if (i0 + i < n && slot < len) k = key_from(slot, W[slot], P[slot]);
