@@ -693,7 +693,8 @@ __device__ __forceinline__ uint32_t ordered(float x) {
 // and a register's order is the slots' order.  The budget-th largest is found by counting, 11, 11 and 10 bits at a time, in a
 // histogram in LDS (11 bits of a float are a quarter of an octave: lanes of a wave meet in few bins but seldom all in one, and where
 // they do one of them counts for all); of the keys that equal it the first slots stay.  What stays past the new end goes, in
-// order, where keys before it left.  128 heads of 4352 keys 12.6 us, 32 of 32768 30.  (Counting with ballots, two bits at a time: 26.5 and 110.)
+// order, where keys before it left.  32 heads of 32768 keys 27 us.  (Counting with ballots, two bits at a time: 110;
+// with a branch for each of a key's conditions: 30.)
 // WHOLE: the rows are moved here too, which saves a launch where few move (evict_whole); their lists then take the histogram's place in LDS.
 constexpr int kWholeMoves = 512;
 template <int KPT, bool WHOLE>
@@ -729,7 +730,8 @@ __global__ void __launch_bounds__(1024) smha_cache_select(const EvictParams p) {
     }
     auto beyond = [&](int i) __attribute__((always_inline)) { return i % (KPT < 8 ? 1 : KPT < 16 ? 2 : 4) == 0 && i >= n; };  // where a lane has no more keys (those it holds past them are 0)
     // All slots before the end (those that are freed are written again below): from the registers where most stay, else only the first waves have
-    // some.  (128 heads of 20000 keys to 19000: 46.2 us by reading again, 42.0 so; 32 of 32768 to 2048: 41.9, 45.6.)
+    // some.  (128 heads of 20000 keys to 19000: 46.2 us by reading again, 42.0 so; 32 of 32768 to
+    // 2048: 41.9, 45.6.)
     if (KPT > 0 && len > p.budget && end > len / 2) {
 #pragma unroll
         for (int i = 0; i < HELD; ++i) {
@@ -1119,9 +1121,9 @@ extern "C" smha_status_t smha_cache_forward(const void *Q, const void *K, const 
     return e == hipSuccess ? SMHA_OK : SMHA_ERR_HIP;
 }
 
-// Whether a head's own workgroup moves its rows.  us of a call by two kernels and by one: 16 x 8 heads of 4352 keys to 4096, x 128: 17.5, 15.3; 2 heads
-// of 1100 to 1024: 9.8, 8.1; 32 heads of 8192 to 7936, 7680, 7168: 16.7, 17.4, 19.1 and 14.9, 17.1, 23.3 (one compute unit moves 1 MB);
-// 512 heads of 8192 to 7680: 76.6, 72.7.  Lengths that are written where they are read need the second kernel: a sequence's other heads may still
+// Whether a head's own workgroup moves its rows.  us of a call by two kernels and by one: 128 heads of 4352 keys to 4096, x 128: 17.2, 15.0; 2 heads
+// of 1100 to 1024: 9.6, 7.9; 1024 of 2176 to 2048: 44.7, 35.6; 32 of 8192 to 7936 and 7680: 15.9, 16.3 and 13.8, 16.2; to 7168 (one compute unit
+// moves 1 MB, if more than the limit were allowed): 19.1, 23.3.  Lengths that are written where they are read need the second kernel: a sequence's other heads may still
 // have to read them.
 static bool evict_whole(const EvictParams &ep) { return ep.moves <= kWholeMoves && ep.len_out != ep.lengths; }
 
