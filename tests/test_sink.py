@@ -357,6 +357,30 @@ def test_scales(scale):
 
 
 @pytest.mark.gpu
+def test_a_large_batch_is_its_parts():
+    """More key heads than the order of workgroups takes in turn at once (280 of 10 tiles each): as in ten calls.  dK and dV may be summed in other
+    parts there: they differ by a rounding each, and by the sums' own, under 1e-5 of at most 1200 products of a few units."""
+    B, each = 70, 7
+    q, k, v, g = tensors(B, 4, 4, 1200, 1200, 64, torch.bfloat16)
+    n = int32([1200 - 13 * (i % 50) for i in range(B)])
+    assert each * 4 * 1200 > 8192  # (dS is rounded in both)
+
+    def step(at):
+        x = [t[at].detach().requires_grad_() for t in (q, k, v)]
+        out = smha.sink_attention(*x, 100, 2, lengths=n[at].contiguous())
+        return (out, *torch.autograd.grad(out, x, g[at]))
+
+    whole = step(slice(None))
+    for i in range(0, B, each):
+        at = slice(i, i + each)
+        for name, a, b in zip(("out", "dq", "dk", "dv"), whole, step(at)):
+            if name in ("out", "dq"):
+                assert torch.equal(a[at], b), (name, i)
+            else:
+                assert bool(((a[at].float() - b.float()).abs() <= 2 * 2.0 ** -8 * b.float().abs() + 1e-2).all()), (name, i)
+
+
+@pytest.mark.gpu
 def test_two_passes_at_once():
     """On two streams, whose kernels and workspaces may overlap in time."""
     inputs = [tensors(2, 8, 2, 700, 700, 128, torch.bfloat16, seed=seed) for seed in (1, 2)]
