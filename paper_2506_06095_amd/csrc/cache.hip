@@ -262,7 +262,6 @@ __device__ __forceinline__ void prefix_wide(const CacheParams &p, const Segment 
 // other and writes the output: nothing is counted, cut or joined, and the call is one launch.
 enum CacheForm { kCut, kWide, kDirect };
 constexpr int cache_groups(int D, int form) { return D == 128 ? 2 : form == kWide ? 3 : 4; }
-constexpr int kDirectTiles = 16;
 template <int D, bool BF16, bool WEIGH, int FORM>
 __global__ void __launch_bounds__(256, cache_groups(D, FORM)) smha_cache_part(const CacheParams p) {
     constexpr int NS = D / 16, NDT = D / 32, CPR = D / 8, LPT = CPR / 2, RPL = 64 / CPR, NO = 16 / RPL, TB = 32 * D * 2;
@@ -1000,6 +999,13 @@ static Strides cache_strides(const int64_t *s, int64_t heads, int64_t rows, int 
     return s ? Strides{s[0], s[1], s[2]} : Strides{heads * rows * d, rows * d, d};
 }
 
+// Tiles of a group up to which a workgroup takes it whole.  Cutting costs a second launch and shares out what one workgroup would read alone (0.37 us a
+// tile); where groups fill the chip by themselves there is little to share.  us of a call, direct and cut: 2 groups x 64 of 500, 700, 1000 and 1500
+// keys: 8.8, 8.9, 10.7, 14.1 and 12.2 (replayed from a graph: 7.0, 8.4, 10.3, 13.6 and 8.5); 32 x 128 of 500, 700, 1000: 9.9, 12.1, 14.8 and 12.2; 128 x 128
+// of 1000: 17.3, 19.4; 512 x 128 of 700, 1000 and 1500: 30, 42, 70 and 35, 47, 75, of 30 to 100 % of those lengths 23, 30, 43 and 31, 37, 50.  No more than 48: with
+// one long sequence among short ones it is the longest that counts.  (A prefix that many groups read is better shared.)
+static int64_t direct_tiles(int d, int P, int64_t groups) { return std::min<int64_t>(48, (d <= 64 ? 24 : 16) + (P ? 0 : groups / 8)); }
+
 struct CacheLayout {
     size_t info, stats, parts, scores, total;
 };
@@ -1018,7 +1024,7 @@ static smha_status_t cache_params(CacheParams &cp, CacheLayout &at, int B, int H
     cp.n_sink = std::min(n_sink, Sk);
     const int64_t rows = (int64_t)cp.G * T, own_tiles = (rows + 31) / 32;
     const int64_t own_tiles_most = std::min<int64_t>((Sk + 31) / 32, ((int64_t)cp.window + cp.n_sink + T) / 32 + 3);
-    cp.direct = !weigh && own_tiles_most + (P + 31) / 32 <= kDirectTiles;
+    cp.direct = !weigh && own_tiles_most + (P + 31) / 32 <= direct_tiles(d, P, B * Hkv * own_tiles);
     cp.wide = !cp.direct && P > 0 && B * rows > 64;  // (one or two tiles of 32 rows: reading the keys once or twice by waves on their own fills the chip better)
     const int64_t prefix_tiles = !P ? 0 : cp.wide ? (B * rows + 127) / 128 : (B * rows + 31) / 32;
     const int64_t groups = (int64_t)Hkv * (prefix_tiles + B * own_tiles);

@@ -84,7 +84,10 @@ CASES = [
     (4, 12, 12, 1, 96, 64, 0, 0, 333, [96, 20, 1, 50], "bhsd"),
     (3, 8, 2, 2, 40, 128, 0, 0, 1, [40, 1, 0], "bshd"),                 # sequences whose first token does not exist
     (40, 8, 2, 1, 70, 128, 0, 0, 5000, [(9 * i) % 71 for i in range(40)], "bhsd"),  # 160 rows on a prefix head
-    (17, 8, 1, 1, 30, 64, 0, 0, 100, list(range(1, 18)), "bhsd"),       # 136 rows: a tile of 128 and one of 8
+    (17, 8, 1, 1, 30, 64, 0, 0, 100, list(range(1, 18)), "bhsd"),
+    (17, 8, 1, 1, 30, 64, 0, 0, 1000, list(range(1, 18)), "bhsd"),      # 136 rows: a tile of 128 and one of 8
+    (70, 2, 1, 1, 2000, 64, 0, 0, 0, [(29 * i) % 2001 for i in range(70)], "bhsd"),
+    (70, 4, 4, 1, 1400, 128, 0, 0, 0, [(1400 - 21 * i) for i in range(67)] + [0, 1, 2], "bshd"),   # 280 groups of up to 44 tiles, whole
     (20, 8, 2, 3, 50, 128, 0, 0, 64, [(3 * i) % 7 for i in range(20)], "bshd"),   # of which many do not exist
     (5, 12, 1, 1, 40, 96, 0, 0, 65, [40, 1, 2, 3, 40], "bhsd"),         # 60 rows, a key past two tiles of 32
     (1, 2, 2, 1, 5, 96, 0, 0, 31, [5], "bhsd"),
