@@ -15,8 +15,10 @@
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
-#include <torch/csrc/autograd/custom_function.h>
+#include <torch/csrc/autograd/function.h>
 #include <torch/csrc/autograd/functions/basic_ops.h>
+#include <torch/csrc/autograd/functions/utils.h>
+#include <torch/csrc/autograd/saved_variable.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "smha.h"
@@ -196,31 +198,25 @@ smha_status_t run_sink_forward(const at::Tensor &q, const at::Tensor &k, const a
                                 c.window, c.n_sink, c.scale, c10::hip::getCurrentHIPStream(q.device().index()).stream());
 }
 
-struct SinkFailed {
-    smha_status_t status;
-};
-
 at::Tensor packed_like(const at::Tensor &t) { return at::empty(t.sizes(), t.options(), at::MemoryFormat::Contiguous); }
 
-struct SinkFunction : torch::autograd::Function<SinkFunction> {
-    static at::Tensor forward(torch::autograd::AutogradContext *ctx, const at::Tensor &q, const at::Tensor &k, const at::Tensor &v,
-                              const std::optional<at::Tensor> &offsets, const std::optional<at::Tensor> &lengths, int64_t window, int64_t n_sink, double scale) {
-        at::Tensor o = packed_like(q), rest = packed_like(q);
-        at::Tensor lse = at::empty({q.size(0), q.size(1), q.size(2)}, q.options().dtype(at::kFloat));
-        const smha_status_t st = run_sink_forward(q, k, v, o, lse.data_ptr<float>(), rest.data_ptr(), offsets ? offsets->data_ptr<int32_t>() : nullptr,
-                                                  lengths ? lengths->data_ptr<int32_t>() : nullptr, {(int)window, (int)n_sink, (float)scale});
-        if (st != SMHA_OK) throw SinkFailed{st};
-        ctx->save_for_backward({q, k, v, o, rest, lse, offsets.value_or(at::Tensor()), lengths.value_or(at::Tensor())});
-        ctx->saved_data["window"] = window;
-        ctx->saved_data["n_sink"] = n_sink;
-        ctx->saved_data["scale"] = scale;
-        return o;
+// The backward pass of one call.
+struct SinkBackward : torch::autograd::Node {
+    torch::autograd::SavedVariable q_, k_, v_, o_, rest_, lse_, offsets_, lengths_;
+    SinkCall call_;
+
+    std::string name() const override { return "SinkAttentionBackward"; }
+
+    void release_variables() override {
+        const std::lock_guard<std::mutex> lock(mutex_);
+        for (auto *t : {&q_, &k_, &v_, &o_, &rest_, &lse_, &offsets_, &lengths_}) t->reset_data();
     }
 
-    static torch::autograd::variable_list backward(torch::autograd::AutogradContext *ctx, const torch::autograd::variable_list &grads) {
-        const auto saved = ctx->get_saved_variables();
-        const at::Tensor &q = saved[0], &k = saved[1], &v = saved[2], &o = saved[3], &rest = saved[4], &lse = saved[5], &offsets = saved[6], &lengths = saved[7];
-        if (!grads[0].defined()) return torch::autograd::variable_list(8);
+    torch::autograd::variable_list apply(torch::autograd::variable_list &&grads) override {
+        const std::lock_guard<std::mutex> lock(mutex_);
+        if (!grads[0].defined()) return torch::autograd::variable_list(3);
+        const at::Tensor q = q_.unpack(), k = k_.unpack(), v = v_.unpack(), o = o_.unpack(shared_from_this()), rest = rest_.unpack(), lse = lse_.unpack(),
+                         offsets = offsets_.unpack(), lengths = lengths_.unpack();
         at::Tensor g = grads[0].detach(), dq, dk, dv;
         {
             const at::AutoGradMode off(false);
@@ -233,18 +229,17 @@ struct SinkFunction : torch::autograd::Function<SinkFunction> {
             dk = packed_like(k);
             dv = packed_like(v);
             const int B = (int)q.size(0), H = (int)q.size(1), Hkv = (int)k.size(1), Sq = (int)q.size(2), Sk = (int)k.size(2), d = (int)q.size(3);
-            const int window = (int)ctx->saved_data["window"].toInt(), n_sink = (int)ctx->saved_data["n_sink"].toInt();
             const c10::DeviceGuard guard(q.device());
             size_t need = 0;
-            smha_status_t st = entries.sink_workspace(B, H, Hkv, Sq, Sk, d, window, n_sink, &need);
+            smha_status_t st = entries.sink_workspace(B, H, Hkv, Sq, Sk, d, call_.window, call_.n_sink, &need);
             const Strides3 qs(q), ks(k), vs(v), ds(g);
             if (st == SMHA_OK) {
                 at::Tensor ws = at::empty({(int64_t)need}, q.options().dtype(at::kByte));
                 st = entries.sink_backward(q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), rest.data_ptr(), lse.data_ptr<float>(), g.data_ptr(), dq.data_ptr(),
                                            dk.data_ptr(), dv.data_ptr(), B, H, Hkv, Sq, Sk, d, (smha_dtype_t)code_of(q.scalar_type()), qs.ptr, ks.ptr, vs.ptr, nullptr, ds.ptr,
                                            nullptr, nullptr, nullptr, offsets.defined() ? offsets.data_ptr<int32_t>() : nullptr,
-                                           lengths.defined() ? lengths.data_ptr<int32_t>() : nullptr, window, n_sink, (float)ctx->saved_data["scale"].toDouble(),
-                                           ws.data_ptr(), need, c10::hip::getCurrentHIPStream(q.device().index()).stream());
+                                           lengths.defined() ? lengths.data_ptr<int32_t>() : nullptr, call_.window, call_.n_sink, call_.scale, ws.data_ptr(), need,
+                                           c10::hip::getCurrentHIPStream(q.device().index()).stream());
             }
             TORCH_CHECK(st == SMHA_OK, "smha_sink_backward: status ", (int)st);
         }
@@ -253,10 +248,42 @@ struct SinkFunction : torch::autograd::Function<SinkFunction> {
             for (auto &t : out) t.requires_grad_();
             out = (*std::make_shared<torch::autograd::DelayedError>("sink_attention cannot be differentiated twice", (int64_t)out.size()))(std::move(out));
         }
-        out.resize(8);
+        for (size_t i = 0; i < 3; ++i)
+            if (!task_should_compute_output(i)) out[i] = at::Tensor();
         return out;
     }
 };
+
+// The forward of a call whose gradients may be wanted: the output, or a status.
+smha_status_t sink_with_graph(const at::Tensor &q, const at::Tensor &k, const at::Tensor &v, const at::Tensor &offsets, const at::Tensor &lengths, const SinkCall &c,
+                              at::Tensor &o) {
+    using torch::autograd::SavedVariable;
+    at::Tensor rest, lse;
+    {
+        const at::AutoGradMode off(false);
+        o = packed_like(q);
+        rest = packed_like(q);
+        lse = at::empty({q.size(0), q.size(1), q.size(2)}, q.options().dtype(at::kFloat));
+        const smha_status_t st = run_sink_forward(q, k, v, o, lse.data_ptr<float>(), rest.data_ptr(), offsets.defined() ? offsets.data_ptr<int32_t>() : nullptr,
+                                                  lengths.defined() ? lengths.data_ptr<int32_t>() : nullptr, c);
+        if (st != SMHA_OK) return st;
+    }
+    const auto node = std::shared_ptr<SinkBackward>(new SinkBackward(), torch::autograd::deleteNode);
+    node->set_next_edges(torch::autograd::collect_next_edges(q, k, v));
+    node->call_ = c;
+    torch::autograd::set_history(o, node);
+    node->q_ = SavedVariable(q, false);
+    node->k_ = SavedVariable(k, false);
+    node->v_ = SavedVariable(v, false);
+    node->o_ = SavedVariable(o, true);
+    node->rest_ = SavedVariable(rest, false);
+    node->lse_ = SavedVariable(lse, false);
+    node->offsets_ = SavedVariable(offsets, false);
+    node->lengths_ = SavedVariable(lengths, false);
+    return SMHA_OK;
+}
+
+bool has_tangent(const at::Tensor &t) { return t._fw_grad(0).defined(); }
 
 // sink_attention(q, k, v, window, n_sink, offsets, lengths, scale) -> the output, a status, or None
 PyObject *sink_attention(PyObject *, PyObject *const *args, Py_ssize_t n) {
@@ -273,12 +300,9 @@ PyObject *sink_attention(PyObject *, PyObject *const *args, Py_ssize_t n) {
     const c10::DeviceGuard guard(q.device());
     at::Tensor o;
     if (at::GradMode::is_enabled() && (q.requires_grad() || k.requires_grad() || v.requires_grad())) {
-        try {
-            using Maybe = std::optional<at::Tensor>;
-            o = SinkFunction::apply(q, k, v, offsets ? Maybe(offsets_t) : Maybe(), lengths ? Maybe(lengths_t) : Maybe(), (int64_t)c.window, (int64_t)c.n_sink, PyFloat_AS_DOUBLE(args[7]));
-        } catch (const SinkFailed &e) {
-            return PyLong_FromLong((long)e.status);
-        }
+        if (has_tangent(q) || has_tangent(k) || has_tangent(v)) Py_RETURN_NONE;  // (forward mode, which the general way refuses)
+        const smha_status_t st = sink_with_graph(q, k, v, offsets_t, lengths_t, c, o);
+        if (st != SMHA_OK) return PyLong_FromLong((long)st);
     } else {
         o = packed_like(q);
         const smha_status_t st = run_sink_forward(q, k, v, o, nullptr, nullptr, offsets, lengths, c);

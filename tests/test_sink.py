@@ -13,6 +13,7 @@ import math
 import pytest
 
 torch = pytest.importorskip("torch")
+import torch.utils.checkpoint  # noqa: E402
 
 import paper_2506_06095_amd as smha  # noqa: E402
 
@@ -184,6 +185,50 @@ def test_gradients_for_some_inputs_and_no_second_derivative(monkeypatch, native)
     assert torch.equal(dq, want[0]) and torch.equal(dv, want[2])
     with pytest.raises(RuntimeError, match="twice" if native else "does not require grad"):
         dq.float().sum().backward()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("native", [True, False])
+def test_the_graph_of_a_call(monkeypatch, native):
+    """What autograd's own operators do: one backward pass unless it is kept, hooks of saved tensors, recomputation, nothing left behind, no forward mode."""
+    from paper_2506_06095_amd import sink
+    if not native:
+        monkeypatch.setattr(sink, "_call", lambda *args: None)
+    q, k, v, g = tensors(1, 2, 2, 64, 64, 64, torch.float16)
+    n = int32([50])
+    x = [t.detach().requires_grad_() for t in (q, k, v)]
+
+    def call():
+        return smha.sink_attention(*x, 16, 1, lengths=n)
+
+    out = call()
+    first = torch.autograd.grad(out, x, g, retain_graph=True)
+    assert all(torch.equal(a, b) for a, b in zip(first, torch.autograd.grad(out, x, g)))
+    with pytest.raises(RuntimeError, match="second time"):
+        torch.autograd.grad(out, x, g)
+    seen = []
+    with torch.autograd.graph.saved_tensors_hooks(lambda t: (seen.append(t.shape), t.cpu())[1], lambda t: t.cuda()):
+        out = call()
+    assert len(seen) >= 6
+    assert all(torch.equal(a, b) for a, b in zip(first, torch.autograd.grad(out, x, g)))
+    again = torch.utils.checkpoint.checkpoint(lambda *y: smha.sink_attention(*y, 16, 1, lengths=n) * 1, *x, use_reentrant=False)
+    assert all(torch.equal(a, b) for a, b in zip(first, torch.autograd.grad(again, x, g)))
+    (dk,) = torch.autograd.grad(call(), (x[1],), g)
+    assert torch.equal(dk, first[1])
+    out = call()
+    out.backward(g)
+    out = call()
+    out.backward(g)
+    assert all(torch.equal(t.grad, d + d) for t, d in zip(x, first))
+    del out, again
+    torch.cuda.synchronize()
+    before = torch.cuda.memory_allocated()
+    for _ in range(3):
+        call()  # (a graph that nothing goes back through)
+        torch.autograd.grad(call(), x, g)
+    assert torch.cuda.memory_allocated() == before
+    with torch.autograd.forward_ad.dual_level(), pytest.raises((RuntimeError, NotImplementedError)):
+        smha.sink_attention(torch.autograd.forward_ad.make_dual(x[0], g), k, v, 16, 1)
 
 
 @pytest.mark.gpu
