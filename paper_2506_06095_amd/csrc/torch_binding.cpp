@@ -200,22 +200,24 @@ smha_status_t run_sink_forward(const at::Tensor &q, const at::Tensor &k, const a
 
 at::Tensor packed_like(const at::Tensor &t) { return at::empty(t.sizes(), t.options(), at::MemoryFormat::Contiguous); }
 
+int64_t lse_bytes(const at::Tensor &q) { return (q.size(0) * q.size(1) * q.size(2) * 4 + 15) / 16 * 16; }
+
 // The backward pass of one call.
 struct SinkBackward : torch::autograd::Node {
-    torch::autograd::SavedVariable q_, k_, v_, o_, rest_, lse_, offsets_, lengths_;
+    torch::autograd::SavedVariable q_, k_, v_, o_, kept_, offsets_, lengths_;  // kept: lse, then what O's rounding left out
     SinkCall call_;
 
     std::string name() const override { return "SinkAttentionBackward"; }
 
     void release_variables() override {
         const std::lock_guard<std::mutex> lock(mutex_);
-        for (auto *t : {&q_, &k_, &v_, &o_, &rest_, &lse_, &offsets_, &lengths_}) t->reset_data();
+        for (auto *t : {&q_, &k_, &v_, &o_, &kept_, &offsets_, &lengths_}) t->reset_data();
     }
 
     torch::autograd::variable_list apply(torch::autograd::variable_list &&grads) override {
         const std::lock_guard<std::mutex> lock(mutex_);
         if (!grads[0].defined()) return torch::autograd::variable_list(3);
-        const at::Tensor q = q_.unpack(), k = k_.unpack(), v = v_.unpack(), o = o_.unpack(shared_from_this()), rest = rest_.unpack(), lse = lse_.unpack(),
+        const at::Tensor q = q_.unpack(), k = k_.unpack(), v = v_.unpack(), o = o_.unpack(shared_from_this()), kept = kept_.unpack(),
                          offsets = offsets_.unpack(), lengths = lengths_.unpack();
         at::Tensor g = grads[0].detach(), dq, dk, dv;
         {
@@ -235,7 +237,7 @@ struct SinkBackward : torch::autograd::Node {
             const Strides3 qs(q), ks(k), vs(v), ds(g);
             if (st == SMHA_OK) {
                 at::Tensor ws = at::empty({(int64_t)need}, q.options().dtype(at::kByte));
-                st = entries.sink_backward(q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), rest.data_ptr(), lse.data_ptr<float>(), g.data_ptr(), dq.data_ptr(),
+                st = entries.sink_backward(q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), static_cast<char *>(kept.data_ptr()) + lse_bytes(q), static_cast<const float *>(kept.data_ptr()), g.data_ptr(), dq.data_ptr(),
                                            dk.data_ptr(), dv.data_ptr(), B, H, Hkv, Sq, Sk, d, (smha_dtype_t)code_of(q.scalar_type()), qs.ptr, ks.ptr, vs.ptr, nullptr, ds.ptr,
                                            nullptr, nullptr, nullptr, offsets.defined() ? offsets.data_ptr<int32_t>() : nullptr,
                                            lengths.defined() ? lengths.data_ptr<int32_t>() : nullptr, call_.window, call_.n_sink, call_.scale, ws.data_ptr(), need,
@@ -258,13 +260,12 @@ struct SinkBackward : torch::autograd::Node {
 smha_status_t sink_with_graph(const at::Tensor &q, const at::Tensor &k, const at::Tensor &v, const at::Tensor &offsets, const at::Tensor &lengths, const SinkCall &c,
                               at::Tensor &o) {
     using torch::autograd::SavedVariable;
-    at::Tensor rest, lse;
+    at::Tensor kept;
     {
         const at::AutoGradMode off(false);
         o = packed_like(q);
-        rest = packed_like(q);
-        lse = at::empty({q.size(0), q.size(1), q.size(2)}, q.options().dtype(at::kFloat));
-        const smha_status_t st = run_sink_forward(q, k, v, o, lse.data_ptr<float>(), rest.data_ptr(), offsets.defined() ? offsets.data_ptr<int32_t>() : nullptr,
+        kept = at::empty({lse_bytes(q) + q.numel() * (int64_t)q.element_size()}, q.options().dtype(at::kByte));
+        const smha_status_t st = run_sink_forward(q, k, v, o, static_cast<float *>(kept.data_ptr()), static_cast<char *>(kept.data_ptr()) + lse_bytes(q), offsets.defined() ? offsets.data_ptr<int32_t>() : nullptr,
                                                   lengths.defined() ? lengths.data_ptr<int32_t>() : nullptr, c);
         if (st != SMHA_OK) return st;
     }
@@ -276,8 +277,7 @@ smha_status_t sink_with_graph(const at::Tensor &q, const at::Tensor &k, const at
     node->k_ = SavedVariable(k, false);
     node->v_ = SavedVariable(v, false);
     node->o_ = SavedVariable(o, true);
-    node->rest_ = SavedVariable(rest, false);
-    node->lse_ = SavedVariable(lse, false);
+    node->kept_ = SavedVariable(kept, false);
     node->offsets_ = SavedVariable(offsets, false);
     node->lengths_ = SavedVariable(lengths, false);
     return SMHA_OK;

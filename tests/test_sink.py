@@ -209,7 +209,7 @@ def test_the_graph_of_a_call(monkeypatch, native):
     seen = []
     with torch.autograd.graph.saved_tensors_hooks(lambda t: (seen.append(t.shape), t.cpu())[1], lambda t: t.cuda()):
         out = call()
-    assert len(seen) >= 6
+    assert len(seen) >= 5
     assert all(torch.equal(a, b) for a, b in zip(first, torch.autograd.grad(out, x, g)))
     again = torch.utils.checkpoint.checkpoint(lambda *y: smha.sink_attention(*y, 16, 1, lengths=n) * 1, *x, use_reentrant=False)
     assert all(torch.equal(a, b) for a, b in zip(first, torch.autograd.grad(again, x, g)))
