@@ -765,7 +765,7 @@ static bool sink_grids_fit(const SinkParams &sp) {
 // Whether dS goes into dQ and dK with what its rounding leaves out.  dQ and dK of rounded dS are 1.44 times as far from 64 bits as their own
 // rounding on average; of few queries, where a few large rows make most of the norm, up to 1.50 (2 x 12 x 68 x 64).  There both halves are
 // multiplied, a product more of three and of four: 1.05 (1.10 where windows are shortest).  us of a backward pass without and with them: 2 x 4 x 128 x 64, window 16: 15.6,
-// 16.4; 1 x 8 x 1024 x 64, window 256: 28.8, 30.9; 1 x 8 x 700 x 128: 48.9, 54.2; 1 x 2 x 1400 x 128: 73.2, 80.8 (most of which the host's 75 us
+// 16.4; 1 x 8 x 1024 x 64, window 256: 28.8, 30.9; 1 x 8 x 700 x 128: 48.9, 54.2; 1 x 2 x 1400 x 128: 73.2, 80.8 (most of which the host's 70 us
 // for a pass hide).  Of more queries errors average out, and products are what such a call lasts.
 static bool fine_ds(const SinkParams &sp) { const int64_t queries = (int64_t)sp.B * sp.H * sp.Sq;
     return queries <= 8192 && queries * std::min<int64_t>(sp.Sk, (int64_t)sp.window + sp.n_sink) <= 1 << 22; }

@@ -11,6 +11,7 @@
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
 #include <c10/core/impl/TorchDispatchModeTLS.h>
+#include <c10/core/Allocator.h>
 #include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Dtype.h>
@@ -198,6 +199,9 @@ smha_status_t run_sink_forward(const at::Tensor &q, const at::Tensor &k, const a
                                 c.window, c.n_sink, c.scale, c10::hip::getCurrentHIPStream(q.device().index()).stream());
 }
 
+// Memory for the work that a call enqueues, from torch's allocator for the current stream, on the current device.
+c10::DataPtr scratch(size_t bytes) { return c10::GetAllocator(c10::DeviceType::CUDA)->allocate(bytes); }
+
 at::Tensor packed_like(const at::Tensor &t) { return at::empty(t.sizes(), t.options(), at::MemoryFormat::Contiguous); }
 
 int64_t lse_bytes(const at::Tensor &q) { return (q.size(0) * q.size(1) * q.size(2) * 4 + 15) / 16 * 16; }
@@ -236,11 +240,11 @@ struct SinkBackward : torch::autograd::Node {
             smha_status_t st = entries.sink_workspace(B, H, Hkv, Sq, Sk, d, call_.window, call_.n_sink, &need);
             const Strides3 qs(q), ks(k), vs(v), ds(g);
             if (st == SMHA_OK) {
-                at::Tensor ws = at::empty({(int64_t)need}, q.options().dtype(at::kByte));
+                const c10::DataPtr ws = scratch(need);
                 st = entries.sink_backward(q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), static_cast<char *>(kept.data_ptr()) + lse_bytes(q), static_cast<const float *>(kept.data_ptr()), g.data_ptr(), dq.data_ptr(),
                                            dk.data_ptr(), dv.data_ptr(), B, H, Hkv, Sq, Sk, d, (smha_dtype_t)code_of(q.scalar_type()), qs.ptr, ks.ptr, vs.ptr, nullptr, ds.ptr,
                                            nullptr, nullptr, nullptr, offsets.defined() ? offsets.data_ptr<int32_t>() : nullptr,
-                                           lengths.defined() ? lengths.data_ptr<int32_t>() : nullptr, call_.window, call_.n_sink, call_.scale, ws.data_ptr(), need,
+                                           lengths.defined() ? lengths.data_ptr<int32_t>() : nullptr, call_.window, call_.n_sink, call_.scale, ws.get(), need,
                                            c10::hip::getCurrentHIPStream(q.device().index()).stream());
             }
             TORCH_CHECK(st == SMHA_OK, "smha_sink_backward: status ", (int)st);
@@ -357,11 +361,11 @@ PyObject *cache_attention(PyObject *, PyObject *const *args, Py_ssize_t n) {
     smha_status_t st = entries.cache_workspace(B, H, Hkv, T, Sk, P, d, window, n_sink, weights != nullptr, &need);
     if (st != SMHA_OK) return PyLong_FromLong((long)st);
     const at::AutoGradMode off(false);
-    at::Tensor o = packed_like(q), ws;
-    if (need) ws = at::empty({(int64_t)need}, q.options().dtype(at::kByte));
+    at::Tensor o = packed_like(q);
+    const c10::DataPtr ws = need ? scratch(need) : c10::DataPtr();
     st = entries.cache_forward(q.data_ptr(), k.data_ptr(), v.data_ptr(), pk, pv, o.data_ptr(), weights, lengths, B, H, Hkv, T, Sk, P, d,
                                (smha_dtype_t)code_of(q.scalar_type()), qs.ptr, ks.ptr, vs.ptr, nullptr, nullptr, nullptr, nullptr, window, n_sink,
-                               (float)PyFloat_AS_DOUBLE(args[9]), need ? ws.data_ptr() : nullptr, need, c10::hip::getCurrentHIPStream(q.device().index()).stream());
+                               (float)PyFloat_AS_DOUBLE(args[9]), ws.get(), need, c10::hip::getCurrentHIPStream(q.device().index()).stream());
     if (st != SMHA_OK) return PyLong_FromLong((long)st);
     if (weights) written(weights_t);
     return THPVariable_Wrap(std::move(o));
@@ -396,9 +400,10 @@ PyObject *cache_evict(PyObject *, PyObject *const *args, Py_ssize_t n) {
     smha_status_t st = entries.cache_evict_workspace(B, Hkv, Sk, d, budget, recent, &need);
     if (st != SMHA_OK) return PyLong_FromLong((long)st);
     const at::AutoGradMode off(false);
-    at::Tensor w2 = packed_like(w), p2 = packed_like(p), len2 = packed_like(len), ws = at::empty({(int64_t)need}, k.options().dtype(at::kByte));
+    at::Tensor w2 = packed_like(w), p2 = packed_like(p), len2 = packed_like(len);
+    const c10::DataPtr ws = scratch(need);
     st = entries.cache_evict(k.data_ptr(), v.data_ptr(), w.data_ptr<float>(), p.data_ptr<int32_t>(), len.data_ptr<int32_t>(), w2.data_ptr<float>(),
-                             p2.data_ptr<int32_t>(), len2.data_ptr<int32_t>(), B, Hkv, Sk, d, budget, recent, ks.ptr, vs.ptr, ws.data_ptr(), need,
+                             p2.data_ptr<int32_t>(), len2.data_ptr<int32_t>(), B, Hkv, Sk, d, budget, recent, ks.ptr, vs.ptr, ws.get(), need,
                              c10::hip::getCurrentHIPStream(k.device().index()).stream());
     if (st != SMHA_OK) return PyLong_FromLong((long)st);
     written(k);
