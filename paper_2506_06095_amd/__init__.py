@@ -20,5 +20,6 @@ _OPERATORS = {**{name: "sink" for name in ("sink_attention", "smha_sink_backward
 def __getattr__(name):  # (these modules need torch when they are imported, which plans on the host do not)
     if name in _OPERATORS:
         import importlib
-        return getattr(importlib.import_module(f".{_OPERATORS[name]}", __name__), name)
+        value = globals()[name] = getattr(importlib.import_module(f".{_OPERATORS[name]}", __name__), name)  # (from now on an ordinary name: this costs 8 us)
+        return value
     raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
