@@ -8,6 +8,7 @@ from __future__ import annotations
 import ctypes as C
 import os
 import subprocess
+import threading
 import warnings
 from typing import Optional, Sequence
 
@@ -127,40 +128,40 @@ def _load():
     return lib
 
 
-_native = _native_module = None  # (forward of _smha_torch, address of smha_forward); the module
+_native = None  # (forward of _smha_torch, address of smha_forward)
+_loading = threading.Lock()
 _LINKED = ("sink_forward", "sink_backward", "sink_workspace", "cache_forward", "cache_workspace", "cache_evict", "cache_evict_workspace")  # in link()'s order
 
 
+def _left_to_python(*args):
+    """What takes no call."""
+    return None
+
+
 def _load_native():
-    """The native way of Plan.forward, built if it is not there or of other sources; where that fails, one that takes no call."""
-    global _native, _native_module
-    if _native is None:
-        lib = _load()
-        import torch  # noqa: F401  (the module uses its libraries)
-        try:
-            if not _build.extension_current():
-                _build.build_extension()
-            from . import _smha_torch
-            _smha_torch.link(*(C.cast(getattr(lib, f"smha_{name}"), C.c_void_p).value for name in _LINKED))
-            _native = (_smha_torch.forward, C.cast(lib.smha_forward, C.c_void_p).value)
-            _native_module = _smha_torch
-        except (ImportError, OSError, subprocess.SubprocessError) as e:
-            warnings.warn(f"no native call path for Plan.forward, every call takes the slower one through ctypes: {e}", RuntimeWarning)
-            _native = (lambda *args: None, 0)
-            _native_module = _NoModule()
-    return _native
+    """The native way of Plan.forward, built if it is not there or of other sources; where that fails, one that takes no call.  Threads whose
+    first calls meet wait for the first of them, and see the whole of it or nothing."""
+    global _native
+    with _loading:
+        if _native is None:
+            lib = _load()
+            import torch  # noqa: F401  (the module uses its libraries)
+            try:
+                if not _build.extension_current():
+                    _build.build_extension()
+                from . import _smha_torch
+                _smha_torch.link(*(C.cast(getattr(lib, f"smha_{name}"), C.c_void_p).value for name in _LINKED))
+                _native = (_smha_torch.forward, C.cast(lib.smha_forward, C.c_void_p).value)
+            except (ImportError, OSError, subprocess.SubprocessError) as e:
+                warnings.warn(f"no native call path for Plan.forward, every call takes the slower one through ctypes: {e}", RuntimeWarning)
+                _native = (_left_to_python, 0)
+        return _native
 
 
 def native_call(name: str):
     """A function of _smha_torch: it answers, gives a status, or None for a call that it leaves to Python (csrc/torch_binding.cpp)."""
-    if _native is None:
-        _load_native()
-    return getattr(_native_module, name)
-
-
-class _NoModule:
-    def __getattr__(self, name):
-        return lambda *args: None
+    forward, _ = _native or _load_native()
+    return _left_to_python if forward is _left_to_python else getattr(forward.__self__, name)
 
 
 def smha_status_string(status: int) -> str:

@@ -18,3 +18,54 @@ def test_a_name_is_looked_up_once():
             "assert all(vars(smha).get(n) is f for n, f in zip(names, first))\n"
             "try:\n    smha.no_such_operator\nexcept AttributeError:\n    pass\nelse:\n    raise SystemExit('found')\n")
     subprocess.run([sys.executable, "-c", code], check=True, cwd=smha.__path__[0] + "/..")
+
+
+@pytest.mark.parametrize("when", ["at first", "when the call path is known"])
+def test_a_first_call_from_two_threads(monkeypatch, when):
+    """Another thread's call in the middle of the first one: it finds the native function, neither an unfinished state nor a second build."""
+    import threading
+    from paper_2506_06095_amd import binding
+    builds = []
+    monkeypatch.setattr(binding, "_native", None)
+    monkeypatch.setattr(binding, "_native_module", None, raising=False)
+    monkeypatch.setattr(binding._build, "extension_current", lambda: False)
+    monkeypatch.setattr(binding._build, "build_extension", lambda: builds.append(threading.get_ident()))
+    got, others = [], []
+
+    def call():
+        try:
+            got.append(binding.native_call("sink_attention"))
+        except Exception as e:  # noqa: BLE001
+            got.append(e)
+
+    def first():
+        def at_line(frame, event, arg):
+            if frame.f_code is binding._load_native.__code__ and not others and (when == "at first" or binding._native is not None):
+                others.append(threading.Thread(target=call))
+                others[0].start()
+                others[0].join(0.2)  # (it may have to wait until the first is done)
+            return at_line
+        sys.settrace(at_line)
+        call()
+        sys.settrace(None)
+
+    thread = threading.Thread(target=first)
+    thread.start()
+    thread.join()
+    others[0].join()
+    assert len(got) == 2 and all(callable(f) and f.__name__ == "sink_attention" for f in got), got
+    assert len(builds) == 1
+
+
+def test_the_native_functions_are_those_of_the_module_in_use(monkeypatch, tmp_path):
+    """Where the native module cannot be had, calls go the general way; once it can, they are its own again."""
+    from paper_2506_06095_amd import binding
+    native = binding.native_call("cache_evict")
+    assert native.__name__ == "cache_evict"
+    with monkeypatch.context() as m:
+        m.setattr(binding, "_native", None)
+        m.setattr(binding._build, "EXT", str(tmp_path / "_smha_torch.so"))
+        m.setenv("CXX", "false")
+        with pytest.warns(RuntimeWarning, match="native call path"):
+            assert binding.native_call("cache_evict")() is None
+    assert binding.native_call("cache_evict") is native
