@@ -403,7 +403,8 @@ smha_status_t smha_cache_forward(const void *Q, const void *K, const void *V, co
  * +inf are equals, and so are NaN and -inf.  Keys that stay keep their slots, but those in slots from `budget` on move, in order, to
  * the slots before it that were freed, with their weights and positions.  Slots from the new length on get weight 0 and
  * position -1; their keys and values stay as they are.
- *   K, V            device, [B][Hkv][Sk][d], any 16-bit type, changed in place; strides as in smha_forward, but a head may be of any size
+ *   K, V            device, [B][Hkv][Sk][d], any 16-bit type, changed in place; strides as in smha_forward, but a head may be of any size;
+ *                   no two heads in one place
  *   weights         device, float [B][Hkv][Sk], positions: int32 [B][Hkv][Sk], lengths: int32 [B]; packed
  *   *_out           what they are then; each may be the input itself, or must not overlap any
  * Not affected by NaN or infinities among the weights beyond what is said above.  No floating-point sums: exact.

@@ -209,4 +209,8 @@ __device__ __forceinline__ void tiles_landed() {
     asm volatile("" ::: "memory");
 }
 
+// --- what their entry points check (strides {batch, head, token}, null: packed)
+// Heads that are written must not lie in one place.
+inline bool apart(const int64_t *s, int B, int H, int d) { return !s || ((B == 1 || s[0] >= d) && (H == 1 || s[1] >= d)); }
+
 }  // namespace smha

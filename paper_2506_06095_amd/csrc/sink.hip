@@ -703,9 +703,6 @@ static bool strides_fit(const int64_t *s, int64_t rows, int d) {
     return s[0] % 8 == 0 && s[1] % 8 == 0 && s[2] % 8 == 0 && s[0] >= 0 && s[1] >= 0 && s[2] >= d && (rows * s[2] + d) * 2 < ((int64_t)1 << 31);
 }
 
-// Heads that are written must not lie in one place.
-static bool apart(const int64_t *s, int B, int H, int d) { return !s || ((B == 1 || s[0] >= d) && (H == 1 || s[1] >= d)); }
-
 static Strides strides_of(const int64_t *s, int64_t heads, int64_t rows, int d) {
     return s ? Strides{s[0], s[1], s[2]} : Strides{heads * rows * d, rows * d, d};
 }

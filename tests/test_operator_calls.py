@@ -69,3 +69,24 @@ def test_the_native_functions_are_those_of_the_module_in_use(monkeypatch, tmp_pa
         with pytest.warns(RuntimeWarning, match="native call path"):
             assert binding.native_call("cache_evict")() is None
     assert binding.native_call("cache_evict") is native
+
+
+# What the C ABI says, on the CPU: status 1 invalid, 2 unsupported, 3 shape.
+
+def abi():
+    import ctypes as C
+    from paper_2506_06095_amd.binding import _load
+    return C, _load(), C.c_void_p(4096)
+
+
+def test_eviction_refuses_heads_that_lie_in_one_place():
+    """Each head moves rows of its own: two that share memory would move them at once."""
+    C, lib, ptr = abi()
+
+    def evict(ks, vs=None, B=2):
+        ks, vs = ((C.c_int64 * 3)(*s) if s else None for s in (ks, vs))
+        return lib.smha_cache_evict(ptr, *[ptr] * 7, B, 2, 8, 64, 4, 1, ks, vs, ptr, 1 << 30, None)
+
+    for bad in ((0, 512, 64), (1024, 0, 64), (1024, 56, 64)):
+        assert evict(bad) == 2 and evict(None, bad) == 2, bad
+    assert evict((0, 0, 64), B=1) == 2  # (one sequence, but two heads in one place)
