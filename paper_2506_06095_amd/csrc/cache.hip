@@ -1102,7 +1102,7 @@ extern "C" smha_status_t smha_cache_forward(const void *Q, const void *K, const 
     if (((uintptr_t)Q | (uintptr_t)K | (uintptr_t)V | (uintptr_t)O | (uintptr_t)workspace | (P ? (uintptr_t)PK | (uintptr_t)PV : 0)) & 15) return SMHA_ERR_UNSUPPORTED;
     if (!cache_strides_fit(q_strides, T, d) || !cache_strides_fit(k_strides, Sk, d) || !cache_strides_fit(v_strides, Sk, d) || !cache_strides_fit(o_strides, T, d))
         return SMHA_ERR_UNSUPPORTED;
-    if (!apart(o_strides, B, H, d)) return SMHA_ERR_UNSUPPORTED;
+    if (!apart(o_strides, B, H, T, d)) return SMHA_ERR_UNSUPPORTED;
     if (P) {
         for (const int64_t *s : {pk_strides, pv_strides}) {
             const int64_t three[3] = {0, s ? s[0] : (int64_t)P * d, s ? s[1] : d};
@@ -1160,7 +1160,7 @@ extern "C" smha_status_t smha_cache_evict(void *K, void *V, const float *weights
     if (((uintptr_t)K | (uintptr_t)V) & 15 || (uintptr_t)workspace & 3) return SMHA_ERR_UNSUPPORTED;
     for (const int64_t *s : {k_strides, v_strides})
         if (s && (s[0] % 8 || s[1] % 8 || s[2] % 8 || s[0] < 0 || s[1] < 0 || s[2] < d)) return SMHA_ERR_UNSUPPORTED;
-    if (!apart(k_strides, B, Hkv, d) || !apart(v_strides, B, Hkv, d)) return SMHA_ERR_UNSUPPORTED;
+    if (!apart(k_strides, B, Hkv, Sk, d) || !apart(v_strides, B, Hkv, Sk, d)) return SMHA_ERR_UNSUPPORTED;
     EvictParams ep{};
     ep.K = (uint16_t *)K; ep.V = (uint16_t *)V;
     ep.ks = cache_strides(k_strides, Hkv, Sk, d); ep.vs = cache_strides(v_strides, Hkv, Sk, d);

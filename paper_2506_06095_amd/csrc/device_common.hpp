@@ -4,6 +4,7 @@
 
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cstdint>
 
 #include "smha.h"
@@ -210,7 +211,20 @@ __device__ __forceinline__ void tiles_landed() {
 }
 
 // --- what their entry points check (strides {batch, head, token}, null: packed)
-// Heads that are written must not lie in one place.
-inline bool apart(const int64_t *s, int B, int H, int d) { return !s || ((B == 1 || s[0] >= d) && (H == 1 || s[1] >= d)); }
+// Rows that are written must not share memory: from the closest rows outwards, each dimension steps over all that those before it span.
+inline bool apart(const int64_t *s, int64_t B, int64_t H, int64_t rows, int64_t d) {
+    if (!s) return true;
+    struct {
+        int64_t n, step;
+    } dims[3] = {{B, s[0]}, {H, s[1]}, {rows, s[2]}};
+    std::sort(dims, dims + 3, [](const auto &x, const auto &y) { return x.step < y.step; });
+    __int128 span = d;
+    for (const auto &dim : dims)
+        if (dim.n > 1) {
+            if (dim.step < span) return false;
+            span += (__int128)dim.step * (dim.n - 1);
+        }
+    return true;
+}
 
 }  // namespace smha

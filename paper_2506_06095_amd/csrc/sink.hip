@@ -804,7 +804,7 @@ extern "C" smha_status_t smha_sink_forward(const void *Q, const void *K, const v
     if (st != SMHA_OK) return st;
     if (((uintptr_t)Q | (uintptr_t)K | (uintptr_t)V | (uintptr_t)O | (uintptr_t)O_rest) & 15) return SMHA_ERR_UNSUPPORTED;
     if (!strides_fit(q_strides, Sq + 128, d) || !strides_fit(k_strides, (int64_t)Sk + 128, d) || !strides_fit(v_strides, (int64_t)Sk + 128, d) || !strides_fit(o_strides, Sq + 128, d) ||
-        !apart(o_strides, B, H, d))
+        !apart(o_strides, B, H, Sq, d))
         return SMHA_ERR_UNSUPPORTED;
     sp.Q = (const uint16_t *)Q; sp.K = (const uint16_t *)K; sp.V = (const uint16_t *)V; sp.O = (uint16_t *)O; sp.lse = lse; sp.rest = (uint16_t *)O_rest;
     sp.qs = strides_of(q_strides, H, Sq, d); sp.ks = strides_of(k_strides, Hkv, Sk, d); sp.vs = strides_of(v_strides, Hkv, Sk, d); sp.os = strides_of(o_strides, H, Sq, d);
@@ -854,7 +854,7 @@ extern "C" smha_status_t smha_sink_backward(const void *Q, const void *K, const 
         if (!strides_fit(s, Sq + 128, d)) return SMHA_ERR_UNSUPPORTED;
     for (const int64_t *s : {k_strides, v_strides, dk_strides, dv_strides})
         if (!strides_fit(s, (int64_t)Sk + 128, d)) return SMHA_ERR_UNSUPPORTED;
-    if (!apart(dq_strides, B, H, d) || !apart(dk_strides, B, Hkv, d) || !apart(dv_strides, B, Hkv, d)) return SMHA_ERR_UNSUPPORTED;
+    if (!apart(dq_strides, B, H, Sq, d) || !apart(dk_strides, B, Hkv, Sk, d) || !apart(dv_strides, B, Hkv, Sk, d)) return SMHA_ERR_UNSUPPORTED;
     sink_cuts(sp);
     sp.Q = (const uint16_t *)Q; sp.K = (const uint16_t *)K; sp.V = (const uint16_t *)V; sp.Oin = (const uint16_t *)O; sp.rest = (uint16_t *)const_cast<void *>(O_rest); sp.dO = (const uint16_t *)dO;
     sp.dQ = (uint16_t *)dQ; sp.dK = (uint16_t *)dK; sp.dV = (uint16_t *)dV; sp.lse = const_cast<float *>(lse);

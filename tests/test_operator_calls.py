@@ -90,3 +90,28 @@ def test_eviction_refuses_heads_that_lie_in_one_place():
     for bad in ((0, 512, 64), (1024, 0, 64), (1024, 56, 64)):
         assert evict(bad) == 2 and evict(None, bad) == 2, bad
     assert evict((0, 0, 64), B=1) == 2  # (one sequence, but two heads in one place)
+
+
+# {batch, head, token} strides of 2 x 2 heads of 8 rows of 64, some of whose rows share memory though every step is wide enough for a row
+OVERLAPPING = [(512, 512, 64), (1024, 448, 64), (512, 960, 64), (64, 512, 64), (128, 64, 64), (1024, 512, 1024), (1536, 128, 128)]
+# and those of layouts whose rows do not: packed, heads outermost, token-major, batch within tokens, with room between, heads of a wider tensor
+APART = [(1024, 512, 64), (512, 1024, 64), (1024, 64, 128), (64, 128, 256), (4096, 1024, 72), (8192, 64, 1024)]
+
+
+@pytest.mark.parametrize("strides", OVERLAPPING + APART, ids=str)
+def test_written_rows_must_not_overlap(strides):
+    """(Without a GPU, a call that is not refused ends with status 5, a HIP error.)"""
+    if torch.cuda.is_available():
+        pytest.skip("the addresses are not real")
+    C, lib, ptr = abi()
+    s = (C.c_int64 * 3)(*strides)
+    args = (2, 2, 2, 8, 8, 64, 0)
+    got = [lib.smha_sink_forward(ptr, ptr, ptr, ptr, None, None, *args, None, None, None, s, None, None, 4, 0, 0.0, None)]
+    for at in (5, 6, 7):  # dq, dk, dv
+        st = [None] * 8
+        st[at] = s
+        got.append(lib.smha_sink_backward(*[ptr] * 10, *args, *st, None, None, 4, 0, 0.0, ptr, 1 << 30, None))
+    got.append(lib.smha_cache_forward(ptr, ptr, ptr, None, None, ptr, None, ptr, 2, 2, 2, 8, 8, 0, 64, 0, None, None, None, None, None, s, None, 0, 0, 0.0, None, 0, None))
+    for k, v in ((s, None), (None, s)):
+        got.append(lib.smha_cache_evict(ptr, *[ptr] * 7, 2, 2, 8, 64, 4, 1, k, v, ptr, 1 << 30, None))
+    assert got == [2 if strides in OVERLAPPING else 5] * 7
