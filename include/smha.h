@@ -375,7 +375,7 @@ smha_status_t smha_sink_backward(const void *Q, const void *K, const void *V, co
  *                   [B], taken as 0 or Sk where outside 0 .. Sk; the new tokens' keys are the last of them).
  *                   Types, head sizes, strides, alignment as in smha_sink_forward
  *   PK, PV          device, [Hkv][P][d], strides {head, key}: keys before those of every sequence, one copy for all; P = 0: none
- *   weights         device, float [B][Hkv][Sk], strides {batch, head} (NULL = packed): what attention each of a sequence's own keys
+ *   weights         device, float [B][Hkv][Sk], strides {batch, head} (NULL = packed; rows apart): what attention each of a sequence's own keys
  *                   received, summed over the T tokens and H / Hkv heads, is added; NULL: not wanted
  *   window, n_sink  as in smha_sink_forward, in a sequence's own keys; a window together with a prefix is UNSUPPORTED
  * Token t of sequence b stands at own key lengths[b] - T + t and sees the keys up to it (in its window, or sinks) and all of the

@@ -1103,6 +1103,10 @@ extern "C" smha_status_t smha_cache_forward(const void *Q, const void *K, const 
     if (!cache_strides_fit(q_strides, T, d) || !cache_strides_fit(k_strides, Sk, d) || !cache_strides_fit(v_strides, Sk, d) || !cache_strides_fit(o_strides, T, d))
         return SMHA_ERR_UNSUPPORTED;
     if (!apart(o_strides, B, H, T, d)) return SMHA_ERR_UNSUPPORTED;
+    if (weights && w_strides) {
+        const int64_t keys[3] = {w_strides[0], w_strides[1], 1};
+        if (keys[0] < 0 || keys[1] < 0 || !apart(keys, B, Hkv, Sk, 1)) return SMHA_ERR_UNSUPPORTED;
+    }
     if (P) {
         for (const int64_t *s : {pk_strides, pv_strides}) {
             const int64_t three[3] = {0, s ? s[0] : (int64_t)P * d, s ? s[1] : d};

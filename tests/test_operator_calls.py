@@ -115,3 +115,20 @@ def test_written_rows_must_not_overlap(strides):
     for k, v in ((s, None), (None, s)):
         got.append(lib.smha_cache_evict(ptr, *[ptr] * 7, 2, 2, 8, 64, 4, 1, k, v, ptr, 1 << 30, None))
     assert got == [2 if strides in OVERLAPPING else 5] * 7
+
+
+def test_accounts_that_overlap_are_refused():
+    """Accounts are read, added to and written without atomics: a key's belongs to one head of one sequence."""
+    if torch.cuda.is_available():
+        pytest.skip("the addresses are not real")
+    C, lib, ptr = abi()
+
+    def weigh(strides, B=2, Hkv=2, Sk=8):
+        return lib.smha_cache_forward(ptr, ptr, ptr, None, None, ptr, ptr, ptr, B, 2 * Hkv, Hkv, 1, Sk, 0, 64, 0, *[None] * 6, (C.c_int64 * 2)(*strides), 0, 0, 0.0, ptr, 1 << 40,
+                                      None)
+
+    for bad in ((0, 8), (16, 0), (8, 8), (16, 7), (-16, 8), (16, -8), (12, 8)):
+        assert weigh(bad) == 2, bad
+    for good in ((16, 8), (8, 16), (100, 9)):
+        assert weigh(good) == 5, good
+    assert weigh((0, 8), B=1) == 5 and weigh((8, 0), Hkv=1) == 5
