@@ -1018,6 +1018,7 @@ static smha_status_t cache_params(CacheParams &cp, CacheLayout &at, int B, int H
     if (H % Hkv) return SMHA_ERR_SHAPE;
     if (dtype != SMHA_F16 && dtype != SMHA_BF16) return SMHA_ERR_UNSUPPORTED;
     if (d < 8 || d > 128 || d % 8) return SMHA_ERR_UNSUPPORTED;
+    if (T >= kRowsEnd || Sk >= kRowsEnd || P >= kRowsEnd || (int64_t)B * H > (1 << 24) || (int64_t)B * H * T > (1 << 24)) return SMHA_ERR_UNSUPPORTED;
     if (P > 0 && window > 0) return SMHA_ERR_UNSUPPORTED;  // (the window would have to run back into the prefix)
     cp.B = B; cp.H = H; cp.Hkv = Hkv; cp.G = H / Hkv; cp.T = T; cp.Sk = Sk; cp.P = P; cp.d = d;
     cp.window = window == 0 || window > Sk ? Sk : window;
@@ -1028,8 +1029,8 @@ static smha_status_t cache_params(CacheParams &cp, CacheLayout &at, int B, int H
     cp.wide = !cp.direct && P > 0 && B * rows > 64;  // (one or two tiles of 32 rows: reading the keys once or twice by waves on their own fills the chip better)
     const int64_t prefix_tiles = !P ? 0 : cp.wide ? (B * rows + 127) / 128 : (B * rows + 31) / 32;
     const int64_t groups = (int64_t)Hkv * (prefix_tiles + B * own_tiles);
-    // (tiles and rows are counted in 32 bits)
-    if ((int64_t)B * H * T > (1 << 24) || groups * (std::max(Sk, P) / 32 + 8) > (1 << 30)) return SMHA_ERR_UNSUPPORTED;
+    // (tiles are counted in 32 bits)
+    if (groups * (std::max(Sk, P) / 32 + 8) > (1 << 30)) return SMHA_ERR_UNSUPPORTED;
     cp.own_tiles = (int)own_tiles;
     cp.prefix_tiles = (int)prefix_tiles;
     const int D = d <= 64 ? 64 : 128;

@@ -211,6 +211,8 @@ __device__ __forceinline__ void tiles_landed() {
 }
 
 // --- what their entry points check (strides {batch, head, token}, null: packed)
+// Rows of a head: 2^31 bytes hold fewer than this.  (With it, products of sizes fit their integers.)
+constexpr int kRowsEnd = 1 << 27;
 // Rows that are written must not share memory: from the closest rows outwards, each dimension steps over all that those before it span.
 inline bool apart(const int64_t *s, int64_t B, int64_t H, int64_t rows, int64_t d) {
     if (!s) return true;

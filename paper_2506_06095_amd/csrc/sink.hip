@@ -717,6 +717,7 @@ static smha_status_t sink_params(SinkParams &sp, int B, int H, int Hkv, int Sq, 
     if (H % Hkv) return SMHA_ERR_SHAPE;
     if (dtype != SMHA_F16 && dtype != SMHA_BF16) return SMHA_ERR_UNSUPPORTED;
     if (d < 8 || d > 128 || d % 8) return SMHA_ERR_UNSUPPORTED;
+    if (Sq >= kRowsEnd || Sk >= kRowsEnd) return SMHA_ERR_UNSUPPORTED;
     // (work items are numbered in 32 bits)
     if ((int64_t)B * H > (1 << 24) || (int64_t)B * H * (std::max(Sq, Sk) / 64 + 2) > (1 << 28)) return SMHA_ERR_UNSUPPORTED;
     if (!grid_fits((int64_t)B * H * ((Sq + 127) / 128))) return SMHA_ERR_UNSUPPORTED;

@@ -132,3 +132,22 @@ def test_accounts_that_overlap_are_refused():
     for good in ((16, 8), (8, 16), (100, 9)):
         assert weigh(good) == 5, good
     assert weigh((0, 8), B=1) == 5 and weigh((8, 0), Hkv=1) == 5
+
+
+def test_sizes_whose_products_pass_64_bits_are_refused():
+    """No memory holds them, but their products come out small; and a workspace's size is only told for calls that are taken."""
+    C, lib, ptr = abi()
+    need = C.c_size_t(7)
+    big, top = 1 << 30, (1 << 31) - 1
+    for sizes in ((big, big, 1, 1 << 26, 8, 0), (big, big, big, 1 << 26, 8, 0), (1 << 22, 1 << 22, 1, 1 << 22, 8, 0), (1, 1, 1, 1, top, 0), (1, 1, 1, 1, 1, top),
+                  (1, 1, 1, 1 << 27, 8, 0), (1, 1, 1, 1, 1 << 27, 0)):
+        for weigh in (0, 1):
+            assert lib.smha_cache_workspace(*sizes, 8, 0, 0, weigh, C.byref(need)) == 2, sizes
+        assert lib.smha_cache_forward(*[ptr] * 6, None, ptr, *sizes, 8, 0, *[None] * 7, 0, 0, 0.0, ptr, 1 << 62, None) == 2, sizes
+    for Sq, Sk in ((8, top), (top, 8), (1 << 27, 8), (8, 1 << 27), (1 << 29, 1 << 29)):
+        assert lib.smha_sink_workspace(1, 1, 1, Sq, Sk, 8, 4, 0, C.byref(need)) == 2, (Sq, Sk)
+        assert lib.smha_sink_forward(*[ptr] * 4, None, None, 1, 1, 1, Sq, Sk, 8, 0, *[None] * 6, 4, 0, 0.0, None) == 2, (Sq, Sk)
+    assert need.value == 7
+    # the longest heads that 2 GiB hold at 8 columns
+    assert lib.smha_sink_workspace(1, 1, 1, 8, (1 << 27) - 129, 8, 4, 0, C.byref(need)) == 0
+    assert lib.smha_cache_workspace(1, 1, 1, 1, (1 << 27) - 65, 0, 8, 4, 0, 0, C.byref(need)) == 0
