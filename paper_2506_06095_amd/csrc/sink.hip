@@ -43,6 +43,7 @@ struct SinkParams {
     float *parts;         // partial dK, dV of key tiles that are cut along their queries
     int n_tiles, n_sink_tiles;              // key tiles, those with sinks
     int chunk_sink, chunk_rest, cut_sink, cut_rest;  // steps of a part, parts at most: of a tile with sinks, of another
+    int places, rest_at;  // partial sums that a key head of a sequence has room for (tiles in one part need none), and where those of tiles without sinks begin
 };
 
 struct Sequence {
@@ -496,7 +497,7 @@ __global__ void __launch_bounds__(256, D == 64 && !FINE ? 3 : 2) smha_sink_bwd_k
         cut = p.cut_rest;
         const int at = turn.item - n_sinks, turns = at / n_rest;
         part = cut - 1 - turns;
-        place = n_sinks + (at - turns * n_rest) * cut + part;
+        place = p.rest_at + (at - turns * n_rest) * cut + part;
         tile = p.n_sink_tiles + at - turns * n_rest;
     }
     const Sequence s = sequence(p, b);
@@ -652,8 +653,8 @@ __global__ void __launch_bounds__(256, D == 64 && !FINE ? 3 : 2) smha_sink_bwd_k
         store_rows<D, C, BF16>(dk, p.scale, slab, lane, p.dK + b * p.dks.b + hk * p.dks.h, p.dks.s, kw, p.Sk, p.d);
         return;
     }
-    // [item][dV, dK][wave][4 accumulators][lane][4]
-    float *const mine = p.parts + (((int64_t)(hk * p.B + b) * p.per + place) * 2 * 4 + w) * (C / 8) * 256 + lane * 4;
+    // [place][dV, dK][wave][4 accumulators][lane][4]
+    float *const mine = p.parts + (((int64_t)(hk * p.B + b) * p.places + place) * 2 * 4 + w) * (C / 8) * 256 + lane * 4;
 #pragma unroll
     for (int i = 0; i < C / 8; ++i) {
         *reinterpret_cast<f32x4 *>(mine + i * 256) = f32x4{dv[i / 4][4 * (i % 4)], dv[i / 4][4 * (i % 4) + 1], dv[i / 4][4 * (i % 4) + 2], dv[i / 4][4 * (i % 4) + 3]};
@@ -670,14 +671,14 @@ __global__ void __launch_bounds__(256) smha_sink_sum(const SinkParams p) {
     const int bh = tile_at / tiles, tile = tile_at - bh * tiles, b = bh / p.Hkv, hk = bh - b * p.Hkv;
     const bool sink = tile < p.n_sink_tiles;
     const int cut = sink ? p.cut_sink : p.cut_rest;
-    const int item = sink ? tile * cut : p.n_sink_tiles * p.cut_sink + (tile - p.n_sink_tiles) * cut;
+    const int place = sink ? tile * cut : p.rest_at + (tile - p.n_sink_tiles) * cut;
     const Sequence s = sequence(p, b);
     const int parts = parts_of(key_tile(p, s, tile * 128).nq * p.G, cut, sink ? p.chunk_sink : p.chunk_rest);
     if (parts == 1) return;  // it was written whole
     uint16_t *const out = is_k ? p.dK + b * p.dks.b + hk * p.dks.h : p.dV + b * p.dvs.b + hk * p.dvs.h;
     const int64_t pitch = is_k ? p.dks.s : p.dvs.s;
     const float factor = is_k ? p.scale : 1.f;
-    const float *const from = p.parts + (((int64_t)(hk * p.B + b) * p.per + item) * 8 + is_k * 4 + w) * (C / 8) * 256;
+    const float *const from = p.parts + (((int64_t)(hk * p.B + b) * p.places + place) * 8 + is_k * 4 + w) * (C / 8) * 256;
     for (int i = threadIdx.x; i < C / 8 * 64; i += 256) {
         f32x4 sum = {0.f, 0.f, 0.f, 0.f};
         for (int c0 = 0; c0 < parts; c0 += 4) {
@@ -750,6 +751,9 @@ static void sink_cuts(SinkParams &sp) {
     sp.cut_sink = (int)((nq * sp.G + sp.chunk_sink - 1) / sp.chunk_sink);
     sp.cut_rest = (int)((near * sp.G + sp.chunk_rest - 1) / sp.chunk_rest);
     if (sp.n_sink_tiles == 0) sp.cut_sink = 1;
+    // (with a few sinks theirs is often the only tile that is cut: 1 x 32 x 131072 x 128, window 1024, would keep 4 GiB for 8 MiB of sums)
+    sp.rest_at = sp.cut_sink > 1 ? (int)((int64_t)sp.n_sink_tiles * sp.cut_sink) : 0;
+    sp.places = (int)(sp.rest_at + (sp.cut_rest > 1 ? (int64_t)(sp.n_tiles - sp.n_sink_tiles) * sp.cut_rest : 0));
 }
 
 static int64_t sink_stats_bytes(const SinkParams &sp) { return (int64_t)2 * sp.B * sp.H * sp.Sqp * 4; }
@@ -830,8 +834,7 @@ extern "C" smha_status_t smha_sink_workspace(int B, int H, int Hkv, int Sq, int 
     if (st != SMHA_OK) return st;
     sink_cuts(sp);
     if (!sink_grids_fit(sp)) return SMHA_ERR_UNSUPPORTED;
-    const bool cut = sp.cut_sink > 1 || sp.cut_rest > 1;
-    *need = (size_t)(sink_stats_bytes(sp) + (cut ? sink_items(sp) * 2 * 128 * sink_width(d) * 4 : 0));
+    *need = (size_t)(sink_stats_bytes(sp) + (int64_t)B * Hkv * sp.places * 2 * 128 * sink_width(d) * 4);
     return SMHA_OK;
 }
 

@@ -151,3 +151,44 @@ def test_sizes_whose_products_pass_64_bits_are_refused():
     # the longest heads that 2 GiB hold at 8 columns
     assert lib.smha_sink_workspace(1, 1, 1, 8, (1 << 27) - 129, 8, 4, 0, C.byref(need)) == 0
     assert lib.smha_cache_workspace(1, 1, 1, 1, (1 << 27) - 65, 0, 8, 4, 0, 0, C.byref(need)) == 0
+
+
+def sink_workspace(*sizes):
+    C, lib, _ = abi()
+    need = C.c_size_t(0)
+    assert lib.smha_sink_workspace(*sizes, C.byref(need)) == 0
+    return need.value
+
+
+def test_a_long_document_with_sinks_needs_little_more_than_one_without():
+    """Places for partial sums belong to key tiles that are cut: here the one with sinks, whose up to 400 parts in all (twelve steps at least, equally
+    shared) are 2 x 128 x columns x 4 bytes each."""
+    for B, H, Hkv, S, d, window in ((1, 32, 32, 131072, 128, 1024), (4, 32, 8, 32768, 128, 512), (1, 32, 8, 131072, 128, 1024), (2, 16, 16, 65536, 64, 256)):
+        without, with_ = (sink_workspace(B, H, Hkv, S, S, d, window, n) for n in (0, 4))
+        assert without == 2 * B * H * S * 4  # lse and delta of every query
+        assert with_ - without <= (400 + B * Hkv) * 2 * 128 * d * 4, (B, H, S, with_ - without)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("case", [
+    # B, H, Hkv, S, d, window, n_sink: tiles that are cut are
+    (1, 2, 2, 1000, 64, 16, 4),      # the sinks' alone
+    (2, 3, 3, 700, 80, 30, 130),     # two of them
+    (2, 4, 2, 1000, 128, 100, 3),    # all
+    (1, 2, 2, 600, 64, 0, 0),        # all, without sinks
+    (1, 1, 1, 150, 32, 16, 2),       # none
+], ids=str)
+def test_a_backward_pass_keeps_to_its_workspace(case):
+    from test_sink import check, reference, tensors
+    B, H, Hkv, S, d, window, n_sink = case
+    q, k, v, g = tensors(B, H, Hkv, S, S, d, torch.bfloat16)
+    want = reference(q, k, v, g, window, n_sink, None, None, 0.0)
+    need = sink_workspace(B, H, Hkv, S, S, d, window, n_sink)
+    out, rest, lse = torch.empty_like(q), torch.empty_like(q), torch.empty(B, H, S, device="cuda")
+    grads = [torch.full_like(t, float("nan")) for t in (q, k, v)]
+    smha.smha_sink_forward(q, k, v, out, lse, window, n_sink, O_rest=rest)
+    room = torch.full((need + 4096,), 0xAB, dtype=torch.uint8, device="cuda")
+    smha.smha_sink_backward(q, k, v, out, lse, g, *grads, window, n_sink, workspace=room[:need], O_rest=rest)
+    for name, got in zip(("out", "dq", "dk", "dv"), (out, *grads)):
+        check(got, want[name], name)
+    assert bool((room[need:] == 0xAB).all())
