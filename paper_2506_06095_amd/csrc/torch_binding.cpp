@@ -206,6 +206,16 @@ at::Tensor packed_like(const at::Tensor &t) { return at::empty(t.sizes(), t.opti
 
 int64_t lse_bytes(const at::Tensor &q) { return (q.size(0) * q.size(1) * q.size(2) * 4 + 15) / 16 * 16; }
 
+// Whether smha_sink_backward reads a gradient as it lies: autograd may hand on expanded and transposed ones, and such of more than 2 GiB between a
+// head's first and last row.
+bool taken(const at::Tensor &g) {
+    if (reinterpret_cast<uintptr_t>(g.data_ptr()) % 16) return false;
+    const Strides3 s(g);
+    if (!s.ptr) return true;
+    return s.ok && s.s[0] % 8 == 0 && s.s[1] % 8 == 0 && s.s[2] % 8 == 0 && s.s[2] >= g.size(3) && s.s[2] <= INT32_MAX &&
+           ((g.size(2) + 128) * s.s[2] + g.size(3)) * 2 <= INT32_MAX;
+}
+
 // The backward pass of one call.
 struct SinkBackward : torch::autograd::Node {
     torch::autograd::SavedVariable q_, k_, v_, o_, kept_, offsets_, lengths_;  // kept: lse, then what O's rounding left out
@@ -226,11 +236,7 @@ struct SinkBackward : torch::autograd::Node {
         at::Tensor g = grads[0].detach(), dq, dk, dv;
         {
             const at::AutoGradMode off(false);
-            const auto gs = g.strides();
-            // (autograd may hand on expanded or transposed gradients)
-            const bool takes = reinterpret_cast<uintptr_t>(g.data_ptr()) % 16 == 0 &&
-                               (g.is_contiguous() || (gs[3] == 1 && gs[0] % 8 == 0 && gs[1] % 8 == 0 && gs[2] % 8 == 0 && gs[2] >= g.size(3)));
-            if (!takes) g = g.clone(at::MemoryFormat::Contiguous);
+            if (!taken(g)) g = g.clone(at::MemoryFormat::Contiguous);
             dq = packed_like(q);
             dk = packed_like(k);
             dv = packed_like(v);

@@ -130,9 +130,15 @@ def smha_sink_backward(Q, K, V, O, lse, dO, dQ, dK, dV, window: int = 0, n_sink:
 
 
 def _takes(t):
-    """Whether the kernels can read a gradient as it lies (autograd may hand on expanded or transposed ones)."""
-    s = t.stride()
-    return t.is_contiguous() and t.data_ptr() % 16 == 0 or (s[3] == 1 and s[0] % 8 == s[1] % 8 == s[2] % 8 == 0 and s[2] >= t.shape[3] and t.data_ptr() % 16 == 0)
+    """Whether the kernels can read a gradient as it lies (autograd may hand on expanded or transposed ones, and such of more than 2 GiB between a
+    head's first and last row)."""
+    if t.data_ptr() % 16:
+        return False
+    if t.is_contiguous():
+        return True
+    (b, h, rows, d), s = t.shape, t.stride()
+    pitch = s[2] if rows > 1 else d
+    return s[3] == 1 and all(n == 1 or step % 8 == 0 for n, step in zip((b, h, rows), s)) and pitch >= d and ((rows + 128) * pitch + d) * 2 < 1 << 31
 
 
 class _SinkAttention(torch.autograd.Function):
