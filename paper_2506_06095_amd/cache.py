@@ -32,6 +32,12 @@ def _written(*tensors):
             torch.autograd.graph.increment_version(t)
 
 
+def _check_no_gradients(name, *tensors):
+    """Gradients would be lost, or leaves written."""
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
+        raise ValueError(f"{name} has no gradients, and writes no tensor that requires them")
+
+
 def _check_workspace(workspace, like):
     if workspace.dtype != torch.uint8 or workspace.device != like.device or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous uint8 tensor on the same GPU")
@@ -55,8 +61,8 @@ def cache_attention(q, k, v, lengths, *, window: int = 0, n_sink: int = 0, prefi
     first `n_sink`.
     prefix: (keys, values), each [Hkv,P,d]: tokens before those of every sequence, which all of them see (not with a window).
     weights: float32 [B,Hkv,Sk]; each key's attention, summed over the tokens and the heads that share it, is added to it.
-    scale: 0 or less for 1/sqrt(d).  No gradients, and values that a token of the sequence sees have to be finite (those before the window, past the
-    length and in the cache's free slots may be anything).  workspace: a uint8 tensor of smha_cache_workspace bytes, by default one is allocated."""
+    scale: 0 or less for 1/sqrt(d).  No gradients (sink_attention has them): no tensor given may require any.  Values that a token of the sequence
+    sees have to be finite (those before the window, past the length and in the cache's free slots may be anything).  workspace: a uint8 tensor of smha_cache_workspace bytes, by default one is allocated."""
     if out is None and workspace is None and stream is None:  # the native way, for every call that it takes (csrc/torch_binding.cpp)
         global _attention
         if _attention is None:
@@ -68,8 +74,7 @@ def cache_attention(q, k, v, lengths, *, window: int = 0, n_sink: int = 0, prefi
                 raise SmhaError(got, "smha_cache_forward")
             return got
     _check_qkv(q, k, v)
-    if torch.is_grad_enabled() and (q.requires_grad or k.requires_grad or v.requires_grad):
-        raise ValueError("cache_attention has no gradients: sink_attention has")
+    _check_no_gradients("cache_attention", q, k, v, *(() if prefix is None else prefix), weights, out)
     (B, H, T, d), (Hkv, Sk) = q.shape, k.shape[1:3]
     if lengths is None:
         raise ValueError("lengths must be given")
@@ -137,7 +142,7 @@ def cache_evict(k, v, weights, positions, lengths, budget: int, recent: int = 0,
     those of the largest weight, the lower slot first among equals (recent keys count as of infinite weight, NaN as of the lowest).  Keys keep
     their slots, except that those that stay past the budget move, in order, to the slots before it that were freed.  Slots from the
     new length on get weight 0 and position -1, and keep their keys.
-    out: the three tensors to write to, by default new ones; they may be the inputs themselves."""
+    out: the three tensors to write to, by default new ones; they may be the inputs themselves.  No gradients."""
     if out is None and workspace is None and stream is None:
         global _evict
         if _evict is None:
@@ -152,8 +157,7 @@ def cache_evict(k, v, weights, positions, lengths, budget: int, recent: int = 0,
     if not k.is_cuda or v.device != k.device:
         raise ValueError("tensors must be on one GPU")
     B, Hkv, Sk, d = k.shape
-    if torch.is_grad_enabled() and (k.requires_grad or v.requires_grad):
-        raise ValueError("cache_evict changes k and v in place: they must not require gradients")
+    _check_no_gradients("cache_evict", k, v, weights, *(() if out is None else out))
     for t in (k, v):
         s = t.stride()
         if any(size > 1 and step < d for size, step in zip((B, Hkv, Sk), s)):

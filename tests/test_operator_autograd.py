@@ -32,3 +32,51 @@ def test_gradients_of_any_layout(monkeypatch, native, strides):
     want = torch.autograd.grad(smha.sink_attention(*x, 2, 1), x, g.contiguous())
     got = torch.autograd.grad(smha.sink_attention(*x, 2, 1), x, g)
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def cache_inputs():
+    q, k, v = randn(2, 4, 1, 64, seed=1), randn(2, 2, 16, 64, seed=2), randn(2, 2, 16, 64, seed=3)
+    return q, k, v, (randn(2, 8, 64, seed=4), randn(2, 8, 64, seed=5)), torch.zeros(2, 2, 16, device="cuda"), torch.tensor([16, 3], dtype=torch.int32, device="cuda")
+
+
+@pytest.mark.gpu
+@WAYS
+@pytest.mark.parametrize("which", ["q", "k", "v", "prefix keys", "prefix values", "weights", "out"])
+def test_attention_on_a_cache_has_no_gradients_of_any_input(monkeypatch, native, which):
+    """A gradient that would be lost, or a leaf that would be written, is refused; with gradients switched off both are allowed."""
+    general_way(monkeypatch, native)
+    q, k, v, (pk, pv), weights, n = cache_inputs()
+    out = torch.empty_like(q)
+    {"q": q, "k": k, "v": v, "prefix keys": pk, "prefix values": pv, "weights": weights, "out": out}[which].requires_grad_()
+    given = dict(prefix=(pk, pv), weights=weights, **(dict(out=out) if which == "out" else {}))
+    with pytest.raises(ValueError, match="gradients"):
+        smha.cache_attention(q, k, v, n, **given)
+    assert bool((weights == 0).all())
+    with torch.no_grad():
+        got = smha.cache_attention(q, k, v, n, **given)
+    assert not got.requires_grad or which == "out"
+    assert 0 < float(weights.sum()) < 8  # (of 8 rows; the prefix has the rest)
+
+
+@pytest.mark.gpu
+@WAYS
+@pytest.mark.parametrize("which", ["k", "v", "weights", "out"])
+def test_eviction_has_no_gradients_of_any_input(monkeypatch, native, which):
+    general_way(monkeypatch, native)
+    _, k, v, _, weights, n = cache_inputs()
+    positions = torch.arange(16, dtype=torch.int32, device="cuda").expand(2, 2, 16).contiguous()
+    out = (torch.empty_like(weights), positions, n)
+    {"k": k, "v": v, "weights": weights, "out": out[0]}[which].requires_grad_()
+    given = dict(out=out) if which == "out" else {}
+    with pytest.raises(ValueError, match="gradients"):
+        smha.cache_evict(k, v, weights, positions, n, 8, **given)
+    with torch.no_grad():
+        assert smha.cache_evict(k, v, weights, positions, n, 8, **given)[2].tolist() == [8, 3]
+
+
+@pytest.mark.gpu
+@WAYS
+def test_a_prefix_in_one_tensor(monkeypatch, native):
+    general_way(monkeypatch, native)
+    q, k, v, prefix, _, n = cache_inputs()
+    assert torch.equal(smha.cache_attention(q, k, v, n, prefix=torch.stack(prefix)), smha.cache_attention(q, k, v, n, prefix=prefix))
