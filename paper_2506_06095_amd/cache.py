@@ -10,7 +10,7 @@ import ctypes as C
 import torch
 
 from .binding import SmhaError, _load, native_call
-from .sink import _CODES, _check_int, _check_per_sequence, _check_qkv, _handle, _on_device, _strides
+from .sink import _CODES, _check_int, _check_no_tangents, _check_per_sequence, _check_qkv, _handle, _on_device, _strides
 
 
 _attention = _evict = None  # functions of _smha_torch
@@ -36,6 +36,7 @@ def _check_no_gradients(name, *tensors):
     """Gradients would be lost, or leaves written."""
     if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
         raise ValueError(f"{name} has no gradients, and writes no tensor that requires them")
+    _check_no_tangents(name, *tensors)
 
 
 def _check_workspace(workspace, like):

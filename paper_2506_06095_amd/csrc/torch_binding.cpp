@@ -293,6 +293,7 @@ smha_status_t sink_with_graph(const at::Tensor &q, const at::Tensor &k, const at
     return SMHA_OK;
 }
 
+// Forward mode, which the general way refuses (it goes by itself: neither gradients that are required nor that are switched off say that there is none).
 bool has_tangent(const at::Tensor &t) { return t._fw_grad(0).defined(); }
 
 // sink_attention(q, k, v, window, n_sink, offsets, lengths, scale) -> the output, a status, or None
@@ -307,10 +308,10 @@ PyObject *sink_attention(PyObject *, PyObject *const *args, Py_ssize_t n) {
     at::Tensor offsets_t, lengths_t;
     if (!per_sequence(args[5], q, offsets, offsets_t) || !per_sequence(args[6], q, lengths, lengths_t)) Py_RETURN_NONE;
     if (!Strides3(q).ok || !Strides3(k).ok || !Strides3(v).ok) Py_RETURN_NONE;
+    if (has_tangent(q) || has_tangent(k) || has_tangent(v)) Py_RETURN_NONE;
     const c10::DeviceGuard guard(q.device());
     at::Tensor o;
     if (at::GradMode::is_enabled() && (q.requires_grad() || k.requires_grad() || v.requires_grad())) {
-        if (has_tangent(q) || has_tangent(k) || has_tangent(v)) Py_RETURN_NONE;  // (forward mode, which the general way refuses)
         const smha_status_t st = sink_with_graph(q, k, v, offsets_t, lengths_t, c, o);
         if (st != SMHA_OK) return PyLong_FromLong((long)st);
     } else {
@@ -327,8 +328,8 @@ void written(const at::Tensor &t) {
     if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
 }
 
-// A gradient of it would be lost, or it would be written though it is a leaf.
-bool wants_gradient(const at::Tensor &t) { return at::GradMode::is_enabled() && t.requires_grad(); }
+// A derivative of it would be lost, or it would be written though it is a leaf.
+bool wants_derivative(const at::Tensor &t) { return (at::GradMode::is_enabled() && t.requires_grad()) || has_tangent(t); }
 
 // cache_attention(q, k, v, lengths, window, n_sink, prefix keys or None, prefix values or None, weights or None, scale) -> the output, a status, or None
 PyObject *cache_attention(PyObject *, PyObject *const *args, Py_ssize_t n) {
@@ -336,7 +337,7 @@ PyObject *cache_attention(PyObject *, PyObject *const *args, Py_ssize_t n) {
     if (n != 10 || !entries.cache_forward || at::impl::torch_function_mode_enabled() || c10::impl::TorchDispatchModeTLS::any_modes_set()) Py_RETURN_NONE;
     if (!plain(args[0]) || !plain(args[1]) || !plain(args[2]) || !PyFloat_CheckExact(args[9])) Py_RETURN_NONE;
     const at::Tensor &q = THPVariable_Unpack(args[0]), &k = THPVariable_Unpack(args[1]), &v = THPVariable_Unpack(args[2]);
-    if (!heads_fit(q, k, v) || wants_gradient(q) || wants_gradient(k) || wants_gradient(v)) Py_RETURN_NONE;
+    if (!heads_fit(q, k, v) || wants_derivative(q) || wants_derivative(k) || wants_derivative(v)) Py_RETURN_NONE;
     const int32_t *lengths;
     at::Tensor lengths_t;
     int window, n_sink;
@@ -348,7 +349,7 @@ PyObject *cache_attention(PyObject *, PyObject *const *args, Py_ssize_t n) {
         if (!plain(args[6], 3) || !plain(args[7], 3)) Py_RETURN_NONE;
         const at::Tensor &a = THPVariable_Unpack(args[6]), &b = THPVariable_Unpack(args[7]);
         if (a.sizes() != b.sizes() || a.size(0) != Hkv || a.size(2) != d || a.size(1) > INT32_MAX || a.scalar_type() != q.scalar_type() ||
-            b.scalar_type() != q.scalar_type() || a.device() != q.device() || b.device() != q.device() || !a.is_contiguous() || !b.is_contiguous() || wants_gradient(a) || wants_gradient(b))
+            b.scalar_type() != q.scalar_type() || a.device() != q.device() || b.device() != q.device() || !a.is_contiguous() || !b.is_contiguous() || wants_derivative(a) || wants_derivative(b))
             Py_RETURN_NONE;
         P = (int)a.size(1);
         pk = a.data_ptr();
@@ -359,7 +360,7 @@ PyObject *cache_attention(PyObject *, PyObject *const *args, Py_ssize_t n) {
     if (args[8] != Py_None) {
         if (!plain(args[8], 3)) Py_RETURN_NONE;
         const at::Tensor &w = THPVariable_Unpack(args[8]);
-        if (w.scalar_type() != at::kFloat || w.size(0) != B || w.size(1) != Hkv || w.size(2) != Sk || w.device() != q.device() || !w.is_contiguous() || wants_gradient(w))
+        if (w.scalar_type() != at::kFloat || w.size(0) != B || w.size(1) != Hkv || w.size(2) != Sk || w.device() != q.device() || !w.is_contiguous() || wants_derivative(w))
             Py_RETURN_NONE;
         weights_t = w;
         weights = w.data_ptr<float>();
@@ -393,7 +394,7 @@ PyObject *cache_evict(PyObject *, PyObject *const *args, Py_ssize_t n) {
     if (!int_from(args[5], budget) || !int_from(args[6], recent)) Py_RETURN_NONE;
     const int type = code_of(k.scalar_type());
     if ((type != SMHA_F16 && type != SMHA_BF16) || v.scalar_type() != k.scalar_type() || k.sizes() != v.sizes() || v.device() != k.device() || !small_sizes(k)) Py_RETURN_NONE;
-    if (wants_gradient(k) || wants_gradient(v) || wants_gradient(w)) Py_RETURN_NONE;
+    if (wants_derivative(k) || wants_derivative(v) || wants_derivative(w)) Py_RETURN_NONE;
     for (const at::Tensor *t : {&w, &p})
         if (t->sizes() != k.sizes().slice(0, 3) || t->device() != k.device() || !t->is_contiguous()) Py_RETURN_NONE;
     if (w.scalar_type() != at::kFloat || p.scalar_type() != at::kInt || len.scalar_type() != at::kInt || len.size(0) != k.size(0) || len.device() != k.device() ||

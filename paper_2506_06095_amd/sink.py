@@ -48,6 +48,12 @@ def _check_qkv(q, k, v):
         raise ValueError("tensors must be on one GPU")
 
 
+def _check_no_tangents(name, *tensors):
+    """Tangents of outputs would be missing."""
+    if any(t is not None and torch.autograd.forward_ad.unpack_dual(t).tangent is not None for t in tensors):
+        raise NotImplementedError(f"{name} has no derivatives in forward mode")
+
+
 def _check_per_sequence(t, name, like):
     """The pointer of an int32 [B] tensor, None for None."""
     if t is None:
@@ -167,7 +173,7 @@ _call = None  # the native way, for every call that it takes
 
 
 def sink_attention(q, k, v, window: int = 0, n_sink: int = 0, *, offsets=None, lengths=None, scale: float = 0.0):
-    """softmax(scale q k^T over visible keys) v, differentiable in q, k and v.
+    """softmax(scale q k^T over visible keys) v, differentiable in q, k and v (once, and not in forward mode).
 
     q [B,H,Sq,d]; k, v [B,Hkv,Sk,d], H a multiple of Hkv; float16 or bfloat16, d a multiple of 8 up to 128.  Query i of sequence b stands at
     offsets[b] + i (default Sk - Sq + i) and exists where that is in 0 .. lengths[b] - 1 (default Sk); it sees key j iff j is not after it and
@@ -183,6 +189,7 @@ def sink_attention(q, k, v, window: int = 0, n_sink: int = 0, *, offsets=None, l
             raise SmhaError(got, "smha_sink_forward")
         return got
     _check_qkv(q, k, v)
+    _check_no_tangents("sink_attention", q, k, v)
     if torch.is_grad_enabled() and (q.requires_grad or k.requires_grad or v.requires_grad):
         return _SinkAttention.apply(q, k, v, window, n_sink, offsets, lengths, scale)
     out = torch.empty(q.shape, dtype=q.dtype, device=q.device)

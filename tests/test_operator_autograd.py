@@ -80,3 +80,33 @@ def test_a_prefix_in_one_tensor(monkeypatch, native):
     general_way(monkeypatch, native)
     q, k, v, prefix, _, n = cache_inputs()
     assert torch.equal(smha.cache_attention(q, k, v, n, prefix=torch.stack(prefix)), smha.cache_attention(q, k, v, n, prefix=prefix))
+
+
+@pytest.mark.gpu
+@WAYS
+@pytest.mark.parametrize("requires_grad", [False, True])
+def test_forward_mode_is_refused(monkeypatch, native, requires_grad):
+    """There are no tangents of outputs: a call with one among its inputs must not drop it, whether gradients are wanted too or not."""
+    general_way(monkeypatch, native)
+    q, k, v, prefix, weights, n = cache_inputs()
+    positions = torch.arange(16, dtype=torch.int32, device="cuda").expand(2, 2, 16).contiguous()
+    keys = k.clone()
+    forward_ad = torch.autograd.forward_ad
+    with forward_ad.dual_level():
+        def dual(t):
+            return forward_ad.make_dual(t.detach().requires_grad_(requires_grad), torch.ones_like(t))
+
+        calls = [lambda: smha.sink_attention(dual(q), k, v, 4, 1), lambda: smha.sink_attention(q, dual(k), v, 4, 1), lambda: smha.sink_attention(q, k, dual(v), 4, 1)]
+        if not requires_grad:  # (else they are refused for that)
+            calls += [lambda: smha.cache_attention(dual(q), k, v, n), lambda: smha.cache_attention(q, dual(k), v, n), lambda: smha.cache_attention(q, k, dual(v), n),
+                      lambda: smha.cache_attention(q, k, v, n, prefix=(dual(prefix[0]), prefix[1])), lambda: smha.cache_attention(q, k, v, n, prefix=(prefix[0], dual(prefix[1]))),
+                      lambda: smha.cache_attention(q, k, v, n, weights=dual(weights)),
+                      lambda: smha.cache_evict(dual(k), v, weights, positions, n, 8), lambda: smha.cache_evict(k, dual(v), weights, positions, n, 8),
+                      lambda: smha.cache_evict(k, v, dual(weights), positions, n, 8)]
+        for i, call in enumerate(calls):
+            with pytest.raises(NotImplementedError, match="forward mode"):
+                print(i, call())
+            with torch.no_grad(), pytest.raises(NotImplementedError, match="forward mode"):  # (which leaves forward mode on)
+                print(i, call())
+        assert torch.equal(smha.cache_attention(q, k, v, n, prefix=prefix), smha.cache_attention(q, keys, v, n, prefix=prefix))
+    assert torch.equal(k, keys) and bool((weights == 0).all())
