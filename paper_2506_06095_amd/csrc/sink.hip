@@ -111,7 +111,8 @@ template <bool BF16> __device__ __forceinline__ uint32_t pack2_left(float a, flo
 
 // A wave's 32 x D accumulators (acc[dt][r] = row j, column 32 dt + 8 (r / 4) + 4 hh + r % 4) to rows row0 .. of a tensor with 16-bit values,
 // through 32 rows of LDS so that whole rows are written; rows from `rows` on are left out.
-// REST: not the rounded values, but what their rounding leaves out.
+// REST: not the rounded values, but what their rounding left out, by the very values that the call before left in `slab` (formed anew they may differ in
+// the last place: a product and its rounding to binary16 are one instruction or two, as the compiler sees fit).
 template <int D, int C, bool BF16, bool REST = false>
 __device__ __forceinline__ void store_rows(const f32x16 (&acc)[C / 32], float factor, char *slab, int lane, uint16_t *base, int64_t pitch, int row0, int rows, int d) {
     constexpr int CPR = D / 8;
@@ -123,9 +124,9 @@ __device__ __forceinline__ void store_rows(const f32x16 (&acc)[C / 32], float fa
             float x[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) x[e] = acc[dt][4 * g + e] * factor;
-            u32x2 v = {pack2<BF16>(x[0], x[1]), pack2<BF16>(x[2], x[3])};
-            if constexpr (REST) v = u32x2{pack2_left<BF16>(x[0], x[1], v[0]), pack2_left<BF16>(x[2], x[3], v[1])};
-            *reinterpret_cast<u32x2 *>(slab + j * D * 2 + (((4 * dt + g) ^ swz_both<D>(j)) * 16) + hh * 8) = v;
+            u32x2 *const at = reinterpret_cast<u32x2 *>(slab + j * D * 2 + (((4 * dt + g) ^ swz_both<D>(j)) * 16) + hh * 8);
+            if constexpr (REST) *at = u32x2{pack2_left<BF16>(x[0], x[1], (*at)[0]), pack2_left<BF16>(x[2], x[3], (*at)[1])};
+            else *at = u32x2{pack2<BF16>(x[0], x[1]), pack2<BF16>(x[2], x[3])};
         }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 #pragma unroll
