@@ -12,7 +12,7 @@ torch = pytest.importorskip("torch")
 
 import paper_2506_06095_amd as smha  # noqa: E402
 from paper_2506_06095_amd import sink  # noqa: E402
-from test_sink import F, int32, rounding, tensors, visible  # noqa: E402
+from test_sink import CASES, F, int32, reference, rounding, tensors, visible  # noqa: E402
 
 TYPES = pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16], ids=["f16", "bf16"])
 
@@ -112,3 +112,17 @@ def test_a_pass_of_autograd_keeps_it(monkeypatch, case, dtype, native):
     x = [t.requires_grad_() for t in (q, k, v)]
     dq, dk, _ = torch.autograd.grad(smha.sink_attention(*x, window, n_sink, offsets=int32(offsets), lengths=int32(lengths)), x, g)
     assert off(dq, want["dq"]) <= 1 and off(dk, want["dk"]) <= 1
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("case", CASES, ids=lambda c: "x".join(str(x) for x in c[:8]))
+def test_lse_is_minus_infinity_where_a_query_sees_nothing(case):
+    """And nowhere else, where it is within its bound."""
+    B, H, Hkv, Sq, Sk, d, window, n_sink, offsets, lengths, layout = case
+    q, k, v, g = tensors(B, H, Hkv, Sq, Sk, d, torch.float16, layout)
+    value, bound = reference(q, k, v, g, window, n_sink, offsets, lengths, 0.0)["lse"]
+    lse = torch.full((B, H, Sq), math.nan, device="cuda")
+    smha.smha_sink_forward(q, k, v, torch.empty_like(q), lse, window, n_sink, int32(offsets), int32(lengths))
+    lse, empty = lse.cpu().double(), torch.isneginf(value)
+    assert bool((lse[empty] == -math.inf).all())
+    assert bool(((lse - value).abs() <= bound)[~empty].all())
