@@ -108,6 +108,16 @@ __device__ __forceinline__ bool all_seen(int p0, int p1, int k0, int k1, int win
 template <bool BF16> __device__ __forceinline__ uint32_t pack2_left(float a, float b, uint32_t v) {
     return pack2<BF16>(a - widen16<BF16>(v & 0xFFFFu), b - widen16<BF16>(v >> 16));
 }
+// a and b as a pair of rounded values and another of what that leaves out.  (The first is a register from then on: the compiler would form a product's
+// rounding to binary16 a second time for the difference, in one instruction where it takes two for the pair, and at ties get the other neighbour.)
+struct Halves {
+    uint32_t hi, lo;
+};
+template <bool BF16> __device__ __forceinline__ Halves halves_of(float a, float b) {
+    uint32_t v = pack2<BF16>(a, b);
+    if constexpr (!BF16) asm("" : "+v"(v));
+    return {v, pack2_left<BF16>(a, b, v)};
+}
 
 // A wave's 32 x D accumulators (acc[dt][r] = row j, column 32 dt + 8 (r / 4) + 4 hh + r % 4) to rows row0 .. of a tensor with 16-bit values,
 // through 32 rows of LDS so that whole rows are written; rows from `rows` on are left out.
@@ -428,8 +438,13 @@ __global__ void __launch_bounds__(256, 2) smha_sink_bwd_q(const SinkParams p) {
                 u32x4 pf[2], left[2];
                 auto ds_pair = [&](int q) __attribute__((always_inline)) {
                     const float lo = sc[2 * q] * (dp[2 * q] - delta), hi = sc[2 * q + 1] * (dp[2 * q + 1] - delta);
-                    pf[q >> 2][q & 3] = pack2<BF16>(lo, hi);
-                    if constexpr (FINE) left[q >> 2][q & 3] = pack2_left<BF16>(lo, hi, pf[q >> 2][q & 3]);
+                    if constexpr (FINE) {
+                        const Halves x = halves_of<BF16>(lo, hi);
+                        pf[q >> 2][q & 3] = x.hi;
+                        left[q >> 2][q & 3] = x.lo;
+                    } else {
+                        pf[q >> 2][q & 3] = pack2<BF16>(lo, hi);
+                    }
                 };
 #pragma unroll
                 for (int q = 0; q < 4; ++q) ds_pair(q);
@@ -634,8 +649,13 @@ __global__ void __launch_bounds__(256, D == 64 && !FINE ? 3 : 2) smha_sink_bwd_k
             }
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                pf[i >> 2][i & 3] = pack2<BF16>(dp[2 * i], dp[2 * i + 1]);
-                if constexpr (FINE) left[i >> 2][i & 3] = pack2_left<BF16>(dp[2 * i], dp[2 * i + 1], pf[i >> 2][i & 3]);
+                if constexpr (FINE) {
+                    const Halves x = halves_of<BF16>(dp[2 * i], dp[2 * i + 1]);
+                    pf[i >> 2][i & 3] = x.hi;
+                    left[i >> 2][i & 3] = x.lo;
+                } else {
+                    pf[i >> 2][i & 3] = pack2<BF16>(dp[2 * i], dp[2 * i + 1]);
+                }
             }
 #pragma unroll
             for (int i = 0; i < 2 * NDT; ++i) {

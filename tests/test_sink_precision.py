@@ -126,3 +126,27 @@ def test_lse_is_minus_infinity_where_a_query_sees_nothing(case):
     lse, empty = lse.cpu().double(), torch.isneginf(value)
     assert bool((lse[empty] == -math.inf).all())
     assert bool(((lse - value).abs() <= bound)[~empty].all())
+
+
+@pytest.mark.gpu
+@TYPES
+@pytest.mark.parametrize("d", [64, 128])
+def test_both_halves_of_ds_make_one_number(dtype, d):
+    """Queries of zeros see three keys of equal weight, one of which is not zero: a row of dQ is one dS times one key and shows dS's error beside its own
+    rounding.  dS to twice its digits is off by u^2 and by what 32 bits leave of dP - delta; one step of the type, as where the halves are taken from two
+    roundings of a tie (one value in 2^14), would be up to two u.  64 x 128 queries, twelve times."""
+    (u, z), H, S = rounding(dtype), 64, 128
+    for seed in range(12):
+        q, k, v, g = tensors(1, H, H, S, S, d, dtype, seed=100 + seed)
+        q.zero_()
+        k[:, :, 1::3] = k[:, :, 2::3] = 0
+        x = [t.requires_grad_() for t in (q, k, v)]
+        (dq,) = torch.autograd.grad(smha.sink_attention(*x, 3), x[:1], g)
+        K, V, G = (t.detach().cpu().double() for t in (k, v, g))
+        seen = visible(S, S, 0, S, 3, 0)
+        P = seen.double() / seen.sum(1, keepdim=True)
+        O = P @ V
+        dS = P * (G @ V.mT - (G * O).sum(-1, keepdim=True))
+        e = P * 2 * (F + u * u) * (G.abs() @ V.abs().mT + (G * O).abs().sum(-1, keepdim=True)) + torch.where(seen, u * u * dS.abs() + 2 * z, 0.0)
+        dQ, bound = d ** -0.5 * dS @ K, d ** -0.5 * e @ K.abs()
+        assert off(dq, (dQ, bound + u * (dQ.abs() + bound) + z)) <= 1, seed
