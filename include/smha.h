@@ -378,6 +378,8 @@ smha_status_t smha_sink_backward(const void *Q, const void *K, const void *V, co
  *   weights         device, float [B][Hkv][Sk], strides {batch, head} (NULL = packed; rows apart): what attention each of a sequence's own keys
  *                   received, summed over the T tokens and H / Hkv heads, is added; NULL: not wanted
  *   window, n_sink  as in smha_sink_forward, in a sequence's own keys; a window together with a prefix is UNSUPPORTED
+ * (A position is a slot of the cache: where keys have moved, as smha_cache_evict moves them, `window` and `n_sink` still count slots, and a recent key
+ * that went to a low slot is outside the window.  Without a window the order of keys does not matter.)
  * Token t of sequence b stands at own key lengths[b] - T + t and sees the keys up to it (in its window, or sinks) and all of the
  * prefix.  Below 0 there is no such token: its output row is zero and it adds to no weight.
  * lengths are read by the kernels (nothing synchronises; a captured call follows them), which divide the keys of all sequences evenly
@@ -402,7 +404,8 @@ smha_status_t smha_cache_forward(const void *Q, const void *K, const void *V, co
  * (recent first: position > highest position - recent; then by weight, falling; then by slot, rising); recent keys and weights of
  * +inf are equals, and so are NaN and -inf.  Keys that stay keep their slots, but those in slots from `budget` on move, in order, to
  * the slots before it that were freed, with their weights and positions.  Slots from the new length on get weight 0 and
- * position -1; their keys and values stay as they are.
+ * position -1; their keys and values stay as they are.  (Slots are then no longer in the order of positions: smha_cache_forward with a window would count
+ * slots.)
  *   K, V            device, [B][Hkv][Sk][d], any 16-bit type, changed in place; strides as in smha_forward, but a head may be of any size;
  *                   no two heads in one place
  *   weights         device, float [B][Hkv][Sk], positions: int32 [B][Hkv][Sk], lengths: int32 [B]; packed

@@ -59,7 +59,8 @@ def cache_attention(q, k, v, lengths, *, window: int = 0, n_sink: int = 0, prefi
     q [B,H,T,d]: the new tokens, whose keys and values are in the cache; k, v [B,Hkv,Sk,d], H a multiple of Hkv; float16 or bfloat16, d a
     multiple of 8 up to 128.  lengths: int32 [B] on the GPU, keys of every sequence, the new tokens' included.  Token t of sequence b stands at
     lengths[b] - T + t (below 0: no such token, its output is zero) and sees the keys up to itself: the last `window` of them (0: all) and the
-    first `n_sink`.
+    first `n_sink`.  These are slots of the cache: after cache_evict, which moves keys, a window no longer holds the most recent tokens (without
+    a window the order of keys does not matter).
     prefix: (keys, values), each [Hkv,P,d]: tokens before those of every sequence, which all of them see (not with a window).
     weights: float32 [B,Hkv,Sk]; each key's attention, summed over the tokens and the heads that share it, is added to it.
     scale: 0 or less for 1/sqrt(d).  No gradients (sink_attention has them): no tensor given may require any.  Values that a token of the sequence
@@ -141,7 +142,8 @@ def cache_evict(k, v, weights, positions, lengths, budget: int, recent: int = 0,
     k, v [B,Hkv,Sk,d] as in cache_attention, changed in place; weights float32 and positions int32 [B,Hkv,Sk], lengths int32 [B], contiguous.  Where a
     sequence has more than `budget` keys, those of a head stay that are among the `recent` last positions (position > highest - recent), then
     those of the largest weight, the lower slot first among equals (recent keys count as of infinite weight, NaN as of the lowest).  Keys keep
-    their slots, except that those that stay past the budget move, in order, to the slots before it that were freed.  Slots from the
+    their slots, except that those that stay past the budget move, in order, to the slots before it that were freed: slots are then not in
+    the order of positions, and the window of cache_attention, which counts slots, is not one of tokens any more.  Slots from the
     new length on get weight 0 and position -1, and keep their keys.
     out: the three tensors to write to, by default new ones; they may be the inputs themselves.  No gradients."""
     if out is None and workspace is None and stream is None:

@@ -192,3 +192,18 @@ def test_a_backward_pass_keeps_to_its_workspace(case):
     for name, got in zip(("out", "dq", "dk", "dv"), (out, *grads)):
         check(got, want[name], name)
     assert bool((room[need:] == 0xAB).all())
+
+
+@pytest.mark.gpu
+def test_a_window_counts_slots_also_after_an_eviction():
+    """As documented: eviction moves recent keys to slots that were freed, where a window does not look for them; without one every key that stayed is seen."""
+    from test_cache import check, evict_inputs, int32, make, reference
+    k, v, w, _ = evict_inputs(2, 2, 80, 64)
+    positions = torch.arange(80, dtype=torch.int32, device="cuda").expand(2, 2, 80).contiguous()
+    q = make(2, 4, 2, 1, 80, 64)[0]
+    w, positions, n = smha.cache_evict(k, v, w, positions, int32([80, 61]), 32, 16)
+    recent = positions[:, :, :32] >= (n.new_tensor([80, 61]) - 16)[:, None, None]
+    assert bool((recent.sum(-1) == 16).all()) and not bool(recent[:, :, 16:].all())  # (they are there, but not in the last slots)
+    for window, n_sink in ((0, 0), (16, 0), (16, 4)):
+        want, bound, _ = reference(q, k, v, n.tolist(), window, n_sink)
+        check(smha.cache_attention(q, k, v, n, window=window, n_sink=n_sink), want, bound, f"window {window}")
