@@ -339,6 +339,8 @@ void smha_plan_destroy(smha_plan_t *plan); /* NULL is allowed */
  *   window          keys that a query sees, itself included; 0: all before it
  *   n_sink          first keys that every later query sees
  *   scale           <= 0 selects 1/sqrt(d)
+ * Scores, exponentials and sums are 32 bits; the probabilities, relative to about the largest, are rounded to `dtype` for the product with V (as in
+ * smha_forward), which adds as much again to O's own rounding.
  * offsets and lengths are read by the kernels: nothing synchronises, and a captured call follows their values.
  * Queries that do not exist give zero rows in O and dQ, keys at and past a sequence's length zero rows in dK
  * and dV; neither's values are read into any result, whatever they are.  Values that are visible to some query have to
@@ -358,7 +360,8 @@ smha_status_t smha_sink_workspace(int B, int H, int Hkv, int Sq, int Sk, int d, 
  * gradient of O.  The result does not depend on the order in which workgroups run: the parts of sums that were cut
  * are added in a fixed order.  P and dS = P (dP - delta) are rounded to `dtype` for the products that use them (of
  * at most 8192 queries in all that see few keys, dS to twice its digits): in binary16 the gradient of O has to be scaled (as such training
- * does) so that dS keeps within that type's range.  workspace: device, 16-byte aligned, smha_sink_workspace bytes or more; the
+ * does) so that dS keeps within that type's range, and P below 2^-14, where
+ * windows are very wide, have fewer digits (96 queries on 20000 keys: dV 1.64 times its own rounding from 64 bits, 1.42 on 1024).  workspace: device, 16-byte aligned, smha_sink_workspace bytes or more; the
  * call's alone until it has run. */
 smha_status_t smha_sink_backward(const void *Q, const void *K, const void *V, const void *O, const void *O_rest,
                                  const float *lse, const void *dO, void *dQ, void *dK, void *dV, int B, int H, int Hkv, int Sq, int Sk, int d,
@@ -382,6 +385,7 @@ smha_status_t smha_sink_backward(const void *Q, const void *K, const void *V, co
  * that went to a low slot is outside the window.  Without a window the order of keys does not matter.)
  * Token t of sequence b stands at own key lengths[b] - T + t and sees the keys up to it (in its window, or sinks) and all of the
  * prefix.  Below 0 there is no such token: its output row is zero and it adds to no weight.
+ * Roundings are those of smha_sink_forward; accounts are sums in 32 bits of unrounded probabilities.
  * lengths are read by the kernels (nothing synchronises; a captured call follows them), which divide the keys of all sequences evenly
  * over the chip whatever the lengths are.  The result does not depend on the order in which workgroups run.  Keys and values before every
  * token's window, past the length and past Sk are never read into a result; those that some token sees have to be finite (a NaN there may reach

@@ -150,3 +150,22 @@ def test_both_halves_of_ds_make_one_number(dtype, d):
         e = P * 2 * (F + u * u) * (G.abs() @ V.abs().mT + (G * O).abs().sum(-1, keepdim=True)) + torch.where(seen, u * u * dS.abs() + 2 * z, 0.0)
         dQ, bound = d ** -0.5 * dS @ K, d ** -0.5 * e @ K.abs()
         assert off(dq, (dQ, bound + u * (dQ.abs() + bound) + z)) <= 1, seed
+
+
+@pytest.mark.gpu
+@TYPES
+@pytest.mark.parametrize("case", [
+    (1, 2, 1, 96, 20000, 64, 0, 0),        # weights of 5e-5, which binary16 holds with fewer digits (z)
+    (1, 2, 2, 200, 6000, 128, 4096, 128),
+    (1, 4, 1, 3000, 3000, 64, 1024, 4),
+], ids=str)
+def test_gradients_over_long_windows(case, dtype):
+    B, H, Hkv, Sq, Sk, d, window, n_sink = case
+    q, k, v, g = tensors(B, H, Hkv, Sq, Sk, d, dtype)
+    want = reference(q, k, v, g, window, n_sink, None, None, 0.0)
+    x = [t.requires_grad_() for t in (q, k, v)]
+    out = smha.sink_attention(*x, window, n_sink)
+    for name, got in zip(("out", "dq", "dk", "dv"), (out, *torch.autograd.grad(out, x, g))):
+        worst = off(got, want[name])
+        print(name, worst, float((got.detach().cpu().double() - want[name][0]).norm() / want[name][0].norm()))
+        assert worst <= 1, name
