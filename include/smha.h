@@ -359,10 +359,10 @@ smha_status_t smha_sink_workspace(int B, int H, int Hkv, int Sq, int Sk, int d, 
 /* Gradients of Q, K and V (of `dtype`, written whole) from O, O_rest (or NULL) and lse of the forward with the same arguments and dO, the
  * gradient of O.  The result does not depend on the order in which workgroups run: the parts of sums that were cut
  * are added in a fixed order.  P and dS = P (dP - delta) are rounded to `dtype` for the products that use them (of
- * at most 8192 queries in all that see few keys, dS to twice its digits): in binary16 the gradient of O has to be scaled (as such training
- * does) so that dS keeps within that type's range, and P below 2^-14, where
- * windows are very wide, have fewer digits (96 queries on 20000 keys: dV 1.64 times its own rounding from 64 bits, 1.42 on 1024).  workspace: device, 16-byte aligned, smha_sink_workspace bytes or more; the
- * call's alone until it has run. */
+ * at most 8192 queries in all that see few keys, dS to twice its digits).  In binary16 the gradient of O has to be scaled (as such training
+ * does) so that dS keeps within that type's range, and P below 2^-14, where windows are very wide, has fewer digits (96 queries on 20000
+ * keys: dV 1.64 times its own rounding from 64 bits, on 1024 keys 1.42).  workspace: device, 16-byte aligned, smha_sink_workspace bytes or more;
+ * the call's alone until it has run. */
 smha_status_t smha_sink_backward(const void *Q, const void *K, const void *V, const void *O, const void *O_rest,
                                  const float *lse, const void *dO, void *dQ, void *dK, void *dV, int B, int H, int Hkv, int Sq, int Sk, int d,
                                  smha_dtype_t dtype, const int64_t q_strides[3], const int64_t k_strides[3],

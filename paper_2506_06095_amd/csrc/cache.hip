@@ -8,7 +8,8 @@
 // sequences are counted on the device and cut into as many segments, of about the same length, as workgroups fit the chip
 // (segments()); lengths are never needed on the host.  A workgroup's four waves take a segment's tiles in turn and join in LDS; segments
 // of the same rows are joined by a second kernel, in a fixed order, which also adds up the keys' accounts from the scores
-// that the first left in memory: 4 G T bytes a key where reading the key once more would take 2 d.
+// that the first left in memory: 8 G T bytes a key, written and read, where reading the key once more would take 2 d (less for up to d / 4 rows on a key
+// head, more beyond).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -255,7 +256,7 @@ __device__ __forceinline__ void prefix_wide(const CacheParams &p, const Segment 
 
 // K, V: one buffer of 32 keys each a wave, refilled as soon as its fragments are read: K of the next tile lands under this tile's softmax
 // and second product, V of the next under the next tile's scores.  Eight waves a compute unit at 128 columns, 16 at 64.
-// 32 x 32 on 8 x 16384 x 128, window 2048: 51 us, 5.3 TB/s; 8 x 32 on 8 x 8192 x 128, weighed: 47 us.
+// 32 x 32 on 8 x 16384 x 128, window 2048: 52 us, 5.1 TB/s; 8 x 32 on 8 x 8192 x 128, weighed: 48 us.
 // Probabilities are rounded to the inputs' type for the second product (half a step each, as in smha_sink_fwd); sums are 32 bits.
 // Forms: segments cut over the chip; with the wide segments of a prefix too (whose registers leave a workgroup less to a unit at 64 columns); or,
 // where a group has few tiles whatever the lengths are, a workgroup a group, which reads the prefix's keys and the sequence's own one after the
@@ -692,7 +693,7 @@ __device__ __forceinline__ uint32_t ordered(float x) {
 // and a register's order is the slots' order.  The budget-th largest is found by counting, 11, 11 and 10 bits at a time, in a
 // histogram in LDS (11 bits of a float are a quarter of an octave: lanes of a wave meet in few bins but seldom all in one, and where
 // they do one of them counts for all); of the keys that equal it the first slots stay.  What stays past the new end goes, in
-// order, where keys before it left.  32 heads of 32768 keys 27 us.  (Counting with ballots, two bits at a time: 110;
+// order, where keys before it left.  32 heads of 32768 keys 27.5 us.  (Counting with ballots, two bits at a time: 110;
 // with a branch for each of a key's conditions: 30.)
 // WHOLE: the rows are moved here too, which saves a launch where few move (evict_whole); their lists then take the histogram's place in LDS.
 constexpr int kWholeMoves = 512;
@@ -966,7 +967,7 @@ __global__ void __launch_bounds__(1024) smha_cache_select(const EvictParams p) {
 }
 
 // K and V rows along the lists: what is read lies past the new end, what is written before it.  And what lies past it afterwards.  Bound by memory: 32
-// heads of 32768 keys x 128 to 2048: 71 MB, 14.6 us.
+// heads of 32768 keys x 128 to 2048: 71 MB, 15.2 us.
 __global__ void __launch_bounds__(256) smha_cache_move(const EvictParams p) {
     const int bh = blockIdx.y, b = bh / p.Hkv, hk = bh - b * p.Hkv;
     const int end = min(min(max(p.lengths[b], 0), p.Sk), p.budget);  // (the same where len_out is lengths and has been written already)
@@ -1000,9 +1001,9 @@ static Strides cache_strides(const int64_t *s, int64_t heads, int64_t rows, int 
 }
 
 // Tiles of a group up to which a workgroup takes it whole.  Cutting costs a second launch and shares out what one workgroup would read alone (0.37 us a
-// tile); where groups fill the chip by themselves there is little to share.  us of a call, direct and cut: 2 groups x 64 of 500, 700, 1000 and 1500
-// keys: 8.8, 8.9, 10.7, 14.1 and 12.2 (replayed from a graph: 7.0, 8.4, 10.3, 13.6 and 8.5); 32 x 128 of 500, 700, 1000: 9.9, 12.1, 14.8 and 12.2; 128 x 128
-// of 1000: 17.3, 19.4; 512 x 128 of 700, 1000 and 1500: 30, 42, 70 and 35, 47, 75, of 30 to 100 % of those lengths 23, 30, 43 and 31, 37, 50.  No more than 48: with
+// tile); where groups fill the chip by themselves there is little to share.  us of a call, direct and cut: 2 groups x 64 of 256, 500, 700,
+// 1000 and 1500 keys: 5.5, 7.2, 8.8, 10.7, 14.1 and 9.0 to 9.3; 32 x 128 of 500, 700, 1000: 9.8, 12.1, 14.8 and 10.9; 128 x 128
+// of 1000: 17.2, 19.5; 512 x 128 of 700, 1000 and 1500: 31, 43, 70 and 35, 48, 75, of 30 to 100 % of those lengths 23, 30, 44 and 31, 37, 50.  No more than 48: with
 // one long sequence among short ones it is the longest that counts.  (A prefix that many groups read is better shared.)
 static int64_t direct_tiles(int d, int P, int64_t groups) { return std::min<int64_t>(48, (d <= 64 ? 24 : 16) + (P ? 0 : groups / 8)); }
 

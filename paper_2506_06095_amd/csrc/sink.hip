@@ -164,9 +164,9 @@ __device__ __forceinline__ void load_operand(u32x4 (&f)[C / 16], const uint16_t 
 // A workgroup is four waves of 32 queries; they share 64-key tiles of K and V, two of each in LDS (the next lands while one is used).
 // The tiles are those of the sinks and those of the window of any of the 128 queries; a wave passes over tiles that its own
 // queries do not see, and forms masks only on tiles that they see in part.
-// P is rounded to the inputs' type for the second product: half a step, 2^-9 (bfloat16) or 2^-12 (binary16) of each weight, independent
+// P is rounded to the inputs' type for the second product: half a step, 2^-8 (bfloat16) or 2^-11 (binary16) of each weight at most, independent
 // from weight to weight, which leaves the output as far off as its own rounding does.  Sums and statistics are 32 bits.
-// Bound by power: 1 x 32 on 8 x 8192 x 128, window 4096, 128 sinks: 435 us, matrix pipes busy half of the cycles at 2.0 GHz (55 % in a large library
+// Bound by power: 1 x 32 on 8 x 8192 x 128, window 4096, 128 sinks: 419 us, matrix pipes busy half of the cycles at 2.0 GHz (55 % in a large library
 // product).  Waves in the mixed phase (masks, exponentials, second product) go first.
 template <int D, int C, bool BF16>
 __global__ void __launch_bounds__(256, D == 64 ? 4 : 2) smha_sink_fwd(const SinkParams p) {
@@ -314,7 +314,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 4 : 2) smha_sink_fwd(const Sink
 // delta from the rounded output alone is as far off as dS is by its own rounding: dQ and dK 1.52 times as far from 64 bits as an evaluation in
 // 32 bits that is rounded once, 1.42 times with what the rounding left out.
 // dS is rounded to the inputs' type for the product with K, as P is in the forward; FINE (see fine_ds): its rounding error is multiplied too.
-// 575 us for the forward's case above, matrix pipes busy 59 %.
+// 563 us for the forward's case above, matrix pipes busy 59 %.
 template <int D, int C, bool BF16, bool FINE>
 __global__ void __launch_bounds__(256, 2) smha_sink_bwd_q(const SinkParams p) {
     constexpr int NS = C / 16, NDT = C / 32, TB = 64 * D * 2, PF = C == 128 ? 6 : 4;
@@ -488,7 +488,7 @@ __device__ __forceinline__ int parts_of(int steps, int cut, int chunk) { return 
 // dK and dV: four waves of 32 keys each over 32-query tiles of Q and dO (and their lse and delta) in LDS, two of each.  A lane owns a key.
 // At 128 columns a wave holds 128 registers of dK and dV; V's 32 beside them leave room for operands that are requested four products
 // ahead, K's do not, and so K stays in LDS (with both in registers every product waited for its operand, and what had spilled was waited for
-// with the tile in flight: 1090 us for the case above, 860 so, matrix pipes busy 49 %).  The exponentials run under the product that gives
+// with the tile in flight: 1062 us for the case above, 815 so, matrix pipes busy 49 %).  The exponentials run under the product that gives
 // dP, the rest of dS under the one that gives dV.
 // A tile's steps (its queries, head by head) may be cut into parts that other workgroups take: the sinks' tiles are seen by every
 // query, and few key heads would leave most of the chip idle.  Parts go to memory in 32 bits and are added in order by smha_sink_sum.
@@ -788,7 +788,7 @@ static bool sink_grids_fit(const SinkParams &sp) {
 // Whether dS goes into dQ and dK with what its rounding leaves out.  dQ and dK of rounded dS are 1.44 times as far from 64 bits as their own
 // rounding on average; of few queries, where a few large rows make most of the norm, up to 1.50 (2 x 12 x 68 x 64).  There both halves are
 // multiplied, a product more of three and of four: 1.05 (1.10 where windows are shortest).  us of a backward pass without and with them: 2 x 4 x 128 x 64, window 16: 15.6,
-// 16.4; 1 x 8 x 1024 x 64, window 256: 28.8, 30.9; 1 x 8 x 700 x 128: 48.9, 54.2; 1 x 2 x 1400 x 128: 73.2, 80.8 (most of which the host's 70 us
+// 16.4; 1 x 8 x 1024 x 64, window 256: 28.1, 30.3; 1 x 8 x 700 x 128: 47.8, 52.4; 1 x 2 x 1400 x 128: 68.7, 76.7 (most of which the host's 65 us
 // for a pass hide).  Of more queries errors average out, and products are what such a call lasts.
 static bool fine_ds(const SinkParams &sp) { const int64_t queries = (int64_t)sp.B * sp.H * sp.Sq;
     return queries <= 8192 && queries * std::min<int64_t>(sp.Sk, (int64_t)sp.window + sp.n_sink) <= 1 << 22; }
