@@ -147,6 +147,10 @@ def _takes(t):
     return s[3] == 1 and all(n == 1 or step % 8 == 0 for n, step in zip((b, h, rows), s)) and pitch >= d and ((rows + 128) * pitch + d) * 2 < 1 << 31
 
 
+def _readable(t):
+    return t if _takes(t) else t.clone(memory_format=torch.contiguous_format)
+
+
 class _SinkAttention(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, v, window, n_sink, offsets, lengths, scale):
@@ -164,7 +168,7 @@ class _SinkAttention(torch.autograd.Function):
         q, k, v, out, rest, lse, offsets, lengths = ctx.saved_tensors
         window, n_sink, scale = ctx.rest
         dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
-        smha_sink_backward(q, k, v, out, lse, grad if _takes(grad) else grad.contiguous(), dq, dk, dv, window, n_sink, offsets, lengths, scale,
+        smha_sink_backward(q, k, v, out, lse, _readable(grad), dq, dk, dv, window, n_sink, offsets, lengths, scale,
                            O_rest=rest)
         return dq, dk, dv, None, None, None, None, None
 

@@ -110,3 +110,14 @@ def test_forward_mode_is_refused(monkeypatch, native, requires_grad):
                 print(i, call())
         assert torch.equal(smha.cache_attention(q, k, v, n, prefix=prefix), smha.cache_attention(q, keys, v, n, prefix=prefix))
     assert torch.equal(k, keys) and bool((weights == 0).all())
+
+
+@pytest.mark.gpu
+@WAYS
+def test_a_packed_gradient_that_begins_anywhere(monkeypatch, native):
+    general_way(monkeypatch, native)
+    x = [randn(1, h, 3, 64, seed=i).requires_grad_() for i, h in enumerate((2, 1, 1))]
+    g = randn(2 * 3 * 64 + 1, seed=9)[1:].view(1, 2, 3, 64)
+    assert g.is_contiguous() and g.data_ptr() % 16
+    want = torch.autograd.grad(smha.sink_attention(*x, 2, 1), x, g.clone())
+    assert all(torch.equal(a, b) for a, b in zip(torch.autograd.grad(smha.sink_attention(*x, 2, 1), x, g), want))
