@@ -206,8 +206,8 @@ at::Tensor packed_like(const at::Tensor &t) { return at::empty(t.sizes(), t.opti
 
 int64_t lse_bytes(const at::Tensor &q) { return (q.size(0) * q.size(1) * q.size(2) * 4 + 15) / 16 * 16; }
 
-// Whether smha_sink_backward reads a gradient as it lies: autograd may hand on expanded and transposed ones, and such of more than 2 GiB between a
-// head's first and last row.
+// Whether smha_sink_backward reads a tensor as it lies: autograd may hand on gradients that are expanded, transposed, or of more than 2 GiB between a
+// head's first and last row, and hooks of saved tensors may give those back with other strides.
 bool taken(const at::Tensor &g) {
     if (reinterpret_cast<uintptr_t>(g.data_ptr()) % 16) return false;
     const Strides3 s(g);
@@ -215,6 +215,8 @@ bool taken(const at::Tensor &g) {
     return s.ok && s.s[0] % 8 == 0 && s.s[1] % 8 == 0 && s.s[2] % 8 == 0 && s.s[2] >= g.size(3) && s.s[2] <= INT32_MAX &&
            ((g.size(2) + 128) * s.s[2] + g.size(3)) * 2 <= INT32_MAX;
 }
+
+at::Tensor readable(const at::Tensor &t) { return taken(t) ? t : t.clone(at::MemoryFormat::Contiguous); }
 
 // The backward pass of one call.
 struct SinkBackward : torch::autograd::Node {
@@ -231,12 +233,14 @@ struct SinkBackward : torch::autograd::Node {
     torch::autograd::variable_list apply(torch::autograd::variable_list &&grads) override {
         const std::lock_guard<std::mutex> lock(mutex_);
         if (!grads[0].defined()) return torch::autograd::variable_list(3);
-        const at::Tensor q = q_.unpack(), k = k_.unpack(), v = v_.unpack(), o = o_.unpack(shared_from_this()), kept = kept_.unpack(),
-                         offsets = offsets_.unpack(), lengths = lengths_.unpack();
+        at::Tensor q = q_.unpack(), k = k_.unpack(), v = v_.unpack(), o = o_.unpack(shared_from_this()), kept = kept_.unpack(), offsets = offsets_.unpack(),
+                   lengths = lengths_.unpack();
         at::Tensor g = grads[0].detach(), dq, dk, dv;
         {
             const at::AutoGradMode off(false);
-            if (!taken(g)) g = g.clone(at::MemoryFormat::Contiguous);
+            for (at::Tensor *t : {&q, &k, &v, &g}) *t = readable(*t);
+            for (at::Tensor *t : {&o, &kept, &offsets, &lengths})
+                if (t->defined()) *t = t->contiguous();
             dq = packed_like(q);
             dk = packed_like(k);
             dv = packed_like(v);

@@ -136,8 +136,8 @@ def smha_sink_backward(Q, K, V, O, lse, dO, dQ, dK, dV, window: int = 0, n_sink:
 
 
 def _takes(t):
-    """Whether the kernels can read a gradient as it lies (autograd may hand on expanded or transposed ones, and such of more than 2 GiB between a
-    head's first and last row)."""
+    """Whether the kernels can read a tensor as it lies (autograd may hand on gradients that are expanded or transposed or of more than 2 GiB between a
+    head's first and last row, and hooks of saved tensors may give those back with other strides)."""
     if t.data_ptr() % 16:
         return False
     if t.is_contiguous():
@@ -165,7 +165,9 @@ class _SinkAttention(torch.autograd.Function):
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, grad):
-        q, k, v, out, rest, lse, offsets, lengths = ctx.saved_tensors
+        saved = ctx.saved_tensors
+        q, k, v, out = (_readable(t) for t in saved[:4])
+        rest, lse, offsets, lengths = (t if t is None else t.contiguous() for t in saved[4:])
         window, n_sink, scale = ctx.rest
         dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
         smha_sink_backward(q, k, v, out, lse, _readable(grad), dq, dk, dv, window, n_sink, offsets, lengths, scale,

@@ -121,3 +121,33 @@ def test_a_packed_gradient_that_begins_anywhere(monkeypatch, native):
     assert g.is_contiguous() and g.data_ptr() % 16
     want = torch.autograd.grad(smha.sink_attention(*x, 2, 1), x, g.clone())
     assert all(torch.equal(a, b) for a, b in zip(torch.autograd.grad(smha.sink_attention(*x, 2, 1), x, g), want))
+
+
+@pytest.mark.gpu
+@WAYS
+def test_hooks_may_give_back_saved_tensors_of_any_layout(monkeypatch, native):
+    """One after the other, a saved tensor comes back with the same values and other strides: the same gradients."""
+    general_way(monkeypatch, native)
+    x = [randn(2, h, 40, 64, seed=i).requires_grad_() for i, h in enumerate((4, 2, 2))]
+    g = randn(2, 4, 40, 64, seed=5)
+    offsets, lengths = (torch.tensor(t, dtype=torch.int32, device="cuda") for t in ([0, -3], [40, 30]))
+    saved = []
+
+    def grads(which):
+        saved.clear()
+
+        def unpack(at):
+            i, t = at
+            if i != which:
+                return t
+            return t.mT.contiguous().mT if t.dim() > 1 else torch.stack([t, torch.zeros_like(t)], 1)[:, 0]
+
+        with torch.autograd.graph.saved_tensors_hooks(lambda t: (saved.append(t), (len(saved) - 1, t))[1], unpack):
+            out = smha.sink_attention(*x, 16, 2, offsets=offsets, lengths=lengths)
+        return torch.autograd.grad(out, x, g)
+
+    want = grads(None)
+    n = len(saved)
+    assert n >= 7
+    for which in range(n):
+        assert all(torch.equal(a, b) for a, b in zip(grads(which), want)), (which, saved[which].shape)
