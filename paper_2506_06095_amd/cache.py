@@ -10,7 +10,7 @@ import ctypes as C
 import torch
 
 from .binding import SmhaError, _load, native_call
-from .sink import _CODES, _check_int, _check_no_tangents, _check_per_sequence, _check_qkv, _handle, _on_device, _strides
+from .sink import _CODES, _check_int, _check_no_tangents, _check_per_sequence, _check_qkv, _handle, _on_device, _strides, _written
 
 
 _attention = _evict = None  # functions of _smha_torch
@@ -23,13 +23,6 @@ def _allocating_on(stream, given):
     if not isinstance(stream, torch.cuda.Stream):
         raise ValueError("a call on a bare stream handle needs its workspace and outputs")
     return torch.cuda.stream(stream)
-
-
-def _written(*tensors):
-    """Autograd refuses to go back through what was saved of a tensor that was written since."""
-    for t in tensors:
-        if t is not None and not t.is_inference():
-            torch.autograd.graph.increment_version(t)
 
 
 def _check_no_gradients(name, *tensors):

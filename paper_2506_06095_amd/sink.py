@@ -71,6 +71,13 @@ def _check_int(value, name):
     return value
 
 
+def _written(*tensors):
+    """Autograd refuses to go back through what was saved of a tensor that was written since."""
+    for t in tensors:
+        if t is not None and not t.is_inference():
+            torch.autograd.graph.increment_version(t)
+
+
 def _check_rest(rest, like):
     if rest is not None and (rest.shape != like.shape or rest.dtype != like.dtype or rest.device != like.device or not rest.is_contiguous()):
         raise ValueError("O_rest must be a contiguous tensor like O")
@@ -95,6 +102,7 @@ def smha_sink_forward(Q, K, V, O, lse=None, window: int = 0, n_sink: int = 0, of
                                        _check_int(window, "window"), _check_int(n_sink, "n_sink"), float(scale), _handle(stream, Q.device))
     if st != 0:
         raise SmhaError(st, "smha_sink_forward")
+    _written(O, lse, O_rest)
 
 
 def smha_sink_workspace(B: int, H: int, Hkv: int, Sq: int, Sk: int, d: int, window: int = 0, n_sink: int = 0) -> int:
@@ -133,6 +141,7 @@ def smha_sink_backward(Q, K, V, O, lse, dO, dQ, dK, dV, window: int = 0, n_sink:
                                         workspace.data_ptr(), workspace.numel(), _handle(stream, Q.device))
     if st != 0:
         raise SmhaError(st, "smha_sink_backward")
+    _written(dQ, dK, dV)
 
 
 def _takes(t):

@@ -151,3 +151,22 @@ def test_hooks_may_give_back_saved_tensors_of_any_layout(monkeypatch, native):
     assert n >= 7
     for which in range(n):
         assert all(torch.equal(a, b) for a, b in zip(grads(which), want)), (which, saved[which].shape)
+
+
+@pytest.mark.gpu
+def test_autograd_notices_what_the_entry_points_write():
+    """A tensor that was saved for a backward pass and then written by smha_sink_forward or smha_sink_backward."""
+    q, k, v, g = randn(1, 2, 8, 64, seed=1), randn(1, 1, 8, 64, seed=2), randn(1, 1, 8, 64, seed=3), randn(1, 2, 8, 64, seed=4)
+    new = {"O": torch.zeros_like(q), "lse": torch.zeros(1, 2, 8, device="cuda"), "O_rest": torch.zeros_like(q), "dQ": torch.zeros_like(q), "dK": torch.zeros_like(k),
+           "dV": torch.zeros_like(v)}
+    factors = {name: torch.ones_like(t).requires_grad_() for name, t in new.items()}
+    later = {name: (factors[name] * t).sum() for name, t in new.items()}
+    smha.smha_sink_forward(q, k, v, new["O"], new["lse"], 4, 1, O_rest=new["O_rest"])
+    smha.smha_sink_backward(q, k, v, new["O"], new["lse"], g, new["dQ"], new["dK"], new["dV"], 4, 1, O_rest=new["O_rest"])
+    for name, value in later.items():
+        with pytest.raises(RuntimeError, match="inplace"):
+            print(name, torch.autograd.grad(value, factors[name]))
+    with torch.inference_mode():  # (whose tensors count no versions)
+        o = torch.empty_like(q)
+        smha.smha_sink_forward(q, k, v, o, window=4, n_sink=1)
+    assert torch.equal(o, new["O"])
