@@ -344,7 +344,8 @@ void smha_plan_destroy(smha_plan_t *plan); /* NULL is allowed */
  * offsets and lengths are read by the kernels: nothing synchronises, and a captured call follows their values.
  * Queries that do not exist give zero rows in O and dQ, keys at and past a sequence's length zero rows in dK
  * and dV; neither's values are read into any result, whatever they are.  Values that are visible to some query have to
- * be finite (a NaN or infinity there may reach other queries of the same 128).
+ * be finite (a NaN or infinity there may reach other queries of the same 128, and one in Q or dO of a query that exists the gradients of
+ * keys that this query does not see).
  * Errors: INVALID_ARG (null, sizes, a negative window or n_sink, too small a workspace), SHAPE (H no multiple of Hkv),
  * UNSUPPORTED (d, dtype, alignment, strides, sizes), HIP.  Enqueues on hip_stream, on the current device. */
 smha_status_t smha_sink_forward(const void *Q, const void *K, const void *V, void *O, float *lse, void *O_rest, int B, int H,
@@ -404,7 +405,7 @@ smha_status_t smha_cache_forward(const void *Q, const void *K, const void *V, co
 
 /* ---- Eviction from a cache by accumulated attention ----
  *
- * Every key head of every sequence keeps min(lengths[b], budget) keys.  Where it has more, keys stay in the order of
+ * Every key head of every sequence keeps min(lengths[b], budget) keys (lengths taken as 0 or Sk where outside 0 .. Sk).  Where it has more, keys stay in the order of
  * (recent first: position > highest position - recent; then by weight, falling; then by slot, rising); recent keys and weights of
  * +inf are equals, and so are NaN and -inf.  Keys that stay keep their slots, but those in slots from `budget` on move, in order, to
  * the slots before it that were freed, with their weights and positions.  Slots from the new length on get weight 0 and
