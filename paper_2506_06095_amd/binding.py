@@ -129,7 +129,7 @@ def _load():
 
 
 _native = None  # (forward of _smha_torch, address of smha_forward)
-_loading = threading.Lock()
+_loading = threading.RLock()
 _LINKED = ("sink_forward", "sink_backward", "sink_workspace", "cache_forward", "cache_workspace", "cache_evict", "cache_evict_workspace")  # in link()'s order
 
 
@@ -153,8 +153,8 @@ def _load_native():
                 _smha_torch.link(*(C.cast(getattr(lib, f"smha_{name}"), C.c_void_p).value for name in _LINKED))
                 _native = (_smha_torch.forward, C.cast(lib.smha_forward, C.c_void_p).value)
             except (ImportError, OSError, subprocess.SubprocessError) as e:
+                _native = (_left_to_python, 0)  # (before the warning: what shows it may make a call)
                 warnings.warn(f"no native call path for Plan.forward, every call takes the slower one through ctypes: {e}", RuntimeWarning)
-                _native = (_left_to_python, 0)
         return _native
 
 

@@ -207,3 +207,28 @@ def test_a_window_counts_slots_also_after_an_eviction():
     for window, n_sink in ((0, 0), (16, 0), (16, 4)):
         want, bound, _ = reference(q, k, v, n.tolist(), window, n_sink)
         check(smha.cache_attention(q, k, v, n, window=window, n_sink=n_sink), want, bound, f"window {window}")
+
+
+def test_a_warning_of_the_first_call_may_call_again(monkeypatch, tmp_path):
+    """What shows the warning that there is no native path (a log, say) may itself make a call."""
+    import threading
+    import warnings
+    from paper_2506_06095_amd import binding
+    monkeypatch.setattr(binding, "_native", None)
+    monkeypatch.setattr(binding._build, "EXT", str(tmp_path / "_smha_torch.so"))
+    monkeypatch.setenv("CXX", "false")
+    shown = []
+
+    def show(*args, **kwargs):
+        shown.append(binding.native_call("cache_evict")())
+
+    def call():
+        with warnings.catch_warnings():
+            warnings.simplefilter("always")
+            warnings.showwarning = show
+            binding.native_call("cache_evict")
+
+    thread = threading.Thread(target=call, daemon=True)
+    thread.start()
+    thread.join(20)
+    assert not thread.is_alive() and shown == [None]
