@@ -425,6 +425,62 @@ smha_status_t smha_cache_evict(void *K, void *V, const float *weights, const int
                                int budget, int recent, const int64_t k_strides[3], const int64_t v_strides[3], void *workspace,
                                size_t workspace_bytes, void *hip_stream);
 
+/* ---- A cache held in 4 bits ----
+ *
+ * A packed row stands for the d columns of one key or value (d a multiple of 8 up to 128), 32 at a time: each group of 32 columns (the last may have
+ * 8, 16 or 24) has a step s and a base m, both binary16, and every column a code c of 0 .. 15, which stands for the binary16 nearest
+ * (ties to even) to c s + m.  The row is smha_packed_row(d) = 4 ceil(d / 32) + d / 2 bytes: (s, m) of each group, then d / 8 words of 32 bits, little
+ * endian, in which columns 0, 2, 4 and 6 of 8 begin at bits 0, 4, 8 and 12, and columns 1, 3, 5 and 7 at bits 16, 20, 24 and 28.  (80 bytes for
+ * 128 columns: 5 bits a value.)
+ * How rows are packed: values beyond +-65280, infinities among them, are taken as +-65280; m is the largest binary16 that is not above the group's
+ * least value (-0 counts as 0), s the smallest with which 15 s + m is not below its largest; c is the number of k in 0 .. 14 for which the value is at
+ * least m + (k + 1/2) s, and 0 where s is 0.  All of it exactly, so that equal inputs give equal bytes.  A value is packed within s / 2 and half a last place
+ * of binary16.  A group that holds a NaN stands for NaN throughout.
+ *
+ *   K, V            device, [B][Hkv][Sk][row] bytes: packed rows; *_strides in bytes, {batch, head, key} (NULL = packed), multiples of 4, no row
+ *                   over another where they are written; 4-byte aligned; less than 2 GiB between a head's first and last byte
+ *   lengths         device, int32 [B]: keys of every sequence, the new tokens' included (taken as 0 or Sk where outside 0 .. Sk)
+ *   offsets         device, int32 [B]
+ * lengths and offsets are read by the kernels: nothing synchronises, and a captured call follows them.  What lies in slots from a length on is never
+ * read into a result.
+ * Errors: INVALID_ARG (null, sizes, K the same as V where they are written, too small a workspace), SHAPE (H no multiple of Hkv), UNSUPPORTED (d, dtype, alignment,
+ * strides, sizes), HIP.  Enqueue on hip_stream, on the current device. */
+
+/* Bytes of a packed row. */
+smha_status_t smha_packed_row(int d, int *bytes);
+
+/* Packs new tokens' keys and values into their slots: token t of sequence b into slot offsets[b] + t (offsets NULL: lengths[b] - T + t), where that is in 0 ..
+ * lengths[b] - 1; other tokens are left out, other slots as they are.
+ *   K_new, V_new    device, [B][Hkv][T][d] of `dtype` (F16 or BF16); strides and alignment as in smha_sink_forward
+ *   K_values, V_values  device, [B][Hkv][T][d] of `dtype`, packed as tensors are (no strides): what the tokens' rows stand for, rounded once more for BF16, zero where a
+ *                   token is left out; both NULL: not wanted.  May be K_new and V_new themselves where these have no strides */
+smha_status_t smha_packed_write(const void *K_new, const void *V_new, void *K, void *V, void *K_values, void *V_values,
+                                const int32_t *lengths, const int32_t *offsets, int B, int Hkv, int T, int Sk, int d,
+                                smha_dtype_t dtype, const int64_t kn_strides[3], const int64_t vn_strides[3],
+                                const int64_t k_strides[3], const int64_t v_strides[3], void *hip_stream);
+
+/* What T slots of every sequence from slot offsets[b] (NULL: 0) on stand for; zeros where a slot is not in 0 .. lengths[b] - 1.
+ *   K_out, V_out    device, [B][Hkv][T][d] of `out_dtype` (F16 and F32: the values; BF16: rounded to it); strides in elements, rows 16-byte aligned,
+ *                   none over another, less than 2 GiB a head */
+smha_status_t smha_packed_read(const void *K, const void *V, void *K_out, void *V_out, const int32_t *lengths, const int32_t *offsets,
+                               int B, int Hkv, int T, int Sk, int d, smha_dtype_t out_dtype, const int64_t k_strides[3],
+                               const int64_t v_strides[3], const int64_t ko_strides[3], const int64_t vo_strides[3],
+                               void *hip_stream);
+
+/* smha_cache_forward (without a prefix and accounts) on packed rows: attention of the last T tokens of every sequence, whose rows are in the cache, one
+ * or a chunk of a prompt.  Q, O: [B][H][T][d] of `dtype`, scale, window and n_sink as there.
+ * Products are formed of Q and the rows' values, both as they are (bfloat16 queries as binary16 times a power of two, by which columns below 2^-31 of a query's largest lose
+ * digits); sums and exponentials are 32 bits; the probabilities, relative to about the largest, are rounded to binary16 for the product with V, whatever
+ * `dtype` is.  The result does not depend on the order in which workgroups run.  Keys before every token's window and past every token's place are never
+ * read into a result; those that some token sees have to stand for something finite (a NaN there may reach other tokens of the sequence).
+ * workspace: device, 16-byte aligned, smha_packed_workspace bytes or more (0, and then NULL will do, where there are few keys); the call's
+ * alone until it has run. */
+smha_status_t smha_packed_workspace(int B, int H, int Hkv, int T, int Sk, int d, int window, int n_sink, size_t *need);
+smha_status_t smha_packed_forward(const void *Q, const void *K, const void *V, void *O, const int32_t *lengths, int B, int H, int Hkv,
+                                  int T, int Sk, int d, smha_dtype_t dtype, const int64_t q_strides[3], const int64_t k_strides[3],
+                                  const int64_t v_strides[3], const int64_t o_strides[3], int window, int n_sink, float scale,
+                                  void *workspace, size_t workspace_bytes, void *hip_stream);
+
 const char *smha_status_string(smha_status_t status);
 
 /* Symbol names of kernels, for matching profiler output (name and duration bookkeeping is left to the caller).

@@ -1,9 +1,9 @@
 """smha: masked multi-head attention for MI355X (gfx950) behind a C ABI.
 
-Beside plans: attention with a window and sinks (`sink`), on a cache, and eviction from it (`cache`).
+Beside plans: attention with a window and sinks (`sink`), on a cache, and eviction from it (`cache`), and a cache held in 4 bits (`packed`).
 
 The compute lives in libsmha.so (HIP); this package is the thin ctypes binding
-(`binding`, `sink`, `cache`) and the in-tree build step (`build`).  There is no CPU fallback: if
+(`binding`, `sink`, `cache`, `packed`) and the in-tree build step (`build`).  There is no CPU fallback: if
 the library is missing or no GPU is usable, calls raise.
 """
 from .binding import (  # noqa: F401
@@ -14,7 +14,8 @@ from .binding import (  # noqa: F401
     smha_plan_from_desc, smha_plan_info, smha_plan_prepare, smha_plan_work_order, smha_status_string)
 
 _OPERATORS = {**{name: "sink" for name in ("sink_attention", "smha_sink_backward", "smha_sink_forward", "smha_sink_workspace")},
-              **{name: "cache" for name in ("cache_attention", "cache_evict", "smha_cache_evict_workspace", "smha_cache_workspace")}}
+              **{name: "cache" for name in ("cache_attention", "cache_evict", "smha_cache_evict_workspace", "smha_cache_workspace")},
+              **{name: "packed" for name in ("packed_attention", "packed_cache", "packed_read", "packed_write", "smha_packed_row", "smha_packed_workspace")}}
 
 
 def __getattr__(name):  # (these modules need torch when they are imported, which plans on the host do not)

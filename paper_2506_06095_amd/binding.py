@@ -115,6 +115,13 @@ def _load():
     lib.smha_cache_evict.argtypes = [vp] * 8 + [i] * 6 + [i64p] * 2 + [vp, C.c_size_t, vp]
     for entry in ("workspace", "forward", "evict_workspace", "evict"):
         getattr(lib, f"smha_cache_{entry}").restype = i
+    lib.smha_packed_row.argtypes = [i, C.POINTER(i)]
+    lib.smha_packed_write.argtypes = [vp] * 8 + [i] * 6 + [i64p] * 4 + [vp]
+    lib.smha_packed_read.argtypes = [vp] * 6 + [i] * 6 + [i64p] * 4 + [vp]
+    lib.smha_packed_workspace.argtypes = [i] * 8 + [C.POINTER(C.c_size_t)]
+    lib.smha_packed_forward.argtypes = [vp] * 5 + [i] * 7 + [i64p] * 4 + [i, i, C.c_float, vp, C.c_size_t, vp]
+    for entry in ("row", "write", "read", "workspace", "forward"):
+        getattr(lib, f"smha_packed_{entry}").restype = i
     lib.smha_sink_forward.restype = lib.smha_sink_workspace.restype = lib.smha_sink_backward.restype = i
     lib.smha_plan_destroy.argtypes = [vp]
     lib.smha_plan_destroy.restype = None

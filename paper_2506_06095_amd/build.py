@@ -17,7 +17,7 @@ LIB = os.path.join(HERE, "libsmha.so")
 EXT = os.path.join(HERE, "_smha_torch.so")
 EXT_SOURCE = os.path.join(CSRC, "torch_binding.cpp")
 ABI_HEADER = os.path.join(ROOT, "include", "smha.h")
-SOURCES = ["kernels.hip", "sink.hip", "cache.hip", "plan.cpp"]
+SOURCES = ["kernels.hip", "sink.hip", "cache.hip", "packed.hip", "plan.cpp"]
 HEADERS = ["smha_internal.hpp", "device_common.hpp", "device_pool.hpp", "block_fwd2.inc", "block_fwd16.inc", "wave_fwd.inc", ABI_HEADER]
 
 
@@ -43,7 +43,7 @@ def compile_and_link(extra=()) -> None:
     """Every source on its own, side by side, then one library; it takes its place when it is whole."""
     with tempfile.TemporaryDirectory() as tmp:
         objects = [os.path.join(tmp, f"{s}.o") for s in SOURCES]
-        with ThreadPoolExecutor(4) as pool:
+        with ThreadPoolExecutor(len(SOURCES)) as pool:
             list(pool.map(lambda so: subprocess.run(command(*so, extra), check=True), zip(SOURCES, objects)))
         part = os.path.join(tmp, "lib.so")
         subprocess.run([hipcc(), "--offload-arch=gfx950", "-shared", "-pthread", *objects, "-o", part], check=True)

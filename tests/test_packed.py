@@ -1,0 +1,347 @@
+"""A cache held in 4 bits: packing against the format's definition, byte for byte; reading back, bit for bit; attention against its formula in 64 bits on
+the values that the rows stand for; all of them together as a serving loop runs them; and refusals.
+
+Tolerance of an output of attention: u |O| (its rounding) + sum_j (2^-11 P + 2^-25) |V| (the probabilities' rounding to binary16, whatever the type;
+relative to a reference that is no larger than the largest score, they sum to 1 at least) + F sum_j P |V|, with u half a step of the type and F = 2e-5
+for sums and exponentials in 32 bits (scores stay below 60, whose exponents are rounded by 60 log2(e) 2^-24 = 5e-6, and are sums of 128 products
+of which no partial sum passes 60 sqrt(128): another 60 * 2^-24 * 2).  Keys and values are what the rows stand for, exactly.
+"""
+import math
+
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import paper_2506_06095_amd as smha  # noqa: E402
+
+F = 2e-5
+TYPES = pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16], ids=["f16", "bf16"])
+
+
+# --- the format, from its definition, on numpy arrays
+
+def row_bytes(d):
+    return 4 * ((d + 31) // 32) + d // 2
+
+
+def pack_group(x):
+    """(s, m, codes) of one group's columns (a list of at most 32 numbers)."""
+    if any(math.isnan(v) for v in x):
+        return np.float16(0), np.float16("nan"), [0] * len(x)
+    x = [max(-65280.0, min(65280.0, float(v))) for v in x]
+    m = np.float16(min(x))
+    if float(m) > min(x):
+        m = np.nextafter(m, np.float16(-np.inf))
+    m = np.float16(0) if m == 0 else m
+    s = np.float16(max(0.0, (max(x) - float(m)) / 15))
+    while s > 0 and 15 * float(np.nextafter(s, np.float16(0))) + float(m) >= max(x):
+        s = np.nextafter(s, np.float16(0))
+    while 15 * float(s) + float(m) < max(x):
+        s = np.nextafter(s, np.float16(np.inf))
+    borders = [float(m) + (k + 0.5) * float(s) for k in range(15)] if s > 0 else [math.inf] * 15  # exact: 41 binary digits at most
+    return s, m, [sum(v >= b for b in borders) for v in x]
+
+
+def pack_rows(x):
+    """[..., d] float64 -> [..., row] uint8."""
+    d = x.shape[-1]
+    out = np.zeros((*x.shape[:-1], row_bytes(d)), np.uint8)
+    G = (d + 31) // 32
+    for at in np.ndindex(*x.shape[:-1]):
+        words = [0] * (d // 8)
+        heads = []
+        for g in range(G):
+            s, m, codes = pack_group(x[at][32 * g:32 * g + 32].tolist())
+            heads += [s, m]
+            for i, c in enumerate(codes):
+                col = 32 * g + i
+                words[col // 8] |= c << (16 * (col % 2) + 4 * (col % 8 // 2))
+        out[at] = np.frombuffer(np.array(heads, "<f2").tobytes() + np.array(words, "<u4").tobytes(), np.uint8)
+    return out
+
+
+def unpack_rows(rows, d):
+    """[..., row] uint8 -> [..., d]: the binary16 values, as float64."""
+    G = (d + 31) // 32
+    rows = np.ascontiguousarray(rows)
+    head = rows[..., :4 * G].copy().view("<f2").astype(np.float64)
+    word = rows[..., 4 * G:].copy().view("<u4")
+    out = np.empty((*rows.shape[:-1], d))
+    for col in range(d):
+        code = (word[..., col // 8] >> (16 * (col % 2) + 4 * (col % 8 // 2))) & 15
+        with np.errstate(invalid="ignore", over="ignore"):
+            out[..., col] = (code * head[..., col // 32 * 2] + head[..., col // 32 * 2 + 1]).astype(np.float16)
+    return out
+
+
+def test_the_format_by_hand():
+    s, m, codes = pack_group([0.0, 15.0, 7.5, 7.49, 14.5, 3.0])
+    assert (s, m, codes) == (1, 0, [0, 15, 8, 7, 15, 3])       # a tie goes up
+    assert pack_group([0.25] * 32)[:2] == (0, 0.25) and pack_group([0.25] * 32)[2] == [0] * 32
+    s, m, codes = pack_group([1e-9, 2e-9])                      # below binary16: a base of 0, the smallest step
+    assert (s, m, codes) == (np.float16(2.0 ** -24), 0, [0, 0])
+    s, m, codes = pack_group([-1e-9, 0.0])
+    assert (s, m, codes) == (np.float16(2.0 ** -24), np.float16(-(2.0 ** -24)), [1, 1])
+    s, m, codes = pack_group([-math.inf, math.inf])
+    assert (s, m, codes) == (8704, -65280, [0, 15]) and np.isfinite(np.float16(15.0 * 8704 - 65280))
+    row = pack_rows(np.arange(8.0)[None] * 15 / 7)
+    assert row.shape == (1, 8) and unpack_rows(row, 8)[0].tolist() == [0, 2, 4, 6, 9, 11, 13, 15]
+    assert row[0, 4:].tolist() == [0x40, 0xD9, 0x62, 0xFB]      # columns 0 2 | 4 6 | 1 3 | 5 7
+
+
+def test_a_row_is_five_bits_a_column_and_says_how_many():
+    assert [smha.smha_packed_row(d) for d in (8, 32, 64, 80, 128)] == [8, 20, 40, 52, 80]
+    widths = [smha.smha_packed_row(d) for d in range(8, 129, 8)]
+    assert widths == [row_bytes(d) for d in range(8, 129, 8)] and len(set(widths)) == 16
+    for d in (0, 4, 12, 136):
+        with pytest.raises(smha.SmhaError):
+            smha.smha_packed_row(d)
+
+
+# --- on the GPU
+
+def int32(values):
+    return torch.tensor(values, dtype=torch.int32, device="cuda")
+
+
+def rows_of(t):
+    return t.float().cpu().double().numpy()
+
+
+def new_tokens(B, Hkv, T, d, dtype, layout="bhsd", seed=1, scale=1.0):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+
+    def new():
+        shape = (B, T, Hkv, d) if layout == "bshd" else (B, Hkv, T, d)
+        t = (torch.randn(shape, generator=gen, device="cuda") * scale).to(dtype)
+        return t.transpose(1, 2) if layout == "bshd" else t
+    return new(), new()
+
+
+def old_cache(B, Hkv, Sk, d, seed=2):
+    """Bytes of any kind."""
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    return tuple(torch.randint(0, 256, (B, Hkv, Sk, row_bytes(d)), generator=gen, device="cuda", dtype=torch.uint8) for _ in range(2))
+
+
+WRITES = [
+    # B, Hkv, T, Sk, d, lengths, offsets, layout
+    (1, 1, 1, 1, 8, [1], None, "bhsd"),
+    (1, 2, 1, 256, 64, [256], None, "bhsd"),
+    (5, 3, 1, 9, 128, [0, 1, 5, 9, 12], None, "bhsd"),              # none, the first, the last, more than there are
+    (3, 2, 7, 10, 80, [3, 10, 7], None, "bshd"),                    # more tokens than keys
+    (3, 2, 7, 10, 96, [3, 10, -4], [0, 2, 0], "bshd"),              # padded behind
+    (4, 1, 6, 12, 40, [12, 12, 12, 12], [-3, 9, 50, -50], "bhsd"),  # partly before the cache and past it, wholly
+    (2, 4, 33, 40, 32, [40, 35], [7, 0], "bhsd"),
+    (2, 1, 3, 8, 24, [8, 7], [2147483647, -2147483648], "bhsd"),    # places past 32 bits
+    (70, 1, 2, 5, 16, [i % 6 for i in range(70)], None, "bhsd"),
+    (1, 2, 21, 30, 120, [30], None, "bshd"),
+]
+
+
+def slots(lengths, offsets, b, T, Sk):
+    """(token, slot) pairs that are kept."""
+    n = min(max(lengths[b], 0), Sk)
+    at = n - T if offsets is None else offsets[b]
+    return [(t, at + t) for t in range(T) if 0 <= at + t < n]
+
+
+@pytest.mark.gpu
+@TYPES
+@pytest.mark.parametrize("case", WRITES, ids=lambda c: "x".join(str(x) for x in c[:5]))
+def test_written_rows_are_the_format(case, dtype):
+    B, Hkv, T, Sk, d, lengths, offsets, layout = case
+    kn, vn = new_tokens(B, Hkv, T, d, dtype, layout)
+    for values in (False, True):
+        k, v = old_cache(B, Hkv, Sk, d)
+        before = (k.cpu().numpy().copy(), v.cpu().numpy().copy())
+        versions = k._version, v._version
+        got = smha.packed_write(kn, vn, k, v, int32(lengths), offsets=None if offsets is None else int32(offsets), values=values)
+        assert k._version > versions[0] and v._version > versions[1]
+        assert (got is None) == (not values)
+        for i, (new, cache) in enumerate(((kn, k), (vn, v))):
+            want, rows = before[i], pack_rows(rows_of(new))
+            kept = np.zeros((B, Hkv, T, d), bool)
+            for b in range(B):
+                for t, slot in slots(lengths, offsets, b, T, Sk):
+                    want[b, :, slot] = rows[b, :, t]
+                    kept[b, :, t] = True
+            assert np.array_equal(cache.cpu().numpy(), want)
+            if values:
+                stands = torch.from_numpy(np.where(kept, unpack_rows(rows, d), 0.0)).to(torch.float32).to(dtype)
+                assert got[i].is_contiguous() and torch.equal(got[i].cpu(), stands)
+
+
+@pytest.mark.gpu
+@TYPES
+def test_values_at_borders_are_packed_exactly(dtype):
+    """Ties, constants, signed zeros, values that differ from a border by less than 32 bits hold, the type's largest and smallest, infinities, NaN."""
+    rng = np.random.default_rng(5)
+    tiny, top = torch.finfo(dtype).smallest_normal, torch.finfo(dtype).max
+    sub = float(torch.tensor(1, dtype=torch.int16).view(dtype))
+    groups = [[0.0] * 32, [-0.0] * 32, [0.0, -0.0] * 16, [-0.0, 0.0] * 16, [0.1] * 32, [-7.25] * 32, [sub] * 32, [-sub, sub] * 16, [tiny, -tiny] * 16,
+              [top, -top] * 16, [math.inf] + [1.0] * 31, [-math.inf, math.inf] * 16, [1.0] * 31 + [math.nan], [math.nan] * 32, [math.inf, math.nan] * 16,
+              [65504.0, -3.0] * 16, [top] * 32, [1e-8] * 16 + [-1e-8] * 16]
+    for _ in range(200):  # multiples of a step: (k + 1/2) s is hit often, also where s was rounded up
+        n = int(rng.integers(1, 31))
+        unit = 2.0 ** rng.integers(-20, 8)
+        groups.append((rng.integers(-n, n + 1, 32) * unit / 2).tolist())
+    for _ in range(100):  # a wide range with values next to 0 or to a border
+        x = rng.standard_normal(32) * 10.0 ** rng.integers(-6, 4)
+        x[rng.integers(0, 32, 8)] *= 1e-6
+        groups.append(x.tolist())
+    for _ in range(50):   # 0 .. 15 steps and halves about a base, with the smallest values of the type added
+        base, step = float(rng.integers(-20, 20)), 2.0 ** rng.integers(-3, 3)
+        groups.append([base, base + 15 * step] + [base + (rng.integers(0, 15) + 0.5) * step for _ in range(29)] + [sub])
+    x = torch.tensor(groups, dtype=torch.float64).to(torch.float32).to(dtype)
+    rows = x.reshape(1, 1, -1, 32)
+    T = rows.shape[2]
+    k, v = smha.packed_cache(1, 1, T, 32)
+    got = smha.packed_write(rows.cuda(), rows.flip(2).cuda(), k, v, int32([T]), values=True)
+    want = pack_rows(rows_of(rows))
+    assert np.array_equal(k.cpu().numpy(), want) and np.array_equal(v.cpu().numpy(), want[:, :, ::-1])
+    stands = unpack_rows(want, 32)
+    assert np.array_equal(got[0].float().cpu().numpy(), torch.from_numpy(stands).float().to(dtype).float().numpy(), equal_nan=True)
+    # within half a step and half a last place of binary16
+    inside = np.clip(rows_of(rows), -65280, 65280)
+    step = want[..., :2].copy().view("<f2").astype(np.float64)
+    finite = ~np.isnan(inside).any(-1)
+    off = np.abs(stands - inside)[finite]
+    assert bool((off <= (step / 2 + np.maximum(2.0 ** -11 * np.abs(stands), 2.0 ** -25))[finite]).all()) and np.isfinite(stands[finite]).all()
+    assert np.isnan(stands[~finite]).all()
+
+
+READS = [
+    # B, Hkv, T, Sk, d, lengths, offsets
+    (1, 1, 1, 1, 8, [1], None),
+    (2, 3, 40, 40, 64, [40, 17], None),
+    (3, 2, 9, 30, 80, [30, 4, 0], None),
+    (3, 2, 9, 30, 128, [30, 33, -1], [25, -4, 0]),
+    (2, 1, 50, 20, 104, [20, 13], [3, -2]),                  # more than there are
+    (2, 1, 3, 8, 24, [8, 7], [2147483647, -2147483648]),
+]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16, torch.float32], ids=["f16", "bf16", "f32"])
+@pytest.mark.parametrize("case", READS, ids=lambda c: "x".join(str(x) for x in c[:5]))
+def test_what_is_read_is_what_the_rows_stand_for(case, dtype):
+    """On rows of any bytes (all of them stand for something, infinities and NaN too)."""
+    B, Hkv, T, Sk, d, lengths, offsets = case
+    k, v = old_cache(B, Hkv, Sk, d)
+    at = None if offsets is None else int32(offsets)
+    got = smha.packed_read(k, v, int32(lengths), offsets=at, tokens=T, dtype=dtype)
+    for out, cache in zip(got, (k, v)):
+        stands = unpack_rows(cache.cpu().numpy(), d)
+        want = np.zeros((B, Hkv, T, d))
+        for b in range(B):
+            for t, slot in slots(lengths, offsets if offsets else [0] * B, b, T, Sk):
+                want[b, :, t] = stands[b, :, slot]
+        want = torch.from_numpy(want).float().to(dtype)
+        assert out.dtype == dtype and torch.equal(out.cpu().nan_to_num(nan=12345.0), want.nan_to_num(nan=12345.0))
+        assert torch.equal(out.cpu().isnan(), want.isnan())
+    # into tensors of other strides
+    into = tuple(torch.full((B, T, Hkv, 2, 128), -1.0, dtype=dtype, device="cuda") for _ in range(2))
+    views = tuple(t[:, :, :, 1, :d].transpose(1, 2) for t in into)
+    back = smha.packed_read(k, v, int32(lengths), offsets=at, tokens=T, dtype=dtype, out=views)
+    assert back[0] is views[0] and back[1] is views[1]
+    for a, b, t in zip(got, views, into):
+        assert torch.equal(a.nan_to_num(), b.nan_to_num()) and bool((t[:, :, :, 0] == -1).all()) and bool((t[:, :, :, 1, d:] == -1).all())
+
+
+@pytest.mark.gpu
+def test_all_slots_are_read_by_default():
+    k, v = smha.packed_cache(2, 2, 37, 64)
+    kn, vn = new_tokens(2, 2, 37, 64, torch.float16)
+    stands = smha.packed_write(kn, vn, k, v, int32([37, 37]), values=True)
+    got = smha.packed_read(k, v, int32([37, 37]))
+    assert all(torch.equal(a, b) and a.dtype == torch.float16 for a, b in zip(stands, got))
+
+
+# --- attention
+
+def reference(q, k, v, lengths, window=0, n_sink=0, scale=0.0):
+    """(out, its bound) in 64 bits on the CPU, on the values that the rows stand for."""
+    (B, H, T, d), (Hkv, Sk) = q.shape, k.shape[1:3]
+    u, z = torch.finfo(q.dtype).eps / 2, 2.0 ** -25 if q.dtype == torch.float16 else 0.0
+    scale = scale if scale > 0 else d ** -0.5
+    q = q.cpu().double()
+    k, v = (torch.from_numpy(unpack_rows(t.cpu().numpy(), d)) for t in (k, v))
+    out, tol = torch.zeros_like(q), torch.zeros_like(q)
+    for b in range(B):
+        n = min(max(lengths[b], 0), Sk)
+        pos = torch.arange(T)[:, None] + n - T
+        j = torch.arange(n)[None, :]
+        seen = (j <= pos) & (pos >= 0)
+        if window:
+            seen &= (pos - j < window) | (j < n_sink)
+        used = seen.any(0)
+        for h in range(H):
+            c = h * Hkv // H
+            K, V = (torch.where(used[:, None], t[b, c, :n], 0.0) for t in (k, v))
+            s = (q[b, h] @ K.T * scale).masked_fill(~seen, -math.inf)
+            P = torch.where(seen, torch.exp(s - torch.logsumexp(s, 1).nan_to_num(neginf=0.0)[:, None]), 0.0)
+            out[b, h] = P @ V
+            tol[b, h] = torch.where(seen, (2.0 ** -11 + F) * P + 2.0 ** -25, 0.0) @ V.abs()
+    return out, tol * (1 + u) + u * out.abs() + z
+
+
+def check(got, want, bound, what="output"):
+    got = got.detach().cpu().double()
+    ok = torch.isfinite(got) & ((got - want).abs() <= bound)
+    assert got.shape == want.shape and bool(ok.all()), f"{what}: {int((~ok).sum())} of {ok.numel()} off, worst {float(((got - want).abs() - bound).max())}"
+
+
+def filled(B, Hkv, Sk, d, seed=3):
+    """A cache whose every slot holds a key."""
+    k, v = smha.packed_cache(B, Hkv, Sk, d)
+    kn, vn = new_tokens(B, Hkv, Sk, d, torch.float16, seed=seed)
+    smha.packed_write(kn, vn, k, v, int32([Sk] * B))
+    return k, v
+
+
+def queries(B, H, T, d, dtype, layout="bhsd", seed=4):
+    return new_tokens(B, H, T, d, dtype, layout, seed)[0]
+
+
+CASES = [
+    # B, H, Hkv, T, Sk, d, window, n_sink, lengths, layout
+    (1, 1, 1, 1, 1, 64, 0, 0, [1], "bhsd"),
+    (1, 8, 2, 1, 256, 64, 64, 4, [256], "bhsd"),
+    (3, 4, 4, 1, 100, 128, 0, 0, [0, 1, 100], "bshd"),               # an empty sequence, one key
+    (2, 6, 2, 3, 333, 80, 50, 7, [333, 2], "bhsd"),                  # fewer keys than tokens
+    (2, 16, 2, 5, 700, 128, 100, 40, [699, 130], "bshd"),            # 40 rows on a key head
+    (2, 16, 1, 4, 97, 32, 0, 0, [97, 33], "bhsd"),                   # 64 rows
+    (1, 16, 2, 40, 120, 64, 60, 3, [119], "bhsd"),                   # 320 rows
+    (1, 4, 1, 1, 20000, 128, 0, 0, [19999], "bhsd"),                 # many segments
+    (2, 4, 2, 1, 9000, 64, 4096, 130, [9000, 8999], "bhsd"),
+    (70, 2, 1, 1, 64, 8, 0, 0, [(7 * i) % 65 for i in range(70)], "bhsd"),   # more sequences than lanes
+    (150, 4, 2, 2, 300, 64, 33, 2, [(31 * i) % 301 for i in range(150)], "bhsd"),
+    (70, 2, 1, 1, 2000, 64, 0, 0, [(29 * i) % 2001 for i in range(70)], "bhsd"),
+    (70, 4, 4, 1, 1400, 128, 0, 0, [(1400 - 21 * i) for i in range(67)] + [0, 1, 2], "bshd"),
+    (2, 2, 1, 1, 50, 64, 1, 0, [50, 49], "bhsd"),                    # a window of one key
+    (1, 2, 1, 130, 130, 128, 0, 0, [130], "bhsd"),                   # a whole prompt
+    (2, 4, 2, 129, 257, 72, 0, 0, [257, 100], "bshd"),               # a chunk; a sequence shorter than it
+    (1, 8, 1, 70, 1000, 104, 200, 70, [1000], "bhsd"),               # 560 rows in a window
+    (1, 3, 1, 11, 66, 16, 5, 2, [66], "bhsd"),                       # 33 rows, three heads a key head
+    (2, 12, 4, 90, 4000, 128, 0, 0, [4000, 1931], "bhsd"),           # 270 rows, long
+    (1, 17, 1, 1, 77, 40, 0, 0, [77], "bhsd"),                       # 17 rows
+    (1, 5, 1, 13, 3000, 56, 0, 0, [2999], "bhsd"),                   # 65 rows
+    (3, 2, 2, 300, 700, 64, 128, 0, [700, 299, 1], "bshd"),
+]
+
+
+@pytest.mark.gpu
+@TYPES
+@pytest.mark.parametrize("case", CASES, ids=lambda c: "x".join(str(x) for x in c[:8]))
+def test_attention_is_the_formula(case, dtype):
+    B, H, Hkv, T, Sk, d, window, n_sink, lengths, layout = case
+    k, v = filled(B, Hkv, Sk, d)
+    q = queries(B, H, T, d, dtype, layout)
+    want, bound = reference(q, k, v, lengths, window, n_sink)
+    out = smha.packed_attention(q, k, v, int32(lengths), window=window, n_sink=n_sink)
+    check(out, want, bound)
+    again = torch.full_like(out, math.nan)
+    assert smha.packed_attention(q, k, v, int32(lengths), window=window, n_sink=n_sink, out=again) is again
+    assert torch.equal(again, out)
