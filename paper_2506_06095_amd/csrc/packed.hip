@@ -207,6 +207,10 @@ __global__ void __launch_bounds__(256) smha_packed_get(const UnpackParams p) {
 // ---------------------------------------------------------------------------------------
 // Attention
 // ---------------------------------------------------------------------------------------
+// The rows that read the same keys, T tokens times G = H / Hkv heads, token by token, are taken 16, 32 or 128 at a time; such a tile of rows and
+// the tiles of keys that it sees are a group.  Memory bounds calls of few rows: a key's 10 d / 8 bytes meet 4 d G T operations.  There
+// every compute unit has to read, whatever the lengths are, so the key tiles of all groups are counted on the device and cut into as many segments, of
+// about the same length, as workgroups fit the chip; segments of one group are joined by a second kernel, in a fixed order.
 struct PackedParams {
     const uint16_t *Q;
     const uint8_t *K, *V;
@@ -215,8 +219,12 @@ struct PackedParams {
     const int32_t *lengths;
     int B, H, Hkv, G, T, Sk, d;
     int window, n_sink;
-    int row_tiles;  // of 16 rows, of a key head's G T
+    int row_tiles;  // of a key head's G T rows
     float c;        // scale * log2(e)
+    int slots;      // segments wanted; 0: a group is a segment
+    int2 *info;     // [groups]: first place, segments.  A place is what a segment of a cut group leaves:
+    float *stats;   // [place][2][rows]: reference (log2 units), sum
+    float *parts;   // [place][rows][D]
 };
 
 // The keys that rows of tokens t0 .. t1 of a sequence see: the tiles of the sinks, then those of the window.
@@ -232,38 +240,136 @@ template <int KT> struct PackedKeys {
         gap0 = n_sink < from ? n_sink : 0;
         gap1 = n_sink < from ? from : 0;
     }
+    // of the rows rows0 .. rows0 + ROWS - 1
+    static __device__ __forceinline__ PackedKeys of(const PackedParams &p, int length, int rows0, int rows_of_tile) {
+        int t0 = 0, t1 = p.T - 1;
+        if (p.row_tiles > 1) {
+            t0 = rows0 / p.G;
+            t1 = (min(rows0 + rows_of_tile, p.G * p.T) - 1) / p.G;
+        }
+        return PackedKeys(length, p.T, p.Sk, p.window, p.n_sink, t0, t1);
+    }
     __device__ __forceinline__ int key(int tile) const { return KT * (tile < head ? tile : first + tile - head); }
 };
+
+struct PackedSegment {
+    int b, hk, rows0, length;  // b < 0: no segment
+    int part, parts;
+    int place, group;          // of its results
+    __device__ __forceinline__ bool whole() const { return parts == 1; }
+};
+
+__device__ __forceinline__ int lanes_sum(int v) {
+#pragma unroll
+    for (int m = 32; m > 0; m >>= 1) v += __shfl_xor(v, m);
+    return __builtin_amdgcn_readfirstlane(v);
+}
+__device__ __forceinline__ int lanes_scan(int v, int lane) {
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+        const int below = __shfl_up(v, m);
+        if (lane >= m) v += below;
+    }
+    return v;
+}
+
+// The segment of a workgroup.  Every wave of the launch computes the same cut: `most` tiles a segment at most, so many that all tiles make `slots` segments;
+// groups shorter than that are a segment each, and then there are more: what does not fit at first starts as others end.  An XCD takes a run of
+// segments: those that read the same keys are neighbours.
+template <int KT, int ROWS, int TURN> __device__ __forceinline__ PackedSegment packed_segment(const PackedParams &p, int lane) {
+    const int xcd = (int)blockIdx.x & 7, slot = (int)blockIdx.x >> 3;
+    PackedSegment s{-1, 0, 0, 0, 0, 1, 0, 0};
+    if (!p.slots) {
+        const int n = p.B * p.Hkv * p.row_tiles, run = (n + 7) / 8, at = xcd * run + slot;
+        if (slot >= run || at >= n) return s;
+        const int bh = at / p.row_tiles;  // a head's last rows, which see the most keys, come first
+        s.b = bh / p.Hkv;
+        s.hk = bh - s.b * p.Hkv;
+        s.rows0 = ROWS * (p.row_tiles - 1 - (at - bh * p.row_tiles));
+        s.length = uniform_load(p.lengths + s.b);
+        return s;
+    }
+    const int E = p.B * p.row_tiles;
+    struct Entry {
+        int b, rows0, length, n;
+    };
+    auto entry = [&](int i) __attribute__((always_inline)) {
+        Entry e{0, 0, 0, 0};
+        if (i < E) {
+            e.b = p.row_tiles > 1 ? i / p.row_tiles : i;
+            e.rows0 = ROWS * (p.row_tiles - 1 - (i - e.b * p.row_tiles));
+            e.length = p.lengths[e.b];
+            e.n = PackedKeys<KT>::of(p, e.length, e.rows0, ROWS).n;
+        }
+        return e;
+    };
+    const Entry first64 = entry(lane);
+    int sum = first64.n;
+    for (int i = 64; i < E; i += 64) sum += entry(i + lane).n;
+    const int total = p.Hkv * lanes_sum(sum);
+    const int most = max(4, ((total + p.slots - 1) / p.slots + TURN - 1) / TURN * TURN);
+    auto parts_of = [&](int i, int n) __attribute__((always_inline)) { return i < E ? max(1, (n + most - 1) / most) : 0; };
+    sum = parts_of(lane, first64.n);
+    for (int i = 64; i < E; i += 64) sum += parts_of(i + lane, entry(i + lane).n);
+    const int n = p.Hkv * lanes_sum(sum), run = (n + 7) / 8;
+    int at = xcd * run + slot, place = 0;
+    if (slot >= run || at >= n) return s;
+    for (int i0 = 0; i0 < E; i0 += 64) {
+        const Entry e = i0 == 0 ? first64 : entry(i0 + lane);
+        const int parts = parts_of(i0 + lane, e.n), mine = p.Hkv * parts, upto = lanes_scan(mine, lane), cut = parts > 1 ? mine : 0, cut_upto = lanes_scan(cut, lane);
+        const uint64_t past = __builtin_amdgcn_ballot_w64(upto > at);
+        if (past) {
+            const int who = __builtin_ctzll(past);
+            s.b = __builtin_amdgcn_readlane(e.b, who);
+            s.rows0 = __builtin_amdgcn_readlane(e.rows0, who);
+            s.length = __builtin_amdgcn_readlane(e.length, who);
+            s.parts = __builtin_amdgcn_readlane(parts, who);
+            const int rest = at - (__builtin_amdgcn_readlane(upto, who) - __builtin_amdgcn_readlane(mine, who));
+            s.hk = rest / s.parts;
+            s.part = rest - s.hk * s.parts;
+            s.place = place + __builtin_amdgcn_readlane(cut_upto, who) - __builtin_amdgcn_readlane(cut, who) + rest;
+            s.group = (s.b * p.Hkv + s.hk) * p.row_tiles + s.rows0 / ROWS;
+            return s;
+        }
+        at -= __builtin_amdgcn_readlane(upto, 63);
+        place += __builtin_amdgcn_readlane(cut_upto, 63);
+    }
+    return s;  // (not reached: the segments counted are those found)
+}
+
+// The reference that a row's segment leaves: -inf says that it has no keys.  (A row of NaN has no largest score either, and must not be passed over.)
+__device__ __forceinline__ float reference_left(float m, float l) { return l == l ? m : 0.f; }
 
 __device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
 
-// A row of queries as the B operand of the scores' product, in binary16: lane (row, u) holds columns (D / 4) u + 8 i ...  bfloat16 rows are brought to
-// 2^14 .. 2^15 by a power of two, by which they fit binary16 without loss (but for columns below 2^-31 of the largest, which lose digits); returns what the scores have to be multiplied by.
-template <int D, bool BF16> __device__ __forceinline__ float load_query(u32x4 (&qf)[D / 32], const uint16_t *row, bool exists, int d, int u) {
-    u32x4 raw[D / 32];
+// A row of queries as the B operand of the scores' product, in binary16: a lane holds N chunks of 8 columns, chunk i from column `col(i)` on, and the row's other
+// columns are in lanes 16 (STEPS16: and 32) apart.  bfloat16 rows are brought to 2^14 .. 2^15 by a power of two, by which they fit binary16 without
+// loss (but for columns below 2^-31 of the largest, which lose digits); returns what the scores have to be multiplied by.
+template <int N, bool BF16, bool STEPS16, typename Col>
+__device__ __forceinline__ float load_query(u32x4 (&qf)[N], const uint16_t *row, bool exists, int d, Col col) {
+    u32x4 raw[N];
 #pragma unroll
-    for (int i = 0; i < D / 32; ++i) {
-        const int col = D / 4 * u + 8 * i;
+    for (int i = 0; i < N; ++i) {
         raw[i] = u32x4{0, 0, 0, 0};
-        if (exists && col < d) raw[i] = *reinterpret_cast<const u32x4 *>(row + col);
+        if (exists && col(i) < d) raw[i] = *reinterpret_cast<const u32x4 *>(row + col(i));
     }
     if constexpr (!BF16) {
 #pragma unroll
-        for (int i = 0; i < D / 32; ++i) qf[i] = raw[i];
+        for (int i = 0; i < N; ++i) qf[i] = raw[i];
         return 1.f;
     } else {
         float top = 0.f;
 #pragma unroll
-        for (int i = 0; i < D / 32; ++i)
+        for (int i = 0; i < N; ++i)
 #pragma unroll
             for (int e = 0; e < 4; ++e) top = fmaxf(top, fmaxf(fabsf(widen16<true>(raw[i][e] & 0xFFFFu)), fabsf(widen16<true>(raw[i][e] >> 16))));
-        top = fmaxf(top, __shfl_xor(top, 16));
+        if (STEPS16) top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, __shfl_xor(top, 32));
         const int e2 = min(15 - __builtin_amdgcn_frexp_expf(top), 100);
 #pragma unroll
-        for (int i = 0; i < D / 32; ++i)
+        for (int i = 0; i < N; ++i)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
                 qf[i][e] = pack2<false>(__builtin_amdgcn_ldexpf(widen16<true>(raw[i][e] & 0xFFFFu), e2), __builtin_amdgcn_ldexpf(widen16<true>(raw[i][e] >> 16), e2));
@@ -271,168 +377,441 @@ template <int D, bool BF16> __device__ __forceinline__ float load_query(u32x4 (&
     }
 }
 
+// Packed rows as a lane reads them: D / 4 columns of a key, those from (D / 4) u on.  Keys past the buffer read as zeros, and so do those between the sinks
+// and the window (which no row of the tile sees; a step and a base of 0 are enough) and the columns that the head does not have.
+template <int D> struct PackedLoad {
+    static constexpr int NW = D / 32;  // words of codes
+    struct Raw {
+        uint32_t head, code[NW];
+    };
+    __amdgpu_buffer_rsrc_t r;
+    int pitch, head_at, codes_at, gap0, gap1;
+    template <int KT> __device__ __forceinline__ PackedLoad(const uint8_t *rows, int64_t pitch_, const PackedKeys<KT> &keys, int d, int u) {
+        const int groups = (d + 31) >> 5, mine = D == 128 ? u : u >> 1;
+        r = make_rsrc(rows, keys.end > 0 ? (int64_t)(keys.end - 1) * pitch_ + 4 * groups + (d >> 1) : 0);
+        pitch = (int)pitch_;
+        head_at = mine < groups ? 4 * mine : (int)kPast;
+        codes_at = 4 * groups + D / 8 * u;
+        gap0 = keys.gap0;
+        gap1 = keys.gap1;
+    }
+    __device__ __forceinline__ Raw operator()(int key) const {
+        Raw x;
+        const int at = key * pitch;
+        x.head = __builtin_amdgcn_raw_buffer_load_b32(r, (key >= gap0 && key < gap1) || head_at == (int)kPast ? (int)kPast : at + head_at, 0, 0);
+        if constexpr (NW == 4) {
+            const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(r, at + codes_at, 0, 0);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x.code[i] = v[i];
+        } else {
+            const u32x2 v = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r, at + codes_at, 0, 0));
+            x.code[0] = v[0];
+            x.code[1] = v[1];
+        }
+        return x;
+    }
+};
+
 // Swizzle of a 32-row tile of values: writes of 16 rows at one chunk of 16 bytes, and transposing reads of 8 rows x 2 chunks (half a wave), all over the banks.
 template <int D> __device__ __forceinline__ int swz_values(int row) {
     if constexpr (D == 128) return ((row & 7) << 1) | ((row >> 3) & 1);
     else return (((row >> 1) & 3) << 1) | ((row >> 3) & 1);
 }
 
-// Four waves take the tiles of 32 keys of a group, 16 rows that read the same keys, in turn, and join in LDS.  A lane unpacks D / 4 columns of two keys: keys are an operand
-// as they come out; values go through LDS once, for the transposing reads that make them the other product's.
-template <int D, bool BF16>
-__global__ void __launch_bounds__(256, 2) smha_packed_part(const PackedParams p) {
-    constexpr int NS = D / 32, NW = D / 32, NC = D / 16, TB = 32 * D * 2;  // steps of the first product; words of codes a lane has of a key; tiles of columns; bytes of a tile
+// Four waves take a segment's tiles of 32 keys in turn and join in LDS.  A lane unpacks D / 4 columns of two keys: keys are an operand as they come out; values go
+// through LDS once, for the transposing reads that make them the other product's.  NR tiles of 16 rows share what is unpacked.
+constexpr int packed_workgroups(int D, int NR) { return D == 64 ? (NR == 1 ? 4 : 3) : NR == 1 ? 3 : 2; }  // of a compute unit
+template <int D, int NR, bool BF16>
+__global__ void __launch_bounds__(256, packed_workgroups(D, NR)) smha_packed_part(const PackedParams p) {
+    constexpr int NS = D / 32, NC = D / 16, TB = 32 * D * 2, ROWS = 16 * NR;  // steps of the first product, tiles of columns, bytes of a tile
     __shared__ __attribute__((aligned(1024))) char all_tiles[4 * TB];
-    __shared__ float team[4][2][16];
+    __shared__ float team[4][2][ROWS];
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = lane & 15, u = lane >> 4;
     char *const smem = all_tiles + w * TB;
     const float NEG_INF = -__builtin_inff();
 
-    const int group = blockIdx.x, bh = group / p.row_tiles, b = bh / p.Hkv, hk = bh - b * p.Hkv, rows0 = 16 * (group - bh * p.row_tiles);
+    const PackedSegment s = packed_segment<32, ROWS, 4>(p, lane);
+    if (s.b < 0) return;
     const int rows = p.G * p.T;
-    const PackedKeys<32> keys(uniform_load(p.lengths + b), p.T, p.Sk, p.window, p.n_sink, rows0 / p.G, (min(rows0 + 16, rows) - 1) / p.G);
-    const int row = rows0 + j, t = row / p.G, g = row - t * p.G, pos = row < rows ? keys.len - p.T + t : -1;  // below 0: no such query
-    u32x4 qf[NS];
-    const float c = fmaxf(p.c * load_query<D, BF16>(qf, p.Q + b * p.qs.b + (hk * p.G + g) * p.qs.h + t * p.qs.s, pos >= 0, p.d, u), 0x1p-126f);  // (never 0: -inf times it)
-
-    // keys from `end` on are past the buffers and read as zeros
-    const int groups = (p.d + 31) >> 5, row_bytes = 4 * groups + (p.d >> 1);
-    const __amdgpu_buffer_rsrc_t rK = make_rsrc(p.K + b * p.ks.b + hk * p.ks.h, keys.end > 0 ? (int64_t)(keys.end - 1) * p.ks.s + row_bytes : 0);
-    const __amdgpu_buffer_rsrc_t rV = make_rsrc(p.V + b * p.vs.b + hk * p.vs.h, keys.end > 0 ? (int64_t)(keys.end - 1) * p.vs.s + row_bytes : 0);
-    const int my_group = D == 128 ? u : u >> 1, codes_at = 4 * groups + D / 8 * u;
-    struct Raw {
-        uint32_t head[2], code[2][NW];
-    };
-    auto load = [&](__amdgpu_buffer_rsrc_t r, int pitch, int key) __attribute__((always_inline)) {
-        Raw x;
+    const auto keys = PackedKeys<32>::of(p, s.length, s.rows0, ROWS);
+    u32x4 qf[NR][NS];
+    int pos[NR];  // below 0: no such query
+    uint16_t *to[NR];
+    float c[NR], thr[NR];
 #pragma unroll
-        for (int a = 0; a < 2; ++a) {
-            const int k = key + 16 * a + j, at = k * pitch;
-            // keys between the sinks and the window read as zeros, and so do the columns that the head does not have
-            const bool read = (k < keys.gap0 || k >= keys.gap1) && my_group < groups;
-            x.head[a] = __builtin_amdgcn_raw_buffer_load_b32(r, read ? at + 4 * my_group : (int)kPast, 0, 0);
-            if constexpr (NW == 4) {
-                const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(r, at + codes_at, 0, 0);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) x.code[a][i] = v[i];
-            } else {
-                const u32x2 v = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r, at + codes_at, 0, 0));
-                x.code[a][0] = v[0];
-                x.code[a][1] = v[1];
-            }
-        }
-        return x;
-    };
-
-    float m_run = NEG_INF, l_run = 0.f;
-    const float thr = raised_over(c);
-    f32x4 o[NC];
-#pragma unroll
-    for (int ct = 0; ct < NC; ++ct) o[ct] = f32x4{0.f, 0.f, 0.f, 0.f};
-    const int tr_row = 4 * u + (j >> 2);
-    Raw k_raw, v_raw;
-    if (w < keys.n) {
-        k_raw = load(rK, (int)p.ks.s, keys.key(w));
-        v_raw = load(rV, (int)p.vs.s, keys.key(w));
+    for (int x = 0; x < NR; ++x) {
+        const int row = s.rows0 + 16 * x + j, t = row / p.G, g = row - t * p.G, h = s.hk * p.G + g;
+        pos[x] = row < rows ? keys.len - p.T + t : -1;
+        to[x] = row < rows ? p.O + s.b * p.os.b + h * p.os.h + t * p.os.s : nullptr;
+        // (never 0: -inf times it)
+        c[x] = fmaxf(p.c * load_query<NS, BF16, true>(qf[x], p.Q + s.b * p.qs.b + h * p.qs.h + t * p.qs.s, pos[x] >= 0, p.d, [&](int i) { return D / 4 * u + 8 * i; }), 0x1p-126f);
+        thr[x] = raised_over(c[x]);
     }
-    for (int tile = w; tile < keys.n; tile += 4) {
+    const PackedLoad<D> loadK(p.K + s.b * p.ks.b + s.hk * p.ks.h, p.ks.s, keys, p.d, u), loadV(p.V + s.b * p.vs.b + s.hk * p.vs.h, p.vs.s, keys, p.d, u);
+
+    float m_run[NR], l_run[NR];
+    f32x4 o[NR][NC];
+#pragma unroll
+    for (int x = 0; x < NR; ++x) {
+        m_run[x] = NEG_INF;
+        l_run[x] = 0.f;
+#pragma unroll
+        for (int ct = 0; ct < NC; ++ct) o[x][ct] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    const int tr_row = 4 * u + (j >> 2);
+    const int begin = (int)((int64_t)keys.n * s.part / s.parts) + w, end = (int)((int64_t)keys.n * (s.part + 1) / s.parts);
+    typename PackedLoad<D>::Raw k_raw[2], v_raw[2];
+    auto request = [&](int tile) __attribute__((always_inline)) {
+        const int key = keys.key(tile) + j;
+#pragma unroll
+        for (int a = 0; a < 2; ++a) k_raw[a] = loadK(key + 16 * a);
+#pragma unroll
+        for (int a = 0; a < 2; ++a) v_raw[a] = loadV(key + 16 * a);
+    };
+    if (begin < end) request(begin);
+    for (int tile = begin; tile < end; tile += 4) {
         const int key = keys.key(tile);
-        const Raw k_now = k_raw, v_now = v_raw;
-        if (tile + 4 < keys.n) {
-            k_raw = load(rK, (int)p.ks.s, keys.key(tile + 4));
-            v_raw = load(rV, (int)p.vs.s, keys.key(tile + 4));
-        }
-        // acc[a][r]: the score of query j and key 16 a + 4 u + r
-        f32x4 acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+        const typename PackedLoad<D>::Raw k_now[2] = {k_raw[0], k_raw[1]}, v_now[2] = {v_raw[0], v_raw[1]};
+        if (tile + 4 < end) request(tile + 4);
+        // acc[x][a][r]: the score of query j and key 16 a + 4 u + r
+        f32x4 acc[NR][2];
+#pragma unroll
+        for (int x = 0; x < NR; ++x) acc[x][0] = acc[x][1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < NS; ++i)
 #pragma unroll
-            for (int a = 0; a < 2; ++a) acc[a] = mfma16(unpack8(k_now.code[a][i], k_now.head[a]), qf[i], acc[a]);
+            for (int a = 0; a < 2; ++a) {
+                const u32x4 kf = unpack8(k_now[a].code[i], k_now[a].head);
+#pragma unroll
+                for (int x = 0; x < NR; ++x) acc[x][a] = mfma16(kf, qf[x][i], acc[x][a]);
+            }
         // values go to LDS under that product
 #pragma unroll
         for (int a = 0; a < 2; ++a)
 #pragma unroll
-            for (int i = 0; i < NW; ++i)
-                *reinterpret_cast<u32x4 *>(smem + (16 * a + j) * D * 2 + (((D / 32 * u + i) ^ swz_values<D>(j)) * 16)) = unpack8(v_now.code[a][i], v_now.head[a]);
-        const uint32_t word = pos >= 0 ? low_bits32(pos - key + 1) & (~low_bits32(pos - p.window + 1 - key) | low_bits32(p.n_sink - key)) : 0;
-        if (__builtin_amdgcn_ballot_w64(word != ~0u) != 0) {
+            for (int i = 0; i < NS; ++i)
+                *reinterpret_cast<u32x4 *>(smem + (16 * a + j) * D * 2 + (((D / 32 * u + i) ^ swz_values<D>(j)) * 16)) = unpack8(v_now[a].code[i], v_now[a].head);
+        u32x4 pf[NR];
+#pragma unroll
+        for (int x = 0; x < NR; ++x) {
+            const uint32_t word = pos[x] >= 0 ? low_bits32(pos[x] - key + 1) & (~low_bits32(pos[x] - p.window + 1 - key) | low_bits32(p.n_sink - key)) : 0;
+            if (__builtin_amdgcn_ballot_w64(word != ~0u) != 0) {
+#pragma unroll
+                for (int a = 0; a < 2; ++a)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) acc[x][a][r] = (word >> (16 * a + 4 * u + r)) & 1 ? acc[x][a][r] : NEG_INF;
+            }
+            float mt = NEG_INF;
 #pragma unroll
             for (int a = 0; a < 2; ++a)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) acc[a][r] = (word >> (16 * a + 4 * u + r)) & 1 ? acc[a][r] : NEG_INF;
-        }
-        float mt = NEG_INF;
+                for (int r = 0; r < 4; ++r) mt = fmaxf(mt, acc[x][a][r]);
+            if (__builtin_amdgcn_ballot_w64(mt > m_run[x] + thr[x]) != 0) {
+                mt = fmaxf(mt, __shfl_xor(mt, 16));
+                mt = fmaxf(mt, __shfl_xor(mt, 32));
+                const float m_new = fmaxf(m_run[x], mt), alpha = fast_exp2((m_run[x] - (m_new == NEG_INF ? 0.f : m_new)) * c[x]);
+                m_run[x] = m_new;
+                l_run[x] *= alpha;
 #pragma unroll
-        for (int a = 0; a < 2; ++a)
+                for (int ct = 0; ct < NC; ++ct) o[x][ct] *= alpha;
+            }
+            const float mc = (m_run[x] == NEG_INF ? 0.f : m_run[x]) * c[x];
+            // Probabilities, relative to about the largest, are rounded to binary16 for the second product, whatever the inputs' type.
 #pragma unroll
-            for (int r = 0; r < 4; ++r) mt = fmaxf(mt, acc[a][r]);
-        if (__builtin_amdgcn_ballot_w64(mt > m_run + thr) != 0) {
-            mt = fmaxf(mt, __shfl_xor(mt, 16));
-            mt = fmaxf(mt, __shfl_xor(mt, 32));
-            const float m_new = fmaxf(m_run, mt), alpha = fast_exp2((m_run - (m_new == NEG_INF ? 0.f : m_new)) * c);
-            m_run = m_new;
-            l_run *= alpha;
-#pragma unroll
-            for (int ct = 0; ct < NC; ++ct) o[ct] *= alpha;
-        }
-        const float mc = (m_run == NEG_INF ? 0.f : m_run) * c;
-        // Probabilities, relative to about the largest, are rounded to binary16 for the second product, whatever the inputs' type.
-        u32x4 pf;
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const float e0 = fast_exp2(fmaf(acc[q >> 1][2 * (q & 1)], c, -mc)), e1 = fast_exp2(fmaf(acc[q >> 1][2 * (q & 1) + 1], c, -mc));
-            pf[q] = pack2<false>(e0, e1);
-            l_run += e0 + e1;
+            for (int q = 0; q < 4; ++q) {
+                const float e0 = fast_exp2(fmaf(acc[x][q >> 1][2 * (q & 1)], c[x], -mc)), e1 = fast_exp2(fmaf(acc[x][q >> 1][2 * (q & 1) + 1], c[x], -mc));
+                pf[x][q] = pack2<false>(e0, e1);
+                l_run[x] += e0 + e1;
+            }
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 #pragma unroll
         for (int ct = 0; ct < NC; ++ct) {
             const int chunk = 2 * ct + ((j & 3) >> 1), at = tr_row * D * 2 + ((chunk ^ swz_values<D>(tr_row)) * 16) + (j & 1) * 8;
             const u32x2 lo = lds_read_tr(reinterpret_cast<const uint16_t *>(smem + at)), hi = lds_read_tr(reinterpret_cast<const uint16_t *>(smem + at + 16 * D * 2));
-            o[ct] = mfma16(u32x4{lo[0], lo[1], hi[0], hi[1]}, pf, o[ct]);
+#pragma unroll
+            for (int x = 0; x < NR; ++x) o[x][ct] = mfma16(u32x4{lo[0], lo[1], hi[0], hi[1]}, pf[x], o[x][ct]);
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the tile is read
     }
 
     // The team joins: every wave leaves its accumulators in its own tile's place and takes a quarter of the columns of all four.
     constexpr int NQ = NC / 4;
-    float l = l_run + __shfl_xor(l_run, 16);
-    l += __shfl_xor(l, 32);
+    if (p.slots && s.part == 0 && threadIdx.x == 0) p.info[s.group] = int2{s.place, s.parts};
 #pragma unroll
-    for (int ct = 0; ct < NC; ++ct) *reinterpret_cast<f32x4 *>(smem + (ct * 64 + lane) * 16) = o[ct];
-    if (u == 0) {
-        team[w][0][j] = m_run * c;
-        team[w][1][j] = l;
+    for (int x = 0; x < NR; ++x) {
+        float l = l_run[x] + __shfl_xor(l_run[x], 16);
+        l += __shfl_xor(l, 32);
+        if (u == 0) {
+            team[w][0][16 * x + j] = m_run[x] * c[x];
+            team[w][1][16 * x + j] = l;
+        }
     }
+#pragma unroll
+    for (int x = 0; x < NR; ++x) {
+        if (x) __syncthreads();
+#pragma unroll
+        for (int ct = 0; ct < NC; ++ct) *reinterpret_cast<f32x4 *>(smem + (ct * 64 + lane) * 16) = o[x][ct];
+        __syncthreads();
+        float m_all = NEG_INF, l_all = 0.f;
+        f32x4 out[NQ];
+#pragma unroll
+        for (int v = 0; v < 4; ++v) m_all = fmaxf(m_all, team[v][0][16 * x + j]);
+#pragma unroll
+        for (int i = 0; i < NQ; ++i) out[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            const float mu = team[v][0][16 * x + j], share = mu != NEG_INF ? fast_exp2(mu - m_all) : 0.f;
+            l_all = fmaf(share, team[v][1][16 * x + j], l_all);
+#pragma unroll
+            for (int i = 0; i < NQ; ++i) {
+                const f32x4 y = *reinterpret_cast<const f32x4 *>(all_tiles + v * TB + ((w * NQ + i) * 64 + lane) * 16);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) out[i][e] = fmaf(share, y[e], out[i][e]);
+            }
+        }
+        if (to[x]) {
+            const float inv = l_all != 0.f ? 1.0f / l_all : 0.f;
+            if (!s.whole() && w == 0 && u == 0) {
+                p.stats[(int64_t)s.place * 2 * ROWS + 16 * x + j] = reference_left(m_all, l_all);
+                p.stats[(int64_t)s.place * 2 * ROWS + ROWS + 16 * x + j] = l_all;
+            }
+#pragma unroll
+            for (int i = 0; i < NQ; ++i) {
+                const int col = 16 * (w * NQ + i) + 4 * u;
+                if (s.whole()) {
+                    if (col < p.d) store4<BF16 ? SMHA_BF16 : SMHA_F16>(to[x], col, out[i][0] * inv, out[i][1] * inv, out[i][2] * inv, out[i][3] * inv);
+                } else {
+                    *reinterpret_cast<f32x4 *>(p.parts + ((int64_t)s.place * ROWS + 16 * x + j) * D + col) = out[i];
+                }
+            }
+        }
+    }
+}
+
+// Many rows on the same keys: four waves of 32 rows share tiles of 64 keys, which all of them unpack into LDS, the next while one is used.  From there it is as in
+// smha_sink_fwd, in binary16 throughout.
+template <int D, bool BF16>
+__global__ void __launch_bounds__(256, D == 64 ? 3 : 2) smha_packed_wide(const PackedParams p) {
+    constexpr int NS = D / 16, NDT = D / 32, TB = 64 * D * 2, ROWS = 128, PF = D == 128 ? 8 : 4;
+    __shared__ __attribute__((aligned(1024))) char smem[4 * TB];  // K[0], K[1], V[0], V[1]
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = lane & 31, hh = lane >> 5;
+    const float NEG_INF = -__builtin_inff();
+
+    const PackedSegment s = packed_segment<64, ROWS, 1>(p, lane);
+    if (s.b < 0) return;
+    const int rows = p.G * p.T;
+    const auto keys = PackedKeys<64>::of(p, s.length, s.rows0, ROWS);
+    const int row0 = s.rows0 + 32 * w, row = row0 + j, t = row / p.G, g = row - t * p.G, h = s.hk * p.G + g;
+    const int pos = row < rows ? keys.len - p.T + t : -1;  // below 0: no such query
+    const int wp0 = keys.len - p.T + row0 / p.G, wp1 = row0 < rows ? keys.len - p.T + (min(row0 + 32, rows) - 1) / p.G : -1;  // the wave's positions
+    const bool every = wp0 >= 0 && row0 + 32 <= rows;
+    u32x4 qf[NS];
+    const float c = fmaxf(p.c * load_query<NS, BF16, false>(qf, p.Q + s.b * p.qs.b + h * p.qs.h + t * p.qs.s, pos >= 0, p.d, [&](int i) { return 16 * i + 8 * hh; }), 0x1p-126f);
+    const float thr = raised_over(c);
+
+    // this lane's part of a tile: D / 4 columns of key 16 w + lane % 16
+    const int kj = 16 * w + (lane & 15), ku = lane >> 4;
+    const PackedLoad<D> loadK(p.K + s.b * p.ks.b + s.hk * p.ks.h, p.ks.s, keys, p.d, ku), loadV(p.V + s.b * p.vs.b + s.hk * p.vs.h, p.vs.s, keys, p.d, ku);
+    auto leave = [&](char *tile, const typename PackedLoad<D>::Raw &x, int i) __attribute__((always_inline)) {
+        *reinterpret_cast<u32x4 *>(tile + kj * D * 2 + (((D / 32 * ku + i) ^ swz_both<D>(kj)) * 16)) = unpack8(x.code[i], x.head);
+    };
+    const int begin = (int)((int64_t)keys.n * s.part / s.parts), end = (int)((int64_t)keys.n * (s.part + 1) / s.parts);
+    typename PackedLoad<D>::Raw k_raw, v_raw;
+    if (begin < end) {
+        k_raw = loadK(keys.key(begin) + kj);
+        v_raw = loadV(keys.key(begin) + kj);
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) {
+            leave(smem, k_raw, i);
+            leave(smem + 2 * TB, v_raw, i);
+        }
+    }
+    if (begin + 1 < end) {
+        k_raw = loadK(keys.key(begin + 1) + kj);
+        v_raw = loadV(keys.key(begin + 1) + kj);
+    }
+
+    const int rd = j * D * 2 + ((hh ^ swz_both<D>(j)) * 16);
+    const int tr_row = 4 * hh + ((lane & 15) >> 2);
+    const int tr = tr_row * D * 2 + ((swz_both<D>(tr_row) ^ (2 * ((lane >> 4) & 1) + ((lane & 3) >> 1))) * 16) + (lane & 1) * 8;
+    float m_run = NEG_INF, l_run = 0.f;
+    f32x16 o[NDT];
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt) o[dt] = zeros16();
     __syncthreads();
-    float mu[4], m_all = NEG_INF, l_all = 0.f;
-    f32x4 out[NQ];
+    for (int tile = begin; tile < end; ++tile) {
+        const int par = (tile - begin) & 1, key = keys.key(tile);
+        if (tile + 1 < end) {
 #pragma unroll
-    for (int x = 0; x < 4; ++x) {
-        mu[x] = team[x][0][j];
-        m_all = fmaxf(m_all, mu[x]);
-    }
-#pragma unroll
-    for (int i = 0; i < NQ; ++i) out[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int x = 0; x < 4; ++x) {
-        const float share = mu[x] != NEG_INF ? fast_exp2(mu[x] - m_all) : 0.f;
-        l_all = fmaf(share, team[x][1][j], l_all);
-#pragma unroll
-        for (int i = 0; i < NQ; ++i) {
-            const f32x4 v = *reinterpret_cast<const f32x4 *>(all_tiles + x * TB + ((w * NQ + i) * 64 + lane) * 16);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) out[i][e] = fmaf(share, v[e], out[i][e]);
+            for (int i = 0; i < D / 32; ++i) {
+                leave(smem + (par ^ 1) * TB, k_raw, i);
+                leave(smem + (2 + (par ^ 1)) * TB, v_raw, i);
+            }
+            if (tile + 2 < end) {
+                k_raw = loadK(keys.key(tile + 2) + kj);
+                v_raw = loadV(keys.key(tile + 2) + kj);
+            }
         }
-    }
-    if (row < rows) {
-        const float inv = l_all != 0.f ? 1.0f / l_all : 0.f;
-        uint16_t *const to = p.O + b * p.os.b + (hk * p.G + g) * p.os.h + t * p.os.s;
+        if (wp1 >= 0 && key <= wp1 && (wp0 - key - 63 < p.window || key < p.n_sink)) {  // some row of the wave sees some key
+            const char *const Kt = smem + par * TB, *const Vt = smem + (2 + par) * TB;
+            f32x16 acc[2] = {zeros16(), zeros16()};
+            auto k_frag = [&](int i) __attribute__((always_inline)) { return *reinterpret_cast<const u32x4 *>(Kt + ((rd ^ (32 * (i >> 1))) + 64 * (i & 1) * D)); };
+            u32x4 kf[PF];
 #pragma unroll
-        for (int i = 0; i < NQ; ++i) {
-            const int col = 16 * (w * NQ + i) + 4 * u;
-            if (col < p.d) store4<BF16 ? SMHA_BF16 : SMHA_F16>(to, col, out[i][0] * inv, out[i][1] * inv, out[i][2] * inv, out[i][3] * inv);
+            for (int i = 0; i < PF; ++i) kf[i] = k_frag(i);
+#pragma unroll
+            for (int i = 0; i < 2 * NS; ++i) {
+                acc[i & 1] = mfma32<false>(kf[i % PF], qf[i >> 1], acc[i & 1]);
+                if (i + PF < 2 * NS) kf[i % PF] = k_frag(i + PF);
+            }
+            if (!(every && key + 63 <= wp0 && (wp1 - key < p.window || key + 63 < p.n_sink))) {  // not every row sees every key
+                const uint64_t word = pos >= 0 ? low_bits(pos - key + 1) & (~low_bits(pos - p.window + 1 - key) | low_bits(p.n_sink - key)) : 0;
+#pragma unroll
+                for (int kt = 0; kt < 2; ++kt) {
+                    const u32x16 keep = keep_of((uint32_t)(word >> (32 * kt)) >> (4 * hh)), sc = __builtin_bit_cast(u32x16, acc[kt]);
+                    acc[kt] = __builtin_bit_cast(f32x16, (sc & keep) | (~keep & 0xFF800000u));
+                }
+            }
+            float mt = NEG_INF;
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) mt = fmaxf(mt, acc[kt][r]);
+            if (__builtin_amdgcn_ballot_w64(mt > m_run + thr) != 0) {
+                mt = fmaxf(mt, __shfl_xor(mt, 32));
+                const float m_new = fmaxf(m_run, mt), alpha = fast_exp2((m_run - (m_new == NEG_INF ? 0.f : m_new)) * c);
+                m_run = m_new;
+                l_run *= alpha;
+#pragma unroll
+                for (int dt = 0; dt < NDT; ++dt) o[dt] *= alpha;
+            }
+            const float mc = (m_run == NEG_INF ? 0.f : m_run) * c;
+            u32x4 pf[4];
+            auto p_pair = [&](int cu, int q) __attribute__((always_inline)) {
+                const float e0 = fast_exp2(fmaf(acc[cu >> 1][8 * (cu & 1) + 2 * q], c, -mc)), e1 = fast_exp2(fmaf(acc[cu >> 1][8 * (cu & 1) + 2 * q + 1], c, -mc));
+                pf[cu][q] = pack2<false>(e0, e1);
+                l_run += e0 + e1;
+            };
+            auto v_frag = [&](int i) __attribute__((always_inline)) {
+                const char *const at = Vt + ((tr ^ (64 * (i % NDT))) + 32 * (i / NDT) * D), *const at8 = Vt + ((tr ^ (64 * (i % NDT)) ^ 32) + 32 * (i / NDT) * D + 16 * D);
+                const u32x2 lo = lds_read_tr(reinterpret_cast<const uint16_t *>(at)), hi = lds_read_tr(reinterpret_cast<const uint16_t *>(at8));
+                return u32x4{lo[0], lo[1], hi[0], hi[1]};
+            };
+            u32x4 vf[PF];
+#pragma unroll
+            for (int i = 0; i < PF; ++i) vf[i] = v_frag(i);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) p_pair(0, q);
+#pragma unroll
+            for (int i = 0; i < 4 * NDT; ++i) {
+                const int cu = i / NDT, dt = i % NDT;
+                o[dt] = mfma32<false>(vf[i % PF], pf[cu], o[dt]);
+                if (i + PF < 4 * NDT) vf[i % PF] = v_frag(i + PF);
+                if (cu < 3) {
+#pragma unroll
+                    for (int q = (4 * dt + NDT - 1) / NDT; q < (4 * dt + NDT + 3) / NDT; ++q) p_pair(cu + 1, q);
+                }
+            }
         }
+        __syncthreads();
+    }
+
+    const float l = l_run + __shfl_xor(l_run, 32);
+    if (p.slots && s.part == 0 && threadIdx.x == 0) p.info[s.group] = int2{s.place, s.parts};
+    if (row >= rows) return;
+    if (s.whole()) {
+        const float inv = l != 0.f ? 1.0f / l : 0.f;
+        uint16_t *const to = p.O + s.b * p.os.b + h * p.os.h + t * p.os.s;
+#pragma unroll
+        for (int i = 0; i < D / 8; ++i) {
+            const int col = 8 * i + 4 * hh;
+            if (col < p.d)
+                store4<BF16 ? SMHA_BF16 : SMHA_F16>(to, col, o[i / 4][4 * (i % 4)] * inv, o[i / 4][4 * (i % 4) + 1] * inv, o[i / 4][4 * (i % 4) + 2] * inv, o[i / 4][4 * (i % 4) + 3] * inv);
+        }
+    } else {
+        if (hh == 0) {
+            p.stats[(int64_t)s.place * 2 * ROWS + 32 * w + j] = reference_left(m_run * c, l);
+            p.stats[(int64_t)s.place * 2 * ROWS + ROWS + 32 * w + j] = l;
+        }
+        float *const part = p.parts + ((int64_t)s.place * ROWS + 32 * w + j) * D + 4 * hh;
+#pragma unroll
+        for (int i = 0; i < D / 8; ++i)
+            *reinterpret_cast<f32x4 *>(part + 8 * i) = f32x4{o[i / 4][4 * (i % 4)], o[i / 4][4 * (i % 4) + 1], o[i / 4][4 * (i % 4) + 2], o[i / 4][4 * (i % 4) + 3]};
+    }
+}
+
+// Joins the segments of a row: W waves a row, wave v takes segments v, v + W, ..., four at a time; a lane D / 64 columns.
+template <int D, int ROWS, int W, bool BF16>
+__global__ void __launch_bounds__(256) smha_packed_join(const PackedParams p) {
+    constexpr int E = D / 64, RPW = 4 / W;
+    __shared__ float lds_ml[2][4];
+    __shared__ float lds_o[4][D];
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), v = w % W, rows = p.G * p.T;
+    const int id = (int)blockIdx.x * RPW + w / W, bh = id / rows, row = id - bh * rows, b = bh / p.Hkv, hk = bh - b * p.Hkv, t = row / p.G, g = row - t * p.G;
+    if (b >= p.B) return;  // (with W = 4 for all of a workgroup's waves or none; with W = 1 none waits for another)
+    const int2 info = uniform_load(p.info + (int64_t)bh * p.row_tiles + row / ROWS);
+    if (info.y <= 1) return;  // written whole
+    const int64_t place0 = info.x;
+    const int in_tile = row % ROWS;
+    const float NEG_INF = -__builtin_inff();
+    float m = NEG_INF, sum = 0.f, acc[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) acc[e] = 0.f;
+    for (int i0 = v; i0 < info.y; i0 += 4 * W) {
+        float ref[4], part[4], x[4][E], top = m;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int64_t place = place0 + (i0 + W * q < info.y ? i0 + W * q : i0);
+            const float *const at = p.parts + (place * ROWS + in_tile) * D + E * lane;
+            ref[q] = p.stats[place * 2 * ROWS + in_tile];
+            part[q] = p.stats[place * 2 * ROWS + ROWS + in_tile];
+#pragma unroll
+            for (int e = 0; e < E; ++e) x[q][e] = at[e];
+        }
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            if (i0 + W * q >= info.y) ref[q] = NEG_INF;
+            top = fmaxf(top, ref[q]);
+        }
+        const float old = m != NEG_INF ? fast_exp2(m - top) : 0.f;
+        sum *= old;
+#pragma unroll
+        for (int e = 0; e < E; ++e) acc[e] *= old;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const float share = ref[q] != NEG_INF ? fast_exp2(ref[q] - top) : 0.f;
+            sum = ref[q] != NEG_INF ? fmaf(share, part[q], sum) : sum;
+#pragma unroll
+            for (int e = 0; e < E; ++e) acc[e] = ref[q] != NEG_INF ? fmaf(share, x[q][e], acc[e]) : acc[e];
+        }
+        m = top;
+    }
+    uint16_t *const to = p.O + b * p.os.b + (hk * p.G + g) * p.os.h + t * p.os.s;
+    if constexpr (W == 1) {
+        const float inv = sum != 0.f ? 1.0f / sum : 0.f;
+        if (E * lane < p.d) {
+            if constexpr (E == 2) *reinterpret_cast<uint32_t *>(to + 2 * lane) = pack2<BF16>(acc[0] * inv, acc[1] * inv);
+            else to[lane] = (uint16_t)pack2<BF16>(acc[0] * inv, 0.f);
+        }
+    } else {
+        if (lane == 0) {
+            lds_ml[0][v] = m;
+            lds_ml[1][v] = sum;
+        }
+#pragma unroll
+        for (int e = 0; e < E; ++e) lds_o[v][E * lane + e] = acc[e];
+        __syncthreads();
+        const float top = fmaxf(fmaxf(lds_ml[0][0], lds_ml[0][1]), fmaxf(lds_ml[0][2], lds_ml[0][3]));
+        float share[4], l = 0.f;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            share[q] = lds_ml[0][q] != NEG_INF ? fast_exp2(lds_ml[0][q] - top) : 0.f;
+            l = fmaf(share[q], lds_ml[1][q], l);
+        }
+        const float inv = l != 0.f ? 1.0f / l : 0.f;
+        for (int col = threadIdx.x; col < p.d; col += 256)
+            to[col] = (uint16_t)pack2<BF16>((share[0] * lds_o[0][col] + share[1] * lds_o[1][col] + share[2] * lds_o[2][col] + share[3] * lds_o[3][col]) * inv, 0.f);
     }
 }
 
@@ -535,35 +914,76 @@ extern "C" smha_status_t smha_packed_read(const void *K, const void *V, void *K_
     return hipGetLastError() == hipSuccess ? SMHA_OK : SMHA_ERR_HIP;
 }
 
-static smha_status_t packed_attention_sizes(int B, int H, int Hkv, int T, int Sk, int d, int window, int n_sink) {
+// How a call is taken, and its workspace.
+struct PackedForm {
+    int rows, row_tiles, slots;  // rows of a tile: 16, 32 or 128; slots: 0 where a group is a segment
+    size_t stats, parts, total;  // after `info`
+};
+static size_t packed_up(size_t n) { return (n + 255) & ~(size_t)255; }
+
+static smha_status_t packed_form(PackedForm &f, int B, int H, int Hkv, int T, int Sk, int d, int window, int n_sink) {
     if (H < 1 || window < 0 || n_sink < 0) return SMHA_ERR_INVALID_ARG;
     const smha_status_t st = packed_sizes(B, Hkv, T, Sk, d);
     if (st != SMHA_OK) return st;
     if (H % Hkv) return SMHA_ERR_SHAPE;
     if ((int64_t)B * H > (1 << 24) || (int64_t)B * H * T > (1 << 24)) return SMHA_ERR_UNSUPPORTED;
+    const int D = d <= 64 ? 64 : 128, rows = H / Hkv * T;
+    f.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : 128;
+    const int KT = f.rows == 128 ? 64 : 32;
+    f.row_tiles = (rows + f.rows - 1) / f.rows;
+    const int64_t groups = (int64_t)B * Hkv * f.row_tiles;
+    if (groups * (Sk / KT + 8) > (1 << 30)) return SMHA_ERR_UNSUPPORTED;  // (tiles are counted in 32 bits)
+    const int64_t see = window == 0 || window > Sk ? Sk : window;
+    const int64_t tiles = std::min<int64_t>((Sk + KT - 1) / KT, (see + std::min(n_sink, Sk) + T) / KT + 3);
+    const int slots = 256 * (f.rows == 128 ? (D == 64 ? 3 : 2) : packed_workgroups(D, f.rows / 16));
+    const bool direct = f.rows == 128 ? groups >= slots || tiles <= 8 : tiles <= 24;
+    f.slots = direct ? 0 : slots;
+    f.stats = f.parts = f.total = 0;
+    if (direct) return SMHA_OK;
+    // cut groups are longer than a segment, so that there are fewer of them than slots, and their segments no more than that and one each
+    const int64_t places = std::min(std::min<int64_t>(2 * slots, slots + groups), groups * ((tiles + 3) / 4));
+    f.stats = packed_up(groups * sizeof(int2));
+    f.parts = f.stats + packed_up((size_t)places * 2 * f.rows * 4);
+    f.total = f.parts + (size_t)places * f.rows * D * 4;
     return SMHA_OK;
 }
 
 extern "C" smha_status_t smha_packed_workspace(int B, int H, int Hkv, int T, int Sk, int d, int window, int n_sink, size_t *need) {
     if (!need) return SMHA_ERR_INVALID_ARG;
-    const smha_status_t st = packed_attention_sizes(B, H, Hkv, T, Sk, d, window, n_sink);
-    if (st != SMHA_OK) return st;
-    *need = 0;
-    return SMHA_OK;
+    PackedForm f{};
+    const smha_status_t st = packed_form(f, B, H, Hkv, T, Sk, d, window, n_sink);
+    if (st == SMHA_OK) *need = f.total;
+    return st;
+}
+
+template <int D, bool BF16> static hipError_t launch_packed(const PackedParams &pp, const PackedForm &f, hipStream_t stream) {
+    const int groups = pp.B * pp.Hkv * pp.row_tiles, segments = groups + pp.slots;
+    const dim3 grid(8 * ((segments + 7) / 8));
+    auto *const part = f.rows == 16 ? smha_packed_part<D, 1, BF16> : f.rows == 32 ? smha_packed_part<D, 2, BF16> : smha_packed_wide<D, BF16>;
+    hipLaunchKernelGGL(part, grid, dim3(256), 0, stream, pp);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || !pp.slots) return e;
+    const int rows = pp.B * pp.H * pp.T;
+    if (f.rows == 128 && rows > 4096) hipLaunchKernelGGL((smha_packed_join<D, 128, 1, BF16>), dim3((rows + 3) / 4), dim3(256), 0, stream, pp);
+    else if (f.rows == 128) hipLaunchKernelGGL((smha_packed_join<D, 128, 4, BF16>), dim3(rows), dim3(256), 0, stream, pp);
+    else if (f.rows == 32) hipLaunchKernelGGL((smha_packed_join<D, 32, 4, BF16>), dim3(rows), dim3(256), 0, stream, pp);
+    else hipLaunchKernelGGL((smha_packed_join<D, 16, 4, BF16>), dim3(rows), dim3(256), 0, stream, pp);
+    return hipGetLastError();
 }
 
 extern "C" smha_status_t smha_packed_forward(const void *Q, const void *K, const void *V, void *O, const int32_t *lengths, int B, int H, int Hkv, int T, int Sk, int d,
                                              smha_dtype_t dtype, const int64_t q_strides[3], const int64_t k_strides[3], const int64_t v_strides[3], const int64_t o_strides[3],
                                              int window, int n_sink, float scale, void *workspace, size_t workspace_bytes, void *hip_stream) {
     if (!Q || !K || !V || !O || !lengths) return SMHA_ERR_INVALID_ARG;
-    const smha_status_t st = packed_attention_sizes(B, H, Hkv, T, Sk, d, window, n_sink);
+    PackedForm f{};
+    const smha_status_t st = packed_form(f, B, H, Hkv, T, Sk, d, window, n_sink);
     if (st != SMHA_OK) return st;
     if (dtype != SMHA_F16 && dtype != SMHA_BF16) return SMHA_ERR_UNSUPPORTED;
+    if (workspace_bytes < f.total || (f.total && !workspace)) return SMHA_ERR_INVALID_ARG;
     if (((uintptr_t)Q | (uintptr_t)O | (uintptr_t)workspace) & 15 || ((uintptr_t)K | (uintptr_t)V) & 3) return SMHA_ERR_UNSUPPORTED;
     if (!value_strides_fit(q_strides, T, d) || !value_strides_fit(o_strides, T, d) || !packed_strides_fit(k_strides, Sk, d) || !packed_strides_fit(v_strides, Sk, d))
         return SMHA_ERR_UNSUPPORTED;
     if (!apart(o_strides, B, H, T, d)) return SMHA_ERR_UNSUPPORTED;
-    (void)workspace_bytes;
     PackedParams pp{};
     pp.Q = (const uint16_t *)Q; pp.K = (const uint8_t *)K; pp.V = (const uint8_t *)V; pp.O = (uint16_t *)O;
     pp.qs = value_strides(q_strides, H, T, d); pp.os = value_strides(o_strides, H, T, d);
@@ -572,10 +992,14 @@ extern "C" smha_status_t smha_packed_forward(const void *Q, const void *K, const
     pp.B = B; pp.H = H; pp.Hkv = Hkv; pp.G = H / Hkv; pp.T = T; pp.Sk = Sk; pp.d = d;
     pp.window = window == 0 || window > Sk ? Sk : window;
     pp.n_sink = std::min(n_sink, Sk);
-    pp.row_tiles = (pp.G * T + 15) / 16;
+    pp.row_tiles = f.row_tiles;
+    pp.slots = f.slots;
     pp.c = (scale > 0.f ? scale : 1.0f / std::sqrt((float)d)) * 1.4426950408889634f;
+    char *const ws = (char *)workspace;
+    pp.info = (int2 *)ws; pp.stats = (float *)(ws + f.stats); pp.parts = (float *)(ws + f.parts);
+    const hipStream_t stream = (hipStream_t)hip_stream;
     const bool bf16 = dtype == SMHA_BF16;
-    auto *const part = d <= 64 ? (bf16 ? smha_packed_part<64, true> : smha_packed_part<64, false>) : (bf16 ? smha_packed_part<128, true> : smha_packed_part<128, false>);
-    hipLaunchKernelGGL(part, dim3((unsigned)(B * Hkv * pp.row_tiles)), dim3(256), 0, (hipStream_t)hip_stream, pp);
-    return hipGetLastError() == hipSuccess ? SMHA_OK : SMHA_ERR_HIP;
+    const hipError_t e = d <= 64 ? (bf16 ? launch_packed<64, true>(pp, f, stream) : launch_packed<64, false>(pp, f, stream))
+                                 : (bf16 ? launch_packed<128, true>(pp, f, stream) : launch_packed<128, false>(pp, f, stream));
+    return e == hipSuccess ? SMHA_OK : SMHA_ERR_HIP;
 }
