@@ -137,7 +137,8 @@ def _load():
 
 _native = None  # (forward of _smha_torch, address of smha_forward)
 _loading = threading.RLock()
-_LINKED = ("sink_forward", "sink_backward", "sink_workspace", "cache_forward", "cache_workspace", "cache_evict", "cache_evict_workspace")  # in link()'s order
+_LINKED = ("sink_forward", "sink_backward", "sink_workspace", "cache_forward", "cache_workspace", "cache_evict", "cache_evict_workspace",
+           "packed_write", "packed_read", "packed_forward", "packed_workspace")  # in link()'s order
 
 
 def _left_to_python(*args):

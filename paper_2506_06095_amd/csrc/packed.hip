@@ -15,6 +15,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <type_traits>
 
 #include "device_common.hpp"
 #include "smha.h"
@@ -29,14 +30,20 @@ static int packed_groups(int d) { return (d + 31) / 32; }
 static int packed_row_bytes(int d) { return 4 * packed_groups(d) + d / 2; }
 
 // What eight codes stand for, as pairs of neighbours; `head`: s in the lower half, m in the upper.  0x6400 + c are the bits of 1024 + c and 0x5400 + 16 c those
-// of 64 + c, so that a pair is three instructions and a shared shift: and-or, the bias off (exact), fused multiply and add.
+// of 64 + c, so that a pair is three instructions and a shared shift: and-or, the bias off (exact), fused multiply and add.  (The first is written out: the
+// compiler makes two of it, each with a constant in its encoding.)
+__device__ __forceinline__ uint32_t and_or(uint32_t x, uint32_t mask, uint32_t bits) {
+    uint32_t y;
+    asm("v_and_or_b32 %0, %1, %2, %3" : "=v"(y) : "v"(x), "s"(mask), "v"(bits));
+    return y;
+}
 __device__ __forceinline__ u32x4 unpack8(uint32_t word, uint32_t head) {
     const f16x2 h = __builtin_bit_cast(f16x2, head), s = {h[0], h[0]}, m = {h[1], h[1]};
     u32x4 v;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const uint32_t w = i < 2 ? word : word >> 8;
-        const f16x2 biased = __builtin_bit_cast(f16x2, i & 1 ? (w & 0x00F000F0u) | 0x54005400u : (w & 0x000F000Fu) | 0x64006400u);
+        const f16x2 biased = __builtin_bit_cast(f16x2, i & 1 ? and_or(w, 0x00F000F0u, 0x54005400u) : and_or(w, 0x000F000Fu, 0x64006400u));
         const _Float16 bias = i & 1 ? (_Float16)64.f : (_Float16)1024.f;
         v[i] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(biased - f16x2{bias, bias}, s, m));
     }
@@ -211,6 +218,16 @@ __global__ void __launch_bounds__(256) smha_packed_get(const UnpackParams p) {
 // the tiles of keys that it sees are a group.  Memory bounds calls of few rows: a key's 10 d / 8 bytes meet 4 d G T operations.  There
 // every compute unit has to read, whatever the lengths are, so the key tiles of all groups are counted on the device and cut into as many segments, of
 // about the same length, as workgroups fit the chip; segments of one group are joined by a second kernel, in a fixed order.
+// n / d for 0 <= n <= 2^30, 0 < d < 2^30: in 32-bit floats, again for what that leaves, and by one for what that does.  (A segment is found by a chain of
+// divisions; the compiler's take twice as many instructions.)
+__device__ __forceinline__ int quotient(int n, int d) {
+    const float inv = __builtin_amdgcn_rcpf((float)d);
+    int q = (int)((float)n * inv);
+    q += (int)((float)(n - q * d) * inv);
+    const int rest = n - q * d;
+    return q + (rest >= d ? 1 : 0) - (rest < 0 ? 1 : 0);
+}
+
 struct PackedParams {
     const uint16_t *Q;
     const uint8_t *K, *V;
@@ -244,8 +261,8 @@ template <int KT> struct PackedKeys {
     static __device__ __forceinline__ PackedKeys of(const PackedParams &p, int length, int rows0, int rows_of_tile) {
         int t0 = 0, t1 = p.T - 1;
         if (p.row_tiles > 1) {
-            t0 = rows0 / p.G;
-            t1 = (min(rows0 + rows_of_tile, p.G * p.T) - 1) / p.G;
+            t0 = quotient(rows0, p.G);
+            t1 = quotient(min(rows0 + rows_of_tile, p.G * p.T) - 1, p.G);
         }
         return PackedKeys(length, p.T, p.Sk, p.window, p.n_sink, t0, t1);
     }
@@ -257,35 +274,39 @@ struct PackedSegment {
     int part, parts;
     int place, group;          // of its results
     __device__ __forceinline__ bool whole() const { return parts == 1; }
+    // its share of n tiles
+    __device__ __forceinline__ void share(int n, int &begin, int &end) const {
+        const int each = parts > 1 ? quotient(n, parts) : n, rest = n - each * parts;
+        begin = each * part + min(rest, part);
+        end = begin + each + (part < rest ? 1 : 0);
+    }
 };
 
-__device__ __forceinline__ int lanes_sum(int v) {
-#pragma unroll
-    for (int m = 32; m > 0; m >>= 1) v += __shfl_xor(v, m);
-    return __builtin_amdgcn_readfirstlane(v);
+// Running sums over a wave's lanes without LDS, and the last of them.
+template <int CTRL, int ROWS> __device__ __forceinline__ int plus_moved(int v) { return v + __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xF, false); }
+__device__ __forceinline__ int lanes_scan(int v) {
+    v = plus_moved<0x111, 0xF>(v);  // row_shr 1, 2, 4, 8: in rows of 16
+    v = plus_moved<0x112, 0xF>(v);
+    v = plus_moved<0x114, 0xF>(v);
+    v = plus_moved<0x118, 0xF>(v);
+    v = plus_moved<0x142, 0xA>(v);     // the first and third row's sums to the second and fourth
+    return plus_moved<0x143, 0xC>(v);  // the first half's to the second
 }
-__device__ __forceinline__ int lanes_scan(int v, int lane) {
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) {
-        const int below = __shfl_up(v, m);
-        if (lane >= m) v += below;
-    }
-    return v;
-}
+__device__ __forceinline__ int lanes_sum(int v) { return __builtin_amdgcn_readlane(lanes_scan(v), 63); }
 
-// The segment of a workgroup.  Every wave of the launch computes the same cut: `most` tiles a segment at most, so many that all tiles make `slots` segments;
-// groups shorter than that are a segment each, and then there are more: what does not fit at first starts as others end.  An XCD takes a run of
-// segments: those that read the same keys are neighbours.
+// The segment of a workgroup.  Every wave of the launch computes the same cut: `most` tiles a segment at most, so many that all tiles make `slots` segments.  A group's last
+// segment is shorter, so that there are more of them then; where that is most of what is over, `most` is raised by it (unless groups are too many for that: what does not fit
+// at first starts as others end).  An XCD takes a run of segments: those that read the same keys are neighbours.
 template <int KT, int ROWS, int TURN> __device__ __forceinline__ PackedSegment packed_segment(const PackedParams &p, int lane) {
     const int xcd = (int)blockIdx.x & 7, slot = (int)blockIdx.x >> 3;
     PackedSegment s{-1, 0, 0, 0, 0, 1, 0, 0};
     if (!p.slots) {
         const int n = p.B * p.Hkv * p.row_tiles, run = (n + 7) / 8, at = xcd * run + slot;
         if (slot >= run || at >= n) return s;
-        const int bh = at / p.row_tiles;  // a head's last rows, which see the most keys, come first
-        s.b = bh / p.Hkv;
-        s.hk = bh - s.b * p.Hkv;
-        s.rows0 = ROWS * (p.row_tiles - 1 - (at - bh * p.row_tiles));
+        const int hb = quotient(at, p.row_tiles);  // a head's last rows, which see the most keys, come first
+        s.hk = quotient(hb, p.B);  // (an XCD has sequences of all lengths)
+        s.b = hb - s.hk * p.B;
+        s.rows0 = ROWS * (p.row_tiles - 1 - (at - hb * p.row_tiles));
         s.length = uniform_load(p.lengths + s.b);
         return s;
     }
@@ -296,7 +317,7 @@ template <int KT, int ROWS, int TURN> __device__ __forceinline__ PackedSegment p
     auto entry = [&](int i) __attribute__((always_inline)) {
         Entry e{0, 0, 0, 0};
         if (i < E) {
-            e.b = p.row_tiles > 1 ? i / p.row_tiles : i;
+            e.b = p.row_tiles > 1 ? quotient(i, p.row_tiles) : i;
             e.rows0 = ROWS * (p.row_tiles - 1 - (i - e.b * p.row_tiles));
             e.length = p.lengths[e.b];
             e.n = PackedKeys<KT>::of(p, e.length, e.rows0, ROWS).n;
@@ -307,16 +328,27 @@ template <int KT, int ROWS, int TURN> __device__ __forceinline__ PackedSegment p
     int sum = first64.n;
     for (int i = 64; i < E; i += 64) sum += entry(i + lane).n;
     const int total = p.Hkv * lanes_sum(sum);
-    const int most = max(4, ((total + p.slots - 1) / p.slots + TURN - 1) / TURN * TURN);
-    auto parts_of = [&](int i, int n) __attribute__((always_inline)) { return i < E ? max(1, (n + most - 1) / most) : 0; };
-    sum = parts_of(lane, first64.n);
-    for (int i = 64; i < E; i += 64) sum += parts_of(i + lane, entry(i + lane).n);
-    const int n = p.Hkv * lanes_sum(sum), run = (n + 7) / 8;
+    auto parts_of = [&](int i, int n, int most) __attribute__((always_inline)) { return i < E ? max(1, quotient(n + most - 1, most)) : 0; };
+    auto segments = [&](int most) __attribute__((always_inline)) {
+        int sum = parts_of(lane, first64.n, most);
+        for (int i = 64; i < E; i += 64) sum += parts_of(i + lane, entry(i + lane).n, most);
+        return p.Hkv * lanes_sum(sum);
+    };
+    auto at_most = [&](int segments) __attribute__((always_inline)) { return max(4, (quotient(total + segments - 1, segments) + TURN - 1) / TURN * TURN); };
+    int most = at_most(p.slots), n = segments(most);
+    if (n > p.slots) {
+        const int over = n - quotient(total, most);
+        if (2 * over < p.slots) {
+            most = at_most(p.slots - over);
+            n = segments(most);
+        }
+    }
+    const int run = (n + 7) / 8;
     int at = xcd * run + slot, place = 0;
     if (slot >= run || at >= n) return s;
     for (int i0 = 0; i0 < E; i0 += 64) {
         const Entry e = i0 == 0 ? first64 : entry(i0 + lane);
-        const int parts = parts_of(i0 + lane, e.n), mine = p.Hkv * parts, upto = lanes_scan(mine, lane), cut = parts > 1 ? mine : 0, cut_upto = lanes_scan(cut, lane);
+        const int parts = parts_of(i0 + lane, e.n, most), mine = p.Hkv * parts, upto = lanes_scan(mine), cut = parts > 1 ? mine : 0, cut_upto = lanes_scan(cut);
         const uint64_t past = __builtin_amdgcn_ballot_w64(upto > at);
         if (past) {
             const int who = __builtin_ctzll(past);
@@ -325,7 +357,7 @@ template <int KT, int ROWS, int TURN> __device__ __forceinline__ PackedSegment p
             s.length = __builtin_amdgcn_readlane(e.length, who);
             s.parts = __builtin_amdgcn_readlane(parts, who);
             const int rest = at - (__builtin_amdgcn_readlane(upto, who) - __builtin_amdgcn_readlane(mine, who));
-            s.hk = rest / s.parts;
+            s.hk = quotient(rest, s.parts);
             s.part = rest - s.hk * s.parts;
             s.place = place + __builtin_amdgcn_readlane(cut_upto, who) - __builtin_amdgcn_readlane(cut, who) + rest;
             s.group = (s.b * p.Hkv + s.hk) * p.row_tiles + s.rows0 / ROWS;
@@ -418,6 +450,14 @@ template <int D> __device__ __forceinline__ int swz_values(int row) {
     else return (((row >> 1) & 3) << 1) | ((row >> 3) & 1);
 }
 
+// Which of 16 rows lane j unpacks into LDS: a write of 8 lanes' 16 bytes goes without conflicts where these chunks are apart, modulo 8, of rows swizzled as above (D: as by
+// swz_values; WIDE: as by swz_both).
+template <int D, bool WIDE = false> __device__ __forceinline__ int mixed(int j) {
+    if constexpr (D == 64) return ((j & 7) << 1) | (j >> 3);
+    else if constexpr (WIDE) return (j & 1) | ((j & 6) << 1) | ((j & 8) >> 2);
+    else return (j & 3) | ((j & 4) << 1) | ((j & 8) >> 1);
+}
+
 // Four waves take a segment's tiles of 32 keys in turn and join in LDS.  A lane unpacks D / 4 columns of two keys: keys are an operand as they come out; values go
 // through LDS once, for the transposing reads that make them the other product's.  NR tiles of 16 rows share what is unpacked.
 constexpr int packed_workgroups(int D, int NR) { return D == 64 ? (NR == 1 ? 4 : 3) : NR == 1 ? 3 : 2; }  // of a compute unit
@@ -434,21 +474,37 @@ __global__ void __launch_bounds__(256, packed_workgroups(D, NR)) smha_packed_par
     if (s.b < 0) return;
     const int rows = p.G * p.T;
     const auto keys = PackedKeys<32>::of(p, s.length, s.rows0, ROWS);
+    const PackedLoad<D> loadK(p.K + s.b * p.ks.b + s.hk * p.ks.h, p.ks.s, keys, p.d, u), loadV(p.V + s.b * p.vs.b + s.hk * p.vs.h, p.vs.s, keys, p.d, u);
+    int begin, end;
+    s.share(keys.n, begin, end);
+    begin += w;
+    const int vj = mixed<D>(j);  // the key of a value that this lane unpacks
+    struct Raw {
+        typename PackedLoad<D>::Raw k[2], v[2];
+    } raw[2];
+    auto request = [&](Raw &x, int tile) __attribute__((always_inline)) {
+        const int key = keys.key(tile);
+#pragma unroll
+        for (int a = 0; a < 2; ++a) x.k[a] = loadK(key + j + 16 * a);
+#pragma unroll
+        for (int a = 0; a < 2; ++a) x.v[a] = loadV(key + vj + 16 * a);
+    };
+    if (begin < end) request(raw[0], begin);
+    if (begin + 4 < end) request(raw[1], begin + 4);
+
     u32x4 qf[NR][NS];
     int pos[NR];  // below 0: no such query
     uint16_t *to[NR];
     float c[NR], thr[NR];
 #pragma unroll
     for (int x = 0; x < NR; ++x) {
-        const int row = s.rows0 + 16 * x + j, t = row / p.G, g = row - t * p.G, h = s.hk * p.G + g;
+        const int row = s.rows0 + 16 * x + j, t = quotient(row, p.G), g = row - t * p.G, h = s.hk * p.G + g;
         pos[x] = row < rows ? keys.len - p.T + t : -1;
         to[x] = row < rows ? p.O + s.b * p.os.b + h * p.os.h + t * p.os.s : nullptr;
         // (never 0: -inf times it)
         c[x] = fmaxf(p.c * load_query<NS, BF16, true>(qf[x], p.Q + s.b * p.qs.b + h * p.qs.h + t * p.qs.s, pos[x] >= 0, p.d, [&](int i) { return D / 4 * u + 8 * i; }), 0x1p-126f);
         thr[x] = raised_over(c[x]);
     }
-    const PackedLoad<D> loadK(p.K + s.b * p.ks.b + s.hk * p.ks.h, p.ks.s, keys, p.d, u), loadV(p.V + s.b * p.vs.b + s.hk * p.vs.h, p.vs.s, keys, p.d, u);
-
     float m_run[NR], l_run[NR];
     f32x4 o[NR][NC];
 #pragma unroll
@@ -459,20 +515,8 @@ __global__ void __launch_bounds__(256, packed_workgroups(D, NR)) smha_packed_par
         for (int ct = 0; ct < NC; ++ct) o[x][ct] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
     const int tr_row = 4 * u + (j >> 2);
-    const int begin = (int)((int64_t)keys.n * s.part / s.parts) + w, end = (int)((int64_t)keys.n * (s.part + 1) / s.parts);
-    typename PackedLoad<D>::Raw k_raw[2], v_raw[2];
-    auto request = [&](int tile) __attribute__((always_inline)) {
-        const int key = keys.key(tile) + j;
-#pragma unroll
-        for (int a = 0; a < 2; ++a) k_raw[a] = loadK(key + 16 * a);
-#pragma unroll
-        for (int a = 0; a < 2; ++a) v_raw[a] = loadV(key + 16 * a);
-    };
-    if (begin < end) request(begin);
-    for (int tile = begin; tile < end; tile += 4) {
+    auto step = [&](int tile, Raw &now) __attribute__((always_inline)) {
         const int key = keys.key(tile);
-        const typename PackedLoad<D>::Raw k_now[2] = {k_raw[0], k_raw[1]}, v_now[2] = {v_raw[0], v_raw[1]};
-        if (tile + 4 < end) request(tile + 4);
         // acc[x][a][r]: the score of query j and key 16 a + 4 u + r
         f32x4 acc[NR][2];
 #pragma unroll
@@ -481,7 +525,7 @@ __global__ void __launch_bounds__(256, packed_workgroups(D, NR)) smha_packed_par
         for (int i = 0; i < NS; ++i)
 #pragma unroll
             for (int a = 0; a < 2; ++a) {
-                const u32x4 kf = unpack8(k_now[a].code[i], k_now[a].head);
+                const u32x4 kf = unpack8(now.k[a].code[i], now.k[a].head);
 #pragma unroll
                 for (int x = 0; x < NR; ++x) acc[x][a] = mfma16(kf, qf[x][i], acc[x][a]);
             }
@@ -490,7 +534,8 @@ __global__ void __launch_bounds__(256, packed_workgroups(D, NR)) smha_packed_par
         for (int a = 0; a < 2; ++a)
 #pragma unroll
             for (int i = 0; i < NS; ++i)
-                *reinterpret_cast<u32x4 *>(smem + (16 * a + j) * D * 2 + (((D / 32 * u + i) ^ swz_values<D>(j)) * 16)) = unpack8(v_now[a].code[i], v_now[a].head);
+                *reinterpret_cast<u32x4 *>(smem + (16 * a + vj) * D * 2 + (((D / 32 * u + i) ^ swz_values<D>(vj)) * 16)) = unpack8(now.v[a].code[i], now.v[a].head);
+        if (tile + 8 < end) request(now, tile + 8);
         u32x4 pf[NR];
 #pragma unroll
         for (int x = 0; x < NR; ++x) {
@@ -533,6 +578,10 @@ __global__ void __launch_bounds__(256, packed_workgroups(D, NR)) smha_packed_par
             for (int x = 0; x < NR; ++x) o[x][ct] = mfma16(u32x4{lo[0], lo[1], hi[0], hi[1]}, pf[x], o[x][ct]);
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the tile is read
+    };
+    for (int tile = begin; tile < end; tile += 8) {
+        step(tile, raw[0]);
+        if (tile + 4 < end) step(tile + 4, raw[1]);
     }
 
     // The team joins: every wave leaves its accumulators in its own tile's place and takes a quarter of the columns of all four.
@@ -589,48 +638,60 @@ __global__ void __launch_bounds__(256, packed_workgroups(D, NR)) smha_packed_par
     }
 }
 
-// Many rows on the same keys: four waves of 32 rows share tiles of 64 keys, which all of them unpack into LDS, the next while one is used.  From there it is as in
-// smha_sink_fwd, in binary16 throughout.
-template <int D, bool BF16>
+// Many rows on the same keys: four waves share tiles of 64 keys, which all of them unpack into LDS, the next one under this one's first product, from words that were
+// requested two tiles before.  KH = 1: a wave takes 32 of 128 rows; KH = 2: a wave takes 32 of 64 rows and one half of the keys, and the halves are joined at the end.  From
+// LDS on it is as in smha_sink_fwd, in binary16 throughout.
+template <int D, int KH, bool BF16>
 __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) smha_packed_wide(const PackedParams p) {
-    constexpr int NS = D / 16, NDT = D / 32, TB = 64 * D * 2, ROWS = 128, PF = D == 128 ? 8 : 4;
+    constexpr int NS = D / 16, NDT = D / 32, NL = D / 32, TB = 64 * D * 2, ROWS = 128 / KH, KTS = 2 / KH;  // KTS: halves of a tile that a wave takes
+    constexpr int PF = KH == 1 && D == 128 ? 8 : 4;  // operands requested ahead
+    constexpr int AHEAD = KH;  // tiles whose words are on their way
     __shared__ __attribute__((aligned(1024))) char smem[4 * TB];  // K[0], K[1], V[0], V[1]
+    __shared__ float team[2][2][32];
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = lane & 31, hh = lane >> 5;
+    const int wr = KH == 1 ? w : w & 1, wk = KH == 1 ? 0 : w >> 1;  // the wave's rows, and its half of the keys
     const float NEG_INF = -__builtin_inff();
 
     const PackedSegment s = packed_segment<64, ROWS, 1>(p, lane);
     if (s.b < 0) return;
     const int rows = p.G * p.T;
     const auto keys = PackedKeys<64>::of(p, s.length, s.rows0, ROWS);
-    const int row0 = s.rows0 + 32 * w, row = row0 + j, t = row / p.G, g = row - t * p.G, h = s.hk * p.G + g;
+    const PackedLoad<D> loadK(p.K + s.b * p.ks.b + s.hk * p.ks.h, p.ks.s, keys, p.d, lane >> 4), loadV(p.V + s.b * p.vs.b + s.hk * p.vs.h, p.vs.s, keys, p.d, lane >> 4);
+    int begin, end;
+    s.share(keys.n, begin, end);
+    // this lane's part of a tile: D / 4 columns of one of the wave's 16 keys
+    const int kj = 16 * w + mixed<D, true>(lane & 15);
+    struct Raw {
+        typename PackedLoad<D>::Raw k, v;
+    } raw[AHEAD];
+    auto request = [&](Raw &x, int tile) __attribute__((always_inline)) {
+        const int key = keys.key(tile) + kj;
+        x.k = loadK(key);
+        x.v = loadV(key);
+    };
+    if (begin < end) request(raw[0], begin);
+    if (AHEAD == 2 && begin + 1 < end) request(raw[AHEAD - 1], begin + 1);
+
+    const int row0 = s.rows0 + 32 * wr, row = row0 + j, t = quotient(row, p.G), g = row - t * p.G, h = s.hk * p.G + g;
     const int pos = row < rows ? keys.len - p.T + t : -1;  // below 0: no such query
-    const int wp0 = keys.len - p.T + row0 / p.G, wp1 = row0 < rows ? keys.len - p.T + (min(row0 + 32, rows) - 1) / p.G : -1;  // the wave's positions
+    const int wp0 = keys.len - p.T + quotient(row0, p.G), wp1 = row0 < rows ? keys.len - p.T + quotient(min(row0 + 32, rows) - 1, p.G) : -1;  // the wave's positions
     const bool every = wp0 >= 0 && row0 + 32 <= rows;
     u32x4 qf[NS];
     const float c = fmaxf(p.c * load_query<NS, BF16, false>(qf, p.Q + s.b * p.qs.b + h * p.qs.h + t * p.qs.s, pos >= 0, p.d, [&](int i) { return 16 * i + 8 * hh; }), 0x1p-126f);
     const float thr = raised_over(c);
 
-    // this lane's part of a tile: D / 4 columns of key 16 w + lane % 16
-    const int kj = 16 * w + (lane & 15), ku = lane >> 4;
-    const PackedLoad<D> loadK(p.K + s.b * p.ks.b + s.hk * p.ks.h, p.ks.s, keys, p.d, ku), loadV(p.V + s.b * p.vs.b + s.hk * p.vs.h, p.vs.s, keys, p.d, ku);
-    auto leave = [&](char *tile, const typename PackedLoad<D>::Raw &x, int i) __attribute__((always_inline)) {
-        *reinterpret_cast<u32x4 *>(tile + kj * D * 2 + (((D / 32 * ku + i) ^ swz_both<D>(kj)) * 16)) = unpack8(x.code[i], x.head);
+    // the i-th of 2 NL chunks of a tile, keys' first
+    const int lv = kj * D * 2 + ((NL * (lane >> 4) ^ (swz_both<D>(kj) & ~(NL - 1))) * 16), lx = swz_both<D>(kj) & (NL - 1);
+    auto leave = [&](int at, int par, const Raw &x, int i) __attribute__((always_inline)) {
+        char *const tile = smem + (i < NL ? par : 2 + par) * TB;
+        const typename PackedLoad<D>::Raw &y = i < NL ? x.k : x.v;
+        *reinterpret_cast<u32x4 *>(tile + at + (((i % NL) ^ lx) * 16)) = unpack8(y.code[i % NL], y.head);
     };
-    const int begin = (int)((int64_t)keys.n * s.part / s.parts), end = (int)((int64_t)keys.n * (s.part + 1) / s.parts);
-    typename PackedLoad<D>::Raw k_raw, v_raw;
     if (begin < end) {
-        k_raw = loadK(keys.key(begin) + kj);
-        v_raw = loadV(keys.key(begin) + kj);
 #pragma unroll
-        for (int i = 0; i < D / 32; ++i) {
-            leave(smem, k_raw, i);
-            leave(smem + 2 * TB, v_raw, i);
-        }
+        for (int i = 0; i < 2 * NL; ++i) leave(lv, 0, raw[0], i);
     }
-    if (begin + 1 < end) {
-        k_raw = loadK(keys.key(begin + 1) + kj);
-        v_raw = loadV(keys.key(begin + 1) + kj);
-    }
+    if (begin + AHEAD < end) request(raw[0], begin + AHEAD);
 
     const int rd = j * D * 2 + ((hh ^ swz_both<D>(j)) * 16);
     const int tr_row = 4 * hh + ((lane & 15) >> 2);
@@ -640,42 +701,42 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) smha_packed_wide(const P
 #pragma unroll
     for (int dt = 0; dt < NDT; ++dt) o[dt] = zeros16();
     __syncthreads();
-    for (int tile = begin; tile < end; ++tile) {
-        const int par = (tile - begin) & 1, key = keys.key(tile);
-        if (tile + 1 < end) {
+    auto step = [&](int tile, auto par_) __attribute__((always_inline)) {
+        const int par = par_;
+        Raw &next = raw[AHEAD == 2 ? par ^ 1 : 0];  // of tile + 1
+        const bool more = tile + 1 < end;
+        const int key = keys.key(tile), key_w = key + 32 * wk;
+        constexpr int KW = 32 * KTS;
+        if (more) {
 #pragma unroll
-            for (int i = 0; i < D / 32; ++i) {
-                leave(smem + (par ^ 1) * TB, k_raw, i);
-                leave(smem + (2 + (par ^ 1)) * TB, v_raw, i);
-            }
-            if (tile + 2 < end) {
-                k_raw = loadK(keys.key(tile + 2) + kj);
-                v_raw = loadV(keys.key(tile + 2) + kj);
-            }
+            for (int i = 0; i < 2 * NL; ++i) leave(lv, par ^ 1, next, i);
+            if (tile + AHEAD + 1 < end) request(next, tile + AHEAD + 1);
         }
-        if (wp1 >= 0 && key <= wp1 && (wp0 - key - 63 < p.window || key < p.n_sink)) {  // some row of the wave sees some key
-            const char *const Kt = smem + par * TB, *const Vt = smem + (2 + par) * TB;
-            f32x16 acc[2] = {zeros16(), zeros16()};
-            auto k_frag = [&](int i) __attribute__((always_inline)) { return *reinterpret_cast<const u32x4 *>(Kt + ((rd ^ (32 * (i >> 1))) + 64 * (i & 1) * D)); };
+        if (wp1 >= 0 && key_w <= wp1 && (wp0 - key_w - (KW - 1) < p.window || key_w < p.n_sink)) {  // some row of the wave sees some key
+            const char *const Kt = smem + par * TB + 32 * wk * D * 2, *const Vt = smem + (2 + par) * TB + 32 * wk * D * 2;
+            f32x16 acc[KTS];
+#pragma unroll
+            for (int kt = 0; kt < KTS; ++kt) acc[kt] = zeros16();
+            auto k_frag = [&](int i) __attribute__((always_inline)) { return *reinterpret_cast<const u32x4 *>(Kt + ((rd ^ (32 * (i / KTS))) + 64 * (i % KTS) * D)); };
             u32x4 kf[PF];
 #pragma unroll
             for (int i = 0; i < PF; ++i) kf[i] = k_frag(i);
 #pragma unroll
-            for (int i = 0; i < 2 * NS; ++i) {
-                acc[i & 1] = mfma32<false>(kf[i % PF], qf[i >> 1], acc[i & 1]);
-                if (i + PF < 2 * NS) kf[i % PF] = k_frag(i + PF);
+            for (int i = 0; i < KTS * NS; ++i) {
+                acc[i % KTS] = mfma32<false>(kf[i % PF], qf[i / KTS], acc[i % KTS]);
+                if (i + PF < KTS * NS) kf[i % PF] = k_frag(i + PF);
             }
-            if (!(every && key + 63 <= wp0 && (wp1 - key < p.window || key + 63 < p.n_sink))) {  // not every row sees every key
-                const uint64_t word = pos >= 0 ? low_bits(pos - key + 1) & (~low_bits(pos - p.window + 1 - key) | low_bits(p.n_sink - key)) : 0;
+            if (!(every && key_w + KW - 1 <= wp0 && (wp1 - key_w < p.window || key_w + KW - 1 < p.n_sink))) {  // not every row sees every key
+                const uint64_t word = pos >= 0 ? low_bits(pos - key_w + 1) & (~low_bits(pos - p.window + 1 - key_w) | low_bits(p.n_sink - key_w)) : 0;
 #pragma unroll
-                for (int kt = 0; kt < 2; ++kt) {
+                for (int kt = 0; kt < KTS; ++kt) {
                     const u32x16 keep = keep_of((uint32_t)(word >> (32 * kt)) >> (4 * hh)), sc = __builtin_bit_cast(u32x16, acc[kt]);
                     acc[kt] = __builtin_bit_cast(f32x16, (sc & keep) | (~keep & 0xFF800000u));
                 }
             }
             float mt = NEG_INF;
 #pragma unroll
-            for (int kt = 0; kt < 2; ++kt)
+            for (int kt = 0; kt < KTS; ++kt)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) mt = fmaxf(mt, acc[kt][r]);
             if (__builtin_amdgcn_ballot_w64(mt > m_run + thr) != 0) {
@@ -687,7 +748,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) smha_packed_wide(const P
                 for (int dt = 0; dt < NDT; ++dt) o[dt] *= alpha;
             }
             const float mc = (m_run == NEG_INF ? 0.f : m_run) * c;
-            u32x4 pf[4];
+            u32x4 pf[2 * KTS];
             auto p_pair = [&](int cu, int q) __attribute__((always_inline)) {
                 const float e0 = fast_exp2(fmaf(acc[cu >> 1][8 * (cu & 1) + 2 * q], c, -mc)), e1 = fast_exp2(fmaf(acc[cu >> 1][8 * (cu & 1) + 2 * q + 1], c, -mc));
                 pf[cu][q] = pack2<false>(e0, e1);
@@ -704,20 +765,54 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) smha_packed_wide(const P
 #pragma unroll
             for (int q = 0; q < 4; ++q) p_pair(0, q);
 #pragma unroll
-            for (int i = 0; i < 4 * NDT; ++i) {
+            for (int i = 0; i < 2 * KTS * NDT; ++i) {
                 const int cu = i / NDT, dt = i % NDT;
                 o[dt] = mfma32<false>(vf[i % PF], pf[cu], o[dt]);
-                if (i + PF < 4 * NDT) vf[i % PF] = v_frag(i + PF);
-                if (cu < 3) {
+                if (i + PF < 2 * KTS * NDT) vf[i % PF] = v_frag(i + PF);
+                if (cu < 2 * KTS - 1) {
 #pragma unroll
                     for (int q = (4 * dt + NDT - 1) / NDT; q < (4 * dt + NDT + 3) / NDT; ++q) p_pair(cu + 1, q);
                 }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        // (not __syncthreads: that would wait for the words on their way)
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    if constexpr (AHEAD == 1) {
+        for (int tile = begin; tile < end; ++tile) step(tile, (tile - begin) & 1);
+    } else {  // (which words a step takes has to be known when it is compiled)
+        for (int tile = begin; tile < end; tile += 2) {
+            step(tile, std::integral_constant<int, 0>{});
+            if (tile + 1 < end) step(tile + 1, std::integral_constant<int, 1>{});
+        }
+    }
+
+    float l = l_run + __shfl_xor(l_run, 32), m = m_run * c;
+    if constexpr (KH == 2) {  // the keys' halves join: the second leaves its accumulators where the tiles were
+        f32x4 *const left = reinterpret_cast<f32x4 *>(smem + wr * (32 * D * 4));
+        if (wk == 1) {
+#pragma unroll
+            for (int i = 0; i < D / 8; ++i) left[i * 64 + lane] = f32x4{o[i / 4][4 * (i % 4)], o[i / 4][4 * (i % 4) + 1], o[i / 4][4 * (i % 4) + 2], o[i / 4][4 * (i % 4) + 3]};
+            if (hh == 0) {
+                team[wr][0][j] = m;
+                team[wr][1][j] = l;
             }
         }
         __syncthreads();
+        if (wk == 1) return;
+        const float mu = team[wr][0][j], top = fmaxf(m, mu), mine = m != NEG_INF ? fast_exp2(m - top) : 0.f, his = mu != NEG_INF ? fast_exp2(mu - top) : 0.f;
+        l = fmaf(his, team[wr][1][j], mine * l);
+        m = top;
+#pragma unroll
+        for (int i = 0; i < D / 8; ++i) {
+            const f32x4 y = left[i * 64 + lane];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[i / 4][4 * (i % 4) + e] = fmaf(his, y[e], mine * o[i / 4][4 * (i % 4) + e]);
+        }
     }
-
-    const float l = l_run + __shfl_xor(l_run, 32);
     if (p.slots && s.part == 0 && threadIdx.x == 0) p.info[s.group] = int2{s.place, s.parts};
     if (row >= rows) return;
     if (s.whole()) {
@@ -731,88 +826,93 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) smha_packed_wide(const P
         }
     } else {
         if (hh == 0) {
-            p.stats[(int64_t)s.place * 2 * ROWS + 32 * w + j] = reference_left(m_run * c, l);
-            p.stats[(int64_t)s.place * 2 * ROWS + ROWS + 32 * w + j] = l;
+            p.stats[(int64_t)s.place * 2 * ROWS + 32 * wr + j] = reference_left(m, l);
+            p.stats[(int64_t)s.place * 2 * ROWS + ROWS + 32 * wr + j] = l;
         }
-        float *const part = p.parts + ((int64_t)s.place * ROWS + 32 * w + j) * D + 4 * hh;
+        float *const part = p.parts + ((int64_t)s.place * ROWS + 32 * wr + j) * D + 4 * hh;
 #pragma unroll
         for (int i = 0; i < D / 8; ++i)
             *reinterpret_cast<f32x4 *>(part + 8 * i) = f32x4{o[i / 4][4 * (i % 4)], o[i / 4][4 * (i % 4) + 1], o[i / 4][4 * (i % 4) + 2], o[i / 4][4 * (i % 4) + 3]};
     }
 }
 
-// Joins the segments of a row: W waves a row, wave v takes segments v, v + W, ..., four at a time; a lane D / 64 columns.
+// Joins the segments of a row, W waves a row: D / 4 lanes read a segment's result, four columns each, and as many segments are read at once as there are
+// such lanes, four times over.  (What a row lasts is its chain of trips to memory.)
 template <int D, int ROWS, int W, bool BF16>
 __global__ void __launch_bounds__(256) smha_packed_join(const PackedParams p) {
-    constexpr int E = D / 64, RPW = 4 / W;
+    constexpr int CL = D / 4, SUB = 64 / CL, RPW = 4 / W;
     __shared__ float lds_ml[2][4];
-    __shared__ float lds_o[4][D];
-    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), v = w % W, rows = p.G * p.T;
-    const int id = (int)blockIdx.x * RPW + w / W, bh = id / rows, row = id - bh * rows, b = bh / p.Hkv, hk = bh - b * p.Hkv, t = row / p.G, g = row - t * p.G;
+    __shared__ __attribute__((aligned(16))) float lds_o[4][D];
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), rows = p.G * p.T, cl = lane % CL;
+    const int id = (int)blockIdx.x * RPW + w / W, bh = quotient(id, rows), row = id - bh * rows, b = quotient(bh, p.Hkv), hk = bh - b * p.Hkv, t = quotient(row, p.G), g = row - t * p.G;
     if (b >= p.B) return;  // (with W = 4 for all of a workgroup's waves or none; with W = 1 none waits for another)
     const int2 info = uniform_load(p.info + (int64_t)bh * p.row_tiles + row / ROWS);
     if (info.y <= 1) return;  // written whole
-    const int64_t place0 = info.x;
-    const int in_tile = row % ROWS;
+    const float *const stats = p.stats + (int64_t)info.x * 2 * ROWS + row % ROWS, *const parts = p.parts + ((int64_t)info.x * ROWS + row % ROWS) * D + 4 * cl;
     const float NEG_INF = -__builtin_inff();
-    float m = NEG_INF, sum = 0.f, acc[E];
-#pragma unroll
-    for (int e = 0; e < E; ++e) acc[e] = 0.f;
-    for (int i0 = v; i0 < info.y; i0 += 4 * W) {
-        float ref[4], part[4], x[4][E], top = m;
+    float m = NEG_INF, sum = 0.f;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    for (int i0 = (w % W) * SUB + lane / CL; i0 < info.y; i0 += 4 * W * SUB) {
+        float ref[4], part[4], top = m;
+        f32x4 x[4];
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            const int64_t place = place0 + (i0 + W * q < info.y ? i0 + W * q : i0);
-            const float *const at = p.parts + (place * ROWS + in_tile) * D + E * lane;
-            ref[q] = p.stats[place * 2 * ROWS + in_tile];
-            part[q] = p.stats[place * 2 * ROWS + ROWS + in_tile];
-#pragma unroll
-            for (int e = 0; e < E; ++e) x[q][e] = at[e];
+            const int i = i0 + W * SUB * q < info.y ? i0 + W * SUB * q : i0;
+            ref[q] = stats[(int64_t)i * 2 * ROWS];
+            part[q] = stats[(int64_t)i * 2 * ROWS + ROWS];
+            x[q] = *reinterpret_cast<const f32x4 *>(parts + (int64_t)i * ROWS * D);
         }
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            if (i0 + W * q >= info.y) ref[q] = NEG_INF;
+            if (i0 + W * SUB * q >= info.y) ref[q] = NEG_INF;
             top = fmaxf(top, ref[q]);
         }
         const float old = m != NEG_INF ? fast_exp2(m - top) : 0.f;
         sum *= old;
 #pragma unroll
-        for (int e = 0; e < E; ++e) acc[e] *= old;
+        for (int e = 0; e < 4; ++e) acc[e] *= old;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const float share = ref[q] != NEG_INF ? fast_exp2(ref[q] - top) : 0.f;
-            sum = ref[q] != NEG_INF ? fmaf(share, part[q], sum) : sum;
+        for (int q = 0; q < 4; ++q)
+            if (ref[q] != NEG_INF) {
+                const float share = fast_exp2(ref[q] - top);
+                sum = fmaf(share, part[q], sum);
 #pragma unroll
-            for (int e = 0; e < E; ++e) acc[e] = ref[q] != NEG_INF ? fmaf(share, x[q][e], acc[e]) : acc[e];
-        }
+                for (int e = 0; e < 4; ++e) acc[e] = fmaf(share, x[q][e], acc[e]);
+            }
+        m = top;
+    }
+    // lanes with the same columns, in the order of a tree
+#pragma unroll
+    for (int far = CL; far < 64; far *= 2) {
+        const float mu = __shfl_xor(m, far), top = fmaxf(m, mu), mine = m != NEG_INF ? fast_exp2(m - top) : 0.f, his = mu != NEG_INF ? fast_exp2(mu - top) : 0.f;
+        sum = mine * sum + his * __shfl_xor(sum, far);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e] = mine * acc[e] + his * __shfl_xor(acc[e], far);
         m = top;
     }
     uint16_t *const to = p.O + b * p.os.b + (hk * p.G + g) * p.os.h + t * p.os.s;
-    if constexpr (W == 1) {
-        const float inv = sum != 0.f ? 1.0f / sum : 0.f;
-        if (E * lane < p.d) {
-            if constexpr (E == 2) *reinterpret_cast<uint32_t *>(to + 2 * lane) = pack2<BF16>(acc[0] * inv, acc[1] * inv);
-            else to[lane] = (uint16_t)pack2<BF16>(acc[0] * inv, 0.f);
-        }
-    } else {
+    if constexpr (W == 4) {
         if (lane == 0) {
-            lds_ml[0][v] = m;
-            lds_ml[1][v] = sum;
+            lds_ml[0][w] = m;
+            lds_ml[1][w] = sum;
         }
-#pragma unroll
-        for (int e = 0; e < E; ++e) lds_o[v][E * lane + e] = acc[e];
+        if (lane < CL) *reinterpret_cast<f32x4 *>(&lds_o[w][4 * cl]) = acc;
         __syncthreads();
+        if (w) return;
         const float top = fmaxf(fmaxf(lds_ml[0][0], lds_ml[0][1]), fmaxf(lds_ml[0][2], lds_ml[0][3]));
-        float share[4], l = 0.f;
+        sum = 0.f;
+        acc = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            share[q] = lds_ml[0][q] != NEG_INF ? fast_exp2(lds_ml[0][q] - top) : 0.f;
-            l = fmaf(share[q], lds_ml[1][q], l);
+            const float share = lds_ml[0][q] != NEG_INF ? fast_exp2(lds_ml[0][q] - top) : 0.f;
+            const f32x4 y = *reinterpret_cast<const f32x4 *>(&lds_o[q][4 * cl]);
+            sum = fmaf(share, lds_ml[1][q], sum);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[e] = fmaf(share, y[e], acc[e]);
         }
-        const float inv = l != 0.f ? 1.0f / l : 0.f;
-        for (int col = threadIdx.x; col < p.d; col += 256)
-            to[col] = (uint16_t)pack2<BF16>((share[0] * lds_o[0][col] + share[1] * lds_o[1][col] + share[2] * lds_o[2][col] + share[3] * lds_o[3][col]) * inv, 0.f);
     }
+    const float inv = sum != 0.f ? 1.0f / sum : 0.f;
+    if (lane < CL && 4 * cl < p.d) store4<BF16 ? SMHA_BF16 : SMHA_F16>(to, 4 * cl, acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
 }
 
 // ---------------------------------------------------------------------------------------
@@ -916,7 +1016,7 @@ extern "C" smha_status_t smha_packed_read(const void *K, const void *V, void *K_
 
 // How a call is taken, and its workspace.
 struct PackedForm {
-    int rows, row_tiles, slots;  // rows of a tile: 16, 32 or 128; slots: 0 where a group is a segment
+    int rows, row_tiles, slots;  // rows of a tile: 16, 32, 64 or 128; slots: 0 where a group is a segment
     size_t stats, parts, total;  // after `info`
 };
 static size_t packed_up(size_t n) { return (n + 255) & ~(size_t)255; }
@@ -928,15 +1028,16 @@ static smha_status_t packed_form(PackedForm &f, int B, int H, int Hkv, int T, in
     if (H % Hkv) return SMHA_ERR_SHAPE;
     if ((int64_t)B * H > (1 << 24) || (int64_t)B * H * T > (1 << 24)) return SMHA_ERR_UNSUPPORTED;
     const int D = d <= 64 ? 64 : 128, rows = H / Hkv * T;
-    f.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : 128;
-    const int KT = f.rows == 128 ? 64 : 32;
+    f.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
+    const bool wide = f.rows >= 64;
+    const int KT = wide ? 64 : 32;
     f.row_tiles = (rows + f.rows - 1) / f.rows;
     const int64_t groups = (int64_t)B * Hkv * f.row_tiles;
     if (groups * (Sk / KT + 8) > (1 << 30)) return SMHA_ERR_UNSUPPORTED;  // (tiles are counted in 32 bits)
     const int64_t see = window == 0 || window > Sk ? Sk : window;
     const int64_t tiles = std::min<int64_t>((Sk + KT - 1) / KT, (see + std::min(n_sink, Sk) + T) / KT + 3);
-    const int slots = 256 * (f.rows == 128 ? (D == 64 ? 3 : 2) : packed_workgroups(D, f.rows / 16));
-    const bool direct = f.rows == 128 ? groups >= slots || tiles <= 8 : tiles <= 24;
+    const int slots = 256 * (wide ? (D == 64 ? 3 : 2) : packed_workgroups(D, f.rows / 16));
+    const bool direct = wide ? groups >= slots || tiles <= 8 : tiles <= 24;
     f.slots = direct ? 0 : slots;
     f.stats = f.parts = f.total = 0;
     if (direct) return SMHA_OK;
@@ -959,13 +1060,14 @@ extern "C" smha_status_t smha_packed_workspace(int B, int H, int Hkv, int T, int
 template <int D, bool BF16> static hipError_t launch_packed(const PackedParams &pp, const PackedForm &f, hipStream_t stream) {
     const int groups = pp.B * pp.Hkv * pp.row_tiles, segments = groups + pp.slots;
     const dim3 grid(8 * ((segments + 7) / 8));
-    auto *const part = f.rows == 16 ? smha_packed_part<D, 1, BF16> : f.rows == 32 ? smha_packed_part<D, 2, BF16> : smha_packed_wide<D, BF16>;
+    auto *const part = f.rows == 16 ? smha_packed_part<D, 1, BF16> : f.rows == 32 ? smha_packed_part<D, 2, BF16> : f.rows == 64 ? smha_packed_wide<D, 2, BF16> : smha_packed_wide<D, 1, BF16>;
     hipLaunchKernelGGL(part, grid, dim3(256), 0, stream, pp);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || !pp.slots) return e;
     const int rows = pp.B * pp.H * pp.T;
     if (f.rows == 128 && rows > 4096) hipLaunchKernelGGL((smha_packed_join<D, 128, 1, BF16>), dim3((rows + 3) / 4), dim3(256), 0, stream, pp);
     else if (f.rows == 128) hipLaunchKernelGGL((smha_packed_join<D, 128, 4, BF16>), dim3(rows), dim3(256), 0, stream, pp);
+    else if (f.rows == 64) hipLaunchKernelGGL((smha_packed_join<D, 64, 4, BF16>), dim3(rows), dim3(256), 0, stream, pp);
     else if (f.rows == 32) hipLaunchKernelGGL((smha_packed_join<D, 32, 4, BF16>), dim3(rows), dim3(256), 0, stream, pp);
     else hipLaunchKernelGGL((smha_packed_join<D, 16, 4, BF16>), dim3(rows), dim3(256), 0, stream, pp);
     return hipGetLastError();

@@ -106,7 +106,8 @@ PyObject *forward(PyObject *, PyObject *const *args, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
-// ---- attention with sinks, attention on a cache, eviction (sink.py and cache.py: the same calls, and the errors of those that are refused here)
+// ---- attention with sinks, attention on a cache, eviction, a cache held in 4 bits (sink.py, cache.py and packed.py: the same calls, and the errors of those that
+// are refused here)
 
 struct Entries {
     decltype(&smha_sink_forward) sink_forward;
@@ -116,21 +117,28 @@ struct Entries {
     decltype(&smha_cache_workspace) cache_workspace;
     decltype(&smha_cache_evict) cache_evict;
     decltype(&smha_cache_evict_workspace) cache_evict_workspace;
+    decltype(&smha_packed_write) packed_write;
+    decltype(&smha_packed_read) packed_read;
+    decltype(&smha_packed_forward) packed_forward;
+    decltype(&smha_packed_workspace) packed_workspace;
 } entries;
+constexpr int kEntries = 11;
 
 // link(the addresses of those, in that order)
 PyObject *link(PyObject *, PyObject *const *args, Py_ssize_t n) {
-    void *at[7];
-    if (n != 7) {
-        PyErr_SetString(PyExc_TypeError, "seven addresses");
+    void *at[kEntries];
+    if (n != kEntries) {
+        PyErr_SetString(PyExc_TypeError, "eleven addresses");
         return nullptr;
     }
-    for (int i = 0; i < 7; ++i) at[i] = PyLong_AsVoidPtr(args[i]);
+    for (int i = 0; i < kEntries; ++i) at[i] = PyLong_AsVoidPtr(args[i]);
     if (PyErr_Occurred()) return nullptr;
     entries = {reinterpret_cast<decltype(entries.sink_forward)>(at[0]), reinterpret_cast<decltype(entries.sink_backward)>(at[1]),
                reinterpret_cast<decltype(entries.sink_workspace)>(at[2]), reinterpret_cast<decltype(entries.cache_forward)>(at[3]),
                reinterpret_cast<decltype(entries.cache_workspace)>(at[4]), reinterpret_cast<decltype(entries.cache_evict)>(at[5]),
-               reinterpret_cast<decltype(entries.cache_evict_workspace)>(at[6])};
+               reinterpret_cast<decltype(entries.cache_evict_workspace)>(at[6]), reinterpret_cast<decltype(entries.packed_write)>(at[7]),
+               reinterpret_cast<decltype(entries.packed_read)>(at[8]), reinterpret_cast<decltype(entries.packed_forward)>(at[9]),
+               reinterpret_cast<decltype(entries.packed_workspace)>(at[10])};
     Py_RETURN_NONE;
 }
 
@@ -432,11 +440,128 @@ PyObject *cache_evict(PyObject *, PyObject *const *args, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
+// A packed cache: uint8 [B,Hkv,Sk,row], keys and values alike.  The columns of its rows, or 0.
+int packed_width(const at::Tensor &k, const at::Tensor &v) {
+    if (k.scalar_type() != at::kByte || v.scalar_type() != at::kByte || k.sizes() != v.sizes() || v.device() != k.device() || !small_sizes(k)) return 0;
+    const int64_t row = k.size(3);
+    for (int d = 8; d <= 128; d += 8)
+        if (4 * ((d + 31) / 32) + d / 2 == row) return d;
+    return 0;
+}
+
+// Rows that are written must not overlap (the entry point looks at all strides together).
+bool steps_over_rows(const at::Tensor &t) {
+    for (int i = 0; i < 3; ++i)
+        if (t.size(i) > 1 && t.stride(i) < t.size(3)) return false;
+    return true;
+}
+
+PyObject *pair_of(at::Tensor &&a, at::Tensor &&b) {
+    PyObject *out = PyTuple_New(2);
+    if (!out) return nullptr;
+    PyTuple_SET_ITEM(out, 0, THPVariable_Wrap(std::move(a)));
+    PyTuple_SET_ITEM(out, 1, THPVariable_Wrap(std::move(b)));
+    return out;
+}
+
+// packed_write(new keys, new values, k, v, lengths, offsets or None, values) -> True, (keys, values), a status, or None
+PyObject *packed_write(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (n != 7 || !entries.packed_write || at::impl::torch_function_mode_enabled() || c10::impl::TorchDispatchModeTLS::any_modes_set()) Py_RETURN_NONE;
+    if (!plain(args[0]) || !plain(args[1]) || !plain(args[2]) || !plain(args[3]) || !PyBool_Check(args[6])) Py_RETURN_NONE;
+    const at::Tensor &kn = THPVariable_Unpack(args[0]), &vn = THPVariable_Unpack(args[1]), &k = THPVariable_Unpack(args[2]), &v = THPVariable_Unpack(args[3]);
+    const int d = packed_width(k, v), type = code_of(kn.scalar_type());
+    if (!d || (type != SMHA_F16 && type != SMHA_BF16) || vn.scalar_type() != kn.scalar_type() || kn.sizes() != vn.sizes() || kn.device() != k.device() || vn.device() != k.device() ||
+        kn.size(0) != k.size(0) || kn.size(1) != k.size(1) || kn.size(3) != d || !small_sizes(kn) || wants_derivative(kn) || wants_derivative(vn) || !steps_over_rows(k) || !steps_over_rows(v))
+        Py_RETURN_NONE;
+    const int32_t *lengths, *offsets;
+    at::Tensor lengths_t, offsets_t;
+    if (args[4] == Py_None || !per_sequence(args[4], k, lengths, lengths_t) || !per_sequence(args[5], k, offsets, offsets_t)) Py_RETURN_NONE;
+    const Strides3 ns(kn), ms(vn), ks(k), vs(v);
+    if (!ns.ok || !ms.ok || !ks.ok || !vs.ok) Py_RETURN_NONE;
+    const c10::DeviceGuard guard(k.device());
+    const at::AutoGradMode off(false);
+    at::Tensor keys, values;
+    if (args[6] == Py_True) {
+        keys = packed_like(kn);
+        values = packed_like(vn);
+    }
+    const smha_status_t st = entries.packed_write(kn.data_ptr(), vn.data_ptr(), k.data_ptr(), v.data_ptr(), keys.defined() ? keys.data_ptr() : nullptr,
+                                                  values.defined() ? values.data_ptr() : nullptr, lengths, offsets, (int)k.size(0), (int)k.size(1), (int)kn.size(2), (int)k.size(2), d,
+                                                  (smha_dtype_t)type, ns.ptr, ms.ptr, ks.ptr, vs.ptr, c10::hip::getCurrentHIPStream(k.device().index()).stream());
+    if (st != SMHA_OK) return PyLong_FromLong((long)st);
+    written(k);
+    written(v);
+    if (!keys.defined()) Py_RETURN_TRUE;
+    return pair_of(std::move(keys), std::move(values));
+    END_HANDLE_TH_ERRORS
+}
+
+// packed_read(k, v, lengths, offsets or None, tokens or None, dtype) -> (keys, values), a status, or None
+PyObject *packed_read(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (n != 6 || !entries.packed_read || at::impl::torch_function_mode_enabled() || c10::impl::TorchDispatchModeTLS::any_modes_set()) Py_RETURN_NONE;
+    if (!plain(args[0]) || !plain(args[1]) || !THPDtype_Check(args[5])) Py_RETURN_NONE;
+    const at::Tensor &k = THPVariable_Unpack(args[0]), &v = THPVariable_Unpack(args[1]);
+    const at::ScalarType out_type = reinterpret_cast<THPDtype *>(args[5])->scalar_type;
+    const int d = packed_width(k, v), type = code_of(out_type);
+    if (!d || type < 0) Py_RETURN_NONE;
+    const int32_t *lengths, *offsets;
+    at::Tensor lengths_t, offsets_t;
+    if (args[2] == Py_None || !per_sequence(args[2], k, lengths, lengths_t) || !per_sequence(args[3], k, offsets, offsets_t)) Py_RETURN_NONE;
+    int tokens = (int)k.size(2);
+    if (args[4] != Py_None && !int_from(args[4], tokens)) Py_RETURN_NONE;
+    const Strides3 ks(k), vs(v);
+    if (!ks.ok || !vs.ok) Py_RETURN_NONE;
+    const c10::DeviceGuard guard(k.device());
+    const at::AutoGradMode off(false);
+    const int64_t shape[4] = {k.size(0), k.size(1), tokens, d};
+    at::Tensor keys = at::empty(shape, k.options().dtype(out_type)), values = at::empty(shape, k.options().dtype(out_type));
+    const smha_status_t st = entries.packed_read(k.data_ptr(), v.data_ptr(), keys.data_ptr(), values.data_ptr(), lengths, offsets, (int)k.size(0), (int)k.size(1), tokens, (int)k.size(2), d,
+                                                 (smha_dtype_t)type, ks.ptr, vs.ptr, nullptr, nullptr, c10::hip::getCurrentHIPStream(k.device().index()).stream());
+    if (st != SMHA_OK) return PyLong_FromLong((long)st);
+    return pair_of(std::move(keys), std::move(values));
+    END_HANDLE_TH_ERRORS
+}
+
+// packed_attention(q, k, v, lengths, window, n_sink, scale) -> the output, a status, or None
+PyObject *packed_attention(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (n != 7 || !entries.packed_forward || at::impl::torch_function_mode_enabled() || c10::impl::TorchDispatchModeTLS::any_modes_set()) Py_RETURN_NONE;
+    if (!plain(args[0]) || !plain(args[1]) || !plain(args[2]) || !PyFloat_CheckExact(args[6])) Py_RETURN_NONE;
+    const at::Tensor &q = THPVariable_Unpack(args[0]), &k = THPVariable_Unpack(args[1]), &v = THPVariable_Unpack(args[2]);
+    const int d = packed_width(k, v), type = code_of(q.scalar_type());
+    if (!d || (type != SMHA_F16 && type != SMHA_BF16) || q.size(0) != k.size(0) || q.size(3) != d || k.size(1) < 1 || q.size(1) % k.size(1) || q.device() != k.device() || !small_sizes(q) ||
+        wants_derivative(q))
+        Py_RETURN_NONE;
+    const int32_t *lengths;
+    at::Tensor lengths_t;
+    int window, n_sink;
+    if (args[3] == Py_None || !per_sequence(args[3], q, lengths, lengths_t) || !int_from(args[4], window) || !int_from(args[5], n_sink)) Py_RETURN_NONE;
+    const Strides3 qs(q), ks(k), vs(v);
+    if (!qs.ok || !ks.ok || !vs.ok) Py_RETURN_NONE;
+    const int B = (int)q.size(0), H = (int)q.size(1), T = (int)q.size(2), Hkv = (int)k.size(1), Sk = (int)k.size(2);
+    const c10::DeviceGuard guard(q.device());
+    size_t need = 0;
+    smha_status_t st = entries.packed_workspace(B, H, Hkv, T, Sk, d, window, n_sink, &need);
+    if (st != SMHA_OK) return PyLong_FromLong((long)st);
+    const at::AutoGradMode off(false);
+    at::Tensor o = packed_like(q);
+    const c10::DataPtr ws = need ? scratch(need) : c10::DataPtr();
+    st = entries.packed_forward(q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lengths, B, H, Hkv, T, Sk, d, (smha_dtype_t)type, qs.ptr, ks.ptr, vs.ptr, nullptr, window, n_sink,
+                                (float)PyFloat_AS_DOUBLE(args[6]), ws.get(), need, c10::hip::getCurrentHIPStream(q.device().index()).stream());
+    if (st != SMHA_OK) return PyLong_FromLong((long)st);
+    return THPVariable_Wrap(std::move(o));
+    END_HANDLE_TH_ERRORS
+}
+
 using Fast = PyObject *(*)(PyObject *, PyObject *const *, Py_ssize_t);
 PyCFunction fast(Fast f) { return reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)); }
 
 PyMethodDef methods[] = {{"link", fast(link), METH_FASTCALL, nullptr}, {"sink_attention", fast(sink_attention), METH_FASTCALL, nullptr},
                          {"cache_attention", fast(cache_attention), METH_FASTCALL, nullptr}, {"cache_evict", fast(cache_evict), METH_FASTCALL, nullptr},
+                         {"packed_write", fast(packed_write), METH_FASTCALL, nullptr}, {"packed_read", fast(packed_read), METH_FASTCALL, nullptr},
+                         {"packed_attention", fast(packed_attention), METH_FASTCALL, nullptr},
                          {"forward", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(forward)), METH_FASTCALL, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_smha_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -8,11 +8,12 @@ import ctypes as C
 
 import torch
 
-from .binding import SMHA_F32, SmhaError, _load
+from .binding import SMHA_F32, SmhaError, _load, native_call
 from .cache import _allocating_on, _check_no_gradients, _check_workspace
 from .sink import _CODES, _check_int, _check_per_sequence, _handle, _on_device, _strides, _written
 
 _READ_CODES = {**_CODES, torch.float32: SMHA_F32}
+_write = _read = _attention = None  # functions of _smha_torch
 
 
 def smha_packed_row(d: int) -> int:
@@ -61,6 +62,15 @@ def packed_write(k_new, v_new, k, v, lengths, *, offsets=None, values: bool = Fa
     token is left out.  values: return (keys, values) like k_new and v_new as the cache stands for them from now on (tokens that are left out: zeros), for attention of
     the prompt itself on what later tokens will see; otherwise None.  Values beyond +-65280 are packed as +-65280, 32 columns among which there
     is a NaN as NaN.  No gradients."""
+    if stream is None:  # the native way, for every call that it takes (csrc/torch_binding.cpp)
+        global _write
+        if _write is None:
+            _write = native_call("packed_write")
+        got = _write(k_new, v_new, k, v, lengths, offsets, values)
+        if got is not None:
+            if type(got) is int:
+                raise SmhaError(got, "smha_packed_write")
+            return None if got is True else got
     d = _width(k, v)
     if k_new.dim() != 4 or k_new.shape != v_new.shape or k_new.shape[:2] != k.shape[:2] or k_new.shape[3] != d:
         raise ValueError("k_new, v_new must be [B,Hkv,T,d], and the cache [B,Hkv,Sk,smha_packed_row(d)]")
@@ -88,6 +98,15 @@ def packed_read(k, v, lengths, *, offsets=None, tokens=None, dtype=torch.float16
     """What `tokens` slots of every sequence (default: all) from slot offsets[b] (default: 0) on stand for: (keys, values), each [B,Hkv,tokens,d] of
     `dtype`, float16, float32 (the same values) or bfloat16 (rounded to it); zeros where a slot is not in 0 .. lengths[b] - 1.  k, v, lengths, offsets as in packed_write.
     out: the two tensors to write to, by default new ones."""
+    if out is None and stream is None:
+        global _read
+        if _read is None:
+            _read = native_call("packed_read")
+        got = _read(k, v, lengths, offsets, tokens, dtype)
+        if got is not None:
+            if type(got) is int:
+                raise SmhaError(got, "smha_packed_read")
+            return got
     d = _width(k, v)
     if lengths is None:
         raise ValueError("lengths must be given")
@@ -128,6 +147,15 @@ def packed_attention(q, k, v, lengths, *, window: int = 0, n_sink: int = 0, out=
     of Hkv; T from one token to a chunk of a prompt.  lengths, window, n_sink, scale, out, workspace (of smha_packed_workspace bytes) as in cache_attention: token t of sequence b
     stands at slot lengths[b] - T + t and sees the keys up to itself, the last `window` of them (0: all) and the first `n_sink`.  No gradients.  Keys that a token of
     the sequence sees have to stand for something finite (others, and free slots, may hold anything)."""
+    if out is None and workspace is None and stream is None:
+        global _attention
+        if _attention is None:
+            _attention = native_call("packed_attention")
+        got = _attention(q, k, v, lengths, window, n_sink, float(scale))
+        if got is not None:
+            if type(got) is int:
+                raise SmhaError(got, "smha_packed_forward")
+            return got
     d = _width(k, v)
     if q.dim() != 4 or q.shape[0] != k.shape[0] or q.shape[3] != d:
         raise ValueError("q must be [B,H,T,d], and the cache [B,Hkv,Sk,smha_packed_row(d)]")
