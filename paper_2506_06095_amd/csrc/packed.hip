@@ -324,30 +324,28 @@ template <int KT, int ROWS, int TURN> __device__ __forceinline__ PackedSegment p
         }
         return e;
     };
-    const Entry first64 = entry(lane);
-    int sum = first64.n;
-    for (int i = 64; i < E; i += 64) sum += entry(i + lane).n;
-    const int total = p.Hkv * lanes_sum(sum);
     auto parts_of = [&](int i, int n, int most) __attribute__((always_inline)) { return i < E ? max(1, quotient(n + most - 1, most)) : 0; };
-    auto segments = [&](int most) __attribute__((always_inline)) {
-        int sum = parts_of(lane, first64.n, most);
-        for (int i = 64; i < E; i += 64) sum += parts_of(i + lane, entry(i + lane).n, most);
-        return p.Hkv * lanes_sum(sum);
-    };
-    auto at_most = [&](int segments) __attribute__((always_inline)) { return max(4, (quotient(total + segments - 1, segments) + TURN - 1) / TURN * TURN); };
-    int most = at_most(p.slots), n = segments(most);
-    if (n > p.slots) {
-        const int over = n - quotient(total, most);
-        if (2 * over < p.slots) {
-            most = at_most(p.slots - over);
-            n = segments(most);
-        }
+    const Entry first64 = entry(lane);  // (most calls have no more)
+    int sum = first64.n;
+    if (__builtin_expect(E > 64, 0))
+        for (int i = 64; i < E; i += 64) sum += entry(i + lane).n;
+    const int total = p.Hkv * lanes_sum(sum);
+    int most = 0, n = 0;
+    for (int wanted = p.slots;;) {
+        most = max(4, (quotient(total + wanted - 1, wanted) + TURN - 1) / TURN * TURN);
+        sum = parts_of(lane, first64.n, most);
+        if (__builtin_expect(E > 64, 0))
+            for (int i = 64; i < E; i += 64) sum += parts_of(i + lane, entry(i + lane).n, most);
+        n = p.Hkv * lanes_sum(sum);
+        if (wanted < p.slots || n <= p.slots) break;
+        wanted -= n - quotient(total, most);  // what is over
+        if (2 * wanted <= p.slots) break;
     }
     const int run = (n + 7) / 8;
     int at = xcd * run + slot, place = 0;
     if (slot >= run || at >= n) return s;
-    for (int i0 = 0; i0 < E; i0 += 64) {
-        const Entry e = i0 == 0 ? first64 : entry(i0 + lane);
+    Entry e = first64;
+    for (int i0 = 0;;) {
         const int parts = parts_of(i0 + lane, e.n, most), mine = p.Hkv * parts, upto = lanes_scan(mine), cut = parts > 1 ? mine : 0, cut_upto = lanes_scan(cut);
         const uint64_t past = __builtin_amdgcn_ballot_w64(upto > at);
         if (past) {
@@ -365,8 +363,10 @@ template <int KT, int ROWS, int TURN> __device__ __forceinline__ PackedSegment p
         }
         at -= __builtin_amdgcn_readlane(upto, 63);
         place += __builtin_amdgcn_readlane(cut_upto, 63);
+        i0 += 64;
+        if (i0 >= E) return s;  // (not reached: the segments counted are those found)
+        e = entry(i0 + lane);
     }
-    return s;  // (not reached: the segments counted are those found)
 }
 
 // The reference that a row's segment leaves: -inf says that it has no keys.  (A row of NaN has no largest score either, and must not be passed over.)
@@ -377,34 +377,33 @@ __device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c) {
 }
 
 // A row of queries as the B operand of the scores' product, in binary16: a lane holds N chunks of 8 columns, chunk i from column `col(i)` on, and the row's other
-// columns are in lanes 16 (STEPS16: and 32) apart.  bfloat16 rows are brought to 2^14 .. 2^15 by a power of two, by which they fit binary16 without
-// loss (but for columns below 2^-31 of the largest, which lose digits); returns what the scores have to be multiplied by.
+// columns are in lanes 16 (STEPS16: and 32) apart.  A row that does not exist and columns that the head does not have are zeros (something that exists is
+// read in their place: loads without branches travel together).  bfloat16 rows are brought to 2^14 .. 2^15 by a power of two, by which they fit binary16
+// without loss (but for columns below 2^-31 of the largest, which lose digits); returns what the scores have to be multiplied by.
 template <int N, bool BF16, bool STEPS16, typename Col>
-__device__ __forceinline__ float load_query(u32x4 (&qf)[N], const uint16_t *row, bool exists, int d, Col col) {
-    u32x4 raw[N];
+__device__ __forceinline__ float load_query(u32x4 (&qf)[N], const uint16_t *row, bool exists, const uint16_t *other, int d, Col col) {
+    if (!exists) row = other;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        raw[i] = u32x4{0, 0, 0, 0};
-        if (exists && col(i) < d) raw[i] = *reinterpret_cast<const u32x4 *>(row + col(i));
-    }
+    for (int i = 0; i < N; ++i) qf[i] = *reinterpret_cast<const u32x4 *>(row + (col(i) < d ? col(i) : 0));
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        if (!exists || col(i) >= d) qf[i] = u32x4{0, 0, 0, 0};
     if constexpr (!BF16) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) qf[i] = raw[i];
         return 1.f;
     } else {
         float top = 0.f;
 #pragma unroll
         for (int i = 0; i < N; ++i)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) top = fmaxf(top, fmaxf(fabsf(widen16<true>(raw[i][e] & 0xFFFFu)), fabsf(widen16<true>(raw[i][e] >> 16))));
+            for (int e = 0; e < 4; ++e) top = fmaxf(top, fmaxf(fabsf(widen16<true>(qf[i][e] & 0xFFFFu)), fabsf(widen16<true>(qf[i][e] >> 16))));
         if (STEPS16) top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, __shfl_xor(top, 32));
         const int e2 = min(15 - __builtin_amdgcn_frexp_expf(top), 100);
+        const float power = __builtin_amdgcn_ldexpf(1.f, e2);
 #pragma unroll
         for (int i = 0; i < N; ++i)
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                qf[i][e] = pack2<false>(__builtin_amdgcn_ldexpf(widen16<true>(raw[i][e] & 0xFFFFu), e2), __builtin_amdgcn_ldexpf(widen16<true>(raw[i][e] >> 16), e2));
+            for (int e = 0; e < 4; ++e) qf[i][e] = pack2<false>(widen16<true>(qf[i][e] & 0xFFFFu) * power, __builtin_bit_cast(float, qf[i][e] & 0xFFFF0000u) * power);
         return __builtin_amdgcn_ldexpf(1.f, -e2);
     }
 }
@@ -479,18 +478,21 @@ __global__ void __launch_bounds__(256, packed_workgroups(D, NR)) smha_packed_par
     s.share(keys.n, begin, end);
     begin += w;
     const int vj = mixed<D>(j);  // the key of a value that this lane unpacks
-    struct Raw {
-        typename PackedLoad<D>::Raw k[2], v[2];
-    } raw[2];
-    auto request = [&](Raw &x, int tile) __attribute__((always_inline)) {
-        const int key = keys.key(tile);
+    typename PackedLoad<D>::Raw k_raw[2], v_raw[2];  // refilled as soon as they are unpacked
+    auto request_k = [&](int tile) __attribute__((always_inline)) {
+        const int key = keys.key(tile) + j;
 #pragma unroll
-        for (int a = 0; a < 2; ++a) x.k[a] = loadK(key + j + 16 * a);
-#pragma unroll
-        for (int a = 0; a < 2; ++a) x.v[a] = loadV(key + vj + 16 * a);
+        for (int a = 0; a < 2; ++a) k_raw[a] = loadK(key + 16 * a);
     };
-    if (begin < end) request(raw[0], begin);
-    if (begin + 4 < end) request(raw[1], begin + 4);
+    auto request_v = [&](int tile) __attribute__((always_inline)) {
+        const int key = keys.key(tile) + vj;
+#pragma unroll
+        for (int a = 0; a < 2; ++a) v_raw[a] = loadV(key + 16 * a);
+    };
+    if (begin < end) {
+        request_k(begin);
+        request_v(begin);
+    }
 
     u32x4 qf[NR][NS];
     int pos[NR];  // below 0: no such query
@@ -502,7 +504,8 @@ __global__ void __launch_bounds__(256, packed_workgroups(D, NR)) smha_packed_par
         pos[x] = row < rows ? keys.len - p.T + t : -1;
         to[x] = row < rows ? p.O + s.b * p.os.b + h * p.os.h + t * p.os.s : nullptr;
         // (never 0: -inf times it)
-        c[x] = fmaxf(p.c * load_query<NS, BF16, true>(qf[x], p.Q + s.b * p.qs.b + h * p.qs.h + t * p.qs.s, pos[x] >= 0, p.d, [&](int i) { return D / 4 * u + 8 * i; }), 0x1p-126f);
+        const uint16_t *const q0 = p.Q + s.b * p.qs.b + s.hk * p.G * p.qs.h;
+        c[x] = fmaxf(p.c * load_query<NS, BF16, true>(qf[x], q0 + g * p.qs.h + t * p.qs.s, pos[x] >= 0, q0, p.d, [&](int i) { return D / 4 * u + 8 * i; }), 0x1p-126f);
         thr[x] = raised_over(c[x]);
     }
     float m_run[NR], l_run[NR];
@@ -515,7 +518,7 @@ __global__ void __launch_bounds__(256, packed_workgroups(D, NR)) smha_packed_par
         for (int ct = 0; ct < NC; ++ct) o[x][ct] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
     const int tr_row = 4 * u + (j >> 2);
-    auto step = [&](int tile, Raw &now) __attribute__((always_inline)) {
+    for (int tile = begin; tile < end; tile += 4) {
         const int key = keys.key(tile);
         // acc[x][a][r]: the score of query j and key 16 a + 4 u + r
         f32x4 acc[NR][2];
@@ -525,17 +528,18 @@ __global__ void __launch_bounds__(256, packed_workgroups(D, NR)) smha_packed_par
         for (int i = 0; i < NS; ++i)
 #pragma unroll
             for (int a = 0; a < 2; ++a) {
-                const u32x4 kf = unpack8(now.k[a].code[i], now.k[a].head);
+                const u32x4 kf = unpack8(k_raw[a].code[i], k_raw[a].head);
 #pragma unroll
                 for (int x = 0; x < NR; ++x) acc[x][a] = mfma16(kf, qf[x][i], acc[x][a]);
             }
+        if (tile + 4 < end) request_k(tile + 4);
         // values go to LDS under that product
 #pragma unroll
         for (int a = 0; a < 2; ++a)
 #pragma unroll
             for (int i = 0; i < NS; ++i)
-                *reinterpret_cast<u32x4 *>(smem + (16 * a + vj) * D * 2 + (((D / 32 * u + i) ^ swz_values<D>(vj)) * 16)) = unpack8(now.v[a].code[i], now.v[a].head);
-        if (tile + 8 < end) request(now, tile + 8);
+                *reinterpret_cast<u32x4 *>(smem + (16 * a + vj) * D * 2 + (((D / 32 * u + i) ^ swz_values<D>(vj)) * 16)) = unpack8(v_raw[a].code[i], v_raw[a].head);
+        if (tile + 4 < end) request_v(tile + 4);
         u32x4 pf[NR];
 #pragma unroll
         for (int x = 0; x < NR; ++x) {
@@ -578,10 +582,6 @@ __global__ void __launch_bounds__(256, packed_workgroups(D, NR)) smha_packed_par
             for (int x = 0; x < NR; ++x) o[x][ct] = mfma16(u32x4{lo[0], lo[1], hi[0], hi[1]}, pf[x], o[x][ct]);
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the tile is read
-    };
-    for (int tile = begin; tile < end; tile += 8) {
-        step(tile, raw[0]);
-        if (tile + 4 < end) step(tile + 4, raw[1]);
     }
 
     // The team joins: every wave leaves its accumulators in its own tile's place and takes a quarter of the columns of all four.
@@ -639,13 +639,12 @@ __global__ void __launch_bounds__(256, packed_workgroups(D, NR)) smha_packed_par
 }
 
 // Many rows on the same keys: four waves share tiles of 64 keys, which all of them unpack into LDS, the next one under this one's first product, from words that were
-// requested two tiles before.  KH = 1: a wave takes 32 of 128 rows; KH = 2: a wave takes 32 of 64 rows and one half of the keys, and the halves are joined at the end.  From
+// requested a tile before.  KH = 1: a wave takes 32 of 128 rows; KH = 2: a wave takes 32 of 64 rows and one half of the keys, and the halves are joined at the end.  From
 // LDS on it is as in smha_sink_fwd, in binary16 throughout.
 template <int D, int KH, bool BF16>
 __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) smha_packed_wide(const PackedParams p) {
     constexpr int NS = D / 16, NDT = D / 32, NL = D / 32, TB = 64 * D * 2, ROWS = 128 / KH, KTS = 2 / KH;  // KTS: halves of a tile that a wave takes
     constexpr int PF = KH == 1 && D == 128 ? 8 : 4;  // operands requested ahead
-    constexpr int AHEAD = KH;  // tiles whose words are on their way
     __shared__ __attribute__((aligned(1024))) char smem[4 * TB];  // K[0], K[1], V[0], V[1]
     __shared__ float team[2][2][32];
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = lane & 31, hh = lane >> 5;
@@ -663,21 +662,21 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) smha_packed_wide(const P
     const int kj = 16 * w + mixed<D, true>(lane & 15);
     struct Raw {
         typename PackedLoad<D>::Raw k, v;
-    } raw[AHEAD];
+    } raw;
     auto request = [&](Raw &x, int tile) __attribute__((always_inline)) {
         const int key = keys.key(tile) + kj;
         x.k = loadK(key);
         x.v = loadV(key);
     };
-    if (begin < end) request(raw[0], begin);
-    if (AHEAD == 2 && begin + 1 < end) request(raw[AHEAD - 1], begin + 1);
+    if (begin < end) request(raw, begin);
 
     const int row0 = s.rows0 + 32 * wr, row = row0 + j, t = quotient(row, p.G), g = row - t * p.G, h = s.hk * p.G + g;
     const int pos = row < rows ? keys.len - p.T + t : -1;  // below 0: no such query
     const int wp0 = keys.len - p.T + quotient(row0, p.G), wp1 = row0 < rows ? keys.len - p.T + quotient(min(row0 + 32, rows) - 1, p.G) : -1;  // the wave's positions
     const bool every = wp0 >= 0 && row0 + 32 <= rows;
     u32x4 qf[NS];
-    const float c = fmaxf(p.c * load_query<NS, BF16, false>(qf, p.Q + s.b * p.qs.b + h * p.qs.h + t * p.qs.s, pos >= 0, p.d, [&](int i) { return 16 * i + 8 * hh; }), 0x1p-126f);
+    const uint16_t *const q0 = p.Q + s.b * p.qs.b + s.hk * p.G * p.qs.h;
+    const float c = fmaxf(p.c * load_query<NS, BF16, false>(qf, q0 + g * p.qs.h + t * p.qs.s, pos >= 0, q0, p.d, [&](int i) { return 16 * i + 8 * hh; }), 0x1p-126f);
     const float thr = raised_over(c);
 
     // the i-th of 2 NL chunks of a tile, keys' first
@@ -689,9 +688,9 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) smha_packed_wide(const P
     };
     if (begin < end) {
 #pragma unroll
-        for (int i = 0; i < 2 * NL; ++i) leave(lv, 0, raw[0], i);
+        for (int i = 0; i < 2 * NL; ++i) leave(lv, 0, raw, i);
     }
-    if (begin + AHEAD < end) request(raw[0], begin + AHEAD);
+    if (begin + 1 < end) request(raw, begin + 1);
 
     const int rd = j * D * 2 + ((hh ^ swz_both<D>(j)) * 16);
     const int tr_row = 4 * hh + ((lane & 15) >> 2);
@@ -701,16 +700,14 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) smha_packed_wide(const P
 #pragma unroll
     for (int dt = 0; dt < NDT; ++dt) o[dt] = zeros16();
     __syncthreads();
-    auto step = [&](int tile, auto par_) __attribute__((always_inline)) {
-        const int par = par_;
-        Raw &next = raw[AHEAD == 2 ? par ^ 1 : 0];  // of tile + 1
-        const bool more = tile + 1 < end;
+    for (int tile = begin; tile < end; ++tile) {
+        const int par = (tile - begin) & 1;
         const int key = keys.key(tile), key_w = key + 32 * wk;
         constexpr int KW = 32 * KTS;
-        if (more) {
+        if (tile + 1 < end) {
 #pragma unroll
-            for (int i = 0; i < 2 * NL; ++i) leave(lv, par ^ 1, next, i);
-            if (tile + AHEAD + 1 < end) request(next, tile + AHEAD + 1);
+            for (int i = 0; i < 2 * NL; ++i) leave(lv, par ^ 1, raw, i);
+            if (tile + 2 < end) request(raw, tile + 2);
         }
         if (wp1 >= 0 && key_w <= wp1 && (wp0 - key_w - (KW - 1) < p.window || key_w < p.n_sink)) {  // some row of the wave sees some key
             const char *const Kt = smem + par * TB + 32 * wk * D * 2, *const Vt = smem + (2 + par) * TB + 32 * wk * D * 2;
@@ -780,16 +777,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) smha_packed_wide(const P
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-    };
-    if constexpr (AHEAD == 1) {
-        for (int tile = begin; tile < end; ++tile) step(tile, (tile - begin) & 1);
-    } else {  // (which words a step takes has to be known when it is compiled)
-        for (int tile = begin; tile < end; tile += 2) {
-            step(tile, std::integral_constant<int, 0>{});
-            if (tile + 1 < end) step(tile + 1, std::integral_constant<int, 1>{});
-        }
     }
-
     float l = l_run + __shfl_xor(l_run, 32), m = m_run * c;
     if constexpr (KH == 2) {  // the keys' halves join: the second leaves its accumulators where the tiles were
         f32x4 *const left = reinterpret_cast<f32x4 *>(smem + wr * (32 * D * 4));
@@ -1065,11 +1053,12 @@ template <int D, bool BF16> static hipError_t launch_packed(const PackedParams &
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || !pp.slots) return e;
     const int rows = pp.B * pp.H * pp.T;
-    if (f.rows == 128 && rows > 4096) hipLaunchKernelGGL((smha_packed_join<D, 128, 1, BF16>), dim3((rows + 3) / 4), dim3(256), 0, stream, pp);
-    else if (f.rows == 128) hipLaunchKernelGGL((smha_packed_join<D, 128, 4, BF16>), dim3(rows), dim3(256), 0, stream, pp);
-    else if (f.rows == 64) hipLaunchKernelGGL((smha_packed_join<D, 64, 4, BF16>), dim3(rows), dim3(256), 0, stream, pp);
-    else if (f.rows == 32) hipLaunchKernelGGL((smha_packed_join<D, 32, 4, BF16>), dim3(rows), dim3(256), 0, stream, pp);
-    else hipLaunchKernelGGL((smha_packed_join<D, 16, 4, BF16>), dim3(rows), dim3(256), 0, stream, pp);
+    const bool alone = rows > 2048;  // a wave a row
+    auto *const join = f.rows == 16   ? (alone ? smha_packed_join<D, 16, 1, BF16> : smha_packed_join<D, 16, 4, BF16>)
+                       : f.rows == 32 ? (alone ? smha_packed_join<D, 32, 1, BF16> : smha_packed_join<D, 32, 4, BF16>)
+                       : f.rows == 64 ? (alone ? smha_packed_join<D, 64, 1, BF16> : smha_packed_join<D, 64, 4, BF16>)
+                                      : (alone ? smha_packed_join<D, 128, 1, BF16> : smha_packed_join<D, 128, 4, BF16>);
+    hipLaunchKernelGGL(join, dim3(alone ? (rows + 3) / 4 : rows), dim3(256), 0, stream, pp);
     return hipGetLastError();
 }
 
