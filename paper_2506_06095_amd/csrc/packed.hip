@@ -1025,7 +1025,7 @@ static smha_status_t packed_form(PackedForm &f, int B, int H, int Hkv, int T, in
     const int64_t see = window == 0 || window > Sk ? Sk : window;
     const int64_t tiles = std::min<int64_t>((Sk + KT - 1) / KT, (see + std::min(n_sink, Sk) + T) / KT + 3);
     const int slots = 256 * (wide ? (D == 64 ? 3 : 2) : packed_workgroups(D, f.rows / 16));
-    const bool direct = wide ? groups >= slots || tiles <= 8 : tiles <= 24;
+    const bool direct = wide ? groups >= slots || tiles <= 8 : tiles <= std::min<int64_t>(48, (D == 64 ? 24 : 16) + groups / 8);
     f.slots = direct ? 0 : slots;
     f.stats = f.parts = f.total = 0;
     if (direct) return SMHA_OK;
@@ -1053,7 +1053,7 @@ template <int D, bool BF16> static hipError_t launch_packed(const PackedParams &
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || !pp.slots) return e;
     const int rows = pp.B * pp.H * pp.T;
-    const bool alone = rows > 2048;  // a wave a row
+    const bool alone = rows > 512;  // a wave a row (960 rows of 9 segments 16.2 us a call with four, 14.7 so; 64 of 47 segments 35.6 and 40.4)
     auto *const join = f.rows == 16   ? (alone ? smha_packed_join<D, 16, 1, BF16> : smha_packed_join<D, 16, 4, BF16>)
                        : f.rows == 32 ? (alone ? smha_packed_join<D, 32, 1, BF16> : smha_packed_join<D, 32, 4, BF16>)
                        : f.rows == 64 ? (alone ? smha_packed_join<D, 64, 1, BF16> : smha_packed_join<D, 64, 4, BF16>)
