@@ -50,6 +50,16 @@ __device__ __forceinline__ u32x4 unpack8(uint32_t word, uint32_t head) {
     return v;
 }
 
+// n / d for 0 <= n <= 2^30, 0 < d < 2^30: in 32-bit floats, again for what that leaves, and by one for what that does.  (Rows and segments are found by chains of
+// divisions; the compiler's take twice as many instructions.)
+__device__ __forceinline__ int quotient(int n, int d) {
+    const float inv = __builtin_amdgcn_rcpf((float)d);
+    int q = (int)((float)n * inv);
+    q += (int)((float)(n - q * d) * inv);
+    const int rest = n - q * d;
+    return q + (rest >= d ? 1 : 0) - (rest < 0 ? 1 : 0);
+}
+
 // Two binary16 values as a pair of bfloat16.
 __device__ __forceinline__ uint32_t as_bf16(uint32_t pair) {
     const f16x2 h = __builtin_bit_cast(f16x2, pair);
@@ -129,28 +139,44 @@ __device__ __forceinline__ uint32_t pack8(u32x4 x, bool there, uint32_t &head) {
     return word;
 }
 
-// A quad of lanes takes a group of a new token's key and of its value.  Memory bounds it: 2 d bytes in and R out for each.
+// Where a row of a call is: token t of key head hk of sequence b, and its slot.
+struct PackedRow {
+    int b, hk, t;
+    int64_t slot;
+    bool kept;
+    __device__ __forceinline__ PackedRow(int row, int T, int Hkv, int Sk, const int32_t *lengths, const int32_t *offsets, bool at_end) {
+        const int bh = quotient(row, T);
+        b = quotient(bh, Hkv);
+        t = row - bh * T;
+        hk = bh - b * Hkv;
+        const int len = min(max(lengths[b], 0), Sk);
+        slot = (offsets ? (int64_t)offsets[b] : at_end ? (int64_t)len - T : 0) + t;
+        kept = slot >= 0 && slot < len;
+    }
+};
+
+// A quad of lanes takes a group of a new token's key and of its value.  Memory bounds it: 2 d bytes in and R out for each, 2 d more with `values`.  4 x 8 x 8192 x 128
+// with values, of 70 to 100 % of that length: 280 MB, 59 us, 4.7 TB/s as in a large copy (65 with stores of values that stay in the caches; 63 and 66 where a
+// thread takes two and four tokens).
 template <int G, bool BF16>
 __global__ void __launch_bounds__(256) smha_packed_put(const PackParams p) {
-    const int64_t quad = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 2;
-    const int at = threadIdx.x & 3, row = (int)(quad / G), g = (int)(quad - (int64_t)row * G), col = 32 * g + 8 * at;
-    const int bh = row / p.T, t = row - bh * p.T, b = bh / p.Hkv, hk = bh - b * p.Hkv;
-    if (b >= p.B) return;
-    const int len = min(max(p.lengths[b], 0), p.Sk);
-    const int64_t slot = (p.offsets ? (int64_t)p.offsets[b] : (int64_t)len - p.T) + t;
-    const bool kept = slot >= 0 && slot < len, there = col < p.d;
+    constexpr int ROWS = 64 / G;  // of a workgroup (of three groups one quad has nothing to do)
+    const int quad = threadIdx.x >> 2, at = threadIdx.x & 3, first = quad / G, g = quad - first * G, col = 32 * g + 8 * at, row = (int)blockIdx.x * ROWS + first;
+    if (first >= ROWS || row >= p.B * p.Hkv * p.T) return;
+    const PackedRow to_row(row, p.T, p.Hkv, p.Sk, p.lengths, p.offsets, true);
+    const bool there = col < p.d;
     u32x4 x[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         x[i] = u32x4{0, 0, 0, 0};
-        if (kept && there) x[i] = *reinterpret_cast<const u32x4 *>(p.x[i] + b * p.xs[i].b + hk * p.xs[i].h + t * p.xs[i].s + col);
+        if (to_row.kept && there) x[i] = *reinterpret_cast<const u32x4 *>(p.x[i] + to_row.b * p.xs[i].b + to_row.hk * p.xs[i].h + to_row.t * p.xs[i].s + col);
     }
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         uint32_t head;
         const uint32_t word = pack8<BF16>(x[i], there, head);
-        if (kept) {
-            uint8_t *const to = p.cache[i] + b * p.cs[i].b + hk * p.cs[i].h + slot * p.cs[i].s;
+        if (to_row.kept) {
+            uint8_t *const to = p.cache[i] + to_row.b * p.cs[i].b + to_row.hk * p.cs[i].h + to_row.slot * p.cs[i].s;
             if (at == 0) *reinterpret_cast<uint32_t *>(to + 4 * g) = head;
             if (there) *reinterpret_cast<uint32_t *>(to + 4 * G + 16 * g + 4 * at) = word;
         }
@@ -159,8 +185,8 @@ __global__ void __launch_bounds__(256) smha_packed_put(const PackParams p) {
             if (BF16)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) v[e] = as_bf16(v[e]);
-            if (!kept) v = u32x4{0, 0, 0, 0};
-            *reinterpret_cast<u32x4 *>(p.values[i] + (int64_t)row * p.d + col) = v;
+            if (!to_row.kept) v = u32x4{0, 0, 0, 0};
+            __builtin_nontemporal_store(v, reinterpret_cast<u32x4 *>(p.values[i] + (int64_t)row * p.d + col));
         }
     }
 }
@@ -173,40 +199,38 @@ struct UnpackParams {
     int B, Hkv, T, Sk, d;
 };
 
-// A lane takes 8 columns of a slot's key and of its value.  Memory bounds it: R bytes in and d values out for each.
+// A lane takes 8 columns of a slot's key and of its value.  Memory bounds it: R bytes in and d values out for each.  4 x 8 x 16384 x 128 of 70 to 100 % of that
+// length to bfloat16: 352 MB, 49 us (of which the cache's 84 MB stay in the last level from call to call; 70 with stores that do, 51 and 50 where a thread
+// takes two and four slots).
 template <int OUT>
 __global__ void __launch_bounds__(256) smha_packed_get(const UnpackParams p) {
-    const int chunks = p.d >> 3, G = (p.d + 31) >> 5;
-    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int row = (int)(id / chunks), chunk = (int)(id - (int64_t)row * chunks);
-    const int bh = row / p.T, t = row - bh * p.T, b = bh / p.Hkv, hk = bh - b * p.Hkv;
-    if (b >= p.B) return;
-    const int len = min(max(p.lengths[b], 0), p.Sk);
-    const int64_t slot = (p.offsets ? (int64_t)p.offsets[b] : 0) + t;
-    const bool kept = slot >= 0 && slot < len;
+    const int chunks = p.d >> 3, G = (p.d + 31) >> 5, at_once = quotient(256, chunks), first = quotient(threadIdx.x, chunks), chunk = (int)threadIdx.x - first * chunks;
+    const int row = (int)blockIdx.x * at_once + first;
+    if (first >= at_once || row >= p.B * p.Hkv * p.T) return;
+    const PackedRow of(row, p.T, p.Hkv, p.Sk, p.lengths, p.offsets, false);
     uint32_t head[2] = {0, 0}, word[2] = {0, 0};
 #pragma unroll
     for (int i = 0; i < 2; ++i)
-        if (kept) {
-            const uint8_t *const from = p.cache[i] + b * p.cs[i].b + hk * p.cs[i].h + slot * p.cs[i].s;
+        if (of.kept) {
+            const uint8_t *const from = p.cache[i] + of.b * p.cs[i].b + of.hk * p.cs[i].h + of.slot * p.cs[i].s;
             head[i] = *reinterpret_cast<const uint32_t *>(from + 4 * (chunk >> 2));
             word[i] = *reinterpret_cast<const uint32_t *>(from + 4 * G + 4 * chunk);
         }
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         u32x4 v = unpack8(word[i], head[i]);
-        const int64_t at = b * p.os[i].b + hk * p.os[i].h + t * p.os[i].s + 8 * chunk;
+        const int64_t at = of.b * p.os[i].b + of.hk * p.os[i].h + of.t * p.os[i].s + 8 * chunk;
         if constexpr (OUT == SMHA_F32) {
             float *const to = (float *)p.out[i] + at;
 #pragma unroll
             for (int h = 0; h < 2; ++h)
-                *reinterpret_cast<f32x4 *>(to + 4 * h) = f32x4{widen16<false>(v[2 * h] & 0xFFFFu), widen16<false>(v[2 * h] >> 16), widen16<false>(v[2 * h + 1] & 0xFFFFu),
-                                                               widen16<false>(v[2 * h + 1] >> 16)};
+                __builtin_nontemporal_store(f32x4{widen16<false>(v[2 * h] & 0xFFFFu), widen16<false>(v[2 * h] >> 16), widen16<false>(v[2 * h + 1] & 0xFFFFu), widen16<false>(v[2 * h + 1] >> 16)},
+                                            reinterpret_cast<f32x4 *>(to + 4 * h));
         } else {
             if (OUT == SMHA_BF16)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) v[e] = as_bf16(v[e]);
-            *reinterpret_cast<u32x4 *>((uint16_t *)p.out[i] + at) = v;
+            __builtin_nontemporal_store(v, reinterpret_cast<u32x4 *>((uint16_t *)p.out[i] + at));
         }
     }
 }
@@ -218,16 +242,6 @@ __global__ void __launch_bounds__(256) smha_packed_get(const UnpackParams p) {
 // the tiles of keys that it sees are a group.  Memory bounds calls of few rows: a key's 10 d / 8 bytes meet 4 d G T operations.  There
 // every compute unit has to read, whatever the lengths are, so the key tiles of all groups are counted on the device and cut into as many segments, of
 // about the same length, as workgroups fit the chip; segments of one group are joined by a second kernel, in a fixed order.
-// n / d for 0 <= n <= 2^30, 0 < d < 2^30: in 32-bit floats, again for what that leaves, and by one for what that does.  (A segment is found by a chain of
-// divisions; the compiler's take twice as many instructions.)
-__device__ __forceinline__ int quotient(int n, int d) {
-    const float inv = __builtin_amdgcn_rcpf((float)d);
-    int q = (int)((float)n * inv);
-    q += (int)((float)(n - q * d) * inv);
-    const int rest = n - q * d;
-    return q + (rest >= d ? 1 : 0) - (rest < 0 ? 1 : 0);
-}
-
 struct PackedParams {
     const uint16_t *Q;
     const uint8_t *K, *V;
@@ -972,8 +986,8 @@ extern "C" smha_status_t smha_packed_write(const void *K_new, const void *V_new,
                       : G == 2 ? (bf16 ? smha_packed_put<2, true> : smha_packed_put<2, false>)
                       : G == 3 ? (bf16 ? smha_packed_put<3, true> : smha_packed_put<3, false>)
                                : (bf16 ? smha_packed_put<4, true> : smha_packed_put<4, false>);
-    const int64_t quads = (int64_t)B * Hkv * T * G;
-    hipLaunchKernelGGL(put, dim3((unsigned)((quads + 63) / 64)), dim3(256), 0, (hipStream_t)hip_stream, pp);
+    const int64_t rows = (int64_t)B * Hkv * T, at_once = 64 / G;
+    hipLaunchKernelGGL(put, dim3((unsigned)((rows + at_once - 1) / at_once)), dim3(256), 0, (hipStream_t)hip_stream, pp);
     return hipGetLastError() == hipSuccess ? SMHA_OK : SMHA_ERR_HIP;
 }
 
@@ -997,8 +1011,8 @@ extern "C" smha_status_t smha_packed_read(const void *K, const void *V, void *K_
     up.lengths = lengths; up.offsets = offsets;
     up.B = B; up.Hkv = Hkv; up.T = T; up.Sk = Sk; up.d = d;
     auto *const get = out_dtype == SMHA_F32 ? smha_packed_get<SMHA_F32> : out_dtype == SMHA_BF16 ? smha_packed_get<SMHA_BF16> : smha_packed_get<SMHA_F16>;
-    const int64_t lanes = (int64_t)B * Hkv * T * (d / 8);
-    hipLaunchKernelGGL(get, dim3((unsigned)((lanes + 255) / 256)), dim3(256), 0, (hipStream_t)hip_stream, up);
+    const int64_t rows = (int64_t)B * Hkv * T, at_once = 256 / (d / 8);
+    hipLaunchKernelGGL(get, dim3((unsigned)((rows + at_once - 1) / at_once)), dim3(256), 0, (hipStream_t)hip_stream, up);
     return hipGetLastError() == hipSuccess ? SMHA_OK : SMHA_ERR_HIP;
 }
 
