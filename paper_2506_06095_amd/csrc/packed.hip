@@ -308,79 +308,134 @@ __device__ __forceinline__ int lanes_scan(int v) {
 }
 __device__ __forceinline__ int lanes_sum(int v) { return __builtin_amdgcn_readlane(lanes_scan(v), 63); }
 
-// The segment of a workgroup.  Every wave of the launch computes the same cut: `most` tiles a segment at most, so many that all tiles make `slots` segments.  A group's last
-// segment is shorter, so that there are more of them then; where that is most of what is over, `most` is raised by it (unless groups are too many for that: what does not fit
-// at first starts as others end).  An XCD takes a run of segments: those that read the same keys are neighbours.
-template <int KT, int ROWS, int TURN> __device__ __forceinline__ PackedSegment packed_segment(const PackedParams &p, int lane) {
-    const int xcd = (int)blockIdx.x & 7, slot = (int)blockIdx.x >> 3;
-    PackedSegment s{-1, 0, 0, 0, 0, 1, 0, 0};
-    if (!p.slots) {
-        const int n = p.B * p.Hkv * p.row_tiles, run = (n + 7) / 8, at = xcd * run + slot;
-        if (slot >= run || at >= n) return s;
-        const int hb = quotient(at, p.row_tiles);  // a head's last rows, which see the most keys, come first
-        s.hk = quotient(hb, p.B);  // (an XCD has sequences of all lengths)
-        s.b = hb - s.hk * p.B;
-        s.rows0 = ROWS * (p.row_tiles - 1 - (at - hb * p.row_tiles));
-        s.length = uniform_load(p.lengths + s.b);
-        return s;
-    }
-    const int E = p.B * p.row_tiles;
+// The segment of a workgroup.  Every workgroup of the launch computes the same cut: `most` tiles a segment at most, so many that all tiles make `wanted` segments.  A
+// group's last segment is shorter, so that there are more of them then; where that is most of what is over, `most` is raised by it.  (Where groups fill the
+// chip by themselves only those are cut that are longer than twice what a slot has to do.)  Segments of the same key head are Hkv or a multiple of it apart, and with
+// eight such heads, or a multiple, on the same XCD.  Up to 64 entries (row tiles of all sequences) are a lane each, and every wave counts by itself; more are
+// counted by the workgroup, in LDS, where its tiles come later.
+constexpr int kPackedEntries = 4096;
+template <int KT, int ROWS, int TURN> struct PackedCut {
+    const PackedParams &p;
+    const int E, lane;
     struct Entry {
         int b, rows0, length, n;
     };
-    auto entry = [&](int i) __attribute__((always_inline)) {
+    __device__ __forceinline__ Entry entry(int i) const {
         Entry e{0, 0, 0, 0};
         if (i < E) {
             e.b = p.row_tiles > 1 ? quotient(i, p.row_tiles) : i;
-            e.rows0 = ROWS * (p.row_tiles - 1 - (i - e.b * p.row_tiles));
+            e.rows0 = ROWS * (p.row_tiles - 1 - (i - e.b * p.row_tiles));  // a sequence's last rows, which see the most keys, come first
             e.length = p.lengths[e.b];
             e.n = PackedKeys<KT>::of(p, e.length, e.rows0, ROWS).n;
         }
         return e;
-    };
-    auto parts_of = [&](int i, int n, int most) __attribute__((always_inline)) { return i < E ? max(1, quotient(n + most - 1, most)) : 0; };
-    const Entry first64 = entry(lane);  // (most calls have no more)
-    int sum = first64.n;
-    if (__builtin_expect(E > 64, 0))
-        for (int i = 64; i < E; i += 64) sum += entry(i + lane).n;
-    const int total = p.Hkv * lanes_sum(sum);
-    int most = 0, n = 0;
-    for (int wanted = p.slots;;) {
-        most = max(4, (quotient(total + wanted - 1, wanted) + TURN - 1) / TURN * TURN);
-        sum = parts_of(lane, first64.n, most);
-        if (__builtin_expect(E > 64, 0))
-            for (int i = 64; i < E; i += 64) sum += parts_of(i + lane, entry(i + lane).n, most);
-        n = p.Hkv * lanes_sum(sum);
-        if (wanted < p.slots || n <= p.slots) break;
-        wanted -= n - quotient(total, most);  // what is over
-        if (2 * wanted <= p.slots) break;
     }
-    const int run = (n + 7) / 8;
-    int at = xcd * run + slot, place = 0;
-    if (slot >= run || at >= n) return s;
-    Entry e = first64;
-    for (int i0 = 0;;) {
-        const int parts = parts_of(i0 + lane, e.n, most), mine = p.Hkv * parts, upto = lanes_scan(mine), cut = parts > 1 ? mine : 0, cut_upto = lanes_scan(cut);
-        const uint64_t past = __builtin_amdgcn_ballot_w64(upto > at);
-        if (past) {
-            const int who = __builtin_ctzll(past);
-            s.b = __builtin_amdgcn_readlane(e.b, who);
-            s.rows0 = __builtin_amdgcn_readlane(e.rows0, who);
-            s.length = __builtin_amdgcn_readlane(e.length, who);
-            s.parts = __builtin_amdgcn_readlane(parts, who);
-            const int rest = at - (__builtin_amdgcn_readlane(upto, who) - __builtin_amdgcn_readlane(mine, who));
-            s.hk = quotient(rest, s.parts);
-            s.part = rest - s.hk * s.parts;
-            s.place = place + __builtin_amdgcn_readlane(cut_upto, who) - __builtin_amdgcn_readlane(cut, who) + rest;
-            s.group = (s.b * p.Hkv + s.hk) * p.row_tiles + s.rows0 / ROWS;
-            return s;
+    static __device__ __forceinline__ int parts_of(int n, int most) { return max(1, quotient(n + most - 1, most)); }
+    static __device__ __forceinline__ int at_most(int total, int segments) { return max(4, (quotient(total + segments - 1, segments) + TURN - 1) / TURN * TURN); }
+    // `count(most)`: segments then
+    template <typename Count> __device__ __forceinline__ void choose(int total, int &most, int &n, Count count) const {
+        for (int wanted = p.slots;;) {
+            most = at_most(total, wanted);
+            n = count(most);
+            if (wanted < p.slots || n <= p.slots) break;
+            wanted -= n - quotient(total, most);  // what is over
+            if (2 * wanted <= p.slots) break;
         }
-        at -= __builtin_amdgcn_readlane(upto, 63);
-        place += __builtin_amdgcn_readlane(cut_upto, 63);
-        i0 += 64;
-        if (i0 >= E) return s;  // (not reached: the segments counted are those found)
-        e = entry(i0 + lane);
     }
+    __device__ __forceinline__ void set(PackedSegment &s, const Entry &e, int parts, int rest, int place) const {
+        s.b = e.b;
+        s.rows0 = e.rows0;
+        s.length = e.length;
+        s.parts = parts;
+        s.hk = quotient(rest, parts);
+        s.part = rest - s.hk * parts;
+        s.place = place + rest;
+        s.group = (s.b * p.Hkv + s.hk) * p.row_tiles + s.rows0 / ROWS;
+    }
+    __device__ __forceinline__ void few(PackedSegment &s, int at) const {
+        const Entry e = entry(lane);
+        auto parts = [&](int most) __attribute__((always_inline)) { return lane < E ? parts_of(e.n, most) : 0; };
+        int most, n;
+        choose(p.Hkv * lanes_sum(e.n), most, n, [&](int most) __attribute__((always_inline)) { return p.Hkv * lanes_sum(parts(most)); });
+        if (at >= n) return;
+        const int mine = parts(most), segs = p.Hkv * mine, upto = lanes_scan(segs), cut = mine > 1 ? segs : 0, cut_upto = lanes_scan(cut);
+        const int who = __builtin_ctzll(__builtin_amdgcn_ballot_w64(upto > at));
+        auto his = [&](int v) __attribute__((always_inline)) { return __builtin_amdgcn_readlane(v, who); };
+        set(s, Entry{his(e.b), his(e.rows0), his(e.length), 0}, his(mine), at - his(upto - segs), his(cut_upto - cut));
+    }
+    __device__ __forceinline__ void many(PackedSegment &s, int at, int *tiles) const {
+        __shared__ int sums[2][4];
+        __shared__ int found[4];
+        const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), per = (E + 255) / 256, first = (int)threadIdx.x * per, last = min(first + per, E);
+        for (int i = threadIdx.x; i < E; i += 256) tiles[i] = entry(i).n;
+        __syncthreads();
+        // a value of every thread: the sum of those before it, and of all
+        auto sum_of = [&](int v, int turn, int &before) __attribute__((always_inline)) {
+            const int upto = lanes_scan(v);
+            __syncthreads();  // (the sums of before are read)
+            if (lane == 63) sums[turn][w] = upto;
+            __syncthreads();
+            int all = 0;
+            before = upto - v;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                const int y = sums[turn][x];
+                before += x < w ? y : 0;
+                all += y;
+            }
+            return __builtin_amdgcn_readfirstlane(all);
+        };
+        int sum = 0, before, most, n;
+        for (int i = first; i < last; ++i) sum += tiles[i];
+        const int total = p.Hkv * sum_of(sum, 0, before);
+        choose(total, most, n, [&](int most) __attribute__((always_inline)) {
+            int sum = 0;
+            for (int i = first; i < last; ++i) sum += parts_of(tiles[i], most);
+            return p.Hkv * sum_of(sum, 0, before);
+        });
+        if (at >= n) return;  // (the whole workgroup)
+        const int start = p.Hkv * before;  // of this thread's entries' segments (the last count was with this `most`)
+        int cuts = 0, cuts_before;
+        for (int i = first; i < last; ++i) {
+            const int parts = parts_of(tiles[i], most);
+            cuts += parts > 1 ? parts : 0;
+        }
+        sum_of(cuts, 1, cuts_before);
+        int from = start, place = p.Hkv * cuts_before;
+        for (int i = first; i < last && from <= at; ++i) {
+            const int parts = parts_of(tiles[i], most);
+            if (at < from + p.Hkv * parts) {
+                found[0] = i;
+                found[1] = parts;
+                found[2] = at - from;
+                found[3] = place;
+            }
+            from += p.Hkv * parts;
+            place += parts > 1 ? p.Hkv * parts : 0;
+        }
+        __syncthreads();
+        const int i = __builtin_amdgcn_readfirstlane(found[0]), parts = __builtin_amdgcn_readfirstlane(found[1]), rest = __builtin_amdgcn_readfirstlane(found[2]);
+        const int b = __builtin_amdgcn_readfirstlane(quotient(i, p.row_tiles));
+        set(s, Entry{b, ROWS * (p.row_tiles - 1 - (i - b * p.row_tiles)), uniform_load(p.lengths + b), 0}, parts, rest, __builtin_amdgcn_readfirstlane(found[3]));
+    }
+};
+template <int KT, int ROWS, int TURN> __device__ __forceinline__ PackedSegment packed_segment(const PackedParams &p, int lane, char *lds) {
+    PackedSegment s{-1, 0, 0, 0, 0, 1, 0, 0};
+    if (p.slots) {
+        const PackedCut<KT, ROWS, TURN> cut{p, p.B * p.row_tiles, lane};
+        if (__builtin_expect(cut.E <= 64, 1)) cut.few(s, blockIdx.x);
+        else cut.many(s, blockIdx.x, reinterpret_cast<int *>(lds));
+        return s;
+    }
+    // groups as they are, an XCD a run of them, with sequences of all lengths
+    const int n = p.B * p.Hkv * p.row_tiles, run = (n + 7) / 8, slot = (int)blockIdx.x >> 3, at = ((int)blockIdx.x & 7) * run + slot;
+    if (slot >= run || at >= n) return s;
+    const int hb = quotient(at, p.row_tiles);
+    s.hk = quotient(hb, p.B);
+    s.b = hb - s.hk * p.B;
+    s.rows0 = ROWS * (p.row_tiles - 1 - (at - hb * p.row_tiles));
+    s.length = uniform_load(p.lengths + s.b);
+    return s;
 }
 
 // The reference that a row's segment leaves: -inf says that it has no keys.  (A row of NaN has no largest score either, and must not be passed over.)
@@ -483,7 +538,7 @@ __global__ void __launch_bounds__(256, packed_workgroups(D, NR)) smha_packed_par
     char *const smem = all_tiles + w * TB;
     const float NEG_INF = -__builtin_inff();
 
-    const PackedSegment s = packed_segment<32, ROWS, 4>(p, lane);
+    const PackedSegment s = packed_segment<32, ROWS, 4>(p, lane, all_tiles);
     if (s.b < 0) return;
     const int rows = p.G * p.T;
     const auto keys = PackedKeys<32>::of(p, s.length, s.rows0, ROWS);
@@ -665,7 +720,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) smha_packed_wide(const P
     const int wr = KH == 1 ? w : w & 1, wk = KH == 1 ? 0 : w >> 1;  // the wave's rows, and its half of the keys
     const float NEG_INF = -__builtin_inff();
 
-    const PackedSegment s = packed_segment<64, ROWS, 1>(p, lane);
+    const PackedSegment s = packed_segment<64, ROWS, 1>(p, lane, smem);
     if (s.b < 0) return;
     const int rows = p.G * p.T;
     const auto keys = PackedKeys<64>::of(p, s.length, s.rows0, ROWS);
@@ -846,75 +901,77 @@ __global__ void __launch_bounds__(256) smha_packed_join(const PackedParams p) {
     __shared__ float lds_ml[2][4];
     __shared__ __attribute__((aligned(16))) float lds_o[4][D];
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), rows = p.G * p.T, cl = lane % CL;
-    const int id = (int)blockIdx.x * RPW + w / W, bh = quotient(id, rows), row = id - bh * rows, b = quotient(bh, p.Hkv), hk = bh - b * p.Hkv, t = quotient(row, p.G), g = row - t * p.G;
-    if (b >= p.B) return;  // (with W = 4 for all of a workgroup's waves or none; with W = 1 none waits for another)
-    const int2 info = uniform_load(p.info + (int64_t)bh * p.row_tiles + row / ROWS);
-    if (info.y <= 1) return;  // written whole
-    const float *const stats = p.stats + (int64_t)info.x * 2 * ROWS + row % ROWS, *const parts = p.parts + ((int64_t)info.x * ROWS + row % ROWS) * D + 4 * cl;
-    const float NEG_INF = -__builtin_inff();
-    float m = NEG_INF, sum = 0.f;
-    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    for (int i0 = (w % W) * SUB + lane / CL; i0 < info.y; i0 += 4 * W * SUB) {
-        float ref[4], part[4], top = m;
-        f32x4 x[4];
+    // (a wave that has a row for itself takes several where there are many)
+    for (int id = (int)blockIdx.x * RPW + w / W; id < p.B * p.Hkv * rows; id += (int)gridDim.x * RPW) {
+        const int bh = quotient(id, rows), row = id - bh * rows, b = quotient(bh, p.Hkv), hk = bh - b * p.Hkv, t = quotient(row, p.G), g = row - t * p.G;
+        const int2 info = uniform_load(p.info + (int64_t)bh * p.row_tiles + row / ROWS);
+        if (info.y <= 1) continue;  // written whole
+        const float *const stats = p.stats + (int64_t)info.x * 2 * ROWS + row % ROWS, *const parts = p.parts + ((int64_t)info.x * ROWS + row % ROWS) * D + 4 * cl;
+        const float NEG_INF = -__builtin_inff();
+        float m = NEG_INF, sum = 0.f;
+        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+        for (int i0 = (w % W) * SUB + lane / CL; i0 < info.y; i0 += 4 * W * SUB) {
+            float ref[4], part[4], top = m;
+            f32x4 x[4];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const int i = i0 + W * SUB * q < info.y ? i0 + W * SUB * q : i0;
-            ref[q] = stats[(int64_t)i * 2 * ROWS];
-            part[q] = stats[(int64_t)i * 2 * ROWS + ROWS];
-            x[q] = *reinterpret_cast<const f32x4 *>(parts + (int64_t)i * ROWS * D);
-        }
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            if (i0 + W * SUB * q >= info.y) ref[q] = NEG_INF;
-            top = fmaxf(top, ref[q]);
-        }
-        const float old = m != NEG_INF ? fast_exp2(m - top) : 0.f;
-        sum *= old;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) acc[e] *= old;
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-            if (ref[q] != NEG_INF) {
-                const float share = fast_exp2(ref[q] - top);
-                sum = fmaf(share, part[q], sum);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) acc[e] = fmaf(share, x[q][e], acc[e]);
+            for (int q = 0; q < 4; ++q) {
+                const int i = i0 + W * SUB * q < info.y ? i0 + W * SUB * q : i0;
+                ref[q] = stats[(int64_t)i * 2 * ROWS];
+                part[q] = stats[(int64_t)i * 2 * ROWS + ROWS];
+                x[q] = *reinterpret_cast<const f32x4 *>(parts + (int64_t)i * ROWS * D);
             }
-        m = top;
-    }
-    // lanes with the same columns, in the order of a tree
 #pragma unroll
-    for (int far = CL; far < 64; far *= 2) {
-        const float mu = __shfl_xor(m, far), top = fmaxf(m, mu), mine = m != NEG_INF ? fast_exp2(m - top) : 0.f, his = mu != NEG_INF ? fast_exp2(mu - top) : 0.f;
-        sum = mine * sum + his * __shfl_xor(sum, far);
+            for (int q = 0; q < 4; ++q) {
+                if (i0 + W * SUB * q >= info.y) ref[q] = NEG_INF;
+                top = fmaxf(top, ref[q]);
+            }
+            const float old = m != NEG_INF ? fast_exp2(m - top) : 0.f;
+            sum *= old;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[e] = mine * acc[e] + his * __shfl_xor(acc[e], far);
-        m = top;
-    }
-    uint16_t *const to = p.O + b * p.os.b + (hk * p.G + g) * p.os.h + t * p.os.s;
-    if constexpr (W == 4) {
-        if (lane == 0) {
-            lds_ml[0][w] = m;
-            lds_ml[1][w] = sum;
+            for (int e = 0; e < 4; ++e) acc[e] *= old;
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                if (ref[q] != NEG_INF) {
+                    const float share = fast_exp2(ref[q] - top);
+                    sum = fmaf(share, part[q], sum);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[e] = fmaf(share, x[q][e], acc[e]);
+                }
+            m = top;
         }
-        if (lane < CL) *reinterpret_cast<f32x4 *>(&lds_o[w][4 * cl]) = acc;
-        __syncthreads();
-        if (w) return;
-        const float top = fmaxf(fmaxf(lds_ml[0][0], lds_ml[0][1]), fmaxf(lds_ml[0][2], lds_ml[0][3]));
-        sum = 0.f;
-        acc = f32x4{0.f, 0.f, 0.f, 0.f};
+        // lanes with the same columns, in the order of a tree
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const float share = lds_ml[0][q] != NEG_INF ? fast_exp2(lds_ml[0][q] - top) : 0.f;
-            const f32x4 y = *reinterpret_cast<const f32x4 *>(&lds_o[q][4 * cl]);
-            sum = fmaf(share, lds_ml[1][q], sum);
+        for (int far = CL; far < 64; far *= 2) {
+            const float mu = __shfl_xor(m, far), top = fmaxf(m, mu), mine = m != NEG_INF ? fast_exp2(m - top) : 0.f, his = mu != NEG_INF ? fast_exp2(mu - top) : 0.f;
+            sum = mine * sum + his * __shfl_xor(sum, far);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) acc[e] = fmaf(share, y[e], acc[e]);
+            for (int e = 0; e < 4; ++e) acc[e] = mine * acc[e] + his * __shfl_xor(acc[e], far);
+            m = top;
         }
+        uint16_t *const to = p.O + b * p.os.b + (hk * p.G + g) * p.os.h + t * p.os.s;
+        if constexpr (W == 4) {
+            if (lane == 0) {
+                lds_ml[0][w] = m;
+                lds_ml[1][w] = sum;
+            }
+            if (lane < CL) *reinterpret_cast<f32x4 *>(&lds_o[w][4 * cl]) = acc;
+            __syncthreads();
+            if (w) return;  // (a workgroup has one row)
+            const float top = fmaxf(fmaxf(lds_ml[0][0], lds_ml[0][1]), fmaxf(lds_ml[0][2], lds_ml[0][3]));
+            sum = 0.f;
+            acc = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const float share = lds_ml[0][q] != NEG_INF ? fast_exp2(lds_ml[0][q] - top) : 0.f;
+                const f32x4 y = *reinterpret_cast<const f32x4 *>(&lds_o[q][4 * cl]);
+                sum = fmaf(share, lds_ml[1][q], sum);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[e] = fmaf(share, y[e], acc[e]);
+            }
+        }
+        const float inv = sum != 0.f ? 1.0f / sum : 0.f;
+        if (lane < CL && 4 * cl < p.d) store4<BF16 ? SMHA_BF16 : SMHA_F16>(to, 4 * cl, acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
     }
-    const float inv = sum != 0.f ? 1.0f / sum : 0.f;
-    if (lane < CL && 4 * cl < p.d) store4<BF16 ? SMHA_BF16 : SMHA_F16>(to, 4 * cl, acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
 }
 
 // ---------------------------------------------------------------------------------------
@@ -1035,16 +1092,22 @@ static smha_status_t packed_form(PackedForm &f, int B, int H, int Hkv, int T, in
     const int KT = wide ? 64 : 32;
     f.row_tiles = (rows + f.rows - 1) / f.rows;
     const int64_t groups = (int64_t)B * Hkv * f.row_tiles;
-    if (groups * (Sk / KT + 8) > (1 << 30)) return SMHA_ERR_UNSUPPORTED;  // (tiles are counted in 32 bits)
+    // (tiles are counted in 32 bits, and a launch has less than 2^32 threads)
+    if (groups * (Sk / KT + 8) > (1 << 30) || groups + 2048 >= 1 << 24) return SMHA_ERR_UNSUPPORTED;
     const int64_t see = window == 0 || window > Sk ? Sk : window;
     const int64_t tiles = std::min<int64_t>((Sk + KT - 1) / KT, (see + std::min(n_sink, Sk) + T) / KT + 3);
     const int slots = 256 * (wide ? (D == 64 ? 3 : 2) : packed_workgroups(D, f.rows / 16));
-    const bool direct = wide ? groups >= slots || tiles <= 8 : tiles <= std::min<int64_t>(48, (D == 64 ? 24 : 16) + groups / 8);
-    f.slots = direct ? 0 : slots;
+    // Groups are taken whole, in one launch, where they have few tiles: cutting costs a second launch and the search for a segment, and shares out what one workgroup
+    // would read alone (us, whole and cut: 64 groups x 128 of 512 keys 8.5 and 9.6, of 1024 12.8 and 11.4; 256 groups of 1024 14.0 and 17.8); where one sequence's fill the chip,
+    // so that lengths hardly matter (2 x 1024 tokens x 32 on 8 x 16384 x 128 545 and 564; 4 x 512 x 32 on 8 x 8192, of 10 to 100 % of that, 237 and 248, but a long sequence among
+    // short ones would be read by half the chip); and where there are too many to count.  (512 x 32 on 8 x 2048 x 128, of 10 to 100 %: 154 and 167.)
+    const bool direct = (int64_t)B * f.row_tiles > kPackedEntries || tiles <= (wide ? 8 : std::min<int64_t>(48, (D == 64 ? 24 : 16) + groups / 8)) ||
+                        (int64_t)Hkv * f.row_tiles >= 256;
+    f.slots = direct ? 0 : groups < slots ? slots : slots / 2;
     f.stats = f.parts = f.total = 0;
     if (direct) return SMHA_OK;
     // cut groups are longer than a segment, so that there are fewer of them than slots, and their segments no more than that and one each
-    const int64_t places = std::min(std::min<int64_t>(2 * slots, slots + groups), groups * ((tiles + 3) / 4));
+    const int64_t places = std::min(std::min<int64_t>(2 * f.slots, f.slots + groups), groups * ((tiles + 3) / 4));
     f.stats = packed_up(groups * sizeof(int2));
     f.parts = f.stats + packed_up((size_t)places * 2 * f.rows * 4);
     f.total = f.parts + (size_t)places * f.rows * D * 4;
@@ -1072,7 +1135,7 @@ template <int D, bool BF16> static hipError_t launch_packed(const PackedParams &
                        : f.rows == 32 ? (alone ? smha_packed_join<D, 32, 1, BF16> : smha_packed_join<D, 32, 4, BF16>)
                        : f.rows == 64 ? (alone ? smha_packed_join<D, 64, 1, BF16> : smha_packed_join<D, 64, 4, BF16>)
                                       : (alone ? smha_packed_join<D, 128, 1, BF16> : smha_packed_join<D, 128, 4, BF16>);
-    hipLaunchKernelGGL(join, dim3(alone ? (rows + 3) / 4 : rows), dim3(256), 0, stream, pp);
+    hipLaunchKernelGGL(join, dim3(alone ? std::min(2048, (rows + 3) / 4) : rows), dim3(256), 0, stream, pp);
     return hipGetLastError();
 }
 

@@ -329,6 +329,11 @@ CASES = [
     (1, 17, 1, 1, 77, 40, 0, 0, [77], "bhsd"),                       # 17 rows
     (1, 5, 1, 13, 3000, 56, 0, 0, [2999], "bhsd"),                   # 65 rows
     (3, 2, 2, 300, 700, 64, 128, 0, [700, 299, 1], "bshd"),
+    (90, 2, 1, 1, 3000, 64, 0, 0, [3000 if i == 50 else 5 + 7 * i for i in range(90)], "bhsd"),   # one long sequence among short ones, counted in LDS
+    (70, 8, 1, 5, 900, 128, 0, 0, [900 - 13 * i for i in range(69)] + [0], "bhsd"),                # 40 rows of each of 70 sequences
+    (300, 1, 1, 1, 1700, 32, 0, 0, [(1701 * i) // 300 for i in range(300)], "bhsd"),
+    (4200, 2, 2, 1, 40, 8, 0, 0, [i % 41 for i in range(4200)], "bhsd"),                           # too many sequences to count
+    (3, 16, 1, 100, 1500, 64, 0, 0, [1500, 90, 700], "bhsd"),                                     # 13 tiles of 128 rows, cut
 ]
 
 
