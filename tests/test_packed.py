@@ -350,3 +350,372 @@ def test_attention_is_the_formula(case, dtype):
     again = torch.full_like(out, math.nan)
     assert smha.packed_attention(q, k, v, int32(lengths), window=window, n_sink=n_sink, out=again) is again
     assert torch.equal(again, out)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T, Sk", [(2, 600), (2, 6000), (30, 600), (30, 9000), (90, 9000)])   # few rows whole and cut, 120 rows, 360
+def test_what_is_not_seen_may_hold_anything(T, Sk):
+    k, v = filled(2, 2, Sk, 128)
+    q = queries(2, 8, T, 128, torch.float16)
+    n, window, n_sink = Sk - 45, 100, 5
+    want = smha.packed_attention(q, k, v, int32([n, 1]), window=window, n_sink=n_sink)
+    first = n - T - window + 1  # the first key in the first token's window
+    for t in (k, v):
+        t[0, :, n:] = 0xFF  # (steps, bases and so values that are NaN)
+        t[0, :, n_sink:first] = 0xFF
+        t[1, :, 1:] = 0xFF
+    assert bool(torch.isfinite(want).all())
+    assert torch.equal(smha.packed_attention(q, k, v, int32([n, 1]), window=window, n_sink=n_sink), want)
+    assert bool((want[1, :, :T - 1] == 0).all()) and bool((want[1, :, T - 1] != 0).any())
+
+
+@pytest.mark.gpu
+@TYPES
+@pytest.mark.parametrize("T, Sk", [(1, 300), (1, 5000), (20, 300)])
+def test_a_query_of_nan_stays_nan_alone(T, Sk, dtype):
+    k, v = filled(1, 2, Sk, 64)
+    q = queries(1, 4, T, 64, dtype)
+    want = smha.packed_attention(q, k, v, int32([Sk]))
+    q[0, 1, 0, 5] = math.nan
+    got = smha.packed_attention(q, k, v, int32([Sk]))
+    assert bool(got[0, 1, 0].isnan().all())
+    got[0, 1, 0] = want[0, 1, 0]
+    assert torch.equal(got, want)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [1, 12, 40])
+def test_queries_of_any_size_are_brought_to_binary16(T):
+    """bfloat16 queries times a power of two, and the scale by its inverse: the same bits, far past what binary16 holds."""
+    k, v = filled(2, 2, 777, 96)
+    q = queries(2, 6, T, 96, torch.bfloat16)
+    want = smha.packed_attention(q, k, v, int32([777, 300]), scale=0.125)
+    for p in (-90, -30, 17, 60):
+        assert torch.equal(smha.packed_attention(q * 2.0 ** p, k, v, int32([777, 300]), scale=0.125 * 2.0 ** -p), want)
+    assert torch.equal(smha.packed_attention(torch.zeros_like(q), k, v, int32([777, 300])), smha.packed_attention(q, k, v, int32([777, 300]), scale=1e-38))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d", [64, 128, 72])
+@pytest.mark.parametrize("T, Sk", [(1, 90), (1, 4000), (20, 4000)])
+def test_caches_of_any_strides(d, T, Sk):
+    """Keys and values side by side, tokens before heads, a head's first byte aligned to 4 and no more."""
+    B, Hkv, R = 2, 3, row_bytes(d)
+    both = torch.randint(0, 256, (B, Sk, Hkv, 2, R + 12), dtype=torch.uint8, device="cuda")
+    k, v = (both[:, :, :, i, 4:4 + R].transpose(1, 2) for i in range(2))
+    packed = smha.packed_cache(B, Hkv, Sk, d)
+    kn, vn = new_tokens(B, Hkv, Sk, d, torch.bfloat16, "bshd")
+    around = both.clone()
+    for cache in ((k, v), packed):
+        smha.packed_write(kn, vn, *cache, int32([Sk, Sk - 7]), offsets=int32([0, 0]))
+    for i, t in enumerate(packed):
+        around[0, :, :, i, 4:4 + R] = t[0].transpose(0, 1)
+        around[1, :Sk - 7, :, i, 4:4 + R] = t[1, :, :Sk - 7].transpose(0, 1)
+    assert torch.equal(both, around)  # and nothing beside the rows is written
+    for a, b in zip(smha.packed_read(k, v, int32([Sk, Sk - 7])), smha.packed_read(*packed, int32([Sk, Sk - 7]))):
+        assert torch.equal(a, b)
+    q = queries(B, 6, T, d, torch.float16)
+    want = smha.packed_attention(q, *packed, int32([Sk, Sk - 7]))
+    assert torch.equal(smha.packed_attention(q, k, v, int32([Sk, Sk - 7])), want)
+    # one row of heads read by all sequences (strides of 0)
+    shared = [t[:1].expand(B, Hkv, Sk, R) for t in packed]
+    assert torch.equal(smha.packed_attention(q, *shared, int32([Sk, Sk]))[0], want[0])
+
+
+@pytest.mark.gpu
+def test_caches_past_32_bits():
+    """A head of nearly 2 GiB, of which the end is read; and batches further apart than 2^32 bytes."""
+    d, R = 128, 80
+    Sk = (2 ** 31 - R) // R - 65
+    k, v = (torch.empty(1, 1, Sk, R, dtype=torch.uint8, device="cuda") for _ in range(2))
+    kn, vn = new_tokens(1, 1, 200, d, torch.float16)
+    smha.packed_write(kn, vn, k, v, int32([Sk]))
+    small = smha.packed_cache(1, 1, 200, d)
+    smha.packed_write(kn, vn, *small, int32([200]))
+    assert torch.equal(k[:, :, Sk - 200:], small[0]) and torch.equal(v[:, :, Sk - 200:], small[1])
+    got = smha.packed_read(k, v, int32([Sk]), offsets=int32([Sk - 200]), tokens=200)
+    assert all(torch.equal(a, b) for a, b in zip(got, smha.packed_read(*small, int32([200]))))
+    for T in (1, 40):
+        q = queries(1, 4, T, d, torch.float16)
+        want, bound = reference(q, *small, [200], window=100)
+        check(smha.packed_attention(q, k, v, int32([Sk]), window=100), want, bound)
+    del k, v
+    k, v = (torch.empty(5, 1, 2 ** 30 // 4 // 4, R, dtype=torch.uint8, device="cuda")[:, :, :300] for _ in range(2))  # 5 GiB apart in all
+    assert k.stride(0) * 4 > 2 ** 32
+    kn, vn = new_tokens(5, 1, 300, d, torch.float16)
+    smha.packed_write(kn, vn, k, v, int32([300] * 5))
+    small = smha.packed_cache(5, 1, 300, d)
+    smha.packed_write(kn, vn, *small, int32([300] * 5))
+    assert torch.equal(k, small[0]) and torch.equal(v, small[1])
+    q = queries(5, 4, 2, d, torch.float16)
+    assert torch.equal(smha.packed_attention(q, k, v, int32([300] * 5)), smha.packed_attention(q, *small, int32([300] * 5)))
+    assert all(torch.equal(a, b) for a, b in zip(smha.packed_read(k, v, int32([300] * 5)), smha.packed_read(*small, int32([300] * 5))))
+
+
+@pytest.mark.gpu
+@TYPES
+def test_a_serving_loop(dtype):
+    """Prompts of different lengths written at once, padded behind, and attended to; then tokens one by one, then three at once. Every output is the formula's on
+    what the cache stands for by then, and what was written before stays."""
+    B, H, Hkv, Sk, d = 3, 8, 2, 200, 80
+    prompts = [150, 1, 77]
+    k, v = smha.packed_cache(B, Hkv, Sk, d)
+    lengths = int32(prompts)
+    kn, vn = new_tokens(B, Hkv, 150, d, dtype, "bshd")
+    kv, vv = smha.packed_write(kn, vn, k, v, lengths, offsets=int32([0] * B), values=True)
+    # the prompt's own attention on what was kept of it: by the 16-bit operator, and (its last 9 tokens) on the packed cache
+    q = queries(B, H, 150, d, dtype)
+    out = smha.sink_attention(q, kv, vv, offsets=int32([0] * B), lengths=lengths)
+    late = torch.stack([q[b, :, max(0, n - 9):n] if n >= 9 else torch.cat([q[b, :, n:9], q[b, :, :n]], 1) for b, n in enumerate(prompts)])
+    want, bound = reference(late, k, v, prompts)
+    got = smha.packed_attention(late, k, v, lengths)
+    check(got, want, bound)
+    # Apart by both ways' roundings of probabilities and outputs (half a step of the largest value each) and by the rounding of values to bfloat16; that of keys moves a
+    # score by u sum |q| |k| / sqrt(d) at most, and so a probability by a factor of exp(2 of that).
+    eps, top = torch.finfo(dtype).eps, float(vv.abs().max())
+    shift = 0.0 if dtype == torch.float16 else eps / 2 * float((late.float().abs() @ kv.float().abs().repeat_interleave(H // Hkv, 1).mT).max()) / math.sqrt(d)
+    for b, n in enumerate(prompts):
+        t = min(n, 9)
+        assert float((got[b, :, 9 - t:].float() - out[b, :, n - t:n].float()).abs().max()) <= (3 * eps + math.expm1(2 * shift)) * top
+    at = prompts
+    for step, T in enumerate([1, 1, 1, 3, 1]):
+        lengths += T
+        at = [n + T for n in at]
+        kn, vn = new_tokens(B, Hkv, T, d, dtype, seed=10 + step)
+        kept = k.clone()
+        kv, vv = smha.packed_write(kn, vn, k, v, lengths, values=True)
+        for b, n in enumerate(at):
+            assert torch.equal(k[b, :, :n - T], kept[b, :, :n - T]) and torch.equal(k[b, :, n:], kept[b, :, n:])
+            assert torch.equal(smha.packed_read(k, v, lengths, dtype=dtype)[1][b, :, n - T:n], vv[b])
+        q = queries(B, H, T, d, dtype, seed=20 + step)
+        for window, n_sink in ((0, 0), (40, 3)):
+            want, bound = reference(q, k, v, at, window, n_sink)
+            check(smha.packed_attention(q, k, v, lengths, window=window, n_sink=n_sink), want, bound, f"step {step}")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("Sk, H, T", [(100, 4, 1), (4000, 4, 1), (4000, 8, 3), (4000, 8, 40)])   # whole; cut; 12 rows; 160 rows
+def test_a_captured_step_follows_lengths_and_inputs(Sk, H, T):
+    B, Hkv, d = 3, 2, 128
+    k, v = filled(B, Hkv, Sk, d)
+    lengths = int32([Sk - 40, 50, T])
+    kn, vn = new_tokens(B, Hkv, T, d, torch.float16)
+    q = queries(B, H, T, d, torch.float16)
+
+    def step():
+        smha.packed_write(kn, vn, k, v, lengths)
+        return smha.packed_attention(q, k, v, lengths), *smha.packed_read(k, v, lengths, offsets=lengths - 8, tokens=8)
+
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        step()
+    stream.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step()
+    for i in range(4):
+        lengths += 7
+        kn.add_(0.25)
+        q.mul_(-1.0)
+        before = k.clone(), v.clone()
+        graph.replay()
+        replayed = [t.clone() for t in got]
+        after = k.clone(), v.clone()
+        torch.cuda.synchronize()
+        k.copy_(before[0])
+        v.copy_(before[1])
+        assert not torch.equal(k, after[0])
+        for a, b in zip(replayed, step()):
+            assert torch.equal(a, b), i
+        assert torch.equal(k, after[0]) and torch.equal(v, after[1])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("Sk", [100, 4000])
+def test_other_streams_workspaces_and_the_way_through_python(Sk):
+    k, v = filled(2, 2, Sk, 64)
+    q = queries(2, 8, 2, 64, torch.bfloat16)
+    lengths = int32([Sk, Sk // 2])
+    want = smha.packed_attention(q, k, v, lengths)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = smha.packed_attention(q, k, v, lengths, stream=side)
+    values = smha.packed_read(k, v, lengths, stream=side, dtype=torch.float32)
+    side.synchronize()
+    assert torch.equal(got, want) and all(torch.equal(a, b) for a, b in zip(values, smha.packed_read(k, v, lengths, dtype=torch.float32)))
+    with torch.cuda.stream(side):
+        got = smha.packed_attention(q, k, v, lengths)
+    side.synchronize()
+    assert torch.equal(got, want)
+    need = smha.smha_packed_workspace(2, 8, 2, 2, Sk, 64)
+    assert (need == 0) == (Sk == 100)
+    out, workspace = torch.empty_like(q), torch.full((need,), 255, dtype=torch.uint8, device="cuda")
+    smha.packed_attention(q, k, v, lengths, out=out, workspace=workspace, stream=torch.cuda.current_stream().cuda_stream)
+    assert torch.equal(out, want)
+    if need:
+        with pytest.raises(smha.SmhaError):
+            smha.packed_attention(q, k, v, lengths, out=out, workspace=workspace[:-16])
+    with pytest.raises(ValueError):
+        smha.packed_attention(q, k, v, lengths, stream=side.cuda_stream)
+    # an output of other strides
+    wide = torch.zeros(2, 2, 8, 128, dtype=q.dtype, device="cuda")
+    into = wide[..., :64].transpose(1, 2)
+    assert smha.packed_attention(q, k, v, lengths, out=into) is into and torch.equal(into, want) and bool((wide[..., 64:] == 0).all())
+    kn, vn = new_tokens(2, 2, 3, 64, torch.float16)
+    a, b = smha.packed_cache(2, 2, Sk, 64), smha.packed_cache(2, 2, Sk, 64)
+    one = smha.packed_write(kn, vn, *a, lengths, values=True)
+    two = smha.packed_write(kn, vn, *b, lengths, values=True, stream=torch.cuda.current_stream())
+    assert all(torch.equal(x, y) for x, y in zip((*a, *one), (*b, *two)))
+
+
+@pytest.mark.gpu
+def test_results_do_not_depend_on_the_order_of_workgroups():
+    k, v = filled(5, 2, 6000, 128)
+    for H, T in ((8, 1), (16, 3), (16, 8), (16, 60)):
+        q = queries(5, H, T, 128, torch.float16)
+        lengths = int32([6000, 5, 3000, 1, 4999])
+        first = smha.packed_attention(q, k, v, lengths)
+        assert all(torch.equal(smha.packed_attention(q, k, v, lengths), first) for _ in range(5))
+
+
+@pytest.mark.gpu
+def test_refusals():
+    k, v = smha.packed_cache(2, 2, 40, 64)
+    kn, vn = new_tokens(2, 2, 3, 64, torch.float16)
+    q = queries(2, 4, 3, 64, torch.float16)
+    n = int32([40, 20])
+    with pytest.raises(ValueError):
+        smha.packed_write(kn.float(), vn.float(), k, v, n)
+    with pytest.raises(ValueError):
+        smha.packed_write(kn, vn.bfloat16(), k, v, n)
+    with pytest.raises(ValueError):
+        smha.packed_write(kn[..., :56], vn[..., :56], k, v, n)
+    with pytest.raises(ValueError):
+        smha.packed_write(kn[:1], vn[:1], k, v, n)
+    with pytest.raises(ValueError):
+        smha.packed_write(kn, vn, k, v, None)
+    with pytest.raises(ValueError):
+        smha.packed_write(kn, vn, k, v, n.long())
+    with pytest.raises(ValueError):
+        smha.packed_write(kn, vn, k, v, n, offsets=n[:1])
+    with pytest.raises(ValueError):
+        smha.packed_write(kn, vn, k.to(torch.int8), v.to(torch.int8), n)
+    with pytest.raises(ValueError):
+        smha.packed_write(kn, vn, k[..., :39], v[..., :39], n)         # no row has as many bytes
+    with pytest.raises(ValueError):
+        smha.packed_write(kn, vn, k[:1].expand_as(k), v, n)            # sequences in one place
+    with pytest.raises(smha.SmhaError):
+        smha.packed_write(kn, vn, k, k, n)
+    overlapping = torch.zeros(2000, dtype=torch.uint8, device="cuda").as_strided((2, 2, 9, 40), (440, 44, 44, 1))
+    with pytest.raises(smha.SmhaError):
+        smha.packed_write(kn, vn, overlapping, v[:, :, :9], n)         # heads a key apart
+    with pytest.raises(ValueError):
+        smha.packed_write(kn.clone().requires_grad_(), vn, k, v, n)    # its gradient would be lost
+    with torch.no_grad():
+        smha.packed_write(kn.clone().requires_grad_(), vn, k, v, n)
+    with torch.autograd.forward_ad.dual_level():
+        dual = torch.autograd.forward_ad.make_dual(kn.float(), kn.float()).to(torch.float16)
+        with pytest.raises(NotImplementedError):
+            smha.packed_write(dual, vn, k, v, n)
+        dual = torch.autograd.forward_ad.make_dual(q.float(), q.float()).to(torch.float16)
+        with pytest.raises(NotImplementedError):
+            smha.packed_attention(dual, k, v, n)
+    misplaced = torch.zeros(3, 2, 40, 42, dtype=torch.uint8, device="cuda")[:2, :, :, 2:]
+    with pytest.raises(smha.SmhaError):
+        smha.packed_read(misplaced, misplaced, n)                      # not whole words apart
+    with pytest.raises(ValueError):
+        smha.packed_read(k, v, n, dtype=torch.float64)
+    with pytest.raises(ValueError):
+        smha.packed_read(k, v, n, tokens=-1)
+    with pytest.raises(smha.SmhaError):
+        smha.packed_read(k, v, n, tokens=0)
+    with pytest.raises(ValueError):
+        smha.packed_read(k, v, n, out=(torch.empty(2, 2, 40, 64, device="cuda"),) * 2)
+    same = torch.empty(2, 2, 40, 64, dtype=torch.float16, device="cuda")
+    with pytest.raises(smha.SmhaError):
+        smha.packed_read(k, v, n, out=(same, same))
+    with pytest.raises(ValueError):
+        smha.packed_attention(q[:, :3], k, v, n)
+    with pytest.raises(ValueError):
+        smha.packed_attention(q.float(), k, v, n)
+    with pytest.raises(ValueError):
+        smha.packed_attention(q, k, v, n, window=-1)
+    with pytest.raises(ValueError):
+        smha.packed_attention(q.clone().requires_grad_(), k, v, n)
+    with pytest.raises(ValueError):
+        smha.cache_attention(q, k, v, n)                               # (of 16-bit caches)
+    with pytest.raises(ValueError):
+        smha.packed_attention(q, k, v.cpu(), n)
+    with pytest.raises(ValueError):
+        smha.packed_cache(1, 1, 1, 64, device="cpu")
+    assert smha.packed_attention(q, k, v, n).shape == q.shape
+
+
+# What the C ABI says, on the CPU: status 1 invalid, 2 unsupported, 3 shape.
+
+def abi():
+    import ctypes as C
+    from paper_2506_06095_amd.binding import _load
+    return C, _load(), C.c_void_p(4096), C.c_void_p(8192)
+
+
+def i64(C, *values):
+    return (C.c_int64 * len(values))(*values)
+
+
+def test_the_abi_refuses_writes():
+    C, lib, p, q = abi()
+
+    def status(kn=p, k=p, v=q, kv=None, vv=None, n=p, B=2, Hkv=2, T=3, Sk=40, d=64, dtype=0, kns=None, ks=None):
+        return lib.smha_packed_write(kn, p, k, v, kv, vv, n, None, B, Hkv, T, Sk, d, dtype, kns, None, ks, None, None)
+
+    for kw in (dict(kn=None), dict(k=None), dict(n=None), dict(v=p), dict(kv=p), dict(vv=p), dict(B=0), dict(Hkv=0), dict(T=0), dict(Sk=0), dict(B=-1), dict(T=-2 ** 31)):
+        assert status(**kw) == 1, kw
+    for kw in (dict(d=0), dict(d=12), dict(d=136), dict(dtype=2), dict(T=1 << 27), dict(Sk=1 << 27), dict(Sk=1 << 26), dict(B=1 << 24, Hkv=2), dict(B=1 << 14, Hkv=1 << 10, T=16),
+               dict(kn=C.c_void_p(4104)), dict(k=C.c_void_p(4098)), dict(kv=p, vv=C.c_void_p(4104)),
+               dict(ks=i64(C, 3200, 1600, 36)),          # rows over one another
+               dict(ks=i64(C, 3200, 40, 40)),            # heads over rows
+               dict(ks=i64(C, 3202, 1600, 40)),          # not whole words
+               dict(ks=i64(C, 0, 1600, 40)),             # sequences in one place
+               dict(ks=i64(C, -3200, 1600, 40)), dict(ks=i64(C, 1 << 40, 1 << 36, 1 << 31)), dict(ks=i64(C, 1 << 62, 1 << 62, 1 << 62)),
+               dict(kns=i64(C, 384, 192, 60)), dict(kns=i64(C, 384, 190, 64)), dict(kns=i64(C, 384, -192, 64)), dict(kns=i64(C, 384, 192, 1 << 30))):
+        assert status(**kw) == 2, kw
+
+
+def test_the_abi_refuses_reads():
+    C, lib, p, q = abi()
+
+    def status(k=p, ko=p, vo=q, n=p, B=2, Hkv=2, T=3, Sk=40, d=64, dtype=0, ks=None, os=None):
+        return lib.smha_packed_read(k, q, ko, vo, n, None, B, Hkv, T, Sk, d, dtype, ks, None, os, None, None)
+
+    for kw in (dict(k=None), dict(ko=None), dict(vo=p), dict(n=None), dict(T=0)):
+        assert status(**kw) == 1, kw
+    for kw in (dict(d=20), dict(dtype=3), dict(ko=C.c_void_p(4104)), dict(k=C.c_void_p(4097)), dict(ks=i64(C, 3200, 1600, 20)), dict(os=i64(C, 384, 0, 64)),
+               dict(os=i64(C, 384, 192, 68)), dict(dtype=2, os=i64(C, 384, 192, 66)), dict(dtype=2, os=i64(C, 1 << 40, 1 << 34, 1 << 28))):
+        assert status(**kw) == 2, kw
+
+
+def test_the_abi_refuses_attention():
+    C, lib, p, q = abi()
+
+    def status(Q=p, k=p, o=p, n=p, B=2, H=4, Hkv=2, T=3, Sk=40, d=64, dtype=0, qs=None, ks=None, os=None, window=0, n_sink=0, ws=None, size=0):
+        return lib.smha_packed_forward(Q, k, q, o, n, B, H, Hkv, T, Sk, d, dtype, qs, ks, None, os, window, n_sink, 0.0, ws, size, None)
+
+    for kw in (dict(Q=None), dict(k=None), dict(o=None), dict(n=None), dict(B=0), dict(H=0), dict(T=0), dict(window=-1), dict(n_sink=-1),
+               dict(Sk=20000), dict(Sk=20000, size=1 << 30), dict(Sk=20000, ws=p, size=100)):   # a workspace is needed
+        assert status(**kw) == 1, kw
+    assert status(H=5) == 3
+    for kw in (dict(d=4), dict(dtype=2), dict(Q=C.c_void_p(4104)), dict(o=C.c_void_p(4104)), dict(k=C.c_void_p(4098)), dict(ws=C.c_void_p(4104), size=16), dict(T=1 << 27),
+               dict(B=1 << 20, H=32, Hkv=32), dict(T=1 << 22, H=4), dict(os=i64(C, 0, 192, 64)), dict(os=i64(C, 768, 64, 64)), dict(qs=i64(C, 768, 192, 68)), dict(ks=i64(C, 3200, 1600, 42))):
+        assert status(**kw) == 2, kw
+    need = C.c_size_t(77)
+    assert lib.smha_packed_workspace(2, 4, 2, 3, 20000, 64, 0, 0, None) == 1
+    assert lib.smha_packed_workspace(2, 5, 2, 3, 20000, 64, 0, 0, C.byref(need)) == 3 and need.value == 77
+    assert lib.smha_packed_workspace(2, 4, 2, 3, 100, 64, 0, 0, C.byref(need)) == 0 and need.value == 0
+    assert lib.smha_packed_workspace(2, 4, 2, 3, 20000, 64, 0, 0, C.byref(need)) == 0 and 0 < need.value < 1 << 24
+
+
+def test_workspaces_stay_small():
+    """What a call needs is bounded by what the chip holds at once, whatever the sizes are."""
+    for B, H, Hkv, T, Sk in ((1, 8, 8, 1, 1 << 24), (64, 64, 8, 1, 1 << 17), (4096, 16, 1, 1, 1 << 14), (64, 64, 1, 100, 1 << 14), (1, 128, 1, 1, 1 << 24)):
+        assert smha.smha_packed_workspace(B, H, Hkv, T, Sk, 128) < 256 << 20
