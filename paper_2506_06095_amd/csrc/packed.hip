@@ -609,6 +609,7 @@ __global__ void __launch_bounds__(256, packed_workgroups(D, NR)) smha_packed_par
             for (int i = 0; i < NS; ++i)
                 *reinterpret_cast<u32x4 *>(smem + (16 * a + vj) * D * 2 + (((D / 32 * u + i) ^ swz_values<D>(vj)) * 16)) = unpack8(v_raw[a].code[i], v_raw[a].head);
         if (tile + 4 < end) request_v(tile + 4);
+        __builtin_amdgcn_s_setprio(1);  // (as in smha_packed_wide; 64 x 32 on 8 x 4096 x 128, 5 tokens: 97 us without, 89)
         u32x4 pf[NR];
 #pragma unroll
         for (int x = 0; x < NR; ++x) {
@@ -651,6 +652,7 @@ __global__ void __launch_bounds__(256, packed_workgroups(D, NR)) smha_packed_par
             for (int x = 0; x < NR; ++x) o[x][ct] = mfma16(u32x4{lo[0], lo[1], hi[0], hi[1]}, pf[x], o[x][ct]);
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the tile is read
+        __builtin_amdgcn_s_setprio(0);
     }
 
     // The team joins: every wave leaves its accumulators in its own tile's place and takes a quarter of the columns of all four.
@@ -709,7 +711,8 @@ __global__ void __launch_bounds__(256, packed_workgroups(D, NR)) smha_packed_par
 
 // Many rows on the same keys: four waves share tiles of 64 keys, which all of them unpack into LDS, the next one under this one's first product, from words that were
 // requested a tile before.  KH = 1: a wave takes 32 of 128 rows; KH = 2: a wave takes 32 of 64 rows and one half of the keys, and the halves are joined at the end.  From
-// LDS on it is as in smha_sink_fwd, in binary16 throughout.
+// LDS on it is as in smha_sink_fwd, in binary16 throughout.  Waves with vector work go first, those in the mixed phase (masks, exponentials, second product) before those that
+// unpack, so that the two of a SIMD are in different phases (2 x 1024 tokens x 32 on 8 x 16384 x 128: 552 us without, 512; 4 x 512 x 32 on 8 x 8192 x 64: 242, 211).
 template <int D, int KH, bool BF16>
 __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) smha_packed_wide(const PackedParams p) {
     constexpr int NS = D / 16, NDT = D / 32, NL = D / 32, TB = 64 * D * 2, ROWS = 128 / KH, KTS = 2 / KH;  // KTS: halves of a tile that a wave takes
@@ -773,6 +776,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) smha_packed_wide(const P
         const int par = (tile - begin) & 1;
         const int key = keys.key(tile), key_w = key + 32 * wk;
         constexpr int KW = 32 * KTS;
+        __builtin_amdgcn_s_setprio(1);
         if (tile + 1 < end) {
 #pragma unroll
             for (int i = 0; i < 2 * NL; ++i) leave(lv, par ^ 1, raw, i);
@@ -780,6 +784,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) smha_packed_wide(const P
         }
         if (wp1 >= 0 && key_w <= wp1 && (wp0 - key_w - (KW - 1) < p.window || key_w < p.n_sink)) {  // some row of the wave sees some key
             const char *const Kt = smem + par * TB + 32 * wk * D * 2, *const Vt = smem + (2 + par) * TB + 32 * wk * D * 2;
+            __builtin_amdgcn_s_setprio(0);
             f32x16 acc[KTS];
 #pragma unroll
             for (int kt = 0; kt < KTS; ++kt) acc[kt] = zeros16();
@@ -792,6 +797,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) smha_packed_wide(const P
                 acc[i % KTS] = mfma32<false>(kf[i % PF], qf[i / KTS], acc[i % KTS]);
                 if (i + PF < KTS * NS) kf[i % PF] = k_frag(i + PF);
             }
+            __builtin_amdgcn_s_setprio(2);
             if (!(every && key_w + KW - 1 <= wp0 && (wp1 - key_w < p.window || key_w + KW - 1 < p.n_sink))) {  // not every row sees every key
                 const uint64_t word = pos >= 0 ? low_bits(pos - key_w + 1) & (~low_bits(pos - p.window + 1 - key_w) | low_bits(p.n_sink - key_w)) : 0;
 #pragma unroll
