@@ -9,7 +9,7 @@
 //
 // Packing, per group: x limited to +-65280; m = the largest binary16 <= min x; s = the smallest binary16 with 15 s + m >= max x; c = the number of k in
 // 0 .. 14 with x >= m + (k + 1/2) s (0 where s = 0).  No value is further from x than s / 2 and half its own last place; 15 s + m
-// exceeds max x by less than 15 steps of s, 120 at most, so that every code stands for something finite.
+// exceeds max x by less than 15 of s's last places, 120 at most, so that every code stands for something finite.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -120,15 +120,26 @@ __device__ __forceinline__ uint32_t pack8(u32x4 x, bool there, uint32_t &head) {
     uint32_t sb = __builtin_bit_cast(uint16_t, (_Float16)((hi - m) * (1.f / 15.f)));
     if (fma(15.0, (double)widen16<false>(sb), (double)m) < (double)hi) ++sb;
     const float s = widen16<false>(sb), inv = sb ? __builtin_amdgcn_rcpf(s) : 0.f;
-    // Of the codes the one below or the right one by 32 bits, and then the border above it in 64, where it is exact: equal inputs and ties give
-    // the same code everywhere.  (These are 4 of 25 instructions a value.)
-    const double s64 = s, m64 = sb ? (double)m : (double)__builtin_inff();
+    // The place among the borders: q is off by 15 (2^-24 + 2^-23) + 2^-21 = 3.2e-6 at most (the difference's rounding, the reciprocal's last place, the sum's rounding).  Where a
+    // lane of the wave has a value that is closer to a border than 2^-16, borders are compared in 64 bits, where they are exact, so that equal inputs and ties give the same
+    // code everywhere.  (Always so: 62 us for the call below.)
     uint32_t word = 0;
+    float least = 1.f, most = 0.f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        const float k = truncf(fmaf(f[e] - m, inv, 0.5f - 0x1p-10f));
-        const uint32_t c = (uint32_t)(int)k + (fma((double)(k + 0.5f), s64, m64) <= (double)f[e] ? 1 : 0);
-        word |= c << (4 * (e / 2) + 16 * (e & 1));
+        const float q = fmaf(f[e] - m, inv, 0.5f), past = __builtin_amdgcn_fractf(q);
+        word |= (uint32_t)(int)q << (4 * (e / 2) + 16 * (e & 1));
+        least = fminf(least, past);
+        most = fmaxf(most, past);
+    }
+    if (__builtin_amdgcn_ballot_w64(there && (least < 0x1p-16f || most > 1.f - 0x1p-16f)) != 0) {
+        const double s64 = s, m64 = sb ? (double)m : (double)__builtin_inff();
+        word = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float k = truncf(fmaf(f[e] - m, inv, 0.5f - 0x1p-10f));  // the right code, or the one below it
+            word |= ((uint32_t)(int)k + (fma((double)(k + 0.5f), s64, m64) <= (double)f[e] ? 1 : 0)) << (4 * (e / 2) + 16 * (e & 1));
+        }
     }
     if (bad != 0.f) {
         sb = 0;
@@ -156,8 +167,8 @@ struct PackedRow {
 };
 
 // A quad of lanes takes a group of a new token's key and of its value.  Memory bounds it: 2 d bytes in and R out for each, 2 d more with `values`.  4 x 8 x 8192 x 128
-// with values, of 70 to 100 % of that length: 280 MB, 59 us, 4.7 TB/s as in a large copy (65 with stores of values that stay in the caches; 63 and 66 where a
-// thread takes two and four tokens).
+// with values, of 70 to 100 % of that length: 280 MB, 57 us, 4.9 TB/s (6 us more with stores of values that stay in the caches, 4 and 6 more where a thread takes
+// two and four tokens).
 template <int G, bool BF16>
 __global__ void __launch_bounds__(256) smha_packed_put(const PackParams p) {
     constexpr int ROWS = 64 / G;  // of a workgroup (of three groups one quad has nothing to do)
@@ -526,7 +537,8 @@ template <int D, bool WIDE = false> __device__ __forceinline__ int mixed(int j) 
     else return (j & 3) | ((j & 4) << 1) | ((j & 8) >> 1);
 }
 
-// Four waves take a segment's tiles of 32 keys in turn and join in LDS.  A lane unpacks D / 4 columns of two keys: keys are an operand as they come out; values go
+// Four waves take a segment's tiles of 32 keys in turn and join in LDS, as they read alone: what bounds it is memory (1024 x 32 on 8 x 2048 x 128: 2.7 GB in 480 us, 5.6 TB/s; 2 x 32 on
+// 8 x 65536: 168 MB in 31 us), with vector instructions on more than half of the cycles.  A lane unpacks D / 4 columns of two keys: keys are an operand as they come out; values go
 // through LDS once, for the transposing reads that make them the other product's.  NR tiles of 16 rows share what is unpacked.
 constexpr int packed_workgroups(int D, int NR) { return D == 64 ? (NR == 1 ? 4 : 3) : NR == 1 ? 3 : 2; }  // of a compute unit
 template <int D, int NR, bool BF16>
@@ -713,6 +725,7 @@ __global__ void __launch_bounds__(256, packed_workgroups(D, NR)) smha_packed_par
 // requested a tile before.  KH = 1: a wave takes 32 of 128 rows; KH = 2: a wave takes 32 of 64 rows and one half of the keys, and the halves are joined at the end.  From
 // LDS on it is as in smha_sink_fwd, in binary16 throughout.  Waves with vector work go first, those in the mixed phase (masks, exponentials, second product) before those that
 // unpack, so that the two of a SIMD are in different phases (2 x 1024 tokens x 32 on 8 x 16384 x 128: 552 us without, 512; 4 x 512 x 32 on 8 x 8192 x 64: 242, 211).
+// Bound by issue (82 % of the cycles) and by power (2.0 GHz): 0.9 PFLOP/s.
 template <int D, int KH, bool BF16>
 __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) smha_packed_wide(const PackedParams p) {
     constexpr int NS = D / 16, NDT = D / 32, NL = D / 32, TB = 64 * D * 2, ROWS = 128 / KH, KTS = 2 / KH;  // KTS: halves of a tile that a wave takes

@@ -212,6 +212,57 @@ def test_values_at_borders_are_packed_exactly(dtype):
     assert np.isnan(stands[~finite]).all()
 
 
+def pack_many(x):
+    """[n, 32] float64 -> (s, m, codes), as pack_group, all rows at once (finite ones, within 65280)."""
+    lo, hi = x.min(1), x.max(1)
+    m = lo.astype(np.float16)
+    m = np.where(m > lo, np.nextafter(m, np.float16(-np.inf)), m) + np.float16(0)
+    s = ((hi - m.astype(np.float64)) / 15).astype(np.float16)
+    for _ in range(2):
+        less = np.nextafter(s, np.float16(0))
+        s = np.where((s > 0) & (15 * less.astype(np.float64) + m >= hi), less, s)
+    for _ in range(2):
+        s = np.where(15 * s.astype(np.float64) + m < hi, np.nextafter(s, np.float16(np.inf)), s)
+    codes = np.zeros(x.shape, np.int64)
+    for k in range(15):
+        codes += (x >= (m.astype(np.float64) + (k + 0.5) * s.astype(np.float64))[:, None]) & (s > 0)[:, None]
+    return s, m, codes
+
+
+@pytest.mark.gpu
+@TYPES
+def test_many_groups_are_packed_exactly(dtype):
+    """Groups of all kinds, most of whose waves hold no value near a border, and groups of which every value is near one."""
+    rng = np.random.default_rng(11)
+    n = 1 << 15
+    size = 10.0 ** rng.uniform(-5, 3, (n, 1))
+    x = rng.standard_normal((n, 32)) * size + rng.standard_normal((n, 1)) * size * (rng.random((n, 1)) < 0.5) * 20
+    x[: n // 2, 1:] = np.round(x[: n // 2, 1:] / size[: n // 2] * 8) * size[: n // 2] / 8  # few values to a group
+    x = torch.from_numpy(np.clip(x, -60000, 60000)).float().to(dtype)
+    # values at a border and next to it: base + (k + 1/2) s and its neighbours, of groups that have these s and base
+    s, m, _ = pack_many(x[n // 2:n // 2 + n // 4].double().numpy())
+    k = rng.integers(0, 15, (n // 4, 30)) + 0.5
+    x[n // 2:n // 2 + n // 4, 2:] = torch.from_numpy(m.astype(np.float64)[:, None] + k * s.astype(np.float64)[:, None]).float().to(dtype)
+    s, m, codes = pack_many(x.double().numpy())
+    word = np.zeros((n, 4), np.uint32)
+    for col in range(32):
+        word[:, col // 8] |= codes[:, col].astype(np.uint32) << np.uint32(16 * (col % 2) + 4 * (col % 8 // 2))
+    want = np.concatenate([np.stack([s, m], 1).astype("<f2").view(np.uint8).reshape(n, 4), word.astype("<u4").view(np.uint8).reshape(n, 16)], 1)
+    k4, v4 = smha.packed_cache(1, 1, n, 32)
+    rows = x.reshape(1, 1, n, 32).cuda()
+    smha.packed_write(rows, rows.flip(2), k4, v4, int32([n]))
+    assert np.array_equal(k4[0, 0].cpu().numpy(), want) and np.array_equal(v4[0, 0].cpu().numpy(), want[::-1])
+
+
+def test_the_two_references_of_the_format_agree():
+    rng = np.random.default_rng(3)
+    x = np.round(rng.standard_normal((200, 32)) * 8) / 8 * 10.0 ** rng.integers(-6, 4, (200, 1))
+    s, m, codes = pack_many(x)
+    for i in range(200):
+        a, b, c = pack_group(x[i].tolist())
+        assert (a, b, c) == (s[i], m[i], codes[i].tolist())
+
+
 READS = [
     # B, Hkv, T, Sk, d, lengths, offsets
     (1, 1, 1, 1, 8, [1], None),
