@@ -385,6 +385,9 @@ CASES = [
     (300, 1, 1, 1, 1700, 32, 0, 0, [(1701 * i) // 300 for i in range(300)], "bhsd"),
     (4200, 2, 2, 1, 40, 8, 0, 0, [i % 41 for i in range(4200)], "bhsd"),                           # too many sequences to count
     (3, 16, 1, 100, 1500, 64, 0, 0, [1500, 90, 700], "bhsd"),                                     # 13 tiles of 128 rows, cut
+    (20, 4, 1, 100, 2000, 64, 0, 0, [2000 - 101 * i for i in range(19)] + [30], "bhsd"),           # 4 tiles of rows of 20 sequences, counted in LDS
+    (300, 4, 4, 1, 1700, 8, 0, 0, [1700 if i == 77 else 40 - i % 40 for i in range(300)], "bhsd"), # groups that fill the chip, of which some are cut
+    (1, 32, 2, 1024, 1100, 64, 100, 3, [1100], "bshd"),                                            # one sequence's that do
 ]
 
 
