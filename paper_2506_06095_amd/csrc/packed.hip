@@ -264,6 +264,7 @@ struct PackedParams {
     int row_tiles;  // of a key head's G T rows
     float c;        // scale * log2(e)
     int slots;      // segments wanted; 0: a group is a segment
+    int most_slots; // of calls that have much to do
     int2 *info;     // [groups]: first place, segments.  A place is what a segment of a cut group leaves:
     float *stats;   // [place][2][rows]: reference (log2 units), sum
     float *parts;   // [place][rows][D]
@@ -343,14 +344,17 @@ template <int KT, int ROWS, int TURN> struct PackedCut {
     }
     static __device__ __forceinline__ int parts_of(int n, int most) { return max(1, quotient(n + most - 1, most)); }
     static __device__ __forceinline__ int at_most(int total, int segments) { return max(4, (quotient(total + segments - 1, segments) + TURN - 1) / TURN * TURN); }
-    // `count(most)`: segments then
+    // `count(most)`: segments then.  Where few rows read much (64 tiles a segment then), twice as many: workgroups start while others read (64 x 32 on 8 x 16384 x 128, of 10 to 100 %:
+    // 162 us in segments of 188 tiles, 146 of 94; 256 groups of 10 to 100 % of 256 tiles 46.6 of 51, 48.1 of 26; a little more than there are slots is worst, 103 us for 84).
     template <typename Count> __device__ __forceinline__ void choose(int total, int &most, int &n, Count count) const {
-        for (int wanted = p.slots;;) {
+        const int target = total >= 64 * p.most_slots ? p.most_slots : p.slots;
+        int wanted = target;
+        for (;;) {
             most = at_most(total, wanted);
             n = count(most);
-            if (wanted < p.slots || n <= p.slots) break;
+            if (wanted < target || n <= target) break;
             wanted -= n - quotient(total, most);  // what is over
-            if (2 * wanted <= p.slots) break;
+            if (2 * wanted <= target) break;
         }
     }
     __device__ __forceinline__ void set(PackedSegment &s, const Entry &e, int parts, int rest, int place) const {
@@ -1094,7 +1098,7 @@ extern "C" smha_status_t smha_packed_read(const void *K, const void *V, void *K_
 
 // How a call is taken, and its workspace.
 struct PackedForm {
-    int rows, row_tiles, slots;  // rows of a tile: 16, 32, 64 or 128; slots: 0 where a group is a segment
+    int rows, row_tiles, slots, most_slots;  // rows of a tile: 16, 32, 64 or 128; slots: 0 where a group is a segment
     size_t stats, parts, total;  // after `info`
 };
 static size_t packed_up(size_t n) { return (n + 255) & ~(size_t)255; }
@@ -1112,7 +1116,7 @@ static smha_status_t packed_form(PackedForm &f, int B, int H, int Hkv, int T, in
     f.row_tiles = (rows + f.rows - 1) / f.rows;
     const int64_t groups = (int64_t)B * Hkv * f.row_tiles;
     // (tiles are counted in 32 bits, and a launch has less than 2^32 threads)
-    if (groups * (Sk / KT + 8) > (1 << 30) || groups + 2048 >= 1 << 24) return SMHA_ERR_UNSUPPORTED;
+    if (groups * (Sk / KT + 8) > (1 << 30) || groups + 4096 >= 1 << 24) return SMHA_ERR_UNSUPPORTED;
     const int64_t see = window == 0 || window > Sk ? Sk : window;
     const int64_t tiles = std::min<int64_t>((Sk + KT - 1) / KT, (see + std::min(n_sink, Sk) + T) / KT + 3);
     const int slots = 256 * (wide ? (D == 64 ? 3 : 2) : packed_workgroups(D, f.rows / 16));
@@ -1123,10 +1127,11 @@ static smha_status_t packed_form(PackedForm &f, int B, int H, int Hkv, int T, in
     const bool direct = (int64_t)B * f.row_tiles > kPackedEntries || tiles <= (wide ? 8 : std::min<int64_t>(48, (D == 64 ? 24 : 16) + groups / 8)) ||
                         (int64_t)Hkv * f.row_tiles >= 256;
     f.slots = direct ? 0 : groups < slots ? slots : slots / 2;
+    f.most_slots = !direct && !wide && groups < slots ? 2 * slots : f.slots;
     f.stats = f.parts = f.total = 0;
     if (direct) return SMHA_OK;
     // cut groups are longer than a segment, so that there are fewer of them than slots, and their segments no more than that and one each
-    const int64_t places = std::min(std::min<int64_t>(2 * f.slots, f.slots + groups), groups * ((tiles + 3) / 4));
+    const int64_t places = std::min(std::min<int64_t>(2 * f.most_slots, f.most_slots + groups), groups * ((tiles + 3) / 4));
     f.stats = packed_up(groups * sizeof(int2));
     f.parts = f.stats + packed_up((size_t)places * 2 * f.rows * 4);
     f.total = f.parts + (size_t)places * f.rows * D * 4;
@@ -1142,7 +1147,7 @@ extern "C" smha_status_t smha_packed_workspace(int B, int H, int Hkv, int T, int
 }
 
 template <int D, bool BF16> static hipError_t launch_packed(const PackedParams &pp, const PackedForm &f, hipStream_t stream) {
-    const int groups = pp.B * pp.Hkv * pp.row_tiles, segments = groups + pp.slots;
+    const int groups = pp.B * pp.Hkv * pp.row_tiles, segments = groups + pp.most_slots;
     const dim3 grid(8 * ((segments + 7) / 8));
     auto *const part = f.rows == 16 ? smha_packed_part<D, 1, BF16> : f.rows == 32 ? smha_packed_part<D, 2, BF16> : f.rows == 64 ? smha_packed_wide<D, 2, BF16> : smha_packed_wide<D, 1, BF16>;
     hipLaunchKernelGGL(part, grid, dim3(256), 0, stream, pp);
@@ -1181,6 +1186,7 @@ extern "C" smha_status_t smha_packed_forward(const void *Q, const void *K, const
     pp.n_sink = std::min(n_sink, Sk);
     pp.row_tiles = f.row_tiles;
     pp.slots = f.slots;
+    pp.most_slots = f.most_slots;
     pp.c = (scale > 0.f ? scale : 1.0f / std::sqrt((float)d)) * 1.4426950408889634f;
     char *const ws = (char *)workspace;
     pp.info = (int2 *)ws; pp.stats = (float *)(ws + f.stats); pp.parts = (float *)(ws + f.parts);

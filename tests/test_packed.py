@@ -407,6 +407,24 @@ def test_attention_is_the_formula(case, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("H, T", [(16, 1), (32, 10)])   # 1 and 20 rows on a key head, with more tiles than are cut into the chip's segments once
+def test_long_caches_as_the_16_bit_operator_reads_them(H, T):
+    """Both operators are within the bound above of the formula on the same binary16 values; sum P |V| by the 16-bit operator on |V|, which is half a percent off at most."""
+    B, Hkv, Sk, d = 2, 16, 110000, 128
+    k, v = filled(B, Hkv, Sk, d)
+    lengths = int32([Sk, Sk - 9999])
+    q = queries(B, H, T, d, torch.float16) * 3
+    got = smha.packed_attention(q, k, v, lengths)
+    assert torch.equal(smha.packed_attention(q, k, v, lengths), got)
+    keys, values = smha.packed_read(k, v, lengths)
+    want = smha.cache_attention(q, keys, values, lengths).double()
+    size = smha.cache_attention(q, keys, values.abs(), lengths).double() * 1.005
+    rows = values.abs().double().sum(2).repeat_interleave(H // Hkv, 1)[:, :, None]
+    bound = 2 * ((2.0 ** -11 + F) * size + 2.0 ** -25 * rows + 2.0 ** -11 * (want.abs() * 1.01) + 2.0 ** -25)
+    assert bool(((got.double() - want).abs() <= bound).all())
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("T, Sk", [(2, 600), (2, 6000), (30, 600), (30, 9000), (90, 9000)])   # few rows whole and cut, 120 rows, 360
 def test_what_is_not_seen_may_hold_anything(T, Sk):
     k, v = filled(2, 2, Sk, 128)
