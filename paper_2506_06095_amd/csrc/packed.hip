@@ -322,8 +322,8 @@ __device__ __forceinline__ int lanes_sum(int v) { return __builtin_amdgcn_readla
 
 // The segment of a workgroup.  Every workgroup of the launch computes the same cut: `most` tiles a segment at most, so many that all tiles make `wanted` segments.  A
 // group's last segment is shorter, so that there are more of them then; where that is most of what is over, `most` is raised by it.  (Where groups fill the
-// chip by themselves only those are cut that are longer than twice what a slot has to do.)  Segments of the same key head are Hkv or a multiple of it apart, and with
-// eight such heads, or a multiple, on the same XCD.  Up to 64 entries (row tiles of all sequences) are a lane each, and every wave counts by itself; more are
+// chip by themselves only those are cut that are longer than twice what a slot has to do.)  Where none are cut, row tiles that read the same keys are a multiple of Hkv
+// segments apart, and so, with eight key heads or a multiple, on the same XCD.  Up to 64 entries (row tiles of all sequences) are a lane each, and every wave counts by itself; more are
 // counted by the workgroup, in LDS, where its tiles come later.
 constexpr int kPackedEntries = 4096;
 template <int KT, int ROWS, int TURN> struct PackedCut {
@@ -725,8 +725,8 @@ __global__ void __launch_bounds__(256, packed_workgroups(D, NR)) smha_packed_par
     }
 }
 
-// Many rows on the same keys: four waves share tiles of 64 keys, which all of them unpack into LDS, the next one under this one's first product, from words that were
-// requested a tile before.  KH = 1: a wave takes 32 of 128 rows; KH = 2: a wave takes 32 of 64 rows and one half of the keys, and the halves are joined at the end.  From
+// Many rows on the same keys: four waves share tiles of 64 keys, which all of them unpack into LDS, the next one before they use this one, from words that were
+// requested two tiles before (one before: 538 us for the 522 of the call below on one card).  KH = 1: a wave takes 32 of 128 rows; KH = 2: a wave takes 32 of 64 rows and one half of the keys, and the halves are joined at the end.  From
 // LDS on it is as in smha_sink_fwd, in binary16 throughout.  Waves with vector work go first, those in the mixed phase (masks, exponentials, second product) before those that
 // unpack, so that the two of a SIMD are in different phases (2 x 1024 tokens x 32 on 8 x 16384 x 128: 552 us without, 512; 4 x 512 x 32 on 8 x 8192 x 64: 242, 211).
 // Bound by issue (82 % of the cycles) and by power (2.0 GHz): 0.9 PFLOP/s.
@@ -751,13 +751,14 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) smha_packed_wide(const P
     const int kj = 16 * w + mixed<D, true>(lane & 15);
     struct Raw {
         typename PackedLoad<D>::Raw k, v;
-    } raw;
+    } raw[2];  // of the next two tiles
     auto request = [&](Raw &x, int tile) __attribute__((always_inline)) {
         const int key = keys.key(tile) + kj;
         x.k = loadK(key);
         x.v = loadV(key);
     };
-    if (begin < end) request(raw, begin);
+    if (begin < end) request(raw[0], begin);
+    if (begin + 1 < end) request(raw[1], begin + 1);
 
     const int row0 = s.rows0 + 32 * wr, row = row0 + j, t = quotient(row, p.G), g = row - t * p.G, h = s.hk * p.G + g;
     const int pos = row < rows ? keys.len - p.T + t : -1;  // below 0: no such query
@@ -777,9 +778,9 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) smha_packed_wide(const P
     };
     if (begin < end) {
 #pragma unroll
-        for (int i = 0; i < 2 * NL; ++i) leave(lv, 0, raw, i);
+        for (int i = 0; i < 2 * NL; ++i) leave(lv, 0, raw[0], i);
     }
-    if (begin + 1 < end) request(raw, begin + 1);
+    if (begin + 2 < end) request(raw[0], begin + 2);
 
     const int rd = j * D * 2 + ((hh ^ swz_both<D>(j)) * 16);
     const int tr_row = 4 * hh + ((lane & 15) >> 2);
@@ -789,15 +790,15 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) smha_packed_wide(const P
 #pragma unroll
     for (int dt = 0; dt < NDT; ++dt) o[dt] = zeros16();
     __syncthreads();
-    for (int tile = begin; tile < end; ++tile) {
+    auto step = [&](int tile, Raw &next) __attribute__((always_inline)) {
         const int par = (tile - begin) & 1;
         const int key = keys.key(tile), key_w = key + 32 * wk;
         constexpr int KW = 32 * KTS;
         __builtin_amdgcn_s_setprio(1);
         if (tile + 1 < end) {
 #pragma unroll
-            for (int i = 0; i < 2 * NL; ++i) leave(lv, par ^ 1, raw, i);
-            if (tile + 2 < end) request(raw, tile + 2);
+            for (int i = 0; i < 2 * NL; ++i) leave(lv, par ^ 1, next, i);
+            if (tile + 3 < end) request(next, tile + 3);
         }
         if (wp1 >= 0 && key_w <= wp1 && (wp0 - key_w - (KW - 1) < p.window || key_w < p.n_sink)) {  // some row of the wave sees some key
             const char *const Kt = smem + par * TB + 32 * wk * D * 2, *const Vt = smem + (2 + par) * TB + 32 * wk * D * 2;
@@ -869,6 +870,10 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) smha_packed_wide(const P
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
+    };
+    for (int tile = begin; tile < end; tile += 2) {
+        step(tile, raw[1]);
+        if (tile + 1 < end) step(tile + 1, raw[0]);
     }
     float l = l_run + __shfl_xor(l_run, 32), m = m_run * c;
     if constexpr (KH == 2) {  // the keys' halves join: the second leaves its accumulators where the tiles were
