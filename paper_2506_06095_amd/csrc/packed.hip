@@ -729,7 +729,7 @@ __global__ void __launch_bounds__(256, packed_workgroups(D, NR)) smha_packed_par
 // requested two tiles before (one before: 538 us for the 522 of the call below on one card).  KH = 1: a wave takes 32 of 128 rows; KH = 2: a wave takes 32 of 64 rows and one half of the keys, and the halves are joined at the end.  From
 // LDS on it is as in smha_sink_fwd, in binary16 throughout.  Waves with vector work go first, those in the mixed phase (masks, exponentials, second product) before those that
 // unpack, so that the two of a SIMD are in different phases (2 x 1024 tokens x 32 on 8 x 16384 x 128: 552 us without, 512; 4 x 512 x 32 on 8 x 8192 x 64: 242, 211).
-// Bound by issue (82 % of the cycles) and by power (2.0 GHz): 0.9 PFLOP/s.
+// Bound by issue (82 % of the cycles) and by power (1.95 GHz): 499 to 515 us now, by the card, 0.9 PFLOP/s.
 template <int D, int KH, bool BF16>
 __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) smha_packed_wide(const PackedParams p) {
     constexpr int NS = D / 16, NDT = D / 32, NL = D / 32, TB = 64 * D * 2, ROWS = 128 / KH, KTS = 2 / KH;  // KTS: halves of a tile that a wave takes
