@@ -470,8 +470,8 @@ smha_status_t smha_packed_read(const void *K, const void *V, void *K_out, void *
 /* smha_cache_forward (without a prefix and accounts) on packed rows: attention of the last T tokens of every sequence, whose rows are in the cache, one
  * or a chunk of a prompt.  Q, O: [B][H][T][d] of `dtype`, scale, window and n_sink as there.
  * Products are formed of Q and the rows' values, both as they are (bfloat16 queries as binary16 times a power of two, by which columns below 2^-31 of a query's largest lose
- * digits); sums and exponentials are 32 bits; the probabilities, relative to about the largest, are rounded to binary16 for the product with V, whatever
- * `dtype` is.  The result does not depend on the order in which workgroups run.  Keys before every token's window and past every token's place are never
+ * digits); sums and exponentials are 32 bits; the probabilities are rounded to binary16 for the product with V, whatever `dtype` is: 2^-11 of themselves, and
+ * 2^-32 of the row's largest below 2^-21 of it.  The result does not depend on the order in which workgroups run.  Keys before every token's window and past every token's place are never
  * read into a result; those that some token sees have to stand for something finite (a NaN there may reach other tokens of the sequence).
  * workspace: device, 16-byte aligned, smha_packed_workspace bytes or more (0, and then NULL will do, where there are few keys); the call's
  * alone until it has run. */

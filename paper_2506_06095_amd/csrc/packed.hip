@@ -453,6 +453,18 @@ template <int KT, int ROWS, int TURN> __device__ __forceinline__ PackedSegment p
     return s;
 }
 
+// Probabilities are rounded to binary16 for the second product, whatever the inputs' type, relative to a reference that is about the row's largest score so far.  They are
+// taken 2^7 times as large, as are their sums, so that the joins and the last division know nothing of it: below 2^-14 binary16 has fewer digits and
+// below 2^-25 none, and where one key has nearly all of the weight (the first of a text often has) the others share what is down there.  Only what is
+// below 2^-32 of the largest is lost so.  The reference is raised by a score 2^4 over it, not 2^8 as in the 16-bit operators: 2^11 times 2^4.99 is binary16's end, as far from
+// the largest as there, where scores are so large that 32 bits leave their exponents whole numbers.
+constexpr float kPackedShift = 7.f;
+__device__ __forceinline__ float packed_raised_over(float c) { return fminf(4.0f / c, 3e38f); }
+// The exponent's constant for a running reference (not yet multiplied by c): fmaf(score, c, this).
+__device__ __forceinline__ float packed_from(float reference, float c) { return fmaf(reference == -__builtin_inff() ? 0.f : -reference, c, kPackedShift); }
+// The reference in powers of two, as that constant has it after its rounding.
+__device__ __forceinline__ float packed_reference(float reference, float c) { return reference == -__builtin_inff() ? reference : kPackedShift - packed_from(reference, c); }
+
 // The reference that a row's segment leaves: -inf says that it has no keys.  (A row of NaN has no largest score either, and must not be passed over.)
 __device__ __forceinline__ float reference_left(float m, float l) { return l == l ? m : 0.f; }
 
@@ -591,7 +603,7 @@ __global__ void __launch_bounds__(256, packed_workgroups(D, NR)) smha_packed_par
         // (never 0: -inf times it)
         const uint16_t *const q0 = p.Q + s.b * p.qs.b + s.hk * p.G * p.qs.h;
         c[x] = fmaxf(p.c * load_query<NS, BF16, true>(qf[x], q0 + g * p.qs.h + t * p.qs.s, pos[x] >= 0, q0, p.d, [&](int i) { return D / 4 * u + 8 * i; }), 0x1p-126f);
-        thr[x] = raised_over(c[x]);
+        thr[x] = packed_raised_over(c[x]);
     }
     float m_run[NR], l_run[NR];
     f32x4 o[NR][NC];
@@ -650,11 +662,10 @@ __global__ void __launch_bounds__(256, packed_workgroups(D, NR)) smha_packed_par
 #pragma unroll
                 for (int ct = 0; ct < NC; ++ct) o[x][ct] *= alpha;
             }
-            const float mc = (m_run[x] == NEG_INF ? 0.f : m_run[x]) * c[x];
-            // Probabilities, relative to about the largest, are rounded to binary16 for the second product, whatever the inputs' type.
+            const float from = packed_from(m_run[x], c[x]);
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const float e0 = fast_exp2(fmaf(acc[x][q >> 1][2 * (q & 1)], c[x], -mc)), e1 = fast_exp2(fmaf(acc[x][q >> 1][2 * (q & 1) + 1], c[x], -mc));
+                const float e0 = fast_exp2(fmaf(acc[x][q >> 1][2 * (q & 1)], c[x], from)), e1 = fast_exp2(fmaf(acc[x][q >> 1][2 * (q & 1) + 1], c[x], from));
                 pf[x][q] = pack2<false>(e0, e1);
                 l_run[x] += e0 + e1;
             }
@@ -679,7 +690,7 @@ __global__ void __launch_bounds__(256, packed_workgroups(D, NR)) smha_packed_par
         float l = l_run[x] + __shfl_xor(l_run[x], 16);
         l += __shfl_xor(l, 32);
         if (u == 0) {
-            team[w][0][16 * x + j] = m_run[x] * c[x];
+            team[w][0][16 * x + j] = packed_reference(m_run[x], c[x]);
             team[w][1][16 * x + j] = l;
         }
     }
@@ -767,7 +778,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) smha_packed_wide(const P
     u32x4 qf[NS];
     const uint16_t *const q0 = p.Q + s.b * p.qs.b + s.hk * p.G * p.qs.h;
     const float c = fmaxf(p.c * load_query<NS, BF16, false>(qf, q0 + g * p.qs.h + t * p.qs.s, pos >= 0, q0, p.d, [&](int i) { return 16 * i + 8 * hh; }), 0x1p-126f);
-    const float thr = raised_over(c);
+    const float thr = packed_raised_over(c);
 
     // the i-th of 2 NL chunks of a tile, keys' first
     const int lv = kj * D * 2 + ((NL * (lane >> 4) ^ (swz_both<D>(kj) & ~(NL - 1))) * 16), lx = swz_both<D>(kj) & (NL - 1);
@@ -837,10 +848,10 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) smha_packed_wide(const P
 #pragma unroll
                 for (int dt = 0; dt < NDT; ++dt) o[dt] *= alpha;
             }
-            const float mc = (m_run == NEG_INF ? 0.f : m_run) * c;
+            const float from = packed_from(m_run, c);
             u32x4 pf[2 * KTS];
             auto p_pair = [&](int cu, int q) __attribute__((always_inline)) {
-                const float e0 = fast_exp2(fmaf(acc[cu >> 1][8 * (cu & 1) + 2 * q], c, -mc)), e1 = fast_exp2(fmaf(acc[cu >> 1][8 * (cu & 1) + 2 * q + 1], c, -mc));
+                const float e0 = fast_exp2(fmaf(acc[cu >> 1][8 * (cu & 1) + 2 * q], c, from)), e1 = fast_exp2(fmaf(acc[cu >> 1][8 * (cu & 1) + 2 * q + 1], c, from));
                 pf[cu][q] = pack2<false>(e0, e1);
                 l_run += e0 + e1;
             };
@@ -875,7 +886,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) smha_packed_wide(const P
         step(tile, raw[1]);
         if (tile + 1 < end) step(tile + 1, raw[0]);
     }
-    float l = l_run + __shfl_xor(l_run, 32), m = m_run * c;
+    float l = l_run + __shfl_xor(l_run, 32), m = packed_reference(m_run, c);
     if constexpr (KH == 2) {  // the keys' halves join: the second leaves its accumulators where the tiles were
         f32x4 *const left = reinterpret_cast<f32x4 *>(smem + wr * (32 * D * 4));
         if (wk == 1) {
