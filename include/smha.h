@@ -443,7 +443,9 @@ smha_status_t smha_cache_evict(void *K, void *V, const float *weights, const int
  *   offsets         device, int32 [B]
  * lengths and offsets are read by the kernels: nothing synchronises, and a captured call follows them.  What lies in slots from a length on is never
  * read into a result.
- * Errors: INVALID_ARG (null, sizes, K the same as V where they are written, too small a workspace), SHAPE (H no multiple of Hkv), UNSUPPORTED (d, dtype, alignment,
+ * Two tensors that one call writes have no byte in common (they may lie within one another: keys and values side by side), and nothing that is written is read
+ * by the same call but where that is said.
+ * Errors: INVALID_ARG (null, sizes, written tensors that share memory, or that reach into one another and are laid out differently, too small a workspace), SHAPE (H no multiple of Hkv), UNSUPPORTED (d, dtype, alignment,
  * strides, sizes), HIP.  Enqueue on hip_stream, on the current device. */
 
 /* Bytes of a packed row. */
@@ -453,7 +455,8 @@ smha_status_t smha_packed_row(int d, int *bytes);
  * lengths[b] - 1; other tokens are left out, other slots as they are.
  *   K_new, V_new    device, [B][Hkv][T][d] of `dtype` (F16 or BF16); strides and alignment as in smha_sink_forward
  *   K_values, V_values  device, [B][Hkv][T][d] of `dtype`, packed as tensors are (no strides): what the tokens' rows stand for, rounded once more for BF16, zero where a
- *                   token is left out; both NULL: not wanted.  May be K_new and V_new themselves where these have no strides */
+ *                   token is left out; both NULL: not wanted.  May be K_new and V_new themselves where these are packed; otherwise they reach into
+ *                   none of the others, nor into each other */
 smha_status_t smha_packed_write(const void *K_new, const void *V_new, void *K, void *V, void *K_values, void *V_values,
                                 const int32_t *lengths, const int32_t *offsets, int B, int Hkv, int T, int Sk, int d,
                                 smha_dtype_t dtype, const int64_t kn_strides[3], const int64_t vn_strides[3],

@@ -1037,6 +1037,42 @@ static Strides value_strides(const int64_t *s, int64_t heads, int64_t rows, int 
     return s ? Strides{s[0], s[1], s[2]} : Strides{heads * rows * d, rows * d, d};
 }
 
+// Whether two tensors of B x H x n rows of `row` bytes have bytes in common; each one's rows are `apart`, strides are in bytes.  Exact where they are laid out alike (keys and
+// values side by side, heads of one tensor); where they are not, those that reach into one another are taken to have.
+struct Laid {
+    uintptr_t at;
+    int64_t n[3], step[3], row;  // (no step where there is one)
+    Laid(const void *p, const int64_t *s, int64_t B, int64_t H, int64_t rows, int64_t row_, int64_t size) : at((uintptr_t)p), n{B, H, rows}, row(row_) {
+        const int64_t packed[3] = {H * rows * row, rows * row, row};
+        for (int i = 0; i < 3; ++i) step[i] = n[i] > 1 ? (s ? s[i] * size : packed[i]) : 0;
+    }
+    __int128 end() const {
+        __int128 e = (__int128)at + row;
+        for (int i = 0; i < 3; ++i) e += (__int128)step[i] * (n[i] - 1);
+        return e;
+    }
+    bool alike(const Laid &o) const { return step[0] == o.step[0] && step[1] == o.step[1] && step[2] == o.step[2]; }
+    bool reaches(const Laid &o) const { return (__int128)at < o.end() && (__int128)o.at < end(); }
+    bool meets(const Laid &o) const {
+        if (!reaches(o) || !alike(o)) return reaches(o);
+        int order[3] = {0, 1, 2};
+        std::sort(order, order + 3, [&](int x, int y) { return step[x] > step[y]; });
+        return meets((__int128)at - (__int128)o.at, order, 0);
+    }
+
+  private:
+    // Whether a whole number of every step brings two rows that are `far` apart over one another.  What the closer dimensions span is less than a step, which leaves two numbers.
+    bool meets(__int128 far, const int *order, int i) const {
+        if (i == 3) return far < row && -far < row;
+        const __int128 s = step[order[i]], most = n[order[i]] - 1;
+        if (s == 0) return meets(far, order, i + 1);
+        const __int128 down = far / s - (far % s < 0 ? 1 : 0);
+        for (__int128 times = down; times <= down + 1; ++times)
+            if (times <= most && -times <= most && meets(far - times * s, order, i + 1)) return true;
+        return false;
+    }
+};
+
 // What all entry points refuse.
 static smha_status_t packed_sizes(int B, int Hkv, int T, int Sk, int d) {
     if (B < 1 || Hkv < 1 || T < 1 || Sk < 1) return SMHA_ERR_INVALID_ARG;
@@ -1068,6 +1104,20 @@ extern "C" smha_status_t smha_packed_write(const void *K_new, const void *V_new,
     if (!value_strides_fit(kn_strides, T, d) || !value_strides_fit(vn_strides, T, d) || !packed_strides_fit(k_strides, Sk, d) || !packed_strides_fit(v_strides, Sk, d))
         return SMHA_ERR_UNSUPPORTED;
     if (!apart(k_strides, B, Hkv, Sk, packed_row_bytes(d)) || !apart(v_strides, B, Hkv, Sk, packed_row_bytes(d))) return SMHA_ERR_UNSUPPORTED;
+    // What is written twice, or read by one lane and written by another, would be as the order of workgroups has it.
+    const Laid caches[2] = {{K, k_strides, B, Hkv, Sk, packed_row_bytes(d), 1}, {V, v_strides, B, Hkv, Sk, packed_row_bytes(d), 1}};
+    if (caches[0].meets(caches[1])) return SMHA_ERR_INVALID_ARG;
+    if (K_values) {
+        const Laid values[2] = {{K_values, nullptr, B, Hkv, T, 2 * d, 2}, {V_values, nullptr, B, Hkv, T, 2 * d, 2}};
+        const Laid tokens[2] = {{K_new, kn_strides, B, Hkv, T, 2 * d, 2}, {V_new, vn_strides, B, Hkv, T, 2 * d, 2}};
+        if (values[0].reaches(values[1])) return SMHA_ERR_INVALID_ARG;
+        for (const Laid &to : values) {
+            for (const Laid &cache : caches)
+                if (to.reaches(cache)) return SMHA_ERR_INVALID_ARG;
+            for (const Laid &from : tokens)  // (a lane has read both of its tokens' columns when it writes theirs)
+                if (to.reaches(from) && !(to.at == from.at && to.alike(from))) return SMHA_ERR_INVALID_ARG;
+        }
+    }
     PackParams pp{};
     pp.x[0] = (const uint16_t *)K_new; pp.x[1] = (const uint16_t *)V_new;
     pp.cache[0] = (uint8_t *)K; pp.cache[1] = (uint8_t *)V;
@@ -1099,6 +1149,7 @@ extern "C" smha_status_t smha_packed_read(const void *K, const void *V, void *K_
     if (!packed_strides_fit(k_strides, Sk, d) || !packed_strides_fit(v_strides, Sk, d) || !value_strides_fit(ko_strides, T, d, size) || !value_strides_fit(vo_strides, T, d, size))
         return SMHA_ERR_UNSUPPORTED;
     if (!apart(ko_strides, B, Hkv, T, d) || !apart(vo_strides, B, Hkv, T, d)) return SMHA_ERR_UNSUPPORTED;
+    if (Laid(K_out, ko_strides, B, Hkv, T, (int64_t)d * size, size).meets(Laid(V_out, vo_strides, B, Hkv, T, (int64_t)d * size, size))) return SMHA_ERR_INVALID_ARG;
     UnpackParams up{};
     up.cache[0] = (const uint8_t *)K; up.cache[1] = (const uint8_t *)V;
     up.out[0] = K_out; up.out[1] = V_out;

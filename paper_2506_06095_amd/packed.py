@@ -59,7 +59,7 @@ def packed_write(k_new, v_new, k, v, lengths, *, offsets=None, values: bool = Fa
 
     lengths: int32 [B] on the GPU, keys of every sequence, the new tokens' included.  Token t of sequence b goes to slot lengths[b] - T + t, or to
     offsets[b] + t (int32 [B] on the GPU: prompts that are padded behind have offsets of 0); where that is not in 0 .. lengths[b] - 1 the
-    token is left out.  values: return (keys, values) like k_new and v_new as the cache stands for them from now on (tokens that are left out: zeros), for attention of
+    token is left out.  k and v may lie side by side in one tensor, but share no memory.  values: return (keys, values) like k_new and v_new as the cache stands for them from now on (tokens that are left out: zeros), for attention of
     the prompt itself on what later tokens will see; otherwise None.  Values beyond +-65280 are packed as +-65280, 32 columns among which there
     is a NaN as NaN.  No gradients."""
     if stream is None:  # the native way, for every call that it takes (csrc/torch_binding.cpp)
@@ -97,7 +97,7 @@ def packed_write(k_new, v_new, k, v, lengths, *, offsets=None, values: bool = Fa
 def packed_read(k, v, lengths, *, offsets=None, tokens=None, dtype=torch.float16, out=None, stream=None):
     """What `tokens` slots of every sequence (default: all) from slot offsets[b] (default: 0) on stand for: (keys, values), each [B,Hkv,tokens,d] of
     `dtype`, float16, float32 (the same values) or bfloat16 (rounded to it); zeros where a slot is not in 0 .. lengths[b] - 1.  k, v, lengths, offsets as in packed_write.
-    out: the two tensors to write to, by default new ones."""
+    out: the two tensors to write to, which share no memory, by default new ones."""
     if out is None and stream is None:
         global _read
         if _read is None:

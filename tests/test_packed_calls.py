@@ -1,0 +1,129 @@
+"""Calls on a cache held in 4 bits that are easy to get wrong around the kernels: tensors that share memory, sizes that are refused."""
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import paper_2506_06095_amd as smha  # noqa: E402
+
+# What the C ABI says, on the CPU: status 1 invalid, 5 a HIP error (a call that was not refused and found no GPU).
+
+BASE = 1 << 20
+no_gpu = pytest.mark.skipif(torch.cuda.is_available(), reason="the addresses are not real")
+
+
+def abi():
+    import ctypes as C
+    from paper_2506_06095_amd.binding import _load
+    return C, _load()
+
+
+def strides(C, s):
+    return (C.c_int64 * 3)(*s) if s else None
+
+
+def written(n, steps, row):
+    """The first bytes of the rows of [n] with strides of `steps` bytes."""
+    return {(b * steps[0] + h * steps[1] + t * steps[2] + i) for b in range(n[0]) for h in range(n[1]) for t in range(n[2]) for i in range(row)}
+
+
+# 2 x 3 heads of 5 rows: strides in rows, of the keys and of the values (None: alike), and the distances in rows at which they are looked at
+LAYOUTS = [
+    ((15, 5, 1), None),      # packed
+    ((30, 5, 1), None),      # room for other heads between sequences
+    ((60, 20, 1), None),
+    ((30, 10, 2), None),     # rows in turn
+    ((30, 1, 6), None),      # tokens before heads, keys and values side by side
+    ((5, 20, 1), None),      # heads outermost
+    ((1, 2, 7), None),
+    ((17, 5, 1), None),
+    ((15, 5, 1), (30, 10, 2)),
+    ((30, 10, 2), (30, 1, 6)),
+]
+
+
+@no_gpu
+@pytest.mark.parametrize("call", ["write", "read"])
+@pytest.mark.parametrize("layout", LAYOUTS, ids=str)
+def test_two_tensors_that_are_written_must_not_share_memory(layout, call):
+    """Against the rows' bytes, one by one, where both have the same strides; where they do not, calls whose tensors reach into one another are refused. Those that lie
+    apart as a whole are taken, however they are laid out."""
+    C, lib = abi()
+    n, d = (2, 3, 5), 64
+    row = 40 if call == "write" else 128  # bytes
+    ks, vs = layout[0], layout[1] or layout[0]
+    ksb, vsb = ([s * row for s in x] for x in (ks, vs))
+    reach = [sum(s * (m - 1) for s, m in zip(x, n)) + row for x in (ksb, vsb)]
+    keys, seen = written(n, ksb, row), set()
+    for at in [r * row for r in range(-70, 71)] + ([4, -4, row // 2, -row // 2 - 4, reach[0] - 4, reach[0], -reach[1], 4 - reach[1]] if call == "write" else [16, -16, reach[0]]):
+        if at == 0:
+            continue
+        values = {at + x for x in written(n, vsb, row)}
+        shared = bool(keys & values) if layout[1] is None else at < reach[0] and -at < reach[1]
+        k, v = C.c_void_p(BASE), C.c_void_p(BASE + at)
+        if call == "write":
+            got = lib.smha_packed_write(C.c_void_p(1 << 24), C.c_void_p(1 << 25), k, v, None, None, C.c_void_p(4096), None, *n[:2], 1, n[2], d, 0, None, None, strides(C, ksb), strides(C, vsb), None)
+        else:
+            got = lib.smha_packed_read(C.c_void_p(1 << 24), C.c_void_p(1 << 25), k, v, C.c_void_p(4096), None, *n, 9, d, 0, None, None, strides(C, [s // 2 for s in ksb]),
+                                       strides(C, [s // 2 for s in vsb]), None)
+        assert got == (1 if shared else 5), (at, got)
+        seen.add(shared)
+    assert seen == {True, False}
+
+
+@no_gpu
+def test_strides_of_one_row_do_not_matter():
+    """Dimensions of one: whatever their strides are, packed tensors beside one another are taken."""
+    C, lib = abi()
+    for ks, vs in ((None, (7 * 4, 40, 40)), ((4, 4, 40), None), ((0, 0, 40), (400, 8, 400))):
+        for at, want in ((40, 5), (-40, 5), (36, 1), (-36, 1)):
+            got = lib.smha_packed_write(C.c_void_p(1 << 24), C.c_void_p(1 << 25), C.c_void_p(BASE), C.c_void_p(BASE + at), None, None, C.c_void_p(4096), None, 1, 1, 1, 1, 64, 0, None, None,
+                                        strides(C, ks), strides(C, vs), None)
+            assert got == want, (ks, vs, at)
+
+
+@no_gpu
+def test_values_go_to_memory_of_their_own():
+    """K_values and V_values: not over one another, the cache, or new tokens, but for those that are read in the same places."""
+    C, lib = abi()
+    B, Hkv, T, Sk, d = 2, 3, 4, 9, 64
+    size, cache = B * Hkv * T * d * 2, B * Hkv * Sk * 40
+    at = {"kn": 1 << 20, "vn": 2 << 20, "k": 3 << 20, "v": 4 << 20, "kv": 5 << 20, "vv": 6 << 20}
+
+    def write(kns=None, vns=None, **places):
+        p = {n: C.c_void_p(x) for n, x in {**at, **places}.items()}
+        return lib.smha_packed_write(p["kn"], p["vn"], p["k"], p["v"], p["kv"], p["vv"], C.c_void_p(4096), None, B, Hkv, T, Sk, d, 0, strides(C, kns), strides(C, vns), None, None, None)
+
+    packed = (Hkv * T * d, T * d, d)
+    assert write() == 5
+    assert write(kv=at["kn"], vv=at["vn"]) == 5 and write(kns=packed, vns=packed, kv=at["kn"], vv=at["vn"]) == 5
+    assert write(kv=at["vn"], vv=at["kn"]) == 5                       # (every lane has read both by then)
+    assert write(kns=(T * Hkv * d, d, Hkv * d), kv=at["kn"]) == 1     # read in another order
+    assert write(kns=(0, 0, 0 + d), kv=at["kn"]) == 1
+    for name in ("kv", "vv"):
+        assert write(**{name: at["kv" if name == "vv" else "vv"]}) == 1
+        for other, bytes_ in (("kv" if name == "vv" else "vv", size), ("kn", size), ("vn", size), ("k", cache), ("v", cache)):
+            for far in (16, bytes_ - 16, -16, 16 - size):
+                assert write(**{name: at[other] + far}) == 1, (name, other, far)
+            for far in ((bytes_ + 15) // 16 * 16, -size):
+                assert write(**{name: at[other] + far}) == 5, (name, other, far)
+
+
+@pytest.mark.gpu
+def test_caches_in_one_tensor_and_over_one_another():
+    both = torch.zeros(2, 40, 6, 80, dtype=torch.uint8, device="cuda")
+    kn, vn = (torch.randn(2, 2, 3, 128, device="cuda").half() for _ in range(2))
+    n = torch.tensor([40, 20], dtype=torch.int32, device="cuda")
+    k, v = (both[:, :, i:i + 2].transpose(1, 2) for i in (0, 3))
+    smha.packed_write(kn, vn, k, v, n)
+    apart = smha.packed_cache(2, 2, 40, 128)
+    smha.packed_write(kn, vn, *apart, n)
+    assert torch.equal(k, apart[0]) and torch.equal(v, apart[1])
+    before = both.clone()
+    for v in (both[:, :, 1:3].transpose(1, 2), both[:, :, :2].transpose(1, 2)):
+        for stream in (None, torch.cuda.current_stream()):
+            with pytest.raises(smha.SmhaError):
+                smha.packed_write(kn, vn, k, v, n, stream=stream)
+    out = torch.empty(2, 3, 40, 128, dtype=torch.float16, device="cuda")
+    with pytest.raises(smha.SmhaError):
+        smha.packed_read(*apart, n, out=(out[:, :2], out[:, 1:]))
+    assert torch.equal(both, before)
