@@ -446,7 +446,11 @@ smha_status_t smha_cache_evict(void *K, void *V, const float *weights, const int
  * Two tensors that one call writes have no byte in common (they may lie within one another: keys and values side by side), and nothing that is written is read
  * by the same call but where that is said.
  * Errors: INVALID_ARG (null, sizes, written tensors that share memory, or that reach into one another and are laid out differently, too small a workspace), SHAPE (H no multiple of Hkv), UNSUPPORTED (d, dtype, alignment,
- * strides, sizes), HIP.  Enqueue on hip_stream, on the current device. */
+ * strides, sizes), HIP.  Enqueue on hip_stream, on the current device.
+ * Sizes that are taken: T and Sk below 2^27, B Hkv up to 2^24, B Hkv T up to SMHA_PACKED_MOST_ROWS, heads of new tokens' and outputs' rows, 64 rows more included, below 2 GiB;
+ * in attention also B H and B H T up to 2^24, and, r being H / Hkv T rows in tiles of n = 16 (r up to 16), 32 (up to 32), 64 (up to 64) or 128, B Hkv ceil(r / n) + 4096
+ * below 2^24 and B Hkv ceil(r / n) (Sk / k + 8) up to 2^30, where k is 32 for n up to 32 and 64 beyond. */
+#define SMHA_PACKED_MOST_ROWS (1 << 27)
 
 /* Bytes of a packed row. */
 smha_status_t smha_packed_row(int d, int *bytes);

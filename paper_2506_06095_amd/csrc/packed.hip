@@ -1078,7 +1078,7 @@ static smha_status_t packed_sizes(int B, int Hkv, int T, int Sk, int d) {
     if (B < 1 || Hkv < 1 || T < 1 || Sk < 1) return SMHA_ERR_INVALID_ARG;
     if (d < 8 || d > 128 || d % 8 || T >= kRowsEnd || Sk >= kRowsEnd) return SMHA_ERR_UNSUPPORTED;
     // (rows are counted in 32 bits, and a launch has less than 2^32 threads)
-    if ((int64_t)B * Hkv > (1 << 24) || (int64_t)B * Hkv * T > (1 << 27)) return SMHA_ERR_UNSUPPORTED;
+    if ((int64_t)B * Hkv > (1 << 24) || (int64_t)B * Hkv * T > SMHA_PACKED_MOST_ROWS) return SMHA_ERR_UNSUPPORTED;
     return SMHA_OK;
 }
 

@@ -456,6 +456,12 @@ bool steps_over_rows(const at::Tensor &t) {
     return true;
 }
 
+// Whether [B][Hkv][T][d] of `size` bytes is of a size that the entry points take: what they would refuse is not allocated first.
+bool outputs_fit(const at::Tensor &cache, int64_t T, int64_t d, int64_t size) {
+    const __int128 heads = (__int128)cache.size(0) * cache.size(1);
+    return heads * T <= SMHA_PACKED_MOST_ROWS && (T + 64) * d * size < (int64_t)1 << 31;
+}
+
 PyObject *pair_of(at::Tensor &&a, at::Tensor &&b) {
     PyObject *out = PyTuple_New(2);
     if (!out) return nullptr;
@@ -483,6 +489,7 @@ PyObject *packed_write(PyObject *, PyObject *const *args, Py_ssize_t n) {
     const at::AutoGradMode off(false);
     at::Tensor keys, values;
     if (args[6] == Py_True) {
+        if (!outputs_fit(k, kn.size(2), d, 2)) Py_RETURN_NONE;
         keys = packed_like(kn);
         values = packed_like(vn);
     }
@@ -512,7 +519,7 @@ PyObject *packed_read(PyObject *, PyObject *const *args, Py_ssize_t n) {
     int tokens = (int)k.size(2);
     if (args[4] != Py_None && !int_from(args[4], tokens)) Py_RETURN_NONE;
     const Strides3 ks(k), vs(v);
-    if (!ks.ok || !vs.ok) Py_RETURN_NONE;
+    if (!ks.ok || !vs.ok || !outputs_fit(k, tokens, d, at::elementSize(out_type))) Py_RETURN_NONE;
     const c10::DeviceGuard guard(k.device());
     const at::AutoGradMode off(false);
     const int64_t shape[4] = {k.size(0), k.size(1), tokens, d};

@@ -43,6 +43,15 @@ def _check_rows_apart(*tensors):
             raise ValueError("what is written must not overlap")
 
 
+_MOST_ROWS, _UNSUPPORTED = 1 << 27, 2  # SMHA_PACKED_MOST_ROWS, SMHA_ERR_UNSUPPORTED
+
+
+def _check_outputs_fit(where, B, Hkv, T, d, dtype):
+    """What the entry points would refuse for its size is not allocated first."""
+    if B * Hkv * T > _MOST_ROWS or (T + 64) * d * dtype.itemsize >= 1 << 31:
+        raise SmhaError(_UNSUPPORTED, where)
+
+
 def packed_cache(B: int, Hkv: int, Sk: int, d: int, *, device=None):
     """An empty cache for packed_write: two uint8 tensors [B,Hkv,Sk,smha_packed_row(d)] of zeros on the GPU (`device`: the current one).  (Any such
     tensors will do, whose rows are contiguous and whose strides are multiples of 4.)"""
@@ -84,6 +93,8 @@ def packed_write(k_new, v_new, k, v, lengths, *, offsets=None, values: bool = Fa
         raise ValueError("lengths must be given")
     n, at = _check_per_sequence(lengths, "lengths", k), _check_per_sequence(offsets, "offsets", k)
     (B, Hkv, T, _), Sk = k_new.shape, k.shape[2]
+    if values:
+        _check_outputs_fit("smha_packed_write", B, Hkv, T, d, k_new.dtype)
     with _on_device(k), _allocating_on(stream, not values):
         out = tuple(torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (k_new, v_new)) if values else None
         st = _load().smha_packed_write(k_new.data_ptr(), v_new.data_ptr(), k.data_ptr(), v.data_ptr(), *((t.data_ptr() for t in out) if values else (None, None)), n, at, B, Hkv,
@@ -120,6 +131,8 @@ def packed_read(k, v, lengths, *, offsets=None, tokens=None, dtype=torch.float16
             raise ValueError("out must be two [B,Hkv,tokens,d] tensors of dtype on the same GPU")
         _check_no_gradients("packed_read", *out)
         _check_rows_apart(*out)
+    if out is None:
+        _check_outputs_fit("smha_packed_read", B, Hkv, T, d, dtype)
     with _on_device(k), _allocating_on(stream, out is not None):
         if out is None:
             out = tuple(torch.empty(B, Hkv, T, d, dtype=dtype, device=k.device) for _ in range(2))
@@ -174,12 +187,13 @@ def packed_attention(q, k, v, lengths, *, window: int = 0, n_sink: int = 0, out=
     if out is not None and (out.shape != q.shape or out.dtype != q.dtype or out.device != q.device):
         raise ValueError("out must be like q")
     with _on_device(q), _allocating_on(stream, workspace is not None and out is not None):
-        if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        need = smha_packed_workspace(B, H, Hkv, T, Sk, d, window, n_sink)  # (sizes that are not taken end here)
         if workspace is None:
-            workspace = torch.empty(smha_packed_workspace(B, H, Hkv, T, Sk, d, window, n_sink), dtype=torch.uint8, device=q.device)
+            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
         else:
             _check_workspace(workspace, q)
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
         st = _load().smha_packed_forward(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), n, B, H, Hkv, T, Sk, d, _CODES[q.dtype],
                                          *(_strides(t) for t in (q, k, v, out)), window, n_sink, float(scale), workspace.data_ptr(), workspace.numel(),
                                          _handle(stream, q.device))

@@ -127,3 +127,51 @@ def test_caches_in_one_tensor_and_over_one_another():
     with pytest.raises(smha.SmhaError):
         smha.packed_read(*apart, n, out=(out[:, :2], out[:, 1:]))
     assert torch.equal(both, before)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("way", ["native", "python"])
+def test_sizes_are_refused_before_anything_is_allocated(way):
+    """(Outputs of such calls would be gigabytes.)"""
+    k, v = smha.packed_cache(2, 2, 40, 128)
+    n = torch.tensor([40, 20], dtype=torch.int32, device="cuda")
+    stream = torch.cuda.current_stream() if way == "python" else None
+    torch.cuda.reset_peak_memory_stats()
+    before = torch.cuda.memory_allocated()
+
+    def refused(call):
+        with pytest.raises(smha.SmhaError) as e:
+            call()
+        assert e.value.status == 2 and torch.cuda.max_memory_allocated() - before < 1 << 20
+
+    # more than 2^27 rows, of heads below 2 GiB; heads of 2 GiB; more rows than there are
+    kc, vc = (t[:1, :1].expand(32, 2, 40, 80) for t in (k, v))
+    many = n[:1].repeat(32)
+    refused(lambda: smha.packed_read(kc, vc, many, tokens=(1 << 21) + 1, stream=stream))
+    refused(lambda: smha.packed_read(k, v, n, tokens=1 << 23, stream=stream))
+    refused(lambda: smha.packed_read(k, v, n, tokens=1 << 22, dtype=torch.float32, stream=stream))
+    for tokens in (1 << 27, (1 << 31) - 1):
+        refused(lambda: smha.packed_read(k[:1], v[:1], n[:1], tokens=tokens, stream=stream))
+    wide = torch.zeros(1, 1, 1, 128, dtype=torch.float16, device="cuda")
+    new = wide.expand(2, 2, 1 << 23, 128)  # (a stride of 0 between tokens is refused too)
+    refused(lambda: smha.packed_write(new, new, k, v, n, values=True, stream=stream))
+    q = wide.expand(2, 4, 1 << 22, 128)
+    refused(lambda: smha.packed_attention(q, k, v, n, stream=stream))
+
+
+@pytest.mark.gpu
+def test_the_largest_read_that_is_taken():
+    """2^27 rows in all, of which few are there; the same by both ways."""
+    k, v = smha.packed_cache(1, 1, 40, 8)
+    kn = torch.randn(1, 1, 40, 8, device="cuda").half()
+    n = torch.tensor([40], dtype=torch.int32, device="cuda")
+    want = smha.packed_write(kn, kn * 2, k, v, n, values=True)
+    kc, vc = (t.expand(8, 1, 40, 8) for t in (k, v))
+    many = n.repeat(8)
+    for stream in (None, torch.cuda.current_stream()):
+        got = smha.packed_read(kc, vc, many, tokens=1 << 24, stream=stream)
+        for g, w in zip(got, want):
+            assert g.shape == (8, 1, 1 << 24, 8) and all(torch.equal(g[b, :, :40], w[0]) for b in range(8)) and not bool(g[:, :, 40:].any())
+        del got
+    with pytest.raises(smha.SmhaError):
+        smha.packed_read(kc, vc, many, tokens=(1 << 24) + 1)
