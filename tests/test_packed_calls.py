@@ -1,4 +1,4 @@
-"""Calls on a cache held in 4 bits that are easy to get wrong around the kernels: tensors that share memory, sizes that are refused."""
+"""Calls on a cache held in 4 bits that are easy to get wrong around the kernels: tensors that share memory, sizes that are refused, tensors of other kinds, threads."""
 import pytest
 
 torch = pytest.importorskip("torch")
@@ -175,3 +175,77 @@ def test_the_largest_read_that_is_taken():
         del got
     with pytest.raises(smha.SmhaError):
         smha.packed_read(kc, vc, many, tokens=(1 << 24) + 1)
+
+
+def inputs():
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    B, H, Hkv, T, Sk, d = 2, 8, 2, 3, 3000, 128
+    kn, vn = (torch.randn(B, Hkv, Sk, d, generator=gen, device="cuda").half() for _ in range(2))
+    q = torch.randn(B, H, T, d, generator=gen, device="cuda").half()
+    n = torch.tensor([Sk, Sk - 100], dtype=torch.int32, device="cuda")
+    k, v = smha.packed_cache(B, Hkv, Sk, d)
+    smha.packed_write(kn, vn, k, v, n)
+    return q, kn, vn, k, v, n
+
+
+@pytest.mark.gpu
+def test_tensors_of_other_kinds_and_modes():
+    """Subclasses and calls under a mode, which the native way leaves to the other: the same results."""
+    q, kn, vn, k, v, n = inputs()
+    want = smha.packed_attention(q, k, v, n), *smha.packed_read(k, v, n), *smha.packed_write(kn, vn, k, v, n, values=True), k.clone(), v.clone()
+
+    class Sub(torch.Tensor):
+        pass
+
+    class Mode(torch.utils._python_dispatch.TorchDispatchMode):
+        def __torch_dispatch__(self, func, types, args=(), kwargs=None):
+            return func(*args, **(kwargs or {}))
+
+    def passes(*tensors):
+        q, kn, vn, k, v, n = tensors
+        return smha.packed_attention(q, k, v, n), *smha.packed_read(k, v, n), *smha.packed_write(kn, vn, k, v, n, values=True), k, v
+
+    def same(got):
+        assert len(got) == len(want) and all(torch.equal(a.as_subclass(torch.Tensor), b) for a, b in zip(got, want))
+
+    same(passes(*(t.as_subclass(Sub) for t in (q, kn, vn, k, v, n))))
+    k.zero_()
+    v.zero_()
+    smha.packed_write(kn, vn, k, v, n)
+    with Mode():
+        same(passes(q, kn, vn, k, v, n))
+    with torch.inference_mode():
+        same(passes(q, kn, vn, k, v, n))
+    with pytest.raises(ValueError):
+        smha.packed_attention(torch.nn.Parameter(q), k, v, n)
+    with torch.no_grad():
+        assert torch.equal(smha.packed_attention(torch.nn.Parameter(q), k, v, n), want[0])
+    with pytest.raises(RuntimeError):
+        torch.vmap(lambda t: smha.packed_attention(t, k, v, n))(q[None])
+
+
+@pytest.mark.gpu
+def test_threads_with_streams_of_their_own():
+    import threading
+    q, kn, vn, k, v, n = inputs()
+    want = smha.packed_attention(q, k, v, n)
+    got, failed = [None] * 4, []
+    torch.cuda.synchronize()
+
+    def work(i):
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                mine = smha.packed_cache(2, 2, 3000, 128)
+                for _ in range(20):
+                    smha.packed_write(kn, vn, *mine, n)
+                    got[i] = smha.packed_attention(q, *mine, n)
+                torch.cuda.current_stream().synchronize()
+        except Exception as e:  # noqa: BLE001
+            failed.append(e)
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not failed and all(torch.equal(g, want) for g in got)

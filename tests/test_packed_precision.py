@@ -86,3 +86,25 @@ def test_scores_that_32_bits_hold_in_whole_steps(T, Sk, size, dtype):
     low, high = (t.repeat_interleave(H // Hkv, 1)[:, :, None] for t in (top.amin(2), top.amax(2)))
     slack = (2.0 ** -11 + torch.finfo(dtype).eps / 2 + F) * torch.maximum(low.abs(), high.abs())
     assert bool(((out >= low - slack) & (out <= high + slack)).all())
+
+
+@pytest.mark.gpu
+@TYPES
+@pytest.mark.parametrize("B, H, Hkv, T, Sk, d, window, n_sink, lengths", [
+    (2, 4, 2, 1, 700, 96, 0, 0, [700, 33]),
+    (1, 8, 1, 3, 5000, 96, 1000, 5, [4999]),
+    (2, 6, 2, 20, 900, 96, 0, 0, [900, 450]),
+    (1, 8, 2, 50, 800, 96, 300, 40, [800]),
+    (2, 4, 2, 1, 700, 88, 0, 0, [700, 1]),
+    (1, 4, 1, 40, 500, 112, 0, 0, [499]),
+    (1, 4, 2, 9, 500, 48, 100, 0, [500]),
+    (1, 4, 1, 40, 500, 24, 0, 0, [500]),
+    (1, 3, 1, 2, 500, 120, 0, 0, [499]),
+], ids=str)
+def test_heads_of_other_widths(B, H, Hkv, T, Sk, d, window, n_sink, lengths, dtype):
+    """(The bound of test_packed.py, which is the wider one.)"""
+    from test_packed import filled, queries, reference
+    k, v = filled(B, Hkv, Sk, d)
+    q = queries(B, H, T, d, dtype)
+    want, bound = reference(q, k, v, lengths, window, n_sink)
+    check(smha.packed_attention(q, k, v, int32(lengths), window=window, n_sink=n_sink), want, bound)
