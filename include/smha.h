@@ -434,7 +434,7 @@ smha_status_t smha_cache_evict(void *K, void *V, const float *weights, const int
  * 128 columns: 5 bits a value.)
  * How rows are packed: values beyond +-65280, infinities among them, are taken as +-65280; m is the largest binary16 that is not above the group's
  * least value (-0 counts as 0), s the smallest with which 15 s + m is not below its largest; c is the number of k in 0 .. 14 for which the value is at
- * least m + (k + 1/2) s, and 0 where s is 0.  All of it exactly, so that equal inputs give equal bytes.  A value is packed within s / 2 and half a last place
+ * least m + (k + 1/2) s, and 0 where s is 0 (15 s + m is finite then: every code of such a group stands for something finite).  All of it exactly, so that equal inputs give equal bytes.  A value is packed within s / 2 and half a last place
  * of binary16.  A group that holds a NaN stands for NaN throughout.
  *
  *   K, V            device, [B][Hkv][Sk][row] bytes: packed rows; *_strides in bytes, {batch, head, key} (NULL = packed), multiples of 4, no row
@@ -479,7 +479,8 @@ smha_status_t smha_packed_read(const void *K, const void *V, void *K_out, void *
  * Products are formed of Q and the rows' values, both as they are (bfloat16 queries as binary16 times a power of two, by which columns below 2^-31 of a query's largest lose
  * digits); sums and exponentials are 32 bits; the probabilities are rounded to binary16 for the product with V, whatever `dtype` is: 2^-11 of themselves, and
  * 2^-32 of the row's largest below 2^-21 of it.  The result does not depend on the order in which workgroups run.  Keys before every token's window and past every token's place are never
- * read into a result; those that some token sees have to stand for something finite (a NaN there may reach other tokens of the sequence).
+ * read into a result; those that some token sees have to stand for something finite with every code, as rows that smha_packed_write packed from finite values do (a NaN there may reach
+ * other tokens of the sequence).
  * workspace: device, 16-byte aligned, smha_packed_workspace bytes or more (0, and then NULL will do, where there are few keys); the call's
  * alone until it has run. */
 smha_status_t smha_packed_workspace(int B, int H, int Hkv, int T, int Sk, int d, int window, int n_sink, size_t *need);

@@ -166,9 +166,9 @@ struct PackedRow {
     }
 };
 
-// A quad of lanes takes a group of a new token's key and of its value.  Memory bounds it: 2 d bytes in and R out for each, 2 d more with `values`.  4 x 8 x 8192 x 128
-// with values, of 70 to 100 % of that length: 280 MB, 57 us, 4.9 TB/s (6 us more with stores of values that stay in the caches, 4 and 6 more where a thread takes
-// two and four tokens).
+// A quad of lanes takes a group of a new token's key and of its value: 2 d bytes in and R out for each, 2 d more with `values`.  Issue of vector instructions (94 % of the
+// cycles) and memory bound it, one as nearly as the other: 4 x 8 x 8192 x 128 with values, of 70 to 100 % of that length: 280 MB, 58.4 us, 4.8 TB/s, which is a copy's rate
+// (6 us more with stores of values that stay in the caches, 4 and 6 more where a thread takes two and four tokens).
 template <int G, bool BF16>
 __global__ void __launch_bounds__(256) smha_packed_put(const PackParams p) {
     constexpr int ROWS = 64 / G;  // of a workgroup (of three groups one quad has nothing to do)
@@ -210,9 +210,9 @@ struct UnpackParams {
     int B, Hkv, T, Sk, d;
 };
 
-// A lane takes 8 columns of a slot's key and of its value.  Memory bounds it: R bytes in and d values out for each.  4 x 8 x 16384 x 128 of 70 to 100 % of that
-// length to bfloat16: 352 MB, 49 us (of which the cache's 84 MB stay in the last level from call to call; 70 with stores that do, 51 and 50 where a thread
-// takes two and four slots).
+// A lane takes 8 columns of a slot's key and of its value: R bytes in and d values out for each.  Issue of vector instructions (82 % of the cycles) and memory bound it: 4 x 8 x
+// 16384 x 128 of 70 to 100 % of that length to bfloat16: 352 MB, 51 us a pass (of which the cache's 84 MB stay in the last level from call to call; 20 more with stores that
+// do, 1 or 2 where a thread takes two and four slots).  To float32 608 MB, 218 us: its two stores of a lane lie 32 bytes apart between lanes, each half of what it touches.
 template <int OUT>
 __global__ void __launch_bounds__(256) smha_packed_get(const UnpackParams p) {
     const int chunks = p.d >> 3, G = (p.d + 31) >> 5, at_once = quotient(256, chunks), first = quotient(threadIdx.x, chunks), chunk = (int)threadIdx.x - first * chunks;
@@ -249,10 +249,10 @@ __global__ void __launch_bounds__(256) smha_packed_get(const UnpackParams p) {
 // ---------------------------------------------------------------------------------------
 // Attention
 // ---------------------------------------------------------------------------------------
-// The rows that read the same keys, T tokens times G = H / Hkv heads, token by token, are taken 16, 32 or 128 at a time; such a tile of rows and
+// The rows that read the same keys, T tokens times G = H / Hkv heads, token by token, are taken 16, 32, 64 or 128 at a time; such a tile of rows and
 // the tiles of keys that it sees are a group.  Memory bounds calls of few rows: a key's 10 d / 8 bytes meet 4 d G T operations.  There
-// every compute unit has to read, whatever the lengths are, so the key tiles of all groups are counted on the device and cut into as many segments, of
-// about the same length, as workgroups fit the chip; segments of one group are joined by a second kernel, in a fixed order.
+// every compute unit has to read, whatever the lengths are, so the key tiles of all groups are counted on the device and cut into segments of about the same length, as many as
+// workgroups fit the chip (twice as many where few rows read much, half where groups fill the chip by themselves); segments of one group are joined by a second kernel, in a fixed order.
 struct PackedParams {
     const uint16_t *Q;
     const uint8_t *K, *V;
@@ -553,8 +553,8 @@ template <int D, bool WIDE = false> __device__ __forceinline__ int mixed(int j) 
     else return (j & 3) | ((j & 4) << 1) | ((j & 8) >> 1);
 }
 
-// Four waves take a segment's tiles of 32 keys in turn and join in LDS, as they read alone: what bounds it is memory (1024 x 32 on 8 x 2048 x 128: 2.7 GB in 480 us, 5.6 TB/s; 2 x 32 on
-// 8 x 65536: 168 MB in 31 us), with vector instructions on more than half of the cycles.  A lane unpacks D / 4 columns of two keys: keys are an operand as they come out; values go
+// Four waves take a segment's tiles of 32 keys in turn and join in LDS, as they read alone: what bounds it is memory (1024 x 32 on 8 x 2048 x 128: 2.7 GB in 513 us, 5.2 TB/s; 2 x 32 on
+// 8 x 65536: 168 MB in 32 us), with vector instructions on more than half of the cycles.  A lane unpacks D / 4 columns of two keys: keys are an operand as they come out; values go
 // through LDS once, for the transposing reads that make them the other product's.  NR tiles of 16 rows share what is unpacked.
 constexpr int packed_workgroups(int D, int NR) { return D == 64 ? (NR == 1 ? 4 : 3) : NR == 1 ? 3 : 2; }  // of a compute unit
 template <int D, int NR, bool BF16>
@@ -637,7 +637,7 @@ __global__ void __launch_bounds__(256, packed_workgroups(D, NR)) smha_packed_par
             for (int i = 0; i < NS; ++i)
                 *reinterpret_cast<u32x4 *>(smem + (16 * a + vj) * D * 2 + (((D / 32 * u + i) ^ swz_values<D>(vj)) * 16)) = unpack8(v_raw[a].code[i], v_raw[a].head);
         if (tile + 4 < end) request_v(tile + 4);
-        __builtin_amdgcn_s_setprio(1);  // (as in smha_packed_wide; 64 x 32 on 8 x 4096 x 128, 5 tokens: 97 us without, 89)
+        __builtin_amdgcn_s_setprio(1);  // (as in smha_packed_wide; 64 x 32 on 8 x 4096 x 128, 5 tokens: 82 us without, 81; of 10 to 100 % of that length 72, 70.5)
         u32x4 pf[NR];
 #pragma unroll
         for (int x = 0; x < NR; ++x) {
@@ -739,8 +739,8 @@ __global__ void __launch_bounds__(256, packed_workgroups(D, NR)) smha_packed_par
 // Many rows on the same keys: four waves share tiles of 64 keys, which all of them unpack into LDS, the next one before they use this one, from words that were
 // requested two tiles before (one before: 538 us for the 522 of the call below on one card).  KH = 1: a wave takes 32 of 128 rows; KH = 2: a wave takes 32 of 64 rows and one half of the keys, and the halves are joined at the end.  From
 // LDS on it is as in smha_sink_fwd, in binary16 throughout.  Waves with vector work go first, those in the mixed phase (masks, exponentials, second product) before those that
-// unpack, so that the two of a SIMD are in different phases (2 x 1024 tokens x 32 on 8 x 16384 x 128: 552 us without, 512; 4 x 512 x 32 on 8 x 8192 x 64: 242, 211).
-// Bound by issue (82 % of the cycles) and by power (1.95 GHz): 499 to 515 us now, by the card, 0.9 PFLOP/s.
+// unpack, so that the two of a SIMD are in different phases (2 x 1024 tokens x 32 on 8 x 16384 x 128: 579 us without, 537, of 70 to 100 % of that length 541, 507; 4 x 512 x 32 on 8 x 8192 x 64: 234, 205).
+// Bound by issue (81 % of the cycles) and by power (1.95 GHz): the second of these calls 505 to 520 us, by the card, 0.9 PFLOP/s.
 template <int D, int KH, bool BF16>
 __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) smha_packed_wide(const PackedParams p) {
     constexpr int NS = D / 16, NDT = D / 32, NL = D / 32, TB = 64 * D * 2, ROWS = 128 / KH, KTS = 2 / KH;  // KTS: halves of a tile that a wave takes
@@ -1188,9 +1188,11 @@ static smha_status_t packed_form(PackedForm &f, int B, int H, int Hkv, int T, in
     const int64_t tiles = std::min<int64_t>((Sk + KT - 1) / KT, (see + std::min(n_sink, Sk) + T) / KT + 3);
     const int slots = 256 * (wide ? (D == 64 ? 3 : 2) : packed_workgroups(D, f.rows / 16));
     // Groups are taken whole, in one launch, where they have few tiles: cutting costs a second launch and the search for a segment, and shares out what one workgroup
-    // would read alone (us, whole and cut: 64 groups x 128 of 512 keys 8.5 and 9.6, of 1024 12.8 and 11.4; 256 groups of 1024 14.0 and 17.8); where one sequence's fill the chip,
-    // so that lengths hardly matter (2 x 1024 tokens x 32 on 8 x 16384 x 128 545 and 564; 4 x 512 x 32 on 8 x 8192, of 10 to 100 % of that, 237 and 248, but a long sequence among
-    // short ones would be read by half the chip); and where there are too many to count.  (512 x 32 on 8 x 2048 x 128, of 10 to 100 %: 154 and 167.)
+    // would read alone (us, whole and cut: 64 groups x 128 of 512 keys 9.3 and 9.8, of 1024 13.8 and 11.4; 256 groups of 1024 14.6 and 18.3); where there are too many to count;
+    // and where one sequence has 256 or more, a workgroup for every compute unit, so that lengths hardly matter (2 x 1024 tokens x 32 on 8 x 16384 x 128 548 and 555, x 64 339
+    // and 387; 1 x 2048 536 and 544, 331 and 377).  With fewer of them a long sequence among short ones would be read by part of the chip (2 x 512 x 32 on 8 x 8192 x 64, of 10
+    // to 100 % of that: 100 and 63; 4 x 512 105 and 97, of full length 172 and 207; 512 x 1 x 32 on 8 x 2048 x 128, of 10 to 100 %, 156 and 168).  The bound does not see that
+    // one sequence of 256 groups leaves half of the slots empty at 128 columns and two thirds at 64: 1 x 1024 tokens x 32 on 8 x 16384 x 128 takes 388 us, 294 if it were cut, x 64 280 and 177.
     const bool direct = (int64_t)B * f.row_tiles > kPackedEntries || tiles <= (wide ? 8 : std::min<int64_t>(48, (D == 64 ? 24 : 16) + groups / 8)) ||
                         (int64_t)Hkv * f.row_tiles >= 256;
     f.slots = direct ? 0 : groups < slots ? slots : slots / 2;

@@ -159,7 +159,7 @@ def packed_attention(q, k, v, lengths, *, window: int = 0, n_sink: int = 0, out=
     q [B,H,T,d], float16 or bfloat16 (whatever the type was that the cache was packed from); k, v uint8 [B,Hkv,Sk,row] as in packed_write, H a multiple
     of Hkv; T from one token to a chunk of a prompt.  lengths, window, n_sink, scale, out, workspace (of smha_packed_workspace bytes) as in cache_attention: token t of sequence b
     stands at slot lengths[b] - T + t and sees the keys up to itself, the last `window` of them (0: all) and the first `n_sink`.  No gradients.  Keys that a token of
-    the sequence sees have to stand for something finite (others, and free slots, may hold anything)."""
+    the sequence sees have to stand for something finite, as what packed_write packed of finite values does (others, and free slots, may hold anything)."""
     if out is None and workspace is None and stream is None:
         global _attention
         if _attention is None:
